@@ -206,7 +206,7 @@ def _draw_cache(case, g, h, room, most):
         x *= torch.exp(0.3 * _normal(g, at))[..., None]
         if case["cache"] == "e4m3":
             amax = x.abs().amax(-1).clamp_min(2.0 ** -60)
-            c[n] = (x * (448.0 / amax)[..., None]).to(torch.float8_e4m3fn)
+            c[n] = (x * (torch.full_like(amax, 448.0) / amax)[..., None]).to(torch.float8_e4m3fn)
             c[n + "_scale"] = amax / 448.0
         else:
             c[n] = x.to(DTYPES[case["cache"]])
@@ -404,7 +404,8 @@ def _plain_append(s):
         scale = None
         if case["cache"] == "e4m3":
             amax = x.abs().amax(-1).clamp_min(2.0 ** -60)
-            scale, x = amax / 448.0, x * (448.0 / amax)[..., None]
+            # (a scalar over a tensor would be a reciprocal and a product)
+            scale, x = amax / 448.0, x * (torch.full_like(amax, 448.0) / amax)[..., None]
         if case["page"]:
             P = case["page"]
             at = (c["table"][b, t // P].to(torch.int64), slice(None), t % P)
