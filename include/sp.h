@@ -64,6 +64,9 @@ typedef enum sp_status {
 } sp_status;
 
 enum { SP_F32 = 0, SP_BF16 = 1 };              /* element types                  */
+enum { SP_E4M3 = 2 };                          /* 8-bit elements of an sp_token_cache
+                                                  (4 exponent, 3 mantissa bits), with
+                                                  a float scale per (token, kv head) */
 enum { SP_POOL_MEAN = 0, SP_POOL_LAST = 1 };   /* which outputs the head reads   */
 enum { SP_KV_CONTIGUOUS = 0, SP_KV_PAGED = 1 };/* cache addressing               */
 
@@ -72,8 +75,9 @@ enum {
     SP_DEV_BAD_SEQ_ID = 1,    /* a sequence id was outside [0, n_seqs)               */
     SP_DEV_BAD_LENGTH = 2,    /* a cached length was < 0 or > max_seq_len            */
     SP_DEV_BAD_PAGE = 4,      /* a page-table entry was outside [0, n_pages)         */
-    SP_DEV_TIMEOUT = 8        /* a tensor-core kernel gave up waiting on a copy or an
+    SP_DEV_TIMEOUT = 8,       /* a tensor-core kernel gave up waiting on a copy or an
                                  MMA (its outputs are invalid; the context is intact) */
+    SP_DEV_BAD_ROW = 16       /* a row, token or node count outside its buffer        */
 };
 
 /* Shapes of the frozen layer and of the probe (Sec. 3.1, 3.2). */
@@ -445,6 +449,163 @@ SP_API sp_status sp_debug_gemm_plan(int M, int N, int K, int n_sm, int lo, int s
 SP_API sp_status sp_project(sp_stream stream, int M, int N, int K, const float *d_x,
                             const void *d_w, float *d_y, int path, void *d_workspace,
                             size_t workspace_bytes);
+
+/* ------------------------------------------------------------------------- */
+/* A token cache that is written: rotary positions, appending, reading back,   */
+/* and the attention of a drafted tree over it.  These calls surround the       */
+/* classify path: they produce the draft head's cache that it reads (Sec. 3.3)  */
+/* and verify the tokens drafted with it.  They need no handle; like the calls  */
+/* above they are asynchronous on their stream and allocate nothing.            */
+/* ------------------------------------------------------------------------- */
+
+/* Rotary positions.  Pair i of a head's first rot_dim dims turns by
+ * p * f_i at position p and is scaled by `amplitude`; the other dims pass
+ * unchanged.  f_i is held as a 64-bit fraction of a turn, so p * f_i mod 1 is
+ * exact in wrapping 64-bit integers at any int32 position (negative ones too). */
+typedef struct sp_rotary {
+    int head_dim;        /* dh, 1..1024                                               */
+    int rot_dim;         /* rotated dims, even, 2..head_dim                           */
+    int interleaved;     /* 0: pair i = dims (i, i + rot_dim/2); 1: (2i, 2i + 1)      */
+    float amplitude;     /* factor on the rotated dims (1 = a rotation)               */
+    const uint64_t *d_turns; /* DEVICE [rot_dim/2]: f_i * 2^64 turns (sp_rotary_plan) */
+} sp_rotary;
+
+/* How the frequencies theta^(-2i/rot_dim) are stretched for contexts `factor`
+ * times the trained length: */
+enum {
+    SP_ROPE_PLAIN = 0,   /* not at all                                                */
+    SP_ROPE_LINEAR = 1,  /* all divided by factor (positions interpolated)            */
+    SP_ROPE_BASE = 2,    /* theta * factor^(rot_dim / (rot_dim - 2)): the fastest pair
+                            keeps its frequency, the slowest is divided by factor     */
+    SP_ROPE_TURNS = 3,   /* pairs that turn at least `many` times over trained_len
+                            keep their frequency, those below `few` turns are divided
+                            by factor, linear in the turns between                    */
+    SP_ROPE_DIMS = 4     /* the same ends, linear in the pair index between (rounded
+                            outwards); the amplitude is 1 + 0.1 ln(factor)            */
+};
+
+/* Fill h_turns [rot_dim/2] (HOST; the caller copies it to the device) and
+ * *amplitude for an sp_rotary.  theta > 1, factor >= 1; trained_len > 0 and
+ * 0 < few < many for the last two kinds (ignored otherwise); SP_ROPE_BASE needs
+ * rot_dim >= 4.  Host only. */
+SP_API sp_status sp_rotary_plan(int kind, int rot_dim, double theta, double factor, double trained_len,
+                                double few, double many, uint64_t *h_turns, float *amplitude);
+
+/* Rotate n_heads heads of n_tokens tokens at d_positions [n_tokens] (int32):
+ *   y_u = a (x_u cos - x_v sin),  y_v = a (x_v cos + x_u sin)   backward = 0
+ * or the adjoint map of gradients, x_u' = a (y_u' cos + y_v' sin),
+ * x_v' = a (y_v' cos - y_u' sin), for backward = 1 (the inverse when a = 1).
+ * Head h of token t starts at element t * token_stride + h * head_stride of x
+ * and of y (dtype SP_F32 or SP_BF16, one type for both; the dims of a head are
+ * contiguous); angles and products are fp32, rounded once.  y may be x with the
+ * same strides, else they must not overlap.  Any alignment of the elements'
+ * own works; 16-byte aligned bases, strides of whole 16 bytes and rotated parts
+ * of whole 16-byte vectors are fast.  n_tokens = 0 is a no-op. */
+SP_API sp_status sp_rotate(sp_stream stream, const sp_rotary *rot, int n_tokens, const int *d_positions,
+                           int backward, int dtype, int n_heads, const void *d_x, long long x_token_stride,
+                           long long x_head_stride, void *d_y, long long y_token_stride,
+                           long long y_head_stride);
+
+/* A cache as these calls see it: the addressing of sp_kv_cache (the same layouts,
+ * so a SP_F32 or SP_BF16 cache is the one sp_classify reads) plus its element
+ * type.  The pools are written by sp_cache_append, which is why `kv` must then
+ * point to memory the caller may write.
+ * SP_E4M3: an element is its 8-bit code times the scale of its (token, kv head);
+ * the scales are float, SP_KV_PAGED: k_scale / v_scale point to
+ * [n_pages][Hkv][page_size] (16-byte aligned), SP_KV_CONTIGUOUS: to DEVICE arrays
+ * of n_seqs device pointers to [L_s][Hkv].  NULL for the other types. */
+typedef struct sp_token_cache {
+    sp_kv_cache kv;
+    int dtype;           /* SP_F32, SP_BF16 or SP_E4M3                                */
+    int n_kv_heads;      /* Hkv                                                       */
+    int head_dim;        /* dh: 32, 64 or 128                                         */
+    int max_seq_len;     /* most tokens of a sequence: a longer one is reported
+                            (SP_DEV_BAD_LENGTH), a token is never written past it     */
+    void *k_scale, *v_scale;
+} sp_token_cache;
+
+/* Where the rows of each sequence sit in a caller's row buffers (keys and values
+ * [n_rows][Hkv][dh] each). */
+typedef struct sp_token_rows {
+    const int *d_row0;   /* DEVICE [batch]: first row of a sequence; NULL: b * max_rows */
+    const int *d_count;  /* DEVICE [batch]: its rows, 0..max_rows; NULL: max_rows       */
+    const int *d_take;   /* DEVICE [batch][max_rows]: the j-th token's row, relative to
+                            the first one (e.g. the accepted path of a tree); NULL: j   */
+    int max_rows;        /* >= 1                                                        */
+    int n_rows;          /* rows of the buffers                                         */
+    long long k_stride;  /* elements from a row to the next; 0 = Hkv * dh               */
+    long long v_stride;
+} sp_token_rows;
+
+/* Append tokens to sequences of a cache: token j (j < count) of batch entry b
+ * goes to position seq_lens[id] + j.  The lengths are read, not advanced: the
+ * caller adds the counts.
+ *   rot        NULL: the keys arrive rotated; else they are rotated at their
+ *              positions on the way (rot->head_dim must be the cache's)
+ *   d_k, d_v   rows in `dtype` (SP_F32 or SP_BF16)
+ *   d_status   optional device int (OR-ed SP_DEV_* bits)
+ * SP_E4M3: scale = max(amax, 2^-60) / 448 over the finite elements of a (token,
+ * kv head), code = the nearest 8-bit value of x * (448 / max(amax, 2^-60)), ties to
+ * even; a non-finite element becomes NaN.  Other types are rounded to nearest.
+ * A sequence may appear once in a batch.  A token without a page, past
+ * max_seq_len or whose row lies outside the buffers is skipped and reported. */
+SP_API sp_status sp_cache_append(sp_stream stream, const sp_token_cache *cache, const sp_rotary *rot,
+                                 int batch, const int *d_seq_ids, const int *d_seq_lens,
+                                 const sp_token_rows *rows, int dtype, const void *d_k, const void *d_v,
+                                 int *d_status);
+
+/* The other way: row j (j < count) of batch entry b becomes the cached token
+ * d_first[b] + (take ? take[b][j] : j) (d_first NULL = 0), zeros past the
+ * sequence's end, in `dtype`; rows from count on are left alone. */
+SP_API sp_status sp_cache_read(sp_stream stream, const sp_token_cache *cache, int batch, const int *d_seq_ids,
+                               const int *d_seq_lens, const int *d_first, const sp_token_rows *rows, int dtype,
+                               void *d_k, void *d_v, int *d_status);
+
+/* Masks and depths of a tree given by its parents (HOST, host only): h_parent[i]
+ * is an earlier node or -1 (hangs on the sequence's last token); bit j of
+ * h_mask[i] is set for j = i and every node above i; h_depth[i] (may be NULL) is
+ * its distance from the sequence's last token minus 1, so that node i sits at
+ * position L_b + h_depth[i].  1 <= n_nodes <= 64. */
+SP_API sp_status sp_tree_masks(int n_nodes, const int *h_parent, uint64_t *h_mask, int *h_depth);
+
+typedef struct sp_tree_dims {
+    int n_q_heads;       /* Hq, a multiple of the cache's Hkv                         */
+    int n_nodes;         /* most nodes of a tree N, 1..64                             */
+    int dtype;           /* of q, k_new, v_new and out.  SP_F32: the arithmetic is fp32
+                            throughout (CUDA cores).  SP_BF16: bf16 or 8-bit products
+                            with fp32 sums on the tensor cores (caches of head_dim 128
+                            in SP_BF16 or SP_E4M3, batch <= 2048), else as SP_F32      */
+    int path;            /* 0 = automatic, 1 = CUDA cores, 2 = tensor cores
+                            (SP_ERR_UNSUPPORTED where they do not apply)              */
+    int shared_mask;     /* 1: d_mask is [N], one tree for the batch; 0: [batch][N]   */
+    float scale;         /* factor on the scores; 0 = 1 / sqrt(dh)                    */
+    long long q_stride;  /* elements from a node's row to the next, multiples of 16    */
+    long long k_stride;  /* bytes; 0 = dense (Hq * dh, Hkv * dh).  Node i of batch     */
+    long long v_stride;  /* entry b is row b * N + i                                  */
+} sp_tree_dims;
+
+/* Bytes of device scratch sp_attend_tree needs (256-byte aligned start); 0 for
+ * invalid dims. */
+SP_API size_t sp_attend_tree_workspace_bytes(const sp_tree_dims *dims, const sp_token_cache *cache, int batch);
+
+/* Attention of a tree of drafted tokens per sequence over [cache ; tree]
+ * (Eq. 1-3 with the causal part replaced by the tree): node i of batch entry b
+ * sees the cached tokens 0..L_b-1 and the nodes j with bit j of its mask set.
+ *   d_mask     uint64 device (see shared_mask); NULL: a chain (0..i)
+ *   d_n_nodes  [batch] int32 device: nodes of each tree, 0..N; NULL: N
+ *   d_q        [batch * N][Hq][dh], rotated; d_k_new, d_v_new [batch * N][Hkv][dh]
+ *   d_out      [batch * N][Hq][dh]: zeros for a node that sees nothing and for the
+ *              nodes from n_nodes on (whose rows are never read)
+ * The keys and values of nodes a node does not see, and what a cache page holds
+ * past its sequence's end, have no influence, NaN and infinities included.  The
+ * cache is only read.  With n_nodes = 1 this is the attention of a decoding step.
+ * SP_E4M3 caches on tensor cores: the codes enter the score product as they are
+ * (queries split exactly into two 8-bit parts) and the value product as 16-bit
+ * floats with probabilities of 11 bits. */
+SP_API sp_status sp_attend_tree(sp_stream stream, const sp_tree_dims *dims, const sp_token_cache *cache, int batch,
+                                const int *d_seq_ids, const int *d_seq_lens, const uint64_t *d_mask,
+                                const int *d_n_nodes, const void *d_q, const void *d_k_new, const void *d_v_new,
+                                void *d_out, void *d_workspace, size_t workspace_bytes, int *d_status);
 
 #ifdef __cplusplus
 }

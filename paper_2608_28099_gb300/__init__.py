@@ -15,10 +15,11 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "_build", "libsp.so")
 
 SP_OK, SP_ERR_INVALID_ARG, SP_ERR_UNSUPPORTED, SP_ERR_CUDA, SP_ERR_OOM, SP_ERR_DEVICE_STATUS = range(6)
-SP_F32, SP_BF16 = 0, 1
+SP_F32, SP_BF16, SP_E4M3 = 0, 1, 2
 SP_POOL_MEAN, SP_POOL_LAST = 0, 1
 SP_KV_CONTIGUOUS, SP_KV_PAGED = 0, 1
-SP_DEV_BAD_SEQ_ID, SP_DEV_BAD_LENGTH, SP_DEV_BAD_PAGE, SP_DEV_TIMEOUT = 1, 2, 4, 8
+SP_DEV_BAD_SEQ_ID, SP_DEV_BAD_LENGTH, SP_DEV_BAD_PAGE, SP_DEV_TIMEOUT, SP_DEV_BAD_ROW = 1, 2, 4, 8, 16
+SP_ROPE_PLAIN, SP_ROPE_LINEAR, SP_ROPE_BASE, SP_ROPE_TURNS, SP_ROPE_DIMS = range(5)
 SP_OPT_SPLIT_TOKENS, SP_OPT_GEMM_PATH, SP_OPT_ATTN_PATH, SP_OPT_PROFILE = 1, 2, 3, 4
 SP_OPT_RECURSIVE = 5
 SP_OPT_ATTN_SEG_COST = 6
@@ -34,7 +35,9 @@ EXPORTED = ["sp_create", "sp_destroy", "sp_classify", "sp_classify_host", "sp_ch
             "sp_last_error", "sp_set_option", "sp_last_launch_count", "sp_attend_workspace_bytes",
             "sp_attend", "sp_stage_times", "sp_project_workspace_bytes", "sp_project",
             "sp_attend_static", "sp_classify_hidden", "sp_classify_hidden_host",
-            "sp_debug_gathered_pages", "sp_debug_gemm_plan"]
+            "sp_debug_gathered_pages", "sp_debug_gemm_plan", "sp_rotary_plan", "sp_rotate",
+            "sp_cache_append", "sp_cache_read", "sp_tree_masks", "sp_attend_tree_workspace_bytes",
+            "sp_attend_tree"]
 
 
 class sp_config(C.Structure):
@@ -68,6 +71,29 @@ class sp_attn_dims(C.Structure):
     _fields_ = [("n_q_heads", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int),
                 ("k_rows", C.c_int), ("kv_dtype", C.c_int), ("max_seq_len", C.c_int),
                 ("split_tokens", C.c_int), ("path", C.c_int)]
+
+
+class sp_rotary(C.Structure):
+    _fields_ = [("head_dim", C.c_int), ("rot_dim", C.c_int), ("interleaved", C.c_int),
+                ("amplitude", C.c_float), ("d_turns", C.c_void_p)]
+
+
+class sp_token_cache(C.Structure):
+    _fields_ = [("kv", sp_kv_cache), ("dtype", C.c_int), ("n_kv_heads", C.c_int),
+                ("head_dim", C.c_int), ("max_seq_len", C.c_int), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p)]
+
+
+class sp_token_rows(C.Structure):
+    _fields_ = [("d_row0", C.c_void_p), ("d_count", C.c_void_p), ("d_take", C.c_void_p),
+                ("max_rows", C.c_int), ("n_rows", C.c_int), ("k_stride", C.c_longlong),
+                ("v_stride", C.c_longlong)]
+
+
+class sp_tree_dims(C.Structure):
+    _fields_ = [("n_q_heads", C.c_int), ("n_nodes", C.c_int), ("dtype", C.c_int),
+                ("path", C.c_int), ("shared_mask", C.c_int), ("scale", C.c_float),
+                ("q_stride", C.c_longlong), ("k_stride", C.c_longlong), ("v_stride", C.c_longlong)]
 
 
 class SpError(RuntimeError):
@@ -112,11 +138,24 @@ def load_library(path: str | None = None):
                                      C.POINTER(sp_kv_cache), vp, vp, vp, vp, i, vp, vp]
     lib.sp_attend.argtypes = [vp, C.POINTER(sp_attn_dims), i, vp, vp, C.POINTER(sp_kv_cache), vp,
                               vp, vp, vp, i, vp, C.c_size_t, vp, vp]
+    d, ll = C.c_double, C.c_longlong
+    lib.sp_rotary_plan.argtypes = [i, i, d, d, d, d, d, vp, C.POINTER(C.c_float)]
+    lib.sp_rotate.argtypes = [vp, C.POINTER(sp_rotary), i, vp, i, i, i, vp, ll, ll, vp, ll, ll]
+    lib.sp_cache_append.argtypes = [vp, C.POINTER(sp_token_cache), C.POINTER(sp_rotary), i, vp, vp,
+                                    C.POINTER(sp_token_rows), i, vp, vp, vp]
+    lib.sp_cache_read.argtypes = [vp, C.POINTER(sp_token_cache), i, vp, vp, vp,
+                                  C.POINTER(sp_token_rows), i, vp, vp, vp]
+    lib.sp_tree_masks.argtypes = [i, vp, vp, vp]
+    lib.sp_attend_tree_workspace_bytes.argtypes = [C.POINTER(sp_tree_dims),
+                                                   C.POINTER(sp_token_cache), i]
+    lib.sp_attend_tree_workspace_bytes.restype = C.c_size_t
+    lib.sp_attend_tree.argtypes = [vp, C.POINTER(sp_tree_dims), C.POINTER(sp_token_cache), i, vp, vp,
+                                   vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
     lib.sp_debug_gathered_pages.argtypes = [vp, vp, C.c_size_t]
     lib.sp_debug_gemm_plan.argtypes = [i, i, i, i, i, i, C.c_size_t, C.POINTER(sp_gemm_plan)]
     for name in EXPORTED:
         if name not in ("sp_last_error", "sp_last_launch_count", "sp_attend_workspace_bytes",
-                        "sp_project_workspace_bytes"):
+                        "sp_project_workspace_bytes", "sp_attend_tree_workspace_bytes"):
             getattr(lib, name).restype = C.c_int
     if path is None:
         _lib = lib
@@ -257,6 +296,62 @@ def sp_attend(stream, dims, batch, seq_ids, seq_lens, kv, q, k_new, v_new, out, 
                                     _ptr(seq_lens), C.byref(kv), _ptr(q), _ptr(k_new), _ptr(v_new),
                                     _ptr(out), int(out_dtype), _ptr(workspace),
                                     int(workspace_bytes), _ptr(status), _ptr(gathered_pages)))
+
+
+def sp_rotary_plan(kind, rot_dim, theta=1.0e4, factor=1.0, trained_len=0.0, few=1.0, many=32.0):
+    """(turns, amplitude): the numpy uint64 table [rot_dim / 2] to copy to the device."""
+    import numpy as np
+    turns = np.zeros(max(int(rot_dim) // 2, 1), dtype=np.uint64)
+    amplitude = C.c_float()
+    _check(load_library().sp_rotary_plan(int(kind), int(rot_dim), theta, factor, trained_len, few,
+                                         many, turns.ctypes.data, C.byref(amplitude)))
+    return turns, amplitude.value
+
+
+def sp_rotate(stream, rot: sp_rotary, n_tokens, positions, backward, dtype, n_heads, x,
+              x_token_stride, x_head_stride, y, y_token_stride, y_head_stride):
+    _check(load_library().sp_rotate(_stream(stream), C.byref(rot), int(n_tokens), _ptr(positions),
+                                    int(backward), int(dtype), int(n_heads), _ptr(x),
+                                    x_token_stride, x_head_stride, _ptr(y), y_token_stride,
+                                    y_head_stride))
+
+
+def sp_cache_append(stream, cache: sp_token_cache, rot, batch, seq_ids, seq_lens,
+                    rows: sp_token_rows, dtype, k, v, status=None):
+    """rot: an sp_rotary that turns the keys on the way, or None (already rotated)."""
+    _check(load_library().sp_cache_append(_stream(stream), C.byref(cache),
+                                          None if rot is None else C.byref(rot), int(batch),
+                                          _ptr(seq_ids), _ptr(seq_lens), C.byref(rows), int(dtype),
+                                          _ptr(k), _ptr(v), _ptr(status)))
+
+
+def sp_cache_read(stream, cache: sp_token_cache, batch, seq_ids, seq_lens, first,
+                  rows: sp_token_rows, dtype, k, v, status=None):
+    _check(load_library().sp_cache_read(_stream(stream), C.byref(cache), int(batch), _ptr(seq_ids),
+                                        _ptr(seq_lens), _ptr(first), C.byref(rows), int(dtype),
+                                        _ptr(k), _ptr(v), _ptr(status)))
+
+
+def sp_tree_masks(parents):
+    """(masks, depths) of a tree given by its nodes' parents: numpy uint64 and int32."""
+    import numpy as np
+    parents = np.ascontiguousarray(parents, dtype=np.int32)
+    masks, depths = np.zeros(len(parents), np.uint64), np.zeros(len(parents), np.int32)
+    _check(load_library().sp_tree_masks(len(parents), parents.ctypes.data, masks.ctypes.data,
+                                        depths.ctypes.data))
+    return masks, depths
+
+
+def sp_attend_tree_workspace_bytes(dims: sp_tree_dims, cache: sp_token_cache, batch) -> int:
+    return load_library().sp_attend_tree_workspace_bytes(C.byref(dims), C.byref(cache), int(batch))
+
+
+def sp_attend_tree(stream, dims: sp_tree_dims, cache: sp_token_cache, batch, seq_ids, seq_lens,
+                   mask, n_nodes, q, k_new, v_new, out, workspace, workspace_bytes, status=None):
+    _check(load_library().sp_attend_tree(_stream(stream), C.byref(dims), C.byref(cache), int(batch),
+                                         _ptr(seq_ids), _ptr(seq_lens), _ptr(mask), _ptr(n_nodes),
+                                         _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out),
+                                         _ptr(workspace), int(workspace_bytes), _ptr(status)))
 
 
 # --------------------------------------------------------------------------- #
