@@ -117,6 +117,7 @@ struct TreeArgs {
     int R;                         // G N query rows of a kv head: row rr = node G + head of the group
     int n_rb, rb_rows;             // row blocks of a kv head and the rows of each (the last has fewer)
     int dtype;                     // of q, k_new, v_new, out
+    bool tensor;                   // which kernel
     float scale_log2;              // log2(e) * scale of the scores
     const int *seq_ids, *seq_lens, *n_nodes;
     const uint64_t *mask;          // NULL: a chain
@@ -149,5 +150,11 @@ __device__ __forceinline__ uint64_t tree_mask(const TreeArgs &a, int b, int i, i
 void plan_tree_simt(TreeArgs *a, int n_sm);
 cudaError_t launch_tree_simt(const TreeArgs &a, cudaStream_t st);
 size_t tree_simt_slots(const TreeArgs &a);
+// tcgen05: head_dim 128, bf16 rows, bf16 or 8-bit caches, B <= 2048; two launches.
+// seg_tab: B int2 of scratch.
+bool tree_tc_supported(const TreeArgs &a);
+void plan_tree_tc(TreeArgs *a, int n_sm);
+size_t tree_tc_slots(const TreeArgs &a);
+cudaError_t launch_tree_tc(const TreeArgs &a, int2 *seg_tab, cudaStream_t st);
 
 }  // namespace sp

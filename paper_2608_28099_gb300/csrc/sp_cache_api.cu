@@ -161,16 +161,22 @@ sp_status check_tree(const sp_tree_dims *d, const sp_token_cache *cache, int bat
     if ((a->qs * es | a->ks * es | a->vs * es) & 15)
         return fail(SP_ERR_INVALID_ARG, "q_stride, k_stride and v_stride must be multiples of 16 bytes");
     a->mask_stride = d->shared_mask ? 0 : a->N;
-    if (d->path == 2) return fail(SP_ERR_UNSUPPORTED, "no tensor-core kernel for these types");
-    plan_tree_simt(a, sm_count());
+    a->tensor = d->path != 1 && tree_tc_supported(*a);
+    if (d->path == 2 && !a->tensor)
+        return fail(SP_ERR_UNSUPPORTED, "the tensor-core kernel needs bf16 rows, a bf16 or 8-bit cache of head_dim 128 "
+                                        "and a batch of at most 2048");
+    if (a->tensor) plan_tree_tc(a, sm_count());
+    else plan_tree_simt(a, sm_count());
     return SP_OK;
 }
 
-size_t tree_slots(const TreeArgs &a) { return tree_simt_slots(a); }
-
+// Workspace: partials [slot][row][dh], their (max, sum), then the tensor-core kernel's
+// table of shares.
+size_t tree_rows(const TreeArgs &a) { return (a.tensor ? tree_tc_slots(a) : tree_simt_slots(a)) * a.rb_rows; }
+size_t tree_o_bytes(const TreeArgs &a) { return align256(tree_rows(a) * a.dh * sizeof(float)); }
+size_t tree_ml_bytes(const TreeArgs &a) { return align256(tree_rows(a) * 2 * sizeof(float)); }
 size_t tree_bytes(const TreeArgs &a) {
-    const size_t rows = tree_slots(a) * a.rb_rows;
-    return align256(rows * a.dh * sizeof(float)) + align256(rows * 2 * sizeof(float)) + 256;
+    return tree_o_bytes(a) + tree_ml_bytes(a) + align256((size_t)a.B * sizeof(int2));
 }
 
 }  // namespace
@@ -321,9 +327,11 @@ sp_status sp_attend_tree(sp_stream stream, const sp_tree_dims *dims, const sp_to
     a.v_new = d_v_new;
     a.out = d_out;
     a.part_o = (float *)d_workspace;
-    a.part_ml = (float *)((char *)d_workspace + align256(tree_slots(a) * a.rb_rows * a.dh * sizeof(float)));
+    a.part_ml = (float *)((char *)d_workspace + tree_o_bytes(a));
     a.status = d_status;
-    return launched(launch_tree_simt(a, (cudaStream_t)stream), "sp_attend_tree");
+    int2 *seg_tab = (int2 *)((char *)a.part_ml + tree_ml_bytes(a));
+    return launched(a.tensor ? launch_tree_tc(a, seg_tab, (cudaStream_t)stream) : launch_tree_simt(a, (cudaStream_t)stream),
+                    "sp_attend_tree");
 }
 
 }  // extern "C"

@@ -974,6 +974,19 @@ bool encode_kv_pages_bf16(CUtensorMap *map, const void *pool, long long n_page_h
     return r == CUDA_SUCCESS;
 }
 
+bool encode_rows_u8(CUtensorMap *map, const void *base, long long rows, int box_rows) {
+    PFN_cuTensorMapEncodeTiled_v12000 fn = encode_fn();
+    if (!fn || ((uintptr_t)base & 15) || rows <= 0 || rows > 0x7fffffffLL || box_rows > 256) return false;
+    cuuint64_t dims[2] = {128, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {128};
+    cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
+    cuuint32_t estr[2] = {1, 1};
+    CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS;
+}
+
 bool encode_q_group_f32(CUtensorMap *map, const float *q, int rows, int Hq, int G, int k) {
     // q [rows = B*k][Hq][128] fp32; one box = the G heads of one kv group for
     // the k rows of one sequence: [k][G][128], unswizzled

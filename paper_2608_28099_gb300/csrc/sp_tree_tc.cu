@@ -1,0 +1,1143 @@
+// Attention of a drafted tree over [cache ; tree] (Eq. 1-3, the causal part replaced
+// by the tree's masks) on tcgen05 tensor cores: head_dim 128, bf16 rows, caches of
+// bf16 or of 8-bit codes with a scale per (token, kv head).
+//
+// Work: the cached tokens of every sequence are cut into tiles of 128, a tile for its
+// nodes behind them; the list of all sequences' tiles is cut into shares as in
+// sp_attn_plan.cuh, and CTA (share, kv head, row block) walks its share; a share's piece
+// of one sequence is a segment.  A pair that lies inside one share is finished there,
+// the others leave partials that a second kernel merges in share order.
+//
+// The G N query rows of a kv head are the MMA's M side:
+//   up to 128 rows: one M tile.  With at most 64 (32) rows the tile holds 2 (4) copies
+//     of them, and copy c keeps the weights of its own 64 (32) tokens of each key tile and
+//     zeros elsewhere: the exponentials of few rows spread over all four SM sub-partitions
+//     (a row is otherwise one thread's work), the product costs what it cost, and the
+//     copies are added up once a segment.  Two pipelines take alternate key tiles, each
+//     with its own scores, softmax warpgroup and output accumulator.
+//   up to 256 rows: two M tiles, one a pipeline, both over every key tile.
+//   more: row blocks, as further CTAs.
+// Per key tile and pipeline:
+//   S = Q K^T     128 x 128, Q in shared memory.  bf16: as they are.  8-bit codes enter
+//                 the product as they are (kind::f8f6f4); q is the sum of two 8-bit
+//                 parts, exact to 2^-18 of the row's largest element, and the token's and
+//                 the row's scales multiply the score
+//   softmax       a row a thread, the running max moved only when it grows by 2^8
+//   O += P V      P over the first half of S in TMEM.  bf16, or, for 8-bit caches, 16-bit
+//                 floats against V's codes as 16-bit floats (exact); V's scale joins the
+//                 exponent, w = 2^(x + log2 v_scale - m), so that w <= 2^8 whatever the
+//                 scales, and the row sum takes w / v_scale
+// The nodes' own keys never lose to the cache's format: bf16 nodes are copied, and for an
+// 8-bit cache their keys are two 8-bit parts in the two halves of the tile (S is the sum
+// of its halves), their values 16-bit floats, both exact for bf16 rows.
+// What a row does not see: scores are replaced by -inf (not added to), rows of a tile past
+// the sequence's end are zeros, and a node's non-finite values are taken out of the
+// product and added afterwards to the rows that see the node.
+//
+// Warps 0-7: the two softmax warpgroups; then producers (K and V rings: TMA boxes of
+// whole pages, cp.async elsewhere), two MMA issuers (the first owns TMEM) and, for 8-bit
+// caches, four warps that turn V's codes into 16-bit floats and the scales into the
+// softmax's constants.  Every wait is time-limited (SP_DEV_TIMEOUT).
+#include <cudaTypedefs.h>
+#include <string.h>
+
+#include "sp_attn_plan.cuh"
+#include "sp_cache.cuh"
+#include "sp_gemm.cuh"
+#include "sp_sm100.cuh"
+
+namespace sp {
+
+namespace {
+
+constexpr int TILE = 128;                       // tokens of a key tile
+constexpr int SLOT16 = TILE * DH * 2;           // K or V of a tile in 16 bits, 32 KB
+constexpr int SLOT8 = TILE * DH;                // in 8 bits, 16 KB
+constexpr int SCALES = 2 * TILE * 4;            // k and v scales of a tile, behind its V codes
+constexpr int PARAMS = 3 * TILE * 4;            // (k scale, log2 v scale) pairs, 1 / v scale
+constexpr int Q_TILE = 128 * DH * 2;            // an M tile of queries: bf16, or two 8-bit parts
+constexpr int CONV = 2;                         // converted V slots
+constexpr int MAX_RING = 8;
+constexpr int SMEM_MAX = 227 * 1024;
+constexpr int SOFT = 256;                       // softmax threads
+constexpr int BAR_EPI = 1, BAR_WG = 2;          // (BAR_WG + 1: the second warpgroup's)
+constexpr uint32_t O_COL = 256;                 // TMEM: S0 S1 [0, 256), O0 O1 [256, 512)
+constexpr int kTreeMinTiles = 2;                // fewest tiles a share holds on average
+constexpr int kTreeSegCost = 4;                 // cost of a segment, in tiles
+
+struct Layout {
+    int nk, nv;                                 // ring slots
+    int off_q, off_k, off_v, off_c, off_tab;    // (off_c: converted V, then its parameters)
+    int smem;
+};
+
+struct Bars {
+    uint64_t k_full[MAX_RING], k_empty[MAX_RING], v_full[MAX_RING], v_empty[MAX_RING];
+    uint64_t c_full[CONV], c_empty[CONV];
+    uint64_t s_full[2], p_full[2], pv_done[2], q_full, fin;
+    unsigned long long vbad[MAX_RING][4];       // nodes with non-finite values, by V slot and warp
+    unsigned long long seg_vbad;
+    uint32_t tmem;
+    int abort;
+    int wsum[32];
+};
+constexpr int OFF_ML = 1024;                    // (max, sum) of [pipeline][lane]
+constexpr int OFF_L = OFF_ML + 2 * 128 * 8;      // 1 / sum of [warpgroup][row]
+constexpr int OFF_CUTS = OFF_L + 2 * 128 * 4;
+constexpr int OFF_FRONT = OFF_CUTS + (MAX_GRP + 4) * 4;
+static_assert(sizeof(Bars) <= OFF_ML, "barrier block");
+
+template <bool E4>
+struct Roles {
+    static constexpr int RING_WARPS = E4 ? 1 : 2;                    // producers of a ring
+    static constexpr int RING_THREADS = RING_WARPS * 32;
+    static constexpr int PROD = 8, MMA = PROD + 2 * RING_WARPS, CVT = MMA + 2;
+    static constexpr int WARPS = CVT + (E4 ? 4 : 0);
+    static constexpr int THREADS = WARPS * 32;
+};
+
+// D[tmem] (+)= A[smem] * B[smem]^T on 8-bit elements (32 of K), issued by one thread.
+__device__ __forceinline__ void mma_e4m3(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc));
+}
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+        "l"(src), "r"(bytes), "r"(smem_u32(bar))
+        : "memory");
+}
+__device__ __forceinline__ void cp_async4(void *dst, const void *src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void expect_tx(uint64_t *bar, uint32_t bytes) {
+    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void tmem_zero16(uint32_t addr) {
+    const float z[16] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    tmem_st16(addr, z);
+}
+
+// The tile list: prefix[b] = tiles of the sequences before b, each sequence's cache id,
+// length and node count.  By all THREADS threads.
+template <int THREADS>
+__device__ __forceinline__ void tree_prefix(const TreeArgs &a, int *prefix, int *sids, int *lens, int *nodes, int *wsum,
+                                            int *status) {
+    const int B = a.B, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int per = (B + THREADS - 1) / THREADS;
+    const int b0 = min(B, (int)threadIdx.x * per), b1 = min(B, b0 + per);
+    int sum = 0;
+#pragma unroll 1
+    for (int b = b0; b < b1; ++b) {
+        const SeqRef sq = resolve_seq(a.seq_ids, a.seq_lens, 0, b, a.cache.kv.n_seqs, a.cache.max_seq_len, status);
+        sids[b] = sq.sid;
+        lens[b] = sq.len;
+        nodes[b] = tree_nodes(a, b, status);
+        const int v = ceil_div(sq.len, TILE) + 1;
+        prefix[b] = v;
+        sum += v;
+    }
+    int incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) wsum[warp] = incl;
+    __syncthreads();
+    int run = incl - sum, tot = 0;
+#pragma unroll 1
+    for (int w = 0; w < THREADS / 32; ++w) {
+        if (w < warp) run += wsum[w];
+        tot += wsum[w];
+    }
+#pragma unroll 1
+    for (int b = b0; b < b1; ++b) {
+        const int v = prefix[b];
+        prefix[b] = run;
+        run += v;
+    }
+    if (threadIdx.x == 0) prefix[B] = tot;
+    __syncthreads();
+}
+
+struct Ring {
+    int n, slot = 0;
+    uint32_t ph = 0;
+    __device__ __forceinline__ explicit Ring(int slots) : n(slots) {}
+    __device__ __forceinline__ void next() {
+        if (++slot == n) {
+            slot = 0;
+            ph ^= 1;
+        }
+    }
+};
+
+// 2^k that brings amax into [128, 256), as (factor, its inverse's exponent -k).
+__device__ __forceinline__ float pow2_scale(float amax, int *k) {
+    int e = (int)((__float_as_uint(amax) >> 23) & 0xff) - 127;
+    e = min(max(e, -100), 120);
+    *k = 7 - e;
+    return __int_as_float((*k + 127) << 23);
+}
+__device__ __forceinline__ float pow2i(int k) { return __int_as_float((k + 127) << 23); }
+
+// The two 8-bit parts of 8 scaled values: hi = rn(x), lo = rn(x - hi).
+__device__ __forceinline__ void split_codes(const float (&x)[8], uint2 *hi, uint2 *lo) {
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        h[i] = float_to_codes2(x[2 * i], x[2 * i + 1]);
+        const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)h[i], __NV_E4M3);
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&r));
+        l[i] = float_to_codes2(x[2 * i] - f.x, x[2 * i + 1] - f.y);
+    }
+    *hi = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
+    *lo = make_uint2(l[0] | l[1] << 16, l[2] | l[3] << 16);
+}
+__device__ __forceinline__ uint32_t pack_half(float a, float b) {
+    const __half2 v = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+// byte offset of 16-byte chunk c (0..7) of row r of an 8-bit tile (128-byte rows, swizzled)
+__device__ __forceinline__ uint32_t off8(int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); }
+
+// ---------------------------------------------------------------------------
+// TPC: rows of a copy, and tokens of a tile that a copy weighs (32, 64, 128); MT: M tiles.
+template <bool E4, int TPC, int MT>
+__global__ void __launch_bounds__(Roles<E4>::THREADS, 1)
+    tree_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                   const __grid_constant__ TreeArgs a, const __grid_constant__ Layout lay, int2 *seg_tab) {
+    typedef Roles<E4> Ro;
+    constexpr int THREADS = Ro::THREADS;
+    constexpr int NC = 128 / TPC;  // copies
+    static_assert(MT == 1 || TPC == 128, "two M tiles hold one copy each");
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    Bars *bars = (Bars *)smem;
+    float2 *ml_s = (float2 *)(smem + OFF_ML);
+    float *l_s = (float *)(smem + OFF_L);
+    int *cuts = (int *)(smem + OFF_CUTS);
+    volatile int *abort = &bars->abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int B = a.B, Hkv = a.Hkv, Hv = Hkv * a.n_rb;
+    int *prefix = (int *)(smem + lay.off_tab), *sids = prefix + B + 1, *lens = sids + B, *nodes = lens + B;
+    const bool paged = a.cache.kv.layout == SP_KV_PAGED;
+    const int P = a.cache.kv.page_size;
+    // the first kernel of its call: nothing of the caller's is read before
+    pdl_wait();
+    pdl_trigger();
+
+    tree_prefix<THREADS>(a, prefix, sids, lens, nodes, bars->wsum, blockIdx.x == 0 ? a.status : nullptr);
+    const int T = prefix[B];
+    const int n_grp = share_count((int)gridDim.x / Hv, T, B, a.plan.tc_min_tiles);
+    const int grp = blockIdx.x / Hv, hv = blockIdx.x - grp * Hv, g = hv / a.n_rb, rb = hv - g * a.n_rb;
+    if (grp >= n_grp) return;  // uniform over the CTA: no share
+    if (threadIdx.x < PLAN_THREADS) build_cuts(a.plan, prefix, T, n_grp, cuts, bars->wsum);
+    if (threadIdx.x == THREADS - 1) {
+#pragma unroll 1
+        for (int i = 0; i < lay.nk; ++i) {
+            mbar_init(&bars->k_full[i], Ro::RING_THREADS);
+            mbar_init(&bars->k_empty[i], MT);
+        }
+#pragma unroll 1
+        for (int i = 0; i < lay.nv; ++i) {
+            mbar_init(&bars->v_full[i], Ro::RING_THREADS);
+            mbar_init(&bars->v_empty[i], E4 ? 128 : MT);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&bars->c_full[i], 128);
+            mbar_init(&bars->c_empty[i], MT);
+            mbar_init(&bars->s_full[i], 1);
+            mbar_init(&bars->p_full[i], 128);
+            mbar_init(&bars->pv_done[i], 1);
+        }
+        mbar_init(&bars->q_full, SOFT);
+        mbar_init(&bars->fin, 2);
+        bars->abort = 0;
+        fence_mbar_init();
+        if (paged) {
+            prefetch_tmap(&map_k);
+            prefetch_tmap(&map_v);
+        }
+    }
+    if (warp == Ro::MMA) {
+        tmem_alloc(&bars->tmem, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = bars->tmem;
+    const int x0 = cuts[grp], x1 = cuts[grp + 1];
+    if (blockIdx.x == 0) {  // for the merge: each sequence's first share and its number of them
+#pragma unroll 1
+        for (int b = threadIdx.x; b < B; b += THREADS) {
+            const int j0 = group_of(cuts, n_grp, prefix[b]);
+            seg_tab[b] = make_int2(j0, group_of(cuts, n_grp, prefix[b + 1] - 1) - j0 + 1);
+        }
+    }
+
+    if (warp >= Ro::PROD && warp < Ro::MMA) {
+        // ------------------------------------------------------------ producers
+        constexpr int PT = Ro::RING_THREADS, ES = E4 ? 1 : 2, CH = DH * ES / 16;  // chunks a row
+        const bool is_v = (warp - Ro::PROD) & 1;
+        const int pidx = (warp - Ro::PROD) >> 1, ptid = pidx * 32 + lane;
+        const bool lead = pidx == 0;
+        uint64_t *full = is_v ? bars->v_full : bars->k_full, *empty = is_v ? bars->v_empty : bars->k_empty;
+        const int slot_bytes = E4 ? SLOT8 + (is_v ? SCALES : 0) : SLOT16;
+        uint8_t *ring = smem + (is_v ? lay.off_v : lay.off_k);
+        const CUtensorMap *map = is_v ? &map_v : &map_k;
+        const uint8_t *pool = (const uint8_t *)(is_v ? a.cache.kv.v_pool : a.cache.kv.k_pool);
+        const bf16 *fresh = (const bf16 *)(is_v ? a.v_new : a.k_new);
+        const long long fs = is_v ? a.vs : a.ks;
+        const uint64_t pol = policy_evict_first();
+        auto dst_off = [](int r, int c) { return E4 ? off8(r, c) : kv_off(r, c); };
+        Ring rg(is_v ? lay.nv : lay.nk);
+        int bad = 0, filled = 0;
+        bool stop = false;
+#pragma unroll 1
+        for (int x = x0; x < x1 && !stop;) {
+            const Seg sg = seg_at(prefix, B, x, x1);
+            x += sg.n;
+            const int b = sg.b, sid = sids[b], L = lens[b];
+            // a contiguous sequence's rows: Hkv rows a token
+            const uint8_t *seq = nullptr;
+            const float *seq_scale[2] = {nullptr, nullptr};
+            if (!paged && L > 0) {
+                seq = (const uint8_t *)(is_v ? a.cache.kv.v_seq : a.cache.kv.k_seq)[sid];
+                if (E4 && is_v) {
+                    seq_scale[0] = ((const float *const *)a.cache.k_scale)[sid];
+                    seq_scale[1] = ((const float *const *)a.cache.v_scale)[sid];
+                }
+            }
+#pragma unroll 1
+            for (int i = 0; i < sg.n; ++i) {
+                const int t = sg.t_a + i, t0 = t * TILE;
+                const bool is_fresh = t == sg.nt - 1;
+                const int n_tok = is_fresh ? 0 : min(TILE, L - t0);
+                const int n_pg = paged ? n_tok / P : 0;  // whole pages
+                int page = -1;                           // page ids (up to eight), asked for before the wait
+                if (paged && lane * P < n_tok) {
+                    const int lp = t0 / P + lane;
+                    page = lp < a.cache.kv.max_pages ? a.cache.kv.page_table[(size_t)sid * a.cache.kv.max_pages + lp] : -1;
+                    if (page < 0 || page >= a.cache.kv.n_pages) page = -1, bad = 1;
+                }
+                // warp-uniform verdict: the collectives below need every lane
+                if (!mbar_wait_warp(&empty[rg.slot], rg.ph ^ 1, abort)) {
+                    stop = true;
+                    break;
+                }
+                uint8_t *dst = ring + rg.slot * slot_bytes;
+                uint8_t *sc = dst + SLOT8;  // (E4 && is_v)
+                bool plain = false;         // this thread wrote shared memory or issued cp.async
+                if (n_pg > 0 && lead) {
+                    const bool ok = lane < n_pg && page >= 0;
+                    const unsigned okm = __ballot_sync(0xffffffffu, ok);
+                    const uint32_t bytes = (uint32_t)(P * DH * ES + (E4 && is_v ? P * 8 : 0));
+                    if (lane == 0 && okm) expect_tx(&full[rg.slot], __popc(okm) * bytes);
+                    __syncwarp();
+                    if (ok) {  // the cache is read once: evict-first keeps queries and partials in L2
+                        const int row = page * Hkv + g;
+                        if constexpr (E4) {
+                            tma_load_2d_hint(dst + lane * P * DH, map, &full[rg.slot], 0, row * P, pol);
+                            if (is_v) {
+                                const size_t at = (size_t)row * P;
+                                bulk_load(sc + lane * P * 4, (const float *)a.cache.k_scale + at, P * 4, &full[rg.slot]);
+                                bulk_load(sc + TILE * 4 + lane * P * 4, (const float *)a.cache.v_scale + at, P * 4,
+                                          &full[rg.slot]);
+                            }
+                        } else {
+                            tma_load_4d_hint(dst + lane * P * 256, map, &full[rg.slot], 0, 0, 0, row * (P / 8), pol);
+                        }
+                    }
+                    // a page outside the pool: zeros
+#pragma unroll 1
+                    for (unsigned miss = ~okm & ((1u << n_pg) - 1u); miss; miss &= miss - 1) {
+                        const int j = __ffs(miss) - 1;
+#pragma unroll 1
+                        for (int e = lane; e < P * CH; e += 32) st_shared_v4(dst + j * P * DH * ES + e * 16, 0, 0, 0, 0);
+                        if (E4 && is_v && lane < P / 4) {
+                            st_shared_v4(sc + j * P * 4 + lane * 16, 0, 0, 0, 0);
+                            st_shared_v4(sc + TILE * 4 + j * P * 4 + lane * 16, 0, 0, 0, 0);
+                        }
+                        plain = true;
+                    }
+                }
+                if (!is_fresh) {
+                    const int r0 = n_pg * (paged ? P : 0);  // first row not covered by TMA
+                    if (r0 < n_tok) {
+                        plain = true;
+                        if (paged) {  // the last, partial page
+                            const int pg = __shfl_sync(0xffffffffu, page, n_pg);
+                            const size_t at = ((size_t)max(pg, 0) * Hkv + g) * P;
+#pragma unroll 1
+                            for (int idx = ptid; idx < (n_tok - r0) * CH; idx += PT) {
+                                const int r = idx / CH, c = idx - r * CH;
+                                if (pg >= 0) cp_async16(dst + dst_off(r0 + r, c), pool + (at + r) * (DH * ES) + c * 16);
+                                else st_shared_v4(dst + dst_off(r0 + r, c), 0, 0, 0, 0);
+                            }
+                            if (E4 && is_v) {
+#pragma unroll 1
+                                for (int r = ptid; r < n_tok - r0; r += PT) {
+                                    if (pg >= 0) {
+                                        cp_async4(sc + (r0 + r) * 4, (const float *)a.cache.k_scale + at + r);
+                                        cp_async4(sc + (TILE + r0 + r) * 4, (const float *)a.cache.v_scale + at + r);
+                                    } else {
+                                        *(float *)(sc + (r0 + r) * 4) = 0.f;
+                                        *(float *)(sc + (TILE + r0 + r) * 4) = 0.f;
+                                    }
+                                }
+                            }
+                        } else {
+                            const uint8_t *src = seq + ((size_t)t0 * Hkv + g) * (DH * ES);
+#pragma unroll 4
+                            for (int idx = ptid; idx < n_tok * CH; idx += PT) {
+                                const int r = idx / CH, c = idx - r * CH;
+                                cp_async16(dst + dst_off(r, c), src + (size_t)r * Hkv * (DH * ES) + c * 16);
+                            }
+                            if (E4 && is_v) {
+#pragma unroll 1
+                                for (int r = ptid; r < n_tok; r += PT) {
+                                    const size_t at = (size_t)(t0 + r) * Hkv + g;
+                                    cp_async4(sc + r * 4, seq_scale[0] + at);
+                                    cp_async4(sc + (TILE + r) * 4, seq_scale[1] + at);
+                                }
+                            }
+                        }
+                    }
+                    // values past the end are multiplied by weights of 0: they must be
+                    // finite (keys there give scores that are replaced)
+                    if (!E4 && is_v && n_tok < TILE) {
+                        plain = true;
+#pragma unroll 1
+                        for (int idx = ptid; idx < (TILE - n_tok) * CH; idx += PT)
+                            st_shared_v4(dst + kv_off(n_tok + idx / CH, idx % CH), 0, 0, 0, 0);
+                    }
+                } else if (!E4 || !is_v) {
+                    // the nodes' rows: 16 lanes a row, 8 elements a lane
+                    plain = true;
+                    const int n = nodes[b], c = lane & 15;
+                    unsigned long long vb = 0;
+#pragma unroll 2
+                    for (int r = pidx * 2 + (lane >> 4); r < 64; r += 2 * Ro::RING_WARPS) {
+                        uint4 u = make_uint4(0, 0, 0, 0);
+                        if (r < n) u = *(const uint4 *)(fresh + ((size_t)b * a.N + r) * fs + (size_t)g * DH + c * 8);
+                        if constexpr (!E4) {
+                            if (is_v) {
+                                uint32_t w[4] = {u.x, u.y, u.z, u.w};
+                                bool odd = false;
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) {
+                                    const bool lo = (w[q] & 0x7f80u) == 0x7f80u, hi = (w[q] & 0x7f800000u) == 0x7f800000u;
+                                    odd = odd || lo || hi;
+                                    w[q] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+                                }
+                                u = make_uint4(w[0], w[1], w[2], w[3]);
+                                const unsigned o = __ballot_sync(0xffffffffu, odd);
+                                const int even = r & ~1;  // (lanes 0-15 hold the even row)
+                                if (o & 0xffffu) vb |= 1ull << even;
+                                if (o >> 16) vb |= 2ull << even;
+                            }
+                            st_shared_v4(dst + kv_off(r, c), u.x, u.y, u.z, u.w);
+                        } else {
+                            // keys as two 8-bit parts, rows r and 64 + r
+                            float v[8];
+                            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+                            float amax = 0.f;
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                v[2 * q] = __uint_as_float(w[q] << 16);
+                                v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
+                                amax = fmaxf(amax, fmaxf(fabsf(v[2 * q]), fabsf(v[2 * q + 1])));
+                            }
+#pragma unroll
+                            for (int o = 1; o < 16; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+                            int k;
+                            const float f = pow2_scale(amax, &k);
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) v[q] *= f;
+                            uint2 hi, lo;
+                            split_codes(v, &hi, &lo);
+                            *(uint2 *)(dst + off8(r, c >> 1) + (c & 1) * 8) = hi;
+                            *(uint2 *)(dst + off8(64 + r, c >> 1) + (c & 1) * 8) = lo;
+                        }
+                    }
+                    if (!E4 && is_v && lane == 0) bars->vbad[rg.slot][pidx] = vb;
+                }
+                if (plain) {
+                    fence_proxy_async();  // this thread's shared-memory stores
+                    cp_async_mbar_arrive(&full[rg.slot]);
+                } else {
+                    mbar_arrive(&full[rg.slot]);
+                }
+                ++filled;
+                rg.next();
+            }
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");  // nothing lands after the CTA is gone
+        if (lead && lane == 0) {
+            // drain TMA writes still in flight (only possible after an abort)
+            Ring rd(rg.n);
+#pragma unroll 1
+            for (int j = 0; j < filled; ++j, rd.next())
+                if (j + rg.n >= filled) mbar_wait_drain(&full[rd.slot], rd.ph);
+        }
+        bad = __any_sync(0xffffffffu, bad);
+        if (bad && lane == 0 && a.status) atomicOr(a.status, SP_DEV_BAD_PAGE);
+    } else if (E4 && warp >= Ro::CVT) {
+        // ------------------------------------------------------------ V codes -> 16-bit floats
+        const int ct = threadIdx.x - Ro::CVT * 32, cw = warp - Ro::CVT;
+        Ring rv(lay.nv), rc(CONV);
+        bool ok = true;
+#pragma unroll 1
+        for (int x = x0; ok && x < x1;) {
+            const Seg sg = seg_at(prefix, B, x, x1);
+            x += sg.n;
+            const int b = sg.b, L = lens[b];
+#pragma unroll 1
+            for (int i = 0; i < sg.n; ++i) {
+                const int t = sg.t_a + i;
+                const bool is_fresh = t == sg.nt - 1;
+                const int n_tok = is_fresh ? 0 : min(TILE, L - t * TILE);
+                ok = mbar_wait_warp(&bars->v_full[rv.slot], rv.ph, abort) &&
+                     mbar_wait_warp(&bars->c_empty[rc.slot], rc.ph ^ 1, abort);
+                if (!ok) break;
+                const uint8_t *src = smem + lay.off_v + rv.slot * (SLOT8 + SCALES);
+                uint8_t *dst = smem + lay.off_c + rc.slot * SLOT16;
+                float *par = (float *)(smem + lay.off_c + CONV * SLOT16 + rc.slot * PARAMS);
+                if (!is_fresh) {
+#pragma unroll 4
+                    for (int idx = ct; idx < TILE * 8; idx += 128) {
+                        const int r = idx >> 3, c = idx & 7;
+                        uint4 u = make_uint4(0, 0, 0, 0);
+                        if (r < n_tok) u = *(const uint4 *)(src + off8(r, c));
+                        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+                        uint32_t h[8];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {
+                            const __half2_raw f = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[q >> 1] >> (16 * (q & 1))),
+                                                                             __NV_E4M3);
+                            h[q] = (uint32_t)f.x | (uint32_t)f.y << 16;
+                        }
+                        st_shared_v4(dst + kv_off(r, 2 * c), h[0], h[1], h[2], h[3]);
+                        st_shared_v4(dst + kv_off(r, 2 * c + 1), h[4], h[5], h[6], h[7]);
+                    }
+                    float ks = 0.f, vs = 1.f;
+                    if (ct < n_tok) {
+                        ks = ((const float *)(src + SLOT8))[ct];
+                        vs = fmaxf(((const float *)(src + SLOT8))[TILE + ct], 7.888609052210118e-31f);  // 2^-100
+                    }
+                    par[2 * ct] = ks * a.scale_log2;
+                    par[2 * ct + 1] = __log2f(vs);
+                    par[2 * TILE + ct] = 1.f / vs;
+                } else {
+                    const int n = nodes[b], c = lane & 15;
+                    unsigned long long vb = 0;
+#pragma unroll 1
+                    for (int r = cw * 2 + (lane >> 4); r < TILE; r += 8) {
+                        uint4 uk = make_uint4(0, 0, 0, 0), uv = uk;
+                        if (r < n) {
+                            const size_t row = (size_t)b * a.N + r;
+                            uk = *(const uint4 *)((const bf16 *)a.k_new + row * a.ks + (size_t)g * DH + c * 8);
+                            uv = *(const uint4 *)((const bf16 *)a.v_new + row * a.vs + (size_t)g * DH + c * 8);
+                        }
+                        const uint32_t wk[4] = {uk.x, uk.y, uk.z, uk.w}, wv[4] = {uv.x, uv.y, uv.z, uv.w};
+                        float v[8], amk = 0.f, amv = 0.f;
+                        bool odd = false;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            amk = fmaxf(amk, fmaxf(fabsf(__uint_as_float(wk[q] << 16)), fabsf(__uint_as_float(wk[q] & 0xffff0000u))));
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const float y = __uint_as_float(e ? wv[q] & 0xffff0000u : wv[q] << 16);
+                                const bool fin = isfinite(y);
+                                odd = odd || !fin;
+                                v[2 * q + e] = fin ? y : 0.f;
+                                amv = fmaxf(amv, fabsf(v[2 * q + e]));
+                            }
+                        }
+#pragma unroll
+                        for (int o = 1; o < 16; o <<= 1) {
+                            amk = fmaxf(amk, __shfl_xor_sync(0xffffffffu, amk, o));
+                            amv = fmaxf(amv, __shfl_xor_sync(0xffffffffu, amv, o));
+                        }
+                        const unsigned o = __ballot_sync(0xffffffffu, odd);
+                        if (r < 64) {
+                            if (o & 0xffffu) vb |= 1ull << (r & ~1);
+                            if (o >> 16) vb |= 2ull << (r & ~1);
+                        }
+                        int kk, kv;
+                        pow2_scale(amk, &kk);
+                        const float f = pow2_scale(amv, &kv);
+                        st_shared_v4(dst + kv_off(r, c), pack_half(v[0] * f, v[1] * f), pack_half(v[2] * f, v[3] * f),
+                                     pack_half(v[4] * f, v[5] * f), pack_half(v[6] * f, v[7] * f));
+                        if (c == 0) {
+                            // an infinite key saturates in its parts: its scores are NaN
+                            par[2 * r] = pow2i(-kk) * a.scale_log2 + (amk - amk);
+                            par[2 * r + 1] = (float)-kv;
+                            par[2 * TILE + r] = pow2i(kv);
+                        }
+                    }
+                    if (lane == 0) bars->vbad[rc.slot][cw] = vb;
+                }
+                fence_proxy_async();
+                mbar_arrive(&bars->c_full[rc.slot]);
+                mbar_arrive(&bars->v_empty[rv.slot]);
+                rv.next();
+                rc.next();
+            }
+        }
+    } else if (warp >= Ro::MMA && warp < Ro::CVT) {
+        // ------------------------------------------------------------ MMA issue
+        // Pipeline w: S of its next tile, then (its softmax done) PV.  Both by the whole
+        // warp, the instructions under `on` (see elect_one).
+        const int w = warp - Ro::MMA;
+        const bool on = elect_one();
+        constexpr uint32_t idesc_s = E4 ? (1u << 4) | ((uint32_t)(TILE >> 3) << 17) | (8u << 24) : idesc_bf16_f32(128, TILE);
+        // 16-bit floats: format bits 0 instead of bf16's 1
+        constexpr uint32_t idesc_o = E4 ? (1u << 4) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | (8u << 24)
+                                        : idesc_bf16_f32_bmn(128, DH);
+        const uint32_t s_tmem = tmem + (uint32_t)(w * 128), o_tmem = tmem + O_COL + (uint32_t)(w * DH);
+        const uint64_t dq = sw128_kmajor_desc(smem + lay.off_q + (MT == 2 ? w * Q_TILE : 0));
+        const uint64_t dk0 = sw128_kmajor_desc_sbo(smem + lay.off_k, E4 ? 1024 : GROUP_STRIDE);
+        const uint64_t dv0 = sw128_mnmajor_desc2(smem + (E4 ? lay.off_c : lay.off_v), HALF_STRIDE, GROUP_STRIDE);
+        uint64_t *vf = E4 ? bars->c_full : bars->v_full, *ve = E4 ? bars->c_empty : bars->v_empty;
+        Ring rk(lay.nk), rv(E4 ? CONV : lay.nv);
+        bool ok = true;
+        uint32_t kp = 0;
+        int j = 0;
+#pragma unroll 1
+        for (int x = x0; ok && x < x1; ++j) {
+            const Seg sg = seg_at(prefix, B, x, x1);
+            x += sg.n;
+            const int n_seg = __shfl_sync(0xffffffffu, sg.n, 0), t_a = __shfl_sync(0xffffffffu, sg.t_a, 0),
+                      nt = __shfl_sync(0xffffffffu, sg.nt, 0);
+            if (!mbar_wait_warp(&bars->q_full, (uint32_t)(j & 1), abort)) break;
+            bool first = true;
+#pragma unroll 1
+            for (int i = 0; i < n_seg; ++i, rk.next(), rv.next()) {
+                if (MT == 1 && (i & 1) != w) continue;  // the other pipeline's tile
+                ok = mbar_wait_warp(&bars->k_full[rk.slot], rk.ph, abort);
+                if (!ok) break;
+                tc_fence_after();
+                fence_proxy_async();  // cp.async data -> tensor-core reads
+                const uint64_t dk = dk0 + (uint32_t)(rk.slot * ((E4 ? SLOT8 : SLOT16) >> 4));
+                if (on) {
+                    if constexpr (E4) {
+#pragma unroll
+                        for (int kk = 0; kk < 8; ++kk)  // part kk / 4, 32 dims each
+                            mma_e4m3(s_tmem, dq + (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2), dk + (uint64_t)((kk & 3) * 2),
+                                     idesc_s, kk > 0);
+                    } else {
+#pragma unroll
+                        for (int kk = 0; kk < 8; ++kk)  // 16 dims: 32 B of a row of dim half kk / 4
+                            mma_bf16(s_tmem, dq + (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2),
+                                     dk + (uint64_t)((kk >> 2) * (HALF_STRIDE >> 4) + (kk & 3) * 2), idesc_s, kk > 0);
+                    }
+                    mma_commit(&bars->k_empty[rk.slot]);
+                    mma_commit(&bars->s_full[w]);
+                }
+                __syncwarp();
+                const bool is_fresh = t_a + i == nt - 1;
+                ok = mbar_wait_warp(&vf[rv.slot], rv.ph, abort) && mbar_wait_warp(&bars->p_full[w], kp, abort);
+                if (!ok) break;
+                kp ^= 1;
+                tc_fence_after();
+                fence_proxy_async();
+                const uint64_t dv = dv0 + (uint32_t)(rv.slot * (SLOT16 >> 4));
+                if (on) {
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)  // 16 tokens: 8 columns of P, two 8-token groups of V
+                        if (kk < 4 || !is_fresh)  // (at most 64 nodes)
+                            mma_bf16_ts(o_tmem, s_tmem + (uint32_t)(kk * 8), dv + (uint64_t)(kk * (2 * GROUP_STRIDE >> 4)),
+                                        idesc_o, !first || kk > 0);
+                    mma_commit(&ve[rv.slot]);
+                }
+                __syncwarp();
+                first = false;
+            }
+            // (without a tile of its own too: no segment's queries may be replaced before
+            // both issuers have passed them)
+            if (on && ok) mma_commit(&bars->pv_done[w]);
+            __syncwarp();
+        }
+        if (on) mma_commit(&bars->fin);  // completes when every MMA of this issuer is done
+        __syncwarp();
+    } else if (warp < 8) {
+        // ------------------------------------------------------------ softmax + epilogue
+        const int wg = warp >> 2, ln = threadIdx.x & 127;  // pipeline; TMEM lane
+        const int cp = ln / TPC, row_t = ln - cp * TPC;    // copy, row of the M tile
+        const int r = (MT == 2 ? wg * 128 : 0) + row_t;    // row of this CTA's block
+        const int rr = rb * a.rb_rows + r;                 // query row of the kv head
+        const bool active = r < a.rb_rows && rr < a.R;
+        const bool warp_active = __any_sync(0xffffffffu, active);
+        const int node = active ? rr / a.G : 0, hl = active ? rr - node * a.G : 0;
+        const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t s_col = lane_base + (uint32_t)(wg * 128), o_col = lane_base + O_COL + (uint32_t)(wg * DH);
+        bool ok = true;
+        uint32_t ks_ph = 0, pv_ph = 0;
+        Ring rv(E4 ? CONV : lay.nv);
+        uint64_t *vf = E4 ? bars->c_full : bars->v_full;
+#pragma unroll 1
+        for (int x = x0; x < x1;) {
+            const Seg sg = seg_at(prefix, B, x, x1);
+            x += sg.n;
+            const int b = sg.b, L = lens[b], n = nodes[b];
+            const bool live = active && node < n;
+            const uint64_t sees = live ? tree_mask(a, b, node, n) : 0;
+            // ---- queries -> shared memory; a thread its own row (each copy its rows)
+            float rs = 1.f;  // 8-bit parts: the row's scale
+            {
+                const uint4 *src = (const uint4 *)((const bf16 *)a.q + ((size_t)b * a.N + node) * a.qs + (size_t)(g * a.G + hl) * DH);
+                uint8_t *q = smem + lay.off_q + (MT == 2 ? wg * Q_TILE : 0);
+                const int c_lo = MT == 2 ? 0 : wg * 8, c_n = MT == 2 ? 16 : 8;
+                if constexpr (!E4) {
+                    uint4 u[16];
+#pragma unroll
+                    for (int c = 0; c < 16; ++c)
+                        if (c < c_n) u[c] = live ? src[c_lo + c] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        if (c >= c_n) break;
+                        const int cc = c_lo + c;
+                        st_shared_v4(q + (cc >> 3) * 16384 + off8(ln, cc & 7), u[c].x, u[c].y, u[c].z, u[c].w);
+                    }
+                } else {
+                    float amax = 0.f;
+#pragma unroll 4
+                    for (int c = 0; c < 16; ++c) {
+                        const uint4 u = live ? src[c] : make_uint4(0, 0, 0, 0);
+                        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                        for (int q4 = 0; q4 < 4; ++q4)
+                            amax = fmaxf(amax, fmaxf(fabsf(__uint_as_float(w[q4] << 16)), fabsf(__uint_as_float(w[q4] & 0xffff0000u))));
+                    }
+                    int k;
+                    const float f = pow2_scale(amax, &k);
+                    rs = pow2i(-k) + (amax - amax);  // (an infinite query: NaN)
+#pragma unroll 2
+                    for (int c = c_lo; c < c_lo + c_n; ++c) {
+                        const uint4 u = live ? src[c] : make_uint4(0, 0, 0, 0);
+                        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+                        float v[8];
+#pragma unroll
+                        for (int q4 = 0; q4 < 4; ++q4) {
+                            v[2 * q4] = __uint_as_float(w[q4] << 16) * f;
+                            v[2 * q4 + 1] = __uint_as_float(w[q4] & 0xffff0000u) * f;
+                        }
+                        uint2 hi, lo;
+                        split_codes(v, &hi, &lo);
+                        *(uint2 *)(q + off8(ln, c >> 1) + (c & 1) * 8) = hi;
+                        *(uint2 *)(q + 16384 + off8(ln, c >> 1) + (c & 1) * 8) = lo;
+                    }
+                }
+                fence_proxy_async();
+                mbar_arrive(&bars->q_full);
+            }
+            // ---- tiles
+            float m = -INFINITY, l = 0.f;
+            bool first = true;
+            unsigned long long vb = 0;
+#pragma unroll 1
+            for (int i = 0; i < sg.n; ++i, rv.next()) {
+                if (MT == 1 && (i & 1) != wg) continue;
+                const int t = sg.t_a + i;
+                const bool is_fresh = t == sg.nt - 1;
+                const int n_tok = is_fresh ? 0 : min(TILE, L - t * TILE);
+                // warp-uniform verdicts: the TMEM loads and stores are warp-collective
+                ok = ok && mbar_wait_warp(&bars->s_full[wg], ks_ph, abort);
+                if (E4 || is_fresh) ok = ok && mbar_wait_warp(&vf[rv.slot], rv.ph, abort);
+                ks_ph ^= 1;
+                if (!ok) continue;
+                tc_fence_after();
+                if (is_fresh) {
+#pragma unroll
+                    for (int w = 0; w < (E4 ? 4 : 2); ++w) vb |= ((volatile unsigned long long *)bars->vbad[rv.slot])[w];
+                }
+                if (!warp_active) {  // its lanes' weights reach no row that is used
+                    mbar_arrive(&bars->p_full[wg]);
+                    first = false;
+                    continue;
+                }
+                const float *par = (const float *)(smem + lay.off_c + CONV * SLOT16 + rv.slot * PARAMS);
+                const bool masked = is_fresh || n_tok < TILE;
+                constexpr int CH = TPC < 32 ? TPC : 32, N_CH = TPC / CH;
+                const int tok0 = cp * TPC;  // this copy's first token
+                // scores of chunk c in log2 units, with log2 of the value's scale (8-bit)
+                auto scores = [&](int c, float (&s)[CH]) {
+                    const int j0 = tok0 + c * CH;
+                    tmem_ld32(s_col + (uint32_t)j0, s);
+                    if constexpr (E4) {
+                        if (is_fresh && j0 < 64) {  // warp-uniform (a copy is whole warps)
+                            float s2[CH];
+                            tmem_ld32(s_col + (uint32_t)(64 + j0), s2);
+#pragma unroll
+                            for (int e = 0; e < CH; ++e) s[e] += s2[e];
+                        }
+#pragma unroll
+                        for (int e = 0; e < CH; e += 2) {
+                            const float4 p2 = *(const float4 *)(par + 2 * (j0 + e));
+                            s[e] = fmaf(s[e] * rs, p2.x, p2.y);
+                            s[e + 1] = fmaf(s[e + 1] * rs, p2.z, p2.w);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < CH; ++e) s[e] *= a.scale_log2;
+                    }
+                    if (masked) {
+                        const uint32_t bits = is_fresh ? (j0 < 64 ? (uint32_t)(sees >> j0) : 0u)
+                                              : n_tok - j0 >= 32 ? ~0u : n_tok > j0 ? (1u << (n_tok - j0)) - 1u : 0u;
+#pragma unroll
+                        for (int e = 0; e < CH; ++e)
+                            if (!((bits >> e) & 1)) s[e] = -INFINITY;
+                    }
+                };
+                float mt = -INFINITY;
+                float sv[TPC <= 64 ? N_CH : 1][CH];  // (up to 64 tokens stay in registers)
+#pragma unroll
+                for (int c = 0; c < N_CH; ++c) {
+                    float(&s)[CH] = sv[TPC <= 64 ? c : 0];
+                    scores(c, s);
+                    float mx[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) mx[e] = fmaxf(fmaxf(s[e], s[e + 8]), fmaxf(s[e + 16], s[e + 24]));
+                    mt = fmaxf(mt, fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])),
+                                         fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7]))));
+                    if constexpr (TPC > 64) tmem_st32(s_col + (uint32_t)(c * CH), s);
+                }
+                const bool grow = mt > m + RESCALE_LOG2 || (m == -INFINITY && mt != -INFINITY);
+                const float m_new = grow ? mt : m;
+                const float alpha = grow ? (m == -INFINITY ? 0.f : fast_exp2(m - m_new)) : 1.f;
+                // (S of this tile was issued behind PV of the pipeline's last one: O is complete)
+                if (!first && __any_sync(0xffffffffu, grow)) {
+#pragma unroll 1
+                    for (int c0 = 0; c0 < DH; c0 += 32) {
+                        float o[32];
+                        tmem_ld32(o_col + c0, o);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] *= alpha;
+                        tmem_st32(o_col + c0, o);
+                    }
+                }
+                l *= alpha;
+                m = m_new;
+                first = false;
+                const float mu = m == -INFINITY ? 0.f : m;  // a row that sees nothing: weights of 0
+                float ps[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < N_CH; ++c) {
+                    float(&s)[CH] = sv[TPC <= 64 ? c : 0];
+                    if constexpr (TPC > 64) tmem_ld32(s_col + (uint32_t)(c * CH), s);
+                    float pk[CH / 2];
+#pragma unroll
+                    for (int e = 0; e < CH; e += 4) {
+                        float w[4];
+#pragma unroll
+                        for (int q4 = 0; q4 < 4; ++q4) w[q4] = fast_exp2(s[e + q4] - mu);
+                        if constexpr (E4) {
+                            const float4 iv = *(const float4 *)(par + 2 * TILE + tok0 + c * CH + e);
+                            ps[0] = fmaf(w[0], iv.x, ps[0]);
+                            ps[1] = fmaf(w[1], iv.y, ps[1]);
+                            ps[2] = fmaf(w[2], iv.z, ps[2]);
+                            ps[3] = fmaf(w[3], iv.w, ps[3]);
+                            pk[e / 2] = __uint_as_float(pack_half(w[0], w[1]));
+                            pk[e / 2 + 1] = __uint_as_float(pack_half(w[2], w[3]));
+                        } else {
+#pragma unroll
+                            for (int q4 = 0; q4 < 4; ++q4) ps[q4] += w[q4];
+                            pk[e / 2] = __uint_as_float(pack_bf16(w[0], w[1]));
+                            pk[e / 2 + 1] = __uint_as_float(pack_bf16(w[2], w[3]));
+                        }
+                    }
+                    // P over S's first half, whose scores this warp has read (chunk c covers
+                    // columns of chunks <= c only)
+                    tmem_st16(s_col + (uint32_t)((tok0 + c * CH) / 2), pk);
+                }
+                if constexpr (NC > 1) {  // the other copies' tokens
+#pragma unroll
+                    for (int z = 0; z < 4; ++z)
+                        if (z * 16 < tok0 / 2 || z * 16 >= (tok0 + TPC) / 2) tmem_zero16(s_col + (uint32_t)(z * 16));
+                }
+                l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+                tc_fence_before();
+                mbar_arrive(&bars->p_full[wg]);
+            }
+
+            // ---- epilogue: the pipelines' (one M tile) and copies' parts of each row are
+            // added; the output (the pair in one share) or a partial is written
+            const int j_first = group_of(cuts, n_grp, sg.xp), j_last = group_of(cuts, n_grp, sg.xp + sg.nt - 1);
+            const bool whole = j_first == j_last;
+            const int n1 = MT == 2 ? sg.n : sg.n >> 1;  // tiles of pipeline 1
+            ml_s[wg * 128 + ln] = make_float2(m, l);
+            const bool has_fresh = sg.t_a + sg.n == sg.nt;
+            if (ln == 0 && (has_fresh ? MT == 2 || ((sg.n - 1) & 1) == wg : wg == 0)) bars->seg_vbad = vb;
+            named_sync(BAR_EPI, SOFT);
+            const unsigned long long seg_vb = *(volatile unsigned long long *)&bars->seg_vbad;
+            float a0, a1 = 0.f, mc, lsum;
+            {
+                mc = -INFINITY;
+                lsum = 0.f;
+                if constexpr (MT == 2) {
+                    mc = m;
+                    lsum = l;
+                    a0 = 1.f;
+                } else {
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll
+                        for (int c = 0; c < NC; ++c) mc = fmaxf(mc, ml_s[p * 128 + c * TPC + row_t].x);
+                    const float mu = mc == -INFINITY ? 0.f : mc;
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll
+                        for (int c = 0; c < NC; ++c) {
+                            const float2 v = ml_s[p * 128 + c * TPC + row_t];
+                            if (v.x != -INFINITY) lsum += fast_exp2(v.x - mu) * v.y;
+                        }
+                    const float m0 = ml_s[ln].x, m1 = ml_s[128 + ln].x;
+                    a0 = m0 == -INFINITY ? 0.f : fast_exp2(m0 - mu);
+                    a1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - mu);
+                }
+            }
+            ok = ok && mbar_wait_warp(&bars->pv_done[0], pv_ph, abort) && mbar_wait_warp(&bars->pv_done[1], pv_ph, abort);
+            pv_ph ^= 1;
+            tc_fence_after();
+            // slot of this segment's partial: a share has at most two, the pair that starts
+            // in it and the one that began before
+            const size_t slot = ((size_t)grp * 2 + (j_first == grp)) * Hv + hv;
+            const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
+            // four dims of row q of the block: y unnormalised
+            auto write = [&](int q, int d, float4 y, float scale) {
+                const int qr = rb * a.rb_rows + q, nd = qr / a.G;
+                if (seg_vb && has_fresh && nd < n) {
+                    for (unsigned long long left = seg_vb & tree_mask(a, b, nd, n); left; left &= left - 1) {
+                        const bf16 *v = (const bf16 *)a.v_new + ((size_t)b * a.N + (__ffsll(left) - 1)) * a.vs + (size_t)g * DH + d;
+                        float *yy = &y.x;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float z = to_f(v[e]);
+                            if (!isfinite(z)) yy[e] += z;
+                        }
+                    }
+                }
+                if (whole) {
+                    const bool on = nd < n && scale != 0.f;
+                    const size_t at = ((size_t)b * a.N + nd) * a.Hq * DH + (size_t)(g * a.G + qr - nd * a.G) * DH + d;
+                    *(uint2 *)((bf16 *)a.out + at) =
+                        on ? make_uint2(pack_bf16(y.x * scale, y.y * scale), pack_bf16(y.z * scale, y.w * scale)) : make_uint2(0, 0);
+                } else {
+                    *(float4 *)(a.part_o + (slot * a.rb_rows + q) * DH + d) = y;
+                }
+            };
+            const int d_lo = MT == 2 ? 0 : wg * (DH / 2), d_n = MT == 2 ? DH : DH / 2;
+            uint8_t *stage = smem + lay.off_q + wg * 16384;  // (queries are done with)
+#pragma unroll 1
+            for (int d0 = d_lo; d0 < d_lo + d_n; d0 += 32) {
+                float o[32];
+                if (ok) {
+                    if constexpr (MT == 2) {
+                        tmem_ld32(o_col + d0, o);
+                    } else {
+                        float o1[32];
+                        tmem_ld32(lane_base + O_COL + d0, o);
+                        if (n1 > 0) tmem_ld32(lane_base + O_COL + DH + d0, o1);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            // a part without a weight: its accumulator may hold anything
+                            const float y0 = a0 != 0.f ? a0 * o[e] : 0.f;
+                            o[e] = n1 > 0 && a1 != 0.f ? fmaf(a1, o1[e], y0) : y0;
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = 0.f;
+                }
+                if constexpr (NC == 1) {
+                    if (active) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4) write(r, d0 + e, make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]), inv);
+                    }
+                } else {
+                    // lane's 32 dims as 8 swizzled chunks; then (row, chunk) units add the copies
+#pragma unroll
+                    for (int q4 = 0; q4 < 8; ++q4)
+                        st_shared_v4(stage + ln * 128 + ((q4 ^ (ln & 7)) << 4), __float_as_uint(o[4 * q4]),
+                                     __float_as_uint(o[4 * q4 + 1]), __float_as_uint(o[4 * q4 + 2]), __float_as_uint(o[4 * q4 + 3]));
+                    if (d0 == d_lo && cp == 0) l_s[wg * 128 + ln] = inv;
+                    named_sync(BAR_WG + wg, 128);
+#pragma unroll 1
+                    for (int it = ln; it < TPC * 8; it += 128) {
+                        const int q = it >> 3, q4 = it & 7;
+                        if (q >= a.rb_rows || rb * a.rb_rows + q >= a.R) continue;
+                        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                        for (int c = 0; c < NC; ++c) {
+                            const int lc = c * TPC + q;
+                            const float4 v = ld_shared_v4f(stage + lc * 128 + ((q4 ^ (lc & 7)) << 4));
+                            y.x += v.x, y.y += v.y, y.z += v.z, y.w += v.w;
+                        }
+                        write(q, d0 + q4 * 4, y, l_s[wg * 128 + q]);
+                    }
+                    named_sync(BAR_WG + wg, 128);
+                }
+            }
+            if (!whole && active && cp == 0 && (MT == 2 || wg == 0))
+                *(float2 *)(a.part_ml + (slot * a.rb_rows + r) * 2) = make_float2(mc, lsum);
+            tc_fence_before();
+            named_sync(BAR_EPI, SOFT);  // O, the queries' buffer and ml_s are free
+        }
+    }
+    // every MMA must be finished before TMEM and shared memory go away
+    mbar_wait_drain(&bars->fin, 0);
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && *abort && a.status) atomicOr(a.status, SP_DEV_TIMEOUT);
+    if (warp == Ro::MMA) tmem_dealloc(tmem, 512);
+}
+
+// Merge of the pairs that lie in several shares: a warp per (sequence, kv head, row),
+// four dims a lane, the partials in share order.  Pairs of one share return at once.
+constexpr int MERGE_THREADS = 256, MERGE_ROWS = 16;
+__global__ void __launch_bounds__(MERGE_THREADS) tree_tc_merge_kernel(const __grid_constant__ TreeArgs a, const int2 *seg_tab) {
+    pdl_wait();
+    pdl_trigger();
+    const int hv = blockIdx.x, b = blockIdx.y, Hv = a.Hkv * a.n_rb, g = hv / a.n_rb, rb = hv - g * a.n_rb;
+    const int2 tab = __ldcg(seg_tab + b);
+    if (tab.y <= 1) return;
+    const int lane = threadIdx.x & 31, c = lane * 4, n = tree_nodes(a, b, nullptr);
+#pragma unroll 1
+    for (int q = blockIdx.z * MERGE_ROWS + (threadIdx.x >> 5); q < min(a.rb_rows, (int)(blockIdx.z + 1) * MERGE_ROWS);
+         q += MERGE_THREADS / 32) {
+        const int rr = rb * a.rb_rows + q;
+        if (rr >= a.R) break;
+        float m = -INFINITY, l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int e0 = 0; e0 < tab.y; e0 += 4) {
+            float2 ml[4];
+            float4 ov[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool in = e0 + e < tab.y;
+                const size_t slot = ((size_t)(tab.x + e0 + e) * 2 + (e0 + e == 0)) * Hv + hv, row = slot * a.rb_rows + q;
+                ml[e] = in ? __ldcg((const float2 *)(a.part_ml + row * 2)) : make_float2(-INFINITY, 0.f);
+                ov[e] = in ? __ldcg((const float4 *)(a.part_o + row * DH + c)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            float mn = m;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mn = fmaxf(mn, ml[e].x);
+            if (mn == -INFINITY) continue;
+            const float al = m == -INFINITY ? 0.f : exp2f(m - mn);
+            l *= al;
+            o.x *= al, o.y *= al, o.z *= al, o.w *= al;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (ml[e].x == -INFINITY) continue;
+                const float w = exp2f(ml[e].x - mn);
+                l += w * ml[e].y;
+                o.x += w * ov[e].x, o.y += w * ov[e].y, o.z += w * ov[e].z, o.w += w * ov[e].w;
+            }
+            m = mn;
+        }
+        const int node = rr / a.G;
+        const bool on = node < n && l != 0.f;
+        const float s = on ? 1.f / l : 0.f;
+        *(uint2 *)((bf16 *)a.out + ((size_t)b * a.N + node) * a.Hq * DH + (size_t)(g * a.G + rr - node * a.G) * DH + c) =
+            on ? make_uint2(pack_bf16(o.x * s, o.y * s), pack_bf16(o.z * s, o.w * s)) : make_uint2(0, 0);
+    }
+}
+
+bool make_layout(const TreeArgs &a, bool e4, int mt, Layout *lay) {
+    const int tab = (4 * a.B + 1) * 4;
+    lay->off_tab = OFF_FRONT;
+    lay->off_q = (OFF_FRONT + tab + 1023) & ~1023;
+    int at = lay->off_q + mt * Q_TILE;
+    lay->off_c = at;
+    if (e4) at += CONV * (SLOT16 + PARAMS);
+    const int room = SMEM_MAX - 1024 - at;
+    const int slot = e4 ? SLOT8 : SLOT16;
+    int slots = e4 ? (room - 1024) / (SLOT8 + SCALES) : room / SLOT16;
+    if (slots < 2) return false;
+    if (slots > 2 * MAX_RING) slots = 2 * MAX_RING;
+    lay->nk = slots / 2;
+    lay->nv = slots - lay->nk;
+    lay->off_k = (at + 1023) & ~1023;
+    lay->off_v = lay->off_k + lay->nk * slot;
+    lay->smem = lay->off_v + lay->nv * (slot + (e4 ? SCALES : 0)) + 1024;
+    return lay->smem <= SMEM_MAX;
+}
+
+int row_tiles(const TreeArgs &a) { return a.rb_rows > 128 ? 2 : 1; }
+
+template <bool E4, int TPC, int MT>
+cudaError_t run(const TreeArgs &a, const Layout &lay, const CUtensorMap &mk, const CUtensorMap &mv, int2 *tab,
+                cudaStream_t st) {
+    static bool attr = false;
+    if (!attr) {
+        const cudaError_t e = cudaFuncSetAttribute(tree_tc_kernel<E4, TPC, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MAX);
+        if (e != cudaSuccess) return e;
+        attr = true;
+    }
+    return launch_k(tree_tc_kernel<E4, TPC, MT>, dim3(a.plan.tc_ctas), dim3(Roles<E4>::THREADS), (size_t)lay.smem, st, mk, mv, a,
+                    lay, tab);
+}
+
+}  // namespace
+
+bool tree_tc_supported(const TreeArgs &a) {
+    Layout lay;
+    return a.dh == DH && a.dtype == SP_BF16 && (a.cache.dtype == SP_BF16 || a.cache.dtype == SP_E4M3) && a.B <= MAX_B &&
+           make_layout(a, a.cache.dtype == SP_E4M3, 2, &lay) &&
+           (a.cache.kv.layout == SP_KV_CONTIGUOUS || (long long)a.cache.kv.n_pages * a.Hkv * a.cache.kv.page_size <= 0x7fffffffLL);
+}
+
+void plan_tree_tc(TreeArgs *a, int n_sm) {
+    a->n_rb = ceil_div(a->R, 256);
+    a->rb_rows = a->n_rb == 1 ? a->R : (ceil_div(a->R, a->n_rb) + 7) / 8 * 8;
+    const int Hv = a->Hkv * a->n_rb;
+    AttnArgs &p = a->plan;
+    p.B = a->B;
+    p.tc_ctas = attn_tc_ctas(n_sm, Hv);
+    if (p.tc_ctas / Hv > MAX_GRP) p.tc_ctas = MAX_GRP * Hv;
+    p.tc_min_tiles = kTreeMinTiles;
+    p.tc_seg_cost = kTreeSegCost;
+    p.tc_merge_kernel = 1;
+}
+
+size_t tree_tc_slots(const TreeArgs &a) { return 2 * (size_t)a.plan.tc_ctas; }
+
+cudaError_t launch_tree_tc(const TreeArgs &a, int2 *seg_tab, cudaStream_t st) {
+    const bool e4 = a.cache.dtype == SP_E4M3;
+    const int mt = row_tiles(a);
+    Layout lay;
+    if (!make_layout(a, e4, mt, &lay)) return cudaErrorInvalidValue;
+    CUtensorMap mk, mv;
+    memset(&mk, 0, sizeof mk);
+    memset(&mv, 0, sizeof mv);
+    if (a.cache.kv.layout == SP_KV_PAGED) {
+        const long long blocks = (long long)a.cache.kv.n_pages * a.Hkv;
+        const int P = a.cache.kv.page_size;
+        const bool ok = e4 ? encode_rows_u8(&mk, a.cache.kv.k_pool, blocks * P, P) && encode_rows_u8(&mv, a.cache.kv.v_pool, blocks * P, P)
+                           : encode_kv_pages_bf16(&mk, a.cache.kv.k_pool, blocks, P) &&
+                                 encode_kv_pages_bf16(&mv, a.cache.kv.v_pool, blocks, P);
+        if (!ok) return cudaErrorInvalidValue;
+    }
+    cudaError_t e;
+    if (mt == 2)
+        e = e4 ? run<true, 128, 2>(a, lay, mk, mv, seg_tab, st) : run<false, 128, 2>(a, lay, mk, mv, seg_tab, st);
+    else if (a.rb_rows <= 32)
+        e = e4 ? run<true, 32, 1>(a, lay, mk, mv, seg_tab, st) : run<false, 32, 1>(a, lay, mk, mv, seg_tab, st);
+    else if (a.rb_rows <= 64)
+        e = e4 ? run<true, 64, 1>(a, lay, mk, mv, seg_tab, st) : run<false, 64, 1>(a, lay, mk, mv, seg_tab, st);
+    else
+        e = e4 ? run<true, 128, 1>(a, lay, mk, mv, seg_tab, st) : run<false, 128, 1>(a, lay, mk, mv, seg_tab, st);
+    if (e != cudaSuccess) return e;
+    return launch_k(tree_tc_merge_kernel, dim3(a.Hkv * a.n_rb, a.B, ceil_div(a.rb_rows, MERGE_ROWS)), dim3(MERGE_THREADS), 0, st, a,
+                    (const int2 *)seg_tab);
+}
+
+}  // namespace sp

@@ -241,7 +241,7 @@ def test_constants(name, value):
 
 
 # ---- stream order ------------------------------------------------------------
-FIRST = ["rotate_kernel", "append_kernel", "read_kernel", "tree_simt_kernel"]
+FIRST = ["rotate_kernel", "append_kernel", "read_kernel", "tree_simt_kernel", "tree_tc_kernel"]
 
 
 @pytest.mark.parametrize("name", FIRST)
@@ -250,4 +250,4 @@ def test_a_first_kernel_touches_the_callers_data_after_its_wait(name):
     body = KERNELS[name]
     before = body[:body.index("pdl_wait()")]
     assert body.index("pdl_wait()") < body.index("pdl_trigger()")
-    assert not re.search(r"resolve_seq|tree_nodes|tree_mask|load|a\.pos\[|chunk_of|build_prefix", before)
+    assert not re.search(r"resolve_seq|tree_nodes|tree_mask|load|a\.pos\[|chunk_of|prefix\(", before)
