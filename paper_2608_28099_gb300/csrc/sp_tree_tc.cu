@@ -35,7 +35,7 @@
 // product and added afterwards to the rows that see the node.
 //
 // Warps 0-7: the two softmax warpgroups; then producers (K and V rings: TMA boxes of
-// whole pages, cp.async elsewhere), two MMA issuers (the first owns TMEM) and, for 8-bit
+// whole pages, cp.async elsewhere), the MMA issuer (it owns TMEM) and, for 8-bit
 // caches, four warps that turn V's codes into 16-bit floats and the scales into the
 // softmax's constants.  Every wait is time-limited (SP_DEV_TIMEOUT).
 #include <cudaTypedefs.h>
@@ -73,8 +73,8 @@ struct Layout {
 
 struct Bars {
     uint64_t k_full[MAX_RING], k_empty[MAX_RING], v_full[MAX_RING], v_empty[MAX_RING];
-    uint64_t c_full[CONV], c_empty[CONV];
-    uint64_t s_full[2], p_full[2], pv_done[2], q_full, fin;
+    uint64_t c_full[CONV], c_empty[CONV], c_par[CONV];
+    uint64_t s_full[2], p_full[2], pv_done, q_full, fin;
     unsigned long long vbad[MAX_RING][4];       // nodes with non-finite values, by V slot and warp
     unsigned long long seg_vbad;
     uint32_t tmem;
@@ -87,14 +87,57 @@ constexpr int OFF_CUTS = OFF_L + 2 * 128 * 4;
 constexpr int OFF_FRONT = OFF_CUTS + (MAX_GRP + 4) * 4;
 static_assert(sizeof(Bars) <= OFF_ML, "barrier block");
 
+// Warp roles: softmax 0-7, MMA 8 (9 idle); 8-bit caches: producers 10-11, converters 12-15;
+// else producers 12-15 (10-11 idle).
+constexpr int THREADS = 512;
+constexpr int MMA = 8, CVT = 12;
 template <bool E4>
 struct Roles {
     static constexpr int RING_WARPS = E4 ? 1 : 2;                    // producers of a ring
     static constexpr int RING_THREADS = RING_WARPS * 32;
-    static constexpr int PROD = 8, MMA = PROD + 2 * RING_WARPS, CVT = MMA + 2;
-    static constexpr int WARPS = CVT + (E4 ? 4 : 0);
-    static constexpr int THREADS = WARPS * 32;
+    static constexpr int PROD = E4 ? 10 : 12;
 };
+// One arrival of a warp whose lanes have all done their part.
+__device__ __forceinline__ void arrive_warp(uint64_t *bar, int lane) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar);
+}
+
+// ---- TMEM stores without a wait behind every one ------------------------------
+__device__ __forceinline__ void st16_async(uint32_t addr, const float *v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
+        "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]),
+        "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
+        : "memory");
+}
+__device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void zero16_async(uint32_t addr) {
+    const float z[16] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    st16_async(addr, z);
+}
+
+// ---- two fp32 operations an instruction ----------------------------------------
+__device__ __forceinline__ void fma2(float &d0, float &d1, float a0, float a1, float b0, float b1, float c0, float c1) {
+    asm("{\n\t.reg .b64 a, b, c, d;\n\t"
+        "mov.b64 a, {%2, %3};\n\t"
+        "mov.b64 b, {%4, %5};\n\t"
+        "mov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\t"
+        "mov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d0), "=f"(d1)
+        : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+}
+__device__ __forceinline__ void mul2(float &d0, float &d1, float a0, float a1, float b0, float b1) {
+    asm("{\n\t.reg .b64 a, b, d;\n\t"
+        "mov.b64 a, {%2, %3};\n\t"
+        "mov.b64 b, {%4, %5};\n\t"
+        "mul.rn.f32x2 d, a, b;\n\t"
+        "mov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d0), "=f"(d1)
+        : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
 
 // D[tmem] (+)= A[smem] * B[smem]^T on 8-bit elements (32 of K), issued by one thread.
 __device__ __forceinline__ void mma_e4m3(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
@@ -116,14 +159,8 @@ __device__ __forceinline__ void cp_async4(void *dst, const void *src) {
 __device__ __forceinline__ void expect_tx(uint64_t *bar, uint32_t bytes) {
     asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void tmem_zero16(uint32_t addr) {
-    const float z[16] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    tmem_st16(addr, z);
-}
-
 // The tile list: prefix[b] = tiles of the sequences before b, each sequence's cache id,
 // length and node count.  By all THREADS threads.
-template <int THREADS>
 __device__ __forceinline__ void tree_prefix(const TreeArgs &a, int *prefix, int *sids, int *lens, int *nodes, int *wsum,
                                             int *status) {
     const int B = a.B, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -202,17 +239,39 @@ __device__ __forceinline__ uint32_t pack_half(float a, float b) {
     const __half2 v = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t *>(&v);
 }
+// Codes 2 hi, 2 hi + 1 of a word as two 16-bit floats.
+__device__ __forceinline__ uint32_t codes2_to_half2(uint32_t w, int hi) {
+    uint32_t h;
+    asm("{\n\t.reg .b16 l, u;\n\t"
+        "mov.b32 {l, u}, %1;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %0, l;\n\t}"
+        : "=r"(h)
+        : "r"(hi ? w >> 16 : w));
+    return h;
+}
 // byte offset of 16-byte chunk c (0..7) of row r of an 8-bit tile (128-byte rows, swizzled)
 __device__ __forceinline__ uint32_t off8(int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); }
+
+// y plus the non-finite values, dims d .. d + 3, of the nodes in `left` (out of line: rare).
+__device__ __forceinline__ float4 add_non_finite(const TreeArgs &a, int b, int g, int d, unsigned long long left, float4 y) {
+    for (; left; left &= left - 1) {
+        const bf16 *v = (const bf16 *)a.v_new + ((size_t)b * a.N + (__ffsll(left) - 1)) * a.vs + (size_t)g * DH + d;
+        const float z[4] = {to_f(v[0]), to_f(v[1]), to_f(v[2]), to_f(v[3])};
+        if (!isfinite(z[0])) y.x += z[0];
+        if (!isfinite(z[1])) y.y += z[1];
+        if (!isfinite(z[2])) y.z += z[2];
+        if (!isfinite(z[3])) y.w += z[3];
+    }
+    return y;
+}
 
 // ---------------------------------------------------------------------------
 // TPC: rows of a copy, and tokens of a tile that a copy weighs (32, 64, 128); MT: M tiles.
 template <bool E4, int TPC, int MT>
-__global__ void __launch_bounds__(Roles<E4>::THREADS, 1)
+__global__ void __launch_bounds__(THREADS, 1)
     tree_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                    const __grid_constant__ TreeArgs a, const __grid_constant__ Layout lay, int2 *seg_tab) {
     typedef Roles<E4> Ro;
-    constexpr int THREADS = Ro::THREADS;
     constexpr int NC = 128 / TPC;  // copies
     static_assert(MT == 1 || TPC == 128, "two M tiles hold one copy each");
     extern __shared__ uint8_t smem_raw[];
@@ -231,7 +290,7 @@ __global__ void __launch_bounds__(Roles<E4>::THREADS, 1)
     pdl_wait();
     pdl_trigger();
 
-    tree_prefix<THREADS>(a, prefix, sids, lens, nodes, bars->wsum, blockIdx.x == 0 ? a.status : nullptr);
+    tree_prefix(a, prefix, sids, lens, nodes, bars->wsum, blockIdx.x == 0 ? a.status : nullptr);
     const int T = prefix[B];
     const int n_grp = share_count((int)gridDim.x / Hv, T, B, a.plan.tc_min_tiles);
     const int grp = blockIdx.x / Hv, hv = blockIdx.x - grp * Hv, g = hv / a.n_rb, rb = hv - g * a.n_rb;
@@ -241,22 +300,23 @@ __global__ void __launch_bounds__(Roles<E4>::THREADS, 1)
 #pragma unroll 1
         for (int i = 0; i < lay.nk; ++i) {
             mbar_init(&bars->k_full[i], Ro::RING_THREADS);
-            mbar_init(&bars->k_empty[i], MT);
+            mbar_init(&bars->k_empty[i], 1);
         }
 #pragma unroll 1
         for (int i = 0; i < lay.nv; ++i) {
             mbar_init(&bars->v_full[i], Ro::RING_THREADS);
-            mbar_init(&bars->v_empty[i], E4 ? 128 : MT);
+            mbar_init(&bars->v_empty[i], E4 ? 4 : 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&bars->c_full[i], 128);
-            mbar_init(&bars->c_empty[i], MT);
+            mbar_init(&bars->c_full[i], 4);
+            mbar_init(&bars->c_par[i], 4);
+            mbar_init(&bars->c_empty[i], 1);
             mbar_init(&bars->s_full[i], 1);
-            mbar_init(&bars->p_full[i], 128);
-            mbar_init(&bars->pv_done[i], 1);
+            mbar_init(&bars->p_full[i], 4);
         }
-        mbar_init(&bars->q_full, SOFT);
-        mbar_init(&bars->fin, 2);
+        mbar_init(&bars->q_full, SOFT / 32);
+        mbar_init(&bars->pv_done, 1);
+        mbar_init(&bars->fin, 1);
         bars->abort = 0;
         fence_mbar_init();
         if (paged) {
@@ -264,7 +324,7 @@ __global__ void __launch_bounds__(Roles<E4>::THREADS, 1)
             prefetch_tmap(&map_v);
         }
     }
-    if (warp == Ro::MMA) {
+    if (warp == MMA) {
         tmem_alloc(&bars->tmem, 512);
         tmem_relinquish();
     }
@@ -281,393 +341,7 @@ __global__ void __launch_bounds__(Roles<E4>::THREADS, 1)
         }
     }
 
-    if (warp >= Ro::PROD && warp < Ro::MMA) {
-        // ------------------------------------------------------------ producers
-        constexpr int PT = Ro::RING_THREADS, ES = E4 ? 1 : 2, CH = DH * ES / 16;  // chunks a row
-        const bool is_v = (warp - Ro::PROD) & 1;
-        const int pidx = (warp - Ro::PROD) >> 1, ptid = pidx * 32 + lane;
-        const bool lead = pidx == 0;
-        uint64_t *full = is_v ? bars->v_full : bars->k_full, *empty = is_v ? bars->v_empty : bars->k_empty;
-        const int slot_bytes = E4 ? SLOT8 + (is_v ? SCALES : 0) : SLOT16;
-        uint8_t *ring = smem + (is_v ? lay.off_v : lay.off_k);
-        const CUtensorMap *map = is_v ? &map_v : &map_k;
-        const uint8_t *pool = (const uint8_t *)(is_v ? a.cache.kv.v_pool : a.cache.kv.k_pool);
-        const bf16 *fresh = (const bf16 *)(is_v ? a.v_new : a.k_new);
-        const long long fs = is_v ? a.vs : a.ks;
-        const uint64_t pol = policy_evict_first();
-        auto dst_off = [](int r, int c) { return E4 ? off8(r, c) : kv_off(r, c); };
-        Ring rg(is_v ? lay.nv : lay.nk);
-        int bad = 0, filled = 0;
-        bool stop = false;
-#pragma unroll 1
-        for (int x = x0; x < x1 && !stop;) {
-            const Seg sg = seg_at(prefix, B, x, x1);
-            x += sg.n;
-            const int b = sg.b, sid = sids[b], L = lens[b];
-            // a contiguous sequence's rows: Hkv rows a token
-            const uint8_t *seq = nullptr;
-            const float *seq_scale[2] = {nullptr, nullptr};
-            if (!paged && L > 0) {
-                seq = (const uint8_t *)(is_v ? a.cache.kv.v_seq : a.cache.kv.k_seq)[sid];
-                if (E4 && is_v) {
-                    seq_scale[0] = ((const float *const *)a.cache.k_scale)[sid];
-                    seq_scale[1] = ((const float *const *)a.cache.v_scale)[sid];
-                }
-            }
-#pragma unroll 1
-            for (int i = 0; i < sg.n; ++i) {
-                const int t = sg.t_a + i, t0 = t * TILE;
-                const bool is_fresh = t == sg.nt - 1;
-                const int n_tok = is_fresh ? 0 : min(TILE, L - t0);
-                const int n_pg = paged ? n_tok / P : 0;  // whole pages
-                int page = -1;                           // page ids (up to eight), asked for before the wait
-                if (paged && lane * P < n_tok) {
-                    const int lp = t0 / P + lane;
-                    page = lp < a.cache.kv.max_pages ? a.cache.kv.page_table[(size_t)sid * a.cache.kv.max_pages + lp] : -1;
-                    if (page < 0 || page >= a.cache.kv.n_pages) page = -1, bad = 1;
-                }
-                // warp-uniform verdict: the collectives below need every lane
-                if (!mbar_wait_warp(&empty[rg.slot], rg.ph ^ 1, abort)) {
-                    stop = true;
-                    break;
-                }
-                uint8_t *dst = ring + rg.slot * slot_bytes;
-                uint8_t *sc = dst + SLOT8;  // (E4 && is_v)
-                bool plain = false;         // this thread wrote shared memory or issued cp.async
-                if (n_pg > 0 && lead) {
-                    const bool ok = lane < n_pg && page >= 0;
-                    const unsigned okm = __ballot_sync(0xffffffffu, ok);
-                    const uint32_t bytes = (uint32_t)(P * DH * ES + (E4 && is_v ? P * 8 : 0));
-                    if (lane == 0 && okm) expect_tx(&full[rg.slot], __popc(okm) * bytes);
-                    __syncwarp();
-                    if (ok) {  // the cache is read once: evict-first keeps queries and partials in L2
-                        const int row = page * Hkv + g;
-                        if constexpr (E4) {
-                            tma_load_2d_hint(dst + lane * P * DH, map, &full[rg.slot], 0, row * P, pol);
-                            if (is_v) {
-                                const size_t at = (size_t)row * P;
-                                bulk_load(sc + lane * P * 4, (const float *)a.cache.k_scale + at, P * 4, &full[rg.slot]);
-                                bulk_load(sc + TILE * 4 + lane * P * 4, (const float *)a.cache.v_scale + at, P * 4,
-                                          &full[rg.slot]);
-                            }
-                        } else {
-                            tma_load_4d_hint(dst + lane * P * 256, map, &full[rg.slot], 0, 0, 0, row * (P / 8), pol);
-                        }
-                    }
-                    // a page outside the pool: zeros
-#pragma unroll 1
-                    for (unsigned miss = ~okm & ((1u << n_pg) - 1u); miss; miss &= miss - 1) {
-                        const int j = __ffs(miss) - 1;
-#pragma unroll 1
-                        for (int e = lane; e < P * CH; e += 32) st_shared_v4(dst + j * P * DH * ES + e * 16, 0, 0, 0, 0);
-                        if (E4 && is_v && lane < P / 4) {
-                            st_shared_v4(sc + j * P * 4 + lane * 16, 0, 0, 0, 0);
-                            st_shared_v4(sc + TILE * 4 + j * P * 4 + lane * 16, 0, 0, 0, 0);
-                        }
-                        plain = true;
-                    }
-                }
-                if (!is_fresh) {
-                    const int r0 = n_pg * (paged ? P : 0);  // first row not covered by TMA
-                    if (r0 < n_tok) {
-                        plain = true;
-                        if (paged) {  // the last, partial page
-                            const int pg = __shfl_sync(0xffffffffu, page, n_pg);
-                            const size_t at = ((size_t)max(pg, 0) * Hkv + g) * P;
-#pragma unroll 1
-                            for (int idx = ptid; idx < (n_tok - r0) * CH; idx += PT) {
-                                const int r = idx / CH, c = idx - r * CH;
-                                if (pg >= 0) cp_async16(dst + dst_off(r0 + r, c), pool + (at + r) * (DH * ES) + c * 16);
-                                else st_shared_v4(dst + dst_off(r0 + r, c), 0, 0, 0, 0);
-                            }
-                            if (E4 && is_v) {
-#pragma unroll 1
-                                for (int r = ptid; r < n_tok - r0; r += PT) {
-                                    if (pg >= 0) {
-                                        cp_async4(sc + (r0 + r) * 4, (const float *)a.cache.k_scale + at + r);
-                                        cp_async4(sc + (TILE + r0 + r) * 4, (const float *)a.cache.v_scale + at + r);
-                                    } else {
-                                        *(float *)(sc + (r0 + r) * 4) = 0.f;
-                                        *(float *)(sc + (TILE + r0 + r) * 4) = 0.f;
-                                    }
-                                }
-                            }
-                        } else {
-                            const uint8_t *src = seq + ((size_t)t0 * Hkv + g) * (DH * ES);
-#pragma unroll 4
-                            for (int idx = ptid; idx < n_tok * CH; idx += PT) {
-                                const int r = idx / CH, c = idx - r * CH;
-                                cp_async16(dst + dst_off(r, c), src + (size_t)r * Hkv * (DH * ES) + c * 16);
-                            }
-                            if (E4 && is_v) {
-#pragma unroll 1
-                                for (int r = ptid; r < n_tok; r += PT) {
-                                    const size_t at = (size_t)(t0 + r) * Hkv + g;
-                                    cp_async4(sc + r * 4, seq_scale[0] + at);
-                                    cp_async4(sc + (TILE + r) * 4, seq_scale[1] + at);
-                                }
-                            }
-                        }
-                    }
-                    // values past the end are multiplied by weights of 0: they must be
-                    // finite (keys there give scores that are replaced)
-                    if (!E4 && is_v && n_tok < TILE) {
-                        plain = true;
-#pragma unroll 1
-                        for (int idx = ptid; idx < (TILE - n_tok) * CH; idx += PT)
-                            st_shared_v4(dst + kv_off(n_tok + idx / CH, idx % CH), 0, 0, 0, 0);
-                    }
-                } else if (!E4 || !is_v) {
-                    // the nodes' rows: 16 lanes a row, 8 elements a lane
-                    plain = true;
-                    const int n = nodes[b], c = lane & 15;
-                    unsigned long long vb = 0;
-#pragma unroll 2
-                    for (int r = pidx * 2 + (lane >> 4); r < 64; r += 2 * Ro::RING_WARPS) {
-                        uint4 u = make_uint4(0, 0, 0, 0);
-                        if (r < n) u = *(const uint4 *)(fresh + ((size_t)b * a.N + r) * fs + (size_t)g * DH + c * 8);
-                        if constexpr (!E4) {
-                            if (is_v) {
-                                uint32_t w[4] = {u.x, u.y, u.z, u.w};
-                                bool odd = false;
-#pragma unroll
-                                for (int q = 0; q < 4; ++q) {
-                                    const bool lo = (w[q] & 0x7f80u) == 0x7f80u, hi = (w[q] & 0x7f800000u) == 0x7f800000u;
-                                    odd = odd || lo || hi;
-                                    w[q] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
-                                }
-                                u = make_uint4(w[0], w[1], w[2], w[3]);
-                                const unsigned o = __ballot_sync(0xffffffffu, odd);
-                                const int even = r & ~1;  // (lanes 0-15 hold the even row)
-                                if (o & 0xffffu) vb |= 1ull << even;
-                                if (o >> 16) vb |= 2ull << even;
-                            }
-                            st_shared_v4(dst + kv_off(r, c), u.x, u.y, u.z, u.w);
-                        } else {
-                            // keys as two 8-bit parts, rows r and 64 + r
-                            float v[8];
-                            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-                            float amax = 0.f;
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                v[2 * q] = __uint_as_float(w[q] << 16);
-                                v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
-                                amax = fmaxf(amax, fmaxf(fabsf(v[2 * q]), fabsf(v[2 * q + 1])));
-                            }
-#pragma unroll
-                            for (int o = 1; o < 16; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-                            int k;
-                            const float f = pow2_scale(amax, &k);
-#pragma unroll
-                            for (int q = 0; q < 8; ++q) v[q] *= f;
-                            uint2 hi, lo;
-                            split_codes(v, &hi, &lo);
-                            *(uint2 *)(dst + off8(r, c >> 1) + (c & 1) * 8) = hi;
-                            *(uint2 *)(dst + off8(64 + r, c >> 1) + (c & 1) * 8) = lo;
-                        }
-                    }
-                    if (!E4 && is_v && lane == 0) bars->vbad[rg.slot][pidx] = vb;
-                }
-                if (plain) {
-                    fence_proxy_async();  // this thread's shared-memory stores
-                    cp_async_mbar_arrive(&full[rg.slot]);
-                } else {
-                    mbar_arrive(&full[rg.slot]);
-                }
-                ++filled;
-                rg.next();
-            }
-        }
-        asm volatile("cp.async.wait_all;" ::: "memory");  // nothing lands after the CTA is gone
-        if (lead && lane == 0) {
-            // drain TMA writes still in flight (only possible after an abort)
-            Ring rd(rg.n);
-#pragma unroll 1
-            for (int j = 0; j < filled; ++j, rd.next())
-                if (j + rg.n >= filled) mbar_wait_drain(&full[rd.slot], rd.ph);
-        }
-        bad = __any_sync(0xffffffffu, bad);
-        if (bad && lane == 0 && a.status) atomicOr(a.status, SP_DEV_BAD_PAGE);
-    } else if (E4 && warp >= Ro::CVT) {
-        // ------------------------------------------------------------ V codes -> 16-bit floats
-        const int ct = threadIdx.x - Ro::CVT * 32, cw = warp - Ro::CVT;
-        Ring rv(lay.nv), rc(CONV);
-        bool ok = true;
-#pragma unroll 1
-        for (int x = x0; ok && x < x1;) {
-            const Seg sg = seg_at(prefix, B, x, x1);
-            x += sg.n;
-            const int b = sg.b, L = lens[b];
-#pragma unroll 1
-            for (int i = 0; i < sg.n; ++i) {
-                const int t = sg.t_a + i;
-                const bool is_fresh = t == sg.nt - 1;
-                const int n_tok = is_fresh ? 0 : min(TILE, L - t * TILE);
-                ok = mbar_wait_warp(&bars->v_full[rv.slot], rv.ph, abort) &&
-                     mbar_wait_warp(&bars->c_empty[rc.slot], rc.ph ^ 1, abort);
-                if (!ok) break;
-                const uint8_t *src = smem + lay.off_v + rv.slot * (SLOT8 + SCALES);
-                uint8_t *dst = smem + lay.off_c + rc.slot * SLOT16;
-                float *par = (float *)(smem + lay.off_c + CONV * SLOT16 + rc.slot * PARAMS);
-                if (!is_fresh) {
-#pragma unroll 4
-                    for (int idx = ct; idx < TILE * 8; idx += 128) {
-                        const int r = idx >> 3, c = idx & 7;
-                        uint4 u = make_uint4(0, 0, 0, 0);
-                        if (r < n_tok) u = *(const uint4 *)(src + off8(r, c));
-                        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-                        uint32_t h[8];
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) {
-                            const __half2_raw f = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[q >> 1] >> (16 * (q & 1))),
-                                                                             __NV_E4M3);
-                            h[q] = (uint32_t)f.x | (uint32_t)f.y << 16;
-                        }
-                        st_shared_v4(dst + kv_off(r, 2 * c), h[0], h[1], h[2], h[3]);
-                        st_shared_v4(dst + kv_off(r, 2 * c + 1), h[4], h[5], h[6], h[7]);
-                    }
-                    float ks = 0.f, vs = 1.f;
-                    if (ct < n_tok) {
-                        ks = ((const float *)(src + SLOT8))[ct];
-                        vs = fmaxf(((const float *)(src + SLOT8))[TILE + ct], 7.888609052210118e-31f);  // 2^-100
-                    }
-                    par[2 * ct] = ks * a.scale_log2;
-                    par[2 * ct + 1] = __log2f(vs);
-                    par[2 * TILE + ct] = 1.f / vs;
-                } else {
-                    const int n = nodes[b], c = lane & 15;
-                    unsigned long long vb = 0;
-#pragma unroll 1
-                    for (int r = cw * 2 + (lane >> 4); r < TILE; r += 8) {
-                        uint4 uk = make_uint4(0, 0, 0, 0), uv = uk;
-                        if (r < n) {
-                            const size_t row = (size_t)b * a.N + r;
-                            uk = *(const uint4 *)((const bf16 *)a.k_new + row * a.ks + (size_t)g * DH + c * 8);
-                            uv = *(const uint4 *)((const bf16 *)a.v_new + row * a.vs + (size_t)g * DH + c * 8);
-                        }
-                        const uint32_t wk[4] = {uk.x, uk.y, uk.z, uk.w}, wv[4] = {uv.x, uv.y, uv.z, uv.w};
-                        float v[8], amk = 0.f, amv = 0.f;
-                        bool odd = false;
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            amk = fmaxf(amk, fmaxf(fabsf(__uint_as_float(wk[q] << 16)), fabsf(__uint_as_float(wk[q] & 0xffff0000u))));
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const float y = __uint_as_float(e ? wv[q] & 0xffff0000u : wv[q] << 16);
-                                const bool fin = isfinite(y);
-                                odd = odd || !fin;
-                                v[2 * q + e] = fin ? y : 0.f;
-                                amv = fmaxf(amv, fabsf(v[2 * q + e]));
-                            }
-                        }
-#pragma unroll
-                        for (int o = 1; o < 16; o <<= 1) {
-                            amk = fmaxf(amk, __shfl_xor_sync(0xffffffffu, amk, o));
-                            amv = fmaxf(amv, __shfl_xor_sync(0xffffffffu, amv, o));
-                        }
-                        const unsigned o = __ballot_sync(0xffffffffu, odd);
-                        if (r < 64) {
-                            if (o & 0xffffu) vb |= 1ull << (r & ~1);
-                            if (o >> 16) vb |= 2ull << (r & ~1);
-                        }
-                        int kk, kv;
-                        pow2_scale(amk, &kk);
-                        const float f = pow2_scale(amv, &kv);
-                        st_shared_v4(dst + kv_off(r, c), pack_half(v[0] * f, v[1] * f), pack_half(v[2] * f, v[3] * f),
-                                     pack_half(v[4] * f, v[5] * f), pack_half(v[6] * f, v[7] * f));
-                        if (c == 0) {
-                            // an infinite key saturates in its parts: its scores are NaN
-                            par[2 * r] = pow2i(-kk) * a.scale_log2 + (amk - amk);
-                            par[2 * r + 1] = (float)-kv;
-                            par[2 * TILE + r] = pow2i(kv);
-                        }
-                    }
-                    if (lane == 0) bars->vbad[rc.slot][cw] = vb;
-                }
-                fence_proxy_async();
-                mbar_arrive(&bars->c_full[rc.slot]);
-                mbar_arrive(&bars->v_empty[rv.slot]);
-                rv.next();
-                rc.next();
-            }
-        }
-    } else if (warp >= Ro::MMA && warp < Ro::CVT) {
-        // ------------------------------------------------------------ MMA issue
-        // Pipeline w: S of its next tile, then (its softmax done) PV.  Both by the whole
-        // warp, the instructions under `on` (see elect_one).
-        const int w = warp - Ro::MMA;
-        const bool on = elect_one();
-        constexpr uint32_t idesc_s = E4 ? (1u << 4) | ((uint32_t)(TILE >> 3) << 17) | (8u << 24) : idesc_bf16_f32(128, TILE);
-        // 16-bit floats: format bits 0 instead of bf16's 1
-        constexpr uint32_t idesc_o = E4 ? (1u << 4) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | (8u << 24)
-                                        : idesc_bf16_f32_bmn(128, DH);
-        const uint32_t s_tmem = tmem + (uint32_t)(w * 128), o_tmem = tmem + O_COL + (uint32_t)(w * DH);
-        const uint64_t dq = sw128_kmajor_desc(smem + lay.off_q + (MT == 2 ? w * Q_TILE : 0));
-        const uint64_t dk0 = sw128_kmajor_desc_sbo(smem + lay.off_k, E4 ? 1024 : GROUP_STRIDE);
-        const uint64_t dv0 = sw128_mnmajor_desc2(smem + (E4 ? lay.off_c : lay.off_v), HALF_STRIDE, GROUP_STRIDE);
-        uint64_t *vf = E4 ? bars->c_full : bars->v_full, *ve = E4 ? bars->c_empty : bars->v_empty;
-        Ring rk(lay.nk), rv(E4 ? CONV : lay.nv);
-        bool ok = true;
-        uint32_t kp = 0;
-        int j = 0;
-#pragma unroll 1
-        for (int x = x0; ok && x < x1; ++j) {
-            const Seg sg = seg_at(prefix, B, x, x1);
-            x += sg.n;
-            const int n_seg = __shfl_sync(0xffffffffu, sg.n, 0), t_a = __shfl_sync(0xffffffffu, sg.t_a, 0),
-                      nt = __shfl_sync(0xffffffffu, sg.nt, 0);
-            if (!mbar_wait_warp(&bars->q_full, (uint32_t)(j & 1), abort)) break;
-            bool first = true;
-#pragma unroll 1
-            for (int i = 0; i < n_seg; ++i, rk.next(), rv.next()) {
-                if (MT == 1 && (i & 1) != w) continue;  // the other pipeline's tile
-                ok = mbar_wait_warp(&bars->k_full[rk.slot], rk.ph, abort);
-                if (!ok) break;
-                tc_fence_after();
-                fence_proxy_async();  // cp.async data -> tensor-core reads
-                const uint64_t dk = dk0 + (uint32_t)(rk.slot * ((E4 ? SLOT8 : SLOT16) >> 4));
-                if (on) {
-                    if constexpr (E4) {
-#pragma unroll
-                        for (int kk = 0; kk < 8; ++kk)  // part kk / 4, 32 dims each
-                            mma_e4m3(s_tmem, dq + (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2), dk + (uint64_t)((kk & 3) * 2),
-                                     idesc_s, kk > 0);
-                    } else {
-#pragma unroll
-                        for (int kk = 0; kk < 8; ++kk)  // 16 dims: 32 B of a row of dim half kk / 4
-                            mma_bf16(s_tmem, dq + (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2),
-                                     dk + (uint64_t)((kk >> 2) * (HALF_STRIDE >> 4) + (kk & 3) * 2), idesc_s, kk > 0);
-                    }
-                    mma_commit(&bars->k_empty[rk.slot]);
-                    mma_commit(&bars->s_full[w]);
-                }
-                __syncwarp();
-                const bool is_fresh = t_a + i == nt - 1;
-                ok = mbar_wait_warp(&vf[rv.slot], rv.ph, abort) && mbar_wait_warp(&bars->p_full[w], kp, abort);
-                if (!ok) break;
-                kp ^= 1;
-                tc_fence_after();
-                fence_proxy_async();
-                const uint64_t dv = dv0 + (uint32_t)(rv.slot * (SLOT16 >> 4));
-                if (on) {
-#pragma unroll
-                    for (int kk = 0; kk < 8; ++kk)  // 16 tokens: 8 columns of P, two 8-token groups of V
-                        if (kk < 4 || !is_fresh)  // (at most 64 nodes)
-                            mma_bf16_ts(o_tmem, s_tmem + (uint32_t)(kk * 8), dv + (uint64_t)(kk * (2 * GROUP_STRIDE >> 4)),
-                                        idesc_o, !first || kk > 0);
-                    mma_commit(&ve[rv.slot]);
-                }
-                __syncwarp();
-                first = false;
-            }
-            // (without a tile of its own too: no segment's queries may be replaced before
-            // both issuers have passed them)
-            if (on && ok) mma_commit(&bars->pv_done[w]);
-            __syncwarp();
-        }
-        if (on) mma_commit(&bars->fin);  // completes when every MMA of this issuer is done
-        __syncwarp();
-    } else if (warp < 8) {
+    if (warp < 8) {
         // ------------------------------------------------------------ softmax + epilogue
         const int wg = warp >> 2, ln = threadIdx.x & 127;  // pipeline; TMEM lane
         const int cp = ln / TPC, row_t = ln - cp * TPC;    // copy, row of the M tile
@@ -681,7 +355,6 @@ __global__ void __launch_bounds__(Roles<E4>::THREADS, 1)
         bool ok = true;
         uint32_t ks_ph = 0, pv_ph = 0;
         Ring rv(E4 ? CONV : lay.nv);
-        uint64_t *vf = E4 ? bars->c_full : bars->v_full;
 #pragma unroll 1
         for (int x = x0; x < x1;) {
             const Seg sg = seg_at(prefix, B, x, x1);
@@ -736,7 +409,7 @@ __global__ void __launch_bounds__(Roles<E4>::THREADS, 1)
                     }
                 }
                 fence_proxy_async();
-                mbar_arrive(&bars->q_full);
+                arrive_warp(&bars->q_full, lane);
             }
             // ---- tiles
             float m = -INFINITY, l = 0.f;
@@ -750,7 +423,9 @@ __global__ void __launch_bounds__(Roles<E4>::THREADS, 1)
                 const int n_tok = is_fresh ? 0 : min(TILE, L - t * TILE);
                 // warp-uniform verdicts: the TMEM loads and stores are warp-collective
                 ok = ok && mbar_wait_warp(&bars->s_full[wg], ks_ph, abort);
-                if (E4 || is_fresh) ok = ok && mbar_wait_warp(&vf[rv.slot], rv.ph, abort);
+                // (8-bit: the tile's constants; the nodes' tile: which nodes are not finite)
+                if constexpr (E4) ok = ok && mbar_wait_warp(&bars->c_par[rv.slot], rv.ph, abort);
+                else if (is_fresh) ok = ok && mbar_wait_warp(&bars->v_full[rv.slot], rv.ph, abort);
                 ks_ph ^= 1;
                 if (!ok) continue;
                 tc_fence_after();
@@ -759,20 +434,19 @@ __global__ void __launch_bounds__(Roles<E4>::THREADS, 1)
                     for (int w = 0; w < (E4 ? 4 : 2); ++w) vb |= ((volatile unsigned long long *)bars->vbad[rv.slot])[w];
                 }
                 if (!warp_active) {  // its lanes' weights reach no row that is used
-                    mbar_arrive(&bars->p_full[wg]);
+                    arrive_warp(&bars->p_full[wg], lane);
                     first = false;
                     continue;
                 }
                 const float *par = (const float *)(smem + lay.off_c + CONV * SLOT16 + rv.slot * PARAMS);
                 const bool masked = is_fresh || n_tok < TILE;
-                constexpr int CH = TPC < 32 ? TPC : 32, N_CH = TPC / CH;
+                constexpr int CH = 32, N_CH = TPC / CH;  // columns in registers at a time
                 const int tok0 = cp * TPC;  // this copy's first token
-                // scores of chunk c in log2 units, with log2 of the value's scale (8-bit)
-                auto scores = [&](int c, float (&s)[CH]) {
-                    const int j0 = tok0 + c * CH;
+                // Columns [j0, j0 + CH) of S; 8-bit: in log2 units, with log2 of the value's scale.
+                auto scores = [&](int j0, float (&s)[CH]) {
                     tmem_ld32(s_col + (uint32_t)j0, s);
                     if constexpr (E4) {
-                        if (is_fresh && j0 < 64) {  // warp-uniform (a copy is whole warps)
+                        if (is_fresh && j0 < 64) {  // the keys' second parts
                             float s2[CH];
                             tmem_ld32(s_col + (uint32_t)(64 + j0), s2);
 #pragma unroll
@@ -781,12 +455,9 @@ __global__ void __launch_bounds__(Roles<E4>::THREADS, 1)
 #pragma unroll
                         for (int e = 0; e < CH; e += 2) {
                             const float4 p2 = *(const float4 *)(par + 2 * (j0 + e));
-                            s[e] = fmaf(s[e] * rs, p2.x, p2.y);
-                            s[e + 1] = fmaf(s[e + 1] * rs, p2.z, p2.w);
+                            mul2(s[e], s[e + 1], s[e], s[e + 1], rs, rs);
+                            fma2(s[e], s[e + 1], s[e], s[e + 1], p2.x, p2.z, p2.y, p2.w);
                         }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < CH; ++e) s[e] *= a.scale_log2;
                     }
                     if (masked) {
                         const uint32_t bits = is_fresh ? (j0 < 64 ? (uint32_t)(sees >> j0) : 0u)
@@ -796,19 +467,28 @@ __global__ void __launch_bounds__(Roles<E4>::THREADS, 1)
                             if (!((bits >> e) & 1)) s[e] = -INFINITY;
                     }
                 };
+                float s[CH];
                 float mt = -INFINITY;
-                float sv[TPC <= 64 ? N_CH : 1][CH];  // (up to 64 tokens stay in registers)
 #pragma unroll
                 for (int c = 0; c < N_CH; ++c) {
-                    float(&s)[CH] = sv[TPC <= 64 ? c : 0];
-                    scores(c, s);
+                    scores(tok0 + c * CH, s);
                     float mx[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) mx[e] = fmaxf(fmaxf(s[e], s[e + 8]), fmaxf(s[e + 16], s[e + 24]));
+                    for (int e = 0; e < 8; ++e) mx[e] = s[e];
+#pragma unroll
+                    for (int h = 8; h < CH; h += 8)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) mx[e] = fmaxf(mx[e], s[h + e]);
                     mt = fmaxf(mt, fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])),
                                          fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7]))));
-                    if constexpr (TPC > 64) tmem_st32(s_col + (uint32_t)(c * CH), s);
+                    // more than fits the registers: scores go back to where they came from
+                    if (N_CH > 1 && (E4 || masked)) {
+#pragma unroll
+                        for (int h = 0; h < CH; h += 16) st16_async(s_col + (uint32_t)(tok0 + c * CH + h), s + h);
+                        st_wait();
+                    }
                 }
+                if constexpr (!E4) mt *= a.scale_log2;
                 const bool grow = mt > m + RESCALE_LOG2 || (m == -INFINITY && mt != -INFINITY);
                 const float m_new = grow ? mt : m;
                 const float alpha = grow ? (m == -INFINITY ? 0.f : fast_exp2(m - m_new)) : 1.f;
@@ -820,8 +500,10 @@ __global__ void __launch_bounds__(Roles<E4>::THREADS, 1)
                         tmem_ld32(o_col + c0, o);
 #pragma unroll
                         for (int e = 0; e < 32; ++e) o[e] *= alpha;
-                        tmem_st32(o_col + c0, o);
+                        st16_async(o_col + c0, o);
+                        st16_async(o_col + c0 + 16, o + 16);
                     }
+                    st_wait();
                 }
                 l *= alpha;
                 m = m_new;
@@ -830,41 +512,45 @@ __global__ void __launch_bounds__(Roles<E4>::THREADS, 1)
                 float ps[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int c = 0; c < N_CH; ++c) {
-                    float(&s)[CH] = sv[TPC <= 64 ? c : 0];
-                    if constexpr (TPC > 64) tmem_ld32(s_col + (uint32_t)(c * CH), s);
+                    if constexpr (N_CH > 1) tmem_ld32(s_col + (uint32_t)(tok0 + c * CH), s);
                     float pk[CH / 2];
 #pragma unroll
                     for (int e = 0; e < CH; e += 4) {
                         float w[4];
 #pragma unroll
-                        for (int q4 = 0; q4 < 4; ++q4) w[q4] = fast_exp2(s[e + q4] - mu);
+                        for (int q = 0; q < 4; q += 2) {
+                            if constexpr (E4) add2(w[q], w[q + 1], s[e + q], s[e + q + 1], -mu, -mu);
+                            else fma2(w[q], w[q + 1], s[e + q], s[e + q + 1], a.scale_log2, a.scale_log2, -mu, -mu);
+                            w[q] = fast_exp2(w[q]);
+                            w[q + 1] = fast_exp2(w[q + 1]);
+                        }
                         if constexpr (E4) {
                             const float4 iv = *(const float4 *)(par + 2 * TILE + tok0 + c * CH + e);
-                            ps[0] = fmaf(w[0], iv.x, ps[0]);
-                            ps[1] = fmaf(w[1], iv.y, ps[1]);
-                            ps[2] = fmaf(w[2], iv.z, ps[2]);
-                            ps[3] = fmaf(w[3], iv.w, ps[3]);
+                            fma2(ps[0], ps[1], w[0], w[1], iv.x, iv.y, ps[0], ps[1]);
+                            fma2(ps[2], ps[3], w[2], w[3], iv.z, iv.w, ps[2], ps[3]);
                             pk[e / 2] = __uint_as_float(pack_half(w[0], w[1]));
                             pk[e / 2 + 1] = __uint_as_float(pack_half(w[2], w[3]));
                         } else {
-#pragma unroll
-                            for (int q4 = 0; q4 < 4; ++q4) ps[q4] += w[q4];
+                            add2(ps[0], ps[1], ps[0], ps[1], w[0], w[1]);
+                            add2(ps[2], ps[3], ps[2], ps[3], w[2], w[3]);
                             pk[e / 2] = __uint_as_float(pack_bf16(w[0], w[1]));
                             pk[e / 2 + 1] = __uint_as_float(pack_bf16(w[2], w[3]));
                         }
                     }
                     // P over S's first half, whose scores this warp has read (chunk c covers
                     // columns of chunks <= c only)
-                    tmem_st16(s_col + (uint32_t)((tok0 + c * CH) / 2), pk);
+#pragma unroll
+                    for (int h = 0; h < CH / 2; h += 16) st16_async(s_col + (uint32_t)((tok0 + c * CH) / 2 + h), pk + h);
                 }
                 if constexpr (NC > 1) {  // the other copies' tokens
 #pragma unroll
                     for (int z = 0; z < 4; ++z)
-                        if (z * 16 < tok0 / 2 || z * 16 >= (tok0 + TPC) / 2) tmem_zero16(s_col + (uint32_t)(z * 16));
+                        if (z * 16 < tok0 / 2 || z * 16 >= (tok0 + TPC) / 2) zero16_async(s_col + (uint32_t)(z * 16));
                 }
+                st_wait();
                 l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
                 tc_fence_before();
-                mbar_arrive(&bars->p_full[wg]);
+                arrive_warp(&bars->p_full[wg], lane);
             }
 
             // ---- epilogue: the pipelines' (one M tile) and copies' parts of each row are
@@ -903,7 +589,7 @@ __global__ void __launch_bounds__(Roles<E4>::THREADS, 1)
                     a1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - mu);
                 }
             }
-            ok = ok && mbar_wait_warp(&bars->pv_done[0], pv_ph, abort) && mbar_wait_warp(&bars->pv_done[1], pv_ph, abort);
+            ok = ok && mbar_wait_warp(&bars->pv_done, pv_ph, abort);
             pv_ph ^= 1;
             tc_fence_after();
             // slot of this segment's partial: a share has at most two, the pair that starts
@@ -913,17 +599,7 @@ __global__ void __launch_bounds__(Roles<E4>::THREADS, 1)
             // four dims of row q of the block: y unnormalised
             auto write = [&](int q, int d, float4 y, float scale) {
                 const int qr = rb * a.rb_rows + q, nd = qr / a.G;
-                if (seg_vb && has_fresh && nd < n) {
-                    for (unsigned long long left = seg_vb & tree_mask(a, b, nd, n); left; left &= left - 1) {
-                        const bf16 *v = (const bf16 *)a.v_new + ((size_t)b * a.N + (__ffsll(left) - 1)) * a.vs + (size_t)g * DH + d;
-                        float *yy = &y.x;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float z = to_f(v[e]);
-                            if (!isfinite(z)) yy[e] += z;
-                        }
-                    }
-                }
+                if (seg_vb && has_fresh && nd < n) y = add_non_finite(a, b, g, d, seg_vb & tree_mask(a, b, nd, n), y);
                 if (whole) {
                     const bool on = nd < n && scale != 0.f;
                     const size_t at = ((size_t)b * a.N + nd) * a.Hq * DH + (size_t)(g * a.G + qr - nd * a.G) * DH + d;
@@ -990,13 +666,409 @@ __global__ void __launch_bounds__(Roles<E4>::THREADS, 1)
             tc_fence_before();
             named_sync(BAR_EPI, SOFT);  // O, the queries' buffer and ml_s are free
         }
+    } else {
+        if (warp >= Ro::PROD && warp < Ro::PROD + 2 * Ro::RING_WARPS) {
+            // ------------------------------------------------------------ producers
+            constexpr int PT = Ro::RING_THREADS, ES = E4 ? 1 : 2, CH = DH * ES / 16;  // chunks a row
+            const bool is_v = (warp - Ro::PROD) & 1;
+            const int pidx = (warp - Ro::PROD) >> 1, ptid = pidx * 32 + lane;
+            const bool lead = pidx == 0;
+            uint64_t *full = is_v ? bars->v_full : bars->k_full, *empty = is_v ? bars->v_empty : bars->k_empty;
+            const int slot_bytes = E4 ? SLOT8 + (is_v ? SCALES : 0) : SLOT16;
+            uint8_t *ring = smem + (is_v ? lay.off_v : lay.off_k);
+            const CUtensorMap *map = is_v ? &map_v : &map_k;
+            const uint8_t *pool = (const uint8_t *)(is_v ? a.cache.kv.v_pool : a.cache.kv.k_pool);
+            const bf16 *fresh = (const bf16 *)(is_v ? a.v_new : a.k_new);
+            const long long fs = is_v ? a.vs : a.ks;
+            const uint64_t pol = policy_evict_first();
+            auto dst_off = [](int r, int c) { return E4 ? off8(r, c) : kv_off(r, c); };
+            Ring rg(is_v ? lay.nv : lay.nk);
+            int bad = 0, filled = 0;
+            bool stop = false;
+#pragma unroll 1
+            for (int x = x0; x < x1 && !stop;) {
+                const Seg sg = seg_at(prefix, B, x, x1);
+                x += sg.n;
+                const int b = sg.b, sid = sids[b], L = lens[b];
+                // a contiguous sequence's rows: Hkv rows a token
+                const uint8_t *seq = nullptr;
+                const float *seq_scale[2] = {nullptr, nullptr};
+                if (!paged && L > 0) {
+                    seq = (const uint8_t *)(is_v ? a.cache.kv.v_seq : a.cache.kv.k_seq)[sid];
+                    if (E4 && is_v) {
+                        seq_scale[0] = ((const float *const *)a.cache.k_scale)[sid];
+                        seq_scale[1] = ((const float *const *)a.cache.v_scale)[sid];
+                    }
+                }
+#pragma unroll 1
+                for (int i = 0; i < sg.n; ++i) {
+                    const int t = sg.t_a + i, t0 = t * TILE;
+                    const bool is_fresh = t == sg.nt - 1;
+                    const int n_tok = is_fresh ? 0 : min(TILE, L - t0);
+                    const int n_pg = paged ? n_tok / P : 0;  // whole pages
+                    int page = -1;                           // page ids (up to eight), asked for before the wait
+                    if (paged && lane * P < n_tok) {
+                        const int lp = t0 / P + lane;
+                        page = lp < a.cache.kv.max_pages ? a.cache.kv.page_table[(size_t)sid * a.cache.kv.max_pages + lp] : -1;
+                        if (page < 0 || page >= a.cache.kv.n_pages) page = -1, bad = 1;
+                    }
+                    // warp-uniform verdict: the collectives below need every lane
+                    if (!mbar_wait_warp(&empty[rg.slot], rg.ph ^ 1, abort)) {
+                        stop = true;
+                        break;
+                    }
+                    uint8_t *dst = ring + rg.slot * slot_bytes;
+                    uint8_t *sc = dst + SLOT8;  // (E4 && is_v)
+                    bool plain = false;         // this thread wrote shared memory or issued cp.async
+                    if (n_pg > 0 && lead) {
+                        const bool ok = lane < n_pg && page >= 0;
+                        const unsigned okm = __ballot_sync(0xffffffffu, ok);
+                        const uint32_t bytes = (uint32_t)(P * DH * ES + (E4 && is_v ? P * 8 : 0));
+                        if (lane == 0 && okm) expect_tx(&full[rg.slot], __popc(okm) * bytes);
+                        __syncwarp();
+                        if (ok) {  // the cache is read once: evict-first keeps queries and partials in L2
+                            const int row = page * Hkv + g;
+                            if constexpr (E4) {
+                                tma_load_2d_hint(dst + lane * P * DH, map, &full[rg.slot], 0, row * P, pol);
+                                if (is_v) {
+                                    const size_t at = (size_t)row * P;
+                                    bulk_load(sc + lane * P * 4, (const float *)a.cache.k_scale + at, P * 4, &full[rg.slot]);
+                                    bulk_load(sc + TILE * 4 + lane * P * 4, (const float *)a.cache.v_scale + at, P * 4,
+                                              &full[rg.slot]);
+                                }
+                            } else {
+                                tma_load_4d_hint(dst + lane * P * 256, map, &full[rg.slot], 0, 0, 0, row * (P / 8), pol);
+                            }
+                        }
+                        // a page outside the pool: zeros
+#pragma unroll 1
+                        for (unsigned miss = ~okm & ((1u << n_pg) - 1u); miss; miss &= miss - 1) {
+                            const int j = __ffs(miss) - 1;
+#pragma unroll 1
+                            for (int e = lane; e < P * CH; e += 32) st_shared_v4(dst + j * P * DH * ES + e * 16, 0, 0, 0, 0);
+                            if (E4 && is_v && lane < P / 4) {
+                                st_shared_v4(sc + j * P * 4 + lane * 16, 0, 0, 0, 0);
+                                st_shared_v4(sc + TILE * 4 + j * P * 4 + lane * 16, 0, 0, 0, 0);
+                            }
+                            plain = true;
+                        }
+                    }
+                    if (!is_fresh) {
+                        const int r0 = n_pg * (paged ? P : 0);  // first row not covered by TMA
+                        if (r0 < n_tok) {
+                            plain = true;
+                            if (paged) {  // the last, partial page
+                                const int pg = __shfl_sync(0xffffffffu, page, n_pg);
+                                const size_t at = ((size_t)max(pg, 0) * Hkv + g) * P;
+#pragma unroll 1
+                                for (int idx = ptid; idx < (n_tok - r0) * CH; idx += PT) {
+                                    const int r = idx / CH, c = idx - r * CH;
+                                    if (pg >= 0) cp_async16(dst + dst_off(r0 + r, c), pool + (at + r) * (DH * ES) + c * 16);
+                                    else st_shared_v4(dst + dst_off(r0 + r, c), 0, 0, 0, 0);
+                                }
+                                if (E4 && is_v) {
+#pragma unroll 1
+                                    for (int r = ptid; r < n_tok - r0; r += PT) {
+                                        if (pg >= 0) {
+                                            cp_async4(sc + (r0 + r) * 4, (const float *)a.cache.k_scale + at + r);
+                                            cp_async4(sc + (TILE + r0 + r) * 4, (const float *)a.cache.v_scale + at + r);
+                                        } else {
+                                            *(float *)(sc + (r0 + r) * 4) = 0.f;
+                                            *(float *)(sc + (TILE + r0 + r) * 4) = 0.f;
+                                        }
+                                    }
+                                }
+                            } else {
+                                const uint8_t *src = seq + ((size_t)t0 * Hkv + g) * (DH * ES);
+#pragma unroll 4
+                                for (int idx = ptid; idx < n_tok * CH; idx += PT) {
+                                    const int r = idx / CH, c = idx - r * CH;
+                                    cp_async16(dst + dst_off(r, c), src + (size_t)r * Hkv * (DH * ES) + c * 16);
+                                }
+                                if (E4 && is_v) {
+#pragma unroll 1
+                                    for (int r = ptid; r < n_tok; r += PT) {
+                                        const size_t at = (size_t)(t0 + r) * Hkv + g;
+                                        cp_async4(sc + r * 4, seq_scale[0] + at);
+                                        cp_async4(sc + (TILE + r) * 4, seq_scale[1] + at);
+                                    }
+                                }
+                            }
+                        }
+                        // values past the end are multiplied by weights of 0: they must be
+                        // finite (keys there give scores that are replaced)
+                        if (!E4 && is_v && n_tok < TILE) {
+                            plain = true;
+#pragma unroll 1
+                            for (int idx = ptid; idx < (TILE - n_tok) * CH; idx += PT)
+                                st_shared_v4(dst + kv_off(n_tok + idx / CH, idx % CH), 0, 0, 0, 0);
+                        }
+                    } else if (!E4 || !is_v) {
+                        // the nodes' rows: 16 lanes a row, 8 elements a lane
+                        plain = true;
+                        const int n = nodes[b], c = lane & 15;
+                        unsigned long long vb = 0;
+#pragma unroll 2
+                        for (int r = pidx * 2 + (lane >> 4); r < 64; r += 2 * Ro::RING_WARPS) {
+                            uint4 u = make_uint4(0, 0, 0, 0);
+                            if (r < n) u = *(const uint4 *)(fresh + ((size_t)b * a.N + r) * fs + (size_t)g * DH + c * 8);
+                            if constexpr (!E4) {
+                                if (is_v) {
+                                    uint32_t w[4] = {u.x, u.y, u.z, u.w};
+                                    bool odd = false;
+#pragma unroll
+                                    for (int q = 0; q < 4; ++q) {
+                                        const bool lo = (w[q] & 0x7f80u) == 0x7f80u, hi = (w[q] & 0x7f800000u) == 0x7f800000u;
+                                        odd = odd || lo || hi;
+                                        w[q] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+                                    }
+                                    u = make_uint4(w[0], w[1], w[2], w[3]);
+                                    const unsigned o = __ballot_sync(0xffffffffu, odd);
+                                    const int even = r & ~1;  // (lanes 0-15 hold the even row)
+                                    if (o & 0xffffu) vb |= 1ull << even;
+                                    if (o >> 16) vb |= 2ull << even;
+                                }
+                                st_shared_v4(dst + kv_off(r, c), u.x, u.y, u.z, u.w);
+                            } else {
+                                // keys as two 8-bit parts, rows r and 64 + r
+                                float v[8];
+                                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+                                float amax = 0.f;
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) {
+                                    v[2 * q] = __uint_as_float(w[q] << 16);
+                                    v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
+                                    amax = fmaxf(amax, fmaxf(fabsf(v[2 * q]), fabsf(v[2 * q + 1])));
+                                }
+#pragma unroll
+                                for (int o = 1; o < 16; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+                                int k;
+                                const float f = pow2_scale(amax, &k);
+#pragma unroll
+                                for (int q = 0; q < 8; ++q) v[q] *= f;
+                                uint2 hi, lo;
+                                split_codes(v, &hi, &lo);
+                                *(uint2 *)(dst + off8(r, c >> 1) + (c & 1) * 8) = hi;
+                                *(uint2 *)(dst + off8(64 + r, c >> 1) + (c & 1) * 8) = lo;
+                            }
+                        }
+                        if (!E4 && is_v && lane == 0) bars->vbad[rg.slot][pidx] = vb;
+                    }
+                    if (plain) {
+                        fence_proxy_async();  // this thread's shared-memory stores
+                        cp_async_mbar_arrive(&full[rg.slot]);
+                    } else {
+                        mbar_arrive(&full[rg.slot]);
+                    }
+                    ++filled;
+                    rg.next();
+                }
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");  // nothing lands after the CTA is gone
+            if (lead && lane == 0) {
+                // drain TMA writes still in flight (only possible after an abort)
+                Ring rd(rg.n);
+#pragma unroll 1
+                for (int j = 0; j < filled; ++j, rd.next())
+                    if (j + rg.n >= filled) mbar_wait_drain(&full[rd.slot], rd.ph);
+            }
+            bad = __any_sync(0xffffffffu, bad);
+            if (bad && lane == 0 && a.status) atomicOr(a.status, SP_DEV_BAD_PAGE);
+        } else if (E4 && warp >= CVT) {
+            // ------------------------------------------------------------ V codes -> 16-bit floats
+            const int ct = threadIdx.x - CVT * 32, cw = warp - CVT;
+            Ring rv(lay.nv), rc(CONV);
+            bool ok = true;
+#pragma unroll 1
+            for (int x = x0; ok && x < x1;) {
+                const Seg sg = seg_at(prefix, B, x, x1);
+                x += sg.n;
+                const int b = sg.b, L = lens[b];
+#pragma unroll 1
+                for (int i = 0; i < sg.n; ++i) {
+                    const int t = sg.t_a + i;
+                    const bool is_fresh = t == sg.nt - 1;
+                    const int n_tok = is_fresh ? 0 : min(TILE, L - t * TILE);
+                    ok = mbar_wait_warp(&bars->v_full[rv.slot], rv.ph, abort) &&
+                         mbar_wait_warp(&bars->c_empty[rc.slot], rc.ph ^ 1, abort);
+                    if (!ok) break;
+                    const uint8_t *src = smem + lay.off_v + rv.slot * (SLOT8 + SCALES);
+                    uint8_t *dst = smem + lay.off_c + rc.slot * SLOT16;
+                    float *par = (float *)(smem + lay.off_c + CONV * SLOT16 + rc.slot * PARAMS);
+                    if (!is_fresh) {
+                        // the softmax's constants first: it does not wait for the values
+                        float ks = 0.f, vs = 1.f;
+                        if (ct < n_tok) {
+                            ks = ((const float *)(src + SLOT8))[ct];
+                            vs = fmaxf(((const float *)(src + SLOT8))[TILE + ct], 7.888609052210118e-31f);  // 2^-100
+                        }
+                        *(float2 *)(par + 2 * ct) = make_float2(ks * a.scale_log2, __log2f(vs));
+                        par[2 * TILE + ct] = __frcp_rn(vs);
+                        arrive_warp(&bars->c_par[rc.slot], lane);
+                        uint4 u[8];
+#pragma unroll
+                        for (int it = 0; it < 8; ++it) {
+                            const int r = it * 16 + (ct >> 3);
+                            u[it] = r < n_tok ? *(const uint4 *)(src + off8(r, ct & 7)) : make_uint4(0, 0, 0, 0);
+                        }
+#pragma unroll
+                        for (int it = 0; it < 8; ++it) {
+                            const int r = it * 16 + (ct >> 3), c = ct & 7;
+                            const uint32_t w[4] = {u[it].x, u[it].y, u[it].z, u[it].w};
+                            uint32_t h[8];
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) h[q] = codes2_to_half2(w[q >> 1], q & 1);
+                            st_shared_v4(dst + kv_off(r, 2 * c), h[0], h[1], h[2], h[3]);
+                            st_shared_v4(dst + kv_off(r, 2 * c + 1), h[4], h[5], h[6], h[7]);
+                        }
+                    } else {
+                        const int n = nodes[b], c = lane & 15;
+                        unsigned long long vb = 0;
+#pragma unroll 1
+                        for (int r = cw * 2 + (lane >> 4); r < TILE; r += 8) {
+                            uint4 uk = make_uint4(0, 0, 0, 0), uv = uk;
+                            if (r < n) {
+                                const size_t row = (size_t)b * a.N + r;
+                                uk = *(const uint4 *)((const bf16 *)a.k_new + row * a.ks + (size_t)g * DH + c * 8);
+                                uv = *(const uint4 *)((const bf16 *)a.v_new + row * a.vs + (size_t)g * DH + c * 8);
+                            }
+                            const uint32_t wk[4] = {uk.x, uk.y, uk.z, uk.w}, wv[4] = {uv.x, uv.y, uv.z, uv.w};
+                            float v[8], amk = 0.f, amv = 0.f;
+                            bool odd = false;
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                amk = fmaxf(amk, fmaxf(fabsf(__uint_as_float(wk[q] << 16)), fabsf(__uint_as_float(wk[q] & 0xffff0000u))));
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    const float y = __uint_as_float(e ? wv[q] & 0xffff0000u : wv[q] << 16);
+                                    const bool fin = isfinite(y);
+                                    odd = odd || !fin;
+                                    v[2 * q + e] = fin ? y : 0.f;
+                                    amv = fmaxf(amv, fabsf(v[2 * q + e]));
+                                }
+                            }
+#pragma unroll
+                            for (int o = 1; o < 16; o <<= 1) {
+                                amk = fmaxf(amk, __shfl_xor_sync(0xffffffffu, amk, o));
+                                amv = fmaxf(amv, __shfl_xor_sync(0xffffffffu, amv, o));
+                            }
+                            const unsigned o = __ballot_sync(0xffffffffu, odd);
+                            if (r < 64) {
+                                if (o & 0xffffu) vb |= 1ull << (r & ~1);
+                                if (o >> 16) vb |= 2ull << (r & ~1);
+                            }
+                            int kk, kv;
+                            pow2_scale(amk, &kk);
+                            const float f = pow2_scale(amv, &kv);
+                            st_shared_v4(dst + kv_off(r, c), pack_half(v[0] * f, v[1] * f), pack_half(v[2] * f, v[3] * f),
+                                         pack_half(v[4] * f, v[5] * f), pack_half(v[6] * f, v[7] * f));
+                            if (c == 0) {
+                                // an infinite key saturates in its parts: its scores are NaN
+                                par[2 * r] = pow2i(-kk) * a.scale_log2 + (amk - amk);
+                                par[2 * r + 1] = (float)-kv;
+                                par[2 * TILE + r] = pow2i(kv);
+                            }
+                        }
+                        if (lane == 0) bars->vbad[rc.slot][cw] = vb;
+                        arrive_warp(&bars->c_par[rc.slot], lane);
+                    }
+                    fence_proxy_async();
+                    arrive_warp(&bars->c_full[rc.slot], lane);
+                    if (lane == 0) mbar_arrive(&bars->v_empty[rv.slot]);
+                    rv.next();
+                    rc.next();
+                }
+            }
+        } else if (warp == MMA) {
+            // ------------------------------------------------------------ MMA issue
+            // Items q of a segment in order: pipeline q & 1, on tile q (one M tile) or q / 2
+            // (two).  S of the first two, then PV of item q once its softmax is done and S of
+            // item q + 2 into the buffer that softmax has read.  One issuer: it sees every use
+            // of every ring slot in order.  (Two, each waiting for its own tiles only, may ask
+            // for a slot's next use before the one in between, the other's, has landed; the
+            // barrier's parity then answers for the use before that.)  By the whole warp, the
+            // instructions under `on` (see elect_one).
+            const bool on = elect_one();
+            constexpr uint32_t idesc_s = E4 ? (1u << 4) | ((uint32_t)(TILE >> 3) << 17) | (8u << 24) : idesc_bf16_f32(128, TILE);
+            // 16-bit floats: format bits 0 instead of bf16's 1
+            constexpr uint32_t idesc_o = E4 ? (1u << 4) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | (8u << 24)
+                                            : idesc_bf16_f32_bmn(128, DH);
+            const uint64_t dq0 = sw128_kmajor_desc(smem + lay.off_q);
+            const uint64_t dk0 = sw128_kmajor_desc_sbo(smem + lay.off_k, E4 ? 1024 : GROUP_STRIDE);
+            const uint64_t dv0 = sw128_mnmajor_desc2(smem + (E4 ? lay.off_c : lay.off_v), HALF_STRIDE, GROUP_STRIDE);
+            uint64_t *vf = E4 ? bars->c_full : bars->v_full, *ve = E4 ? bars->c_empty : bars->v_empty;
+            Ring rk(lay.nk), rv(E4 ? CONV : lay.nv);
+            bool ok = true;
+            uint32_t kp = 0;  // phases of p_full, a bit a pipeline
+            int j = 0;
+            auto issue_s = [&](int q) {
+                const int w = q & 1;
+                ok = ok && mbar_wait_warp(&bars->k_full[rk.slot], rk.ph, abort);
+                if (!ok) return;
+                tc_fence_after();
+                fence_proxy_async();  // cp.async data -> tensor-core reads
+                const uint64_t dk = dk0 + (uint32_t)(rk.slot * ((E4 ? SLOT8 : SLOT16) >> 4));
+                const uint64_t dq = dq0 + (uint32_t)(MT == 2 ? w * (Q_TILE >> 4) : 0);
+                const uint32_t d = tmem + (uint32_t)(w * 128);
+                if (on) {
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk) {
+                        // 8-bit: part kk / 4, 32 dims each; else 16 dims, 32 B of a row of dim half kk / 4
+                        const uint64_t aq = dq + (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2);
+                        if constexpr (E4) mma_e4m3(d, aq, dk + (uint64_t)((kk & 3) * 2), idesc_s, kk > 0);
+                        else mma_bf16(d, aq, dk + (uint64_t)((kk >> 2) * (HALF_STRIDE >> 4) + (kk & 3) * 2), idesc_s, kk > 0);
+                    }
+                    if (MT == 1 || w) mma_commit(&bars->k_empty[rk.slot]);
+                    mma_commit(&bars->s_full[w]);
+                }
+                __syncwarp();
+                if (MT == 1 || w) rk.next();
+            };
+#pragma unroll 1
+            for (int x = x0; ok && x < x1; ++j) {
+                const Seg sg = seg_at(prefix, B, x, x1);
+                x += sg.n;
+                // the same in every lane, and known to be
+                const int items = __shfl_sync(0xffffffffu, sg.n, 0) * MT;
+                const bool has_fresh = __shfl_sync(0xffffffffu, (int)(sg.t_a + sg.n == sg.nt), 0);
+                if (!mbar_wait_warp(&bars->q_full, (uint32_t)(j & 1), abort)) break;
+#pragma unroll 1
+                for (int q = -2; ok && q < items; ++q) {
+                    if (q >= 0) {
+                        const int w = q & 1;
+                        ok = mbar_wait_warp(&vf[rv.slot], rv.ph, abort) && mbar_wait_warp(&bars->p_full[w], (kp >> w) & 1, abort);
+                        if (!ok) break;
+                        kp ^= 1u << w;
+                        tc_fence_after();
+                        fence_proxy_async();
+                        const uint64_t dv = dv0 + (uint32_t)(rv.slot * (SLOT16 >> 4));
+                        const bool half = has_fresh && q >= items - MT;  // at most 64 nodes
+                        const uint32_t acc = q >= 2;
+                        if (on) {
+#pragma unroll
+                            for (int kk = 0; kk < 8; ++kk)  // 16 tokens: 8 columns of P, two 8-token groups of V
+                                if (kk < 4 || !half)
+                                    mma_bf16_ts(tmem + O_COL + (uint32_t)(w * DH), tmem + (uint32_t)(w * 128 + kk * 8),
+                                                dv + (uint64_t)(kk * (2 * GROUP_STRIDE >> 4)), idesc_o, kk > 0 ? 1u : acc);
+                            if (MT == 1 || w) mma_commit(&ve[rv.slot]);
+                            if (q == items - 1) mma_commit(&bars->pv_done);
+                        }
+                        __syncwarp();
+                        if (MT == 1 || w) rv.next();
+                    }
+                    if (q + 2 < items) issue_s(q + 2);
+                }
+            }
+            if (on) mma_commit(&bars->fin);  // completes when every MMA is done
+            __syncwarp();
+        }
     }
     // every MMA must be finished before TMEM and shared memory go away
     mbar_wait_drain(&bars->fin, 0);
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && *abort && a.status) atomicOr(a.status, SP_DEV_TIMEOUT);
-    if (warp == Ro::MMA) tmem_dealloc(tmem, 512);
+    if (warp == MMA) tmem_dealloc(tmem, 512);
 }
 
 // Merge of the pairs that lie in several shares: a warp per (sequence, kv head, row),
@@ -1082,7 +1154,7 @@ cudaError_t run(const TreeArgs &a, const Layout &lay, const CUtensorMap &mk, con
         if (e != cudaSuccess) return e;
         attr = true;
     }
-    return launch_k(tree_tc_kernel<E4, TPC, MT>, dim3(a.plan.tc_ctas), dim3(Roles<E4>::THREADS), (size_t)lay.smem, st, mk, mv, a,
+    return launch_k(tree_tc_kernel<E4, TPC, MT>, dim3(a.plan.tc_ctas), dim3(THREADS), (size_t)lay.smem, st, mk, mv, a,
                     lay, tab);
 }
 

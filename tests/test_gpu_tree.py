@@ -276,3 +276,40 @@ def test_offsets_past_32_bits(torch):
             assert torch.equal(got, want)
         else:  # bf16 of the same value within the two paths' bounds
             assert bool(((got.double() - want.double()).abs() <= 2.0 ** -6 * want.double().abs() + 2.0 ** -8).all())
+
+
+@pytest.mark.parametrize("cdt", [sp.SP_BF16, sp.SP_E4M3])
+@pytest.mark.parametrize("N,page", [(4, 16), (13, 0), (16, 16), (25, 32), (40, 16)])
+def test_long_shares_of_many_sequences(torch, cdt, N, page):
+    # dozens of tiles and several sequences a block: rings wrap, segments follow one
+    # another; every launch gives the same bits, near the fp32 kernel's result
+    hkv, hq, dh, B = 8, 32, 128, 48
+    rng = np.random.default_rng(N)
+    lens = [int(x) for x in rng.integers(0, 3000, B)]
+    cache = Cache(cdt, hkv, dh, [max(x, 1) for x in lens], page, junk=0.0)
+    g = torch.Generator(device="cuda").manual_seed(N)
+    for pool in (cache.k, cache.v):
+        pool.copy_(torch.randn(pool.shape, generator=g, device="cuda").mul_(1 if cdt == sp.SP_BF16 else 60).to(pool.dtype))
+    if cdt == sp.SP_E4M3:
+        for sc in (cache.ks, cache.vs):
+            sc.copy_(torch.rand(sc.shape, generator=g, device="cuda") / 40)
+    q, k, v = (torch.randn((B, N, h, dh), generator=g, device="cuda").to(torch.bfloat16) for h in (hq, hkv, hkv))
+    masks = mask_tensor(torch, np.stack([sp.sp_tree_masks(random_parents(rng, N))[0] for _ in range(B)]))
+    n_nodes = [int(x) for x in rng.integers(0, N + 1, B)]
+    dims = sp.sp_tree_dims(hq, N, sp.SP_BF16, 2, 0, 0.0, 0, 0, 0)
+    first, status = tree_call(torch, cache, dims, lens, masks, n_nodes, q, k, v)
+    assert status == 0
+    args = [torch.tensor(x, dtype=torch.int32).cuda() for x in (lens, n_nodes)]
+    size = sp.sp_attend_tree_workspace_bytes(dims, cache.desc, B)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    outs = [torch.empty((B, N, hq, dh), dtype=torch.bfloat16, device="cuda") for _ in range(8)]
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for i in range(400):
+        sp.sp_attend_tree(stream, dims, cache.desc, B, None, args[0], masks, args[1], q, k, v, outs[i % 8], ws, size)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o.cpu(), first) for o in outs)
+    dims.path = 1
+    ref, _ = tree_call(torch, cache, dims, lens, masks, n_nodes, q, k, v)
+    # two bf16 roundings of the result, weights of 8 bits: 2^-8 each, in the 2-norm
+    assert float((first.double() - ref.double()).norm()) <= 3 * 2.0 ** -8 * float(ref.double().norm())
