@@ -67,14 +67,15 @@ constexpr int kTreeSegCost = 4;                 // cost of a segment, in tiles
 
 struct Layout {
     int nk, nv;                                 // ring slots
-    int off_q, off_k, off_v, off_c, off_tab;    // (off_c: converted V, then its parameters)
+    int off_q, off_k, off_v, off_c, off_st, off_tab;  // (off_c: converted V, then its parameters;
+                                                // off_st: staging of the copies' parts)
     int smem;
 };
 
 struct Bars {
     uint64_t k_full[MAX_RING], k_empty[MAX_RING], v_full[MAX_RING], v_empty[MAX_RING];
     uint64_t c_full[CONV], c_empty[CONV], c_par[CONV];
-    uint64_t s_full[2], p_full[2], pv_done, q_full, fin;
+    uint64_t s_full[2], p_full[2], pv_done, q_full, q_empty, fin;
     unsigned long long vbad[MAX_RING][4];       // nodes with non-finite values, by V slot and warp
     unsigned long long seg_vbad;
     uint32_t tmem;
@@ -83,19 +84,35 @@ struct Bars {
 };
 constexpr int OFF_ML = 1024;                    // (max, sum) of [pipeline][lane]
 constexpr int OFF_L = OFF_ML + 2 * 128 * 8;      // 1 / sum of [warpgroup][row]
-constexpr int OFF_CUTS = OFF_L + 2 * 128 * 4;
+constexpr int OFF_SEES = OFF_L + 2 * 128 * 4;   // nodes that a row sees, [segment parity][row]
+constexpr int OFF_RS = OFF_SEES + 2 * 256 * 8;  // scale of a row's 8-bit queries, the same
+constexpr int OFF_CUTS = OFF_RS + 2 * 256 * 4;
 constexpr int OFF_FRONT = OFF_CUTS + (MAX_GRP + 4) * 4;
 static_assert(sizeof(Bars) <= OFF_ML, "barrier block");
 
-// Warp roles: softmax 0-7, MMA 8 (9 idle); 8-bit caches: producers 10-11, converters 12-15;
-// else producers 12-15 (10-11 idle).
+// Warp roles: softmax 0-7, MMA 8; 8-bit caches: producers 10-11, converters 12-15 (queries
+// too; 9 idle); else queries 9-11, producers 12-15.
 constexpr int THREADS = 512;
 constexpr int MMA = 8, CVT = 12;
+// Registers a thread: the softmax warps take what the other roles leave of the launch's
+// 128 (8 x 144 + 8 x 112 = 16 x 128 a lane).  With 128 everywhere 50 to 350 bytes a thread
+// spill, more in all than the L1 that the shared memory leaves holds: a reload then waits
+// for the L2 behind the cache stream.
+constexpr int SOFT_REGS = 144, OTHER_REGS = 112;
+template <int N>
+__device__ __forceinline__ void regs_inc() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void regs_dec() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
 template <bool E4>
 struct Roles {
     static constexpr int RING_WARPS = E4 ? 1 : 2;                    // producers of a ring
     static constexpr int RING_THREADS = RING_WARPS * 32;
     static constexpr int PROD = E4 ? 10 : 12;
+    static constexpr int Q_WARP = E4 ? CVT : 9, Q_WARPS = E4 ? 4 : 3;  // load the queries
 };
 // One arrival of a warp whose lanes have all done their part.
 __device__ __forceinline__ void arrive_warp(uint64_t *bar, int lane) {
@@ -111,6 +128,11 @@ __device__ __forceinline__ void st16_async(uint32_t addr, const float *v) {
         "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]),
         "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
         : "memory");
+}
+template <int W>
+__device__ __forceinline__ void tmem_ldw(uint32_t addr, float (&v)[W]) {
+    static_assert(W == 16, "");
+    tmem_ld16(addr, v);
 }
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void zero16_async(uint32_t addr) {
@@ -252,17 +274,74 @@ __device__ __forceinline__ uint32_t codes2_to_half2(uint32_t w, int hi) {
 // byte offset of 16-byte chunk c (0..7) of row r of an 8-bit tile (128-byte rows, swizzled)
 __device__ __forceinline__ uint32_t off8(int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); }
 
-// y plus the non-finite values, dims d .. d + 3, of the nodes in `left` (out of line: rare).
-__device__ __forceinline__ float4 add_non_finite(const TreeArgs &a, int b, int g, int d, unsigned long long left, float4 y) {
-    for (; left; left &= left - 1) {
-        const bf16 *v = (const bf16 *)a.v_new + ((size_t)b * a.N + (__ffsll(left) - 1)) * a.vs + (size_t)g * DH + d;
-        const float z[4] = {to_f(v[0]), to_f(v[1]), to_f(v[2]), to_f(v[3])};
-        if (!isfinite(z[0])) y.x += z[0];
-        if (!isfinite(z[1])) y.y += z[1];
-        if (!isfinite(z[2])) y.z += z[2];
-        if (!isfinite(z[3])) y.w += z[3];
+// The queries of sequence b into the score product's A operand, each copy of a row (dead
+// rows: zeros), as bf16 [dim half][row][128 B] or as two 8-bit parts [part][row][128 B], and
+// what its softmax thread needs of it: the nodes it sees and the parts' scale.  16 lanes a
+// row; by warps wi of nw.
+template <bool E4, int TPC, int MT>
+__device__ __forceinline__ void load_queries(const TreeArgs &a, int b, int n, int g, int rb, uint8_t *Q,
+                                             unsigned long long *sees, float *scale, int wi, int nw, int lane) {
+    const int c = lane & 15;
+#pragma unroll 2
+    for (int r = wi * 2 + (lane >> 4); r < TPC * MT; r += 2 * nw) {
+        const int rr = rb * a.rb_rows + r, node = rr / a.G;
+        const bool live = r < a.rb_rows && rr < a.R && node < n;
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (live)
+            u = *(const uint4 *)((const bf16 *)a.q + ((size_t)b * a.N + node) * a.qs + (size_t)(g * a.G + rr - node * a.G) * DH + c * 8);
+        if (c == 0) sees[r] = live ? tree_mask(a, b, node, n) : 0;
+        uint8_t *q = Q + (MT == 2 ? (r >> 7) * Q_TILE : 0);
+        const int rt = MT == 2 ? r & 127 : r;
+        if constexpr (!E4) {
+#pragma unroll
+            for (int k = 0; k < 128 / TPC; ++k)
+                st_shared_v4(q + (c >> 3) * 16384 + off8(k * TPC + rt, c & 7), u.x, u.y, u.z, u.w);
+        } else {
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+            float v[8], amax = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = __uint_as_float(w[i] << 16);
+                v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+                amax = fmaxf(amax, fmaxf(fabsf(v[2 * i]), fabsf(v[2 * i + 1])));
+            }
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+            int k2;
+            const float f = pow2_scale(amax, &k2);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= f;
+            uint2 hi, lo;
+            split_codes(v, &hi, &lo);
+            if (c == 0) scale[r] = pow2i(-k2) + (amax - amax);  // (an infinite query: NaN)
+#pragma unroll
+            for (int k = 0; k < 128 / TPC; ++k) {
+                *(uint2 *)(q + off8(k * TPC + rt, c >> 1) + (c & 1) * 8) = hi;
+                *(uint2 *)(q + 16384 + off8(k * TPC + rt, c >> 1) + (c & 1) * 8) = lo;
+            }
+        }
     }
-    return y;
+    fence_proxy_async();  // -> tensor-core reads
+}
+
+// The non-finite values of the nodes in `odd` added to what was written for the rows of
+// the block that see them: the output, or the partial at part.  A row a thread (rare).
+__device__ __forceinline__ void add_non_finite(const TreeArgs &a, int b, int g, int rb, int n, unsigned long long odd,
+                                               bool whole, float *part, int q) {
+    const int rr = rb * a.rb_rows + q, node = rr / a.G;
+    if (q >= a.rb_rows || rr >= a.R || node >= n) return;
+    bf16 *out = (bf16 *)a.out + (((size_t)b * a.N + node) * a.Hq + (g * a.G + rr - node * a.G)) * DH;
+#pragma unroll 1
+    for (unsigned long long left = odd & tree_mask(a, b, node, n); left; left &= left - 1) {
+        const bf16 *v = (const bf16 *)a.v_new + ((size_t)b * a.N + (__ffsll(left) - 1)) * a.vs + (size_t)g * DH;
+#pragma unroll 1
+        for (int d = 0; d < DH; ++d) {
+            const float z = to_f(v[d]);
+            if (isfinite(z)) continue;
+            if (whole) out[d] = __float2bfloat16_rn(to_f(out[d]) + z);
+            else part[(size_t)q * DH + d] += z;
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -314,7 +393,8 @@ __global__ void __launch_bounds__(THREADS, 1)
             mbar_init(&bars->s_full[i], 1);
             mbar_init(&bars->p_full[i], 4);
         }
-        mbar_init(&bars->q_full, SOFT / 32);
+        mbar_init(&bars->q_full, Ro::Q_WARPS);
+        mbar_init(&bars->q_empty, 1 + SOFT / 32);
         mbar_init(&bars->pv_done, 1);
         mbar_init(&bars->fin, 1);
         bars->abort = 0;
@@ -342,6 +422,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
 
     if (warp < 8) {
+        regs_inc<SOFT_REGS>();
         // ------------------------------------------------------------ softmax + epilogue
         const int wg = warp >> 2, ln = threadIdx.x & 127;  // pipeline; TMEM lane
         const int cp = ln / TPC, row_t = ln - cp * TPC;    // copy, row of the M tile
@@ -349,78 +430,38 @@ __global__ void __launch_bounds__(THREADS, 1)
         const int rr = rb * a.rb_rows + r;                 // query row of the kv head
         const bool active = r < a.rb_rows && rr < a.R;
         const bool warp_active = __any_sync(0xffffffffu, active);
-        const int node = active ? rr / a.G : 0, hl = active ? rr - node * a.G : 0;
         const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t s_col = lane_base + (uint32_t)(wg * 128), o_col = lane_base + O_COL + (uint32_t)(wg * DH);
         bool ok = true;
-        uint32_t ks_ph = 0, pv_ph = 0;
+        uint32_t ks_ph = 0, seg_ph = 0;
         Ring rv(E4 ? CONV : lay.nv);
 #pragma unroll 1
         for (int x = x0; x < x1;) {
-            const Seg sg = seg_at(prefix, B, x, x1);
-            x += sg.n;
-            const int b = sg.b, L = lens[b], n = nodes[b];
-            const bool live = active && node < n;
-            const uint64_t sees = live ? tree_mask(a, b, node, n) : 0;
-            // ---- queries -> shared memory; a thread its own row (each copy its rows)
-            float rs = 1.f;  // 8-bit parts: the row's scale
+            const int xs = x;   // segment start (what the epilogue needs is found again then)
+            int n_tiles, last;  // tiles; the nodes' tile, if it is here
+            int left;           // cached tokens from the segment's start on
             {
-                const uint4 *src = (const uint4 *)((const bf16 *)a.q + ((size_t)b * a.N + node) * a.qs + (size_t)(g * a.G + hl) * DH);
-                uint8_t *q = smem + lay.off_q + (MT == 2 ? wg * Q_TILE : 0);
-                const int c_lo = MT == 2 ? 0 : wg * 8, c_n = MT == 2 ? 16 : 8;
-                if constexpr (!E4) {
-                    uint4 u[16];
-#pragma unroll
-                    for (int c = 0; c < 16; ++c)
-                        if (c < c_n) u[c] = live ? src[c_lo + c] : make_uint4(0, 0, 0, 0);
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) {
-                        if (c >= c_n) break;
-                        const int cc = c_lo + c;
-                        st_shared_v4(q + (cc >> 3) * 16384 + off8(ln, cc & 7), u[c].x, u[c].y, u[c].z, u[c].w);
-                    }
-                } else {
-                    float amax = 0.f;
-#pragma unroll 4
-                    for (int c = 0; c < 16; ++c) {
-                        const uint4 u = live ? src[c] : make_uint4(0, 0, 0, 0);
-                        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                        for (int q4 = 0; q4 < 4; ++q4)
-                            amax = fmaxf(amax, fmaxf(fabsf(__uint_as_float(w[q4] << 16)), fabsf(__uint_as_float(w[q4] & 0xffff0000u))));
-                    }
-                    int k;
-                    const float f = pow2_scale(amax, &k);
-                    rs = pow2i(-k) + (amax - amax);  // (an infinite query: NaN)
-#pragma unroll 2
-                    for (int c = c_lo; c < c_lo + c_n; ++c) {
-                        const uint4 u = live ? src[c] : make_uint4(0, 0, 0, 0);
-                        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-                        float v[8];
-#pragma unroll
-                        for (int q4 = 0; q4 < 4; ++q4) {
-                            v[2 * q4] = __uint_as_float(w[q4] << 16) * f;
-                            v[2 * q4 + 1] = __uint_as_float(w[q4] & 0xffff0000u) * f;
-                        }
-                        uint2 hi, lo;
-                        split_codes(v, &hi, &lo);
-                        *(uint2 *)(q + off8(ln, c >> 1) + (c & 1) * 8) = hi;
-                        *(uint2 *)(q + 16384 + off8(ln, c >> 1) + (c & 1) * 8) = lo;
-                    }
-                }
-                fence_proxy_async();
-                arrive_warp(&bars->q_full, lane);
+                const Seg sg = seg_at(prefix, B, x, x1);
+                n_tiles = sg.n;
+                last = sg.nt - 1 - sg.t_a;
+                left = lens[sg.b] - sg.t_a * TILE;
             }
+            x += n_tiles;
+            // this segment's queries are there, and with them what the row sees and its scale
+            ok = ok && mbar_wait_warp(&bars->q_full, seg_ph, abort);
+            // (the next ones may come once every softmax warp has seen these and their scores
+            // are done: the scores alone run ahead by a whole short segment)
+            arrive_warp(&bars->q_empty, lane);
+            const int row_s = (int)seg_ph * 256 + r;
+            const float rs = E4 ? ((volatile float *)(smem + OFF_RS))[row_s] : 1.f;
             // ---- tiles
             float m = -INFINITY, l = 0.f;
             bool first = true;
-            unsigned long long vb = 0;
 #pragma unroll 1
-            for (int i = 0; i < sg.n; ++i, rv.next()) {
+            for (int i = 0; i < n_tiles; ++i, rv.next()) {
                 if (MT == 1 && (i & 1) != wg) continue;
-                const int t = sg.t_a + i;
-                const bool is_fresh = t == sg.nt - 1;
-                const int n_tok = is_fresh ? 0 : min(TILE, L - t * TILE);
+                const bool is_fresh = i == last;
+                const int n_tok = is_fresh ? 0 : min(TILE, left - i * TILE);
                 // warp-uniform verdicts: the TMEM loads and stores are warp-collective
                 ok = ok && mbar_wait_warp(&bars->s_full[wg], ks_ph, abort);
                 // (8-bit: the tile's constants; the nodes' tile: which nodes are not finite)
@@ -429,9 +470,11 @@ __global__ void __launch_bounds__(THREADS, 1)
                 ks_ph ^= 1;
                 if (!ok) continue;
                 tc_fence_after();
-                if (is_fresh) {
+                if (is_fresh && ln == 0) {  // (the segment's last tile)
+                    unsigned long long vb = 0;
 #pragma unroll
                     for (int w = 0; w < (E4 ? 4 : 2); ++w) vb |= ((volatile unsigned long long *)bars->vbad[rv.slot])[w];
+                    bars->seg_vbad = vb;
                 }
                 if (!warp_active) {  // its lanes' weights reach no row that is used
                     arrive_warp(&bars->p_full[wg], lane);
@@ -460,7 +503,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                         }
                     }
                     if (masked) {
-                        const uint32_t bits = is_fresh ? (j0 < 64 ? (uint32_t)(sees >> j0) : 0u)
+                        const uint32_t bits = is_fresh ? (j0 < 64 ? (uint32_t)(((volatile unsigned long long *)(smem + OFF_SEES))[row_s] >> j0) : 0u)
                                               : n_tok - j0 >= 32 ? ~0u : n_tok > j0 ? (1u << (n_tok - j0)) - 1u : 0u;
 #pragma unroll
                         for (int e = 0; e < CH; ++e)
@@ -555,14 +598,14 @@ __global__ void __launch_bounds__(THREADS, 1)
 
             // ---- epilogue: the pipelines' (one M tile) and copies' parts of each row are
             // added; the output (the pair in one share) or a partial is written
+            const Seg sg = seg_at(prefix, B, xs, x1);
+            const int b = sg.b, n = nodes[b];
             const int j_first = group_of(cuts, n_grp, sg.xp), j_last = group_of(cuts, n_grp, sg.xp + sg.nt - 1);
             const bool whole = j_first == j_last;
             const int n1 = MT == 2 ? sg.n : sg.n >> 1;  // tiles of pipeline 1
             ml_s[wg * 128 + ln] = make_float2(m, l);
-            const bool has_fresh = sg.t_a + sg.n == sg.nt;
-            if (ln == 0 && (has_fresh ? MT == 2 || ((sg.n - 1) & 1) == wg : wg == 0)) bars->seg_vbad = vb;
             named_sync(BAR_EPI, SOFT);
-            const unsigned long long seg_vb = *(volatile unsigned long long *)&bars->seg_vbad;
+            const bool odd = sg.t_a + sg.n == sg.nt && *(volatile unsigned long long *)&bars->seg_vbad;  // uniform
             float a0, a1 = 0.f, mc, lsum;
             {
                 mc = -INFINITY;
@@ -589,84 +632,104 @@ __global__ void __launch_bounds__(THREADS, 1)
                     a1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - mu);
                 }
             }
-            ok = ok && mbar_wait_warp(&bars->pv_done, pv_ph, abort);
-            pv_ph ^= 1;
+            ok = ok && mbar_wait_warp(&bars->pv_done, seg_ph, abort);
+            seg_ph ^= 1;
             tc_fence_after();
             // slot of this segment's partial: a share has at most two, the pair that starts
             // in it and the one that began before
             const size_t slot = ((size_t)grp * 2 + (j_first == grp)) * Hv + hv;
             const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
-            // four dims of row q of the block: y unnormalised
-            auto write = [&](int q, int d, float4 y, float scale) {
+            // where row q of the block goes: the output, or the partial's row
+            auto dest = [&](int q, bool *on) {
                 const int qr = rb * a.rb_rows + q, nd = qr / a.G;
-                if (seg_vb && has_fresh && nd < n) y = add_non_finite(a, b, g, d, seg_vb & tree_mask(a, b, nd, n), y);
-                if (whole) {
-                    const bool on = nd < n && scale != 0.f;
-                    const size_t at = ((size_t)b * a.N + nd) * a.Hq * DH + (size_t)(g * a.G + qr - nd * a.G) * DH + d;
-                    *(uint2 *)((bf16 *)a.out + at) =
-                        on ? make_uint2(pack_bf16(y.x * scale, y.y * scale), pack_bf16(y.z * scale, y.w * scale)) : make_uint2(0, 0);
+                *on = nd < n;
+                return whole ? (uint8_t *)((bf16 *)a.out + (((size_t)b * a.N + nd) * a.Hq + (g * a.G + qr - nd * a.G)) * DH)
+                             : (uint8_t *)(a.part_o + (slot * a.rb_rows + q) * DH);
+            };
+            auto write = [&](uint8_t *to, bool on, int d, float4 y, float scale) {  // four dims, unnormalised
+                if (whole)
+                    *(uint2 *)(to + d * 2) = on && scale != 0.f ? make_uint2(pack_bf16(y.x * scale, y.y * scale),
+                                                                             pack_bf16(y.z * scale, y.w * scale))
+                                                                : make_uint2(0, 0);
+                else
+                    *(float4 *)(to + d * 4) = y;
+            };
+            // dims [d, d + W) of this lane's row: both pipelines' parts (one M tile)
+            auto parts = [&](int d, auto &o) {
+                constexpr int W = sizeof(o) / sizeof(float);
+                if (!ok) {
+#pragma unroll
+                    for (int e = 0; e < W; ++e) o[e] = 0.f;
+                } else if constexpr (MT == 2) {
+                    tmem_ldw<W>(o_col + d, o);
                 } else {
-                    *(float4 *)(a.part_o + (slot * a.rb_rows + q) * DH + d) = y;
+                    float o1[W];
+                    tmem_ldw<W>(lane_base + O_COL + d, o);
+                    if (n1 > 0) tmem_ldw<W>(lane_base + O_COL + DH + d, o1);
+#pragma unroll
+                    for (int e = 0; e < W; ++e) {
+                        // a part without a weight: its accumulator may hold anything
+                        const float y0 = a0 != 0.f ? a0 * o[e] : 0.f;
+                        o[e] = n1 > 0 && a1 != 0.f ? fmaf(a1, o1[e], y0) : y0;
+                    }
                 }
             };
-            const int d_lo = MT == 2 ? 0 : wg * (DH / 2), d_n = MT == 2 ? DH : DH / 2;
-            uint8_t *stage = smem + lay.off_q + wg * 16384;  // (queries are done with)
+            const int d_lo = MT == 2 ? 0 : wg * (DH / 2), d_hi = MT == 2 ? DH : d_lo + DH / 2;
+            if constexpr (NC == 1) {
+                bool on = false;
+                uint8_t *to = active ? dest(r, &on) : nullptr;
 #pragma unroll 1
-            for (int d0 = d_lo; d0 < d_lo + d_n; d0 += 32) {
-                float o[32];
-                if (ok) {
-                    if constexpr (MT == 2) {
-                        tmem_ld32(o_col + d0, o);
-                    } else {
-                        float o1[32];
-                        tmem_ld32(lane_base + O_COL + d0, o);
-                        if (n1 > 0) tmem_ld32(lane_base + O_COL + DH + d0, o1);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            // a part without a weight: its accumulator may hold anything
-                            const float y0 = a0 != 0.f ? a0 * o[e] : 0.f;
-                            o[e] = n1 > 0 && a1 != 0.f ? fmaf(a1, o1[e], y0) : y0;
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = 0.f;
-                }
-                if constexpr (NC == 1) {
+                for (int d = d_lo; d < d_hi; d += 16) {
+                    float o[16];
+                    parts(d, o);
                     if (active) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 4) write(r, d0 + e, make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]), inv);
+                        for (int e = 0; e < 16; e += 4) write(to, on, d + e, make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]), inv);
                     }
-                } else {
-                    // lane's 32 dims as 8 swizzled chunks; then (row, chunk) units add the copies
+                }
+            } else {
+                // 16 dims of every lane as four swizzled chunks; then (row, chunk) units add the copies
+                uint8_t *stage = smem + lay.off_st + wg * 8192;
+                if (cp == 0) l_s[wg * 128 + ln] = inv;
+#pragma unroll 1
+                for (int d = d_lo; d < d_hi; d += 16) {
+                    float o[16];
+                    parts(d, o);
 #pragma unroll
-                    for (int q4 = 0; q4 < 8; ++q4)
-                        st_shared_v4(stage + ln * 128 + ((q4 ^ (ln & 7)) << 4), __float_as_uint(o[4 * q4]),
-                                     __float_as_uint(o[4 * q4 + 1]), __float_as_uint(o[4 * q4 + 2]), __float_as_uint(o[4 * q4 + 3]));
-                    if (d0 == d_lo && cp == 0) l_s[wg * 128 + ln] = inv;
+                    for (int q = 0; q < 4; ++q)
+                        st_shared_v4(stage + ln * 64 + ((q ^ ((ln >> 1) & 3)) << 4), __float_as_uint(o[4 * q]),
+                                     __float_as_uint(o[4 * q + 1]), __float_as_uint(o[4 * q + 2]), __float_as_uint(o[4 * q + 3]));
                     named_sync(BAR_WG + wg, 128);
 #pragma unroll 1
-                    for (int it = ln; it < TPC * 8; it += 128) {
-                        const int q = it >> 3, q4 = it & 7;
+                    for (int it = ln; it < TPC * 4; it += 128) {
+                        const int q = it >> 2, c = it & 3;
                         if (q >= a.rb_rows || rb * a.rb_rows + q >= a.R) continue;
                         float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                        for (int c = 0; c < NC; ++c) {
-                            const int lc = c * TPC + q;
-                            const float4 v = ld_shared_v4f(stage + lc * 128 + ((q4 ^ (lc & 7)) << 4));
+                        for (int k = 0; k < NC; ++k) {
+                            const int lc = k * TPC + q;
+                            const float4 v = ld_shared_v4f(stage + lc * 64 + ((c ^ ((lc >> 1) & 3)) << 4));
                             y.x += v.x, y.y += v.y, y.z += v.z, y.w += v.w;
                         }
-                        write(q, d0 + q4 * 4, y, l_s[wg * 128 + q]);
+                        bool on;
+                        uint8_t *to = dest(q, &on);
+                        write(to, on, d + c * 4, y, l_s[wg * 128 + q]);
                     }
                     named_sync(BAR_WG + wg, 128);
                 }
             }
             if (!whole && active && cp == 0 && (MT == 2 || wg == 0))
                 *(float2 *)(a.part_ml + (slot * a.rb_rows + r) * 2) = make_float2(mc, lsum);
+            if (odd) {  // (uniform) values that were kept out of the product: to the rows that see them
+                named_sync(BAR_EPI, SOFT);
+                add_non_finite(a, b, g, rb, n, *(volatile unsigned long long *)&bars->seg_vbad, whole,
+                               a.part_o + slot * a.rb_rows * DH, threadIdx.x);
+            }
             tc_fence_before();
-            named_sync(BAR_EPI, SOFT);  // O, the queries' buffer and ml_s are free
+            named_sync(BAR_EPI, SOFT);  // both accumulators and ml_s are free
         }
     } else {
+        regs_dec<OTHER_REGS>();
         if (warp >= Ro::PROD && warp < Ro::PROD + 2 * Ro::RING_WARPS) {
             // ------------------------------------------------------------ producers
             constexpr int PT = Ro::RING_THREADS, ES = E4 ? 1 : 2, CH = DH * ES / 16;  // chunks a row
@@ -879,11 +942,17 @@ __global__ void __launch_bounds__(THREADS, 1)
             const int ct = threadIdx.x - CVT * 32, cw = warp - CVT;
             Ring rv(lay.nv), rc(CONV);
             bool ok = true;
+            uint32_t seg_ph = 0;
 #pragma unroll 1
-            for (int x = x0; ok && x < x1;) {
+            for (int x = x0; ok && x < x1; seg_ph ^= 1) {
                 const Seg sg = seg_at(prefix, B, x, x1);
                 x += sg.n;
                 const int b = sg.b, L = lens[b];
+                ok = mbar_wait_warp(&bars->q_empty, seg_ph ^ 1, abort);
+                if (!ok) break;
+                load_queries<E4, TPC, MT>(a, b, nodes[b], g, rb, smem + lay.off_q, (unsigned long long *)(smem + OFF_SEES) + seg_ph * 256,
+                                          (float *)(smem + OFF_RS) + seg_ph * 256, cw, 4, lane);
+                arrive_warp(&bars->q_full, lane);
 #pragma unroll 1
                 for (int i = 0; i < sg.n; ++i) {
                     const int t = sg.t_a + i;
@@ -979,6 +1048,19 @@ __global__ void __launch_bounds__(THREADS, 1)
                     rc.next();
                 }
             }
+        } else if (!E4 && warp >= Ro::Q_WARP && warp < Ro::Q_WARP + Ro::Q_WARPS) {
+            // ------------------------------------------------------------ queries
+            uint32_t seg_ph = 0;
+#pragma unroll 1
+            for (int x = x0; x < x1; seg_ph ^= 1) {
+                const Seg sg = seg_at(prefix, B, x, x1);
+                x += sg.n;
+                if (!mbar_wait_warp(&bars->q_empty, seg_ph ^ 1, abort)) break;
+                load_queries<E4, TPC, MT>(a, sg.b, nodes[sg.b], g, rb, smem + lay.off_q,
+                                          (unsigned long long *)(smem + OFF_SEES) + seg_ph * 256, nullptr, warp - Ro::Q_WARP,
+                                          Ro::Q_WARPS, lane);
+                arrive_warp(&bars->q_full, lane);
+            }
         } else if (warp == MMA) {
             // ------------------------------------------------------------ MMA issue
             // Items q of a segment in order: pipeline q & 1, on tile q (one M tile) or q / 2
@@ -1001,7 +1083,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             bool ok = true;
             uint32_t kp = 0;  // phases of p_full, a bit a pipeline
             int j = 0;
-            auto issue_s = [&](int q) {
+            auto issue_s = [&](int q, bool last_s) {
                 const int w = q & 1;
                 ok = ok && mbar_wait_warp(&bars->k_full[rk.slot], rk.ph, abort);
                 if (!ok) return;
@@ -1020,6 +1102,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                     }
                     if (MT == 1 || w) mma_commit(&bars->k_empty[rk.slot]);
                     mma_commit(&bars->s_full[w]);
+                    if (last_s) mma_commit(&bars->q_empty);  // (the segment's last scores)
                 }
                 __syncwarp();
                 if (MT == 1 || w) rk.next();
@@ -1056,7 +1139,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                         __syncwarp();
                         if (MT == 1 || w) rv.next();
                     }
-                    if (q + 2 < items) issue_s(q + 2);
+                    if (q + 2 < items) issue_s(q + 2, q + 3 == items);
                 }
             }
             if (on) mma_commit(&bars->fin);  // completes when every MMA is done
@@ -1130,6 +1213,8 @@ bool make_layout(const TreeArgs &a, bool e4, int mt, Layout *lay) {
     int at = lay->off_q + mt * Q_TILE;
     lay->off_c = at;
     if (e4) at += CONV * (SLOT16 + PARAMS);
+    lay->off_st = at;
+    at += 2 * 8192;
     const int room = SMEM_MAX - 1024 - at;
     const int slot = e4 ? SLOT8 : SLOT16;
     int slots = e4 ? (room - 1024) / (SLOT8 + SCALES) : room / SLOT16;
