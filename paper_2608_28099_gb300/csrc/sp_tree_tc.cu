@@ -53,8 +53,7 @@ namespace {
 constexpr int TILE = 128;                       // tokens of a key tile
 constexpr int SLOT16 = TILE * DH * 2;           // K or V of a tile in 16 bits, 32 KB
 constexpr int SLOT8 = TILE * DH;                // in 8 bits, 16 KB
-constexpr int SCALES = 2 * TILE * 4;            // k and v scales of a tile, behind its V codes
-constexpr int PARAMS = 3 * TILE * 4;            // (k scale, log2 v scale) pairs, 1 / v scale
+constexpr int PARAMS = 3 * TILE * 4;            // k scales and log2 v scales by pairs, 1 / v scale
 constexpr int Q_TILE = 128 * DH * 2;            // an M tile of queries: bf16, or two 8-bit parts
 constexpr int CONV = 2;                         // converted V slots
 constexpr int MAX_RING = 8;
@@ -90,15 +89,10 @@ constexpr int OFF_CUTS = OFF_RS + 2 * 256 * 4;
 constexpr int OFF_FRONT = OFF_CUTS + (MAX_GRP + 4) * 4;
 static_assert(sizeof(Bars) <= OFF_ML, "barrier block");
 
-// Warp roles: softmax 0-7, MMA 8; 8-bit caches: producers 10-11, converters 12-15 (queries
-// too; 9 idle); else queries 9-11, producers 12-15.
+// Warp roles: softmax 0-7, MMA 8; 8-bit caches: producers 9-11, converters 12-15 (queries
+// too); else queries 9-11, producers 12-15.
 constexpr int THREADS = 512;
 constexpr int MMA = 8, CVT = 12;
-// Registers a thread: the softmax warps take what the other roles leave of the launch's
-// 128 (8 x 144 + 8 x 112 = 16 x 128 a lane).  With 128 everywhere 50 to 350 bytes a thread
-// spill, more in all than the L1 that the shared memory leaves holds: a reload then waits
-// for the L2 behind the cache stream.
-constexpr int SOFT_REGS = 144, OTHER_REGS = 112;
 template <int N>
 __device__ __forceinline__ void regs_inc() {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
@@ -109,10 +103,13 @@ __device__ __forceinline__ void regs_dec() {
 }
 template <bool E4>
 struct Roles {
-    static constexpr int RING_WARPS = E4 ? 1 : 2;                    // producers of a ring
-    static constexpr int RING_THREADS = RING_WARPS * 32;
-    static constexpr int PROD = E4 ? 10 : 12;
-    static constexpr int Q_WARP = E4 ? CVT : 9, Q_WARPS = E4 ? 4 : 3;  // load the queries
+    static constexpr int K_WARP = E4 ? 9 : 12, V_WARP = K_WARP + 2, V_WARPS = E4 ? 1 : 2;  // producers
+    static constexpr int Q_WARP = E4 ? CVT : 9, Q_WARPS = E4 ? 4 : 3;                       // load the queries
+    // Registers a thread: the softmax warps take what the other roles leave of the launch's
+    // 128 (8 x 144 + 8 x 112 = 8 x 160 + 8 x 96 = 16 x 128 a lane).  With 128 everywhere 50 to
+    // 350 bytes a thread spill, more in all than the L1 that the shared memory leaves holds: a
+    // reload then waits for the L2 behind the cache stream.  So: 0 (bf16), at most 8.
+    static constexpr int SOFT_REGS = E4 ? 144 : 160, OTHER_REGS = E4 ? 112 : 96;
 };
 // One arrival of a warp whose lanes have all done their part.
 __device__ __forceinline__ void arrive_warp(uint64_t *bar, int lane) {
@@ -120,7 +117,38 @@ __device__ __forceinline__ void arrive_warp(uint64_t *bar, int lane) {
     if (lane == 0) mbar_arrive(bar);
 }
 
-// ---- TMEM stores without a wait behind every one ------------------------------
+// ---- TMEM accesses without a wait behind every one ----------------------------
+__device__ __forceinline__ void ld32_async(uint32_t addr, float *v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
+          "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]),
+          "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]),
+          "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+        : "r"(addr));
+}
+// Earlier loads complete; 32 of their values are named so that no use moves in front.
+__device__ __forceinline__ void ld_wait(float *v) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                   "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14])
+                 :
+                 : "memory");
+    asm volatile(""
+                 : "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]),
+                   "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]));
+    asm volatile("" : "+f"(v[29]), "+f"(v[30]), "+f"(v[31]));
+}
+template <int N>
+__device__ __forceinline__ void load_cols(uint32_t addr, float (&v)[N]) {  // N columns, complete
+    static_assert(N == 32 || N == 64, "");
+    ld32_async(addr, v);
+    if constexpr (N == 64) ld32_async(addr + 32, v + 32);
+    ld_wait(v);
+    if constexpr (N == 64) ld_wait(v + 32);
+}
 __device__ __forceinline__ void st16_async(uint32_t addr, const float *v) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
@@ -174,9 +202,6 @@ __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t b
         "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
         "l"(src), "r"(bytes), "r"(smem_u32(bar))
         : "memory");
-}
-__device__ __forceinline__ void cp_async4(void *dst, const void *src) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
 }
 __device__ __forceinline__ void expect_tx(uint64_t *bar, uint32_t bytes) {
     asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
@@ -271,6 +296,9 @@ __device__ __forceinline__ uint32_t codes2_to_half2(uint32_t w, int hi) {
         : "r"(hi ? w >> 16 : w));
     return h;
 }
+// A tile's constants: for tokens 2 i, 2 i + 1 their k scales, then log2 of their v scales
+// (operand pairs of two-wide instructions); this is token t's k scale.
+__device__ __forceinline__ int par_at(int t) { return 4 * (t >> 1) + (t & 1); }
 // byte offset of 16-byte chunk c (0..7) of row r of an 8-bit tile (128-byte rows, swizzled)
 __device__ __forceinline__ uint32_t off8(int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); }
 
@@ -344,6 +372,23 @@ __device__ __forceinline__ void add_non_finite(const TreeArgs &a, int b, int g, 
     }
 }
 
+// n cached rows (`step` bytes apart) into rows r0 .. of a slot in the MMA's layout, 16 bytes
+// at a time by 64 threads: zeros if there is no source.  A thread keeps its chunk of the row
+// and walks rows 8 (8-bit) or 4 apart, so that addresses advance by constants.
+template <bool E4>
+__device__ __forceinline__ void copy_rows(uint8_t *dst, int r0, int n, const uint8_t *src, size_t step, bool have, int t) {
+    constexpr int CH = E4 ? 8 : 16, APART = 64 / CH;
+    const int c = t & (CH - 1), r = t / CH;
+    src += (size_t)r * step + c * 16;
+    const size_t hop = step * APART;
+#pragma unroll 4
+    for (int i = r; i < n; i += APART, src += hop) {
+        uint8_t *d = dst + (E4 ? off8(r0 + i, c) : kv_off(r0 + i, c));
+        if (have) cp_async16(d, src);
+        else st_shared_v4(d, 0, 0, 0, 0);
+    }
+}
+
 // ---------------------------------------------------------------------------
 // TPC: rows of a copy, and tokens of a tile that a copy weighs (32, 64, 128); MT: M tiles.
 template <bool E4, int TPC, int MT>
@@ -365,6 +410,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     int *prefix = (int *)(smem + lay.off_tab), *sids = prefix + B + 1, *lens = sids + B, *nodes = lens + B;
     const bool paged = a.cache.kv.layout == SP_KV_PAGED;
     const int P = a.cache.kv.page_size;
+    constexpr int ROW = DH * (E4 ? 1 : 2);  // bytes of a cached row
     // the first kernel of its call: nothing of the caller's is read before
     pdl_wait();
     pdl_trigger();
@@ -378,12 +424,12 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (threadIdx.x == THREADS - 1) {
 #pragma unroll 1
         for (int i = 0; i < lay.nk; ++i) {
-            mbar_init(&bars->k_full[i], Ro::RING_THREADS);
+            mbar_init(&bars->k_full[i], 64);
             mbar_init(&bars->k_empty[i], 1);
         }
 #pragma unroll 1
         for (int i = 0; i < lay.nv; ++i) {
-            mbar_init(&bars->v_full[i], Ro::RING_THREADS);
+            mbar_init(&bars->v_full[i], Ro::V_WARPS * 32);
             mbar_init(&bars->v_empty[i], E4 ? 4 : 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -401,7 +447,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         fence_mbar_init();
         if (paged) {
             prefetch_tmap(&map_k);
-            prefetch_tmap(&map_v);
+            if (!E4) prefetch_tmap(&map_v);
         }
     }
     if (warp == MMA) {
@@ -422,7 +468,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
 
     if (warp < 8) {
-        regs_inc<SOFT_REGS>();
+        regs_inc<Ro::SOFT_REGS>();
         // ------------------------------------------------------------ softmax + epilogue
         const int wg = warp >> 2, ln = threadIdx.x & 127;  // pipeline; TMEM lane
         const int cp = ln / TPC, row_t = ln - cp * TPC;    // copy, row of the M tile
@@ -483,54 +529,63 @@ __global__ void __launch_bounds__(THREADS, 1)
                 }
                 const float *par = (const float *)(smem + lay.off_c + CONV * SLOT16 + rv.slot * PARAMS);
                 const bool masked = is_fresh || n_tok < TILE;
-                constexpr int CH = 32, N_CH = TPC / CH;  // columns in registers at a time
+                constexpr int CH = TPC == 128 && !E4 ? 64 : 32, N_CH = TPC / CH;  // columns in registers at a time
                 const int tok0 = cp * TPC;  // this copy's first token
                 // Columns [j0, j0 + CH) of S; 8-bit: in log2 units, with log2 of the value's scale.
                 auto scores = [&](int j0, float (&s)[CH]) {
-                    tmem_ld32(s_col + (uint32_t)j0, s);
+                    load_cols<CH>(s_col + (uint32_t)j0, s);
                     if constexpr (E4) {
                         if (is_fresh && j0 < 64) {  // the keys' second parts
-                            float s2[CH];
-                            tmem_ld32(s_col + (uint32_t)(64 + j0), s2);
 #pragma unroll
-                            for (int e = 0; e < CH; ++e) s[e] += s2[e];
+                            for (int h = 0; h < CH; h += 32) {
+                                float s2[32];
+                                load_cols<32>(s_col + (uint32_t)(64 + j0 + h), s2);
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) s[h + e] += s2[e];
+                            }
                         }
+                        const float *pj = par + 2 * j0;
 #pragma unroll
                         for (int e = 0; e < CH; e += 2) {
-                            const float4 p2 = *(const float4 *)(par + 2 * (j0 + e));
+                            const float4 p2 = *(const float4 *)(pj + 2 * e);
                             mul2(s[e], s[e + 1], s[e], s[e + 1], rs, rs);
-                            fma2(s[e], s[e + 1], s[e], s[e + 1], p2.x, p2.z, p2.y, p2.w);
+                            fma2(s[e], s[e + 1], s[e], s[e + 1], p2.x, p2.y, p2.z, p2.w);
                         }
                     }
                     if (masked) {
-                        const uint32_t bits = is_fresh ? (j0 < 64 ? (uint32_t)(((volatile unsigned long long *)(smem + OFF_SEES))[row_s] >> j0) : 0u)
-                                              : n_tok - j0 >= 32 ? ~0u : n_tok > j0 ? (1u << (n_tok - j0)) - 1u : 0u;
 #pragma unroll
-                        for (int e = 0; e < CH; ++e)
-                            if (!((bits >> e) & 1)) s[e] = -INFINITY;
+                        for (int h = 0; h < CH; h += 32) {
+                            const int j = j0 + h;
+                            const uint32_t bits =
+                                is_fresh ? (j < 64 ? (uint32_t)(((volatile unsigned long long *)(smem + OFF_SEES))[row_s] >> j) : 0u)
+                                : n_tok - j >= 32 ? ~0u : n_tok > j ? (1u << (n_tok - j)) - 1u : 0u;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!((bits >> e) & 1)) s[h + e] = -INFINITY;
+                        }
                     }
                 };
                 float s[CH];
                 float mt = -INFINITY;
-#pragma unroll
+#pragma unroll 1
                 for (int c = 0; c < N_CH; ++c) {
                     scores(tok0 + c * CH, s);
                     float mx[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) mx[e] = s[e];
+                    for (int e = 0; e < 8; ++e) mx[e] = fmaxf(s[e], s[e + 8]);
 #pragma unroll
-                    for (int h = 8; h < CH; h += 8)
+                    for (int h = 16; h < CH; h += 16)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) mx[e] = fmaxf(mx[e], s[h + e]);
+                        for (int e = 0; e < 8; ++e) mx[e] = fmaxf(mx[e], fmaxf(s[h + e], s[h + 8 + e]));
                     mt = fmaxf(mt, fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])),
                                          fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7]))));
                     // more than fits the registers: scores go back to where they came from
                     if (N_CH > 1 && (E4 || masked)) {
 #pragma unroll
                         for (int h = 0; h < CH; h += 16) st16_async(s_col + (uint32_t)(tok0 + c * CH + h), s + h);
-                        st_wait();
                     }
                 }
+                if (N_CH > 1 && (E4 || masked)) st_wait();
                 if constexpr (!E4) mt *= a.scale_log2;
                 const bool grow = mt > m + RESCALE_LOG2 || (m == -INFINITY && mt != -INFINITY);
                 const float m_new = grow ? mt : m;
@@ -540,7 +595,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll 1
                     for (int c0 = 0; c0 < DH; c0 += 32) {
                         float o[32];
-                        tmem_ld32(o_col + c0, o);
+                        load_cols<32>(o_col + c0, o);
 #pragma unroll
                         for (int e = 0; e < 32; ++e) o[e] *= alpha;
                         st16_async(o_col + c0, o);
@@ -553,9 +608,9 @@ __global__ void __launch_bounds__(THREADS, 1)
                 first = false;
                 const float mu = m == -INFINITY ? 0.f : m;  // a row that sees nothing: weights of 0
                 float ps[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
+#pragma unroll 1
                 for (int c = 0; c < N_CH; ++c) {
-                    if constexpr (N_CH > 1) tmem_ld32(s_col + (uint32_t)(tok0 + c * CH), s);
+                    if constexpr (N_CH > 1) load_cols<CH>(s_col + (uint32_t)(tok0 + c * CH), s);
                     float pk[CH / 2];
 #pragma unroll
                     for (int e = 0; e < CH; e += 4) {
@@ -729,22 +784,18 @@ __global__ void __launch_bounds__(THREADS, 1)
             named_sync(BAR_EPI, SOFT);  // both accumulators and ml_s are free
         }
     } else {
-        regs_dec<OTHER_REGS>();
-        if (warp >= Ro::PROD && warp < Ro::PROD + 2 * Ro::RING_WARPS) {
+        regs_dec<Ro::OTHER_REGS>();
+        if (warp >= Ro::K_WARP && warp < Ro::V_WARP + Ro::V_WARPS) {
             // ------------------------------------------------------------ producers
-            constexpr int PT = Ro::RING_THREADS, ES = E4 ? 1 : 2, CH = DH * ES / 16;  // chunks a row
-            const bool is_v = (warp - Ro::PROD) & 1;
-            const int pidx = (warp - Ro::PROD) >> 1, ptid = pidx * 32 + lane;
-            const bool lead = pidx == 0;
+            const bool is_v = warp >= Ro::V_WARP;
+            const int pidx = warp - (is_v ? Ro::V_WARP : Ro::K_WARP), ptid = pidx * 32 + lane;
+            const bool lead = pidx == 0, rows8 = E4 && is_v;  // (rows8: V's codes, plain rows of 128 bytes)
             uint64_t *full = is_v ? bars->v_full : bars->k_full, *empty = is_v ? bars->v_empty : bars->k_empty;
-            const int slot_bytes = E4 ? SLOT8 + (is_v ? SCALES : 0) : SLOT16;
+            const int slot_bytes = E4 ? SLOT8 : SLOT16;
             uint8_t *ring = smem + (is_v ? lay.off_v : lay.off_k);
             const CUtensorMap *map = is_v ? &map_v : &map_k;
             const uint8_t *pool = (const uint8_t *)(is_v ? a.cache.kv.v_pool : a.cache.kv.k_pool);
-            const bf16 *fresh = (const bf16 *)(is_v ? a.v_new : a.k_new);
-            const long long fs = is_v ? a.vs : a.ks;
             const uint64_t pol = policy_evict_first();
-            auto dst_off = [](int r, int c) { return E4 ? off8(r, c) : kv_off(r, c); };
             Ring rg(is_v ? lay.nv : lay.nk);
             int bad = 0, filled = 0;
             bool stop = false;
@@ -753,16 +804,11 @@ __global__ void __launch_bounds__(THREADS, 1)
                 const Seg sg = seg_at(prefix, B, x, x1);
                 x += sg.n;
                 const int b = sg.b, sid = sids[b], L = lens[b];
-                // a contiguous sequence's rows: Hkv rows a token
+                // a contiguous sequence's rows of head g, a token apart
                 const uint8_t *seq = nullptr;
-                const float *seq_scale[2] = {nullptr, nullptr};
-                if (!paged && L > 0) {
-                    seq = (const uint8_t *)(is_v ? a.cache.kv.v_seq : a.cache.kv.k_seq)[sid];
-                    if (E4 && is_v) {
-                        seq_scale[0] = ((const float *const *)a.cache.k_scale)[sid];
-                        seq_scale[1] = ((const float *const *)a.cache.v_scale)[sid];
-                    }
-                }
+                if (!paged && L > 0)
+                    seq = (const uint8_t *)(is_v ? a.cache.kv.v_seq : a.cache.kv.k_seq)[sid] + (size_t)g * ROW;
+                const size_t seq_step = (size_t)Hkv * ROW;
 #pragma unroll 1
                 for (int i = 0; i < sg.n; ++i) {
                     const int t = sg.t_a + i, t0 = t * TILE;
@@ -781,141 +827,125 @@ __global__ void __launch_bounds__(THREADS, 1)
                         break;
                     }
                     uint8_t *dst = ring + rg.slot * slot_bytes;
-                    uint8_t *sc = dst + SLOT8;  // (E4 && is_v)
-                    bool plain = false;         // this thread wrote shared memory or issued cp.async
-                    if (n_pg > 0 && lead) {
-                        const bool ok = lane < n_pg && page >= 0;
-                        const unsigned okm = __ballot_sync(0xffffffffu, ok);
-                        const uint32_t bytes = (uint32_t)(P * DH * ES + (E4 && is_v ? P * 8 : 0));
-                        if (lane == 0 && okm) expect_tx(&full[rg.slot], __popc(okm) * bytes);
-                        __syncwarp();
-                        if (ok) {  // the cache is read once: evict-first keeps queries and partials in L2
-                            const int row = page * Hkv + g;
-                            if constexpr (E4) {
-                                tma_load_2d_hint(dst + lane * P * DH, map, &full[rg.slot], 0, row * P, pol);
-                                if (is_v) {
-                                    const size_t at = (size_t)row * P;
-                                    bulk_load(sc + lane * P * 4, (const float *)a.cache.k_scale + at, P * 4, &full[rg.slot]);
-                                    bulk_load(sc + TILE * 4 + lane * P * 4, (const float *)a.cache.v_scale + at, P * 4,
-                                              &full[rg.slot]);
-                                }
-                            } else {
-                                tma_load_4d_hint(dst + lane * P * 256, map, &full[rg.slot], 0, 0, 0, row * (P / 8), pol);
-                            }
-                        }
-                        // a page outside the pool: zeros
+                    bool plain = false;  // this thread wrote shared memory or issued cp.async
+                    if (rows8) {
+                        // V's codes as they lie: a bulk copy a page (a copy a row of a
+                        // contiguous cache took 60 cycles to issue each), else cp.async
+                        if (paged) {
+                            const int rows = min(P, n_tok - lane * P);  // of this lane's page
+                            const bool ok = rows > 0 && page >= 0;
+                            const unsigned bytes = __reduce_add_sync(0xffffffffu, ok ? rows * ROW : 0);
+                            if (lane == 0 && bytes) expect_tx(&full[rg.slot], bytes);
+                            __syncwarp();
+                            if (ok) {
+                                bulk_load(dst + lane * P * ROW, pool + ((size_t)page * Hkv + g) * P * ROW, rows * ROW, &full[rg.slot]);
+                            } else if (rows > 0) {  // a page outside the pool: zeros
+                                plain = true;
 #pragma unroll 1
-                        for (unsigned miss = ~okm & ((1u << n_pg) - 1u); miss; miss &= miss - 1) {
-                            const int j = __ffs(miss) - 1;
-#pragma unroll 1
-                            for (int e = lane; e < P * CH; e += 32) st_shared_v4(dst + j * P * DH * ES + e * 16, 0, 0, 0, 0);
-                            if (E4 && is_v && lane < P / 4) {
-                                st_shared_v4(sc + j * P * 4 + lane * 16, 0, 0, 0, 0);
-                                st_shared_v4(sc + TILE * 4 + j * P * 4 + lane * 16, 0, 0, 0, 0);
+                                for (int e = 0; e < rows * 8; ++e) st_shared_v4(dst + lane * P * ROW + e * 16, 0, 0, 0, 0);
                             }
+                        } else if (n_tok > 0) {
                             plain = true;
+                            const int c = lane & 7;
+                            const uint8_t *src = seq + (size_t)(t0 + (lane >> 3)) * seq_step + c * 16;
+                            uint8_t *d = dst + lane * 16;
+                            const size_t hop = 4 * seq_step;
+#pragma unroll 8
+                            for (int r = lane >> 3; r < n_tok; r += 4, src += hop, d += 512) cp_async16(d, src);
                         }
-                    }
-                    if (!is_fresh) {
+                    } else {
+                        if (n_pg > 0 && lead) {
+                            const bool ok = lane < n_pg && page >= 0;
+                            const unsigned okm = __ballot_sync(0xffffffffu, ok);
+                            if (lane == 0 && okm) expect_tx(&full[rg.slot], __popc(okm) * P * ROW);
+                            __syncwarp();
+                            if (ok) {  // the cache is read once: evict-first keeps queries and partials in L2
+                                const int row = page * Hkv + g;
+                                if constexpr (E4) tma_load_2d_hint(dst + lane * P * ROW, map, &full[rg.slot], 0, row * P, pol);
+                                else tma_load_4d_hint(dst + lane * P * ROW, map, &full[rg.slot], 0, 0, 0, row * (P / 8), pol);
+                            }
+                            // a page outside the pool: zeros
+#pragma unroll 1
+                            for (unsigned miss = ~okm & ((1u << n_pg) - 1u); miss; miss &= miss - 1) {
+                                const int j = __ffs(miss) - 1;
+#pragma unroll 1
+                                for (int e = lane; e < P * ROW / 16; e += 32) st_shared_v4(dst + j * P * ROW + e * 16, 0, 0, 0, 0);
+                                plain = true;
+                            }
+                        }
                         const int r0 = n_pg * (paged ? P : 0);  // first row not covered by TMA
                         if (r0 < n_tok) {
                             plain = true;
+                            const uint8_t *src = seq + (size_t)t0 * seq_step;
+                            size_t step = seq_step;
+                            bool have = true;
                             if (paged) {  // the last, partial page
                                 const int pg = __shfl_sync(0xffffffffu, page, n_pg);
-                                const size_t at = ((size_t)max(pg, 0) * Hkv + g) * P;
-#pragma unroll 1
-                                for (int idx = ptid; idx < (n_tok - r0) * CH; idx += PT) {
-                                    const int r = idx / CH, c = idx - r * CH;
-                                    if (pg >= 0) cp_async16(dst + dst_off(r0 + r, c), pool + (at + r) * (DH * ES) + c * 16);
-                                    else st_shared_v4(dst + dst_off(r0 + r, c), 0, 0, 0, 0);
-                                }
-                                if (E4 && is_v) {
-#pragma unroll 1
-                                    for (int r = ptid; r < n_tok - r0; r += PT) {
-                                        if (pg >= 0) {
-                                            cp_async4(sc + (r0 + r) * 4, (const float *)a.cache.k_scale + at + r);
-                                            cp_async4(sc + (TILE + r0 + r) * 4, (const float *)a.cache.v_scale + at + r);
-                                        } else {
-                                            *(float *)(sc + (r0 + r) * 4) = 0.f;
-                                            *(float *)(sc + (TILE + r0 + r) * 4) = 0.f;
-                                        }
-                                    }
-                                }
-                            } else {
-                                const uint8_t *src = seq + ((size_t)t0 * Hkv + g) * (DH * ES);
-#pragma unroll 4
-                                for (int idx = ptid; idx < n_tok * CH; idx += PT) {
-                                    const int r = idx / CH, c = idx - r * CH;
-                                    cp_async16(dst + dst_off(r, c), src + (size_t)r * Hkv * (DH * ES) + c * 16);
-                                }
-                                if (E4 && is_v) {
-#pragma unroll 1
-                                    for (int r = ptid; r < n_tok; r += PT) {
-                                        const size_t at = (size_t)(t0 + r) * Hkv + g;
-                                        cp_async4(sc + r * 4, seq_scale[0] + at);
-                                        cp_async4(sc + (TILE + r) * 4, seq_scale[1] + at);
-                                    }
-                                }
+                                have = pg >= 0;
+                                src = pool + ((size_t)max(pg, 0) * Hkv + g) * P * ROW;
+                                step = ROW;
                             }
+                            copy_rows<E4>(dst, r0, n_tok - r0, src, step, have, ptid);
                         }
                         // values past the end are multiplied by weights of 0: they must be
                         // finite (keys there give scores that are replaced)
-                        if (!E4 && is_v && n_tok < TILE) {
+                        if (!E4 && is_v && !is_fresh && n_tok < TILE) {
                             plain = true;
 #pragma unroll 1
-                            for (int idx = ptid; idx < (TILE - n_tok) * CH; idx += PT)
-                                st_shared_v4(dst + kv_off(n_tok + idx / CH, idx % CH), 0, 0, 0, 0);
+                            for (int idx = ptid; idx < (TILE - n_tok) * 16; idx += 64)
+                                st_shared_v4(dst + kv_off(n_tok + (idx >> 4), idx & 15), 0, 0, 0, 0);
                         }
-                    } else if (!E4 || !is_v) {
-                        // the nodes' rows: 16 lanes a row, 8 elements a lane
-                        plain = true;
-                        const int n = nodes[b], c = lane & 15;
-                        unsigned long long vb = 0;
+                        if (is_fresh) {
+                            // the nodes' rows: 16 lanes a row, 8 elements a lane
+                            plain = true;
+                            const bf16 *fresh = (const bf16 *)(is_v ? a.v_new : a.k_new) + (size_t)g * DH;
+                            const long long fs = is_v ? a.vs : a.ks;
+                            const int n = nodes[b], c = lane & 15;
+                            unsigned long long vb = 0;
 #pragma unroll 2
-                        for (int r = pidx * 2 + (lane >> 4); r < 64; r += 2 * Ro::RING_WARPS) {
-                            uint4 u = make_uint4(0, 0, 0, 0);
-                            if (r < n) u = *(const uint4 *)(fresh + ((size_t)b * a.N + r) * fs + (size_t)g * DH + c * 8);
-                            if constexpr (!E4) {
-                                if (is_v) {
-                                    uint32_t w[4] = {u.x, u.y, u.z, u.w};
-                                    bool odd = false;
+                            for (int r = pidx * 2 + (lane >> 4); r < 64; r += 4) {
+                                uint4 u = make_uint4(0, 0, 0, 0);
+                                if (r < n) u = *(const uint4 *)(fresh + ((size_t)b * a.N + r) * fs + c * 8);
+                                uint32_t w[4] = {u.x, u.y, u.z, u.w};
+                                if constexpr (!E4) {
+                                    if (is_v) {
+                                        bool odd = false;
+#pragma unroll
+                                        for (int q = 0; q < 4; ++q) {
+                                            const bool lo = (w[q] & 0x7f80u) == 0x7f80u, hi = (w[q] & 0x7f800000u) == 0x7f800000u;
+                                            odd = odd || lo || hi;
+                                            w[q] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+                                        }
+                                        const unsigned o = __ballot_sync(0xffffffffu, odd);
+                                        const int even = r & ~1;  // (lanes 0-15 hold the even row)
+                                        if (o & 0xffffu) vb |= 1ull << even;
+                                        if (o >> 16) vb |= 2ull << even;
+                                    }
+                                    st_shared_v4(dst + kv_off(r, c), w[0], w[1], w[2], w[3]);
+                                } else {
+                                    // keys as two 8-bit parts, rows r and 64 + r
+                                    float v[8];
+                                    float amax = 0.f;
 #pragma unroll
                                     for (int q = 0; q < 4; ++q) {
-                                        const bool lo = (w[q] & 0x7f80u) == 0x7f80u, hi = (w[q] & 0x7f800000u) == 0x7f800000u;
-                                        odd = odd || lo || hi;
-                                        w[q] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+                                        v[2 * q] = __uint_as_float(w[q] << 16);
+                                        v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
+                                        amax = fmaxf(amax, fmaxf(fabsf(v[2 * q]), fabsf(v[2 * q + 1])));
                                     }
-                                    u = make_uint4(w[0], w[1], w[2], w[3]);
-                                    const unsigned o = __ballot_sync(0xffffffffu, odd);
-                                    const int even = r & ~1;  // (lanes 0-15 hold the even row)
-                                    if (o & 0xffffu) vb |= 1ull << even;
-                                    if (o >> 16) vb |= 2ull << even;
+#pragma unroll
+                                    for (int o = 1; o < 16; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+                                    int k;
+                                    const float f = pow2_scale(amax, &k);
+#pragma unroll
+                                    for (int q = 0; q < 8; ++q) v[q] *= f;
+                                    uint2 hi, lo;
+                                    split_codes(v, &hi, &lo);
+                                    *(uint2 *)(dst + off8(r, c >> 1) + (c & 1) * 8) = hi;
+                                    *(uint2 *)(dst + off8(64 + r, c >> 1) + (c & 1) * 8) = lo;
                                 }
-                                st_shared_v4(dst + kv_off(r, c), u.x, u.y, u.z, u.w);
-                            } else {
-                                // keys as two 8-bit parts, rows r and 64 + r
-                                float v[8];
-                                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-                                float amax = 0.f;
-#pragma unroll
-                                for (int q = 0; q < 4; ++q) {
-                                    v[2 * q] = __uint_as_float(w[q] << 16);
-                                    v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
-                                    amax = fmaxf(amax, fmaxf(fabsf(v[2 * q]), fabsf(v[2 * q + 1])));
-                                }
-#pragma unroll
-                                for (int o = 1; o < 16; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-                                int k;
-                                const float f = pow2_scale(amax, &k);
-#pragma unroll
-                                for (int q = 0; q < 8; ++q) v[q] *= f;
-                                uint2 hi, lo;
-                                split_codes(v, &hi, &lo);
-                                *(uint2 *)(dst + off8(r, c >> 1) + (c & 1) * 8) = hi;
-                                *(uint2 *)(dst + off8(64 + r, c >> 1) + (c & 1) * 8) = lo;
                             }
+                            if (!E4 && is_v && lane == 0) bars->vbad[rg.slot][pidx] = vb;
                         }
-                        if (!E4 && is_v && lane == 0) bars->vbad[rg.slot][pidx] = vb;
                     }
                     if (plain) {
                         fence_proxy_async();  // this thread's shared-memory stores
@@ -929,7 +959,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
             asm volatile("cp.async.wait_all;" ::: "memory");  // nothing lands after the CTA is gone
             if (lead && lane == 0) {
-                // drain TMA writes still in flight (only possible after an abort)
+                // drain copies still in flight (only possible after an abort)
                 Ring rd(rg.n);
 #pragma unroll 1
                 for (int j = 0; j < filled; ++j, rd.next())
@@ -953,6 +983,27 @@ __global__ void __launch_bounds__(THREADS, 1)
                 load_queries<E4, TPC, MT>(a, b, nodes[b], g, rb, smem + lay.off_q, (unsigned long long *)(smem + OFF_SEES) + seg_ph * 256,
                                           (float *)(smem + OFF_RS) + seg_ph * 256, cw, 4, lane);
                 arrive_warp(&bars->q_full, lane);
+                // this thread's token of a tile: its scales are asked for a tile ahead, where they
+                // sit (a page table entry) two tiles ahead
+                const int sid = sids[b];
+                const float *sk = nullptr, *sv = nullptr;
+                if (L > 0) {
+                    sk = scale_base(a.cache, sid, 0) + (paged ? (size_t)g * P : g);
+                    sv = scale_base(a.cache, sid, 1) + (paged ? (size_t)g * P : g);
+                }
+                auto place = [&](int i) {  // -1: no such token, or no page
+                    const int tok = (sg.t_a + i) * TILE + ct;
+                    if (i >= sg.n || tok >= L) return -1ll;
+                    if (!paged) return (long long)tok * Hkv;
+                    const int lp = tok / P;
+                    const int page = lp < a.cache.kv.max_pages ? __ldg(a.cache.kv.page_table + (size_t)sid * a.cache.kv.max_pages + lp) : -1;
+                    return page < 0 || page >= a.cache.kv.n_pages ? -1ll : (long long)page * Hkv * P + (tok - lp * P);
+                };
+                auto scales = [&](long long at) {
+                    return at < 0 ? make_float2(0.f, 0.f) : make_float2(__ldg(sk + at), __ldg(sv + at));
+                };
+                float2 next = scales(place(0));
+                long long at = place(1);
 #pragma unroll 1
                 for (int i = 0; i < sg.n; ++i) {
                     const int t = sg.t_a + i;
@@ -961,24 +1012,28 @@ __global__ void __launch_bounds__(THREADS, 1)
                     ok = mbar_wait_warp(&bars->v_full[rv.slot], rv.ph, abort) &&
                          mbar_wait_warp(&bars->c_empty[rc.slot], rc.ph ^ 1, abort);
                     if (!ok) break;
-                    const uint8_t *src = smem + lay.off_v + rv.slot * (SLOT8 + SCALES);
+                    const float2 sc = next;
+                    next = scales(at);
+                    at = place(i + 2);
+                    const uint8_t *src = smem + lay.off_v + rv.slot * SLOT8;
                     uint8_t *dst = smem + lay.off_c + rc.slot * SLOT16;
                     float *par = (float *)(smem + lay.off_c + CONV * SLOT16 + rc.slot * PARAMS);
                     if (!is_fresh) {
                         // the softmax's constants first: it does not wait for the values
                         float ks = 0.f, vs = 1.f;
                         if (ct < n_tok) {
-                            ks = ((const float *)(src + SLOT8))[ct];
-                            vs = fmaxf(((const float *)(src + SLOT8))[TILE + ct], 7.888609052210118e-31f);  // 2^-100
+                            ks = sc.x;
+                            vs = fmaxf(sc.y, 7.888609052210118e-31f);  // 2^-100
                         }
-                        *(float2 *)(par + 2 * ct) = make_float2(ks * a.scale_log2, __log2f(vs));
+                        par[par_at(ct)] = ks * a.scale_log2;
+                        par[par_at(ct) + 2] = __log2f(vs);
                         par[2 * TILE + ct] = __frcp_rn(vs);
                         arrive_warp(&bars->c_par[rc.slot], lane);
                         uint4 u[8];
 #pragma unroll
                         for (int it = 0; it < 8; ++it) {
                             const int r = it * 16 + (ct >> 3);
-                            u[it] = r < n_tok ? *(const uint4 *)(src + off8(r, ct & 7)) : make_uint4(0, 0, 0, 0);
+                            u[it] = r < n_tok ? *(const uint4 *)(src + r * 128 + (ct & 7) * 16) : make_uint4(0, 0, 0, 0);
                         }
 #pragma unroll
                         for (int it = 0; it < 8; ++it) {
@@ -1033,8 +1088,8 @@ __global__ void __launch_bounds__(THREADS, 1)
                                          pack_half(v[4] * f, v[5] * f), pack_half(v[6] * f, v[7] * f));
                             if (c == 0) {
                                 // an infinite key saturates in its parts: its scores are NaN
-                                par[2 * r] = pow2i(-kk) * a.scale_log2 + (amk - amk);
-                                par[2 * r + 1] = (float)-kv;
+                                par[par_at(r)] = pow2i(-kk) * a.scale_log2 + (amk - amk);
+                                par[par_at(r) + 2] = (float)-kv;
                                 par[2 * TILE + r] = pow2i(kv);
                             }
                         }
@@ -1217,14 +1272,14 @@ bool make_layout(const TreeArgs &a, bool e4, int mt, Layout *lay) {
     at += 2 * 8192;
     const int room = SMEM_MAX - 1024 - at;
     const int slot = e4 ? SLOT8 : SLOT16;
-    int slots = e4 ? (room - 1024) / (SLOT8 + SCALES) : room / SLOT16;
+    int slots = (e4 ? room - 1024 : room) / slot;
     if (slots < 2) return false;
     if (slots > 2 * MAX_RING) slots = 2 * MAX_RING;
     lay->nk = slots / 2;
     lay->nv = slots - lay->nk;
     lay->off_k = (at + 1023) & ~1023;
     lay->off_v = lay->off_k + lay->nk * slot;
-    lay->smem = lay->off_v + lay->nv * (slot + (e4 ? SCALES : 0)) + 1024;
+    lay->smem = lay->off_v + lay->nv * slot + 1024;
     return lay->smem <= SMEM_MAX;
 }
 
@@ -1278,7 +1333,7 @@ cudaError_t launch_tree_tc(const TreeArgs &a, int2 *seg_tab, cudaStream_t st) {
     if (a.cache.kv.layout == SP_KV_PAGED) {
         const long long blocks = (long long)a.cache.kv.n_pages * a.Hkv;
         const int P = a.cache.kv.page_size;
-        const bool ok = e4 ? encode_rows_u8(&mk, a.cache.kv.k_pool, blocks * P, P) && encode_rows_u8(&mv, a.cache.kv.v_pool, blocks * P, P)
+        const bool ok = e4 ? encode_rows_u8(&mk, a.cache.kv.k_pool, blocks * P, P)
                            : encode_kv_pages_bf16(&mk, a.cache.kv.k_pool, blocks, P) &&
                                  encode_kv_pages_bf16(&mv, a.cache.kv.v_pool, blocks, P);
         if (!ok) return cudaErrorInvalidValue;
