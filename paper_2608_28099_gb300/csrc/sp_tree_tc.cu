@@ -28,8 +28,8 @@
 //                 exponent, w = 2^(x + log2 v_scale - m), so that w <= 2^8 whatever the
 //                 scales, and the row sum takes w / v_scale
 // The nodes' own keys never lose to the cache's format: bf16 nodes are copied, and for an
-// 8-bit cache their keys are two 8-bit parts in the two halves of the tile (S is the sum
-// of its halves), their values 16-bit floats, both exact for bf16 rows.
+// 8-bit cache their keys are two 8-bit parts in the two halves of the tile, added up in the
+// same scores, their values 16-bit floats, both exact for bf16 rows.
 // What a row does not see: scores are replaced by -inf (not added to), rows of a tile past
 // the sequence's end are zeros, and a node's non-finite values are taken out of the
 // product and added afterwards to the rows that see the node.
@@ -106,11 +106,28 @@ struct Roles {
     static constexpr int K_WARP = E4 ? 9 : 12, V_WARP = K_WARP + 2, V_WARPS = E4 ? 1 : 2;  // producers
     static constexpr int Q_WARP = E4 ? CVT : 9, Q_WARPS = E4 ? 4 : 3;                       // load the queries
     // Registers a thread: the softmax warps take what the other roles leave of the launch's
-    // 128 (8 x 144 + 8 x 112 = 8 x 160 + 8 x 96 = 16 x 128 a lane).  With 128 everywhere 50 to
+    // 128 (8 x 136 + 8 x 120 = 8 x 160 + 8 x 96 = 16 x 128 a lane).  With 128 everywhere 50 to
     // 350 bytes a thread spill, more in all than the L1 that the shared memory leaves holds: a
     // reload then waits for the L2 behind the cache stream.  So: 0 (bf16), at most 8.
-    static constexpr int SOFT_REGS = E4 ? 144 : 160, OTHER_REGS = E4 ? 112 : 96;
+    static constexpr int SOFT_REGS = E4 ? 136 : 160, OTHER_REGS = E4 ? 120 : 96;
 };
+// mbar_wait by a whole warp with one verdict, in few instructions: the kernel waits in some
+// twenty places and its loops have to stay in the instruction cache.
+__device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort) {
+    bool done = mbar_try_wait(bar, parity);
+    if (!__all_sync(0xffffffffu, done)) {
+        const uint64_t t0 = global_ns();
+#pragma unroll 1
+        while (!done) {
+            done = mbar_try_wait(bar, parity);
+            if (!done && (*abort || global_ns() - t0 > kWaitLimitNs)) {
+                *abort = 1;
+                break;
+            }
+        }
+    }
+    return __all_sync(0xffffffffu, done);
+}
 // One arrival of a warp whose lanes have all done their part.
 __device__ __forceinline__ void arrive_warp(uint64_t *bar, int lane) {
     __syncwarp();
@@ -409,7 +426,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int B = a.B, Hkv = a.Hkv, Hv = Hkv * a.n_rb;
     int *prefix = (int *)(smem + lay.off_tab), *sids = prefix + B + 1, *lens = sids + B, *nodes = lens + B;
     const bool paged = a.cache.kv.layout == SP_KV_PAGED;
-    const int P = a.cache.kv.page_size;
+    const int P = a.cache.kv.page_size, P_bits = 31 - __clz(max(P, 1));  // 16, 32 or 64 (0 contiguous)
     constexpr int ROW = DH * (E4 ? 1 : 2);  // bytes of a cached row
     // the first kernel of its call: nothing of the caller's is read before
     pdl_wait();
@@ -494,7 +511,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
             x += n_tiles;
             // this segment's queries are there, and with them what the row sees and its scale
-            ok = ok && mbar_wait_warp(&bars->q_full, seg_ph, abort);
+            ok = ok && wait_warp(&bars->q_full, seg_ph, abort);
             // (the next ones may come once every softmax warp has seen these and their scores
             // are done: the scores alone run ahead by a whole short segment)
             arrive_warp(&bars->q_empty, lane);
@@ -509,10 +526,10 @@ __global__ void __launch_bounds__(THREADS, 1)
                 const bool is_fresh = i == last;
                 const int n_tok = is_fresh ? 0 : min(TILE, left - i * TILE);
                 // warp-uniform verdicts: the TMEM loads and stores are warp-collective
-                ok = ok && mbar_wait_warp(&bars->s_full[wg], ks_ph, abort);
+                ok = ok && wait_warp(&bars->s_full[wg], ks_ph, abort);
                 // (8-bit: the tile's constants; the nodes' tile: which nodes are not finite)
-                if constexpr (E4) ok = ok && mbar_wait_warp(&bars->c_par[rv.slot], rv.ph, abort);
-                else if (is_fresh) ok = ok && mbar_wait_warp(&bars->v_full[rv.slot], rv.ph, abort);
+                if constexpr (E4) ok = ok && wait_warp(&bars->c_par[rv.slot], rv.ph, abort);
+                else if (is_fresh) ok = ok && wait_warp(&bars->v_full[rv.slot], rv.ph, abort);
                 ks_ph ^= 1;
                 if (!ok) continue;
                 tc_fence_after();
@@ -535,15 +552,6 @@ __global__ void __launch_bounds__(THREADS, 1)
                 auto scores = [&](int j0, float (&s)[CH]) {
                     load_cols<CH>(s_col + (uint32_t)j0, s);
                     if constexpr (E4) {
-                        if (is_fresh && j0 < 64) {  // the keys' second parts
-#pragma unroll
-                            for (int h = 0; h < CH; h += 32) {
-                                float s2[32];
-                                load_cols<32>(s_col + (uint32_t)(64 + j0 + h), s2);
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) s[h + e] += s2[e];
-                            }
-                        }
                         const float *pj = par + 2 * j0;
 #pragma unroll
                         for (int e = 0; e < CH; e += 2) {
@@ -687,7 +695,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                     a1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - mu);
                 }
             }
-            ok = ok && mbar_wait_warp(&bars->pv_done, seg_ph, abort);
+            ok = ok && wait_warp(&bars->pv_done, seg_ph, abort);
             seg_ph ^= 1;
             tc_fence_after();
             // slot of this segment's partial: a share has at most two, the pair that starts
@@ -814,15 +822,15 @@ __global__ void __launch_bounds__(THREADS, 1)
                     const int t = sg.t_a + i, t0 = t * TILE;
                     const bool is_fresh = t == sg.nt - 1;
                     const int n_tok = is_fresh ? 0 : min(TILE, L - t0);
-                    const int n_pg = paged ? n_tok / P : 0;  // whole pages
+                    const int n_pg = paged ? n_tok >> P_bits : 0;  // whole pages
                     int page = -1;                           // page ids (up to eight), asked for before the wait
                     if (paged && lane * P < n_tok) {
-                        const int lp = t0 / P + lane;
+                        const int lp = (t0 >> P_bits) + lane;
                         page = lp < a.cache.kv.max_pages ? a.cache.kv.page_table[(size_t)sid * a.cache.kv.max_pages + lp] : -1;
                         if (page < 0 || page >= a.cache.kv.n_pages) page = -1, bad = 1;
                     }
                     // warp-uniform verdict: the collectives below need every lane
-                    if (!mbar_wait_warp(&empty[rg.slot], rg.ph ^ 1, abort)) {
+                    if (!wait_warp(&empty[rg.slot], rg.ph ^ 1, abort)) {
                         stop = true;
                         break;
                     }
@@ -978,7 +986,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 const Seg sg = seg_at(prefix, B, x, x1);
                 x += sg.n;
                 const int b = sg.b, L = lens[b];
-                ok = mbar_wait_warp(&bars->q_empty, seg_ph ^ 1, abort);
+                ok = wait_warp(&bars->q_empty, seg_ph ^ 1, abort);
                 if (!ok) break;
                 load_queries<E4, TPC, MT>(a, b, nodes[b], g, rb, smem + lay.off_q, (unsigned long long *)(smem + OFF_SEES) + seg_ph * 256,
                                           (float *)(smem + OFF_RS) + seg_ph * 256, cw, 4, lane);
@@ -995,9 +1003,9 @@ __global__ void __launch_bounds__(THREADS, 1)
                     const int tok = (sg.t_a + i) * TILE + ct;
                     if (i >= sg.n || tok >= L) return -1ll;
                     if (!paged) return (long long)tok * Hkv;
-                    const int lp = tok / P;
+                    const int lp = tok >> P_bits;
                     const int page = lp < a.cache.kv.max_pages ? __ldg(a.cache.kv.page_table + (size_t)sid * a.cache.kv.max_pages + lp) : -1;
-                    return page < 0 || page >= a.cache.kv.n_pages ? -1ll : (long long)page * Hkv * P + (tok - lp * P);
+                    return page < 0 || page >= a.cache.kv.n_pages ? -1ll : (long long)page * Hkv * P + (tok & (P - 1));
                 };
                 auto scales = [&](long long at) {
                     return at < 0 ? make_float2(0.f, 0.f) : make_float2(__ldg(sk + at), __ldg(sv + at));
@@ -1009,8 +1017,8 @@ __global__ void __launch_bounds__(THREADS, 1)
                     const int t = sg.t_a + i;
                     const bool is_fresh = t == sg.nt - 1;
                     const int n_tok = is_fresh ? 0 : min(TILE, L - t * TILE);
-                    ok = mbar_wait_warp(&bars->v_full[rv.slot], rv.ph, abort) &&
-                         mbar_wait_warp(&bars->c_empty[rc.slot], rc.ph ^ 1, abort);
+                    ok = wait_warp(&bars->v_full[rv.slot], rv.ph, abort) &&
+                         wait_warp(&bars->c_empty[rc.slot], rc.ph ^ 1, abort);
                     if (!ok) break;
                     const float2 sc = next;
                     next = scales(at);
@@ -1029,21 +1037,26 @@ __global__ void __launch_bounds__(THREADS, 1)
                         par[par_at(ct) + 2] = __log2f(vs);
                         par[2 * TILE + ct] = __frcp_rn(vs);
                         arrive_warp(&bars->c_par[rc.slot], lane);
-                        uint4 u[8];
+                        // 16 rows of 8 chunks a step of the four warps: its row's place in an
+                        // 8-row group is the thread's own, so addresses advance by constants
+                        const int r0 = ct >> 3, c = ct & 7;
+                        const uint8_t *from = src + ct * 16;
+                        uint8_t *to0 = dst + kv_off(r0, 2 * c), *to1 = dst + kv_off(r0, 2 * c + 1);
+#pragma unroll 1
+                        for (int it = 0; it < 8; it += 4) {
+                            uint4 u[4];
 #pragma unroll
-                        for (int it = 0; it < 8; ++it) {
-                            const int r = it * 16 + (ct >> 3);
-                            u[it] = r < n_tok ? *(const uint4 *)(src + r * 128 + (ct & 7) * 16) : make_uint4(0, 0, 0, 0);
-                        }
+                            for (int k = 0; k < 4; ++k) u[k] = *(const uint4 *)(from + (it + k) * 2048);
 #pragma unroll
-                        for (int it = 0; it < 8; ++it) {
-                            const int r = it * 16 + (ct >> 3), c = ct & 7;
-                            const uint32_t w[4] = {u[it].x, u[it].y, u[it].z, u[it].w};
-                            uint32_t h[8];
+                            for (int k = 0; k < 4; ++k) {
+                                if (r0 + (it + k) * 16 >= n_tok) u[k] = make_uint4(0, 0, 0, 0);
+                                const uint32_t w[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
+                                uint32_t h[8];
 #pragma unroll
-                            for (int q = 0; q < 8; ++q) h[q] = codes2_to_half2(w[q >> 1], q & 1);
-                            st_shared_v4(dst + kv_off(r, 2 * c), h[0], h[1], h[2], h[3]);
-                            st_shared_v4(dst + kv_off(r, 2 * c + 1), h[4], h[5], h[6], h[7]);
+                                for (int q = 0; q < 8; ++q) h[q] = codes2_to_half2(w[q >> 1], q & 1);
+                                st_shared_v4(to0 + (it + k) * 2 * GROUP_STRIDE, h[0], h[1], h[2], h[3]);
+                                st_shared_v4(to1 + (it + k) * 2 * GROUP_STRIDE, h[4], h[5], h[6], h[7]);
+                            }
                         }
                     } else {
                         const int n = nodes[b], c = lane & 15;
@@ -1110,7 +1123,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             for (int x = x0; x < x1; seg_ph ^= 1) {
                 const Seg sg = seg_at(prefix, B, x, x1);
                 x += sg.n;
-                if (!mbar_wait_warp(&bars->q_empty, seg_ph ^ 1, abort)) break;
+                if (!wait_warp(&bars->q_empty, seg_ph ^ 1, abort)) break;
                 load_queries<E4, TPC, MT>(a, sg.b, nodes[sg.b], g, rb, smem + lay.off_q,
                                           (unsigned long long *)(smem + OFF_SEES) + seg_ph * 256, nullptr, warp - Ro::Q_WARP,
                                           Ro::Q_WARPS, lane);
@@ -1127,6 +1140,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             // instructions under `on` (see elect_one).
             const bool on = elect_one();
             constexpr uint32_t idesc_s = E4 ? (1u << 4) | ((uint32_t)(TILE >> 3) << 17) | (8u << 24) : idesc_bf16_f32(128, TILE);
+            constexpr uint32_t idesc_s64 = (1u << 4) | ((uint32_t)(64 >> 3) << 17) | (8u << 24);
             // 16-bit floats: format bits 0 instead of bf16's 1
             constexpr uint32_t idesc_o = E4 ? (1u << 4) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | (8u << 24)
                                             : idesc_bf16_f32_bmn(128, DH);
@@ -1138,9 +1152,9 @@ __global__ void __launch_bounds__(THREADS, 1)
             bool ok = true;
             uint32_t kp = 0;  // phases of p_full, a bit a pipeline
             int j = 0;
-            auto issue_s = [&](int q, bool last_s) {
+            auto issue_s = [&](int q, bool last_s, bool nodes_tile) {
                 const int w = q & 1;
-                ok = ok && mbar_wait_warp(&bars->k_full[rk.slot], rk.ph, abort);
+                ok = ok && wait_warp(&bars->k_full[rk.slot], rk.ph, abort);
                 if (!ok) return;
                 tc_fence_after();
                 fence_proxy_async();  // cp.async data -> tensor-core reads
@@ -1148,12 +1162,20 @@ __global__ void __launch_bounds__(THREADS, 1)
                 const uint64_t dq = dq0 + (uint32_t)(MT == 2 ? w * (Q_TILE >> 4) : 0);
                 const uint32_t d = tmem + (uint32_t)(w * 128);
                 if (on) {
+                    if constexpr (E4) {
+                        // the nodes' tile: 64 columns, the keys' two parts added in them
+                        const uint32_t id = nodes_tile ? idesc_s64 : idesc_s;
+#pragma unroll 1
+                        for (int part = 0; part < (nodes_tile ? 2 : 1); ++part)
 #pragma unroll
-                    for (int kk = 0; kk < 8; ++kk) {
-                        // 8-bit: part kk / 4, 32 dims each; else 16 dims, 32 B of a row of dim half kk / 4
-                        const uint64_t aq = dq + (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2);
-                        if constexpr (E4) mma_e4m3(d, aq, dk + (uint64_t)((kk & 3) * 2), idesc_s, kk > 0);
-                        else mma_bf16(d, aq, dk + (uint64_t)((kk >> 2) * (HALF_STRIDE >> 4) + (kk & 3) * 2), idesc_s, kk > 0);
+                            for (int kk = 0; kk < 8; ++kk)  // part kk / 4 of the queries, 32 dims each
+                                mma_e4m3(d, dq + (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2),
+                                         dk + (uint64_t)(part * (8192 >> 4) + (kk & 3) * 2), id, kk > 0 ? 1u : (uint32_t)part);
+                    } else {
+#pragma unroll
+                        for (int kk = 0; kk < 8; ++kk)  // 16 dims: 32 B of a row of dim half kk / 4
+                            mma_bf16(d, dq + (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2),
+                                     dk + (uint64_t)((kk >> 2) * (HALF_STRIDE >> 4) + (kk & 3) * 2), idesc_s, kk > 0);
                     }
                     if (MT == 1 || w) mma_commit(&bars->k_empty[rk.slot]);
                     mma_commit(&bars->s_full[w]);
@@ -1169,12 +1191,12 @@ __global__ void __launch_bounds__(THREADS, 1)
                 // the same in every lane, and known to be
                 const int items = __shfl_sync(0xffffffffu, sg.n, 0) * MT;
                 const bool has_fresh = __shfl_sync(0xffffffffu, (int)(sg.t_a + sg.n == sg.nt), 0);
-                if (!mbar_wait_warp(&bars->q_full, (uint32_t)(j & 1), abort)) break;
+                if (!wait_warp(&bars->q_full, (uint32_t)(j & 1), abort)) break;
 #pragma unroll 1
                 for (int q = -2; ok && q < items; ++q) {
                     if (q >= 0) {
                         const int w = q & 1;
-                        ok = mbar_wait_warp(&vf[rv.slot], rv.ph, abort) && mbar_wait_warp(&bars->p_full[w], (kp >> w) & 1, abort);
+                        ok = wait_warp(&vf[rv.slot], rv.ph, abort) && wait_warp(&bars->p_full[w], (kp >> w) & 1, abort);
                         if (!ok) break;
                         kp ^= 1u << w;
                         tc_fence_after();
@@ -1194,7 +1216,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                         __syncwarp();
                         if (MT == 1 || w) rv.next();
                     }
-                    if (q + 2 < items) issue_s(q + 2, q + 3 == items);
+                    if (q + 2 < items) issue_s(q + 2, q + 3 == items, has_fresh && q + 2 >= items - MT);
                 }
             }
             if (on) mma_commit(&bars->fin);  // completes when every MMA is done
