@@ -34,95 +34,98 @@ __device__ __forceinline__ void storev(T *p, const float (&v)[V]) {
     }
 }
 
-// Rotate (or turn back) heads.  A block takes a few tokens: it first forms the
-// (cos, sin) of their pairs in shared memory (one sincospif a (token, pair), shared by
-// all heads), then its threads walk the (token, head, vector) units; a unit reads the
-// two vectors that turn into one another (half layout) or one vector of whole pairs
-// (interleaved), or copies a vector of the dims that pass.  V elements a vector: 16
-// bytes, or 1 (2 interleaved) where a stride, base or width does not allow that.
+// Rotate (or turn back) heads.  A thread has one unit of a head -- the two vectors that
+// turn into one another (half layout), one vector of whole pairs (interleaved), or one
+// vector of the dims that pass -- for every head it visits of one token, U heads' loads in
+// flight, the first of them issued before the block forms its tokens' (cos, sin) in shared
+// memory (one sincospif a (token, pair), shared by all heads).  V elements a vector: 16
+// bytes, or 1 (2 interleaved) where a stride, base or width does not allow that.  A block
+// is one token, or as many as fill it.  HBM-bound where large: TIMED
 template <typename T, int V, bool INTER>
 __global__ void __launch_bounds__(THREADS) rotate_kernel(const __grid_constant__ RotateArgs a) {
     extern __shared__ float2 cs[];  // [token][pair]
+    constexpr int U = INTER ? 4 : 2, W = INTER ? V / 2 : V;  // heads in flight, pairs of a unit
     pdl_wait();
     pdl_trigger();
-    const int half = a.rot.half, t0 = blockIdx.x * a.tokens_per_block;
-    const int nt = min(a.tokens_per_block, a.n_tokens - t0);
+    const int half = a.rot.half, turn = (INTER ? a.rot.rot : half) / V, units = turn + (a.dh - a.rot.rot) / V;
+    const int wide = min(units, THREADS), heads = min(a.n_heads, THREADS / wide), nt = a.tokens_per_block;
+    const int per = wide * heads, tl = threadIdx.x / per, rest = threadIdx.x - tl * per, h0 = rest / wide;
+    const int t0 = blockIdx.x * nt, t = t0 + tl;
+    const bool mine = tl < nt && t < a.n_tokens;
+    int c = rest - h0 * wide;
+    auto place = [&](int unit) { return unit < turn ? unit * V : a.rot.rot + (unit - turn) * V; };
+    float p[U][V], q[INTER ? 1 : U][V];
+    auto load = [&](int unit, int h) {
+        const T *x = (const T *)a.x + t * a.xt + place(unit);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int hh = h + u * heads;
+            if (hh >= a.n_heads) continue;
+            loadv<T, V>(x + hh * a.xh, p[u]);
+            if constexpr (!INTER) {
+                if (unit < turn) loadv<T, V>(x + hh * a.xh + half, q[u]);
+            }
+        }
+    };
+    if (mine) load(c, h0);
     for (int i = threadIdx.x; i < nt * half; i += THREADS) {
-        const int t = i / half;
-        float2 v = rotary_cs(a.rot, a.pos[t0 + t], i - t * half);
+        const int k = i / half;
+        if (t0 + k >= a.n_tokens) break;
+        float2 v = rotary_cs(a.rot, a.pos[t0 + k], i - k * half);
         if (a.backward) v.y = -v.y;
         cs[i] = v;
     }
     __syncthreads();
-    const int turn = (INTER ? a.rot.rot : half) / V, units = turn + (a.dh - a.rot.rot) / V;
-    const int per_token = a.n_heads * units;
-    for (int u = threadIdx.x; u < nt * per_token; u += THREADS) {
-        const int t = u / per_token, r = u - t * per_token, h = r / units, c = r - h * units;
-        const T *x = (const T *)a.x + (t0 + t) * a.xt + h * a.xh;
-        T *y = (T *)a.y + (t0 + t) * a.yt + h * a.yh;
-        if (c >= turn) {
-            const int e = a.rot.rot + (c - turn) * V;
-            float v[V];
-            loadv<T, V>(x + e, v);
-            storev<T, V>(y + e, v);
-        } else if constexpr (INTER) {
-            float v[V];
-            loadv<T, V>(x + c * V, v);
-            const float2 *w = cs + t * half + c * (V / 2);
+    if (!mine) return;
+    for (bool first = true; c < units; c += wide, first = false) {
+        const bool turns = c < turn;
+        float2 k[W];
+        if (turns) {
 #pragma unroll
-            for (int i = 0; i < V; i += 2) {
-                const float2 k = w[i / 2];
-                const float p = v[i], q = v[i + 1];
-                v[i] = p * k.x - q * k.y;
-                v[i + 1] = q * k.x + p * k.y;
-            }
-            storev<T, V>(y + c * V, v);
-        } else {
-            float p[V], q[V];
-            loadv<T, V>(x + c * V, p);
-            loadv<T, V>(x + half + c * V, q);
-            const float2 *w = cs + t * half + c * V;
+            for (int i = 0; i < W; ++i) k[i] = cs[tl * half + c * W + i];
+        }
+        T *y = (T *)a.y + t * a.yt + place(c);
+        for (int h = h0; h < a.n_heads; h += U * heads) {
+            if (!first || h != h0) load(c, h);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float2 k = w[i];
-                const float s = p[i];
-                p[i] = s * k.x - q[i] * k.y;
-                q[i] = q[i] * k.x + s * k.y;
+            for (int u = 0; u < U; ++u) {
+                const int hh = h + u * heads;
+                if (hh >= a.n_heads) continue;
+                if (turns) {
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        float *one, *two;
+                        if constexpr (INTER) one = &p[u][2 * i], two = &p[u][2 * i + 1];
+                        else one = &p[u][i], two = &q[u][i];
+                        const float f = *one;
+                        *one = f * k[i].x - *two * k[i].y;
+                        *two = *two * k[i].x + f * k[i].y;
+                    }
+                    if constexpr (!INTER) storev<T, V>(y + hh * a.yh + half, q[u]);
+                }
+                storev<T, V>(y + hh * a.yh, p[u]);
             }
-            storev<T, V>(y + c * V, p);
-            storev<T, V>(y + half + c * V, q);
         }
     }
 }
 
-template <typename T, int V>
-cudaError_t run_rotate(const RotateArgs &a, cudaStream_t st) {
+template <typename T, int V, bool INTER>
+cudaError_t run_rotate(RotateArgs a, cudaStream_t st) {
+    const int turn = (INTER ? a.rot.rot : a.rot.half) / V, units = turn + (a.dh - a.rot.rot) / V;
+    const int wide = units < THREADS ? units : THREADS, fit = THREADS / wide;
+    const int per = wide * (a.n_heads < fit ? a.n_heads : fit);
+    a.tokens_per_block = THREADS / per;
     const dim3 grid(ceil_div(a.n_tokens, a.tokens_per_block));
-    const size_t smem = (size_t)a.tokens_per_block * a.rot.half * sizeof(float2);
-    if (a.rot.interleaved) return launch_k(rotate_kernel<T, V == 1 ? 2 : V, true>, grid, dim3(THREADS), smem, st, a);
-    return launch_k(rotate_kernel<T, V, false>, grid, dim3(THREADS), smem, st, a);
+    const size_t smem = (size_t)a.tokens_per_block * a.rot.half * sizeof(float2);  // (at most 16 KB: a token has half / V threads)
+    return launch_k(rotate_kernel<T, V, INTER>, grid, dim3(THREADS), smem, st, a);
+}
+template <typename T, int V>
+cudaError_t pick_rotate(const RotateArgs &a, cudaStream_t st) {
+    if (a.rot.interleaved) return run_rotate<T, V == 1 ? 2 : V, true>(a, st);
+    return run_rotate<T, V, false>(a, st);
 }
 
-// 8 elements of a row, in vectors where the caller's rows allow them.
-__device__ __forceinline__ void load_row8(const void *p, int dtype, long long e, int vec, float (&v)[8]) {
-    if (dtype == SP_F32) {
-        const float *s = (const float *)p + e;
-        if (vec) {
-            load8(s, v);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = s[i];
-        }
-    } else {
-        const bf16 *s = (const bf16 *)p + e;
-        if (vec) {
-            load8(s, v);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = to_f(s[i]);
-        }
-    }
-}
+// 8 elements to a row, in vectors where the row allows them.
 __device__ __forceinline__ void store_row8(void *p, int dtype, long long e, int vec, const float (&v)[8]) {
     if (dtype == SP_F32) {
         float *d = (float *)p + e;
@@ -145,10 +148,77 @@ __device__ __forceinline__ void store_row8(void *p, int dtype, long long e, int 
     }
 }
 
-// The tokens of batch entry b that a copy kernel's block works on.
+// 8 elements of a row as they are in memory, and as floats.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const void *p, long long e, int vec) {
+        const float *s = (const float *)p + e;
+        if (vec) {
+            a = *(const float4 *)s, b = *(const float4 *)(s + 4);
+        } else {
+            a = make_float4(s[0], s[1], s[2], s[3]), b = make_float4(s[4], s[5], s[6], s[7]);
+        }
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    }
+};
+template <>
+struct Raw8<bf16> {
+    uint4 u;
+    __device__ __forceinline__ void load(const void *p, long long e, int vec) {
+        const uint16_t *s = (const uint16_t *)p + e;
+        if (vec) {
+            u = *(const uint4 *)s;
+        } else {
+            u = make_uint4(s[0] | (uint32_t)s[1] << 16, s[2] | (uint32_t)s[3] << 16, s[4] | (uint32_t)s[5] << 16,
+                           s[6] | (uint32_t)s[7] << 16);
+        }
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+};
+// 16 elements of a cached row.
+template <typename T>
+struct Cached16 {
+    static constexpr bool codes = false;
+    Raw8<T> a, b;
+    __device__ __forceinline__ void load(const void *base, const float *, long long row, int dh, int e) {
+        a.load(base, row * dh + e, 1);
+        b.load(base, row * dh + e + 8, 1);
+    }
+    __device__ __forceinline__ void get(float (&v0)[8], float (&v1)[8]) const { a.get(v0), b.get(v1); }
+};
+struct Code16 {  // codes and their row's scale
+    static constexpr bool codes = true;
+    uint4 u;
+    float s;
+    __device__ __forceinline__ void load(const void *base, const float *scale, long long row, int dh, int e) {
+        u = *(const uint4 *)((const uint8_t *)base + row * dh + e);
+        s = scale[row];
+    }
+    __device__ __forceinline__ void get(float (&v0)[8], float (&v1)[8]) const {
+        codes_to_float(make_uint2(u.x, u.y), v0);
+        codes_to_float(make_uint2(u.z, u.w), v1);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v0[i] *= s, v1[i] *= s;
+    }
+};
+
+// The tokens of a batch entry that a copy kernel's block works on.
 struct Chunk {
     SeqRef sq;
-    int b, count, row0, j0, n;
+    int b, count, j0, n;
+    long long row0;
 };
 __device__ __forceinline__ Chunk chunk_of(const CopyArgs &a, int *status) {
     Chunk c;
@@ -156,175 +226,260 @@ __device__ __forceinline__ Chunk chunk_of(const CopyArgs &a, int *status) {
     c.b = b;
     c.sq = resolve_seq(a.seq_ids, a.seq_lens, 0, b, a.cache.kv.n_seqs, a.cache.max_seq_len, status);
     c.count = a.rows.count ? a.rows.count[b] : a.rows.max_rows;
+    c.row0 = a.rows.row0 ? a.rows.row0[b] : (long long)b * a.rows.max_rows;
     if (c.count < 0 || c.count > a.rows.max_rows) {
         if (status) atomicOr(status, SP_DEV_BAD_ROW);
         c.count = c.count < 0 ? 0 : a.rows.max_rows;
     }
-    c.row0 = a.rows.row0 ? a.rows.row0[b] : b * a.rows.max_rows;
     c.j0 = (blockIdx.x - b * a.chunks) * a.tokens_per_block;
     c.n = max(0, min(a.tokens_per_block, c.count - c.j0));
     return c;
 }
-__device__ __forceinline__ bool row_of(const CopyArgs &a, const Chunk &c, int j, bool take, long long *row) {
-    *row = (long long)c.row0 + (take && a.rows.take ? a.rows.take[(size_t)c.b * a.rows.max_rows + j] : j);
-    return *row >= 0 && *row < a.rows.n_rows;
-}
 
-// Append: a block takes a few tokens of one sequence, dh / 8 lanes a (token, K or V,
-// head) row, eight elements a lane.  The row's amax is a shuffle among its lanes; the
-// partner of a rotated element is read again (its line is in L1).
-template <int LANES>
+constexpr int MAX_TOK = 32;  // tokens of a block
+
+// The (token, K or V, head) rows of a block in order, `step` at a time.
+struct RowWalk {
+    int j, is_v, h;
+    __device__ __forceinline__ RowWalk(int r, int Hkv) : j(r / (2 * Hkv)), is_v((r / Hkv) & 1), h(r % Hkv) {}
+    __device__ __forceinline__ void next(int step, int Hkv) {
+        h += step;
+        while (h >= Hkv) {
+            h -= Hkv;
+            j += is_v;
+            is_v ^= 1;
+        }
+    }
+};
+
+// Append: a block takes a few tokens of one sequence, dh / 16 lanes a (token, K or V,
+// head) row, two chunks of eight elements a lane: chunks that turn into one another (half
+// layout), so that a rotation stays in its lane, else neighbours.  U rows' loads are in
+// flight, the first of them issued before the block looks up its tokens' pages and forms
+// their (cos, sin).  The row's amax is a shuffle among its lanes.  Bound by its
+// instructions (about ten an element: rotation, amax, scale, conversion).  TIMED
+template <int LANES, typename T>
 __global__ void __launch_bounds__(THREADS) append_kernel(const __grid_constant__ CopyArgs a) {
     extern __shared__ float2 cs[];  // [token][pair]
+    __shared__ long long place[MAX_TOK];  // the cache's (token, head 0) row; -1: skipped
+    constexpr int U = 2, G = THREADS / LANES;  // rows in flight, rows of a pass
     pdl_wait();
     pdl_trigger();
     const Chunk ck = chunk_of(a, threadIdx.x == 0 && blockIdx.x % a.chunks == 0 ? a.status : nullptr);
+    if (ck.n == 0 || ck.sq.sid < 0) return;  // uniform over the block
     const CacheDev &c = a.cache;
-    const int half = a.rot.half, Hkv = c.Hkv, dh = LANES * 8;
+    const int half = a.rot.half, Hkv = c.Hkv, dh = LANES * 16;
+    const int rows = ck.n * 2 * Hkv, lane = threadIdx.x % LANES, first = threadIdx.x / LANES;
+    const int passes = ceil_div(rows, G);
+    // this lane's two chunks
+    const bool in_lane = !a.rot.interleaved && half % 8 == 0;  // (0 without a rotation)
+    const int nh = in_lane ? half / 8 : 0;
+    const int e0 = 8 * (lane < nh ? lane : 2 * lane), e1 = 8 * (lane < nh ? lane + nh : 2 * lane + 1);
+    Raw8<T> x0[U], x1[U];
+    auto source = [&](int j, int is_v, int h) {  // the row's first element; -1: none
+        const long long row = ck.row0 + (a.rows.take ? a.rows.take[(size_t)ck.b * a.rows.max_rows + ck.j0 + j] : ck.j0 + j);
+        return row >= 0 && row < a.rows.n_rows ? row * (is_v ? a.rows.v_stride : a.rows.k_stride) + h * dh : -1;
+    };
+    auto load = [&](RowWalk w, int pass) {
+#pragma unroll
+        for (int u = 0; u < U; ++u, w.next(G, Hkv)) {
+            if (first + (pass + u) * G >= rows) continue;
+            const long long at = source(w.j, w.is_v, w.h);
+            if (at < 0) continue;
+            x0[u].load(w.is_v ? a.v : a.k, at + e0, a.vec);
+            x1[u].load(w.is_v ? a.v : a.k, at + e1, a.vec);
+        }
+    };
+    RowWalk w(first, Hkv);
+    load(w, 0);
+    if ((int)threadIdx.x < ck.n) {
+        const int j = threadIdx.x, t = ck.sq.len + ck.j0 + j;
+        long long dst = -1;
+        int bad = 0, step;
+        if (t >= c.max_seq_len) bad = SP_DEV_BAD_LENGTH;
+        else if (source(j, 0, 0) < 0) bad = SP_DEV_BAD_ROW;
+        else if (!cache_row(c, ck.sq.sid, t, &dst, &step)) bad = SP_DEV_BAD_PAGE;
+        place[j] = bad ? -1 : dst;
+        if (bad && a.status) atomicOr(a.status, bad);
+    }
     for (int i = threadIdx.x; i < ck.n * half; i += THREADS) {
         const int t = i / half;
         cs[i] = rotary_cs(a.rot, ck.sq.len + ck.j0 + t, i - t * half);
     }
     __syncthreads();
-    const int rows = ck.sq.sid < 0 ? 0 : ck.n * 2 * Hkv;  // rows of this block
-    const int lane = threadIdx.x % LANES;
-    int bad = 0;
-    for (int r0 = threadIdx.x / LANES; r0 < ceil_div(rows, THREADS / LANES) * (THREADS / LANES); r0 += THREADS / LANES) {
-        const bool in = r0 < rows;  // (whole warps stay for the shuffles)
-        const int r = in ? r0 : 0, j = r / (2 * Hkv), rem = r - j * 2 * Hkv, is_v = rem / Hkv, h = rem - is_v * Hkv;
-        const int t = ck.sq.len + ck.j0 + j;
-        long long src = 0, dst = 0;
-        int step = 0;
-        bool ok = in;
-        if (ok && t >= c.max_seq_len) ok = false, bad |= SP_DEV_BAD_LENGTH;
-        if (ok && !row_of(a, ck, ck.j0 + j, true, &src)) ok = false, bad |= SP_DEV_BAD_ROW;
-        if (ok && !cache_row(c, ck.sq.sid, t, &dst, &step)) ok = false, bad |= SP_DEV_BAD_PAGE;
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        const long long e0 = src * (is_v ? a.rows.v_stride : a.rows.k_stride) + h * dh;
-        const void *from = is_v ? a.v : a.k;
-        const int e = lane * 8;
-        if (ok) {
-            load_row8(from, a.dtype, e0 + e, a.vec, v);
-            if (!is_v && e < a.rot.rot) {
-                const float2 *w = cs + j * half;
-                if (a.rot.interleaved) {
+    const int head_step = c.kv.layout == SP_KV_PAGED ? c.kv.page_size : 1;
+    void *kb = cache_base(c, ck.sq.sid, 0), *vb = cache_base(c, ck.sq.sid, 1);
+    float *ks = nullptr, *vs = nullptr;
+    if (c.dtype == SP_E4M3) ks = scale_base(c, ck.sq.sid, 0), vs = scale_base(c, ck.sq.sid, 1);
+#pragma unroll 1
+    for (int pass = 0; pass < passes; pass += U) {
+        if (pass > 0) load(w, pass);
 #pragma unroll
-                    for (int i = 0; i < 8; i += 2) {
-                        if (e + i >= a.rot.rot) break;
-                        const float2 k = w[(e + i) / 2];
-                        const float p = v[i], q = v[i + 1];
-                        v[i] = p * k.x - q * k.y;
-                        v[i + 1] = q * k.x + p * k.y;
+        for (int u = 0; u < U; ++u, w.next(G, Hkv)) {
+            if (pass + u >= passes) break;  // (whole warps stay for the shuffles)
+            const long long p0 = first + (pass + u) * G < rows ? place[w.j] : -1;
+            const bool ok = p0 >= 0;
+            const long long dst = p0 + (long long)w.h * head_step;
+            float v0[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, v1[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (ok) x0[u].get(v0), x1[u].get(v1);
+            if (ok && half && !w.is_v) {
+                const float2 *k = cs + w.j * half;
+                if (in_lane) {
+                    if (lane < nh) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float2 f = k[e0 + i];
+                            const float p = v0[i];
+                            v0[i] = p * f.x - v1[i] * f.y;
+                            v1[i] = v1[i] * f.x + p * f.y;
+                        }
                     }
-                } else if (half % 8 == 0) {
-                    float o[8];
-                    const bool lo = e < half;
-                    load_row8(from, a.dtype, e0 + (lo ? e + half : e - half), a.vec, o);
+                } else if (a.rot.interleaved) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float2 k = w[(lo ? e : e - half) + i];
-                        v[i] = lo ? v[i] * k.x - o[i] * k.y : v[i] * k.x + o[i] * k.y;
+                    for (int i = 0; i < 16; i += 2) {
+                        if (e0 + i >= a.rot.rot) break;  // (chunks 2 l and 2 l + 1)
+                        const float2 f = k[e0 / 2 + i / 2];
+                        float &one = i < 8 ? v0[i & 7] : v1[i & 7], &two = i < 8 ? v0[(i & 7) + 1] : v1[(i & 7) + 1];
+                        const float p = one;
+                        one = p * f.x - two * f.y;
+                        two = two * f.x + p * f.y;
                     }
-                } else {
+                } else {  // pairs across lanes: the partner is read from the row
+                    const long long at = source(w.j, 0, w.h);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        if (e + i >= a.rot.rot) break;
-                        const bool lo = e + i < half;
-                        const int pair = lo ? e + i : e + i - half;
-                        const long long at = e0 + (lo ? e + i + half : pair);
-                        const float o = a.dtype == SP_F32 ? ((const float *)from)[at] : to_f(((const bf16 *)from)[at]);
-                        const float2 k = w[pair];
-                        v[i] = lo ? v[i] * k.x - o * k.y : v[i] * k.x + o * k.y;
+                    for (int i = 0; i < 16; ++i) {
+                        if (e0 + i >= a.rot.rot) break;
+                        const bool one = e0 + i < half;
+                        const int pair = one ? e0 + i : e0 + i - half;
+                        const float z = to_f(((const T *)a.k)[at + (one ? e0 + i + half : pair)]);
+                        const float2 f = k[pair];
+                        float &y = i < 8 ? v0[i & 7] : v1[i & 7];
+                        y = one ? y * f.x - z * f.y : y * f.x + z * f.y;
                     }
                 }
             }
-        }
-        if (c.dtype == SP_E4M3) {
-            float amax = kMinAmax;
+            if (c.dtype == SP_E4M3) {
+                float amax = kMinAmax;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) amax = fmaxf(amax, isfinite(v[i]) ? fabsf(v[i]) : 0.f);
+                for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fmaxf(fabsf(v0[i]), fabsf(v1[i])));  // (a NaN is no maximum)
 #pragma unroll
-            for (int o = 1; o < LANES; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-            const float inv = kMaxCode / amax;
-            if (ok) {
-                uint32_t w[4];
+                for (int q = 1; q < LANES; q <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, q));
+                if (__any_sync(0xffffffffu, amax == INFINITY)) {  // rare: infinities do not set the scale, and become NaN
+                    amax = kMinAmax;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)  // x - x: 0, or NaN for what is not finite
-                    w[i] = float_to_codes2(v[2 * i] * inv + (v[2 * i] - v[2 * i]),
-                                           v[2 * i + 1] * inv + (v[2 * i + 1] - v[2 * i + 1]));
-                const long long row = dst + (long long)h * step;
-                *(uint2 *)((uint8_t *)cache_base(c, ck.sq.sid, is_v) + row * dh + e) =
-                    make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
-                if (lane == 0) scale_base(c, ck.sq.sid, is_v)[row] = amax / kMaxCode;
+                    for (int i = 0; i < 8; ++i) {
+                        v0[i] += v0[i] - v0[i];
+                        v1[i] += v1[i] - v1[i];
+                        amax = fmaxf(amax, fmaxf(fabsf(v0[i]), fabsf(v1[i])));
+                    }
+#pragma unroll
+                    for (int q = 1; q < LANES; q <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, q));
+                }
+                if (ok) {
+                    const float inv = kMaxCode / amax;
+                    auto codes = [&](const float(&v)[8]) {
+                        return make_uint2(float_to_codes2(v[0] * inv, v[1] * inv) | float_to_codes2(v[2] * inv, v[3] * inv) << 16,
+                                          float_to_codes2(v[4] * inv, v[5] * inv) | float_to_codes2(v[6] * inv, v[7] * inv) << 16);
+                    };
+                    uint8_t *to = (uint8_t *)(w.is_v ? vb : kb) + dst * dh;
+                    *(uint2 *)(to + e0) = codes(v0);
+                    *(uint2 *)(to + e1) = codes(v1);
+                    if (lane == 0) (w.is_v ? vs : ks)[dst] = amax * (1.f / kMaxCode);
+                }
+            } else if (ok) {
+                store_row8(w.is_v ? vb : kb, c.dtype, dst * dh + e0, 1, v0);
+                store_row8(w.is_v ? vb : kb, c.dtype, dst * dh + e1, 1, v1);
             }
-        } else if (ok) {
-            store_row8(cache_base(c, ck.sq.sid, is_v), c.dtype, (dst + (long long)h * step) * dh + e, 1, v);
         }
     }
-    if (bad && a.status) atomicOr(a.status, bad);
 }
 
-// Read back: the same units the other way; tokens outside the sequence give zeros.
-template <int LANES>
+// Read back: rows the other way, 16 elements a lane; tokens outside the sequence give
+// zeros.  A block's tokens are looked up once, then U rows a thread are in flight.  CT: the
+// cache's elements (Code16: 8 bits).  TIMED
+template <int LANES, typename CT>
 __global__ void __launch_bounds__(THREADS) read_kernel(const __grid_constant__ CopyArgs a) {
+    __shared__ long long out_row[MAX_TOK], place[MAX_TOK];
+    constexpr int U = CT::codes ? 4 : 2, G = THREADS / LANES;  // rows in flight, rows of a pass
     pdl_wait();
     pdl_trigger();
     const Chunk ck = chunk_of(a, threadIdx.x == 0 && blockIdx.x % a.chunks == 0 ? a.status : nullptr);
+    if (ck.n == 0) return;  // uniform over the block
     const CacheDev &c = a.cache;
-    const int Hkv = c.Hkv, dh = LANES * 8, rows = ck.n * 2 * Hkv, lane = threadIdx.x % LANES, e = lane * 8;
-    const int first = a.first ? a.first[ck.b] : 0;
-    int bad = 0;
-#pragma unroll 2
-    for (int r = threadIdx.x / LANES; r < rows; r += THREADS / LANES) {
-        const int j = r / (2 * Hkv), rem = r - j * 2 * Hkv, is_v = rem / Hkv, h = rem - is_v * Hkv;
-        long long dst, src;
-        if (!row_of(a, ck, ck.j0 + j, false, &dst)) {
-            bad |= SP_DEV_BAD_ROW;
-            continue;
-        }
-        const int jj = a.rows.take ? a.rows.take[(size_t)ck.b * a.rows.max_rows + ck.j0 + j] : ck.j0 + j;
-        const long long t = (long long)first + jj;
-        int step;
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (ck.sq.sid >= 0 && t >= 0 && t < ck.sq.len) {
-            if (cache_row(c, ck.sq.sid, (int)t, &src, &step)) {
-                src += (long long)h * step;
-                const void *base = cache_base(c, ck.sq.sid, is_v);
-                if (c.dtype == SP_E4M3) {
-                    codes_to_float(*(const uint2 *)((const uint8_t *)base + src * dh + e), v);
-                    const float s = scale_base(c, ck.sq.sid, is_v)[src];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] *= s;
-                } else {
-                    load_row8(base, c.dtype, src * dh + e, 1, v);
-                }
-            } else {
-                bad |= SP_DEV_BAD_PAGE;
-            }
-        }
-        store_row8(is_v ? a.v : a.k, a.dtype, dst * (is_v ? a.rows.v_stride : a.rows.k_stride) + h * dh + e, a.vec, v);
+    const int Hkv = c.Hkv, dh = LANES * 16, rows = ck.n * 2 * Hkv, e = threadIdx.x % LANES * 16;
+    const int head_step = c.kv.layout == SP_KV_PAGED ? c.kv.page_size : 1, sid = ck.sq.sid;
+    if ((int)threadIdx.x < ck.n) {
+        const int j = ck.j0 + threadIdx.x;
+        const long long t = (a.first ? a.first[ck.b] : 0) +
+                            (long long)(a.rows.take ? a.rows.take[(size_t)ck.b * a.rows.max_rows + j] : j);
+        long long dst = ck.row0 + j, src = -1;
+        int bad = 0, step;
+        if (dst < 0 || dst >= a.rows.n_rows) bad = SP_DEV_BAD_ROW, dst = -1;
+        else if (sid >= 0 && t >= 0 && t < ck.sq.len && !cache_row(c, sid, (int)t, &src, &step)) bad = SP_DEV_BAD_PAGE, src = -1;
+        out_row[threadIdx.x] = dst;
+        place[threadIdx.x] = src;
+        if (bad && a.status) atomicOr(a.status, bad);
     }
-    if (bad && a.status) atomicOr(a.status, bad);
+    const void *kb = nullptr, *vb = nullptr;
+    const float *ks = nullptr, *vs = nullptr;
+    if (sid >= 0) {
+        kb = cache_base(c, sid, 0), vb = cache_base(c, sid, 1);
+        if constexpr (CT::codes) ks = scale_base(c, sid, 0), vs = scale_base(c, sid, 1);
+    }
+    __syncthreads();
+    RowWalk w(threadIdx.x / LANES, Hkv);
+#pragma unroll 1
+    for (int r = threadIdx.x / LANES; r < rows; r += U * G) {
+        CT x[U];
+        RowWalk s = w;
+#pragma unroll
+        for (int u = 0; u < U; ++u, s.next(G, Hkv)) {
+            const long long p0 = r + u * G < rows ? place[s.j] : -1;
+            if (p0 < 0) continue;
+            x[u].load(s.is_v ? vb : kb, s.is_v ? vs : ks, p0 + (long long)s.h * head_step, dh, e);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u, w.next(G, Hkv)) {
+            const long long row = r + u * G < rows ? out_row[w.j] : -1;
+            if (row < 0) continue;
+            float v0[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, v1[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (place[w.j] >= 0) x[u].get(v0, v1);
+            const long long to = row * (w.is_v ? a.rows.v_stride : a.rows.k_stride) + w.h * dh + e;
+            store_row8(w.is_v ? a.v : a.k, a.dtype, to, a.vec, v0);
+            store_row8(w.is_v ? a.v : a.k, a.dtype, to + 8, a.vec, v1);
+        }
+    }
 }
 
-// Tokens a block takes: several where that still leaves every SM a few blocks.
+template <int LANES>
+cudaError_t run_append(const CopyArgs &a, dim3 grid, cudaStream_t st) {
+    const size_t smem = (size_t)a.tokens_per_block * a.rot.half * sizeof(float2);
+    if (a.dtype == SP_F32) return launch_k(append_kernel<LANES, float>, grid, dim3(THREADS), smem, st, a);
+    return launch_k(append_kernel<LANES, bf16>, grid, dim3(THREADS), smem, st, a);
+}
+template <int LANES>
+cudaError_t run_read(const CopyArgs &a, dim3 grid, cudaStream_t st) {
+    if (a.cache.dtype == SP_E4M3) return launch_k(read_kernel<LANES, Code16>, grid, dim3(THREADS), 0, st, a);
+    if (a.cache.dtype == SP_F32) return launch_k(read_kernel<LANES, Cached16<float>>, grid, dim3(THREADS), 0, st, a);
+    return launch_k(read_kernel<LANES, Cached16<bf16>>, grid, dim3(THREADS), 0, st, a);
+}
+
+// Tokens a block takes: as many as leave every SM two blocks (a block looks them up first).
 int tokens_a_block(long long tokens, int n_sm) {
-    int t = 8;
-    while (t > 1 && tokens < (long long)t * n_sm * 8) t >>= 1;
+    int t = MAX_TOK;
+    while (t > 1 && tokens < (long long)t * n_sm * 2) t >>= 1;
     return t;
 }
 
 }  // namespace
 
-cudaError_t launch_rotate(int dtype, const RotateArgs &in, int n_sm, cudaStream_t st) {
-    RotateArgs a = in;
+cudaError_t launch_rotate(int dtype, const RotateArgs &a, cudaStream_t st) {
     const int es = dtype == SP_F32 ? 4 : 2, V = 16 / es;
     const long long strides = a.xt | a.xh | a.yt | a.yh;
     const bool vec = !(((uintptr_t)a.x | (uintptr_t)a.y) & 15) && strides % V == 0 &&
                      (a.rot.interleaved ? a.rot.rot : a.rot.half) % V == 0 && (a.dh - a.rot.rot) % V == 0;
-    a.tokens_per_block = tokens_a_block(a.n_tokens, n_sm);
-    if (dtype == SP_F32) return vec ? run_rotate<float, 4>(a, st) : run_rotate<float, 1>(a, st);
-    return vec ? run_rotate<bf16, 8>(a, st) : run_rotate<bf16, 1>(a, st);
+    if (dtype == SP_F32) return vec ? pick_rotate<float, 4>(a, st) : pick_rotate<float, 1>(a, st);
+    return vec ? pick_rotate<bf16, 8>(a, st) : pick_rotate<bf16, 1>(a, st);
 }
 
 cudaError_t launch_append(const CopyArgs &in, int n_sm, cudaStream_t st) {
@@ -333,10 +488,9 @@ cudaError_t launch_append(const CopyArgs &in, int n_sm, cudaStream_t st) {
     a.chunks = ceil_div(a.rows.max_rows, a.tokens_per_block);
     if ((long long)a.chunks * a.B > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
     const dim3 grid(a.chunks * a.B);
-    const size_t smem = (size_t)a.tokens_per_block * a.rot.half * sizeof(float2);
-    if (a.cache.dh == 128) return launch_k(append_kernel<16>, grid, dim3(THREADS), smem, st, a);
-    if (a.cache.dh == 64) return launch_k(append_kernel<8>, grid, dim3(THREADS), smem, st, a);
-    return launch_k(append_kernel<4>, grid, dim3(THREADS), smem, st, a);
+    if (a.cache.dh == 128) return run_append<8>(a, grid, st);
+    if (a.cache.dh == 64) return run_append<4>(a, grid, st);
+    return run_append<2>(a, grid, st);
 }
 
 cudaError_t launch_read(const CopyArgs &in, int n_sm, cudaStream_t st) {
@@ -345,9 +499,9 @@ cudaError_t launch_read(const CopyArgs &in, int n_sm, cudaStream_t st) {
     a.chunks = ceil_div(a.rows.max_rows, a.tokens_per_block);
     if ((long long)a.chunks * a.B > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
     const dim3 grid(a.chunks * a.B);
-    if (a.cache.dh == 128) return launch_k(read_kernel<16>, grid, dim3(THREADS), 0, st, a);
-    if (a.cache.dh == 64) return launch_k(read_kernel<8>, grid, dim3(THREADS), 0, st, a);
-    return launch_k(read_kernel<4>, grid, dim3(THREADS), 0, st, a);
+    if (a.cache.dh == 128) return run_read<8>(a, grid, st);
+    if (a.cache.dh == 64) return run_read<4>(a, grid, st);
+    return run_read<2>(a, grid, st);
 }
 
 }  // namespace sp
