@@ -56,7 +56,7 @@ constexpr int SLOT8 = TILE * DH;                // in 8 bits, 16 KB
 constexpr int PARAMS = 3 * TILE * 4;            // k scales and log2 v scales by pairs, 1 / v scale
 constexpr int Q_TILE = 128 * DH * 2;            // an M tile of queries: bf16, or two 8-bit parts
 constexpr int CONV = 2;                         // converted V slots
-constexpr int MAX_RING = 8;
+constexpr int MAX_RING = 8, MAX_AHEAD = 3;     // slots of a ring; tiles that V and scales are copied ahead
 constexpr int SMEM_MAX = 227 * 1024;
 constexpr int SOFT = 256;                       // softmax threads
 constexpr int BAR_EPI = 1, BAR_WG = 2;          // (BAR_WG + 1: the second warpgroup's)
@@ -66,8 +66,9 @@ constexpr int kTreeSegCost = 4;                 // cost of a segment, in tiles
 
 struct Layout {
     int nk, nv;                                 // ring slots
-    int off_q, off_k, off_v, off_c, off_st, off_tab;  // (off_c: converted V, then its parameters;
-                                                // off_st: staging of the copies' parts)
+    int off_q, off_k, off_v, off_c, off_st, off_sc, off_tab;  // (off_c: converted V, then its
+                                                // constants; off_st: staging of the copies'
+                                                // parts; off_sc: of the scales)
     int smem;
 };
 
@@ -89,10 +90,20 @@ constexpr int OFF_CUTS = OFF_RS + 2 * 256 * 4;
 constexpr int OFF_FRONT = OFF_CUTS + (MAX_GRP + 4) * 4;
 static_assert(sizeof(Bars) <= OFF_ML, "barrier block");
 
-// Warp roles: softmax 0-7, MMA 8; 8-bit caches: producers 9-11, converters 12-15 (queries
-// too); else queries 9-11, producers 12-15.
+// Warp roles: softmax 0-7, MMA 8; bf16 caches: queries 9-11, producers 12-15; 8-bit caches:
+// K producers 9-10, the tiles' constants 11, converters 12-15 (values, queries).
 constexpr int THREADS = 512;
-constexpr int MMA = 8, CVT = 12;
+constexpr int MMA = 8, SCALES = 11, CVT = 12, CVT_WARPS = 4;
+template <bool E4>
+struct Roles {
+    static constexpr int K_WARP = E4 ? 9 : 12, V_WARP = K_WARP + 2, V_WARPS = E4 ? 0 : 2;  // producers
+    static constexpr int Q_WARP = E4 ? CVT : 9, Q_WARPS = E4 ? CVT_WARPS : 3;              // load the queries
+    // Registers a thread: the softmax warps take what the other roles leave of the launch's
+    // 128 (8 x 136 + 8 x 120 = 8 x 160 + 8 x 96 = 16 x 128 a lane).  With 128 everywhere 50 to
+    // 350 bytes a thread spill, more in all than the L1 that the shared memory leaves holds: a
+    // reload then waits for the L2 behind the cache stream.
+    static constexpr int SOFT_REGS = E4 ? 136 : 160, OTHER_REGS = E4 ? 120 : 96;
+};
 template <int N>
 __device__ __forceinline__ void regs_inc() {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
@@ -101,16 +112,6 @@ template <int N>
 __device__ __forceinline__ void regs_dec() {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
-template <bool E4>
-struct Roles {
-    static constexpr int K_WARP = E4 ? 9 : 12, V_WARP = K_WARP + 2, V_WARPS = E4 ? 1 : 2;  // producers
-    static constexpr int Q_WARP = E4 ? CVT : 9, Q_WARPS = E4 ? 4 : 3;                       // load the queries
-    // Registers a thread: the softmax warps take what the other roles leave of the launch's
-    // 128 (8 x 136 + 8 x 120 = 8 x 160 + 8 x 96 = 16 x 128 a lane).  With 128 everywhere 50 to
-    // 350 bytes a thread spill, more in all than the L1 that the shared memory leaves holds: a
-    // reload then waits for the L2 behind the cache stream.  So: 0 (bf16), at most 8.
-    static constexpr int SOFT_REGS = E4 ? 136 : 160, OTHER_REGS = E4 ? 120 : 96;
-};
 // mbar_wait by a whole warp with one verdict, in few instructions: the kernel waits in some
 // twenty places and its loops have to stay in the instruction cache.
 __device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort) {
@@ -214,12 +215,6 @@ __device__ __forceinline__ void mma_e4m3(uint32_t d, uint64_t a, uint64_t b, uin
         "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
         "l"(a), "l"(b), "r"(idesc), "r"(acc));
 }
-__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
-    asm volatile(
-        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
-        "l"(src), "r"(bytes), "r"(smem_u32(bar))
-        : "memory");
-}
 __device__ __forceinline__ void expect_tx(uint64_t *bar, uint32_t bytes) {
     asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
@@ -277,6 +272,75 @@ struct Ring {
     }
 };
 
+// A CTA's share: tiles [x0, x1) of the list, pieces of sequences [b0, b1).
+struct Share {
+    const int *prefix;
+    int x0, x1, b0, b1;
+};
+// Its piece of sequence b.
+__device__ __forceinline__ Seg piece(const Share &sh, int b) {
+    const int p0 = sh.prefix[b], p1 = sh.prefix[b + 1], lo = max(p0, sh.x0);
+    Seg s;
+    s.b = b;
+    s.xp = p0;
+    s.nt = p1 - p0;
+    s.t_a = lo - p0;
+    s.n = min(p1, sh.x1) - lo;
+    return s;
+}
+
+// The key tiles of a share, in order.
+struct TileWalk {
+    const Share &sh;
+    Seg sg;
+    int b, i;  // sequence, tile of its piece
+    __device__ __forceinline__ explicit TileWalk(const Share &s) : sh(s), b(s.b0), i(0) {
+        if (!done()) sg = piece(sh, b);
+    }
+    __device__ __forceinline__ bool done() const { return b >= sh.b1; }
+    __device__ __forceinline__ int tile() const { return sg.t_a + i; }
+    __device__ __forceinline__ bool fresh() const { return sg.t_a + i == sg.nt - 1; }  // the nodes' tile
+    __device__ __forceinline__ int tokens(const int *lens) const {                     // cached ones
+        return fresh() ? 0 : min(TILE, lens[b] - tile() * TILE);
+    }
+    __device__ __forceinline__ void next() {
+        if (++i < sg.n) return;
+        i = 0;
+        if (++b < sh.b1) sg = piece(sh, b);
+    }
+};
+// Page ids of the tiles that a warp asks for, 32 at a time (lane j: page first + j of
+// sequence b).
+struct Pages {
+    int b = -1, first = 0, ids = 0, bits;
+    bool paged;
+    __device__ __forceinline__ Pages(bool pg, int P_bits) : bits(P_bits), paged(pg) {}
+    // before the rows of sequence b from t0 on are asked for; by the whole warp
+    __device__ __forceinline__ void at(const TreeArgs &a, const int *sids, const int *lens, int b_, int t0, int lane) {
+        const int lp = t0 >> bits;
+        if (!paged || (b == b_ && lp + (TILE >> bits) <= first + 32)) return;
+        b = b_;
+        first = lp;
+        ids = -1;
+        if ((long long)(lp + lane) << bits < lens[b] && lp + lane < a.cache.kv.max_pages)
+            ids = __ldg(a.cache.kv.page_table + (size_t)sids[b] * a.cache.kv.max_pages + lp + lane);
+        if (ids >= a.cache.kv.n_pages) ids = -1;
+    }
+    // page of row r of the tile (negative: none)
+    __device__ __forceinline__ int page(int t0, int r) const {
+        return __shfl_sync(0xffffffffu, ids, (t0 >> bits) - first + (r >> bits));
+    }
+};
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+        "l"(src), "r"(bytes), "r"(smem_u32(bar))
+        : "memory");
+}
+__device__ __forceinline__ void cp_async4(void *dst, const void *src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+
 // 2^k that brings amax into [128, 256), as (factor, its inverse's exponent -k).
 __device__ __forceinline__ float pow2_scale(float amax, int *k) {
     int e = (int)((__float_as_uint(amax) >> 23) & 0xff) - 127;
@@ -303,15 +367,14 @@ __device__ __forceinline__ uint32_t pack_half(float a, float b) {
     const __half2 v = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t *>(&v);
 }
-// Codes 2 hi, 2 hi + 1 of a word as two 16-bit floats.
-__device__ __forceinline__ uint32_t codes2_to_half2(uint32_t w, int hi) {
-    uint32_t h;
+// The four codes of a word as 16-bit floats.
+__device__ __forceinline__ void codes4_to_half4(uint32_t w, uint32_t *h0, uint32_t *h1) {
     asm("{\n\t.reg .b16 l, u;\n\t"
-        "mov.b32 {l, u}, %1;\n\t"
-        "cvt.rn.f16x2.e4m3x2 %0, l;\n\t}"
-        : "=r"(h)
-        : "r"(hi ? w >> 16 : w));
-    return h;
+        "mov.b32 {l, u}, %2;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %0, l;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %1, u;\n\t}"
+        : "=r"(*h0), "=r"(*h1)
+        : "r"(w));
 }
 // A tile's constants: for tokens 2 i, 2 i + 1 their k scales, then log2 of their v scales
 // (operand pairs of two-wide instructions); this is token t's k scale.
@@ -446,12 +509,12 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
 #pragma unroll 1
         for (int i = 0; i < lay.nv; ++i) {
-            mbar_init(&bars->v_full[i], Ro::V_WARPS * 32);
-            mbar_init(&bars->v_empty[i], E4 ? 4 : 1);
+            mbar_init(&bars->v_full[i], 64);  // two warps; 8-bit: one, twice a lane
+            mbar_init(&bars->v_empty[i], E4 ? CVT_WARPS : 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&bars->c_full[i], 4);
-            mbar_init(&bars->c_par[i], 4);
+            mbar_init(&bars->c_full[i], CVT_WARPS);
+            mbar_init(&bars->c_par[i], CVT_WARPS);
             mbar_init(&bars->c_empty[i], 1);
             mbar_init(&bars->s_full[i], 1);
             mbar_init(&bars->p_full[i], 4);
@@ -475,7 +538,11 @@ __global__ void __launch_bounds__(THREADS, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = bars->tmem;
-    const int x0 = cuts[grp], x1 = cuts[grp + 1];
+    Share sh{prefix, cuts[grp], cuts[grp + 1], 0, 0};
+    if (sh.x0 < sh.x1) {
+        sh.b0 = seg_at(prefix, B, sh.x0, sh.x1).b;
+        sh.b1 = seg_at(prefix, B, sh.x1 - 1, sh.x1).b + 1;
+    }
     if (blockIdx.x == 0) {  // for the merge: each sequence's first share and its number of them
 #pragma unroll 1
         for (int b = threadIdx.x; b < B; b += THREADS) {
@@ -499,17 +566,15 @@ __global__ void __launch_bounds__(THREADS, 1)
         uint32_t ks_ph = 0, seg_ph = 0;
         Ring rv(E4 ? CONV : lay.nv);
 #pragma unroll 1
-        for (int x = x0; x < x1;) {
-            const int xs = x;   // segment start (what the epilogue needs is found again then)
+        for (int b = sh.b0; b < sh.b1; ++b) {
             int n_tiles, last;  // tiles; the nodes' tile, if it is here
             int left;           // cached tokens from the segment's start on
             {
-                const Seg sg = seg_at(prefix, B, x, x1);
+                const Seg sg = piece(sh, b);  // (the epilogue finds it again)
                 n_tiles = sg.n;
                 last = sg.nt - 1 - sg.t_a;
-                left = lens[sg.b] - sg.t_a * TILE;
+                left = lens[b] - sg.t_a * TILE;
             }
-            x += n_tiles;
             // this segment's queries are there, and with them what the row sees and its scale
             ok = ok && wait_warp(&bars->q_full, seg_ph, abort);
             // (the next ones may come once every softmax warp has seen these and their scores
@@ -536,7 +601,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 if (is_fresh && ln == 0) {  // (the segment's last tile)
                     unsigned long long vb = 0;
 #pragma unroll
-                    for (int w = 0; w < (E4 ? 4 : 2); ++w) vb |= ((volatile unsigned long long *)bars->vbad[rv.slot])[w];
+                    for (int w = 0; w < (E4 ? CVT_WARPS : 2); ++w) vb |= ((volatile unsigned long long *)bars->vbad[rv.slot])[w];
                     bars->seg_vbad = vb;
                 }
                 if (!warp_active) {  // its lanes' weights reach no row that is used
@@ -661,8 +726,8 @@ __global__ void __launch_bounds__(THREADS, 1)
 
             // ---- epilogue: the pipelines' (one M tile) and copies' parts of each row are
             // added; the output (the pair in one share) or a partial is written
-            const Seg sg = seg_at(prefix, B, xs, x1);
-            const int b = sg.b, n = nodes[b];
+            const Seg sg = piece(sh, b);
+            const int n = nodes[b];
             const int j_first = group_of(cuts, n_grp, sg.xp), j_last = group_of(cuts, n_grp, sg.xp + sg.nt - 1);
             const bool whole = j_first == j_last;
             const int n1 = MT == 2 ? sg.n : sg.n >> 1;  // tiles of pipeline 1
@@ -793,11 +858,11 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
     } else {
         regs_dec<Ro::OTHER_REGS>();
-        if (warp >= Ro::K_WARP && warp < Ro::V_WARP + Ro::V_WARPS) {
+        if (warp >= Ro::K_WARP && warp < Ro::K_WARP + 2 + Ro::V_WARPS) {
             // ------------------------------------------------------------ producers
-            const bool is_v = warp >= Ro::V_WARP;
+            const bool is_v = !E4 && warp >= Ro::V_WARP;
             const int pidx = warp - (is_v ? Ro::V_WARP : Ro::K_WARP), ptid = pidx * 32 + lane;
-            const bool lead = pidx == 0, rows8 = E4 && is_v;  // (rows8: V's codes, plain rows of 128 bytes)
+            const bool lead = pidx == 0;
             uint64_t *full = is_v ? bars->v_full : bars->k_full, *empty = is_v ? bars->v_empty : bars->k_empty;
             const int slot_bytes = E4 ? SLOT8 : SLOT16;
             uint8_t *ring = smem + (is_v ? lay.off_v : lay.off_k);
@@ -808,10 +873,9 @@ __global__ void __launch_bounds__(THREADS, 1)
             int bad = 0, filled = 0;
             bool stop = false;
 #pragma unroll 1
-            for (int x = x0; x < x1 && !stop;) {
-                const Seg sg = seg_at(prefix, B, x, x1);
-                x += sg.n;
-                const int b = sg.b, sid = sids[b], L = lens[b];
+            for (int b = sh.b0; b < sh.b1 && !stop; ++b) {
+                const Seg sg = piece(sh, b);
+                const int sid = sids[b], L = lens[b];
                 // a contiguous sequence's rows of head g, a token apart
                 const uint8_t *seq = nullptr;
                 if (!paged && L > 0)
@@ -836,124 +900,98 @@ __global__ void __launch_bounds__(THREADS, 1)
                     }
                     uint8_t *dst = ring + rg.slot * slot_bytes;
                     bool plain = false;  // this thread wrote shared memory or issued cp.async
-                    if (rows8) {
-                        // V's codes as they lie: a bulk copy a page (a copy a row of a
-                        // contiguous cache took 60 cycles to issue each), else cp.async
-                        if (paged) {
-                            const int rows = min(P, n_tok - lane * P);  // of this lane's page
-                            const bool ok = rows > 0 && page >= 0;
-                            const unsigned bytes = __reduce_add_sync(0xffffffffu, ok ? rows * ROW : 0);
-                            if (lane == 0 && bytes) expect_tx(&full[rg.slot], bytes);
-                            __syncwarp();
-                            if (ok) {
-                                bulk_load(dst + lane * P * ROW, pool + ((size_t)page * Hkv + g) * P * ROW, rows * ROW, &full[rg.slot]);
-                            } else if (rows > 0) {  // a page outside the pool: zeros
-                                plain = true;
-#pragma unroll 1
-                                for (int e = 0; e < rows * 8; ++e) st_shared_v4(dst + lane * P * ROW + e * 16, 0, 0, 0, 0);
-                            }
-                        } else if (n_tok > 0) {
-                            plain = true;
-                            const int c = lane & 7;
-                            const uint8_t *src = seq + (size_t)(t0 + (lane >> 3)) * seq_step + c * 16;
-                            uint8_t *d = dst + lane * 16;
-                            const size_t hop = 4 * seq_step;
-#pragma unroll 8
-                            for (int r = lane >> 3; r < n_tok; r += 4, src += hop, d += 512) cp_async16(d, src);
+                    if (n_pg > 0 && lead) {
+                        const bool ok = lane < n_pg && page >= 0;
+                        const unsigned okm = __ballot_sync(0xffffffffu, ok);
+                        if (lane == 0 && okm) expect_tx(&full[rg.slot], __popc(okm) * P * ROW);
+                        __syncwarp();
+                        if (ok) {  // the cache is read once: evict-first keeps queries and partials in L2
+                            const int row = page * Hkv + g;
+                            if constexpr (E4) tma_load_2d_hint(dst + lane * P * ROW, map, &full[rg.slot], 0, row * P, pol);
+                            else tma_load_4d_hint(dst + lane * P * ROW, map, &full[rg.slot], 0, 0, 0, row * (P / 8), pol);
                         }
-                    } else {
-                        if (n_pg > 0 && lead) {
-                            const bool ok = lane < n_pg && page >= 0;
-                            const unsigned okm = __ballot_sync(0xffffffffu, ok);
-                            if (lane == 0 && okm) expect_tx(&full[rg.slot], __popc(okm) * P * ROW);
-                            __syncwarp();
-                            if (ok) {  // the cache is read once: evict-first keeps queries and partials in L2
-                                const int row = page * Hkv + g;
-                                if constexpr (E4) tma_load_2d_hint(dst + lane * P * ROW, map, &full[rg.slot], 0, row * P, pol);
-                                else tma_load_4d_hint(dst + lane * P * ROW, map, &full[rg.slot], 0, 0, 0, row * (P / 8), pol);
-                            }
-                            // a page outside the pool: zeros
+                        // a page outside the pool: zeros
 #pragma unroll 1
-                            for (unsigned miss = ~okm & ((1u << n_pg) - 1u); miss; miss &= miss - 1) {
-                                const int j = __ffs(miss) - 1;
+                        for (unsigned miss = ~okm & ((1u << n_pg) - 1u); miss; miss &= miss - 1) {
+                            const int j = __ffs(miss) - 1;
 #pragma unroll 1
-                                for (int e = lane; e < P * ROW / 16; e += 32) st_shared_v4(dst + j * P * ROW + e * 16, 0, 0, 0, 0);
-                                plain = true;
-                            }
-                        }
-                        const int r0 = n_pg * (paged ? P : 0);  // first row not covered by TMA
-                        if (r0 < n_tok) {
+                            for (int e = lane; e < P * ROW / 16; e += 32) st_shared_v4(dst + j * P * ROW + e * 16, 0, 0, 0, 0);
                             plain = true;
-                            const uint8_t *src = seq + (size_t)t0 * seq_step;
-                            size_t step = seq_step;
-                            bool have = true;
-                            if (paged) {  // the last, partial page
-                                const int pg = __shfl_sync(0xffffffffu, page, n_pg);
-                                have = pg >= 0;
-                                src = pool + ((size_t)max(pg, 0) * Hkv + g) * P * ROW;
-                                step = ROW;
-                            }
-                            copy_rows<E4>(dst, r0, n_tok - r0, src, step, have, ptid);
                         }
-                        // values past the end are multiplied by weights of 0: they must be
-                        // finite (keys there give scores that are replaced)
-                        if (!E4 && is_v && !is_fresh && n_tok < TILE) {
-                            plain = true;
+                    }
+                    const int r0 = n_pg * (paged ? P : 0);  // first row not covered by TMA
+                    if (r0 < n_tok) {
+                        plain = true;
+                        const uint8_t *src = seq + (size_t)t0 * seq_step;
+                        size_t step = seq_step;
+                        bool have = true;
+                        if (paged) {  // the last, partial page
+                            const int pg = __shfl_sync(0xffffffffu, page, n_pg);
+                            have = pg >= 0;
+                            src = pool + ((size_t)max(pg, 0) * Hkv + g) * P * ROW;
+                            step = ROW;
+                        }
+                        copy_rows<E4>(dst, r0, n_tok - r0, src, step, have, ptid);
+                    }
+                    // values past the end are multiplied by weights of 0: they must be
+                    // finite (keys there give scores that are replaced)
+                    if (!E4 && is_v && !is_fresh && n_tok < TILE) {
+                        plain = true;
 #pragma unroll 1
-                            for (int idx = ptid; idx < (TILE - n_tok) * 16; idx += 64)
-                                st_shared_v4(dst + kv_off(n_tok + (idx >> 4), idx & 15), 0, 0, 0, 0);
-                        }
-                        if (is_fresh) {
-                            // the nodes' rows: 16 lanes a row, 8 elements a lane
-                            plain = true;
-                            const bf16 *fresh = (const bf16 *)(is_v ? a.v_new : a.k_new) + (size_t)g * DH;
-                            const long long fs = is_v ? a.vs : a.ks;
-                            const int n = nodes[b], c = lane & 15;
-                            unsigned long long vb = 0;
+                        for (int idx = ptid; idx < (TILE - n_tok) * 16; idx += 64)
+                            st_shared_v4(dst + kv_off(n_tok + (idx >> 4), idx & 15), 0, 0, 0, 0);
+                    }
+                    if (is_fresh) {
+                        // the nodes' rows: 16 lanes a row, 8 elements a lane (scores of the rows
+                        // after the last node's are replaced: of V these rows must be zeros)
+                        plain = true;
+                        const bf16 *fresh = (const bf16 *)(is_v ? a.v_new : a.k_new) + (size_t)g * DH;
+                        const long long fs = is_v ? a.vs : a.ks;
+                        const int n = nodes[b], c = lane & 15;
+                        unsigned long long vb = 0;
 #pragma unroll 2
-                            for (int r = pidx * 2 + (lane >> 4); r < 64; r += 4) {
-                                uint4 u = make_uint4(0, 0, 0, 0);
-                                if (r < n) u = *(const uint4 *)(fresh + ((size_t)b * a.N + r) * fs + c * 8);
-                                uint32_t w[4] = {u.x, u.y, u.z, u.w};
-                                if constexpr (!E4) {
-                                    if (is_v) {
-                                        bool odd = false;
-#pragma unroll
-                                        for (int q = 0; q < 4; ++q) {
-                                            const bool lo = (w[q] & 0x7f80u) == 0x7f80u, hi = (w[q] & 0x7f800000u) == 0x7f800000u;
-                                            odd = odd || lo || hi;
-                                            w[q] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
-                                        }
-                                        const unsigned o = __ballot_sync(0xffffffffu, odd);
-                                        const int even = r & ~1;  // (lanes 0-15 hold the even row)
-                                        if (o & 0xffffu) vb |= 1ull << even;
-                                        if (o >> 16) vb |= 2ull << even;
-                                    }
-                                    st_shared_v4(dst + kv_off(r, c), w[0], w[1], w[2], w[3]);
-                                } else {
-                                    // keys as two 8-bit parts, rows r and 64 + r
-                                    float v[8];
-                                    float amax = 0.f;
+                        for (int r = pidx * 2 + (lane >> 4); r < (is_v ? 64 : (n + 1) & ~1); r += 4) {
+                            uint4 u = make_uint4(0, 0, 0, 0);
+                            if (r < n) u = *(const uint4 *)(fresh + ((size_t)b * a.N + r) * fs + c * 8);
+                            uint32_t w[4] = {u.x, u.y, u.z, u.w};
+                            if constexpr (!E4) {
+                                if (is_v) {
+                                    bool odd = false;
 #pragma unroll
                                     for (int q = 0; q < 4; ++q) {
-                                        v[2 * q] = __uint_as_float(w[q] << 16);
-                                        v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
-                                        amax = fmaxf(amax, fmaxf(fabsf(v[2 * q]), fabsf(v[2 * q + 1])));
+                                        const bool lo = (w[q] & 0x7f80u) == 0x7f80u, hi = (w[q] & 0x7f800000u) == 0x7f800000u;
+                                        odd = odd || lo || hi;
+                                        w[q] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
                                     }
-#pragma unroll
-                                    for (int o = 1; o < 16; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-                                    int k;
-                                    const float f = pow2_scale(amax, &k);
-#pragma unroll
-                                    for (int q = 0; q < 8; ++q) v[q] *= f;
-                                    uint2 hi, lo;
-                                    split_codes(v, &hi, &lo);
-                                    *(uint2 *)(dst + off8(r, c >> 1) + (c & 1) * 8) = hi;
-                                    *(uint2 *)(dst + off8(64 + r, c >> 1) + (c & 1) * 8) = lo;
+                                    const unsigned o = __ballot_sync(0xffffffffu, odd);
+                                    const int even = r & ~1;  // (lanes 0-15 hold the even row)
+                                    if (o & 0xffffu) vb |= 1ull << even;
+                                    if (o >> 16) vb |= 2ull << even;
                                 }
+                                st_shared_v4(dst + kv_off(r, c), w[0], w[1], w[2], w[3]);
+                            } else {
+                                // keys as two 8-bit parts, rows r and 64 + r
+                                float v[8];
+                                float amax = 0.f;
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) {
+                                    v[2 * q] = __uint_as_float(w[q] << 16);
+                                    v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
+                                    amax = fmaxf(amax, fmaxf(fabsf(v[2 * q]), fabsf(v[2 * q + 1])));
+                                }
+#pragma unroll
+                                for (int o = 1; o < 16; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+                                int k;
+                                const float f = pow2_scale(amax, &k);
+#pragma unroll
+                                for (int q = 0; q < 8; ++q) v[q] *= f;
+                                uint2 hi, lo;
+                                split_codes(v, &hi, &lo);
+                                *(uint2 *)(dst + off8(r, c >> 1) + (c & 1) * 8) = hi;
+                                *(uint2 *)(dst + off8(64 + r, c >> 1) + (c & 1) * 8) = lo;
                             }
-                            if (!E4 && is_v && lane == 0) bars->vbad[rg.slot][pidx] = vb;
                         }
+                        if (!E4 && is_v && lane == 0) bars->vbad[rg.slot][pidx] = vb;
                     }
                     if (plain) {
                         fence_proxy_async();  // this thread's shared-memory stores
@@ -976,155 +1014,207 @@ __global__ void __launch_bounds__(THREADS, 1)
             bad = __any_sync(0xffffffffu, bad);
             if (bad && lane == 0 && a.status) atomicOr(a.status, SP_DEV_BAD_PAGE);
         } else if (E4 && warp >= CVT) {
-            // ------------------------------------------------------------ V codes -> 16-bit floats
+            // ------------------------------------------------------------ converters
+            // V's codes to 16-bit floats in shared memory: 16 codes at a time, eight times a
+            // thread and tile (rows r0 + 16 k, chunk c)
             const int ct = threadIdx.x - CVT * 32, cw = warp - CVT;
-            Ring rv(lay.nv), rc(CONV);
-            bool ok = true;
+            const int r0 = ct >> 3, c = ct & 7, flip = c >> 2;
+            Ring rv(lay.nv);
+            Ring rc(CONV);
             uint32_t seg_ph = 0;
-#pragma unroll 1
-            for (int x = x0; ok && x < x1; seg_ph ^= 1) {
-                const Seg sg = seg_at(prefix, B, x, x1);
-                x += sg.n;
-                const int b = sg.b, L = lens[b];
-                ok = wait_warp(&bars->q_empty, seg_ph ^ 1, abort);
-                if (!ok) break;
-                load_queries<E4, TPC, MT>(a, b, nodes[b], g, rb, smem + lay.off_q, (unsigned long long *)(smem + OFF_SEES) + seg_ph * 256,
-                                          (float *)(smem + OFF_RS) + seg_ph * 256, cw, 4, lane);
-                arrive_warp(&bars->q_full, lane);
-                // this thread's token of a tile: its scales are asked for a tile ahead, where they
-                // sit (a page table entry) two tiles ahead
-                const int sid = sids[b];
-                const float *sk = nullptr, *sv = nullptr;
-                if (L > 0) {
-                    sk = scale_base(a.cache, sid, 0) + (paged ? (size_t)g * P : g);
-                    sv = scale_base(a.cache, sid, 1) + (paged ? (size_t)g * P : g);
+            bool ok = true;
+            auto convert = [&](const uint8_t *src, uint8_t *dst) {
+                // (the two halves of the chunks in turns: 8 lanes then cover all banks)
+                const uint8_t *src0 = src + flip * 8, *src1 = src + 8 - flip * 8;
+                uint8_t *to0 = dst + kv_off(r0, 2 * c + flip), *to1 = dst + kv_off(r0, 2 * c + 1 - flip);
+#pragma unroll 2
+                for (int k = 0; k < 8; ++k) {
+                    const uint2 z0 = *(const uint2 *)(src0 + k * 2048), z1 = *(const uint2 *)(src1 + k * 2048);
+                    uint32_t h[8];
+                    codes4_to_half4(z0.x, &h[0], &h[1]);
+                    codes4_to_half4(z0.y, &h[2], &h[3]);
+                    codes4_to_half4(z1.x, &h[4], &h[5]);
+                    codes4_to_half4(z1.y, &h[6], &h[7]);
+                    st_shared_v4(to0 + k * 2 * GROUP_STRIDE, h[0], h[1], h[2], h[3]);
+                    st_shared_v4(to1 + k * 2 * GROUP_STRIDE, h[4], h[5], h[6], h[7]);
                 }
-                auto place = [&](int i) {  // -1: no such token, or no page
-                    const int tok = (sg.t_a + i) * TILE + ct;
-                    if (i >= sg.n || tok >= L) return -1ll;
-                    if (!paged) return (long long)tok * Hkv;
-                    const int lp = tok >> P_bits;
-                    const int page = lp < a.cache.kv.max_pages ? __ldg(a.cache.kv.page_table + (size_t)sid * a.cache.kv.max_pages + lp) : -1;
-                    return page < 0 || page >= a.cache.kv.n_pages ? -1ll : (long long)page * Hkv * P + (tok & (P - 1));
-                };
-                auto scales = [&](long long at) {
-                    return at < 0 ? make_float2(0.f, 0.f) : make_float2(__ldg(sk + at), __ldg(sv + at));
-                };
-                float2 next = scales(place(0));
-                long long at = place(1);
+            };
 #pragma unroll 1
-                for (int i = 0; i < sg.n; ++i) {
-                    const int t = sg.t_a + i;
-                    const bool is_fresh = t == sg.nt - 1;
-                    const int n_tok = is_fresh ? 0 : min(TILE, L - t * TILE);
-                    ok = wait_warp(&bars->v_full[rv.slot], rv.ph, abort) &&
-                         wait_warp(&bars->c_empty[rc.slot], rc.ph ^ 1, abort);
+            for (TileWalk w(sh); !w.done(); w.next(), rc.next()) {
+                const int b = w.b;
+                if (w.i == 0) {  // a segment's queries
+                    ok = wait_warp(&bars->q_empty, seg_ph ^ 1, abort);
                     if (!ok) break;
-                    const float2 sc = next;
-                    next = scales(at);
-                    at = place(i + 2);
-                    const uint8_t *src = smem + lay.off_v + rv.slot * SLOT8;
-                    uint8_t *dst = smem + lay.off_c + rc.slot * SLOT16;
-                    float *par = (float *)(smem + lay.off_c + CONV * SLOT16 + rc.slot * PARAMS);
-                    if (!is_fresh) {
-                        // the softmax's constants first: it does not wait for the values
-                        float ks = 0.f, vs = 1.f;
-                        if (ct < n_tok) {
-                            ks = sc.x;
-                            vs = fmaxf(sc.y, 7.888609052210118e-31f);  // 2^-100
-                        }
-                        par[par_at(ct)] = ks * a.scale_log2;
-                        par[par_at(ct) + 2] = __log2f(vs);
-                        par[2 * TILE + ct] = __frcp_rn(vs);
-                        arrive_warp(&bars->c_par[rc.slot], lane);
-                        // 16 rows of 8 chunks a step of the four warps: its row's place in an
-                        // 8-row group is the thread's own, so addresses advance by constants
-                        const int r0 = ct >> 3, c = ct & 7;
-                        const uint8_t *from = src + ct * 16;
-                        uint8_t *to0 = dst + kv_off(r0, 2 * c), *to1 = dst + kv_off(r0, 2 * c + 1);
-#pragma unroll 1
-                        for (int it = 0; it < 8; it += 4) {
-                            uint4 u[4];
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) u[k] = *(const uint4 *)(from + (it + k) * 2048);
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                if (r0 + (it + k) * 16 >= n_tok) u[k] = make_uint4(0, 0, 0, 0);
-                                const uint32_t w[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
-                                uint32_t h[8];
-#pragma unroll
-                                for (int q = 0; q < 8; ++q) h[q] = codes2_to_half2(w[q >> 1], q & 1);
-                                st_shared_v4(to0 + (it + k) * 2 * GROUP_STRIDE, h[0], h[1], h[2], h[3]);
-                                st_shared_v4(to1 + (it + k) * 2 * GROUP_STRIDE, h[4], h[5], h[6], h[7]);
-                            }
-                        }
-                    } else {
-                        const int n = nodes[b], c = lane & 15;
-                        unsigned long long vb = 0;
-#pragma unroll 1
-                        for (int r = cw * 2 + (lane >> 4); r < TILE; r += 8) {
-                            uint4 uk = make_uint4(0, 0, 0, 0), uv = uk;
-                            if (r < n) {
-                                const size_t row = (size_t)b * a.N + r;
-                                uk = *(const uint4 *)((const bf16 *)a.k_new + row * a.ks + (size_t)g * DH + c * 8);
-                                uv = *(const uint4 *)((const bf16 *)a.v_new + row * a.vs + (size_t)g * DH + c * 8);
-                            }
-                            const uint32_t wk[4] = {uk.x, uk.y, uk.z, uk.w}, wv[4] = {uv.x, uv.y, uv.z, uv.w};
-                            float v[8], amk = 0.f, amv = 0.f;
-                            bool odd = false;
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                amk = fmaxf(amk, fmaxf(fabsf(__uint_as_float(wk[q] << 16)), fabsf(__uint_as_float(wk[q] & 0xffff0000u))));
-#pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    const float y = __uint_as_float(e ? wv[q] & 0xffff0000u : wv[q] << 16);
-                                    const bool fin = isfinite(y);
-                                    odd = odd || !fin;
-                                    v[2 * q + e] = fin ? y : 0.f;
-                                    amv = fmaxf(amv, fabsf(v[2 * q + e]));
-                                }
-                            }
-#pragma unroll
-                            for (int o = 1; o < 16; o <<= 1) {
-                                amk = fmaxf(amk, __shfl_xor_sync(0xffffffffu, amk, o));
-                                amv = fmaxf(amv, __shfl_xor_sync(0xffffffffu, amv, o));
-                            }
-                            const unsigned o = __ballot_sync(0xffffffffu, odd);
-                            if (r < 64) {
-                                if (o & 0xffffu) vb |= 1ull << (r & ~1);
-                                if (o >> 16) vb |= 2ull << (r & ~1);
-                            }
-                            int kk, kv;
-                            pow2_scale(amk, &kk);
-                            const float f = pow2_scale(amv, &kv);
-                            st_shared_v4(dst + kv_off(r, c), pack_half(v[0] * f, v[1] * f), pack_half(v[2] * f, v[3] * f),
-                                         pack_half(v[4] * f, v[5] * f), pack_half(v[6] * f, v[7] * f));
-                            if (c == 0) {
-                                // an infinite key saturates in its parts: its scores are NaN
-                                par[par_at(r)] = pow2i(-kk) * a.scale_log2 + (amk - amk);
-                                par[par_at(r) + 2] = (float)-kv;
-                                par[2 * TILE + r] = pow2i(kv);
-                            }
-                        }
-                        if (lane == 0) bars->vbad[rc.slot][cw] = vb;
-                        arrive_warp(&bars->c_par[rc.slot], lane);
-                    }
-                    fence_proxy_async();
-                    arrive_warp(&bars->c_full[rc.slot], lane);
-                    if (lane == 0) mbar_arrive(&bars->v_empty[rv.slot]);
-                    rv.next();
-                    rc.next();
+                    load_queries<E4, TPC, MT>(a, b, nodes[b], g, rb, smem + lay.off_q, (unsigned long long *)(smem + OFF_SEES) + seg_ph * 256,
+                                              (float *)(smem + OFF_RS) + seg_ph * 256, cw, CVT_WARPS, lane);
+                    arrive_warp(&bars->q_full, lane);
+                    seg_ph ^= 1;
                 }
+                ok = wait_warp(&bars->c_empty[rc.slot], rc.ph ^ 1, abort);
+                if (!ok) break;
+                uint8_t *dst = smem + lay.off_c + rc.slot * SLOT16;
+                float *par = (float *)(smem + lay.off_c + CONV * SLOT16 + rc.slot * PARAMS);
+                if (w.fresh()) {
+                    if (ct >= 64) par[2 * TILE + ct] = 0.f;  // (weights of 0 are multiplied by these)
+                    const int n = nodes[b], c16 = lane & 15;
+                    unsigned long long vb = 0;
+#pragma unroll 1
+                    for (int r = cw * 2 + (lane >> 4); r < 64; r += 8) {
+                        if ((r & ~1) >= n) {  // (the pair of rows of this warp)
+                            st_shared_v4(dst + kv_off(r, c16), 0, 0, 0, 0);
+                            if (c16 == 0) par[2 * TILE + r] = 0.f;
+                            continue;
+                        }
+                        uint4 uk = make_uint4(0, 0, 0, 0), uv = uk;
+                        if (r < n) {
+                            const size_t row = (size_t)b * a.N + r;
+                            uk = *(const uint4 *)((const bf16 *)a.k_new + row * a.ks + (size_t)g * DH + c16 * 8);
+                            uv = *(const uint4 *)((const bf16 *)a.v_new + row * a.vs + (size_t)g * DH + c16 * 8);
+                        }
+                        const uint32_t wk[4] = {uk.x, uk.y, uk.z, uk.w}, wv[4] = {uv.x, uv.y, uv.z, uv.w};
+                        float v[8], amk = 0.f, amv = 0.f;
+                        bool odd = false;
+#pragma unroll
+                        for (int q4 = 0; q4 < 4; ++q4) {
+                            amk = fmaxf(amk, fmaxf(fabsf(__uint_as_float(wk[q4] << 16)), fabsf(__uint_as_float(wk[q4] & 0xffff0000u))));
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const float y = __uint_as_float(e ? wv[q4] & 0xffff0000u : wv[q4] << 16);
+                                const bool fin = isfinite(y);
+                                odd = odd || !fin;
+                                v[2 * q4 + e] = fin ? y : 0.f;
+                                amv = fmaxf(amv, fabsf(v[2 * q4 + e]));
+                            }
+                        }
+#pragma unroll
+                        for (int o = 1; o < 16; o <<= 1) {
+                            amk = fmaxf(amk, __shfl_xor_sync(0xffffffffu, amk, o));
+                            amv = fmaxf(amv, __shfl_xor_sync(0xffffffffu, amv, o));
+                        }
+                        const unsigned o = __ballot_sync(0xffffffffu, odd);
+                        if (o & 0xffffu) vb |= 1ull << (r & ~1);
+                        if (o >> 16) vb |= 2ull << (r & ~1);
+                        int kk, kv;
+                        pow2_scale(amk, &kk);
+                        const float f = pow2_scale(amv, &kv);
+                        st_shared_v4(dst + kv_off(r, c16), pack_half(v[0] * f, v[1] * f), pack_half(v[2] * f, v[3] * f),
+                                     pack_half(v[4] * f, v[5] * f), pack_half(v[6] * f, v[7] * f));
+                        if (c16 == 0) {
+                            // an infinite key saturates in its parts: its scores are NaN
+                            par[par_at(r)] = pow2i(-kk) * a.scale_log2 + (amk - amk);
+                            par[par_at(r) + 2] = (float)-kv;
+                            par[2 * TILE + r] = pow2i(kv);
+                        }
+                    }
+                    if (lane == 0) bars->vbad[rc.slot][cw] = vb;
+                    arrive_warp(&bars->c_par[rc.slot], lane);
+                } else {
+                    ok = wait_warp(&bars->v_full[rv.slot], rv.ph, abort);
+                    if (!ok) break;
+                    {  // token ct's constants
+                        const float *sc = (const float *)(smem + lay.off_sc) + rv.slot * 2 * TILE + ct;
+                        const float lg = __log2f(fmaxf(sc[TILE], 7.888609052210118e-31f));  // (2^-100)
+                        par[par_at(ct)] = sc[0] * a.scale_log2;
+                        par[par_at(ct) + 2] = lg;
+                        par[2 * TILE + ct] = fast_exp2(-lg);  // (a weight times its inverse: lg's error cancels)
+                    }
+                    arrive_warp(&bars->c_par[rc.slot], lane);
+                    convert(smem + lay.off_v + rv.slot * SLOT8 + ct * 16, dst);
+                    arrive_warp(&bars->v_empty[rv.slot], lane);
+                    rv.next();
+                }
+                fence_proxy_async();
+                arrive_warp(&bars->c_full[rc.slot], lane);
+            }
+        } else if (E4 && warp == SCALES) {
+            // ------------------------------------------------------------ V's codes and scales
+            // as they lie, for the converters; a row of 128 bytes is 8 lanes'
+            Ring rg(lay.nv);
+            Pages pages(paged, P_bits);
+            int filled = 0;
+            bool stop = false;
+#pragma unroll 1
+            for (int b = sh.b0; b < sh.b1 && !stop; ++b) {
+                const Seg sg = piece(sh, b);
+                const int sid = sids[b], L = lens[b];
+                const float *sk = nullptr, *sv = nullptr;
+                const uint8_t *v = (const uint8_t *)a.cache.kv.v_pool;
+                int t0 = sg.t_a * TILE;
+                if (L > 0) {
+                    sk = scale_base(a.cache, sid, 0);
+                    sv = scale_base(a.cache, sid, 1);
+                    if (!paged) v = (const uint8_t *)a.cache.kv.v_seq[sid] + (size_t)(t0 + (lane >> 3)) * (Hkv * ROW) + g * ROW + (lane & 7) * 16;
+                }
+#pragma unroll 1
+                for (const int end = min(L, t0 + sg.n * TILE); t0 < end; t0 += TILE) {
+                    const int n_tok = min(TILE, L - t0);
+                    pages.at(a, sids, lens, b, t0, lane);
+                    if (!wait_warp(&bars->v_empty[rg.slot], rg.ph ^ 1, abort)) {
+                        stop = true;
+                        break;
+                    }
+                    uint8_t *dst = smem + lay.off_v + rg.slot * SLOT8;
+                    float *sc = (float *)(smem + lay.off_sc) + rg.slot * 2 * TILE + lane;
+                    if (paged) {  // a bulk copy a page
+                        const int rows = min(P, n_tok - lane * P), pg = pages.page(t0, lane * P);
+                        const bool ok = rows > 0 && pg >= 0;
+                        const unsigned bytes = __reduce_add_sync(0xffffffffu, ok ? rows * ROW : 0);
+                        if (lane == 0 && bytes) expect_tx(&bars->v_full[rg.slot], bytes);
+                        __syncwarp();
+                        if (ok) {
+                            bulk_load(dst + lane * P * ROW, v + ((size_t)pg * Hkv + g) * P * ROW, rows * ROW, &bars->v_full[rg.slot]);
+                        } else if (rows > 0) {  // a page outside the pool: zeros
+#pragma unroll 1
+                            for (int e = 0; e < rows * 8; ++e) st_shared_v4(dst + lane * P * ROW + e * 16, 0, 0, 0, 0);
+                        }
+#pragma unroll 1
+                        for (int r = lane; r < TILE; r += 32, sc += 32) {
+                            const int pr = pages.page(t0, r);
+                            if (r < n_tok && pr >= 0) {
+                                const size_t at = ((size_t)pr * Hkv + g) * P + (r & (P - 1));
+                                cp_async4(sc, sk + at);
+                                cp_async4(sc + TILE, sv + at);
+                            } else {
+                                sc[0] = sc[TILE] = 0.f;
+                            }
+                        }
+                    } else {  // (a bulk copy a row took 60 cycles to issue each)
+                        const size_t hop = (size_t)(4 * Hkv) * ROW;
+                        uint8_t *d = dst + lane * 16;
+#pragma unroll 8
+                        for (int r = lane >> 3; r < n_tok; r += 4, v += hop, d += 512) cp_async16(d, v);
+                        size_t at = (size_t)(t0 + lane) * Hkv + g;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k, at += 32 * Hkv)
+                            if (lane + 32 * k < n_tok) {
+                                cp_async4(sc + 32 * k, sk + at);
+                                cp_async4(sc + TILE + 32 * k, sv + at);
+                            }
+                    }
+                    // past the end: weights of 0 times zeros
+#pragma unroll 1
+                    for (int e = n_tok * 8 + lane; e < TILE * 8; e += 32) st_shared_v4(dst + e * 16, 0, 0, 0, 0);
+                    fence_proxy_async();
+                    cp_async_mbar_arrive(&bars->v_full[rg.slot]);
+                    mbar_arrive(&bars->v_full[rg.slot]);  // (the zeros)
+                    ++filled;
+                    rg.next();
+                }
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");  // nothing lands after the CTA is gone
+            if (lane == 0) {                                  // (bulk copies: only after an abort)
+                Ring rd(lay.nv);
+#pragma unroll 1
+                for (int j = 0; j < filled; ++j, rd.next())
+                    if (j + lay.nv >= filled) mbar_wait_drain(&bars->v_full[rd.slot], rd.ph);
             }
         } else if (!E4 && warp >= Ro::Q_WARP && warp < Ro::Q_WARP + Ro::Q_WARPS) {
             // ------------------------------------------------------------ queries
             uint32_t seg_ph = 0;
 #pragma unroll 1
-            for (int x = x0; x < x1; seg_ph ^= 1) {
-                const Seg sg = seg_at(prefix, B, x, x1);
-                x += sg.n;
+            for (int b = sh.b0; b < sh.b1; ++b, seg_ph ^= 1) {
                 if (!wait_warp(&bars->q_empty, seg_ph ^ 1, abort)) break;
-                load_queries<E4, TPC, MT>(a, sg.b, nodes[sg.b], g, rb, smem + lay.off_q,
+                load_queries<E4, TPC, MT>(a, b, nodes[b], g, rb, smem + lay.off_q,
                                           (unsigned long long *)(smem + OFF_SEES) + seg_ph * 256, nullptr, warp - Ro::Q_WARP,
                                           Ro::Q_WARPS, lane);
                 arrive_warp(&bars->q_full, lane);
@@ -1185,9 +1275,8 @@ __global__ void __launch_bounds__(THREADS, 1)
                 if (MT == 1 || w) rk.next();
             };
 #pragma unroll 1
-            for (int x = x0; ok && x < x1; ++j) {
-                const Seg sg = seg_at(prefix, B, x, x1);
-                x += sg.n;
+            for (int b = sh.b0; ok && b < sh.b1; ++b, ++j) {
+                const Seg sg = piece(sh, b);
                 // the same in every lane, and known to be
                 const int items = __shfl_sync(0xffffffffu, sg.n, 0) * MT;
                 const bool has_fresh = __shfl_sync(0xffffffffu, (int)(sg.t_a + sg.n == sg.nt), 0);
@@ -1292,14 +1381,15 @@ bool make_layout(const TreeArgs &a, bool e4, int mt, Layout *lay) {
     if (e4) at += CONV * (SLOT16 + PARAMS);
     lay->off_st = at;
     at += 2 * 8192;
-    const int room = SMEM_MAX - 1024 - at;
-    const int slot = e4 ? SLOT8 : SLOT16;
-    int slots = (e4 ? room - 1024 : room) / slot;
+    lay->off_sc = at;
+    if (e4) at += MAX_AHEAD * 2 * TILE * 4;
+    at = (at + 1023) & ~1023;
+    const int slot = e4 ? SLOT8 : SLOT16, slots = (SMEM_MAX - 1024 - at) / slot;
     if (slots < 2) return false;
-    if (slots > 2 * MAX_RING) slots = 2 * MAX_RING;
-    lay->nk = slots / 2;
-    lay->nv = slots - lay->nk;
-    lay->off_k = (at + 1023) & ~1023;
+    // (8-bit: V's part is what the converters copy ahead)
+    lay->nv = e4 ? (slots / 2 < MAX_AHEAD ? slots / 2 : MAX_AHEAD) : slots / 2 < MAX_RING ? slots / 2 : MAX_RING;
+    lay->nk = slots - lay->nv < MAX_RING ? slots - lay->nv : MAX_RING;
+    lay->off_k = at;
     lay->off_v = lay->off_k + lay->nk * slot;
     lay->smem = lay->off_v + lay->nv * slot + 1024;
     return lay->smem <= SMEM_MAX;
