@@ -132,13 +132,15 @@ struct TreeArgs {
     int *status;
 };
 
-__device__ __forceinline__ int tree_nodes(const TreeArgs &a, int b, int *status) {
-    int n = a.n_nodes ? a.n_nodes[b] : a.N;
+__device__ __forceinline__ int checked_nodes(const TreeArgs &a, int n, int *status) {
     if (n < 0 || n > a.N) {
         if (status) atomicOr(status, SP_DEV_BAD_ROW);
         n = n < 0 ? 0 : a.N;
     }
     return n;
+}
+__device__ __forceinline__ int tree_nodes(const TreeArgs &a, int b, int *status) {
+    return checked_nodes(a, a.n_nodes ? a.n_nodes[b] : a.N, status);
 }
 // The nodes that node i of sequence b sees.
 __device__ __forceinline__ uint64_t tree_mask(const TreeArgs &a, int b, int i, int n) {

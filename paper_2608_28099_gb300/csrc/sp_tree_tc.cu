@@ -62,7 +62,7 @@ constexpr int SOFT = 256;                       // softmax threads
 constexpr int BAR_EPI = 1, BAR_WG = 2;          // (BAR_WG + 1: the second warpgroup's)
 constexpr uint32_t O_COL = 256;                 // TMEM: S0 S1 [0, 256), O0 O1 [256, 512)
 constexpr int kTreeMinTiles = 2;                // fewest tiles a share holds on average
-constexpr int kTreeSegCost = 4;                 // cost of a segment, in tiles
+constexpr int kTreeSegCost = 3;                 // cost of a segment, in tiles
 
 struct Layout {
     int nk, nv;                                 // ring slots
@@ -228,10 +228,11 @@ __device__ __forceinline__ void tree_prefix(const TreeArgs &a, int *prefix, int 
     int sum = 0;
 #pragma unroll 1
     for (int b = b0; b < b1; ++b) {
+        const int n = a.n_nodes ? a.n_nodes[b] : a.N;  // (asked for beside the length)
         const SeqRef sq = resolve_seq(a.seq_ids, a.seq_lens, 0, b, a.cache.kv.n_seqs, a.cache.max_seq_len, status);
         sids[b] = sq.sid;
         lens[b] = sq.len;
-        nodes[b] = tree_nodes(a, b, status);
+        nodes[b] = checked_nodes(a, n, status);
         const int v = ceil_div(sq.len, TILE) + 1;
         prefix[b] = v;
         sum += v;
@@ -390,42 +391,57 @@ template <bool E4, int TPC, int MT>
 __device__ __forceinline__ void load_queries(const TreeArgs &a, int b, int n, int g, int rb, uint8_t *Q,
                                              unsigned long long *sees, float *scale, int wi, int nw, int lane) {
     const int c = lane & 15;
-#pragma unroll 2
-    for (int r = wi * 2 + (lane >> 4); r < TPC * MT; r += 2 * nw) {
-        const int rr = rb * a.rb_rows + r, node = rr / a.G;
-        const bool live = r < a.rb_rows && rr < a.R && node < n;
-        uint4 u = make_uint4(0, 0, 0, 0);
-        if (live)
-            u = *(const uint4 *)((const bf16 *)a.q + ((size_t)b * a.N + node) * a.qs + (size_t)(g * a.G + rr - node * a.G) * DH + c * 8);
-        if (c == 0) sees[r] = live ? tree_mask(a, b, node, n) : 0;
-        uint8_t *q = Q + (MT == 2 ? (r >> 7) * Q_TILE : 0);
-        const int rt = MT == 2 ? r & 127 : r;
-        if constexpr (!E4) {
+    // pairs of rows whose loads are under way together: one node's wait for one latency (8-bit:
+    // two, the code has to stay small)
+    constexpr int AT_ONCE = E4 ? 2 : 4;
+#pragma unroll 1
+    for (int r1 = wi * 2 + (lane >> 4); r1 < TPC * MT; r1 += AT_ONCE * 2 * nw) {
+        uint4 ahead[AT_ONCE];
 #pragma unroll
-            for (int k = 0; k < 128 / TPC; ++k)
-                st_shared_v4(q + (c >> 3) * 16384 + off8(k * TPC + rt, c & 7), u.x, u.y, u.z, u.w);
-        } else {
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-            float v[8], amax = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[2 * i] = __uint_as_float(w[i] << 16);
-                v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-                amax = fmaxf(amax, fmaxf(fabsf(v[2 * i]), fabsf(v[2 * i + 1])));
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int r = r1 + k * 2 * nw, rr = rb * a.rb_rows + r, node = rr / a.G;
+            ahead[k] = make_uint4(0, 0, 0, 0);
+            unsigned long long bits = 0;
+            if (r < a.rb_rows && rr < a.R && node < n) {
+                ahead[k] = *(const uint4 *)((const bf16 *)a.q + ((size_t)b * a.N + node) * a.qs + (size_t)(g * a.G + rr - node * a.G) * DH + c * 8);
+                if (c == 0) bits = tree_mask(a, b, node, n);
             }
+            if (c == 0 && r < TPC * MT) sees[r] = bits;
+        }
 #pragma unroll
-            for (int o = 1; o < 16; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-            int k2;
-            const float f = pow2_scale(amax, &k2);
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int r = r1 + k * 2 * nw;
+            if (r - (lane >> 4) >= TPC * MT) break;
+            const uint4 u = ahead[k];
+            uint8_t *q = Q + (MT == 2 ? (r >> 7) * Q_TILE : 0);
+            const int rt = MT == 2 ? r & 127 : r;
+            if constexpr (!E4) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= f;
-            uint2 hi, lo;
-            split_codes(v, &hi, &lo);
-            if (c == 0) scale[r] = pow2i(-k2) + (amax - amax);  // (an infinite query: NaN)
+                for (int k = 0; k < 128 / TPC; ++k)
+                    st_shared_v4(q + (c >> 3) * 16384 + off8(k * TPC + rt, c & 7), u.x, u.y, u.z, u.w);
+            } else {
+                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+                float v[8], amax = 0.f;
 #pragma unroll
-            for (int k = 0; k < 128 / TPC; ++k) {
-                *(uint2 *)(q + off8(k * TPC + rt, c >> 1) + (c & 1) * 8) = hi;
-                *(uint2 *)(q + 16384 + off8(k * TPC + rt, c >> 1) + (c & 1) * 8) = lo;
+                for (int i = 0; i < 4; ++i) {
+                    v[2 * i] = __uint_as_float(w[i] << 16);
+                    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+                    amax = fmaxf(amax, fmaxf(fabsf(v[2 * i]), fabsf(v[2 * i + 1])));
+                }
+#pragma unroll
+                for (int o = 1; o < 16; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+                int k2;
+                const float f = pow2_scale(amax, &k2);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= f;
+                uint2 hi, lo;
+                split_codes(v, &hi, &lo);
+                if (c == 0) scale[r] = pow2i(-k2) + (amax - amax);  // (an infinite query: NaN)
+#pragma unroll
+                for (int k = 0; k < 128 / TPC; ++k) {
+                    *(uint2 *)(q + off8(k * TPC + rt, c >> 1) + (c & 1) * 8) = hi;
+                    *(uint2 *)(q + 16384 + off8(k * TPC + rt, c >> 1) + (c & 1) * 8) = lo;
+                }
             }
         }
     }
