@@ -153,10 +153,11 @@ void plan_tree_simt(TreeArgs *a, int n_sm);
 cudaError_t launch_tree_simt(const TreeArgs &a, cudaStream_t st);
 size_t tree_simt_slots(const TreeArgs &a);
 // tcgen05: head_dim 128, bf16 rows, bf16 or 8-bit caches, B <= 2048; two launches.
-// seg_tab: B int2 of scratch.
+// split_tab: tree_tc_groups int2 of scratch.
 bool tree_tc_supported(const TreeArgs &a);
 void plan_tree_tc(TreeArgs *a, int n_sm);
 size_t tree_tc_slots(const TreeArgs &a);
-cudaError_t launch_tree_tc(const TreeArgs &a, int2 *seg_tab, cudaStream_t st);
+int tree_tc_groups(const TreeArgs &a);
+cudaError_t launch_tree_tc(const TreeArgs &a, int2 *split_tab, cudaStream_t st);
 
 }  // namespace sp

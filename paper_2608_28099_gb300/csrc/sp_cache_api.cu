@@ -171,12 +171,12 @@ sp_status check_tree(const sp_tree_dims *d, const sp_token_cache *cache, int bat
 }
 
 // Workspace: partials [slot][row][dh], their (max, sum), then the tensor-core kernel's
-// table of shares.
+// table of shares (never nothing: 0 bytes answer an error).
 size_t tree_rows(const TreeArgs &a) { return (a.tensor ? tree_tc_slots(a) : tree_simt_slots(a)) * a.rb_rows; }
 size_t tree_o_bytes(const TreeArgs &a) { return align256(tree_rows(a) * a.dh * sizeof(float)); }
 size_t tree_ml_bytes(const TreeArgs &a) { return align256(tree_rows(a) * 2 * sizeof(float)); }
 size_t tree_bytes(const TreeArgs &a) {
-    return tree_o_bytes(a) + tree_ml_bytes(a) + align256((size_t)a.B * sizeof(int2));
+    return tree_o_bytes(a) + tree_ml_bytes(a) + align256((size_t)(a.tensor ? tree_tc_groups(a) : 1) * sizeof(int2));
 }
 
 }  // namespace
@@ -329,8 +329,8 @@ sp_status sp_attend_tree(sp_stream stream, const sp_tree_dims *dims, const sp_to
     a.part_o = (float *)d_workspace;
     a.part_ml = (float *)((char *)d_workspace + tree_o_bytes(a));
     a.status = d_status;
-    int2 *seg_tab = (int2 *)((char *)a.part_ml + tree_ml_bytes(a));
-    return launched(a.tensor ? launch_tree_tc(a, seg_tab, (cudaStream_t)stream) : launch_tree_simt(a, (cudaStream_t)stream),
+    int2 *split_tab = (int2 *)((char *)a.part_ml + tree_ml_bytes(a));
+    return launched(a.tensor ? launch_tree_tc(a, split_tab, (cudaStream_t)stream) : launch_tree_simt(a, (cudaStream_t)stream),
                     "sp_attend_tree");
 }
 

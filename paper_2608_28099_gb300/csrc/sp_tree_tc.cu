@@ -408,11 +408,11 @@ __device__ __forceinline__ void load_queries(const TreeArgs &a, int b, int n, in
             }
             if (c == 0 && r < TPC * MT) sees[r] = bits;
         }
-#pragma unroll
+#pragma unroll(E4 ? 1 : AT_ONCE)
         for (int k = 0; k < AT_ONCE; ++k) {
             const int r = r1 + k * 2 * nw;
             if (r - (lane >> 4) >= TPC * MT) break;
-            const uint4 u = ahead[k];
+            const uint4 u = E4 && k ? ahead[1] : ahead[E4 ? 0 : k];
             uint8_t *q = Q + (MT == 2 ? (r >> 7) * Q_TILE : 0);
             const int rt = MT == 2 ? r & 127 : r;
             if constexpr (!E4) {
@@ -490,7 +490,7 @@ __device__ __forceinline__ void copy_rows(uint8_t *dst, int r0, int n, const uin
 template <bool E4, int TPC, int MT>
 __global__ void __launch_bounds__(THREADS, 1)
     tree_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                   const __grid_constant__ TreeArgs a, const __grid_constant__ Layout lay, int2 *seg_tab) {
+                   const __grid_constant__ TreeArgs a, const __grid_constant__ Layout lay, int2 *split_tab) {
     typedef Roles<E4> Ro;
     constexpr int NC = 128 / TPC;  // copies
     static_assert(MT == 1 || TPC == 128, "two M tiles hold one copy each");
@@ -507,9 +507,10 @@ __global__ void __launch_bounds__(THREADS, 1)
     const bool paged = a.cache.kv.layout == SP_KV_PAGED;
     const int P = a.cache.kv.page_size, P_bits = 31 - __clz(max(P, 1));  // 16, 32 or 64 (0 contiguous)
     constexpr int ROW = DH * (E4 ? 1 : 2);  // bytes of a cached row
-    // the first kernel of its call: nothing of the caller's is read before
+    // the first kernel of its call: nothing of the caller's is read before.  (The next kernel may
+    // not start before the end: blocks that wait on SMs whose share is done slowed the others,
+    // 200 sequences of 50 to 600 tokens from 104 to 119 us.)
     pdl_wait();
-    pdl_trigger();
 
     tree_prefix(a, prefix, sids, lens, nodes, bars->wsum, blockIdx.x == 0 ? a.status : nullptr);
     const int T = prefix[B];
@@ -559,11 +560,15 @@ __global__ void __launch_bounds__(THREADS, 1)
         sh.b0 = seg_at(prefix, B, sh.x0, sh.x1).b;
         sh.b1 = seg_at(prefix, B, sh.x1 - 1, sh.x1).b + 1;
     }
-    if (blockIdx.x == 0) {  // for the merge: each sequence's first share and its number of them
+    if (blockIdx.x == 0) {  // for the merge: the sequence that goes on behind the share where it starts, its shares
 #pragma unroll 1
-        for (int b = threadIdx.x; b < B; b += THREADS) {
-            const int j0 = group_of(cuts, n_grp, prefix[b]);
-            seg_tab[b] = make_int2(j0, group_of(cuts, n_grp, prefix[b + 1] - 1) - j0 + 1);
+        for (int j = threadIdx.x; j < (int)gridDim.x / Hv; j += THREADS) {
+            int2 t = make_int2(0, 0);
+            if (j < n_grp && cuts[j] < cuts[j + 1]) {
+                const int b = seg_at(prefix, B, cuts[j + 1] - 1, T).b;
+                if (prefix[b] >= cuts[j]) t = make_int2(b, group_of(cuts, n_grp, prefix[b + 1] - 1) - j + 1);
+            }
+            split_tab[j] = t;
         }
     }
 
@@ -965,7 +970,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                         const long long fs = is_v ? a.vs : a.ks;
                         const int n = nodes[b], c = lane & 15;
                         unsigned long long vb = 0;
-#pragma unroll 2
+#pragma unroll 1
                         for (int r = pidx * 2 + (lane >> 4); r < (is_v ? 64 : (n + 1) & ~1); r += 4) {
                             uint4 u = make_uint4(0, 0, 0, 0);
                             if (r < n) u = *(const uint4 *)(fresh + ((size_t)b * a.N + r) * fs + c * 8);
@@ -1197,10 +1202,10 @@ __global__ void __launch_bounds__(THREADS, 1)
                     } else {  // (a bulk copy a row took 60 cycles to issue each)
                         const size_t hop = (size_t)(4 * Hkv) * ROW;
                         uint8_t *d = dst + lane * 16;
-#pragma unroll 8
+#pragma unroll 4
                         for (int r = lane >> 3; r < n_tok; r += 4, v += hop, d += 512) cp_async16(d, v);
                         size_t at = (size_t)(t0 + lane) * Hkv + g;
-#pragma unroll
+#pragma unroll 1
                         for (int k = 0; k < 4; ++k, at += 32 * Hkv)
                             if (lane + 32 * k < n_tok) {
                                 cp_async4(sc + 32 * k, sk + at);
@@ -1336,43 +1341,43 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (warp == MMA) tmem_dealloc(tmem, 512);
 }
 
-// Merge of the pairs that lie in several shares: a warp per (sequence, kv head, row),
-// four dims a lane, the partials in share order.  Pairs of one share return at once.
-constexpr int MERGE_THREADS = 256, MERGE_ROWS = 16;
-__global__ void __launch_bounds__(MERGE_THREADS) tree_tc_merge_kernel(const __grid_constant__ TreeArgs a, const int2 *seg_tab) {
+// Merge of the pairs that lie in several shares (at most one starts in each share): a warp
+// per (share, kv head, row), four dims a lane, the partials in share order, MERGE_AT of them
+// under way together.  The kernel is all latency: with four at a time and two rows a warp, one
+// sequence of 2048 tokens took 20.0 instead of 15.9 us.
+constexpr int MERGE_THREADS = 128, MERGE_ROWS = 4, MERGE_AT = 8;
+__global__ void __launch_bounds__(MERGE_THREADS) tree_tc_merge_kernel(const __grid_constant__ TreeArgs a, const int2 *split_tab) {
     pdl_wait();
-    pdl_trigger();
-    const int hv = blockIdx.x, b = blockIdx.y, Hv = a.Hkv * a.n_rb, g = hv / a.n_rb, rb = hv - g * a.n_rb;
-    const int2 tab = __ldcg(seg_tab + b);
+    const int hv = blockIdx.x, j0 = blockIdx.y, Hv = a.Hkv * a.n_rb, g = hv / a.n_rb, rb = hv - g * a.n_rb;
+    const int2 tab = __ldcg(split_tab + j0);
     if (tab.y <= 1) return;
-    const int lane = threadIdx.x & 31, c = lane * 4, n = tree_nodes(a, b, nullptr);
-#pragma unroll 1
-    for (int q = blockIdx.z * MERGE_ROWS + (threadIdx.x >> 5); q < min(a.rb_rows, (int)(blockIdx.z + 1) * MERGE_ROWS);
-         q += MERGE_THREADS / 32) {
-        const int rr = rb * a.rb_rows + q;
-        if (rr >= a.R) break;
+    const int b = tab.x, nodes = a.n_nodes ? __ldg(a.n_nodes + b) : a.N;
+    static_assert(MERGE_ROWS == MERGE_THREADS / 32, "a row a warp");
+    const int lane = threadIdx.x & 31, c = lane * 4, n = checked_nodes(a, nodes, nullptr);
+    const int q = blockIdx.z * MERGE_ROWS + (threadIdx.x >> 5), rr = rb * a.rb_rows + q;
+    if (q < a.rb_rows && rr < a.R) {
         float m = -INFINITY, l = 0.f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-        for (int e0 = 0; e0 < tab.y; e0 += 4) {
-            float2 ml[4];
-            float4 ov[4];
+        for (int e0 = 0; e0 < tab.y; e0 += MERGE_AT) {
+            float2 ml[MERGE_AT];
+            float4 ov[MERGE_AT];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < MERGE_AT; ++e) {
                 const bool in = e0 + e < tab.y;
-                const size_t slot = ((size_t)(tab.x + e0 + e) * 2 + (e0 + e == 0)) * Hv + hv, row = slot * a.rb_rows + q;
+                const size_t slot = ((size_t)(j0 + e0 + e) * 2 + (e0 + e == 0)) * Hv + hv, row = slot * a.rb_rows + q;
                 ml[e] = in ? __ldcg((const float2 *)(a.part_ml + row * 2)) : make_float2(-INFINITY, 0.f);
                 ov[e] = in ? __ldcg((const float4 *)(a.part_o + row * DH + c)) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
             float mn = m;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) mn = fmaxf(mn, ml[e].x);
+            for (int e = 0; e < MERGE_AT; ++e) mn = fmaxf(mn, ml[e].x);
             if (mn == -INFINITY) continue;
             const float al = m == -INFINITY ? 0.f : exp2f(m - mn);
             l *= al;
             o.x *= al, o.y *= al, o.z *= al, o.w *= al;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < MERGE_AT; ++e) {
                 if (ml[e].x == -INFINITY) continue;
                 const float w = exp2f(ml[e].x - mn);
                 l += w * ml[e].y;
@@ -1448,9 +1453,10 @@ void plan_tree_tc(TreeArgs *a, int n_sm) {
     p.tc_merge_kernel = 1;
 }
 
+int tree_tc_groups(const TreeArgs &a) { return a.plan.tc_ctas / (a.Hkv * a.n_rb); }
 size_t tree_tc_slots(const TreeArgs &a) { return 2 * (size_t)a.plan.tc_ctas; }
 
-cudaError_t launch_tree_tc(const TreeArgs &a, int2 *seg_tab, cudaStream_t st) {
+cudaError_t launch_tree_tc(const TreeArgs &a, int2 *split_tab, cudaStream_t st) {
     const bool e4 = a.cache.dtype == SP_E4M3;
     const int mt = row_tiles(a);
     Layout lay;
@@ -1468,16 +1474,16 @@ cudaError_t launch_tree_tc(const TreeArgs &a, int2 *seg_tab, cudaStream_t st) {
     }
     cudaError_t e;
     if (mt == 2)
-        e = e4 ? run<true, 128, 2>(a, lay, mk, mv, seg_tab, st) : run<false, 128, 2>(a, lay, mk, mv, seg_tab, st);
+        e = e4 ? run<true, 128, 2>(a, lay, mk, mv, split_tab, st) : run<false, 128, 2>(a, lay, mk, mv, split_tab, st);
     else if (a.rb_rows <= 32)
-        e = e4 ? run<true, 32, 1>(a, lay, mk, mv, seg_tab, st) : run<false, 32, 1>(a, lay, mk, mv, seg_tab, st);
+        e = e4 ? run<true, 32, 1>(a, lay, mk, mv, split_tab, st) : run<false, 32, 1>(a, lay, mk, mv, split_tab, st);
     else if (a.rb_rows <= 64)
-        e = e4 ? run<true, 64, 1>(a, lay, mk, mv, seg_tab, st) : run<false, 64, 1>(a, lay, mk, mv, seg_tab, st);
+        e = e4 ? run<true, 64, 1>(a, lay, mk, mv, split_tab, st) : run<false, 64, 1>(a, lay, mk, mv, split_tab, st);
     else
-        e = e4 ? run<true, 128, 1>(a, lay, mk, mv, seg_tab, st) : run<false, 128, 1>(a, lay, mk, mv, seg_tab, st);
+        e = e4 ? run<true, 128, 1>(a, lay, mk, mv, split_tab, st) : run<false, 128, 1>(a, lay, mk, mv, split_tab, st);
     if (e != cudaSuccess) return e;
-    return launch_k(tree_tc_merge_kernel, dim3(a.Hkv * a.n_rb, a.B, ceil_div(a.rb_rows, MERGE_ROWS)), dim3(MERGE_THREADS), 0, st, a,
-                    (const int2 *)seg_tab);
+    return launch_k(tree_tc_merge_kernel, dim3(a.Hkv * a.n_rb, tree_tc_groups(a), ceil_div(a.rb_rows, MERGE_ROWS)), dim3(MERGE_THREADS), 0, st, a,
+                    (const int2 *)split_tab);
 }
 
 }  // namespace sp
