@@ -42,7 +42,7 @@ __device__ __forceinline__ void storev(T *p, const float (&v)[V]) {
 // bytes, or 1 (2 interleaved) where a stride, base or width does not allow that.  A block
 // is one token, or as many as fill it.  HBM-bound where large: TIMED
 template <typename T, int V, bool INTER>
-__global__ void __launch_bounds__(THREADS) rotate_kernel(const __grid_constant__ RotateArgs a) {
+__global__ void __launch_bounds__(THREADS, !INTER && sizeof(T) == 4 ? 5 : 4) rotate_kernel(const __grid_constant__ RotateArgs a) {
     extern __shared__ float2 cs[];  // [token][pair]
     constexpr int U = INTER ? 4 : 2, W = INTER ? V / 2 : V;  // heads in flight, pairs of a unit
     pdl_wait();
@@ -236,7 +236,7 @@ __device__ __forceinline__ Chunk chunk_of(const CopyArgs &a, int *status) {
     return c;
 }
 
-constexpr int MAX_TOK = 32;  // tokens of a block
+constexpr int MAX_TOK = 16;  // tokens of a block (32: the long contexts below read in 72 instead of 68 us)
 
 // The (token, K or V, head) rows of a block in order, `step` at a time.
 struct RowWalk {
@@ -400,7 +400,7 @@ __global__ void __launch_bounds__(THREADS) append_kernel(const __grid_constant__
 template <int LANES, typename CT>
 __global__ void __launch_bounds__(THREADS) read_kernel(const __grid_constant__ CopyArgs a) {
     __shared__ long long out_row[MAX_TOK], place[MAX_TOK];
-    constexpr int U = CT::codes ? 4 : 2, G = THREADS / LANES;  // rows in flight, rows of a pass
+    constexpr int U = 2, G = THREADS / LANES;  // rows in flight, rows of a pass
     pdl_wait();
     pdl_trigger();
     const Chunk ck = chunk_of(a, threadIdx.x == 0 && blockIdx.x % a.chunks == 0 ? a.status : nullptr);
