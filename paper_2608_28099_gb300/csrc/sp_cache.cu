@@ -42,7 +42,7 @@ __device__ __forceinline__ void storev(T *p, const float (&v)[V]) {
 // bytes, or 1 (2 interleaved) where a stride, base or width does not allow that.  A block
 // is one token, or as many as fill it.  HBM-bound where large: TIMED
 template <typename T, int V, bool INTER>
-__global__ void __launch_bounds__(THREADS, !INTER && sizeof(T) == 4 ? 5 : 4) rotate_kernel(const __grid_constant__ RotateArgs a) {
+__global__ void __launch_bounds__(THREADS, !INTER && V == 4 ? 5 : 4) rotate_kernel(const __grid_constant__ RotateArgs a) {
     extern __shared__ float2 cs[];  // [token][pair]
     constexpr int U = INTER ? 4 : 2, W = INTER ? V / 2 : V;  // heads in flight, pairs of a unit
     pdl_wait();

@@ -507,9 +507,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const bool paged = a.cache.kv.layout == SP_KV_PAGED;
     const int P = a.cache.kv.page_size, P_bits = 31 - __clz(max(P, 1));  // 16, 32 or 64 (0 contiguous)
     constexpr int ROW = DH * (E4 ? 1 : 2);  // bytes of a cached row
-    // the first kernel of its call: nothing of the caller's is read before.  (The next kernel may
-    // not start before the end: blocks that wait on SMs whose share is done slowed the others,
-    // 200 sequences of 50 to 600 tokens from 104 to 119 us.)
+    // the first kernel of its call: nothing of the caller's is read before
     pdl_wait();
 
     tree_prefix(a, prefix, sids, lens, nodes, bars->wsum, blockIdx.x == 0 ? a.status : nullptr);
@@ -1337,6 +1335,9 @@ __global__ void __launch_bounds__(THREADS, 1)
     mbar_wait_drain(&bars->fin, 0);
     tc_fence_before();
     __syncthreads();
+    // The next kernel may start only now, and the merge lets none start: blocks that waited on
+    // SMs whose share was done slowed the others (200 sequences of 50 to 600 tokens: 104 -> 119 us).
+    pdl_trigger();
     if (threadIdx.x == 0 && *abort && a.status) atomicOr(a.status, SP_DEV_TIMEOUT);
     if (warp == MMA) tmem_dealloc(tmem, 512);
 }
