@@ -7,7 +7,12 @@
 // tiles of 32 tokens, decoded to fp32 in shared memory, a token a lane for the scores,
 // dh / 32 dims a lane for the values; a warp owns four rows with their running (max,
 // sum, O).  Shares are merged by a second kernel.  Bound by shared-memory reads (5
-// vector loads per 16 multiply-adds a lane in the score product).
+// vector loads per 16 multiply-adds a lane in the score product).  Five sequences of 0 to 500
+// tokens, 11 nodes, head_dim 32, fp32: 16.8 us with the merge, latency.  Where the tensor-core
+// kernel applies this one is not taken: one sequence of 2048 tokens, 8 nodes, 33 against 16 us;
+// 64 tokens, one node, 18 against 12; 64 sequences of 1024 to 8192 tokens, 16 nodes, 4315
+// against 190 (an empty cache alone is faster here, 8.3 against 11.0, and lengths are not known
+// to the host).
 #include "sp_cache.cuh"
 #include "sp_sm100.cuh"
 

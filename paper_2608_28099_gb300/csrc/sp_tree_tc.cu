@@ -34,10 +34,27 @@
 // the sequence's end are zeros, and a node's non-finite values are taken out of the
 // product and added afterwards to the rows that see the node.
 //
-// Warps 0-7: the two softmax warpgroups; then producers (K and V rings: TMA boxes of
-// whole pages, cp.async elsewhere), the MMA issuer (it owns TMEM) and, for 8-bit
-// caches, four warps that turn V's codes into 16-bit floats and the scales into the
-// softmax's constants.  Every wait is time-limited (SP_DEV_TIMEOUT).
+// Warps 0-7: the two softmax warpgroups; then the MMA issuer (it owns TMEM) and the loaders.
+// bf16: three warps load queries, two each K and V (TMA boxes of whole pages, cp.async
+// elsewhere).  8-bit: two warps load K, one V's codes as they lie and the scales, and four turn
+// these into 16-bit floats and the softmax's constants, and load the queries.  Every wait is
+// time-limited (SP_DEV_TIMEOUT).
+//
+// What bounds it, with the merge:
+//   bf16          HBM.  64 sequences of 1024 to 8192 tokens, 32 query heads, 8 kv heads, 16
+//                 nodes: 209 us, 5.9 TB/s.  One sequence of 2048 tokens, 8 nodes: 15.4 us, of
+//                 which 2.7 to know the shares, 2 to the first scores, 1.6 for an epilogue and
+//                 4 for the merge and its launch
+//   8-bit         the chain of a pipeline, scores -> softmax -> product -> next scores (half of
+//                 TMEM is scores, half outputs: no room for the next scores before the product
+//                 has read the weights).  8 sequences of 32768 tokens, 40 heads, 32 nodes (160
+//                 rows, two M tiles): 380 us, 0.45 PFLOP/s, some 5000 cycles of softmax in 6800
+//                 a tile.  128 sequences of 300 to 4000 tokens, 32 heads, one node: 194 us, 3.0
+//                 TB/s, 2600 cycles a tile that the conversion, the V loader and the MMA issuer
+//                 fill to 60 - 80 %.
+// The kernel's code is as large as what the instruction caches hold: loops are unrolled as
+// little as their latency allows (unrolling the conversion and the loaders from 95 to 105 KB of
+// code took the 128 sequences from 287 to 378 us), and waits are few instructions.
 #include <cudaTypedefs.h>
 #include <string.h>
 
@@ -61,8 +78,11 @@ constexpr int SMEM_MAX = 227 * 1024;
 constexpr int SOFT = 256;                       // softmax threads
 constexpr int BAR_EPI = 1, BAR_WG = 2;          // (BAR_WG + 1: the second warpgroup's)
 constexpr uint32_t O_COL = 256;                 // TMEM: S0 S1 [0, 256), O0 O1 [256, 512)
-constexpr int kTreeMinTiles = 2;                // fewest tiles a share holds on average
-constexpr int kTreeSegCost = 3;                 // cost of a segment, in tiles
+// Fewest tiles a share holds on average (one sequence of 2048 tokens, 8 kv heads: 26.1, 20.1,
+// 21.0, 21.4 us with 1, 2, 3, 4), and the cost of a segment in tiles (200 sequences of 50 to 600
+// tokens, 8-bit: 109, 109, 112, 113 us with 2, 3, 4, 6; long ones 195, 195, 194, 197).
+constexpr int kTreeMinTiles = 2;
+constexpr int kTreeSegCost = 3;
 
 struct Layout {
     int nk, nv;                                 // ring slots
@@ -91,9 +111,9 @@ constexpr int OFF_FRONT = OFF_CUTS + (MAX_GRP + 4) * 4;
 static_assert(sizeof(Bars) <= OFF_ML, "barrier block");
 
 // Warp roles: softmax 0-7, MMA 8; bf16 caches: queries 9-11, producers 12-15; 8-bit caches:
-// K producers 9-10, the tiles' constants 11, converters 12-15 (values, queries).
+// K producers 9-10, V's codes and scales 11, converters 12-15 (values, constants, queries).
 constexpr int THREADS = 512;
-constexpr int MMA = 8, SCALES = 11, CVT = 12, CVT_WARPS = 4;
+constexpr int MMA = 8, V_CODES = 11, CVT = 12, CVT_WARPS = 4;
 template <bool E4>
 struct Roles {
     static constexpr int K_WARP = E4 ? 9 : 12, V_WARP = K_WARP + 2, V_WARPS = E4 ? 0 : 2;  // producers
@@ -299,11 +319,7 @@ struct TileWalk {
         if (!done()) sg = piece(sh, b);
     }
     __device__ __forceinline__ bool done() const { return b >= sh.b1; }
-    __device__ __forceinline__ int tile() const { return sg.t_a + i; }
     __device__ __forceinline__ bool fresh() const { return sg.t_a + i == sg.nt - 1; }  // the nodes' tile
-    __device__ __forceinline__ int tokens(const int *lens) const {                     // cached ones
-        return fresh() ? 0 : min(TILE, lens[b] - tile() * TILE);
-    }
     __device__ __forceinline__ void next() {
         if (++i < sg.n) return;
         i = 0;
@@ -1145,7 +1161,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 fence_proxy_async();
                 arrive_warp(&bars->c_full[rc.slot], lane);
             }
-        } else if (E4 && warp == SCALES) {
+        } else if (E4 && warp == V_CODES) {
             // ------------------------------------------------------------ V's codes and scales
             // as they lie, for the converters; a row of 128 bytes is 8 lanes'
             Ring rg(lay.nv);
@@ -1474,6 +1490,14 @@ cudaError_t launch_tree_tc(const TreeArgs &a, int2 *split_tab, cudaStream_t st) 
         if (!ok) return cudaErrorInvalidValue;
     }
     cudaError_t e;
+    // Two M tiles against two blocks of up to 128 rows, which read the cache twice but overlap
+    // scores and softmax: 8 sequences of 32768 tokens, 160 rows, 8-bit 389 against 432 us, bf16
+    // 247 against 270; 32 of 500 to 9000, 200 rows, 296 against 321 and 199 against 199.  (One
+    // sequence of 30000 tokens, whose cache the L2 holds: 66 against 56.)
+    // Four copies of up to 32 rows against two and one: 128 sequences of 300 to 4000 tokens,
+    // 4 rows, 8-bit, 197, 206, 263 us; 64 of 1024 to 8192, 32 rows, bf16 185, 189, 190, 8-bit
+    // 198, 190, 233.  Two of up to 64 rows against one: 64 rows, bf16 190 and 192, 8-bit 223
+    // and 253.
     if (mt == 2)
         e = e4 ? run<true, 128, 2>(a, lay, mk, mv, split_tab, st) : run<false, 128, 2>(a, lay, mk, mv, split_tab, st);
     else if (a.rb_rows <= 32)
