@@ -8,19 +8,8 @@ namespace sp {
 namespace {
 
 constexpr int THREADS = 256;
+constexpr int GROUPS = 4;  // most token groups of a rotating block (16: the same)
 
-template <typename T, int V>
-__device__ __forceinline__ void loadv(const T *p, float (&v)[V]) {
-    if constexpr (V == 8 && sizeof(T) == 2) {
-        load8(p, v);
-    } else if constexpr (V == 4 && sizeof(T) == 4) {
-        const float4 f = *(const float4 *)p;
-        v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w;
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = to_f(p[i]);
-    }
-}
 template <typename T, int V>
 __device__ __forceinline__ void storev(T *p, const float (&v)[V]) {
     if constexpr (V == 8 && sizeof(T) == 2) {
@@ -34,20 +23,56 @@ __device__ __forceinline__ void storev(T *p, const float (&v)[V]) {
     }
 }
 
+// V elements as they lie: 16 bytes, or one by one.
+template <typename T, int V>
+struct RawVec {
+    static constexpr bool WIDE = V * sizeof(T) == 16;
+    union {
+        uint4 w;
+        T e[V];
+    };
+    __device__ __forceinline__ RawVec() {}
+    __device__ __forceinline__ void load(const T *p) {
+        if constexpr (WIDE) {
+            w = *(const uint4 *)p;
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) e[i] = p[i];
+        }
+    }
+    __device__ __forceinline__ void store(T *p) const {
+        if constexpr (WIDE) {
+            *(uint4 *)p = w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) p[i] = e[i];
+        }
+    }
+    __device__ __forceinline__ void get(float (&v)[V]) const {
+        if constexpr (V == 8) {
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(u[i] << 16), v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = to_f(e[i]);
+        }
+    }
+};
+
 // Rotate (or turn back) heads.  A thread has one unit of a head -- the two vectors that
 // turn into one another (half layout), one vector of whole pairs (interleaved), or one
-// vector of the dims that pass -- for every head it visits of one token, U heads' loads in
-// flight, the first of them issued before the block forms its tokens' (cos, sin) in shared
-// memory (one sincospif a (token, pair), shared by all heads).  V elements a vector: 16
-// bytes, or 1 (2 interleaved) where a stride, base or width does not allow that.  A block
-// is one token, or as many as fill it.  HBM-bound where large: 4099 tokens of 40 fp32 heads
-// turned back in 26.4 us, 6.35 TB/s; 16384 tokens of 48 bf16 heads, half of each in pairs, in
-// 85 us, 4.7 TB/s (56 % of the issue slots, a block a token: its (cos, sin) and its barrier are
-// not hidden); 16 tokens in 5.3 us (a launch).  fp32 halves: five blocks an SM instead of four
-// took 26.4 instead of 28.2 us, the pairs' four heads in flight then spill (103 us); two of
-// them in flight took 90.6 us.
+// vector of the dims that pass -- for every head it visits of a token, U heads at a time: the
+// next ones' loads are under way, as they lie, while these are turned.  (cos, sin) of the
+// block's tokens are formed in shared memory behind the first loads (one sincospif a (token,
+// pair), shared by all heads).  V elements a vector: 16 bytes, or 1 (2 interleaved) where a
+// stride, base or width does not allow that.  A group of tokens fills the block; a block takes
+// up to GROUPS of them one after another.  HBM-bound where large: 16384 tokens of 48 bf16
+// heads, half of each in pairs, 61 us, 6.6 TB/s (one group a block, hence nothing to load
+// ahead: 69; values held as floats: 85); 4099 tokens of 40 fp32 heads turned back, one group a
+// block, 27.3 us, 6.2 TB/s; 16 tokens 5.3 us (a launch).
 template <typename T, int V, bool INTER>
-__global__ void __launch_bounds__(THREADS, !INTER && V == 4 ? 5 : 4) rotate_kernel(const __grid_constant__ RotateArgs a) {
+__global__ void __launch_bounds__(THREADS, 4) rotate_kernel(const __grid_constant__ RotateArgs a) {
     extern __shared__ float2 cs[];  // [token][pair]
     constexpr int U = INTER ? 4 : 2, W = INTER ? V / 2 : V;  // heads in flight, pairs of a unit
     pdl_wait();
@@ -55,79 +80,106 @@ __global__ void __launch_bounds__(THREADS, !INTER && V == 4 ? 5 : 4) rotate_kern
     const int half = a.rot.half, turn = (INTER ? a.rot.rot : half) / V, units = turn + (a.dh - a.rot.rot) / V;
     const int wide = min(units, THREADS), heads = min(a.n_heads, THREADS / wide), nt = a.tokens_per_block;
     const int per = wide * heads, tl = threadIdx.x / per, rest = threadIdx.x - tl * per, h0 = rest / wide;
-    const int t0 = blockIdx.x * nt, t = t0 + tl;
-    const bool mine = tl < nt && t < a.n_tokens;
-    int c = rest - h0 * wide;
+    const int c0 = rest - h0 * wide, t0 = blockIdx.x * nt * a.groups, end = min(t0 + nt * a.groups, a.n_tokens);
+    struct Vecs {
+        RawVec<T, V> p[U], q[INTER ? 1 : U];
+    };
+    struct At {  // what a thread does next: heads h, h + heads .. of a unit of token t
+        int t, c, h;
+    };
     auto place = [&](int unit) { return unit < turn ? unit * V : a.rot.rot + (unit - turn) * V; };
-    float p[U][V], q[INTER ? 1 : U][V];
-    auto load = [&](int unit, int h) {
-        const T *x = (const T *)a.x + t * a.xt + place(unit);
+    auto load = [&](At i, Vecs &v) {
+        const T *x = (const T *)a.x + i.t * a.xt + i.h * a.xh + place(i.c);
+        const long long step = heads * a.xh;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int hh = h + u * heads;
-            if (hh >= a.n_heads) continue;
-            loadv<T, V>(x + hh * a.xh, p[u]);
+        for (int u = 0; u < U; ++u, x += step) {
+            if (i.h + u * heads >= a.n_heads) break;
+            v.p[u].load(x);
             if constexpr (!INTER) {
-                if (unit < turn) loadv<T, V>(x + hh * a.xh + half, q[u]);
+                if (i.c < turn) v.q[u].load(x + half);
             }
         }
     };
-    if (mine) load(c, h0);
-    for (int i = threadIdx.x; i < nt * half; i += THREADS) {
+    At at{tl < nt ? t0 + tl : end, c0, h0};
+    Vecs v, ahead;
+    if (at.t < end) load(at, v);
+    for (int i = threadIdx.x; i < (end - t0) * half; i += THREADS) {
         const int k = i / half;
-        if (t0 + k >= a.n_tokens) break;
-        float2 v = rotary_cs(a.rot, a.pos[t0 + k], i - k * half);
-        if (a.backward) v.y = -v.y;
-        cs[i] = v;
+        float2 f = rotary_cs(a.rot, a.pos[t0 + k], i - k * half);
+        if (a.backward) f.y = -f.y;
+        cs[i] = f;
     }
     __syncthreads();
-    if (!mine) return;
-    for (bool first = true; c < units; c += wide, first = false) {
-        const bool turns = c < turn;
-        float2 k[W];
-        if (turns) {
-#pragma unroll
-            for (int i = 0; i < W; ++i) k[i] = cs[tl * half + c * W + i];
-        }
-        T *y = (T *)a.y + t * a.yt + place(c);
-        for (int h = h0; h < a.n_heads; h += U * heads) {
-            if (!first || h != h0) load(c, h);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int hh = h + u * heads;
-                if (hh >= a.n_heads) continue;
-                if (turns) {
-#pragma unroll
-                    for (int i = 0; i < W; ++i) {
-                        float *one, *two;
-                        if constexpr (INTER) one = &p[u][2 * i], two = &p[u][2 * i + 1];
-                        else one = &p[u][i], two = &q[u][i];
-                        const float f = *one;
-                        *one = f * k[i].x - *two * k[i].y;
-                        *two = *two * k[i].x + f * k[i].y;
-                    }
-                    if constexpr (!INTER) storev<T, V>(y + hh * a.yh + half, q[u]);
-                }
-                storev<T, V>(y + hh * a.yh, p[u]);
+#pragma unroll 1
+    while (at.t < end) {
+        At next = at;
+        next.h += U * heads;
+        if (next.h >= a.n_heads) {
+            next.h = h0;
+            next.c += wide;
+            if (next.c >= units) {
+                next.c = c0;
+                next.t += nt;
             }
         }
+        if (next.t < end) load(next, ahead);
+        T *y = (T *)a.y + at.t * a.yt + at.h * a.yh + place(at.c);
+        const long long step = heads * a.yh;
+        if (at.c < turn) {
+            float2 k[W];
+#pragma unroll
+            for (int i = 0; i < W; ++i) k[i] = cs[(at.t - t0) * half + at.c * W + i];
+#pragma unroll
+            for (int u = 0; u < U; ++u, y += step) {
+                if (at.h + u * heads >= a.n_heads) break;
+                float p[V], q[INTER ? 1 : V];
+                v.p[u].get(p);
+                if constexpr (!INTER) v.q[u].get(q);
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    float *one, *two;
+                    if constexpr (INTER) one = &p[2 * i], two = &p[2 * i + 1];
+                    else one = &p[i], two = &q[i];
+                    const float f = *one;
+                    *one = f * k[i].x - *two * k[i].y;
+                    *two = *two * k[i].x + f * k[i].y;
+                }
+                if constexpr (!INTER) storev<T, V>(y + half, q);
+                storev<T, V>(y, p);
+            }
+        } else {  // dims that pass
+#pragma unroll
+            for (int u = 0; u < U; ++u, y += step) {
+                if (at.h + u * heads >= a.n_heads) break;
+                v.p[u].store(y);
+            }
+        }
+        v = ahead;
+        at = next;
     }
 }
 
 template <typename T, int V, bool INTER>
-cudaError_t run_rotate(RotateArgs a, cudaStream_t st) {
+cudaError_t run_rotate(RotateArgs a, int n_sm, cudaStream_t st) {
     const int turn = (INTER ? a.rot.rot : a.rot.half) / V, units = turn + (a.dh - a.rot.rot) / V;
     const int wide = units < THREADS ? units : THREADS, fit = THREADS / wide;
     const int per = wide * (a.n_heads < fit ? a.n_heads : fit);
     a.tokens_per_block = THREADS / per;
-    const dim3 grid(ceil_div(a.n_tokens, a.tokens_per_block));
-    const size_t smem = (size_t)a.tokens_per_block * a.rot.half * sizeof(float2);  // (at most 16 KB: a token has half / V threads)
+    // Groups of such tokens a block: up to GROUPS as long as every SM has 16 blocks, four rounds of
+    // four (with half as many 4099 tokens took 27.5 instead of 27.3 us, with a quarter 31.8).
+    a.groups = 1;
+    while (a.groups < GROUPS && (long long)a.groups * 2 * a.tokens_per_block * n_sm * 16 <= a.n_tokens &&
+           a.groups * 2 * a.tokens_per_block * a.rot.half <= 4096)
+        a.groups *= 2;
+    const int tokens = a.tokens_per_block * a.groups;
+    const dim3 grid(ceil_div(a.n_tokens, tokens));
+    const size_t smem = (size_t)tokens * a.rot.half * sizeof(float2);  // (at most 32 KB)
     return launch_k(rotate_kernel<T, V, INTER>, grid, dim3(THREADS), smem, st, a);
 }
 template <typename T, int V>
-cudaError_t pick_rotate(const RotateArgs &a, cudaStream_t st) {
-    if (a.rot.interleaved) return run_rotate<T, V == 1 ? 2 : V, true>(a, st);
-    return run_rotate<T, V, false>(a, st);
+cudaError_t pick_rotate(const RotateArgs &a, int n_sm, cudaStream_t st) {
+    if (a.rot.interleaved) return run_rotate<T, V == 1 ? 2 : V, true>(a, n_sm, st);
+    return run_rotate<T, V, false>(a, n_sm, st);
 }
 
 // 8 elements to a row, in vectors where the row allows them.
@@ -484,13 +536,13 @@ int tokens_a_block(long long tokens, int n_sm) {
 
 }  // namespace
 
-cudaError_t launch_rotate(int dtype, const RotateArgs &a, cudaStream_t st) {
+cudaError_t launch_rotate(int dtype, const RotateArgs &a, int n_sm, cudaStream_t st) {
     const int es = dtype == SP_F32 ? 4 : 2, V = 16 / es;
     const long long strides = a.xt | a.xh | a.yt | a.yh;
     const bool vec = !(((uintptr_t)a.x | (uintptr_t)a.y) & 15) && strides % V == 0 &&
                      (a.rot.interleaved ? a.rot.rot : a.rot.half) % V == 0 && (a.dh - a.rot.rot) % V == 0;
-    if (dtype == SP_F32) return vec ? pick_rotate<float, 4>(a, st) : pick_rotate<float, 1>(a, st);
-    return vec ? pick_rotate<bf16, 8>(a, st) : pick_rotate<bf16, 1>(a, st);
+    if (dtype == SP_F32) return vec ? pick_rotate<float, 4>(a, n_sm, st) : pick_rotate<float, 1>(a, n_sm, st);
+    return vec ? pick_rotate<bf16, 8>(a, n_sm, st) : pick_rotate<bf16, 1>(a, n_sm, st);
 }
 
 cudaError_t launch_append(const CopyArgs &in, int n_sm, cudaStream_t st) {

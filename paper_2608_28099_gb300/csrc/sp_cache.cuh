@@ -91,9 +91,9 @@ struct RotateArgs {
     const void *x;
     void *y;
     long long xt, xh, yt, yh;  // strides, elements
-    int tokens_per_block;      // (set by the launch)
+    int tokens_per_block, groups;  // (set by the launch)
 };
-cudaError_t launch_rotate(int dtype, const RotateArgs &a, cudaStream_t st);
+cudaError_t launch_rotate(int dtype, const RotateArgs &a, int n_sm, cudaStream_t st);
 
 struct CopyArgs {  // append (rows -> cache) and read (cache -> rows)
     CacheDev cache;

@@ -251,7 +251,7 @@ sp_status sp_rotate(sp_stream stream, const sp_rotary *rot, int n_tokens, const 
     a.xh = x_head_stride;
     a.yt = y_token_stride;
     a.yh = y_head_stride;
-    return launched(launch_rotate(dtype, a, (cudaStream_t)stream), "sp_rotate");
+    return launched(launch_rotate(dtype, a, sm_count(), (cudaStream_t)stream), "sp_rotate");
 }
 
 sp_status sp_cache_append(sp_stream stream, const sp_token_cache *cache, const sp_rotary *rot, int batch,
