@@ -249,23 +249,24 @@ template <typename T>
 struct Cached16 {
     static constexpr bool codes = false;
     Raw8<T> a, b;
-    __device__ __forceinline__ void load(const void *base, const float *, long long row, int dh, int e) {
-        a.load(base, row * dh + e, 1);
-        b.load(base, row * dh + e + 8, 1);
+    __device__ __forceinline__ void load(const void *base, const float *, long long row, int dh, int e0, int e1) {
+        a.load(base, row * dh + e0, 1);
+        b.load(base, row * dh + e1, 1);
     }
     __device__ __forceinline__ void get(float (&v0)[8], float (&v1)[8]) const { a.get(v0), b.get(v1); }
 };
 struct Code16 {  // codes and their row's scale
     static constexpr bool codes = true;
-    uint4 u;
+    uint2 a, b;
     float s;
-    __device__ __forceinline__ void load(const void *base, const float *scale, long long row, int dh, int e) {
-        u = *(const uint4 *)((const uint8_t *)base + row * dh + e);
+    __device__ __forceinline__ void load(const void *base, const float *scale, long long row, int dh, int e0, int e1) {
+        const uint8_t *p = (const uint8_t *)base + row * dh;
+        a = *(const uint2 *)(p + e0), b = *(const uint2 *)(p + e1);
         s = scale[row];
     }
     __device__ __forceinline__ void get(float (&v0)[8], float (&v1)[8]) const {
-        codes_to_float(make_uint2(u.x, u.y), v0);
-        codes_to_float(make_uint2(u.z, u.w), v1);
+        codes_to_float(a, v0);
+        codes_to_float(b, v1);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v0[i] *= s, v1[i] *= s;
     }
@@ -295,17 +296,18 @@ __device__ __forceinline__ Chunk chunk_of(const CopyArgs &a, int *status) {
 
 constexpr int MAX_TOK = 16;  // tokens of a block (32: the long contexts below read in 72 instead of 68 us)
 
-// The (token, K or V, head) rows of a block in order, `step` at a time.
+// The (token, K or V, head) rows of a block in order, a fixed step at a time.
 struct RowWalk {
-    int j, is_v, h;
-    __device__ __forceinline__ RowWalk(int r, int Hkv) : j(r / (2 * Hkv)), is_v((r / Hkv) & 1), h(r % Hkv) {}
-    __device__ __forceinline__ void next(int step, int Hkv) {
-        h += step;
-        while (h >= Hkv) {
-            h -= Hkv;
-            j += is_v;
-            is_v ^= 1;
-        }
+    int jv, h;                 // 2 token + (V), head
+    int heads, step_jv, step_h;
+    __device__ __forceinline__ RowWalk(int r, int step, int Hkv)
+        : jv(r / Hkv), h(r - r / Hkv * Hkv), heads(Hkv), step_jv(step / Hkv), step_h(step - step / Hkv * Hkv) {}
+    __device__ __forceinline__ int j() const { return jv >> 1; }
+    __device__ __forceinline__ int is_v() const { return jv & 1; }
+    __device__ __forceinline__ void next() {
+        h += step_h;
+        jv += step_jv;
+        if (h >= heads) h -= heads, ++jv;
     }
 };
 
@@ -314,12 +316,17 @@ struct RowWalk {
 // layout), so that a rotation stays in its lane, else neighbours.  U rows' loads are in
 // flight, the first of them issued before the block looks up its tokens' pages and forms
 // their (cos, sin).  The row's amax is a shuffle among its lanes.  Bound by its
-// instructions (about ten an element: rotation, amax, scale, conversion): 12 prompts of 500 to
-// 4000 tokens, 8 kv heads, rotated and quantised in 51 to 60 us, 2.8 to 3.3 TB/s; 64 accepted
-// paths of up to 6 tokens in 4.7 us (a launch).  One row in flight took 75 to 85 us, 64
-// registers (four blocks an SM) 60 us.
+// instructions (about ten an element: rotation, amax, scale, conversion) and its loads' latency:
+// 12 prompts of 500 to 4000 tokens, 8 kv heads, rotated and quantised at 3.2 to 4.0 TB/s, 42 to
+// 52 us by the lengths drawn; 64 accepted paths of up to 6 tokens in 4.6 us (a launch).  Three
+// blocks an SM took 52 to 55 us, one row in flight 75 to 85.  (fp32 rows hold twice the
+// registers: two blocks.)
+template <typename T>
+constexpr int kAppendBlocks = 2;  // blocks an SM
+template <>
+constexpr int kAppendBlocks<bf16> = 4;
 template <int LANES, typename T>
-__global__ void __launch_bounds__(THREADS) append_kernel(const __grid_constant__ CopyArgs a) {
+__global__ void __launch_bounds__(THREADS, kAppendBlocks<T>) append_kernel(const __grid_constant__ CopyArgs a) {
     extern __shared__ float2 cs[];  // [token][pair]
     __shared__ long long place[MAX_TOK];  // the cache's (token, head 0) row; -1: skipped
     constexpr int U = 2, G = THREADS / LANES;  // rows in flight, rows of a pass
@@ -342,15 +349,15 @@ __global__ void __launch_bounds__(THREADS) append_kernel(const __grid_constant__
     };
     auto load = [&](RowWalk w, int pass) {
 #pragma unroll
-        for (int u = 0; u < U; ++u, w.next(G, Hkv)) {
+        for (int u = 0; u < U; ++u, w.next()) {
             if (first + (pass + u) * G >= rows) continue;
-            const long long at = source(w.j, w.is_v, w.h);
+            const long long at = source(w.j(), w.is_v(), w.h);
             if (at < 0) continue;
-            x0[u].load(w.is_v ? a.v : a.k, at + e0, a.vec);
-            x1[u].load(w.is_v ? a.v : a.k, at + e1, a.vec);
+            x0[u].load(w.is_v() ? a.v : a.k, at + e0, a.vec);
+            x1[u].load(w.is_v() ? a.v : a.k, at + e1, a.vec);
         }
     };
-    RowWalk w(first, Hkv);
+    RowWalk w(first, G, Hkv);
     load(w, 0);
     if ((int)threadIdx.x < ck.n) {
         const int j = threadIdx.x, t = ck.sq.len + ck.j0 + j;
@@ -375,15 +382,15 @@ __global__ void __launch_bounds__(THREADS) append_kernel(const __grid_constant__
     for (int pass = 0; pass < passes; pass += U) {
         if (pass > 0) load(w, pass);
 #pragma unroll
-        for (int u = 0; u < U; ++u, w.next(G, Hkv)) {
+        for (int u = 0; u < U; ++u, w.next()) {
             if (pass + u >= passes) break;  // (whole warps stay for the shuffles)
-            const long long p0 = first + (pass + u) * G < rows ? place[w.j] : -1;
+            const long long p0 = first + (pass + u) * G < rows ? place[w.j()] : -1;
             const bool ok = p0 >= 0;
             const long long dst = p0 + (long long)w.h * head_step;
             float v0[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, v1[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (ok) x0[u].get(v0), x1[u].get(v1);
-            if (ok && half && !w.is_v) {
-                const float2 *k = cs + w.j * half;
+            if (ok && half && !w.is_v()) {
+                const float2 *k = cs + w.j() * half;
                 if (in_lane) {
                     if (lane < nh) {
 #pragma unroll
@@ -405,7 +412,7 @@ __global__ void __launch_bounds__(THREADS) append_kernel(const __grid_constant__
                         two = two * f.x + p * f.y;
                     }
                 } else {  // pairs across lanes: the partner is read from the row
-                    const long long at = source(w.j, 0, w.h);
+                    const long long at = source(w.j(), 0, w.h);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         if (e0 + i >= a.rot.rot) break;
@@ -441,14 +448,14 @@ __global__ void __launch_bounds__(THREADS) append_kernel(const __grid_constant__
                         return make_uint2(float_to_codes2(v[0] * inv, v[1] * inv) | float_to_codes2(v[2] * inv, v[3] * inv) << 16,
                                           float_to_codes2(v[4] * inv, v[5] * inv) | float_to_codes2(v[6] * inv, v[7] * inv) << 16);
                     };
-                    uint8_t *to = (uint8_t *)(w.is_v ? vb : kb) + dst * dh;
+                    uint8_t *to = (uint8_t *)(w.is_v() ? vb : kb) + dst * dh;
                     *(uint2 *)(to + e0) = codes(v0);
                     *(uint2 *)(to + e1) = codes(v1);
-                    if (lane == 0) (w.is_v ? vs : ks)[dst] = amax * (1.f / kMaxCode);
+                    if (lane == 0) (w.is_v() ? vs : ks)[dst] = amax * (1.f / kMaxCode);
                 }
             } else if (ok) {
-                store_row8(w.is_v ? vb : kb, c.dtype, dst * dh + e0, 1, v0);
-                store_row8(w.is_v ? vb : kb, c.dtype, dst * dh + e1, 1, v1);
+                store_row8(w.is_v() ? vb : kb, c.dtype, dst * dh + e0, 1, v0);
+                store_row8(w.is_v() ? vb : kb, c.dtype, dst * dh + e1, 1, v1);
             }
         }
     }
@@ -457,8 +464,9 @@ __global__ void __launch_bounds__(THREADS) append_kernel(const __grid_constant__
 // Read back: rows the other way, 16 elements a lane; tokens outside the sequence give
 // zeros.  A block's tokens are looked up once, then U rows a thread are in flight.  CT: the
 // cache's elements (Code16: 8 bits).  Bound by its loads' latency and HBM: 6 contexts of 3000
-// to 9000 tokens, 8 kv heads, 8-bit, as bf16 in 64 to 66 us, 4.6 TB/s; 3 of 100 to 700 tokens
-// as fp32 in 7.9 us.  Four rows in flight took 66 to 68 and 8.2 us, five blocks an SM 66 and 9.4.
+// to 9000 tokens, 8 kv heads, 8-bit, as bf16 in 60 us, 4.9 TB/s; 3 of 100 to 700 tokens as fp32
+// in 7.1 us.  Sixteen neighbouring elements a lane, whose halves are stored 32 bytes apart, took
+// 65 and 7.9 us, five blocks an SM 56 and 8.2, the next rows' loads under way 71 and 8.3.
 template <int LANES, typename CT>
 __global__ void __launch_bounds__(THREADS) read_kernel(const __grid_constant__ CopyArgs a) {
     __shared__ long long out_row[MAX_TOK], place[MAX_TOK];
@@ -468,7 +476,8 @@ __global__ void __launch_bounds__(THREADS) read_kernel(const __grid_constant__ C
     const Chunk ck = chunk_of(a, threadIdx.x == 0 && blockIdx.x % a.chunks == 0 ? a.status : nullptr);
     if (ck.n == 0) return;  // uniform over the block
     const CacheDev &c = a.cache;
-    const int Hkv = c.Hkv, dh = LANES * 16, rows = ck.n * 2 * Hkv, e = threadIdx.x % LANES * 16;
+    const int Hkv = c.Hkv, dh = LANES * 16, rows = ck.n * 2 * Hkv;
+    const int e0 = threadIdx.x % LANES * 8, e1 = e0 + dh / 2;  // two chunks: neighbours store side by side
     const int head_step = c.kv.layout == SP_KV_PAGED ? c.kv.page_size : 1, sid = ck.sq.sid;
     if ((int)threadIdx.x < ck.n) {
         const int j = ck.j0 + threadIdx.x;
@@ -489,26 +498,26 @@ __global__ void __launch_bounds__(THREADS) read_kernel(const __grid_constant__ C
         if constexpr (CT::codes) ks = scale_base(c, sid, 0), vs = scale_base(c, sid, 1);
     }
     __syncthreads();
-    RowWalk w(threadIdx.x / LANES, Hkv);
+    RowWalk w(threadIdx.x / LANES, G, Hkv);
 #pragma unroll 1
     for (int r = threadIdx.x / LANES; r < rows; r += U * G) {
         CT x[U];
         RowWalk s = w;
 #pragma unroll
-        for (int u = 0; u < U; ++u, s.next(G, Hkv)) {
-            const long long p0 = r + u * G < rows ? place[s.j] : -1;
+        for (int u = 0; u < U; ++u, s.next()) {
+            const long long p0 = r + u * G < rows ? place[s.j()] : -1;
             if (p0 < 0) continue;
-            x[u].load(s.is_v ? vb : kb, s.is_v ? vs : ks, p0 + (long long)s.h * head_step, dh, e);
+            x[u].load(s.is_v() ? vb : kb, s.is_v() ? vs : ks, p0 + (long long)s.h * head_step, dh, e0, e1);
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u, w.next(G, Hkv)) {
-            const long long row = r + u * G < rows ? out_row[w.j] : -1;
+        for (int u = 0; u < U; ++u, w.next()) {
+            const long long row = r + u * G < rows ? out_row[w.j()] : -1;
             if (row < 0) continue;
             float v0[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, v1[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (place[w.j] >= 0) x[u].get(v0, v1);
-            const long long to = row * (w.is_v ? a.rows.v_stride : a.rows.k_stride) + w.h * dh + e;
-            store_row8(w.is_v ? a.v : a.k, a.dtype, to, a.vec, v0);
-            store_row8(w.is_v ? a.v : a.k, a.dtype, to + 8, a.vec, v1);
+            if (place[w.j()] >= 0) x[u].get(v0, v1);
+            const long long to = row * (w.is_v() ? a.rows.v_stride : a.rows.k_stride) + w.h * dh;
+            store_row8(w.is_v() ? a.v : a.k, a.dtype, to + e0, a.vec, v0);
+            store_row8(w.is_v() ? a.v : a.k, a.dtype, to + e1, a.vec, v1);
         }
     }
 }
