@@ -464,7 +464,7 @@ __global__ void __launch_bounds__(THREADS, kAppendBlocks<T>) append_kernel(const
 // Read back: rows the other way, 16 elements a lane; tokens outside the sequence give
 // zeros.  A block's tokens are looked up once, then U rows a thread are in flight.  CT: the
 // cache's elements (Code16: 8 bits).  Bound by its loads' latency and HBM: 6 contexts of 3000
-// to 9000 tokens, 8 kv heads, 8-bit, as bf16 in 60 us, 4.9 TB/s; 3 of 100 to 700 tokens as fp32
+// to 9000 tokens, 8 kv heads, 8-bit, as bf16 in 58 to 60 us, 5 TB/s; 3 of 100 to 700 tokens as fp32
 // in 7.1 us.  Sixteen neighbouring elements a lane, whose halves are stored 32 bytes apart, took
 // 65 and 7.9 us, five blocks an SM 56 and 8.2, the next rows' loads under way 71 and 8.3.
 template <int LANES, typename CT>
