@@ -358,6 +358,12 @@ __device__ __forceinline__ void cp_async4(void *dst, const void *src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
 }
 
+// One of four (a loop that stays small over values that were loaded together).
+__device__ __forceinline__ uint4 pick(const uint4 (&x)[4], int k) {
+    const uint4 a = k & 1 ? x[1] : x[0], b = k & 1 ? x[3] : x[2];
+    return k & 2 ? b : a;
+}
+
 // 2^k that brings amax into [128, 256), as (factor, its inverse's exponent -k).
 __device__ __forceinline__ float pow2_scale(float amax, int *k) {
     int e = (int)((__float_as_uint(amax) >> 23) & 0xff) - 127;
@@ -402,16 +408,16 @@ __device__ __forceinline__ uint32_t off8(int r, int c) { return (uint32_t)(r * 1
 // The queries of sequence b into the score product's A operand, each copy of a row (dead
 // rows: zeros), as bf16 [dim half][row][128 B] or as two 8-bit parts [part][row][128 B], and
 // what its softmax thread needs of it: the nodes it sees and the parts' scale.  16 lanes a
-// row; by warps wi of nw.
+// row; the first `rows` of them (an even number) by warps wi of nw.
 template <bool E4, int TPC, int MT>
 __device__ __forceinline__ void load_queries(const TreeArgs &a, int b, int n, int g, int rb, uint8_t *Q,
-                                             unsigned long long *sees, float *scale, int wi, int nw, int lane) {
+                                             unsigned long long *sees, float *scale, int rows, int wi, int nw, int lane) {
     const int c = lane & 15;
-    // pairs of rows whose loads are under way together: one node's wait for one latency (8-bit:
-    // two, the code has to stay small)
-    constexpr int AT_ONCE = E4 ? 2 : 4;
+    // pairs of rows whose loads are under way together: they wait for one latency (200 sequences
+    // of 10 to 16 tokens, 64 nodes, 8-bit, with the nodes' rows likewise: 387 -> 353 us)
+    constexpr int AT_ONCE = 4;
 #pragma unroll 1
-    for (int r1 = wi * 2 + (lane >> 4); r1 < TPC * MT; r1 += AT_ONCE * 2 * nw) {
+    for (int r1 = wi * 2 + (lane >> 4); r1 < rows; r1 += AT_ONCE * 2 * nw) {
         uint4 ahead[AT_ONCE];
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
@@ -422,13 +428,13 @@ __device__ __forceinline__ void load_queries(const TreeArgs &a, int b, int n, in
                 ahead[k] = *(const uint4 *)((const bf16 *)a.q + ((size_t)b * a.N + node) * a.qs + (size_t)(g * a.G + rr - node * a.G) * DH + c * 8);
                 if (c == 0) bits = tree_mask(a, b, node, n);
             }
-            if (c == 0 && r < TPC * MT) sees[r] = bits;
+            if (c == 0 && r < rows) sees[r] = bits;
         }
 #pragma unroll(E4 ? 1 : AT_ONCE)
         for (int k = 0; k < AT_ONCE; ++k) {
             const int r = r1 + k * 2 * nw;
-            if (r - (lane >> 4) >= TPC * MT) break;
-            const uint4 u = E4 && k ? ahead[1] : ahead[E4 ? 0 : k];
+            if (r - (lane >> 4) >= rows) break;
+            const uint4 u = E4 ? pick(ahead, k) : ahead[k];  // (8-bit: the code has to stay small)
             uint8_t *q = Q + (MT == 2 ? (r >> 7) * Q_TILE : 0);
             const int rt = MT == 2 ? r & 127 : r;
             if constexpr (!E4) {
@@ -520,6 +526,9 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int B = a.B, Hkv = a.Hkv, Hv = Hkv * a.n_rb;
     int *prefix = (int *)(smem + lay.off_tab), *sids = prefix + B + 1, *lens = sids + B, *nodes = lens + B;
+    // rows of a segment's queries that are loaded; the others, and what belongs to them, are
+    // cleared with the first two segments (two buffers) and stay so
+    const int live_rows = (a.rb_rows + 1) & ~1;
     const bool paged = a.cache.kv.layout == SP_KV_PAGED;
     const int P = a.cache.kv.page_size, P_bits = 31 - __clz(max(P, 1));  // 16, 32 or 64 (0 contiguous)
     constexpr int ROW = DH * (E4 ? 1 : 2);  // bytes of a cached row
@@ -984,10 +993,20 @@ __global__ void __launch_bounds__(THREADS, 1)
                         const long long fs = is_v ? a.vs : a.ks;
                         const int n = nodes[b], c = lane & 15;
                         unsigned long long vb = 0;
+                        // rows whose loads are under way together (bf16: one, its loaders' registers are few)
+                        constexpr int AT_ONCE = E4 ? 4 : 1;
+                        uint4 some[AT_ONCE];
 #pragma unroll 1
-                        for (int r = pidx * 2 + (lane >> 4); r < (is_v ? 64 : (n + 1) & ~1); r += 4) {
-                            uint4 u = make_uint4(0, 0, 0, 0);
-                            if (r < n) u = *(const uint4 *)(fresh + ((size_t)b * a.N + r) * fs + c * 8);
+                        for (int r = pidx * 2 + (lane >> 4), k = 0; r < (is_v ? 64 : (n + 1) & ~1); r += 4, ++k) {
+                            if (k % AT_ONCE == 0) {
+#pragma unroll
+                                for (int e = 0; e < AT_ONCE; ++e) {
+                                    some[e] = make_uint4(0, 0, 0, 0);
+                                    if (r + 4 * e < n) some[e] = *(const uint4 *)(fresh + ((size_t)b * a.N + r + 4 * e) * fs + c * 8);
+                                }
+                            }
+                            uint4 u = some[0];
+                            if constexpr (E4) u = pick(some, k & 3);
                             uint32_t w[4] = {u.x, u.y, u.z, u.w};
                             if constexpr (!E4) {
                                 if (is_v) {
@@ -1081,7 +1100,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                     ok = wait_warp(&bars->q_empty, seg_ph ^ 1, abort);
                     if (!ok) break;
                     load_queries<E4, TPC, MT>(a, b, nodes[b], g, rb, smem + lay.off_q, (unsigned long long *)(smem + OFF_SEES) + seg_ph * 256,
-                                              (float *)(smem + OFF_RS) + seg_ph * 256, cw, CVT_WARPS, lane);
+                                              (float *)(smem + OFF_RS) + seg_ph * 256, b - sh.b0 < 2 ? TPC * MT : live_rows, cw, CVT_WARPS, lane);
                     arrive_warp(&bars->q_full, lane);
                     seg_ph ^= 1;
                 }
@@ -1093,19 +1112,27 @@ __global__ void __launch_bounds__(THREADS, 1)
                     if (ct >= 64) par[2 * TILE + ct] = 0.f;  // (weights of 0 are multiplied by these)
                     const int n = nodes[b], c16 = lane & 15;
                     unsigned long long vb = 0;
+                    uint4 two_k[2], two_v[2];  // (rows whose loads are under way together)
 #pragma unroll 1
-                    for (int r = cw * 2 + (lane >> 4); r < 64; r += 8) {
+                    for (int r = cw * 2 + (lane >> 4), k = 0; r < 64; r += 8, ++k) {
                         if ((r & ~1) >= n) {  // (the pair of rows of this warp)
                             st_shared_v4(dst + kv_off(r, c16), 0, 0, 0, 0);
                             if (c16 == 0) par[2 * TILE + r] = 0.f;
                             continue;
                         }
-                        uint4 uk = make_uint4(0, 0, 0, 0), uv = uk;
-                        if (r < n) {
-                            const size_t row = (size_t)b * a.N + r;
-                            uk = *(const uint4 *)((const bf16 *)a.k_new + row * a.ks + (size_t)g * DH + c16 * 8);
-                            uv = *(const uint4 *)((const bf16 *)a.v_new + row * a.vs + (size_t)g * DH + c16 * 8);
+                        if ((k & 1) == 0) {
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                two_k[e] = two_v[e] = make_uint4(0, 0, 0, 0);
+                                if (r + 8 * e < n) {
+                                    const size_t row = (size_t)b * a.N + r + 8 * e;
+                                    two_k[e] = *(const uint4 *)((const bf16 *)a.k_new + row * a.ks + (size_t)g * DH + c16 * 8);
+                                    two_v[e] = *(const uint4 *)((const bf16 *)a.v_new + row * a.vs + (size_t)g * DH + c16 * 8);
+                                }
+                            }
                         }
+                        const uint4 uk = two_k[0], uv = two_v[0];
+                        two_k[0] = two_k[1], two_v[0] = two_v[1];
                         const uint32_t wk[4] = {uk.x, uk.y, uk.z, uk.w}, wv[4] = {uv.x, uv.y, uv.z, uv.w};
                         float v[8], amk = 0.f, amv = 0.f;
                         bool odd = false;
@@ -1250,8 +1277,8 @@ __global__ void __launch_bounds__(THREADS, 1)
             for (int b = sh.b0; b < sh.b1; ++b, seg_ph ^= 1) {
                 if (!wait_warp(&bars->q_empty, seg_ph ^ 1, abort)) break;
                 load_queries<E4, TPC, MT>(a, b, nodes[b], g, rb, smem + lay.off_q,
-                                          (unsigned long long *)(smem + OFF_SEES) + seg_ph * 256, nullptr, warp - Ro::Q_WARP,
-                                          Ro::Q_WARPS, lane);
+                                          (unsigned long long *)(smem + OFF_SEES) + seg_ph * 256, nullptr,
+                                          b - sh.b0 < 2 ? TPC * MT : live_rows, warp - Ro::Q_WARP, Ro::Q_WARPS, lane);
                 arrive_warp(&bars->q_full, lane);
             }
         } else if (warp == MMA) {
