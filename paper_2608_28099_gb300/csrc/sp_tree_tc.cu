@@ -48,7 +48,7 @@
 //   8-bit         the chain of a pipeline, scores -> softmax -> product -> next scores (half of
 //                 TMEM is scores, half outputs: no room for the next scores before the product
 //                 has read the weights).  8 sequences of 32768 tokens, 40 heads, 32 nodes (160
-//                 rows, two M tiles): 380 us, 0.45 PFLOP/s, some 5000 cycles of softmax in 6800
+//                 rows, two M tiles): 377 us, 0.46 PFLOP/s, some 5000 cycles of softmax in 6800
 //                 a tile.  128 sequences of 300 to 4000 tokens, 32 heads, one node: 194 us, 3.0
 //                 TB/s, 2600 cycles a tile that the conversion, the V loader and the MMA issuer
 //                 fill to 60 - 80 %.
