@@ -360,18 +360,20 @@ __global__ void __launch_bounds__(THREADS, kAppendBlocks<T>) append_kernel(const
     RowWalk w(first, G, Hkv);
     load(w, 0);
     if ((int)threadIdx.x < ck.n) {
-        const int j = threadIdx.x, t = ck.sq.len + ck.j0 + j;
+        const int j = threadIdx.x;
+        const long long t = (long long)ck.sq.len + ck.j0 + j;  // (a length near max_seq_len's own limit passes 31 bits)
         long long dst = -1;
         int bad = 0, step;
         if (t >= c.max_seq_len) bad = SP_DEV_BAD_LENGTH;
         else if (source(j, 0, 0) < 0) bad = SP_DEV_BAD_ROW;
-        else if (!cache_row(c, ck.sq.sid, t, &dst, &step)) bad = SP_DEV_BAD_PAGE;
+        else if (!cache_row(c, ck.sq.sid, (int)t, &dst, &step)) bad = SP_DEV_BAD_PAGE;
         place[j] = bad ? -1 : dst;
         if (bad && a.status) atomicOr(a.status, bad);
     }
     for (int i = threadIdx.x; i < ck.n * half; i += THREADS) {
         const int t = i / half;
-        cs[i] = rotary_cs(a.rot, ck.sq.len + ck.j0 + t, i - t * half);
+        // (a position that wraps is past max_seq_len: its token is skipped)
+        cs[i] = rotary_cs(a.rot, (int)((unsigned)ck.sq.len + ck.j0 + t), i - t * half);
     }
     __syncthreads();
     const int head_step = c.kv.layout == SP_KV_PAGED ? c.kv.page_size : 1;

@@ -1,0 +1,41 @@
+"""Lengths that are wrong, and positions at the ends of their range: reported, and nothing
+is written or read where it does not belong."""
+import numpy as np
+import pytest
+
+import paper_2608_28099_gb300 as sp
+from gpu_util import ensure_built, torch_dev
+from test_gpu_token_cache import append, make_rows
+from token_cache_util import Cache
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    ensure_built()
+    return torch_dev()
+
+
+def bits(t):
+    import torch
+    return t.view(torch.uint8)
+
+
+@pytest.mark.parametrize("cdt", [sp.SP_E4M3, sp.SP_BF16])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("short", [0, 10, 4000, 6000])
+def test_positions_that_pass_31_bits_are_skipped(torch, cdt, page, short):
+    # the largest bound that is accepted, a length `short` below it and more rows than the
+    # bound leaves: tokens without a page, tokens past the bound, and none that wrapped
+    hkv, dh, most = 2, 128, 2 ** 31 - 1 - 4096
+    k = torch.randn((10000, hkv, dh), generator=torch.Generator().manual_seed(1)).cuda()
+    cache, want = (Cache(cdt, hkv, dh, [40, 40], page, junk=3.0) for _ in range(2))
+    cache.desc.max_seq_len = most
+    turns, amplitude = sp.sp_rotary_plan(sp.SP_ROPE_PLAIN, dh)
+    turns = torch.from_numpy(turns.view(np.int64)).cuda()
+    rot = sp.sp_rotary(dh, dh, 0, amplitude, turns.data_ptr())
+    for r in (None, rot):
+        status = append(torch, cache, [most - short, 5], make_rows(torch, [5000, 0], 5000, 10000), sp.SP_F32, k, k, r)
+        assert status == (sp.SP_DEV_BAD_PAGE if short else 0) | (sp.SP_DEV_BAD_LENGTH if short < 5000 else 0)
+        assert torch.equal(bits(cache.k), bits(want.k)) and torch.equal(bits(cache.v), bits(want.v))
