@@ -548,7 +548,8 @@ typedef struct sp_token_rows {
  * kv head), code = the nearest 8-bit value of x * (448 / max(amax, 2^-60)), ties to
  * even; a non-finite element becomes NaN.  Other types are rounded to nearest.
  * A sequence may appear once in a batch.  A token without a page, past
- * max_seq_len or whose row lies outside the buffers is skipped and reported. */
+ * max_seq_len or whose row lies outside the buffers is skipped and reported, and so
+ * are all tokens of a sequence with a negative length. */
 SP_API sp_status sp_cache_append(sp_stream stream, const sp_token_cache *cache, const sp_rotary *rot,
                                  int batch, const int *d_seq_ids, const int *d_seq_lens,
                                  const sp_token_rows *rows, int dtype, const void *d_k, const void *d_v,

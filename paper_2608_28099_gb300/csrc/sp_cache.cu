@@ -293,6 +293,11 @@ __device__ __forceinline__ Chunk chunk_of(const CopyArgs &a, int *status) {
     c.n = max(0, min(a.tokens_per_block, c.count - c.j0));
     return c;
 }
+// A negative length is reported and reads as 0.  Nothing may be written for it: the new tokens
+// would take the places of the sequence's first ones.
+__device__ __forceinline__ bool may_write(const CopyArgs &a, const Chunk &c) {
+    return c.sq.sid >= 0 && a.seq_lens[c.sq.sid] >= 0;
+}
 
 constexpr int MAX_TOK = 16;  // tokens of a block (32: the long contexts below read in 72 instead of 68 us)
 
@@ -333,7 +338,7 @@ __global__ void __launch_bounds__(THREADS, kAppendBlocks<T>) append_kernel(const
     pdl_wait();
     pdl_trigger();
     const Chunk ck = chunk_of(a, threadIdx.x == 0 && blockIdx.x % a.chunks == 0 ? a.status : nullptr);
-    if (ck.n == 0 || ck.sq.sid < 0) return;  // uniform over the block
+    if (ck.n == 0 || !may_write(a, ck)) return;  // uniform over the block
     const CacheDev &c = a.cache;
     const int half = a.rot.half, Hkv = c.Hkv, dh = LANES * 16;
     const int rows = ck.n * 2 * Hkv, lane = threadIdx.x % LANES, first = threadIdx.x / LANES;

@@ -39,3 +39,20 @@ def test_positions_that_pass_31_bits_are_skipped(torch, cdt, page, short):
         status = append(torch, cache, [most - short, 5], make_rows(torch, [5000, 0], 5000, 10000), sp.SP_F32, k, k, r)
         assert status == (sp.SP_DEV_BAD_PAGE if short else 0) | (sp.SP_DEV_BAD_LENGTH if short < 5000 else 0)
         assert torch.equal(bits(cache.k), bits(want.k)) and torch.equal(bits(cache.v), bits(want.v))
+
+
+@pytest.mark.parametrize("cdt", [sp.SP_E4M3, sp.SP_BF16, sp.SP_F32])
+@pytest.mark.parametrize("page", [0, 16])
+@pytest.mark.parametrize("length", [-1, -3, -2 ** 31])
+def test_a_negative_length_appends_nothing(torch, cdt, page, length):
+    hkv, dh = 2, 128
+    k = torch.randn((12, hkv, dh), generator=torch.Generator().manual_seed(1)).cuda()
+    cache, want = (Cache(cdt, hkv, dh, [40, 40, 40], page, junk=3.0) for _ in range(2))
+    assert append(torch, cache, [length, 5, length], make_rows(torch, None, 4, 12), sp.SP_F32, k, k) == sp.SP_DEV_BAD_LENGTH
+    want.put(1, 5, k[4:8].cpu(), k[4:8].cpu())
+    for a, b in ((cache.k, want.k), (cache.v, want.v)):
+        assert torch.equal(bits(a), bits(b))
+    if cdt == sp.SP_E4M3:
+        other = torch.ones_like(cache.ks, dtype=torch.bool)
+        other[cache._at(1, np.arange(5, 9))] = False
+        assert bool((cache.ks[other] == 1).all()) and bool((cache.vs[other] == 1).all())
