@@ -142,14 +142,15 @@ sp_status check_tree(const sp_tree_dims *d, const sp_token_cache *cache, int bat
     if (d->path < 0 || d->path > 2) return fail(SP_ERR_INVALID_ARG, "bad path %d", d->path);
     if (d->shared_mask != 0 && d->shared_mask != 1) return fail(SP_ERR_INVALID_ARG, "shared_mask must be 0 or 1");
     if (!isfinite(d->scale) || d->scale < 0.f) return fail(SP_ERR_INVALID_ARG, "scale must be finite and >= 0");
+    const long long rows = (long long)(d->n_q_heads / Hkv) * d->n_nodes;  // of a kv head
+    if (Hkv * ceil_div_ll(rows, 32) > 65535) return fail(SP_ERR_UNSUPPORTED, "too many query rows");
     a->B = batch;
     a->Hq = d->n_q_heads;
     a->Hkv = Hkv;
     a->G = d->n_q_heads / Hkv;
     a->N = d->n_nodes;
     a->dh = dh;
-    a->R = a->G * a->N;
-    if ((long long)Hkv * ceil_div(a->R, 32) > 65535) return fail(SP_ERR_UNSUPPORTED, "too many query rows");
+    a->R = (int)rows;
     a->dtype = d->dtype;
     a->scale_log2 = (float)(1.4426950408889634 * (d->scale > 0.f ? (double)d->scale : 1.0 / sqrt((double)dh)));
     a->qs = d->q_stride ? d->q_stride : (long long)a->Hq * dh;

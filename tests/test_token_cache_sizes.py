@@ -1,0 +1,52 @@
+"""Sizes whose products pass 32 bits are refused on the host (no GPU).  The calls run in a
+process of their own: a division by a product that wrapped to 0 would end it."""
+import subprocess
+import sys
+
+import pytest
+
+import paper_2608_28099_gb300 as sp
+from conftest import ROOT
+from paper_2608_28099_gb300 import build_lib
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    build_lib.build()
+
+
+CALLS = """
+import sys
+sys.path.insert(0, {root!r})
+import paper_2608_28099_gb300 as sp
+kv = sp.sp_kv_cache({layout}, 0xA0000, 0xB0000, 0x100000, 0x200000, 0x300000, 16, 8, 4, 4)
+cache = sp.sp_token_cache(kv, {cache}, {hkv}, {dh}, 64, 0x400000, 0x500000)
+def status(call, *args):
+    try:
+        call(*args)
+    except sp.SpError as e:
+        return e.status
+dims = sp.sp_tree_dims({hq}, {nodes}, {dtype}, {path}, 0, 0.0, 0, 0, 0)
+rows = sp.sp_token_rows(None, None, None, 4, 16, 0, 0)
+print(sp.sp_attend_tree_workspace_bytes(dims, cache, 4),
+      status(sp.sp_attend_tree, None, dims, cache, 4, None, 0x600000, None, None, 0x700000, 0x800000, 0x900000, 0xA00000,
+             0xB00000, 1 << 60),
+      status(sp.sp_cache_append, None, cache, None, 4, None, 0x600000, rows, 1, 0x700000, 0x800000),
+      status(sp.sp_cache_read, None, cache, 4, None, 0x600000, None, rows, 1, 0x700000, 0x800000))
+"""
+
+
+def answers(**kw):
+    a = dict(root=ROOT, layout=sp.SP_KV_PAGED, cache=sp.SP_E4M3, hkv=1, dh=128, hq=4, nodes=4, dtype=sp.SP_BF16, path=0)
+    a.update(kw)
+    r = subprocess.run([sys.executable, "-c", CALLS.format(**a)], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, (r.returncode, r.stderr[-500:])
+    return r.stdout.split()
+
+
+@pytest.mark.parametrize("path", [0, 1, 2])
+@pytest.mark.parametrize("hq,nodes", [(1 << 26, 64), (1 << 25, 64), (1 << 30, 4), (1 << 30, 1), ((1 << 26) + 1, 64),
+                                      (3 << 25, 64), (2 ** 31 - 1, 64)])
+def test_query_rows_past_32_bits(path, hq, nodes):
+    got = answers(hq=hq, nodes=nodes, path=path)
+    assert got[0] == "0" and int(got[1]) == sp.SP_ERR_UNSUPPORTED
