@@ -62,6 +62,8 @@ sp_status check_cache(const sp_token_cache *c, CacheDev *out) {
     if (c->n_kv_heads < 1) return fail(SP_ERR_INVALID_ARG, "n_kv_heads must be >= 1");
     if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128)
         return fail(SP_ERR_UNSUPPORTED, "head_dim %d unsupported (32, 64, 128)", c->head_dim);
+    // (a block's rows and a head's place in a row are 32-bit numbers in the kernels)
+    if ((long long)c->n_kv_heads * c->head_dim > 0x7fffffffLL / 8) return fail(SP_ERR_UNSUPPORTED, "too many heads");
     if (c->max_seq_len < 0 || c->max_seq_len > 0x7fffffff - 4096)
         return fail(SP_ERR_INVALID_ARG, "max_seq_len out of range");
     if (kv.n_seqs < 1) return fail(SP_ERR_INVALID_ARG, "kv.n_seqs must be >= 1");

@@ -50,3 +50,11 @@ def answers(**kw):
 def test_query_rows_past_32_bits(path, hq, nodes):
     got = answers(hq=hq, nodes=nodes, path=path)
     assert got[0] == "0" and int(got[1]) == sp.SP_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("layout", [sp.SP_KV_PAGED, sp.SP_KV_CONTIGUOUS])
+@pytest.mark.parametrize("hkv,dh", [(1 << 27, 32), (1 << 24, 128), (1 << 30, 64), (2 ** 31 - 1, 128)])
+def test_heads_past_32_bits(layout, hkv, dh):
+    # a block's rows (16 tokens of K and V), and a head's place in a row, are 32-bit numbers
+    got = answers(layout=layout, hkv=hkv, dh=dh, hq=hkv, nodes=1)
+    assert got[0] == "0" and [int(x) for x in got[1:]] == [sp.SP_ERR_UNSUPPORTED] * 3
