@@ -23,7 +23,7 @@ __device__ __forceinline__ void storev(T *p, const float (&v)[V]) {
     }
 }
 
-// V elements as they lie: 16 bytes, or one by one.
+// V elements as they lie: 16 bytes, or one by one, of which `left` exist.
 template <typename T, int V>
 struct RawVec {
     static constexpr bool WIDE = V * sizeof(T) == 16;
@@ -32,20 +32,22 @@ struct RawVec {
         T e[V];
     };
     __device__ __forceinline__ RawVec() {}
-    __device__ __forceinline__ void load(const T *p) {
+    __device__ __forceinline__ void load(const T *p, int left) {
         if constexpr (WIDE) {
             w = *(const uint4 *)p;
         } else {
 #pragma unroll
-            for (int i = 0; i < V; ++i) e[i] = p[i];
+            for (int i = 0; i < V; ++i)
+                if (i < left) e[i] = p[i];
         }
     }
-    __device__ __forceinline__ void store(T *p) const {
+    __device__ __forceinline__ void store(T *p, int left) const {
         if constexpr (WIDE) {
             *(uint4 *)p = w;
         } else {
 #pragma unroll
-            for (int i = 0; i < V; ++i) p[i] = e[i];
+            for (int i = 0; i < V; ++i)
+                if (i < left) p[i] = e[i];
         }
     }
     __device__ __forceinline__ void get(float (&v)[V]) const {
@@ -62,8 +64,9 @@ struct RawVec {
 
 // Rotate (or turn back) heads.  A thread has one unit of a head -- the two vectors that
 // turn into one another (half layout), one vector of whole pairs (interleaved), or one
-// vector of the dims that pass -- for every head it visits of a token, U heads at a time: the
-// next ones' loads are under way, as they lie, while these are turned.  (cos, sin) of the
+// vector of the dims that pass (a pair's scalar vector may have one element left) -- for every
+// head it visits of a token, U heads at a time: the next ones' loads are under way, as they
+// lie, while these are turned.  (cos, sin) of the
 // block's tokens are formed in shared memory behind the first loads (one sincospif a (token,
 // pair), shared by all heads).  V elements a vector: 16 bytes, or 1 (2 interleaved) where a
 // stride, base or width does not allow that.  A group of tokens fills the block; a block takes
@@ -77,7 +80,7 @@ __global__ void __launch_bounds__(THREADS, 4) rotate_kernel(const __grid_constan
     constexpr int U = INTER ? 4 : 2, W = INTER ? V / 2 : V;  // heads in flight, pairs of a unit
     pdl_wait();
     pdl_trigger();
-    const int half = a.rot.half, turn = (INTER ? a.rot.rot : half) / V, units = turn + (a.dh - a.rot.rot) / V;
+    const int half = a.rot.half, turn = (INTER ? a.rot.rot : half) / V, units = turn + ceil_div(a.dh - a.rot.rot, V);
     const int wide = min(units, THREADS), heads = min(a.n_heads, THREADS / wide), nt = a.tokens_per_block;
     const int per = wide * heads, tl = threadIdx.x / per, rest = threadIdx.x - tl * per, h0 = rest / wide;
     const int c0 = rest - h0 * wide, t0 = blockIdx.x * nt * a.groups, end = min(t0 + nt * a.groups, a.n_tokens);
@@ -94,9 +97,9 @@ __global__ void __launch_bounds__(THREADS, 4) rotate_kernel(const __grid_constan
 #pragma unroll
         for (int u = 0; u < U; ++u, x += step) {
             if (i.h + u * heads >= a.n_heads) break;
-            v.p[u].load(x);
+            v.p[u].load(x, a.dh - place(i.c));
             if constexpr (!INTER) {
-                if (i.c < turn) v.q[u].load(x + half);
+                if (i.c < turn) v.q[u].load(x + half, V);
             }
         }
     };
@@ -151,7 +154,7 @@ __global__ void __launch_bounds__(THREADS, 4) rotate_kernel(const __grid_constan
 #pragma unroll
             for (int u = 0; u < U; ++u, y += step) {
                 if (at.h + u * heads >= a.n_heads) break;
-                v.p[u].store(y);
+                v.p[u].store(y, a.dh - place(at.c));
             }
         }
         v = ahead;
@@ -161,7 +164,7 @@ __global__ void __launch_bounds__(THREADS, 4) rotate_kernel(const __grid_constan
 
 template <typename T, int V, bool INTER>
 cudaError_t run_rotate(RotateArgs a, int n_sm, cudaStream_t st) {
-    const int turn = (INTER ? a.rot.rot : a.rot.half) / V, units = turn + (a.dh - a.rot.rot) / V;
+    const int turn = (INTER ? a.rot.rot : a.rot.half) / V, units = turn + ceil_div(a.dh - a.rot.rot, V);
     const int wide = units < THREADS ? units : THREADS, fit = THREADS / wide;
     const int per = wide * (a.n_heads < fit ? a.n_heads : fit);
     a.tokens_per_block = THREADS / per;
