@@ -56,6 +56,7 @@
 // little as their latency allows (unrolling the conversion and the loaders from 95 to 105 KB of
 // code took the 128 sequences from 287 to 378 us), and waits are few instructions.
 #include <cudaTypedefs.h>
+#include <float.h>
 #include <string.h>
 
 #include "sp_attn_plan.cuh"
@@ -775,6 +776,9 @@ __global__ void __launch_bounds__(THREADS, 1)
             const int j_first = group_of(cuts, n_grp, sg.xp), j_last = group_of(cuts, n_grp, sg.xp + sg.nt - 1);
             const bool whole = j_first == j_last;
             const int n1 = MT == 2 ? sg.n : sg.n >> 1;  // tiles of pipeline 1
+            // NaN scores alone leave a sum of NaN and no max, which would pass for a part that has
+            // seen nothing: the least finite max keeps the sum in what is added up and merged
+            if (l != l) m = fmaxf(m, -FLT_MAX);
             ml_s[wg * 128 + ln] = make_float2(m, l);
             named_sync(BAR_EPI, SOFT);
             const bool odd = sg.t_a + sg.n == sg.nt && *(volatile unsigned long long *)&bars->seg_vbad;  // uniform
