@@ -1179,7 +1179,8 @@ __global__ void __launch_bounds__(THREADS, 1)
                     if (!ok) break;
                     {  // token ct's constants
                         const float *sc = (const float *)(smem + lay.off_sc) + rv.slot * 2 * TILE + ct;
-                        const float lg = __log2f(fmaxf(sc[TILE], 7.888609052210118e-31f));  // (2^-100)
+                        const float floor = 7.888609052210118e-31f;  // 2^-100
+                        const float lg = __log2f(sc[TILE] < floor ? floor : sc[TILE]);  // (a NaN stays)
                         par[par_at(ct)] = sc[0] * a.scale_log2;
                         par[par_at(ct) + 2] = lg;
                         par[2 * TILE + ct] = fast_exp2(-lg);  // (a weight times its inverse: lg's error cancels)
@@ -1255,6 +1256,8 @@ __global__ void __launch_bounds__(THREADS, 1)
                             if (lane + 32 * k < n_tok) {
                                 cp_async4(sc + 32 * k, sk + at);
                                 cp_async4(sc + TILE + 32 * k, sv + at);
+                            } else {  // (weights of 0 are multiplied by what is made of these)
+                                sc[32 * k] = sc[TILE + 32 * k] = 0.f;
                             }
                     }
                     // past the end: weights of 0 times zeros

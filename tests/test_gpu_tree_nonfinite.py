@@ -132,3 +132,33 @@ def test_nan_keys_of_a_split_sequence(torch, cdt, path, G, N, tokens):
 @pytest.mark.parametrize("G,N", ROWS)
 def test_a_nan_key_alone_in_a_pipeline(torch, cdt, path, G, N):
     check_cached_key(torch, cdt, path, G, N, 129, [128])
+
+
+# ---- scales --------------------------------------------------------------------
+@pytest.mark.parametrize("path", [1, 2])
+@pytest.mark.parametrize("page", [0, 16, 64])
+@pytest.mark.parametrize("which", ["ks", "vs"])
+@pytest.mark.parametrize("G,N", ROWS)
+def test_a_nan_scale(torch, path, page, which, G, N):
+    # the token's values, or its score, are NaN; the next call finds what this one left in
+    # shared memory and must not be touched by it
+    c = Call(torch, sp.SP_E4M3, path, G, N, [40, 300, 7], page)
+    clean = c.run()
+    c.run()
+    scales = getattr(c.cache, which)
+    for s, t in ((0, 39), (1, 5)):
+        at = c.cache._at(s, [t])
+        row = scales[at].clone()
+        row[..., 0] = NAN
+        scales[at] = row
+    touched = torch.zeros_like(clean, dtype=torch.bool)
+    touched[:2, :, c.heads(0)] = True
+
+    def call():
+        out, status = tree_call(torch, c.cache, c.dims, c.lens, None, None, c.q.cuda(), c.k.cuda(), c.v.cuda())
+        assert status == 0
+        return out
+    got = call()
+    assert bool(torch.isnan(got[touched]).all())
+    same_elsewhere(torch, got, clean, touched)
+    assert torch.equal(c.run(), clean)
