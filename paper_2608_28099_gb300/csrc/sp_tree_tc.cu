@@ -365,10 +365,11 @@ __device__ __forceinline__ uint4 pick(const uint4 (&x)[4], int k) {
     return k & 2 ? b : a;
 }
 
-// 2^k that brings amax into [128, 256), as (factor, its inverse's exponent -k).
+// 2^k that brings a finite amax from 2^-100 on into [128, 256) (a smaller one: k = 107), as the
+// factor and k; both 2^k and 2^-k are normal numbers.
 __device__ __forceinline__ float pow2_scale(float amax, int *k) {
     int e = (int)((__float_as_uint(amax) >> 23) & 0xff) - 127;
-    e = min(max(e, -100), 120);
+    e = min(max(e, -100), 127);
     *k = 7 - e;
     return __int_as_float((*k + 127) << 23);
 }
