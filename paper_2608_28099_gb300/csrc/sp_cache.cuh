@@ -13,6 +13,7 @@ namespace sp {
 // any code stay far from the ends of fp32, and log2 of the scale is finite.
 constexpr float kMinAmax = 8.673617379884035e-19f;  // 2^-60
 constexpr float kMaxCode = 448.f;                   // the largest 8-bit value
+constexpr float kLeastWeight = 1.401298464324817e-45f;  // 2^-149, where a weight that a row sees would be 0
 
 // A cache as the kernels see it.
 struct CacheDev {

@@ -32,6 +32,12 @@ struct Smem {
     float v[TOK][DH];
 };
 
+// A weight, never 0: what vanishes beside the maximum still hands on a NaN or an infinity (2^-149 of
+// a finite value adds nothing).
+__device__ __forceinline__ float some_exp2(float x) {
+    const float y = exp2f(x);
+    return y == 0.f ? kLeastWeight : y;
+}
 __device__ __forceinline__ float warp_max(float x) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
@@ -136,8 +142,8 @@ __global__ void __launch_bounds__(THREADS) tree_simt_kernel(const __grid_constan
             const float mn = fmaxf(m[r], warp_max(x));
             // (a NaN score is not a maximum: it makes its own weight, and so the row, NaN)
             const float mu = mn == -INFINITY ? 0.f : mn;
-            const float al = m[r] == -INFINITY ? 0.f : exp2f(m[r] - mu);
-            sc[r] = visible ? exp2f(x - mu) : 0.f;
+            const float al = m[r] == -INFINITY ? 0.f : some_exp2(m[r] - mu);
+            sc[r] = visible ? x == -INFINITY ? 0.f : some_exp2(x - mu) : 0.f;
             l[r] = l[r] * al + warp_sum(sc[r]);
             m[r] = mn;
 #pragma unroll
@@ -204,7 +210,7 @@ __global__ void __launch_bounds__(THREADS) tree_merge_kernel(const __grid_consta
         const float mn = fmaxf(m, ml.x);
         if (ml.y == 0.f && ml.x == -INFINITY) continue;
         const float mu = mn == -INFINITY ? 0.f : mn;
-        const float al = m == -INFINITY ? 0.f : exp2f(m - mu), be = ml.x == -INFINITY ? 1.f : exp2f(ml.x - mu);
+        const float al = m == -INFINITY ? 0.f : some_exp2(m - mu), be = ml.x == -INFINITY ? 1.f : some_exp2(ml.x - mu);
         l = l * al + ml.y * be;
 #pragma unroll
         for (int d = 0; d < D; ++d) o[d] = o[d] * al + a.part_o[row * DH + lane + 32 * d] * be;

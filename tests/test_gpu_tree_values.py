@@ -1,0 +1,63 @@
+"""NaN and infinities among the values that a row sees, whatever their weight."""
+import pytest
+
+import paper_2608_28099_gb300 as sp
+from gpu_util import ensure_built, torch_dev
+from test_gpu_tree_nonfinite import KINDS, ROWS, Call, same_elsewhere
+
+pytestmark = pytest.mark.gpu
+
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module")
+def torch():
+    ensure_built()
+    return torch_dev()
+
+
+def the_same_kind(torch, got, want):
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    assert torch.equal(got.nan_to_num(0.0, 1.0, -1.0), want.nan_to_num(0.0, 1.0, -1.0))
+
+
+def check_cached_values(torch, cdt, path, G, N, length, scale, pairs):
+    """pairs: (token, value) put into dim 7 of head 0; the rows get their sum there (NaN from
+    an 8-bit cache, which holds no infinities)."""
+    c = Call(torch, cdt, path, G, N, [length, 20], scale=scale)
+    for t, _ in pairs:
+        c.kv[0][1][t, 0, 7] = 0.0  # (not the element that sets an 8-bit row's scale)
+    clean = c.run()
+    for t, x in pairs:
+        c.kv[0][1][t, 0, 7] = x
+    got = c.run()
+    touched = torch.zeros_like(clean, dtype=torch.bool)
+    touched[0, :, c.heads(0), 7] = True
+    the_same_kind(torch, got[touched], torch.full_like(got[touched], sum(x for _, x in pairs) if cdt == sp.SP_BF16 else NAN))
+    same_elsewhere(torch, got, clean, touched)
+
+
+def check_node_values(torch, cdt, path, G, N, length, scale, value):
+    """Node 1's value is not finite; it is seen by itself and by nodes 2 and up, beside the cache."""
+    c = Call(torch, cdt, path, G, N, [length, 20], scale=scale)
+    clean = c.run()
+    c.v[:, 1, 0, 7] = value
+    got = c.run()
+    touched = torch.zeros_like(clean, dtype=torch.bool)
+    touched[:, 1:, c.heads(0), 7] = True
+    the_same_kind(torch, got[touched], torch.full_like(got[touched], value))
+    same_elsewhere(torch, got, clean, touched)
+
+
+# scores spread over hundreds of powers of two: almost every weight is below 2^-149
+STEEP = 40.0
+
+
+@pytest.mark.parametrize("cdt", [sp.SP_BF16, sp.SP_E4M3])
+@pytest.mark.parametrize("G,N", ROWS)
+@pytest.mark.parametrize("value", [NAN, INF, -INF])
+@pytest.mark.parametrize("length,tokens", [(300, (0, 150, 299)), (2000, (1000,))])
+def test_values_of_vanishing_weight_on_cuda_cores(torch, cdt, G, N, value, length, tokens):
+    for t in tokens:
+        check_cached_values(torch, cdt, 1, G, N, length, STEEP, [(t, value)])
+    check_node_values(torch, cdt, 1, G, N, length, STEEP, value)
