@@ -805,8 +805,9 @@ __global__ void __launch_bounds__(THREADS, 1)
                             if (v.x != -INFINITY) lsum += fast_exp2(v.x - mu) * v.y;
                         }
                     const float m0 = ml_s[ln].x, m1 = ml_s[128 + ln].x;
-                    a0 = m0 == -INFINITY ? 0.f : fast_exp2(m0 - mu);
-                    a1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - mu);
+                    // (0: nothing was seen; a part that vanishes beside the others may hold a NaN)
+                    a0 = m0 == -INFINITY ? 0.f : fmaxf(fast_exp2(m0 - mu), kLeastWeight);
+                    a1 = m1 == -INFINITY ? 0.f : fmaxf(fast_exp2(m1 - mu), kLeastWeight);
                 }
             }
             ok = ok && wait_warp(&bars->pv_done, seg_ph, abort);
@@ -1425,13 +1426,13 @@ __global__ void __launch_bounds__(MERGE_THREADS) tree_tc_merge_kernel(const __gr
 #pragma unroll
             for (int e = 0; e < MERGE_AT; ++e) mn = fmaxf(mn, ml[e].x);
             if (mn == -INFINITY) continue;
-            const float al = m == -INFINITY ? 0.f : exp2f(m - mn);
+            const float al = m == -INFINITY ? 0.f : fmaxf(exp2f(m - mn), kLeastWeight);
             l *= al;
             o.x *= al, o.y *= al, o.z *= al, o.w *= al;
 #pragma unroll
             for (int e = 0; e < MERGE_AT; ++e) {
                 if (ml[e].x == -INFINITY) continue;
-                const float w = exp2f(ml[e].x - mn);
+                const float w = fmaxf(exp2f(ml[e].x - mn), kLeastWeight);
                 l += w * ml[e].y;
                 o.x += w * ov[e].x, o.y += w * ov[e].y, o.z += w * ov[e].z, o.w += w * ov[e].w;
             }

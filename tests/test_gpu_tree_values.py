@@ -61,3 +61,18 @@ def test_values_of_vanishing_weight_on_cuda_cores(torch, cdt, G, N, value, lengt
     for t in tokens:
         check_cached_values(torch, cdt, 1, G, N, length, STEEP, [(t, value)])
     check_node_values(torch, cdt, 1, G, N, length, STEEP, value)
+
+
+@pytest.mark.parametrize("G,N", ROWS)
+@pytest.mark.parametrize("length,tokens", [(300, (0, 150, 299)), (2000, (1000,))])
+def test_values_of_vanishing_weight_from_an_8_bit_cache(torch, G, N, length, tokens):
+    for t in tokens:
+        check_cached_values(torch, sp.SP_E4M3, 2, G, N, length, STEEP, [(t, NAN)])
+
+
+@pytest.mark.parametrize("cdt", [sp.SP_BF16, sp.SP_E4M3])
+@pytest.mark.parametrize("G,N", ROWS)
+@pytest.mark.parametrize("value", [NAN, INF, -INF])
+@pytest.mark.parametrize("length", [40, 300, 2000])
+def test_node_values_of_vanishing_weight(torch, cdt, G, N, value, length):
+    check_node_values(torch, cdt, 2, G, N, length, STEEP, value)
