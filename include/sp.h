@@ -511,7 +511,7 @@ SP_API sp_status sp_rotate(sp_stream stream, const sp_rotary *rot, int n_tokens,
  * type.  The pools are written by sp_cache_append, which is why `kv` must then
  * point to memory the caller may write.
  * SP_E4M3: an element is its 8-bit code times the scale of its (token, kv head);
- * the scales are float, SP_KV_PAGED: k_scale / v_scale point to
+ * the scales are float, finite and >= 0 (or NaN), SP_KV_PAGED: k_scale / v_scale point to
  * [n_pages][Hkv][page_size] (16-byte aligned), SP_KV_CONTIGUOUS: to DEVICE arrays
  * of n_seqs device pointers to [L_s][Hkv].  NULL for the other types. */
 typedef struct sp_token_cache {
@@ -598,11 +598,15 @@ SP_API size_t sp_attend_tree_workspace_bytes(const sp_tree_dims *dims, const sp_
  *   d_out      [batch * N][Hq][dh]: zeros for a node that sees nothing and for the
  *              nodes from n_nodes on (whose rows are never read)
  * The keys and values of nodes a node does not see, and what a cache page holds
- * past its sequence's end, have no influence, NaN and infinities included.  The
- * cache is only read.  With n_nodes = 1 this is the attention of a decoding step.
+ * past its sequence's end, have no influence, NaN and infinities included.  What a
+ * node does see reaches it: a NaN score makes its row NaN, a NaN or infinite value its
+ * dim of the row, however small the weight.  The cache is only read.  With n_nodes = 1
+ * this is the attention of a decoding step.
  * SP_E4M3 caches on tensor cores: the codes enter the score product as they are
- * (queries split exactly into two 8-bit parts) and the value product as 16-bit
- * floats with probabilities of 11 bits. */
+ * (queries and the nodes' keys in two 8-bit parts, to 2^-18 of a row's largest element)
+ * and the value product as 16-bit floats with probabilities of 11 bits.  As in the cache
+ * itself an infinite element of a query or of a node's key counts as NaN there, and a
+ * row whose queries times a key's codes pass fp32 becomes NaN. */
 SP_API sp_status sp_attend_tree(sp_stream stream, const sp_tree_dims *dims, const sp_token_cache *cache, int batch,
                                 const int *d_seq_ids, const int *d_seq_lens, const uint64_t *d_mask,
                                 const int *d_n_nodes, const void *d_q, const void *d_k_new, const void *d_v_new,

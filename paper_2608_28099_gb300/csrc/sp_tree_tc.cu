@@ -29,10 +29,15 @@
 //                 scales, and the row sum takes w / v_scale
 // The nodes' own keys never lose to the cache's format: bf16 nodes are copied, and for an
 // 8-bit cache their keys are two 8-bit parts in the two halves of the tile, added up in the
-// same scores, their values 16-bit floats, both exact for bf16 rows.
+// same scores (to 2^-18 of a key's largest element), their values 16-bit floats (exact but for
+// elements below 2^-24 of a value's largest).
 // What a row does not see: scores are replaced by -inf (not added to), rows of a tile past
 // the sequence's end are zeros, and a node's non-finite values are taken out of the
-// product and added afterwards to the rows that see the node.
+// product and added afterwards to the rows that see the node.  What it does see: NaN scores
+// leave a sum of NaN (in a part with no other score the least finite max stands for theirs), a
+// weight that vanishes beside the row's max is never 0 where parts are added, and dims that
+// come out infinite or NaN are made of the cached values again (bf16; 8-bit caches hold no
+// infinities).
 //
 // Warps 0-7: the two softmax warpgroups; then the MMA issuer (it owns TMEM) and the loaders.
 // bf16: three warps load queries, two each K and V (TMA boxes of whole pages, cp.async
@@ -99,6 +104,8 @@ struct Bars {
     uint64_t s_full[2], p_full[2], pv_done, q_full, q_empty, fin;
     unsigned long long vbad[MAX_RING][4];       // nodes with non-finite values, by V slot and warp
     unsigned long long seg_vbad;
+    unsigned odd_dims[3][DH / 32];              // dims with +inf, -inf, NaN among a segment's cached values
+    int odd_cached;                             // a row of the segment came out infinite or NaN
     uint32_t tmem;
     int abort;
     int wsum[32];
@@ -492,6 +499,34 @@ __device__ __forceinline__ void add_non_finite(const TreeArgs &a, int b, int g, 
     }
 }
 
+// Which dims of the cached values of tokens [t, t_end) of head g are not finite, bf16.  16 threads
+// a token, 8 dims each (rare).
+__device__ __forceinline__ void odd_cached_dims(const CacheDev &c, int sid, int g, int t, int t_end, unsigned (*dims)[DH / 32]) {
+    if (t >= t_end) return;
+    const uint16_t *v = (const uint16_t *)cache_base(c, sid, 1);
+    const int chunk = threadIdx.x & 15, shift = chunk * 8 & 31;
+    unsigned up = 0, down = 0, nan = 0;
+#pragma unroll 1
+    for (t += threadIdx.x >> 4; t < t_end; t += SOFT / 16) {
+        long long row;
+        int step;
+        if (!cache_row(c, sid, t, &row, &step)) continue;
+        const uint4 u = *(const uint4 *)(v + (row + (long long)g * step) * DH + chunk * 8);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t x = w[i >> 1] >> (i & 1) * 16 & 0xffffu;
+            const unsigned bit = 1u << (shift + i);
+            up |= x == 0x7f80u ? bit : 0;
+            down |= x == 0xff80u ? bit : 0;
+            nan |= (x & 0x7fffu) > 0x7f80u ? bit : 0;
+        }
+    }
+    if (up) atomicOr(&dims[0][chunk >> 2], up);
+    if (down) atomicOr(&dims[1][chunk >> 2], down);
+    if (nan) atomicOr(&dims[2][chunk >> 2], nan);
+}
+
 // n cached rows (`step` bytes apart) into rows r0 .. of a slot in the MMA's layout, 16 bytes
 // at a time by 64 threads: zeros if there is no source.  A thread keeps its chunk of the row
 // and walks rows 8 (8-bit) or 4 apart, so that addresses advance by constants.
@@ -566,6 +601,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         mbar_init(&bars->pv_done, 1);
         mbar_init(&bars->fin, 1);
         bars->abort = 0;
+        bars->odd_cached = 0;
         fence_mbar_init();
         if (paged) {
             prefetch_tmap(&map_k);
@@ -824,7 +860,9 @@ __global__ void __launch_bounds__(THREADS, 1)
                 return whole ? (uint8_t *)((bf16 *)a.out + (((size_t)b * a.N + nd) * a.Hq + (g * a.G + qr - nd * a.G)) * DH)
                              : (uint8_t *)(a.part_o + (slot * a.rb_rows + q) * DH);
             };
+            float probe = 0.f;  // NaN: a value written is not finite
             auto write = [&](uint8_t *to, bool on, int d, float4 y, float scale) {  // four dims, unnormalised
+                if constexpr (!E4) probe = fmaf(y.w, 0.f, fmaf(y.z, 0.f, fmaf(y.y, 0.f, fmaf(y.x, 0.f, probe))));
                 if (whole)
                     *(uint2 *)(to + d * 2) = on && scale != 0.f ? make_uint2(pack_bf16(y.x * scale, y.y * scale),
                                                                              pack_bf16(y.z * scale, y.w * scale))
@@ -898,13 +936,42 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
             if (!whole && active && cp == 0 && (MT == 2 || wg == 0))
                 *(float2 *)(a.part_ml + (slot * a.rb_rows + r) * 2) = make_float2(mc, lsum);
-            if (odd) {  // (uniform) values that were kept out of the product: to the rows that see them
-                named_sync(BAR_EPI, SOFT);
-                add_non_finite(a, b, g, rb, n, *(volatile unsigned long long *)&bars->seg_vbad, whole,
-                               a.part_o + slot * a.rb_rows * DH, threadIdx.x);
-            }
+            if (probe != probe) bars->odd_cached = 1;
             tc_fence_before();
-            named_sync(BAR_EPI, SOFT);  // both accumulators and ml_s are free
+            named_sync(BAR_EPI, SOFT);  // both accumulators and ml_s are free, the rows are written
+            const bool lost = !E4 && *(volatile int *)&bars->odd_cached;
+            if (lost || odd) {  // (uniform, rare)
+                if (lost) {
+                    // An infinite cached value is NaN where another copy, or a weight that underflows,
+                    // has multiplied it by 0.  Every row sees the segment's cached tokens: the dims
+                    // that have such values get the sum of them
+                    named_sync(BAR_EPI, SOFT);
+                    if (threadIdx.x < 3 * (DH / 32)) (&bars->odd_dims[0][0])[threadIdx.x] = 0;
+                    if (threadIdx.x == 0) bars->odd_cached = 0;
+                    named_sync(BAR_EPI, SOFT);
+                    odd_cached_dims(a.cache, sids[b], g, sg.t_a * TILE, min(lens[b], (sg.t_a + sg.n) * TILE), bars->odd_dims);
+                    named_sync(BAR_EPI, SOFT);
+                    bool on = false;
+                    uint8_t *to = nullptr;
+                    if (active && cp == 0 && (MT == 2 || wg == 0) && isfinite(lsum) && lsum != 0.f) to = dest(r, &on);
+#pragma unroll 1
+                    for (int w = 0; on && w < DH / 32; ++w) {
+                        const volatile unsigned(*dims)[DH / 32] = bars->odd_dims;
+                        const unsigned up = dims[0][w], down = dims[1][w], nan = dims[2][w];
+#pragma unroll 1
+                        for (unsigned left = up | down | nan; left; left &= left - 1) {
+                            const int e = __ffs(left) - 1, d = w * 32 + e;
+                            const float z = (nan | (up & down)) >> e & 1 ? NAN : up >> e & 1 ? INFINITY : -INFINITY;
+                            if (whole) ((bf16 *)to)[d] = __float2bfloat16_rn(z);
+                            else ((float *)to)[d] = z;
+                        }
+                    }
+                }
+                if (odd)  // values that were kept out of the product: to the rows that see them
+                    add_non_finite(a, b, g, rb, n, *(volatile unsigned long long *)&bars->seg_vbad, whole,
+                                   a.part_o + slot * a.rb_rows * DH, threadIdx.x);
+                named_sync(BAR_EPI, SOFT);
+            }
         }
     } else {
         regs_dec<Ro::OTHER_REGS>();

@@ -76,3 +76,60 @@ def test_values_of_vanishing_weight_from_an_8_bit_cache(torch, G, N, length, tok
 @pytest.mark.parametrize("length", [40, 300, 2000])
 def test_node_values_of_vanishing_weight(torch, cdt, G, N, value, length):
     check_node_values(torch, cdt, 2, G, N, length, STEEP, value)
+
+
+@pytest.mark.parametrize("G,N", ROWS)
+@pytest.mark.parametrize("value", [NAN, INF, -INF])
+@pytest.mark.parametrize("length,tokens", [(300, (0, 150, 299)), (2000, (1000,))])
+def test_values_of_vanishing_weight_from_a_bf16_cache(torch, G, N, value, length, tokens):
+    for t in tokens:
+        check_cached_values(torch, sp.SP_BF16, 2, G, N, length, STEEP, [(t, value)])
+
+
+@pytest.mark.parametrize("cdt,path", KINDS)
+@pytest.mark.parametrize("G,N", ROWS)
+@pytest.mark.parametrize("length", [1, 33, 128, 300, 3000])
+def test_non_finite_cached_values(torch, cdt, path, G, N, length):
+    for pairs in ([(length - 1, INF)], [(0, -INF)], [(length // 2, NAN)]):
+        check_cached_values(torch, cdt, path, G, N, length, 0.0, pairs)
+    if length > 1:
+        for last in (INF, -INF):
+            check_cached_values(torch, cdt, path, G, N, length, 0.0, [(0, INF), (length - 1, last)])
+
+
+@pytest.mark.parametrize("page", [0, 32, 64])
+@pytest.mark.parametrize("G,N", ROWS)
+def test_infinite_values_in_every_dim_and_layout(torch, page, G, N):
+    # every third dim of head 1 infinite somewhere in the context, and the same call once more without
+    c = Call(torch, sp.SP_BF16, 2, G, N, [700, 20, 150], page)
+    clean = c.run()
+    keep = [[k.clone(), v.clone()] for k, v in c.kv]
+    touched = torch.zeros_like(clean, dtype=torch.bool)
+    want = clean.clone()
+    for b in (0, 2):
+        for d in range(0, 128, 3):
+            value = INF if d % 2 else -INF
+            c.kv[b][1][(d * 37) % c.lens[b], 1, d] = value
+            touched[b, :, c.heads(1), d] = True
+            want[b, :, c.heads(1), d] = value
+    got = c.run()
+    the_same_kind(torch, got[touched], want[touched])
+    same_elsewhere(torch, got, clean, touched)
+    c.kv = keep
+    assert torch.equal(c.run(), clean)
+
+
+@pytest.mark.parametrize("path", [1, 2])
+@pytest.mark.parametrize("G,N", ROWS)
+@pytest.mark.parametrize("length", [40, 900])
+def test_cached_and_new_values_meet(torch, path, G, N, length):
+    # node 1's value is -inf, a cached one +inf: NaN where a row sees both
+    masks = [1 << i | (2 if i > 2 else 0) for i in range(N)]
+    c = Call(torch, sp.SP_BF16, path, G, N, [length, 20], mask=masks)
+    c.kv[0][1][length - 1, 0, 7] = INF
+    c.v[:, 1, 0, 7] = -INF
+    out = c.run()[..., c.heads(0), 7]
+    both = [i for i in range(N) if masks[i] & 2]
+    one = [i for i in range(N) if not masks[i] & 2]
+    assert bool(torch.isnan(out[0, both]).all()) and bool((out[0, one] == INF).all())
+    assert bool((out[1, both] == -INF).all()) and bool(torch.isfinite(out[1, one]).all())
