@@ -1,5 +1,7 @@
 """Sizes whose products pass 32 bits are refused on the host (no GPU).  The calls run in a
-process of their own: a division by a product that wrapped to 0 would end it."""
+process of their own, without a device: a division by a product that wrapped to 0 would end it,
+and a call that is not refused must not reach a GPU with the addresses made up here."""
+import os
 import subprocess
 import sys
 
@@ -30,16 +32,19 @@ dims = sp.sp_tree_dims({hq}, {nodes}, {dtype}, {path}, 0, 0.0, 0, 0, 0)
 rows = sp.sp_token_rows(None, None, None, 4, 16, 0, 0)
 print(sp.sp_attend_tree_workspace_bytes(dims, cache, 4),
       status(sp.sp_attend_tree, None, dims, cache, 4, None, 0x600000, None, None, 0x700000, 0x800000, 0x900000, 0xA00000,
-             0xB00000, 1 << 60),
-      status(sp.sp_cache_append, None, cache, None, 4, None, 0x600000, rows, 1, 0x700000, 0x800000),
-      status(sp.sp_cache_read, None, cache, 4, None, 0x600000, None, rows, 1, 0x700000, 0x800000))
+             0xB00000, 1 << 60))
+if {copies}:
+    print(status(sp.sp_cache_append, None, cache, None, 4, None, 0x600000, rows, 1, 0x700000, 0x800000),
+          status(sp.sp_cache_read, None, cache, 4, None, 0x600000, None, rows, 1, 0x700000, 0x800000))
 """
 
 
 def answers(**kw):
-    a = dict(root=ROOT, layout=sp.SP_KV_PAGED, cache=sp.SP_E4M3, hkv=1, dh=128, hq=4, nodes=4, dtype=sp.SP_BF16, path=0)
+    a = dict(root=ROOT, layout=sp.SP_KV_PAGED, cache=sp.SP_E4M3, hkv=1, dh=128, hq=4, nodes=4, dtype=sp.SP_BF16, path=0,
+             copies=False)
     a.update(kw)
-    r = subprocess.run([sys.executable, "-c", CALLS.format(**a)], capture_output=True, text=True, timeout=120)
+    r = subprocess.run([sys.executable, "-c", CALLS.format(**a)], capture_output=True, text=True, timeout=120,
+                       env=dict(os.environ, CUDA_VISIBLE_DEVICES=""))
     assert r.returncode == 0, (r.returncode, r.stderr[-500:])
     return r.stdout.split()
 
@@ -56,5 +61,5 @@ def test_query_rows_past_32_bits(path, hq, nodes):
 @pytest.mark.parametrize("hkv,dh", [(1 << 27, 32), (1 << 24, 128), (1 << 30, 64), (2 ** 31 - 1, 128)])
 def test_heads_past_32_bits(layout, hkv, dh):
     # a block's rows (16 tokens of K and V), and a head's place in a row, are 32-bit numbers
-    got = answers(layout=layout, hkv=hkv, dh=dh, hq=hkv, nodes=1)
+    got = answers(layout=layout, hkv=hkv, dh=dh, hq=hkv, nodes=1, copies=True)
     assert got[0] == "0" and [int(x) for x in got[1:]] == [sp.SP_ERR_UNSUPPORTED] * 3
