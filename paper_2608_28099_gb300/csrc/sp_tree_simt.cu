@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(THREADS) tree_simt_kernel(const __grid_constan
     int *status = threadIdx.x == 0 && hv == 0 && split == 0 ? a.status : nullptr;
     const SeqRef sq = resolve_seq(a.seq_ids, a.seq_lens, 0, b, a.cache.kv.n_seqs, a.cache.max_seq_len, status);
     const int n = tree_nodes(a, b, status), total = sq.len + n;
-    const int t_lo = min(total, split * a.split_tokens), t_hi = min(total, t_lo + a.split_tokens);
+    const int t_lo = min(total, split * a.split_tokens), t_hi = t_lo + min(a.split_tokens, total - t_lo);
     const int row0 = rb * a.rb_rows;
 
     for (int i = threadIdx.x; i < ROWS * C; i += THREADS) {
@@ -256,7 +256,7 @@ void plan_tree_simt(TreeArgs *a, int n_sm) {
     const int most = ceil_div(longest, 128);
     if (splits > most) splits = most;
     a->split_tokens = ceil_div(ceil_div(longest, (int)splits), TOK) * TOK;
-    a->n_splits = ceil_div(longest, a->split_tokens);
+    a->n_splits = (longest - 1) / a->split_tokens + 1;  // (their sum may pass 31 bits)
 }
 
 size_t tree_simt_slots(const TreeArgs &a) {

@@ -63,3 +63,14 @@ def test_heads_past_32_bits(layout, hkv, dh):
     # a block's rows (16 tokens of K and V), and a head's place in a row, are 32-bit numbers
     got = answers(layout=layout, hkv=hkv, dh=dh, hq=hkv, nodes=1, copies=True)
     assert got[0] == "0" and [int(x) for x in got[1:]] == [sp.SP_ERR_UNSUPPORTED] * 3
+
+
+@pytest.mark.parametrize("batch,hq,hkv,nodes", [(1, 4, 2, 5), (1, 8, 1, 64), (3, 4, 2, 5), (200, 4, 2, 5), (600, 16, 8, 64)])
+@pytest.mark.parametrize("longest", [2 ** 30, 2 ** 31 - 5000, 2 ** 31 - 1 - 4096])
+def test_the_workspace_of_any_length_bound(batch, hq, hkv, nodes, longest):
+    # far above the number of shares the bound changes their length, not their number
+    def size(most):
+        kv = sp.sp_kv_cache(sp.SP_KV_PAGED, None, None, 0x100000, 0x200000, 0x300000, 16, 8, 4, batch)
+        cache = sp.sp_token_cache(kv, sp.SP_F32, hkv, 128, most, None, None)
+        return sp.sp_attend_tree_workspace_bytes(sp.sp_tree_dims(hq, nodes, sp.SP_F32, 0, 0, 0.0, 0, 0, 0), cache, batch)
+    assert 0 < size(longest) == size(2 ** 26)
