@@ -592,6 +592,8 @@ SP_API size_t sp_attend_tree_workspace_bytes(const sp_tree_dims *dims, const sp_
 /* Attention of a tree of drafted tokens per sequence over [cache ; tree]
  * (Eq. 1-3 with the causal part replaced by the tree): node i of batch entry b
  * sees the cached tokens 0..L_b-1 and the nodes j with bit j of its mask set.
+ * A length past max_seq_len, or past what the page table has room for, is cut there and
+ * reported (SP_DEV_BAD_LENGTH).
  *   d_mask     uint64 device (see shared_mask); NULL: a chain (0..i)
  *   d_n_nodes  [batch] int32 device: nodes of each tree, 0..N; NULL: N
  *   d_q        [batch * N][Hq][dh], rotated; d_k_new, d_v_new [batch * N][Hkv][dh]

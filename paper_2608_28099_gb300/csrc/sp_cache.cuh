@@ -120,6 +120,10 @@ struct TreeArgs {
     int dtype;                     // of q, k_new, v_new, out
     bool tensor;                   // which kernel
     float scale_log2;              // log2(e) * scale of the scores
+    // Most cached tokens of a sequence: max_seq_len, or what the page table has room for.
+    // max_seq_len may be no bound at all, and a corrupt length would then keep a kernel at it for
+    // seconds, with tile numbers of more than 31 bits.
+    int most_len;
     const int *seq_ids, *seq_lens, *n_nodes;
     const uint64_t *mask;          // NULL: a chain
     int mask_stride;               // words from a sequence to the next (0: shared)

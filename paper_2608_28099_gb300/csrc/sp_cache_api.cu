@@ -164,6 +164,8 @@ sp_status check_tree(const sp_tree_dims *d, const sp_token_cache *cache, int bat
     if ((a->qs * es | a->ks * es | a->vs * es) & 15)
         return fail(SP_ERR_INVALID_ARG, "q_stride, k_stride and v_stride must be multiples of 16 bytes");
     a->mask_stride = d->shared_mask ? 0 : a->N;
+    const long long paged = (long long)cache->kv.max_pages_per_seq * cache->kv.page_size;
+    a->most_len = cache->kv.layout == SP_KV_PAGED && paged < cache->max_seq_len ? (int)paged : cache->max_seq_len;
     a->tensor = d->path != 1 && tree_tc_supported(*a);
     if (d->path == 2 && !a->tensor)
         return fail(SP_ERR_UNSUPPORTED, "the tensor-core kernel needs bf16 rows, a bf16 or 8-bit cache of head_dim 128 "

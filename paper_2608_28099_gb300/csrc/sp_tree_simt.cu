@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(THREADS) tree_simt_kernel(const __grid_constan
     const int hv = blockIdx.y, g = hv / a.n_rb, rb = hv - g * a.n_rb, b = blockIdx.z, split = blockIdx.x;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int *status = threadIdx.x == 0 && hv == 0 && split == 0 ? a.status : nullptr;
-    const SeqRef sq = resolve_seq(a.seq_ids, a.seq_lens, 0, b, a.cache.kv.n_seqs, a.cache.max_seq_len, status);
+    const SeqRef sq = resolve_seq(a.seq_ids, a.seq_lens, 0, b, a.cache.kv.n_seqs, a.most_len, status);
     const int n = tree_nodes(a, b, status), total = sq.len + n;
     const int t_lo = min(total, split * a.split_tokens), t_hi = t_lo + min(a.split_tokens, total - t_lo);
     const int row0 = rb * a.rb_rows;

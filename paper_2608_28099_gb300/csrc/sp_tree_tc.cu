@@ -257,7 +257,7 @@ __device__ __forceinline__ void tree_prefix(const TreeArgs &a, int *prefix, int 
 #pragma unroll 1
     for (int b = b0; b < b1; ++b) {
         const int n = a.n_nodes ? a.n_nodes[b] : a.N;  // (asked for beside the length)
-        const SeqRef sq = resolve_seq(a.seq_ids, a.seq_lens, 0, b, a.cache.kv.n_seqs, a.cache.max_seq_len, status);
+        const SeqRef sq = resolve_seq(a.seq_ids, a.seq_lens, 0, b, a.cache.kv.n_seqs, a.most_len, status);
         sids[b] = sq.sid;
         lens[b] = sq.len;
         nodes[b] = checked_nodes(a, n, status);
@@ -1564,6 +1564,8 @@ void plan_tree_tc(TreeArgs *a, int n_sm) {
     a->n_rb = ceil_div(a->R, 256);
     a->rb_rows = a->n_rb == 1 ? a->R : (ceil_div(a->R, a->n_rb) + 7) / 8 * 8;
     const int Hv = a->Hkv * a->n_rb;
+    // (the tile list's numbers stay below 2^30)
+    a->most_len = (int)min((long long)a->most_len, (long long)((1 << 30) / a->B - 1) * TILE);
     AttnArgs &p = a->plan;
     p.B = a->B;
     p.tc_ctas = attn_tc_ctas(n_sm, Hv);

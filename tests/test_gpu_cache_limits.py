@@ -6,6 +6,7 @@ import pytest
 import paper_2608_28099_gb300 as sp
 from gpu_util import ensure_built, torch_dev
 from test_gpu_token_cache import append, make_rows
+from test_gpu_tree import tree_call
 from token_cache_util import Cache
 
 pytestmark = pytest.mark.gpu
@@ -56,3 +57,21 @@ def test_a_negative_length_appends_nothing(torch, cdt, page, length):
         other = torch.ones_like(cache.ks, dtype=torch.bool)
         other[cache._at(1, np.arange(5, 9))] = False
         assert bool((cache.ks[other] == 1).all()) and bool((cache.vs[other] == 1).all())
+
+
+@pytest.mark.parametrize("cdt,path", [(sp.SP_BF16, 1), (sp.SP_BF16, 2), (sp.SP_E4M3, 1), (sp.SP_E4M3, 2), (sp.SP_F32, 1)])
+@pytest.mark.parametrize("B", [1, 200])
+def test_a_length_that_the_page_table_has_no_room_for_is_cut(torch, cdt, path, B):
+    # the largest bound that is accepted stands for "none"; a corrupt length ends where the pages do
+    hkv, dh, N, most = 2, 128, 5, 2 ** 31 - 1 - 4096
+    cache = Cache(cdt, hkv, dh, [64] * B, 16, spare_pages=0)
+    g = torch.Generator().manual_seed(3)
+    for s in range(B):
+        cache.put(s, 0, *(torch.randn((64, hkv, dh), generator=g) for _ in range(2)))
+    q, k, v = (torch.randn((B, N, h, dh), generator=g).to(torch.bfloat16).cuda() for h in (4, hkv, hkv))
+    dims = sp.sp_tree_dims(4, N, sp.SP_BF16, path, 0, 0.0, 0, 0, 0)
+    lens = [64 if s % 3 == 1 else most - s for s in range(B)]
+    want, status = tree_call(torch, cache, dims, [64] * B, None, None, q, k, v, max_len=most)
+    assert status == 0
+    got, status = tree_call(torch, cache, dims, lens, None, None, q, k, v, max_len=most)
+    assert status == sp.SP_DEV_BAD_LENGTH and torch.equal(got, want)
