@@ -544,8 +544,8 @@ typedef struct sp_token_rows {
  *              positions on the way (rot->head_dim must be the cache's)
  *   d_k, d_v   rows in `dtype` (SP_F32 or SP_BF16)
  *   d_status   optional device int (OR-ed SP_DEV_* bits)
- * SP_E4M3: scale = max(amax, 2^-60) / 448 over the finite elements of a (token,
- * kv head), code = the nearest 8-bit value of x * (448 / max(amax, 2^-60)), ties to
+ * SP_E4M3: scale = max(amax, 2^-60) * (1 / 448), the factor and the product in fp32,
+ * over the finite elements of a (token, kv head), code = the nearest 8-bit value of x * (448 / max(amax, 2^-60)), ties to
  * even; a non-finite element becomes NaN.  Other types are rounded to nearest.
  * A sequence may appear once in a batch.  A token without a page, past
  * max_seq_len or whose row lies outside the buffers is skipped and reported, and so
