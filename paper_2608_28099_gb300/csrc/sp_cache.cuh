@@ -153,6 +153,19 @@ __device__ __forceinline__ uint64_t tree_mask(const TreeArgs &a, int b, int i, i
     return (a.mask ? a.mask[(size_t)b * a.mask_stride + i] : (2ull << i) - 1) & all;
 }
 
+// Lets a kernel take `bytes` of dynamic shared memory on the current device.  The calls have no
+// handle that would tie them to one, and the limit is each device's own: asked for once a device
+// (known: the kernel's).
+constexpr int MAX_DEVICES = 64;
+template <typename Kern>
+inline cudaError_t allow_smem(Kern kernel, int bytes, bool (&known)[MAX_DEVICES]) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (dev < MAX_DEVICES && known[dev])) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev < MAX_DEVICES) known[dev] = true;
+    return e;
+}
 // CUDA cores: every shape, fp32 arithmetic; shares of a sequence merged by a second kernel.
 void plan_tree_simt(TreeArgs *a, int n_sm);
 cudaError_t launch_tree_simt(const TreeArgs &a, cudaStream_t st);

@@ -29,14 +29,14 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // SMs of the current device, asked for once a device (a call's launch path).
 int sm_count() {
-    static int known[64] = {};
+    static int known[MAX_DEVICES] = {};
     int dev = 0, n = 152;
     if (cudaGetDevice(&dev) != cudaSuccess) {
         cudaGetLastError();  // (no device: the host-only checks still answer)
         return n;
     }
-    if (dev >= 0 && dev < 64 && known[dev]) return known[dev];
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && dev >= 0 && dev < 64)
+    if (dev >= 0 && dev < MAX_DEVICES && known[dev]) return known[dev];
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && dev >= 0 && dev < MAX_DEVICES)
         known[dev] = n;
     return n;
 }

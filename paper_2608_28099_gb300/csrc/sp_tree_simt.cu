@@ -229,15 +229,11 @@ __global__ void __launch_bounds__(THREADS) tree_merge_kernel(const __grid_consta
 
 template <int DH>
 cudaError_t run(const TreeArgs &a, cudaStream_t st) {
-    static bool attr = false;
-    if (!attr) {
-        const cudaError_t e = cudaFuncSetAttribute(tree_simt_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                   (int)sizeof(Smem<DH>));
-        if (e != cudaSuccess) return e;
-        attr = true;
-    }
+    static bool known[MAX_DEVICES] = {};
+    cudaError_t e = allow_smem(tree_simt_kernel<DH>, (int)sizeof(Smem<DH>), known);
+    if (e != cudaSuccess) return e;
     const dim3 grid(a.n_splits, a.Hkv * a.n_rb, a.B);
-    cudaError_t e = launch_k(tree_simt_kernel<DH>, grid, dim3(THREADS), sizeof(Smem<DH>), st, a);
+    e = launch_k(tree_simt_kernel<DH>, grid, dim3(THREADS), sizeof(Smem<DH>), st, a);
     if (e != cudaSuccess || a.n_splits == 1) return e;
     const long long rows = (long long)a.B * a.Hkv * a.R;
     return launch_k(tree_merge_kernel<DH>, dim3((unsigned)ceil_div_ll(rows, THREADS / 32)), dim3(THREADS), 0, st, a);

@@ -1541,12 +1541,9 @@ int row_tiles(const TreeArgs &a) { return a.rb_rows > 128 ? 2 : 1; }
 template <bool E4, int TPC, int MT>
 cudaError_t run(const TreeArgs &a, const Layout &lay, const CUtensorMap &mk, const CUtensorMap &mv, int2 *tab,
                 cudaStream_t st) {
-    static bool attr = false;
-    if (!attr) {
-        const cudaError_t e = cudaFuncSetAttribute(tree_tc_kernel<E4, TPC, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MAX);
-        if (e != cudaSuccess) return e;
-        attr = true;
-    }
+    static bool known[MAX_DEVICES] = {};
+    const cudaError_t e = allow_smem(tree_tc_kernel<E4, TPC, MT>, SMEM_MAX, known);
+    if (e != cudaSuccess) return e;
     return launch_k(tree_tc_kernel<E4, TPC, MT>, dim3(a.plan.tc_ctas), dim3(THREADS), (size_t)lay.smem, st, mk, mv, a,
                     lay, tab);
 }
