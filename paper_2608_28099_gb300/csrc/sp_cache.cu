@@ -66,14 +66,14 @@ struct RawVec {
 // turn into one another (half layout), one vector of whole pairs (interleaved), or one
 // vector of the dims that pass (a pair's scalar vector may have one element left) -- for every
 // head it visits of a token, U heads at a time: the next ones' loads are under way, as they
-// lie, while these are turned.  (cos, sin) of the
-// block's tokens are formed in shared memory behind the first loads (one sincospif a (token,
-// pair), shared by all heads).  V elements a vector: 16 bytes, or 1 (2 interleaved) where a
-// stride, base or width does not allow that.  A group of tokens fills the block; a block takes
-// up to GROUPS of them one after another.  HBM-bound where large: 16384 tokens of 48 bf16
-// heads, half of each in pairs, 61 us, 6.6 TB/s (one group a block, hence nothing to load
-// ahead: 69; values held as floats: 85); 4099 tokens of 40 fp32 heads turned back, one group a
-// block, 27.3 us, 6.2 TB/s; 16 tokens 5.3 us (a launch).
+// lie, while these are turned.  (cos, sin) of the block's tokens are formed in shared memory
+// behind the first loads (one sincospif a (token, pair), shared by all heads).  V elements a
+// vector: 16 bytes, or 1 (2 interleaved) where a stride, base or width does not allow that.  A
+// group of tokens fills the block; a block takes up to GROUPS of them one after another.
+// HBM-bound where large: 16384 tokens of 48 bf16 heads, half of each in pairs, 61 us, 6.6 TB/s
+// (one group a block, hence nothing to load ahead: 69; values held as floats: 85); 4099 tokens of
+// 40 fp32 heads turned back, one group a block, 27.3 us, 6.2 TB/s; 16 tokens 5.3 to 5.8 us (a
+// launch).
 template <typename T, int V, bool INTER>
 __global__ void __launch_bounds__(THREADS, 4) rotate_kernel(const __grid_constant__ RotateArgs a) {
     extern __shared__ float2 cs[];  // [token][pair]
@@ -326,7 +326,8 @@ struct RowWalk {
 // their (cos, sin).  The row's amax is a shuffle among its lanes.  Bound by its
 // instructions (about ten an element: rotation, amax, scale, conversion) and its loads' latency:
 // 12 prompts of 500 to 4000 tokens, 8 kv heads, rotated and quantised at 3.2 to 4.0 TB/s, 42 to
-// 52 us by the lengths drawn; 64 accepted paths of up to 6 tokens in 4.6 us (a launch).  Three
+// 55 us by the lengths drawn (into bf16 pages, less to compute and more to write, 47 where 8 bits
+// take 50: 5.0 TB/s); 64 accepted paths of up to 6 tokens in 4.7 us (a launch).  Three
 // blocks an SM took 52 to 55 us, one row in flight 75 to 85.  (fp32 rows hold twice the
 // registers: two blocks.)
 template <typename T>
@@ -475,9 +476,10 @@ __global__ void __launch_bounds__(THREADS, kAppendBlocks<T>) append_kernel(const
 // Read back: rows the other way, 16 elements a lane; tokens outside the sequence give
 // zeros.  A block's tokens are looked up once, then U rows a thread are in flight.  CT: the
 // cache's elements (Code16: 8 bits).  Bound by its loads' latency and HBM: 6 contexts of 3000
-// to 9000 tokens, 8 kv heads, 8-bit, as bf16 in 58 to 60 us, 5 TB/s; 3 of 100 to 700 tokens as fp32
-// in 7.1 us.  Sixteen neighbouring elements a lane, whose halves are stored 32 bytes apart, took
-// 65 and 7.9 us, five blocks an SM 56 and 8.2, the next rows' loads under way 71 and 8.3.
+// to 9000 tokens, 8 kv heads, 8-bit, as bf16 in 58 to 62 us, 5 TB/s (from bf16 pages 67 us, 5.7
+// TB/s, from contiguous bf16 62); 3 of 100 to 700 tokens as fp32 in 7.2 us.  Sixteen neighbouring
+// elements a lane, whose halves are stored 32 bytes apart, took 65 and 7.9 us, five blocks an SM
+// 56 and 8.2, the next rows' loads under way 71 and 8.3.
 template <int LANES, typename CT>
 __global__ void __launch_bounds__(THREADS) read_kernel(const __grid_constant__ CopyArgs a) {
     __shared__ long long out_row[MAX_TOK], place[MAX_TOK];

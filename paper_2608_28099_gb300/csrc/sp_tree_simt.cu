@@ -8,11 +8,12 @@
 // dh / 32 dims a lane for the values; a warp owns four rows with their running (max,
 // sum, O).  Shares are merged by a second kernel.  Bound by shared-memory reads (5
 // vector loads per 16 multiply-adds a lane in the score product).  Five sequences of 0 to 500
-// tokens, 11 nodes, head_dim 32, fp32: 16.8 us with the merge, latency.  Where the tensor-core
-// kernel applies this one is not taken: one sequence of 2048 tokens, 8 nodes, 33 against 16 us;
-// 64 tokens, one node, 18 against 12; 64 sequences of 1024 to 8192 tokens, 16 nodes, 4315
-// against 190 (an empty cache alone is faster here, 8.3 against 11.0, and lengths are not known
-// to the host).
+// tokens, 11 nodes, head_dim 32, fp32: 17 us with the merge, latency; eight of 1000 to 4000, 16
+// nodes, 16 heads of 128, fp32: 180 us, 16 TFLOP/s.  Where the tensor-core kernel applies this
+// one is not taken: one sequence of 2048 tokens, 8 nodes, 33 against 16 us; 64 tokens, one node,
+// 18 against 12; 64 sequences of 1024 to 8192 tokens, 16 nodes, 4315 against 190 (an empty cache
+// alone is faster here, 8.3 against 11.0, and lengths are not known to the host).  Those 64
+// sequences with heads of 64 (32) dims, which that kernel does not take: 2990 (2035) us.
 #include "sp_cache.cuh"
 #include "sp_sm100.cuh"
 
@@ -150,7 +151,7 @@ __global__ void __launch_bounds__(THREADS) tree_simt_kernel(const __grid_constan
             for (int d = 0; d < D; ++d) o[r][d] *= al;
         }
         // a weight of 0 is skipped: what a row does not see (NaN, infinities) must not
-        // reach it as 0 * v
+        // reach it as 0 * v (what it sees has at least the least weight)
 #pragma unroll 4
         for (int x = 0; x < TOK; ++x) {
             float v[D];

@@ -47,15 +47,15 @@
 //
 // What bounds it, with the merge:
 //   bf16          HBM.  64 sequences of 1024 to 8192 tokens, 32 query heads, 8 kv heads, 16
-//                 nodes: 209 us, 5.9 TB/s.  One sequence of 2048 tokens, 8 nodes: 15.4 us, of
-//                 which 2.7 to know the shares, 2 to the first scores, 1.6 for an epilogue and
-//                 4 for the merge and its launch
+//                 nodes: 210 to 220 us, 5.6 to 5.9 TB/s.  One sequence of 2048 tokens, 8 nodes:
+//                 15.6 to 16.2 us, of which 2.7 to know the shares, 2 to the first scores, 1.6
+//                 for an epilogue and 4 for the merge and its launch
 //   8-bit         the chain of a pipeline, scores -> softmax -> product -> next scores (half of
 //                 TMEM is scores, half outputs: no room for the next scores before the product
 //                 has read the weights).  8 sequences of 32768 tokens, 40 heads, 32 nodes (160
 //                 rows, two M tiles): 377 us, 0.46 PFLOP/s, some 5000 cycles of softmax in 6800
-//                 a tile.  128 sequences of 300 to 4000 tokens, 32 heads, one node: 194 us, 3.0
-//                 TB/s, 2600 cycles a tile that the conversion, the V loader and the MMA issuer
+//                 a tile.  128 sequences of 300 to 4000 tokens, 32 heads, one node: 185 to 196 us,
+//                 3.0 TB/s, 2600 cycles a tile that the conversion, the V loader and the MMA issuer
 //                 fill to 60 - 80 %.
 // The kernel's code is as large as what the instruction caches hold: loops are unrolled as
 // little as their latency allows (unrolling the conversion and the loaders from 95 to 105 KB of
