@@ -296,11 +296,6 @@ __device__ __forceinline__ Chunk chunk_of(const CopyArgs &a, int *status) {
     c.n = max(0, min(a.tokens_per_block, c.count - c.j0));
     return c;
 }
-// A negative length is reported and reads as 0.  Nothing may be written for it: the new tokens
-// would take the places of the sequence's first ones.
-__device__ __forceinline__ bool may_write(const CopyArgs &a, const Chunk &c) {
-    return c.sq.sid >= 0 && a.seq_lens[c.sq.sid] >= 0;
-}
 
 constexpr int MAX_TOK = 16;  // tokens of a block (32: the long contexts below read in 72 instead of 68 us)
 
@@ -342,7 +337,7 @@ __global__ void __launch_bounds__(THREADS, kAppendBlocks<T>) append_kernel(const
     pdl_wait();
     pdl_trigger();
     const Chunk ck = chunk_of(a, threadIdx.x == 0 && blockIdx.x % a.chunks == 0 ? a.status : nullptr);
-    if (ck.n == 0 || !may_write(a, ck)) return;  // uniform over the block
+    if (ck.n == 0 || ck.sq.sid < 0) return;  // uniform over the block
     const CacheDev &c = a.cache;
     const int half = a.rot.half, Hkv = c.Hkv, dh = LANES * 16;
     const int rows = ck.n * 2 * Hkv, lane = threadIdx.x % LANES, first = threadIdx.x / LANES;
@@ -373,7 +368,8 @@ __global__ void __launch_bounds__(THREADS, kAppendBlocks<T>) append_kernel(const
         const long long t = (long long)ck.sq.len + ck.j0 + j;  // (a length near max_seq_len's own limit passes 31 bits)
         long long dst = -1;
         int bad = 0, step;
-        if (t >= c.max_seq_len) bad = SP_DEV_BAD_LENGTH;
+        // (a negative length reads as 0 above: its tokens would take the places of the first ones)
+        if (t >= c.max_seq_len || a.seq_lens[ck.sq.sid] < 0) bad = SP_DEV_BAD_LENGTH;
         else if (source(j, 0, 0) < 0) bad = SP_DEV_BAD_ROW;
         else if (!cache_row(c, ck.sq.sid, (int)t, &dst, &step)) bad = SP_DEV_BAD_PAGE;
         place[j] = bad ? -1 : dst;
