@@ -498,9 +498,10 @@ SP_API sp_status sp_rotary_plan(int kind, int rot_dim, double theta, double fact
  * Head h of token t starts at element t * token_stride + h * head_stride of x
  * and of y (dtype SP_F32 or SP_BF16, one type for both; the dims of a head are
  * contiguous); angles and products are fp32, rounded once.  y may be x with the
- * same strides, else they must not overlap.  Any alignment of the elements'
- * own works; 16-byte aligned bases, strides of whole 16 bytes and rotated parts
- * of whole 16-byte vectors are fast.  n_tokens = 0 is a no-op. */
+ * same strides, else they must not overlap; heads of y must not overlap one another.
+ * Any alignment of the elements' own works; 16-byte aligned bases, strides of whole
+ * 16 bytes and rotated parts of whole 16-byte vectors are fast.  n_tokens = 0 is a
+ * no-op. */
 SP_API sp_status sp_rotate(sp_stream stream, const sp_rotary *rot, int n_tokens, const int *d_positions,
                            int backward, int dtype, int n_heads, const void *d_x, long long x_token_stride,
                            long long x_head_stride, void *d_y, long long y_token_stride,

@@ -41,6 +41,21 @@ int sm_count() {
     return n;
 }
 
+// Whether any two of n x m blocks of `width` elements, a and b (>= width) apart, overlap.
+bool blocks_overlap(long long n, long long a, long long m, long long b, long long width) {
+    if (n < 2 || m < 2) return false;
+    if (a > b) {
+        const long long x = a, y = n;
+        a = b, b = x, n = m, m = y;
+    }
+    for (long long j = 1; j < m; ++j) {  // blocks of the wider step, as far as those of the other reach
+        const long long i = j * b / a, rest = j * b - i * a;
+        if (i >= n) break;
+        if (rest < width || (i + 1 < n && a - rest < width)) return true;
+    }
+    return false;
+}
+
 bool float_type(int dtype) { return dtype == SP_F32 || dtype == SP_BF16; }
 
 sp_status check_rotary(const sp_rotary *r, RotaryDev *out) {
@@ -241,7 +256,8 @@ sp_status sp_rotate(sp_stream stream, const sp_rotary *rot, int n_tokens, const 
     if ((((uintptr_t)d_x) | ((uintptr_t)d_y)) & (es - 1)) return fail(SP_ERR_INVALID_ARG, "x and y must be aligned to their type");
     if (x_token_stride < 0 || x_head_stride < 0 || y_token_stride < 0 || y_head_stride < 0)
         return fail(SP_ERR_INVALID_ARG, "strides must be >= 0");
-    if ((n_heads > 1 && y_head_stride < rot->head_dim) || (n_tokens > 1 && y_token_stride < rot->head_dim))
+    if ((n_heads > 1 && y_head_stride < rot->head_dim) || (n_tokens > 1 && y_token_stride < rot->head_dim) ||
+        blocks_overlap(n_heads, y_head_stride, n_tokens, y_token_stride, rot->head_dim))
         return fail(SP_ERR_INVALID_ARG, "heads or tokens of y overlap");
     if (d_x == d_y && (x_token_stride != y_token_stride || x_head_stride != y_head_stride))
         return fail(SP_ERR_INVALID_ARG, "in place needs equal strides");
