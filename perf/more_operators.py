@@ -288,7 +288,7 @@ def _plan(case, s):
         else:
             p["dh"] = new((n, d))
             p["dw"] = new((V, d)) if case["head"] else None
-            size = sp.sp_vocab_loss_backward_workspace_bytes(p["dims"], case["head"])
+            size = sp.sp_vocab_loss_backward_workspace_bytes(p["dims"])
     p["bytes"] = size
     p["ws"] = new((max(size, 1),), torch.uint8)
     return p
