@@ -615,6 +615,123 @@ SP_API sp_status sp_attend_tree(sp_stream stream, const sp_tree_dims *dims, cons
                                 const int *d_n_nodes, const void *d_q, const void *d_k_new, const void *d_v_new,
                                 void *d_out, void *d_workspace, size_t workspace_bytes, int *d_status);
 
+/* Attention of a tree as sp_attend_tree (every argument and rule is its), for training: d_lse
+ * [batch * N][Hq] float receives the log of the sum of each row's exponentials, log sum_t
+ * exp(scale q.k_t), -inf for a row that sees nothing; d_out has sp_attend_tree's bits. */
+SP_API sp_status sp_attend_tree_lse(sp_stream stream, const sp_tree_dims *dims, const sp_token_cache *cache, int batch,
+                                    const int *d_seq_ids, const int *d_seq_lens, const uint64_t *d_mask,
+                                    const int *d_n_nodes, const void *d_q, const void *d_k_new, const void *d_v_new,
+                                    void *d_out, float *d_lse, void *d_workspace, size_t workspace_bytes, int *d_status);
+
+/* Bytes of device scratch sp_attend_tree_backward needs (256-byte aligned start); 0 for
+ * invalid dims. */
+SP_API size_t sp_attend_tree_backward_workspace_bytes(const sp_tree_dims *dims, const sp_token_cache *cache, int batch);
+
+/* Backward pass of sp_attend_tree_lse: gradients of the nodes' queries, keys and values.  The
+ * cache is a constant, as it is to a probe that is taught (Sec. 3.2: the base model and the draft
+ * layer are frozen); with d_mask = NULL the nodes are a probe's soft-prompt rows.
+ *   d_out, d_lse   what the forward pass wrote; d_grad_out [batch * N][Hq][dh]
+ *   d_grad_q, d_grad_k, d_grad_v: rows of dims' q_stride, k_stride and v_stride elements in
+ *       dims' dtype, so that they may be the parts of one gradient of a fused projection (the
+ *       heads of a row are written, nothing between them); zeros for nodes from n_nodes on
+ *       and queries that see nothing.  They must not overlap one another or an input.
+ * Gradients of the query heads that share a kv head are added in one order: two calls on the same
+ * arguments give the same bits.  What a row does not see has no influence (see sp_attend_tree); a
+ * row that sees a NaN or an infinity may have gradients of NaN in all dims.
+ * SP_F32, and shapes that the tensor cores do not take, are computed in fp32 on CUDA cores;
+ * SP_BF16 over SP_BF16 caches of head_dim 128 (batch <= 2048) on tensor cores, with weights and their
+ * gradients rounded to bf16 as operands of products with fp32 sums. */
+SP_API sp_status sp_attend_tree_backward(sp_stream stream, const sp_tree_dims *dims, const sp_token_cache *cache,
+                                         int batch, const int *d_seq_ids, const int *d_seq_lens, const uint64_t *d_mask,
+                                         const int *d_n_nodes, const void *d_q, const void *d_k_new,
+                                         const void *d_v_new, const void *d_out, const float *d_lse,
+                                         const void *d_grad_out, void *d_grad_q, void *d_grad_k, void *d_grad_v,
+                                         void *d_workspace, size_t workspace_bytes, int *d_status);
+
+/* ------------------------------------------------------------------------- */
+/* Row norms and the vocabulary loss: what a probe, a soft prompt or a draft    */
+/* layer's readout is taught with.  No handle; asynchronous, nothing allocated. */
+/* ------------------------------------------------------------------------- */
+typedef struct sp_norm_dims {
+    int n_rows;          /* >= 0                                                      */
+    int d;               /* elements of a row, 1..2^24                                */
+    int dtype;           /* SP_F32 or SP_BF16: rows and their gradients               */
+    int out_dtype;       /* of sp_norm's y: dtype, or SP_E4M3                         */
+    float eps;           /* added to the mean square, >= 0                            */
+    long long x_stride;  /* elements from a row to the next; 0 = d: of x and grad_x,  */
+    long long r_stride;  /* of residual and grad_sum,                                 */
+    long long s_stride;  /* of sum,                                                   */
+    long long y_stride;  /* of y and grad_y                                           */
+} sp_norm_dims;
+
+/* Root-mean-square norm of rows with a residual's addition (Sec. 3.1, the layer's norms):
+ *   s = x + residual (NULL: s = x),  y = s / sqrt(mean(s^2) + eps) * gain (NULL: ones)
+ * s enters the norm in fp32, unrounded; d_sum (NULL: not wanted) receives it rounded to dtype.
+ * SP_E4M3 rows: codes in d_y and a scale a row in d_y_scale [n_rows], formed as
+ * sp_cache_append forms them (from the largest finite element; non-finite ones become NaN).
+ * d_sum or d_y (of dtype) may be d_x or d_residual with the same stride; otherwise outputs overlap
+ * nothing.  Rows whose squares leave the range of fp32 are normed all the same.  Any alignment of
+ * the elements' own works; d a multiple of 8 and 16-byte aligned rows (8-byte for codes) are fast. */
+SP_API sp_status sp_norm(sp_stream stream, const sp_norm_dims *dims, const void *d_x, const void *d_residual,
+                         const float *d_gain, void *d_sum, void *d_y, float *d_y_scale);
+
+/* Bytes of device scratch sp_norm_backward needs where the gain's gradient is wanted (256-byte
+ * aligned start); 0 for invalid dims. */
+SP_API size_t sp_norm_backward_workspace_bytes(const sp_norm_dims *dims);
+
+/* Backward pass of y = s rstd gain at s = d_sum (out_dtype is ignored), xh = s rstd:
+ *   grad_x = rstd (gain grad_y - xh mean(gain grad_y xh)) + grad_sum (NULL: 0)
+ *   grad_gain [d] (NULL: not wanted; then no workspace) = sum over rows of grad_y xh
+ * grad_x is the gradient of x and of the residual alike; grad_sum what reaches the sum past the
+ * norm.  d_grad_x may be any of the input rows with the same stride.  Rows are added in one
+ * order: the same bits every time on one kind of device.  n_rows = 0: grad_gain is cleared. */
+SP_API sp_status sp_norm_backward(sp_stream stream, const sp_norm_dims *dims, const void *d_grad_y, const void *d_sum,
+                                  const float *d_gain, const void *d_grad_sum, void *d_grad_x, float *d_grad_gain,
+                                  void *d_workspace, size_t workspace_bytes);
+
+typedef struct sp_vocab_dims {
+    int n_tokens;        /* 0..4000000                                                */
+    int vocab;           /* rows of the head V, 1..2^24                               */
+    int d_model;         /* d, 1..2^20                                                */
+    int dtype;           /* of h, w and their gradients.  SP_F32: fp32 on CUDA cores.
+                            SP_BF16: products of bf16 with fp32 sums on the tensor
+                            cores where d_model and the strides are multiples of 8
+                            (rows 16-byte aligned then), else as SP_F32               */
+    int path;            /* 0 = automatic, 1 = CUDA cores, 2 = tensor cores
+                            (SP_ERR_UNSUPPORTED where they do not apply)              */
+    long long h_stride;  /* elements from a row of h (grad_h) to the next; 0 = d      */
+    long long w_stride;  /* the same of w (grad_w)                                    */
+} sp_vocab_dims;
+
+/* Bytes of device scratch the two calls need (256-byte aligned start); 0 for invalid dims. */
+SP_API size_t sp_vocab_loss_workspace_bytes(const sp_vocab_dims *dims);
+SP_API size_t sp_vocab_loss_backward_workspace_bytes(const sp_vocab_dims *dims);
+
+/* Cross entropy over a vocabulary (the frozen or trained LM head of Sec. 3.1 and Sec. 5) without
+ * keeping the logits l_v = h.w_v of a token:
+ *   lse = log sum_v exp(l_v),  loss = lse - l_target
+ *   d_h [n][d], d_w [V][d]; d_targets [n] int32 device: a negative one means that the token has
+ *   none (its loss and lse are 0, its row of h is not used); one >= V is reported
+ *   (SP_DEV_BAD_ROW) and taken for none
+ *   d_loss, d_lse [n] float
+ *   d_status       optional device int (OR-ed SP_DEV_* bits)
+ * A token with a NaN or +infinite logit has NaN for both. */
+SP_API sp_status sp_vocab_loss(sp_stream stream, const sp_vocab_dims *dims, const void *d_h, const void *d_w,
+                               const int *d_targets, float *d_loss, float *d_lse, void *d_workspace,
+                               size_t workspace_bytes, int *d_status);
+
+/* Its gradients, the logits formed again a piece of the vocabulary at a time:
+ *   g_v = grad_loss (exp(l_v - lse) - [v = target]),  grad_h = sum_v g_v w_v,  grad_w_v = sum g_v h
+ *   d_lse          what the forward pass wrote; d_grad_loss [n] float (NULL: ones)
+ *   d_grad_h       [n][d], zeros for tokens without a target
+ *   d_grad_w       [V][d], or NULL: the head is frozen
+ * On tensor cores g is rounded to bf16 as an operand (the target's p - 1 is formed before).  Sums
+ * run in one order.  The gradients must not overlap each other or an input. */
+SP_API sp_status sp_vocab_loss_backward(sp_stream stream, const sp_vocab_dims *dims, const void *d_h, const void *d_w,
+                                        const int *d_targets, const float *d_lse, const float *d_grad_loss,
+                                        void *d_grad_h, void *d_grad_w, void *d_workspace, size_t workspace_bytes,
+                                        int *d_status);
+
 #ifdef __cplusplus
 }
 #endif

@@ -37,7 +37,10 @@ EXPORTED = ["sp_create", "sp_destroy", "sp_classify", "sp_classify_host", "sp_ch
             "sp_attend_static", "sp_classify_hidden", "sp_classify_hidden_host",
             "sp_debug_gathered_pages", "sp_debug_gemm_plan", "sp_rotary_plan", "sp_rotate",
             "sp_cache_append", "sp_cache_read", "sp_tree_masks", "sp_attend_tree_workspace_bytes",
-            "sp_attend_tree"]
+            "sp_attend_tree", "sp_attend_tree_lse", "sp_attend_tree_backward_workspace_bytes",
+            "sp_attend_tree_backward", "sp_norm", "sp_norm_backward_workspace_bytes", "sp_norm_backward",
+            "sp_vocab_loss_workspace_bytes", "sp_vocab_loss", "sp_vocab_loss_backward_workspace_bytes",
+            "sp_vocab_loss_backward"]
 
 
 class sp_config(C.Structure):
@@ -96,6 +99,17 @@ class sp_tree_dims(C.Structure):
                 ("q_stride", C.c_longlong), ("k_stride", C.c_longlong), ("v_stride", C.c_longlong)]
 
 
+class sp_norm_dims(C.Structure):
+    _fields_ = [("n_rows", C.c_int), ("d", C.c_int), ("dtype", C.c_int), ("out_dtype", C.c_int),
+                ("eps", C.c_float), ("x_stride", C.c_longlong), ("r_stride", C.c_longlong),
+                ("s_stride", C.c_longlong), ("y_stride", C.c_longlong)]
+
+
+class sp_vocab_dims(C.Structure):
+    _fields_ = [("n_tokens", C.c_int), ("vocab", C.c_int), ("d_model", C.c_int), ("dtype", C.c_int),
+                ("path", C.c_int), ("h_stride", C.c_longlong), ("w_stride", C.c_longlong)]
+
+
 class SpError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"status {status}: {msg}")
@@ -129,10 +143,8 @@ def load_library(path: str | None = None):
     lib.sp_last_launch_count.argtypes = [vp]
     lib.sp_last_launch_count.restype = C.c_int
     lib.sp_attend_workspace_bytes.argtypes = [C.POINTER(sp_attn_dims), i]
-    lib.sp_attend_workspace_bytes.restype = C.c_size_t
     lib.sp_stage_times.argtypes = [vp, C.POINTER(C.c_float), i]
     lib.sp_project_workspace_bytes.argtypes = [i, i, i]
-    lib.sp_project_workspace_bytes.restype = C.c_size_t
     lib.sp_project.argtypes = [vp, i, i, i, vp, vp, vp, i, vp, C.c_size_t]
     lib.sp_attend_static.argtypes = [vp, C.POINTER(sp_attn_dims), i, vp, vp,
                                      C.POINTER(sp_kv_cache), vp, vp, vp, vp, i, vp, vp]
@@ -148,14 +160,27 @@ def load_library(path: str | None = None):
     lib.sp_tree_masks.argtypes = [i, vp, vp, vp]
     lib.sp_attend_tree_workspace_bytes.argtypes = [C.POINTER(sp_tree_dims),
                                                    C.POINTER(sp_token_cache), i]
-    lib.sp_attend_tree_workspace_bytes.restype = C.c_size_t
     lib.sp_attend_tree.argtypes = [vp, C.POINTER(sp_tree_dims), C.POINTER(sp_token_cache), i, vp, vp,
                                    vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    tree = [vp, C.POINTER(sp_tree_dims), C.POINTER(sp_token_cache), i, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.sp_attend_tree_lse.argtypes = tree + [vp, vp, C.c_size_t, vp]
+    lib.sp_attend_tree_backward_workspace_bytes.argtypes = [C.POINTER(sp_tree_dims), C.POINTER(sp_token_cache), i]
+    lib.sp_attend_tree_backward.argtypes = tree + [vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.sp_norm.argtypes = [vp, C.POINTER(sp_norm_dims), vp, vp, vp, vp, vp, vp]
+    lib.sp_norm_backward_workspace_bytes.argtypes = [C.POINTER(sp_norm_dims)]
+    lib.sp_norm_backward.argtypes = [vp, C.POINTER(sp_norm_dims), vp, vp, vp, vp, vp, vp, vp, C.c_size_t]
+    lib.sp_vocab_loss_workspace_bytes.argtypes = [C.POINTER(sp_vocab_dims)]
+    lib.sp_vocab_loss.argtypes = [vp, C.POINTER(sp_vocab_dims), vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.sp_vocab_loss_backward_workspace_bytes.argtypes = [C.POINTER(sp_vocab_dims)]
+    lib.sp_vocab_loss_backward.argtypes = [vp, C.POINTER(sp_vocab_dims), vp, vp, vp, vp, vp, vp, vp, vp,
+                                           C.c_size_t, vp]
+    for name in EXPORTED:
+        if name.endswith("_workspace_bytes"):
+            getattr(lib, name).restype = C.c_size_t
     lib.sp_debug_gathered_pages.argtypes = [vp, vp, C.c_size_t]
     lib.sp_debug_gemm_plan.argtypes = [i, i, i, i, i, i, C.c_size_t, C.POINTER(sp_gemm_plan)]
     for name in EXPORTED:
-        if name not in ("sp_last_error", "sp_last_launch_count", "sp_attend_workspace_bytes",
-                        "sp_project_workspace_bytes", "sp_attend_tree_workspace_bytes"):
+        if name not in ("sp_last_error", "sp_last_launch_count") and not name.endswith("_workspace_bytes"):
             getattr(lib, name).restype = C.c_int
     if path is None:
         _lib = lib
@@ -352,6 +377,66 @@ def sp_attend_tree(stream, dims: sp_tree_dims, cache: sp_token_cache, batch, seq
                                          _ptr(seq_ids), _ptr(seq_lens), _ptr(mask), _ptr(n_nodes),
                                          _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out),
                                          _ptr(workspace), int(workspace_bytes), _ptr(status)))
+
+
+def sp_attend_tree_lse(stream, dims: sp_tree_dims, cache: sp_token_cache, batch, seq_ids, seq_lens, mask, n_nodes, q,
+                       k_new, v_new, out, lse, workspace, workspace_bytes, status=None):
+    _check(load_library().sp_attend_tree_lse(_stream(stream), C.byref(dims), C.byref(cache), int(batch), _ptr(seq_ids),
+                                             _ptr(seq_lens), _ptr(mask), _ptr(n_nodes), _ptr(q), _ptr(k_new),
+                                             _ptr(v_new), _ptr(out), _ptr(lse), _ptr(workspace), int(workspace_bytes),
+                                             _ptr(status)))
+
+
+def sp_attend_tree_backward_workspace_bytes(dims: sp_tree_dims, cache: sp_token_cache, batch) -> int:
+    return load_library().sp_attend_tree_backward_workspace_bytes(C.byref(dims), C.byref(cache), int(batch))
+
+
+def sp_attend_tree_backward(stream, dims: sp_tree_dims, cache: sp_token_cache, batch, seq_ids, seq_lens, mask, n_nodes,
+                            q, k_new, v_new, out, lse, grad_out, grad_q, grad_k, grad_v, workspace, workspace_bytes,
+                            status=None):
+    _check(load_library().sp_attend_tree_backward(
+        _stream(stream), C.byref(dims), C.byref(cache), int(batch), _ptr(seq_ids), _ptr(seq_lens), _ptr(mask),
+        _ptr(n_nodes), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(lse), _ptr(grad_out), _ptr(grad_q),
+        _ptr(grad_k), _ptr(grad_v), _ptr(workspace), int(workspace_bytes), _ptr(status)))
+
+
+def sp_norm(stream, dims: sp_norm_dims, x, residual, gain, sum, y, y_scale=None):
+    """residual, gain, sum: None for none, ones, not wanted; y_scale: of 8-bit rows."""
+    _check(load_library().sp_norm(_stream(stream), C.byref(dims), _ptr(x), _ptr(residual), _ptr(gain), _ptr(sum), _ptr(y),
+                                  _ptr(y_scale)))
+
+
+def sp_norm_backward_workspace_bytes(dims: sp_norm_dims) -> int:
+    return load_library().sp_norm_backward_workspace_bytes(C.byref(dims))
+
+
+def sp_norm_backward(stream, dims: sp_norm_dims, grad_y, sum, gain, grad_sum, grad_x, grad_gain=None, workspace=None,
+                     workspace_bytes=0):
+    """grad_sum: a gradient that reaches the sum past the norm, or None."""
+    _check(load_library().sp_norm_backward(_stream(stream), C.byref(dims), _ptr(grad_y), _ptr(sum), _ptr(gain),
+                                           _ptr(grad_sum), _ptr(grad_x), _ptr(grad_gain), _ptr(workspace),
+                                           int(workspace_bytes)))
+
+
+def sp_vocab_loss_workspace_bytes(dims: sp_vocab_dims) -> int:
+    return load_library().sp_vocab_loss_workspace_bytes(C.byref(dims))
+
+
+def sp_vocab_loss(stream, dims: sp_vocab_dims, h, w, targets, loss, lse, workspace, workspace_bytes, status=None):
+    _check(load_library().sp_vocab_loss(_stream(stream), C.byref(dims), _ptr(h), _ptr(w), _ptr(targets), _ptr(loss),
+                                        _ptr(lse), _ptr(workspace), int(workspace_bytes), _ptr(status)))
+
+
+def sp_vocab_loss_backward_workspace_bytes(dims: sp_vocab_dims) -> int:
+    return load_library().sp_vocab_loss_backward_workspace_bytes(C.byref(dims))
+
+
+def sp_vocab_loss_backward(stream, dims: sp_vocab_dims, h, w, targets, lse, grad_loss, grad_h, grad_w, workspace,
+                           workspace_bytes, status=None):
+    """grad_loss: None for ones; grad_w: None under a frozen head."""
+    _check(load_library().sp_vocab_loss_backward(_stream(stream), C.byref(dims), _ptr(h), _ptr(w), _ptr(targets),
+                                                 _ptr(lse), _ptr(grad_loss), _ptr(grad_h), _ptr(grad_w),
+                                                 _ptr(workspace), int(workspace_bytes), _ptr(status)))
 
 
 # --------------------------------------------------------------------------- #

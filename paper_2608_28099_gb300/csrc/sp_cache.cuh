@@ -130,6 +130,7 @@ struct TreeArgs {
     const void *q, *k_new, *v_new;
     long long qs, ks, vs;          // elements from a node's row to the next
     void *out;
+    float *lse;                    // NULL, or [B N][Hq]: log of the sum of a row's exponentials
     int n_splits, split_tokens;    // CUDA cores: shares of a sequence's [cache ; tree]
     AttnArgs plan;                 // tensor cores: what sp_attn_plan.cuh cuts the work by
     float *part_o, *part_ml;       // [slot][rb_rows][dh] unnormalised, [slot][rb_rows][2] (max in
@@ -146,6 +147,10 @@ __device__ __forceinline__ int checked_nodes(const TreeArgs &a, int n, int *stat
 }
 __device__ __forceinline__ int tree_nodes(const TreeArgs &a, int b, int *status) {
     return checked_nodes(a, a.n_nodes ? a.n_nodes[b] : a.N, status);
+}
+// log of a row's sum of exponentials from its (max in log2 units, sum); -inf: it sees nothing.
+__device__ __forceinline__ void store_lse(const TreeArgs &a, int b, int node, int head, float m, float l) {
+    a.lse[((size_t)b * a.N + node) * a.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
 }
 // The nodes that node i of sequence b sees.
 __device__ __forceinline__ uint64_t tree_mask(const TreeArgs &a, int b, int i, int n) {
@@ -177,5 +182,28 @@ void plan_tree_tc(TreeArgs *a, int n_sm);
 size_t tree_tc_slots(const TreeArgs &a);
 int tree_tc_groups(const TreeArgs &a);
 cudaError_t launch_tree_tc(const TreeArgs &a, int2 *split_tab, cudaStream_t st);
+
+// The backward pass (sp_tree_back.cu): TreeArgs with `out` the forward pass's output and `lse` its
+// log sums, both read.
+struct TreeBackArgs {
+    TreeArgs t;
+    const void *dout;
+    void *dq, *dk, *dv;            // rows qs, ks, vs elements apart
+    float2 *stat;                  // [B][Hkv][R]: (log sum in log2 units, +inf for a row that sees
+                                   // nothing; sum of out * dout)
+    float *dq_new;                 // [B][Hkv][R][dh]: the nodes' own part of dq, unscaled
+    float scale;
+};
+// Row statistics, gradients of the nodes' keys and values, the nodes' part of dq.
+cudaError_t launch_tree_back_rows(const TreeBackArgs &a, cudaStream_t st);
+// The cache's part of dq on CUDA cores in shares (t.part_o: [slot][row][dh]), and the sum of all parts.
+cudaError_t launch_tree_back_simt(const TreeBackArgs &a, cudaStream_t st);
+size_t tree_back_simt_slots(const TreeArgs &a);
+// The same on tensor cores: head_dim 128, bf16 rows and cache, B <= 2048.
+inline bool tree_back_tc_supported(const TreeArgs &) { return false; }
+inline void plan_tree_back_tc(TreeArgs *, int) {}
+inline size_t tree_back_tc_slots(const TreeArgs &) { return 0; }
+inline int tree_back_tc_groups(const TreeArgs &) { return 0; }
+inline cudaError_t launch_tree_back_tc(const TreeBackArgs &, int2 *, cudaStream_t) { return cudaErrorInvalidValue; }
 
 }  // namespace sp

@@ -1,45 +1,14 @@
 // C entry points of the token-cache operators: argument checks and launches.
 #include <math.h>
-#include <stdarg.h>
-#include <stdio.h>
 #include <string.h>
 
 #include "sp_cache.cuh"
 #include "sp_gemm.cuh"
+#include "sp_host.cuh"
 
 using namespace sp;
 
 namespace {
-
-sp_status fail(sp_status st, const char *fmt, ...) {
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof buf, fmt, ap);
-    va_end(ap);
-    set_error_text(buf);
-    return st;
-}
-
-sp_status launched(cudaError_t e, const char *what) {
-    return e == cudaSuccess ? SP_OK : fail(SP_ERR_CUDA, "%s: launch failed: %s", what, cudaGetErrorString(e));
-}
-
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-
-// SMs of the current device, asked for once a device (a call's launch path).
-int sm_count() {
-    static int known[MAX_DEVICES] = {};
-    int dev = 0, n = 152;
-    if (cudaGetDevice(&dev) != cudaSuccess) {
-        cudaGetLastError();  // (no device: the host-only checks still answer)
-        return n;
-    }
-    if (dev >= 0 && dev < MAX_DEVICES && known[dev]) return known[dev];
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && dev >= 0 && dev < MAX_DEVICES)
-        known[dev] = n;
-    return n;
-}
 
 // Whether any two of n x m blocks of `width` elements, a and b (>= width) apart, overlap.
 bool blocks_overlap(long long n, long long a, long long m, long long b, long long width) {
@@ -55,8 +24,6 @@ bool blocks_overlap(long long n, long long a, long long m, long long b, long lon
     }
     return false;
 }
-
-bool float_type(int dtype) { return dtype == SP_F32 || dtype == SP_BF16; }
 
 sp_status check_rotary(const sp_rotary *r, RotaryDev *out) {
     if (!r) return fail(SP_ERR_INVALID_ARG, "rotary is NULL");
@@ -144,7 +111,7 @@ sp_status check_copy(const sp_token_cache *cache, int batch, const int *d_seq_id
 }
 
 // Shapes of a tree call; fills what does not depend on the buffers.
-sp_status check_tree(const sp_tree_dims *d, const sp_token_cache *cache, int batch, TreeArgs *a) {
+sp_status check_tree(const sp_tree_dims *d, const sp_token_cache *cache, int batch, bool backward, TreeArgs *a) {
     memset(a, 0, sizeof *a);
     if (!d) return fail(SP_ERR_INVALID_ARG, "dims is NULL");
     sp_status s = check_cache(cache, &a->cache);
@@ -181,11 +148,12 @@ sp_status check_tree(const sp_tree_dims *d, const sp_token_cache *cache, int bat
     a->mask_stride = d->shared_mask ? 0 : a->N;
     const long long paged = (long long)cache->kv.max_pages_per_seq * cache->kv.page_size;
     a->most_len = cache->kv.layout == SP_KV_PAGED && paged < cache->max_seq_len ? (int)paged : cache->max_seq_len;
-    a->tensor = d->path != 1 && tree_tc_supported(*a);
+    a->tensor = d->path != 1 && (backward ? tree_back_tc_supported(*a) : tree_tc_supported(*a));
     if (d->path == 2 && !a->tensor)
-        return fail(SP_ERR_UNSUPPORTED, "the tensor-core kernel needs bf16 rows, a bf16 or 8-bit cache of head_dim 128 "
-                                        "and a batch of at most 2048");
-    if (a->tensor) plan_tree_tc(a, sm_count());
+        return fail(SP_ERR_UNSUPPORTED, "the tensor-core kernel needs bf16 rows, a bf16 %scache of head_dim 128 "
+                                        "and a batch of at most 2048", backward ? "" : "or 8-bit ");
+    if (a->tensor && backward) plan_tree_back_tc(a, sm_count());
+    else if (a->tensor) plan_tree_tc(a, sm_count());
     else plan_tree_simt(a, sm_count());
     return SP_OK;
 }
@@ -197,6 +165,61 @@ size_t tree_o_bytes(const TreeArgs &a) { return align256(tree_rows(a) * a.dh * s
 size_t tree_ml_bytes(const TreeArgs &a) { return align256(tree_rows(a) * 2 * sizeof(float)); }
 size_t tree_bytes(const TreeArgs &a) {
     return tree_o_bytes(a) + tree_ml_bytes(a) + align256((size_t)(a.tensor ? tree_tc_groups(a) : 1) * sizeof(int2));
+}
+
+// Workspace of the backward pass: row statistics, the nodes' part of dq, the shares' parts, the
+// tensor-core kernel's table of shares.
+size_t back_rows(const TreeArgs &a) { return (size_t)a.B * a.Hkv * a.R; }
+size_t back_stat_bytes(const TreeArgs &a) { return align256(back_rows(a) * sizeof(float2)); }
+size_t back_row_bytes(const TreeArgs &a) { return align256(back_rows(a) * a.dh * sizeof(float)); }
+size_t back_part_bytes(const TreeArgs &a) {
+    return align256((a.tensor ? tree_back_tc_slots(a) : tree_back_simt_slots(a)) * a.rb_rows * a.dh * sizeof(float));
+}
+size_t back_bytes(const TreeArgs &a) {
+    return back_stat_bytes(a) + back_row_bytes(a) + back_part_bytes(a) +
+           align256((size_t)(a.tensor ? tree_back_tc_groups(a) : 1) * sizeof(int2));
+}
+
+// What a tree call's buffers have to be, forward and backward.
+sp_status check_tree_buffers(const sp_token_cache *cache, int batch, const int *d_seq_ids, const int *d_seq_lens,
+                             const void *d_q, const void *d_k_new, const void *d_v_new, const void *d_out,
+                             const void *d_workspace) {
+    if (!d_seq_lens || !d_q || !d_k_new || !d_v_new || !d_out || !d_workspace)
+        return fail(SP_ERR_INVALID_ARG, "a required pointer is NULL");
+    if (!d_seq_ids && batch > cache->kv.n_seqs)
+        return fail(SP_ERR_INVALID_ARG, "batch %d exceeds n_seqs %d with implicit ids", batch, cache->kv.n_seqs);
+    if (((uintptr_t)d_workspace) & 255) return fail(SP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    if ((((uintptr_t)d_q) | ((uintptr_t)d_k_new) | ((uintptr_t)d_v_new) | ((uintptr_t)d_out)) & 15)
+        return fail(SP_ERR_INVALID_ARG, "queries, new keys/values and the output must be 16-byte aligned");
+    return SP_OK;
+}
+
+sp_status attend_tree(sp_stream stream, const sp_tree_dims *dims, const sp_token_cache *cache, int batch,
+                      const int *d_seq_ids, const int *d_seq_lens, const uint64_t *d_mask, const int *d_n_nodes,
+                      const void *d_q, const void *d_k_new, const void *d_v_new, void *d_out, float *d_lse,
+                      void *d_workspace, size_t workspace_bytes, int *d_status, const char *name) {
+    TreeArgs a;
+    sp_status s = check_tree(dims, cache, batch, false, &a);
+    if (s != SP_OK) return s;
+    s = check_tree_buffers(cache, batch, d_seq_ids, d_seq_lens, d_q, d_k_new, d_v_new, d_out, d_workspace);
+    if (s != SP_OK) return s;
+    const size_t need = tree_bytes(a);
+    if (workspace_bytes < need) return fail(SP_ERR_INVALID_ARG, "workspace too small (%zu < %zu)", workspace_bytes, need);
+    a.seq_ids = d_seq_ids;
+    a.seq_lens = d_seq_lens;
+    a.n_nodes = d_n_nodes;
+    a.mask = d_mask;
+    a.q = d_q;
+    a.k_new = d_k_new;
+    a.v_new = d_v_new;
+    a.out = d_out;
+    a.lse = d_lse;
+    a.part_o = (float *)d_workspace;
+    a.part_ml = (float *)((char *)d_workspace + tree_o_bytes(a));
+    a.status = d_status;
+    int2 *split_tab = (int2 *)((char *)a.part_ml + tree_ml_bytes(a));
+    return launched(a.tensor ? launch_tree_tc(a, split_tab, (cudaStream_t)stream) : launch_tree_simt(a, (cudaStream_t)stream),
+                    name);
 }
 
 }  // namespace
@@ -320,24 +343,49 @@ sp_status sp_tree_masks(int n_nodes, const int *h_parent, uint64_t *h_mask, int 
 
 size_t sp_attend_tree_workspace_bytes(const sp_tree_dims *dims, const sp_token_cache *cache, int batch) {
     TreeArgs a;
-    return check_tree(dims, cache, batch, &a) == SP_OK ? tree_bytes(a) : 0;
+    return check_tree(dims, cache, batch, false, &a) == SP_OK ? tree_bytes(a) : 0;
 }
 
 sp_status sp_attend_tree(sp_stream stream, const sp_tree_dims *dims, const sp_token_cache *cache, int batch,
                          const int *d_seq_ids, const int *d_seq_lens, const uint64_t *d_mask, const int *d_n_nodes,
                          const void *d_q, const void *d_k_new, const void *d_v_new, void *d_out, void *d_workspace,
                          size_t workspace_bytes, int *d_status) {
+    return attend_tree(stream, dims, cache, batch, d_seq_ids, d_seq_lens, d_mask, d_n_nodes, d_q, d_k_new, d_v_new, d_out,
+                       nullptr, d_workspace, workspace_bytes, d_status, "sp_attend_tree");
+}
+
+sp_status sp_attend_tree_lse(sp_stream stream, const sp_tree_dims *dims, const sp_token_cache *cache, int batch,
+                             const int *d_seq_ids, const int *d_seq_lens, const uint64_t *d_mask, const int *d_n_nodes,
+                             const void *d_q, const void *d_k_new, const void *d_v_new, void *d_out, float *d_lse,
+                             void *d_workspace, size_t workspace_bytes, int *d_status) {
+    if (!d_lse) return fail(SP_ERR_INVALID_ARG, "a required pointer is NULL");
+    if (((uintptr_t)d_lse) & 3) return fail(SP_ERR_INVALID_ARG, "lse must be aligned to its type");
+    return attend_tree(stream, dims, cache, batch, d_seq_ids, d_seq_lens, d_mask, d_n_nodes, d_q, d_k_new, d_v_new, d_out,
+                       d_lse, d_workspace, workspace_bytes, d_status, "sp_attend_tree_lse");
+}
+
+size_t sp_attend_tree_backward_workspace_bytes(const sp_tree_dims *dims, const sp_token_cache *cache, int batch) {
     TreeArgs a;
-    sp_status s = check_tree(dims, cache, batch, &a);
+    return check_tree(dims, cache, batch, true, &a) == SP_OK ? back_bytes(a) : 0;
+}
+
+sp_status sp_attend_tree_backward(sp_stream stream, const sp_tree_dims *dims, const sp_token_cache *cache, int batch,
+                                  const int *d_seq_ids, const int *d_seq_lens, const uint64_t *d_mask, const int *d_n_nodes,
+                                  const void *d_q, const void *d_k_new, const void *d_v_new, const void *d_out,
+                                  const float *d_lse, const void *d_grad_out, void *d_grad_q, void *d_grad_k, void *d_grad_v,
+                                  void *d_workspace, size_t workspace_bytes, int *d_status) {
+    TreeBackArgs x;
+    memset(&x, 0, sizeof x);
+    TreeArgs &a = x.t;
+    sp_status s = check_tree(dims, cache, batch, true, &a);
     if (s != SP_OK) return s;
-    if (!d_seq_lens || !d_q || !d_k_new || !d_v_new || !d_out || !d_workspace)
-        return fail(SP_ERR_INVALID_ARG, "a required pointer is NULL");
-    if (!d_seq_ids && batch > cache->kv.n_seqs)
-        return fail(SP_ERR_INVALID_ARG, "batch %d exceeds n_seqs %d with implicit ids", batch, cache->kv.n_seqs);
-    if (((uintptr_t)d_workspace) & 255) return fail(SP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-    if ((((uintptr_t)d_q) | ((uintptr_t)d_k_new) | ((uintptr_t)d_v_new) | ((uintptr_t)d_out)) & 15)
-        return fail(SP_ERR_INVALID_ARG, "queries, new keys/values and the output must be 16-byte aligned");
-    const size_t need = tree_bytes(a);
+    s = check_tree_buffers(cache, batch, d_seq_ids, d_seq_lens, d_q, d_k_new, d_v_new, d_out, d_workspace);
+    if (s != SP_OK) return s;
+    if (!d_lse || !d_grad_out || !d_grad_q || !d_grad_k || !d_grad_v) return fail(SP_ERR_INVALID_ARG, "a required pointer is NULL");
+    if ((((uintptr_t)d_grad_out) | ((uintptr_t)d_grad_q) | ((uintptr_t)d_grad_k) | ((uintptr_t)d_grad_v)) & 15)
+        return fail(SP_ERR_INVALID_ARG, "gradients must be 16-byte aligned");
+    if (((uintptr_t)d_lse) & 3) return fail(SP_ERR_INVALID_ARG, "lse must be aligned to its type");
+    const size_t need = back_bytes(a);
     if (workspace_bytes < need) return fail(SP_ERR_INVALID_ARG, "workspace too small (%zu < %zu)", workspace_bytes, need);
     a.seq_ids = d_seq_ids;
     a.seq_lens = d_seq_lens;
@@ -346,13 +394,26 @@ sp_status sp_attend_tree(sp_stream stream, const sp_tree_dims *dims, const sp_to
     a.q = d_q;
     a.k_new = d_k_new;
     a.v_new = d_v_new;
-    a.out = d_out;
-    a.part_o = (float *)d_workspace;
-    a.part_ml = (float *)((char *)d_workspace + tree_o_bytes(a));
+    a.out = const_cast<void *>(d_out);
+    a.lse = const_cast<float *>(d_lse);
     a.status = d_status;
-    int2 *split_tab = (int2 *)((char *)a.part_ml + tree_ml_bytes(a));
-    return launched(a.tensor ? launch_tree_tc(a, split_tab, (cudaStream_t)stream) : launch_tree_simt(a, (cudaStream_t)stream),
-                    "sp_attend_tree");
+    x.dout = d_grad_out;
+    x.dq = d_grad_q;
+    x.dk = d_grad_k;
+    x.dv = d_grad_v;
+    x.scale = dims->scale > 0.f ? dims->scale : (float)(1.0 / sqrt((double)cache->head_dim));
+    char *at = (char *)d_workspace;
+    x.stat = (float2 *)at;
+    at += back_stat_bytes(a);
+    x.dq_new = (float *)at;
+    at += back_row_bytes(a);
+    a.part_o = (float *)at;
+    at += back_part_bytes(a);
+    int2 *split_tab = (int2 *)at;
+    const cudaStream_t st = (cudaStream_t)stream;
+    cudaError_t e = launch_tree_back_rows(x, st);
+    if (e == cudaSuccess) e = a.tensor ? launch_tree_back_tc(x, split_tab, st) : launch_tree_back_simt(x, st);
+    return launched(e, "sp_attend_tree_backward");
 }
 
 }  // extern "C"

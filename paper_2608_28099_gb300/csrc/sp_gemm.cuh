@@ -42,6 +42,9 @@ struct TcPlan {
 };
 
 bool encode_kmajor_bf16(CUtensorMap *map, const void *base, int rows, int K, int box_rows);
+// TMA map of rows of `cols` bf16, `stride` elements apart, by boxes of 64 columns x box_rows,
+// 128-byte swizzle, zeros outside.
+bool encode_tile_bf16(CUtensorMap *map, const void *base, long long cols, long long rows, long long stride, int box_rows);
 // TMA map of a paged K or V pool [n_page_heads][page_size][128] bf16 whose box
 // is one (page, head) block in the attention kernel's shared-memory tile layout.
 bool encode_kv_pages_bf16(CUtensorMap *map, const void *pool, long long n_page_heads, int page_size);

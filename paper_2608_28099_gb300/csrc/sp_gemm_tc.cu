@@ -956,6 +956,18 @@ bool encode_kmajor_bf16(CUtensorMap *map, const void *base, int rows, int K, int
     return r == CUDA_SUCCESS;
 }
 
+bool encode_tile_bf16(CUtensorMap *map, const void *base, long long cols, long long rows, long long stride, int box_rows) {
+    PFN_cuTensorMapEncodeTiled_v12000 fn = encode_fn();
+    if (!fn || ((uintptr_t)base & 15) || stride % 8 || cols > 0x7fffffffLL || rows > 0x7fffffffLL) return false;
+    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)stride * 2};
+    cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+    cuuint32_t estr[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool encode_kv_pages_bf16(CUtensorMap *map, const void *pool, long long n_page_heads, int page_size) {
     // pool [n_page_heads][page_size][128] bf16 viewed as (64 dims, 8 rows,
     // 2 dim halves, row groups of 8): one box = one (page, head) block laid out

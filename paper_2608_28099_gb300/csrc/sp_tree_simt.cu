@@ -181,6 +181,7 @@ __global__ void __launch_bounds__(THREADS) tree_simt_kernel(const __grid_constan
                 if (a.dtype == SP_F32) ((float *)a.out)[at + lane + 32 * d] = y;
                 else ((bf16 *)a.out)[at + lane + 32 * d] = __float2bfloat16_rn(y);
             }
+            if (a.lse && lane == 0) store_lse(a, b, node, g * a.G + rr - node * a.G, m[r], live[r] ? l[r] : 0.f);
         } else {
             const size_t slot = ((size_t)b * gridDim.y + hv) * a.n_splits + split, row = slot * a.rb_rows + local;
 #pragma unroll
@@ -226,6 +227,7 @@ __global__ void __launch_bounds__(THREADS) tree_merge_kernel(const __grid_consta
         if (a.dtype == SP_F32) ((float *)a.out)[at + lane + 32 * d] = y;
         else ((bf16 *)a.out)[at + lane + 32 * d] = __float2bfloat16_rn(y);
     }
+    if (a.lse && lane == 0) store_lse(a, b, node, g * a.G + rr - node * a.G, m, live ? l : 0.f);
 }
 
 template <int DH>

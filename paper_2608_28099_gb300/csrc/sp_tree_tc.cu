@@ -934,8 +934,10 @@ __global__ void __launch_bounds__(THREADS, 1)
                     named_sync(BAR_WG + wg, 128);
                 }
             }
-            if (!whole && active && cp == 0 && (MT == 2 || wg == 0))
-                *(float2 *)(a.part_ml + (slot * a.rb_rows + r) * 2) = make_float2(mc, lsum);
+            if (active && cp == 0 && (MT == 2 || wg == 0)) {
+                if (!whole) *(float2 *)(a.part_ml + (slot * a.rb_rows + r) * 2) = make_float2(mc, lsum);
+                else if (a.lse) store_lse(a, b, rr / a.G, g * a.G + rr % a.G, mc, rr / a.G < n ? lsum : 0.f);
+            }
             if (probe != probe) bars->odd_cached = 1;
             tc_fence_before();
             named_sync(BAR_EPI, SOFT);  // both accumulators and ml_s are free, the rows are written
@@ -1510,6 +1512,7 @@ __global__ void __launch_bounds__(MERGE_THREADS) tree_tc_merge_kernel(const __gr
         const float s = on ? 1.f / l : 0.f;
         *(uint2 *)((bf16 *)a.out + ((size_t)b * a.N + node) * a.Hq * DH + (size_t)(g * a.G + rr - node * a.G) * DH + c) =
             on ? make_uint2(pack_bf16(o.x * s, o.y * s), pack_bf16(o.z * s, o.w * s)) : make_uint2(0, 0);
+        if (a.lse && lane == 0) store_lse(a, b, node, g * a.G + rr - node * a.G, m, on ? l : 0.f);
     }
 }
 

@@ -1,0 +1,361 @@
+// The vocabulary loss's products on tcgen05 tensor cores, bf16 with fp32 sums:
+//   LOSS  logits of the kept tokens, whose epilogue leaves each row's (max, sum) over 128 columns
+//   GRAD  the same logits, whose epilogue leaves g = dloss (p - 1_t) in bf16 for a piece of the vocabulary
+//   DH    dh (+)= g W over the piece, fp32 planes
+//   DW    dW = g^T h of the piece, bf16
+// Work: tiles of 256 x 256 by pairs of CTAs (tcgen05.mma.cta_group::2, M = 256: each CTA holds 128
+// rows of A and half of B's 256), K in blocks of 64 through a ring of TMA tiles, two accumulators in
+// TMEM so that the epilogue of one tile runs beside the products of the next; persistent, a pair
+// takes tiles in turn.  The operands lie as their tensors do: K contiguous (K-major) for the logits
+// and for g in DH, the other index contiguous (MN-major) for W in DH and for both in DW; no
+// operand is transposed in memory.  The number of kept tokens is read on the device: ignored tokens
+// cost no product.
+#include <string.h>
+
+#include "sp_gemm.cuh"
+#include "sp_sm100.cuh"
+#include "sp_train.cuh"
+
+namespace sp {
+
+namespace {
+
+using namespace sm100;
+
+enum { LOSS = 0, GRAD = 1, DH = 2, DW = 3 };
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr int TM = 256, TN = 256, BK = 64;       // a pair's tile; a CTA holds 128 x 256 of it
+constexpr int HALF = 128 * BK * 2;               // a CTA's part of an operand's k-block, 16 KB
+constexpr int STAGE = 2 * HALF, STAGES = 6;
+constexpr int OFF_BAR = STAGES * STAGE, SMEM = OFF_BAR + 256 + 1024 /*align*/;
+constexpr int THREADS = 384;                     // warps 0-7 epilogue, 8 TMA, 9 MMA (rank 0), 10 TMEM
+constexpr int TMA = 8, MMA = 9, TMEM = 10, EPI_THREADS = 256;
+constexpr int TMEM_COLS = 2 * TN;
+constexpr long long GRAD_BYTES = 256ll << 20;    // most bytes of a piece's g
+
+template <int KIND>
+struct Kind {
+    static constexpr bool A_MN = KIND == DW, B_MN = KIND == DH || KIND == DW;
+};
+
+// Tiles of a product over `count` kept tokens and `piece` vocabulary rows.
+struct Tiles {
+    int m, n, kb, splits;
+    __device__ __forceinline__ int items() const { return m * n * splits; }
+};
+template <int KIND>
+__device__ __forceinline__ Tiles tiles_of(const VocabArgs &a, int count, int piece, int splits) {
+    Tiles t;
+    t.m = KIND == DW ? ceil_div(piece, TM) : ceil_div(KIND == GRAD ? max(count, 1) : count, TM);
+    t.n = ceil_div(KIND == LOSS || KIND == GRAD ? piece : a.d, TN);
+    // (without a token DW is a product of zeros: k-block 0 of g and h is cleared)
+    t.kb = KIND == DH ? ceil_div(piece, BK) : KIND == DW ? ceil_div(max(count, 1), BK) : ceil_div(a.d, BK);
+    t.splits = splits;
+    return t;
+}
+struct Item {
+    int m0, n0, nt, kb0, nkb, split;
+};
+// Neighbouring pairs take tiles that share what does not stay in L2: rows of the vocabulary (LOSS,
+// GRAD), columns of W (DH); DW walks all of h's columns (which stay) for a tile of g.
+template <int KIND>
+__device__ __forceinline__ Item item_of(const Tiles &t, int it, int kb_per_split) {
+    Item x;
+    int m, n;
+    if (KIND == DW) {
+        n = it % t.n, m = it / t.n;
+        x.split = 0;
+    } else {
+        m = it % t.m;
+        const int q = it / t.m;
+        n = q % t.n, x.split = q / t.n;
+    }
+    x.m0 = m * TM, x.n0 = n * TN, x.nt = n;
+    x.kb0 = x.split * kb_per_split;
+    x.nkb = min(kb_per_split, t.kb - x.kb0);
+    return x;
+}
+
+template <int KIND>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
+    vocab_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                    const __grid_constant__ VocabArgs a, int v0, int splits, int kb_per_split) {
+    typedef Kind<KIND> Ki;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint64_t *full = (uint64_t *)(smem + OFF_BAR);  // rank 0's: both CTAs' copies
+    uint64_t *empty = full + STAGES;
+    uint64_t *acc_full = empty + STAGES;            // [2]
+    uint64_t *acc_empty = acc_full + 2;             // [2], rank 0's: one arrival a CTA
+    uint64_t *fin = acc_empty + 2;
+    uint32_t *tmem_slot = (uint32_t *)(fin + 1);
+    volatile int *abort = (volatile int *)(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int cl = blockIdx.x >> 1, n_cl = gridDim.x >> 1;
+
+    if (warp == TMA && lane == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(&full[s], 1);
+            mbar_init(&empty[s], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&acc_full[i], 1);
+            mbar_init(&acc_empty[i], 2);
+        }
+        mbar_init(fin, 1);
+        *abort = 0;
+        fence_mbar_init();
+        prefetch_tmap(&map_a);
+        prefetch_tmap(&map_b);
+    }
+    __syncwarp();
+    cluster_arrive();  // both CTAs' barriers exist before either signals the other's
+    if (warp == TMEM) tmem_alloc_pair(tmem_slot, TMEM_COLS);
+    cluster_wait();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    pdl_wait();
+    const int piece = min(a.piece, a.V - v0), count = *a.count;
+    const Tiles t = tiles_of<KIND>(a, count, piece, splits);
+    const int n_items = t.items();
+
+    if (warp == TMA && lane == 0) {
+        // what is read again soon stays in L2, the vocabulary's rows of LOSS pass through
+        const uint64_t pol_a = KIND == LOSS || KIND == GRAD ? policy_evict_last() : policy_evict_normal();
+        const uint64_t pol_b = KIND == LOSS ? policy_evict_first() : KIND == DW ? policy_evict_last() : policy_evict_normal();
+        int gi = 0;
+        bool ok = true;
+        for (int it = cl; ok && it < n_items; it += n_cl) {
+            const Item x = item_of<KIND>(t, it, kb_per_split);
+            const int ma = x.m0 + (int)rank * 128, nb = x.n0 + (int)rank * 128;
+            for (int i = 0; i < x.nkb; ++i, ++gi) {
+                const int s = gi % STAGES, k = (x.kb0 + i) * BK;
+                if (gi >= STAGES && !mbar_wait(&empty[s], ((gi / STAGES) & 1) ^ 1, abort)) {
+                    ok = false;
+                    break;
+                }
+                if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * STAGE);
+                const uint32_t bar = map_rank(&full[s], 0);
+                uint8_t *sa = smem + s * STAGE, *sb = sa + HALF;
+                if (Ki::A_MN) {
+                    tma_load_2d_pair(sa, &map_a, bar, ma, k, pol_a);
+                    tma_load_2d_pair(sa + HALF / 2, &map_a, bar, ma + 64, k, pol_a);
+                } else {
+                    tma_load_2d_pair(sa, &map_a, bar, k, ma, pol_a);
+                }
+                if (Ki::B_MN) {
+                    const int kv = KIND == DH ? v0 + k : k;
+                    tma_load_2d_pair(sb, &map_b, bar, nb, kv, pol_b);
+                    tma_load_2d_pair(sb + HALF / 2, &map_b, bar, nb + 64, kv, pol_b);
+                } else {
+                    tma_load_2d_pair(sb, &map_b, bar, k, v0 + nb, pol_b);
+                }
+            }
+        }
+        // nothing may land in this CTA after it is gone
+        for (int j = gi > STAGES ? gi - STAGES : 0; j < gi; ++j)
+            if (!mbar_wait_drain(&empty[j % STAGES], (j / STAGES) & 1)) break;
+    } else if (warp == MMA && lane == 0 && rank == 0) {
+        constexpr uint32_t idesc = idesc_bf16_f32(TM, TN) | (Ki::A_MN ? 1u << 15 : 0u) | (Ki::B_MN ? 1u << 16 : 0u);
+        // a step of 16 along K: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major tile
+        constexpr uint64_t step_a = Ki::A_MN ? 2048 >> 4 : 32 >> 4, step_b = Ki::B_MN ? 2048 >> 4 : 32 >> 4;
+        int gi = 0, n = 0;
+        bool ok = true;
+        for (int it = cl; ok && it < n_items; it += n_cl, ++n) {
+            const Item x = item_of<KIND>(t, it, kb_per_split);
+            const int buf = n & 1;
+            const uint32_t acc = tmem + (uint32_t)(buf * TN);
+            // both CTAs' epilogues have read this accumulator's previous tile
+            if (n >= 2 && !mbar_wait_cluster(&acc_empty[buf], ((n >> 1) - 1) & 1, abort)) break;
+            tc_fence_after();
+            for (int i = 0; i < x.nkb; ++i, ++gi) {
+                const int s = gi % STAGES;
+                if (!mbar_wait(&full[s], (gi / STAGES) & 1, abort)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const uint8_t *sa = smem + s * STAGE, *sb = sa + HALF;
+                const uint64_t da = Ki::A_MN ? sw128_mnmajor_desc(sa, HALF / 2) : sw128_kmajor_desc(sa);
+                const uint64_t db = Ki::B_MN ? sw128_mnmajor_desc(sb, HALF / 2) : sw128_kmajor_desc(sb);
+#pragma unroll
+                for (int kk = 0; kk < BK / 16; ++kk)
+                    mma_bf16_pair(acc, da + step_a * kk, db + step_b * kk, idesc, (i > 0 || kk > 0) ? 1u : 0u);
+                mma_commit_pair(&empty[s]);
+            }
+            if (ok) mma_commit_pair(&acc_full[buf]);
+        }
+        mma_commit_pair(fin);  // every MMA is finished before TMEM and shared memory go away
+        mbar_wait_drain(fin, 0);
+    } else if (warp < 8) {
+        // a row a thread: warp w reads TMEM lanes 32 (w & 3).. and columns 128 (w >> 2)..
+        const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane;
+        int n = 0;
+        for (int it = cl; it < n_items; it += n_cl, ++n) {
+            const Item x = item_of<KIND>(t, it, kb_per_split);
+            const int buf = n & 1, m = x.m0 + (int)rank * 128 + row;
+            VocabRow info{0.f, 0.f, -1, 0};
+            if ((KIND == LOSS || KIND == GRAD) && m < count) info = a.rows[m];
+            const bool have = __all_sync(0xffffffffu, mbar_wait(&acc_full[buf], (n >> 1) & 1, abort));
+            tc_fence_after();
+            if (!have) break;
+            const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * TN + half * 128);
+            const int c0 = x.n0 + half * 128;     // first column
+            float mx = -INFINITY, sum = 0.f;
+#pragma unroll 1
+            for (int c = 0; c < 128; c += 32) {
+                float v[32];
+                __syncwarp();  // (rows that store nothing have skipped ahead)
+                tmem_ld32(at + c, v);
+                if constexpr (KIND == LOSS) {
+                    const int left = piece - (c0 + c);
+                    float top = mx;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        v[j] = j < left ? v[j] * LOG2E : -INFINITY;
+                        top = fmaxf(top, v[j]);
+                    }
+                    const int hit = info.target - (c0 + c);
+                    if (hit >= 0 && hit < 32) {  // (rare: once a row)
+                        float z = 0.f;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z = j == hit ? v[j] : z;
+                        a.at[m] = z;
+                    }
+                    const float mu = top == -INFINITY ? 0.f : top;
+                    sum *= mx == -INFINITY ? 1.f : fast_exp2(mx - mu);
+                    mx = top;
+                    float s4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) s4[j & 3] += fast_exp2(v[j] - mu);
+                    sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                } else if constexpr (KIND == GRAD) {
+                    const int left = m < count ? piece - (c0 + c) : 0, hit = info.target - v0 - (c0 + c);
+                    uint32_t w[16];
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) {
+                        float g[2];
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            const float p = fast_exp2(fmaf(v[j + q], LOG2E, -info.lse2));
+                            g[q] = j + q < left ? (j + q == hit ? p - 1.f : p) * info.g : 0.f;
+                        }
+                        w[j / 2] = pack2_bf16(g[0], g[1]);
+                    }
+                    uint4 *to = (uint4 *)((bf16 *)a.grad + (size_t)m * a.piece + c0 + c);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) to[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+                } else if constexpr (KIND == DH) {
+                    if (m >= count) continue;
+                    float *to = a.acc + ((size_t)x.split * a.n + m) * a.d + c0 + c;
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) {
+                        if (c0 + c + j >= a.d) break;
+                        float4 y = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                        if (v0) {
+                            const float4 z = *(const float4 *)(to + j);
+                            y.x += z.x, y.y += z.y, y.z += z.z, y.w += z.w;
+                        }
+                        *(float4 *)(to + j) = y;
+                    }
+                } else {
+                    if (m >= piece) continue;
+                    bf16 *to = (bf16 *)a.dw + (size_t)(v0 + m) * a.ws + c0 + c;
+#pragma unroll
+                    for (int j = 0; j < 32; j += 8) {
+                        if (c0 + c + j >= a.d) break;
+                        *(uint4 *)(to + j) = make_uint4(pack2_bf16(v[j], v[j + 1]), pack2_bf16(v[j + 2], v[j + 3]),
+                                                        pack2_bf16(v[j + 4], v[j + 5]), pack2_bf16(v[j + 6], v[j + 7]));
+                    }
+                }
+            }
+            if (KIND == LOSS && m < count) a.part[(size_t)m * a.parts + 2 * x.nt + half] = make_float2(mx, sum);
+            tc_fence_before();
+            asm volatile("bar.sync 1, %0;" ::"n"(EPI_THREADS) : "memory");
+            if (threadIdx.x == 0) mbar_arrive_remote(map_rank(&acc_empty[buf], 0));
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    pdl_trigger();
+    if (threadIdx.x == 0 && *abort && a.status) atomicOr(a.status, SP_DEV_TIMEOUT);
+    // rank 0's last commit arrives on both CTAs' barriers: each waits until it has landed
+    if (threadIdx.x == 0 && rank != 0) mbar_wait_drain(fin, 0);
+    __syncwarp();
+    cluster_sync();  // no signal or MMA of the other CTA may still target this one
+    if (warp == TMEM) tmem_dealloc_pair(tmem, TMEM_COLS);
+}
+
+template <int KIND>
+cudaError_t run(const VocabArgs &a, const CUtensorMap &ma, const CUtensorMap &mb, int v0, int n_sm, cudaStream_t st) {
+    static bool known[MAX_DEVICES] = {};
+    const cudaError_t e = allow_smem(vocab_tc_kernel<KIND>, SMEM, known);
+    if (e != cudaSuccess) return e;
+    const int piece = a.V - v0 < a.piece ? a.V - v0 : a.piece;
+    const long long m = KIND == DW ? ceil_div(piece, TM) : a.pad / TM, n = ceil_div(KIND == LOSS || KIND == GRAD ? piece : a.d, TN);
+    const int kb = ceil_div(KIND == DH ? piece : a.d, BK), splits = KIND == DH ? a.planes : 1;
+    const int per = KIND == DW ? 0x7fffffff : ceil_div(kb, splits);
+    const long long items = m * n * splits;
+    const int pairs = n_sm / 2 > 0 ? n_sm / 2 : 1;
+    return launch_k(vocab_tc_kernel<KIND>, dim3(2 * (items < pairs ? (unsigned)items : (unsigned)pairs)), dim3(THREADS), (size_t)SMEM,
+                    st, ma, mb, a, v0, splits, per);
+}
+
+}  // namespace
+
+bool vocab_tc_supported(const VocabArgs &a) {
+    return a.dtype == SP_BF16 && a.d % 8 == 0 && a.hs % 8 == 0 && a.ws % 8 == 0;
+}
+
+void plan_vocab_tc(VocabArgs *a, bool backward, int n_sm) {
+    a->pad = ceil_div(a->n, TM) * TM;
+    a->planes = 1;
+    const int tiles = ceil_div(a->V, TN);
+    a->parts = 2 * tiles;
+    a->piece = tiles * TN;
+    a->n_pieces = 1;
+    if (!backward) return;
+    long long most = GRAD_BYTES / 2 / a->pad / TN;  // tiles of a piece
+    if (most < 1) most = 1;
+    a->n_pieces = (int)ceil_div_ll(tiles, most);
+    a->piece = ceil_div(tiles, a->n_pieces) * TN;
+    a->n_pieces = ceil_div(a->V, a->piece);
+    // few tiles of dh: K is split over the pairs that would be idle
+    const long long t = (long long)(a->pad / TM) * ceil_div(a->d, TN);
+    const int pairs = n_sm / 2 > 0 ? n_sm / 2 : 1, kb = a->piece / BK;
+    int s = t < pairs ? (int)(pairs / t) : 1;
+    if (s > kb / 8) s = kb / 8 > 0 ? kb / 8 : 1;
+    // no split may be empty, of the last, shorter piece neither
+    const int last_kb = ceil_div(a->V - (a->n_pieces - 1) * a->piece, BK);
+    while (s > 1 && ((s - 1) * ceil_div(kb, s) >= kb || (s - 1) * ceil_div(last_kb, s) >= last_kb)) --s;
+    a->planes = s;
+}
+
+cudaError_t launch_vocab_loss_tc(const VocabArgs &a, int n_sm, cudaStream_t st) {
+    CUtensorMap mh, mw;
+    if (!encode_tile_bf16(&mh, a.hc, a.d, a.pad, a.d, 128) || !encode_tile_bf16(&mw, a.w, a.d, a.V, a.ws, 128))
+        return cudaErrorInvalidValue;
+    return run<LOSS>(a, mh, mw, 0, n_sm, st);
+}
+
+cudaError_t launch_vocab_backward_tc(const VocabArgs &a, int n_sm, cudaStream_t st) {
+    CUtensorMap mh, mw, mg, mwt, mgt, mht;
+    if (!encode_tile_bf16(&mh, a.hc, a.d, a.pad, a.d, 128) || !encode_tile_bf16(&mw, a.w, a.d, a.V, a.ws, 128) ||
+        !encode_tile_bf16(&mg, a.grad, a.piece, a.pad, a.piece, 128) || !encode_tile_bf16(&mwt, a.w, a.d, a.V, a.ws, 64) ||
+        !encode_tile_bf16(&mgt, a.grad, a.piece, a.pad, a.piece, 64) || !encode_tile_bf16(&mht, a.hc, a.d, a.pad, a.d, 64))
+        return cudaErrorInvalidValue;
+    for (int i = 0; i < a.n_pieces; ++i) {
+        const int v0 = i * a.piece;
+        cudaError_t e = run<GRAD>(a, mh, mw, v0, n_sm, st);
+        if (e == cudaSuccess) e = run<DH>(a, mg, mwt, v0, n_sm, st);
+        if (e == cudaSuccess && a.dw) e = run<DW>(a, mgt, mht, v0, n_sm, st);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace sp
