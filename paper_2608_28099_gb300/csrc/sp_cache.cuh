@@ -200,10 +200,10 @@ cudaError_t launch_tree_back_rows(const TreeBackArgs &a, cudaStream_t st);
 cudaError_t launch_tree_back_simt(const TreeBackArgs &a, cudaStream_t st);
 size_t tree_back_simt_slots(const TreeArgs &a);
 // The same on tensor cores: head_dim 128, bf16 rows and cache, B <= 2048.
-inline bool tree_back_tc_supported(const TreeArgs &) { return false; }
-inline void plan_tree_back_tc(TreeArgs *, int) {}
-inline size_t tree_back_tc_slots(const TreeArgs &) { return 0; }
-inline int tree_back_tc_groups(const TreeArgs &) { return 0; }
-inline cudaError_t launch_tree_back_tc(const TreeBackArgs &, int2 *, cudaStream_t) { return cudaErrorInvalidValue; }
+bool tree_back_tc_supported(const TreeArgs &a);
+void plan_tree_back_tc(TreeArgs *a, int n_sm);
+size_t tree_back_tc_slots(const TreeArgs &a);
+int tree_back_tc_groups(const TreeArgs &a);
+cudaError_t launch_tree_back_tc(const TreeBackArgs &a, int2 *split_tab, cudaStream_t st);
 
 }  // namespace sp

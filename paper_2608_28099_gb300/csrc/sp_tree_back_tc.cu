@@ -1,0 +1,704 @@
+// The cache's part of the backward pass of tree attention (sp_tree_back.cu) on tcgen05 tensor
+// cores: head_dim 128, bf16 rows and cache.  Per key tile of 64 cached tokens and block of up to 128
+// query rows of a kv head, rows on the MMA's M side:
+//   S = Q K^T, dP = dO V^T   128 x 64 each, all operands in shared memory
+//   ds = p (dP - D)          p = exp(scale S - lse), a row a thread, written as bf16 over S in TMEM
+//   dQ += ds K               from TMEM; K is read a second time where it lies (MN-major)
+// The log sums are known, so that a tile's weights are final: nothing is rescaled, two softmax
+// warpgroups take alternate tiles into one accumulator, and parts of dQ are sums.
+//
+// Work: the cached tokens of every sequence are cut into tiles, the list of all tiles into shares (as
+// in sp_attn_plan.cuh), CTA (share, kv head, row block) walks its share; its piece of a sequence is
+// a segment.  A pair that lies inside one share is finished there (with the nodes' part, formed by the
+// kernel in front), the others leave partials that a second kernel adds in share order.
+//
+// Warps 0-7 softmax; 8-11 load queries and output gradients and write dQ out, two accumulators of
+// which alternate between segments; 12 MMA issuer and TMEM; 13-14 K, 15-16 V (TMA boxes of whole
+// pages, cp.async elsewhere).  TMEM: [S dP] x 2 in columns 0-255, dQ x 2 behind.  Every wait is
+// time-limited (SP_DEV_TIMEOUT).
+#include <string.h>
+
+#include "sp_attn_plan.cuh"
+#include "sp_cache.cuh"
+#include "sp_gemm.cuh"
+
+namespace sp {
+
+namespace {
+
+constexpr int TILE = 64;
+constexpr int SLOT = TILE * DH * 2;             // K or V of a tile, 16 KB
+constexpr int A_TILE = 128 * DH * 2;            // an M tile of queries or output gradients, 32 KB
+constexpr int A_HALF = A_TILE / 2;              // its 64-dim halves
+constexpr int ROWS = 128;                       // most rows of a block
+constexpr int MAX_RING = 8;
+constexpr int SMEM_MAX = 227 * 1024;
+constexpr int THREADS = 544;
+constexpr int EPI = 8, MMA = 12, K_WARP = 13, V_WARP = 15;
+constexpr uint32_t Q_COL = 256;                 // TMEM: dQ accumulators
+// Fewest tiles a share holds on average, and the cost of a segment in tiles.
+constexpr int kBackMinTiles = 4;
+constexpr int kBackSegCost = 4;
+
+struct Layout {
+    int nk, nv;                                 // ring slots
+    int n_q;                                    // buffers of queries: 2 up to 64 rows
+    int off_q, off_do, off_k, off_v, off_tab;
+    int smem;
+};
+struct Bars {
+    uint64_t k_full[MAX_RING], k_empty[MAX_RING], v_full[MAX_RING], v_empty[MAX_RING];
+    uint64_t s_full[2], p_full[2], q_full[2], q_empty[2], dq_full[2], dq_empty[2], fin;
+    uint32_t tmem;
+    int abort;
+    int wsum[32];
+};
+constexpr int OFF_CUTS = 1024;
+constexpr int OFF_FRONT = OFF_CUTS + (MAX_GRP + 4) * 4;
+static_assert(sizeof(Bars) <= OFF_CUTS, "barrier block");
+
+__device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort) {
+    return mbar_wait_warp(bar, parity, abort);
+}
+__device__ __forceinline__ void arrive_warp(uint64_t *bar, int lane) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar);
+}
+__device__ __forceinline__ void expect_tx(uint64_t *bar, uint32_t bytes) {
+    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void ld32_async(uint32_t addr, float *v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
+          "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]),
+          "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]),
+          "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+        : "r"(addr));
+}
+// Earlier loads complete; these 32 values are named so that no use moves in front.
+__device__ __forceinline__ void ld_wait(float *v) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                   "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14])
+                 :
+                 : "memory");
+    asm volatile(""
+                 : "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]),
+                   "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]));
+    asm volatile("" : "+f"(v[29]), "+f"(v[30]), "+f"(v[31]));
+}
+__device__ __forceinline__ void st16_async(uint32_t addr, const uint32_t *v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+        "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+__device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// The tile list: prefix[b] = tiles of the sequences before b (one for an empty sequence), each
+// sequence's cache id, length and node count.  By all THREADS threads.
+__device__ __forceinline__ void back_prefix(const TreeArgs &a, int *prefix, int *sids, int *lens, int *nodes, int *wsum,
+                                            int *status) {
+    const int B = a.B, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int per = (B + THREADS - 1) / THREADS;
+    const int b0 = min(B, (int)threadIdx.x * per), b1 = min(B, b0 + per);
+    int sum = 0;
+#pragma unroll 1
+    for (int b = b0; b < b1; ++b) {
+        const int n = a.n_nodes ? a.n_nodes[b] : a.N;  // (asked for beside the length)
+        const SeqRef sq = resolve_seq(a.seq_ids, a.seq_lens, 0, b, a.cache.kv.n_seqs, a.most_len, status);
+        sids[b] = sq.sid;
+        lens[b] = sq.len;
+        nodes[b] = checked_nodes(a, n, nullptr);
+        const int v = max(1, ceil_div(sq.len, TILE));
+        prefix[b] = v;
+        sum += v;
+    }
+    int incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) wsum[warp] = incl;
+    __syncthreads();
+    int run = incl - sum, tot = 0;
+#pragma unroll 1
+    for (int w = 0; w < THREADS / 32; ++w) {
+        if (w < warp) run += wsum[w];
+        tot += wsum[w];
+    }
+#pragma unroll 1
+    for (int b = b0; b < b1; ++b) {
+        const int v = prefix[b];
+        prefix[b] = run;
+        run += v;
+    }
+    if (threadIdx.x == 0) prefix[B] = tot;
+    __syncthreads();
+}
+
+struct Ring {
+    int n, slot = 0;
+    uint32_t ph = 0;
+    __device__ __forceinline__ explicit Ring(int slots) : n(slots) {}
+    __device__ __forceinline__ void next() {
+        if (++slot == n) {
+            slot = 0;
+            ph ^= 1;
+        }
+    }
+};
+// A CTA's share: tiles [x0, x1) of the list, pieces of sequences [b0, b1).
+struct Share {
+    const int *prefix;
+    int x0, x1, b0, b1;
+};
+__device__ __forceinline__ Seg piece(const Share &sh, int b) {
+    const int p0 = sh.prefix[b], p1 = sh.prefix[b + 1], lo = max(p0, sh.x0);
+    Seg s;
+    s.b = b;
+    s.xp = p0;
+    s.nt = p1 - p0;
+    s.t_a = lo - p0;
+    s.n = min(p1, sh.x1) - lo;
+    return s;
+}
+// Where a walk over the share's tiles stands: tile i of segment j (sequence b0 + j).
+struct Walk {
+    const Share &sh;
+    Seg sg;
+    int j = 0, i = 0;
+    __device__ __forceinline__ explicit Walk(const Share &s) : sh(s) { sg = piece(sh, sh.b0); }
+    __device__ __forceinline__ bool first() const { return i == 0; }
+    __device__ __forceinline__ bool last() const { return i == sg.n - 1; }
+    __device__ __forceinline__ void next() {
+        if (++i < sg.n) return;
+        i = 0;
+        if (sh.b0 + ++j < sh.b1) sg = piece(sh, sh.b0 + j);
+    }
+};
+
+// Queries and output gradients of sequence b into the A operands, rows [r0, r0 + rows) of the tiles;
+// zeros for rows of nodes that are not there.  16 lanes a row, four rows of each under way together.
+__device__ __forceinline__ void load_rows(const TreeBackArgs &x, int b, int n, int g, int rb, uint8_t *Q, uint8_t *dO, int r0,
+                                          int wi, int lane) {
+    const TreeArgs &a = x.t;
+    const int c = lane & 15;
+    constexpr int AT_ONCE = 4;
+#pragma unroll 1
+    for (int r1 = wi * 2 + (lane >> 4); r1 < a.rb_rows; r1 += AT_ONCE * 8) {
+        uint4 q[AT_ONCE], go[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int r = r1 + k * 8, rr = rb * a.rb_rows + r, node = rr / a.G;
+            q[k] = go[k] = make_uint4(0, 0, 0, 0);
+            if (r < a.rb_rows && rr < a.R && node < n) {
+                const size_t head = (size_t)(g * a.G + rr - node * a.G) * DH + c * 8, row = (size_t)b * a.N + node;
+                q[k] = *(const uint4 *)((const bf16 *)a.q + row * a.qs + head);
+                go[k] = *(const uint4 *)((const bf16 *)x.dout + row * a.Hq * DH + head);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int r = r0 + r1 + k * 8;
+            if (r1 + k * 8 >= a.rb_rows) break;
+            const uint32_t at = (uint32_t)((c >> 3) * A_HALF + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+            st_shared_v4(Q + at, q[k].x, q[k].y, q[k].z, q[k].w);
+            st_shared_v4(dO + at, go[k].x, go[k].y, go[k].z, go[k].w);
+        }
+    }
+    fence_proxy_async();  // -> tensor-core reads
+}
+
+__global__ void __launch_bounds__(THREADS, 1)
+    tree_back_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                        const __grid_constant__ TreeBackArgs args, const __grid_constant__ Layout lay, int2 *split_tab) {
+    const TreeArgs &a = args.t;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    Bars *bars = (Bars *)smem;
+    int *cuts = (int *)(smem + OFF_CUTS);
+    volatile int *abort = &bars->abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int B = a.B, Hkv = a.Hkv, Hv = Hkv * a.n_rb;
+    int *prefix = (int *)(smem + lay.off_tab), *sids = prefix + B + 1, *lens = sids + B, *nodes = lens + B;
+    const bool paged = a.cache.kv.layout == SP_KV_PAGED;
+    const int P = a.cache.kv.page_size, P_bits = 31 - __clz(max(P, 1));
+    constexpr int ROW = DH * 2;
+    // The kernel in front of this one has waited for the caller's earlier work before it let this one
+    // start: lengths, counts, queries and the cache may be read; its own results only behind the wait.
+    back_prefix(a, prefix, sids, lens, nodes, bars->wsum, blockIdx.x == 0 ? a.status : nullptr);
+    const int T = prefix[B];
+    const int n_grp = share_count((int)gridDim.x / Hv, T, B, a.plan.tc_min_tiles);
+    const int grp = blockIdx.x / Hv, hv = blockIdx.x - grp * Hv, g = hv / a.n_rb, rb = hv - g * a.n_rb;
+    if (grp >= n_grp) return;  // uniform over the CTA: no share
+    if (threadIdx.x < PLAN_THREADS) build_cuts(a.plan, prefix, T, n_grp, cuts, bars->wsum);
+    if (threadIdx.x == THREADS - 1) {
+#pragma unroll 1
+        for (int i = 0; i < lay.nk; ++i) {
+            mbar_init(&bars->k_full[i], 64);
+            mbar_init(&bars->k_empty[i], 1);
+        }
+#pragma unroll 1
+        for (int i = 0; i < lay.nv; ++i) {
+            mbar_init(&bars->v_full[i], 64);
+            mbar_init(&bars->v_empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&bars->s_full[i], 1);
+            mbar_init(&bars->p_full[i], 4);
+            mbar_init(&bars->q_full[i], 4);
+            mbar_init(&bars->q_empty[i], 1);
+            mbar_init(&bars->dq_full[i], 1);
+            mbar_init(&bars->dq_empty[i], 4);
+        }
+        mbar_init(&bars->fin, 1);
+        bars->abort = 0;
+        fence_mbar_init();
+        if (paged) {
+            prefetch_tmap(&map_k);
+            prefetch_tmap(&map_v);
+        }
+    }
+    if (warp == MMA) {
+        tmem_alloc(&bars->tmem, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = bars->tmem;
+    Share sh{prefix, cuts[grp], cuts[grp + 1], 0, 0};
+    if (sh.x0 < sh.x1) {
+        sh.b0 = seg_at(prefix, B, sh.x0, sh.x1).b;
+        sh.b1 = seg_at(prefix, B, sh.x1 - 1, sh.x1).b + 1;
+    }
+    const int n_tiles = max(sh.x1 - sh.x0, 0);
+    if (blockIdx.x == 0) {  // for the merge: the sequence that goes on behind the share where it starts, its shares
+#pragma unroll 1
+        for (int j = threadIdx.x; j < (int)gridDim.x / Hv; j += THREADS) {
+            int2 t = make_int2(0, 0);
+            if (j < n_grp && cuts[j] < cuts[j + 1]) {
+                const int b = seg_at(prefix, B, cuts[j + 1] - 1, T).b;
+                if (prefix[b] >= cuts[j]) t = make_int2(b, group_of(cuts, n_grp, prefix[b + 1] - 1) - j + 1);
+            }
+            split_tab[j] = t;
+        }
+    }
+
+    if (warp < 8) {
+        // ------------------------------------------------------------ weights and their gradients
+        const int w = warp >> 2, r = threadIdx.x & 127;  // tiles of this parity; row, TMEM lane
+        const int rr = rb * a.rb_rows + r;
+        const bool active = r < a.rb_rows && rr < a.R;
+        const bool warp_active = __any_sync(0xffffffffu, active);
+        const uint32_t s_col = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(w * 128);
+        pdl_wait();  // the row statistics
+        bool ok = true;
+        uint32_t ph = 0;
+        int at = 0;  // tiles in front of the segment
+#pragma unroll 1
+        for (int b = sh.b0; ok && b < sh.b1; ++b) {
+            const Seg sg = piece(sh, b);
+            const int left = lens[b] - sg.t_a * TILE;
+            float2 st = make_float2(INFINITY, 0.f);
+            if (active) st = __ldcg(args.stat + ((size_t)b * Hkv + g) * a.R + rr);
+#pragma unroll 1
+            for (int i = (at + w) & 1; i < sg.n; i += 2) {
+                ok = ok && wait_warp(&bars->s_full[w], ph, abort);
+                ph ^= 1;
+                if (!ok) break;
+                tc_fence_after();
+                if (warp_active) {
+                    const int n_tok = left - i * TILE;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float s[32], d[32];
+                        ld32_async(s_col + c * 32, s);
+                        ld32_async(s_col + 64 + c * 32, d);
+                        ld_wait(s);
+                        ld_wait(d);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const float p = fast_exp2(fmaf(s[e], a.scale_log2, -st.x));
+                            s[e] = p * (d[e] - st.y);
+                        }
+                        if (n_tok < TILE) {  // past the end: what was loaded there is nothing
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (c * 32 + e >= n_tok) s[e] = 0.f;
+                        }
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) pk[e] = pack_bf16(s[2 * e], s[2 * e + 1]);
+                        st16_async(s_col + c * 16, pk);  // over scores that this warp has read
+                    }
+                    st_wait();
+                }
+                tc_fence_before();
+                arrive_warp(&bars->p_full[w], lane);
+            }
+            at += sg.n;
+        }
+    } else if (warp < MMA) {
+        // ------------------------------------------------------------ queries in, dQ out
+        const int quad = warp - EPI, r = quad * 32 + lane, rr = rb * a.rb_rows + r;
+        const bool active = r < a.rb_rows && rr < a.R;
+        const bool warp_active = __any_sync(0xffffffffu, active);
+        const uint32_t lane_base = tmem + ((uint32_t)(quad * 32) << 16) + Q_COL;
+        const int n_seg = sh.b1 - sh.b0;
+        const auto load = [&](int j) {
+            const int buf = lay.n_q == 2 ? j & 1 : 0, use = lay.n_q == 2 ? j >> 1 : j;
+            if (!wait_warp(&bars->q_empty[buf], (use & 1) ^ 1, abort)) return false;
+            const int b = sh.b0 + j;
+            load_rows(args, b, nodes[b], g, rb, smem + lay.off_q, smem + lay.off_do, buf * 64, quad, lane);
+            arrive_warp(&bars->q_full[buf], lane);
+            return true;
+        };
+        bool ok = n_seg == 0 || load(0);
+        pdl_wait();  // the nodes' part of dQ; nothing is written before
+#pragma unroll 1
+        for (int j = 0; ok && j < n_seg; ++j) {
+            if (j + 1 < n_seg) ok = load(j + 1);
+            const int b = sh.b0 + j, buf = j & 1;
+            const Seg sg = piece(sh, b);
+            const int n = nodes[b];
+            const int j_first = group_of(cuts, n_grp, sg.xp), j_last = group_of(cuts, n_grp, sg.xp + sg.nt - 1);
+            const bool whole = j_first == j_last;
+            const size_t slot = ((size_t)grp * 2 + (j_first == grp)) * Hv + hv;
+            const int node = rr / a.G;
+            const size_t row = ((size_t)b * Hkv + g) * a.R + rr;
+            bool live = false;
+            if (active && whole) live = node < n && __ldcg(&args.stat[row].x) != INFINITY;
+            ok = ok && wait_warp(&bars->dq_full[buf], (j >> 1) & 1, abort);
+            if (!ok) break;
+            tc_fence_after();
+            if (warp_active) {
+#pragma unroll 1
+                for (int d = 0; d < DH; d += 32) {
+                    float v[32];
+                    __syncwarp();
+                    ld32_async(lane_base + (uint32_t)(buf * DH + d), v);
+                    ld_wait(v);
+                    if (!active) continue;
+                    if (whole) {
+                        bf16 *to = (bf16 *)args.dq + ((size_t)b * a.N + node) * a.qs + (size_t)(g * a.G + rr - node * a.G) * DH + d;
+                        const float4 *more = (const float4 *)(args.dq_new + row * DH + d);
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8) {
+                            const float4 x = __ldcg(more + e / 4), y = __ldcg(more + e / 4 + 1);
+                            const float f = args.scale;
+                            *(uint4 *)(to + e) = live ? make_uint4(pack_bf16((v[e] + x.x) * f, (v[e + 1] + x.y) * f),
+                                                                   pack_bf16((v[e + 2] + x.z) * f, (v[e + 3] + x.w) * f),
+                                                                   pack_bf16((v[e + 4] + y.x) * f, (v[e + 5] + y.y) * f),
+                                                                   pack_bf16((v[e + 6] + y.z) * f, (v[e + 7] + y.w) * f))
+                                                      : make_uint4(0, 0, 0, 0);
+                        }
+                    } else {
+                        float *to = a.part_o + (slot * a.rb_rows + r) * DH + d;
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4) *(float4 *)(to + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                    }
+                }
+            }
+            tc_fence_before();
+            arrive_warp(&bars->dq_empty[buf], lane);
+        }
+    } else if (warp >= K_WARP) {
+        // ------------------------------------------------------------ K and V
+        const bool is_v = warp >= V_WARP;
+        const int pidx = warp - (is_v ? V_WARP : K_WARP), ptid = pidx * 32 + lane;
+        const bool lead = pidx == 0;
+        uint64_t *full = is_v ? bars->v_full : bars->k_full, *empty = is_v ? bars->v_empty : bars->k_empty;
+        uint8_t *ring = smem + (is_v ? lay.off_v : lay.off_k);
+        const CUtensorMap *map = is_v ? &map_v : &map_k;
+        const uint8_t *pool = (const uint8_t *)(is_v ? a.cache.kv.v_pool : a.cache.kv.k_pool);
+        const uint64_t pol = policy_evict_first();
+        Ring rg(is_v ? lay.nv : lay.nk);
+        int bad = 0, filled = 0;
+        bool stop = false;
+#pragma unroll 1
+        for (int b = sh.b0; b < sh.b1 && !stop; ++b) {
+            const Seg sg = piece(sh, b);
+            const int sid = sids[b], L = lens[b];
+            const uint8_t *seq = nullptr;  // a contiguous sequence's rows of head g, a token apart
+            if (!paged && L > 0)
+                seq = (const uint8_t *)(is_v ? a.cache.kv.v_seq : a.cache.kv.k_seq)[sid] + (size_t)g * ROW;
+            const size_t seq_step = (size_t)Hkv * ROW;
+#pragma unroll 1
+            for (int i = 0; i < sg.n; ++i) {
+                const int t0 = (sg.t_a + i) * TILE, n_tok = min(TILE, L - t0);
+                const int n_pg = paged ? n_tok >> P_bits : 0;  // whole pages
+                int page = -1;                                 // ids, asked for before the wait
+                if (paged && lane * P < n_tok) {
+                    const int lp = (t0 >> P_bits) + lane;
+                    page = lp < a.cache.kv.max_pages ? __ldg(a.cache.kv.page_table + (size_t)sid * a.cache.kv.max_pages + lp) : -1;
+                    if (page < 0 || page >= a.cache.kv.n_pages) page = -1, bad = 1;
+                }
+                // warp-uniform verdict: the collectives below need every lane
+                if (!wait_warp(&empty[rg.slot], rg.ph ^ 1, abort)) {
+                    stop = true;
+                    break;
+                }
+                uint8_t *dst = ring + rg.slot * SLOT;
+                bool plain = false;  // this thread wrote shared memory or issued cp.async
+                if (n_pg > 0 && lead) {
+                    const bool have = lane < n_pg && page >= 0;
+                    const unsigned okm = __ballot_sync(0xffffffffu, have);
+                    if (lane == 0 && okm) expect_tx(&full[rg.slot], __popc(okm) * P * ROW);
+                    __syncwarp();
+                    if (have)  // the cache is read once: evict-first keeps queries and partials in L2
+                        tma_load_4d_hint(dst + lane * P * ROW, map, &full[rg.slot], 0, 0, 0, (page * Hkv + g) * (P / 8), pol);
+#pragma unroll 1
+                    for (unsigned miss = ~okm & ((1u << n_pg) - 1u); miss; miss &= miss - 1) {  // zeros
+                        const int j = __ffs(miss) - 1;
+#pragma unroll 1
+                        for (int e = lane; e < P * ROW / 16; e += 32) st_shared_v4(dst + j * P * ROW + e * 16, 0, 0, 0, 0);
+                        plain = true;
+                    }
+                }
+                const int r0 = n_pg * (paged ? P : 0);  // first row not covered by TMA
+                if (r0 < n_tok) {
+                    plain = true;
+                    const uint8_t *src = seq + (size_t)t0 * seq_step;
+                    size_t step = seq_step;
+                    bool have = true;
+                    if (paged) {  // the last, partial page
+                        const int pg = __shfl_sync(0xffffffffu, page, n_pg);
+                        have = pg >= 0;
+                        src = pool + ((size_t)max(pg, 0) * Hkv + g) * P * ROW;
+                        step = ROW;
+                    }
+                    const int c = ptid & 15, r1 = ptid >> 4;
+                    src += (size_t)r1 * step + c * 16;
+#pragma unroll 4
+                    for (int r = r1; r < n_tok - r0; r += 4, src += 4 * step) {
+                        uint8_t *d = dst + kv_off(r0 + r, c);
+                        if (have) cp_async16(d, src);
+                        else st_shared_v4(d, 0, 0, 0, 0);
+                    }
+                }
+                if (n_tok < TILE) {  // rows past the end meet gradients of 0: they must be finite
+                    plain = true;
+                    const int from = max(n_tok, 0);
+#pragma unroll 1
+                    for (int idx = ptid; idx < (TILE - from) * 16; idx += 64)
+                        st_shared_v4(dst + kv_off(from + (idx >> 4), idx & 15), 0, 0, 0, 0);
+                }
+                if (plain) {
+                    fence_proxy_async();  // this thread's shared-memory stores
+                    cp_async_mbar_arrive(&full[rg.slot]);
+                } else {
+                    mbar_arrive(&full[rg.slot]);
+                }
+                ++filled;
+                rg.next();
+            }
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");  // nothing lands after the CTA is gone
+        if (lead && lane == 0) {
+            // drain copies still in flight (only possible after an abort)
+            Ring rd(rg.n);
+#pragma unroll 1
+            for (int j = 0; j < filled; ++j, rd.next())
+                if (j + rg.n >= filled) mbar_wait_drain(&full[rd.slot], rd.ph);
+        }
+        bad = __any_sync(0xffffffffu, bad);
+        if (bad && lane == 0 && a.status) atomicOr(a.status, SP_DEV_BAD_PAGE);
+    } else {
+        // ------------------------------------------------------------ MMA issue
+        // S and dP run up to two tiles ahead of dQ, into the buffer that the softmax of two tiles
+        // before has read (its gradients are in front of it in the pipe).  One issuer sees every use
+        // of every slot in order.
+        const bool on = elect_one();
+        constexpr uint32_t idesc_s = idesc_bf16_f32(128, TILE), idesc_q = idesc_bf16_f32_bmn(128, DH);
+        const uint64_t dq0 = sw128_kmajor_desc(smem + lay.off_q), do0 = sw128_kmajor_desc(smem + lay.off_do);
+        const uint64_t dk0 = sw128_kmajor_desc_sbo(smem + lay.off_k, GROUP_STRIDE);
+        const uint64_t dv0 = sw128_kmajor_desc_sbo(smem + lay.off_v, GROUP_STRIDE);
+        const uint64_t dkt0 = sw128_mnmajor_desc2(smem + lay.off_k, HALF_STRIDE, GROUP_STRIDE);
+        Ring rk(lay.nk), rv(lay.nv), rk2(lay.nk);  // of S, of dP, of dQ
+        uint32_t p_ph = 0;                         // phases of p_full, a bit a buffer
+        bool ok = n_tiles > 0;
+        if (ok) {
+            Walk in(sh), out(sh);
+            int ahead = 0;  // tiles whose S is issued, whose dQ is not
+            int issued = 0, done = 0;
+#pragma unroll 1
+            while (ok && done < n_tiles) {
+#pragma unroll 1
+                while (ok && issued < n_tiles && ahead < 2) {
+                    const int qb = lay.n_q == 2 ? in.j & 1 : 0, use = lay.n_q == 2 ? in.j >> 1 : in.j;
+                    if (in.first()) {
+                        // (queries that are not there yet do not hold up the tiles under way)
+                        if (ahead > 0 && !__all_sync(0xffffffffu, mbar_try_wait(&bars->q_full[qb], use & 1))) break;
+                        ok = wait_warp(&bars->q_full[qb], use & 1, abort);
+                    }
+                    ok = ok && wait_warp(&bars->k_full[rk.slot], rk.ph, abort) && wait_warp(&bars->v_full[rv.slot], rv.ph, abort);
+                    if (!ok) break;
+                    tc_fence_after();
+                    fence_proxy_async();  // cp.async data -> tensor-core reads
+                    const uint32_t d = tmem + (uint32_t)((issued & 1) * 128);
+                    const uint64_t q = dq0 + (uint32_t)(qb * (64 * 128 >> 4)), go = do0 + (uint32_t)(qb * (64 * 128 >> 4));
+                    const uint64_t k = dk0 + (uint32_t)(rk.slot * (SLOT >> 4)), v = dv0 + (uint32_t)(rv.slot * (SLOT >> 4));
+                    if (on) {
+#pragma unroll
+                        for (int kk = 0; kk < 8; ++kk)  // 16 dims: 32 B of a row of dim half kk / 4
+                            mma_bf16(d, q + (uint64_t)((kk >> 2) * (A_HALF >> 4) + (kk & 3) * 2),
+                                     k + (uint64_t)((kk >> 2) * (HALF_STRIDE >> 4) + (kk & 3) * 2), idesc_s, kk > 0);
+#pragma unroll
+                        for (int kk = 0; kk < 8; ++kk)
+                            mma_bf16(d + 64, go + (uint64_t)((kk >> 2) * (A_HALF >> 4) + (kk & 3) * 2),
+                                     v + (uint64_t)((kk >> 2) * (HALF_STRIDE >> 4) + (kk & 3) * 2), idesc_s, kk > 0);
+                        mma_commit(&bars->v_empty[rv.slot]);
+                        mma_commit(&bars->s_full[issued & 1]);
+                        if (in.last()) mma_commit(&bars->q_empty[qb]);
+                    }
+                    __syncwarp();
+                    rk.next();
+                    rv.next();
+                    in.next();
+                    ++issued;
+                    ++ahead;
+                }
+                if (!ok) break;
+                const int w = done & 1, buf = out.j & 1;
+                // (both segments ago: their dQ has been read)
+                if (out.first() && out.j >= 2) ok = wait_warp(&bars->dq_empty[buf], ((out.j >> 1) - 1) & 1, abort);
+                ok = ok && wait_warp(&bars->p_full[w], (p_ph >> w) & 1, abort);
+                if (!ok) break;
+                p_ph ^= 1u << w;
+                tc_fence_after();
+                const uint64_t k = dkt0 + (uint32_t)(rk2.slot * (SLOT >> 4));
+                if (on) {
+#pragma unroll
+                    for (int kk = 0; kk < TILE / 16; ++kk)  // 16 tokens: 8 columns of ds, two 8-token groups of K
+                        mma_bf16_ts(tmem + Q_COL + (uint32_t)(buf * DH), tmem + (uint32_t)(w * 128 + kk * 8),
+                                    k + (uint64_t)(kk * (2 * GROUP_STRIDE >> 4)), idesc_q, kk > 0 || !out.first());
+                    mma_commit(&bars->k_empty[rk2.slot]);
+                    if (out.last()) mma_commit(&bars->dq_full[buf]);
+                }
+                __syncwarp();
+                rk2.next();
+                out.next();
+                ++done;
+                --ahead;
+            }
+        }
+        if (on) mma_commit(&bars->fin);  // completes when every MMA is done
+        __syncwarp();
+    }
+    // every MMA must be finished before TMEM and shared memory go away
+    mbar_wait_drain(&bars->fin, 0);
+    tc_fence_before();
+    __syncthreads();
+    pdl_trigger();
+    if (threadIdx.x == 0 && *abort && a.status) atomicOr(a.status, SP_DEV_TIMEOUT);
+    if (warp == MMA) tmem_dealloc(tmem, 512);
+}
+
+// dQ of the pairs that lie in several shares (at most one starts in each share): a warp per (share,
+// kv head, row), four dims a lane, the partials in share order, SUM_AT of them under way together.
+constexpr int SUM_THREADS = 128, SUM_ROWS = SUM_THREADS / 32, SUM_AT = 8;
+__global__ void __launch_bounds__(SUM_THREADS) tree_back_tc_sum_kernel(const __grid_constant__ TreeBackArgs args, const int2 *split_tab) {
+    const TreeArgs &a = args.t;
+    pdl_wait();
+    const int hv = blockIdx.x, j0 = blockIdx.y, Hv = a.Hkv * a.n_rb, g = hv / a.n_rb, rb = hv - g * a.n_rb;
+    const int2 tab = __ldcg(split_tab + j0);
+    if (tab.y <= 1) return;
+    const int b = tab.x, lane = threadIdx.x & 31, c = lane * 4;
+    const int q = blockIdx.z * SUM_ROWS + (threadIdx.x >> 5), rr = rb * a.rb_rows + q;
+    if (q >= a.rb_rows || rr >= a.R) return;
+    const size_t at = ((size_t)b * a.Hkv + g) * a.R + rr;
+    float4 s = __ldcg((const float4 *)(args.dq_new + at * DH + c));
+    const bool live = __ldcg(&args.stat[at].x) != INFINITY;  // (+inf for a node that is not there, too)
+#pragma unroll 1
+    for (int e0 = 0; e0 < tab.y; e0 += SUM_AT) {
+        float4 v[SUM_AT];
+#pragma unroll
+        for (int e = 0; e < SUM_AT; ++e) {
+            const size_t slot = ((size_t)(j0 + e0 + e) * 2 + (e0 + e == 0)) * Hv + hv;
+            v[e] = e0 + e < tab.y ? __ldcg((const float4 *)(a.part_o + (slot * a.rb_rows + q) * DH + c)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int e = 0; e < SUM_AT; ++e) s.x += v[e].x, s.y += v[e].y, s.z += v[e].z, s.w += v[e].w;
+    }
+    const int node = rr / a.G;
+    const float f = args.scale;
+    *(uint2 *)((bf16 *)args.dq + ((size_t)b * a.N + node) * a.qs + (size_t)(g * a.G + rr - node * a.G) * DH + c) =
+        live ? make_uint2(pack_bf16(s.x * f, s.y * f), pack_bf16(s.z * f, s.w * f)) : make_uint2(0, 0);
+}
+
+bool make_layout(const TreeArgs &a, int rb_rows, Layout *lay) {
+    const int tab = (4 * a.B + 1) * 4;
+    lay->off_tab = OFF_FRONT;
+    lay->n_q = rb_rows <= 64 ? 2 : 1;
+    // (a second buffer is the tile's other 64 rows; the product of a block of up to 64 rows reads
+    // whatever lies behind them, into rows that nobody uses)
+    lay->off_q = (OFF_FRONT + tab + 1023) & ~1023;
+    lay->off_do = lay->off_q + A_TILE;
+    const int at = lay->off_do + A_TILE, slots = (SMEM_MAX - 1024 - at) / SLOT;
+    if (slots < 4) return false;
+    lay->nv = slots / 2 < MAX_RING ? slots / 2 : MAX_RING;
+    lay->nk = slots - lay->nv < MAX_RING ? slots - lay->nv : MAX_RING;
+    lay->off_k = at;
+    lay->off_v = lay->off_k + lay->nk * SLOT;
+    lay->smem = lay->off_v + lay->nv * SLOT + 1024;
+    return lay->smem <= SMEM_MAX;
+}
+
+}  // namespace
+
+bool tree_back_tc_supported(const TreeArgs &a) {
+    Layout lay;
+    return a.dh == DH && a.dtype == SP_BF16 && a.cache.dtype == SP_BF16 && a.B <= MAX_B && make_layout(a, ROWS, &lay) &&
+           (a.cache.kv.layout == SP_KV_CONTIGUOUS || (long long)a.cache.kv.n_pages * a.Hkv * a.cache.kv.page_size <= 0x7fffffffLL);
+}
+
+void plan_tree_back_tc(TreeArgs *a, int n_sm) {
+    a->n_rb = ceil_div(a->R, ROWS);
+    a->rb_rows = ceil_div(a->R, a->n_rb);
+    const int Hv = a->Hkv * a->n_rb;
+    // (the tile list's numbers stay below 2^30)
+    const long long most = (long long)((1 << 30) / a->B - 1) * TILE;
+    if (a->most_len > most) a->most_len = (int)most;
+    AttnArgs &p = a->plan;
+    p.B = a->B;
+    p.tc_ctas = attn_tc_ctas(n_sm, Hv);
+    if (p.tc_ctas / Hv > MAX_GRP) p.tc_ctas = MAX_GRP * Hv;
+    p.tc_min_tiles = kBackMinTiles;
+    p.tc_seg_cost = kBackSegCost;
+    p.tc_merge_kernel = 1;
+}
+
+int tree_back_tc_groups(const TreeArgs &a) { return a.plan.tc_ctas / (a.Hkv * a.n_rb); }
+size_t tree_back_tc_slots(const TreeArgs &a) { return 2 * (size_t)a.plan.tc_ctas; }
+
+cudaError_t launch_tree_back_tc(const TreeBackArgs &args, int2 *split_tab, cudaStream_t st) {
+    const TreeArgs &a = args.t;
+    Layout lay;
+    if (!make_layout(a, a.rb_rows, &lay)) return cudaErrorInvalidValue;
+    CUtensorMap mk, mv;
+    memset(&mk, 0, sizeof mk);
+    memset(&mv, 0, sizeof mv);
+    if (a.cache.kv.layout == SP_KV_PAGED) {
+        const long long blocks = (long long)a.cache.kv.n_pages * a.Hkv;
+        if (!encode_kv_pages_bf16(&mk, a.cache.kv.k_pool, blocks, a.cache.kv.page_size) ||
+            !encode_kv_pages_bf16(&mv, a.cache.kv.v_pool, blocks, a.cache.kv.page_size))
+            return cudaErrorInvalidValue;
+    }
+    static bool known[MAX_DEVICES] = {};
+    cudaError_t e = allow_smem(tree_back_tc_kernel, SMEM_MAX, known);
+    if (e != cudaSuccess) return e;
+    e = launch_k(tree_back_tc_kernel, dim3(a.plan.tc_ctas), dim3(THREADS), (size_t)lay.smem, st, mk, mv, args, lay, split_tab);
+    if (e != cudaSuccess) return e;
+    return launch_k(tree_back_tc_sum_kernel, dim3(a.Hkv * a.n_rb, tree_back_tc_groups(a), ceil_div(a.rb_rows, SUM_ROWS)),
+                    dim3(SUM_THREADS), 0, st, args, (const int2 *)split_tab);
+}
+
+}  // namespace sp
