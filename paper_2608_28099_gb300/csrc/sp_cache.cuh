@@ -196,6 +196,7 @@ struct TreeBackArgs {
 };
 // Row statistics, gradients of the nodes' keys and values, the nodes' part of dq.
 cudaError_t launch_tree_back_rows(const TreeBackArgs &a, cudaStream_t st);
+cudaError_t launch_tree_back_rows_tc(const TreeBackArgs &a, cudaStream_t st);  // bf16 rows of 128 dims
 // The cache's part of dq on CUDA cores in shares (t.part_o: [slot][row][dh]), and the sum of all parts.
 cudaError_t launch_tree_back_simt(const TreeBackArgs &a, cudaStream_t st);
 size_t tree_back_simt_slots(const TreeArgs &a);
