@@ -1,7 +1,7 @@
 // The cache's part of the backward pass of tree attention (sp_tree_back.cu) on tcgen05 tensor
 // cores: head_dim 128, bf16 rows and cache.  Per key tile of 64 cached tokens and block of up to 128
 // query rows of a kv head, rows on the MMA's M side:
-//   S = Q K^T, dP = dO V^T   128 x 64 each, all operands in shared memory
+//   S = Q K^T, dP = dO V^T   128 x 64 each, Q and dO in TMEM, K and V in shared memory
 //   ds = p (dP - D)          p = exp(scale S - lse), a row a thread, written as bf16 over S in TMEM
 //   dQ += ds K               from TMEM; K is read a second time where it lies (MN-major)
 // The log sums are known, so that a tile's weights are final: nothing is rescaled, two softmax
@@ -12,10 +12,10 @@
 // a segment.  A pair that lies inside one share is finished there (with the nodes' part, formed by the
 // kernel in front), the others leave partials that a second kernel adds in share order.
 //
-// Warps 0-7 softmax; 8-11 load queries and output gradients and write dQ out, two accumulators of
-// which alternate between segments; 12 MMA issuer and TMEM; 13-14 K, 15-16 V (TMA boxes of whole
-// pages, cp.async elsewhere).  TMEM: [S dP] x 2 in columns 0-255, dQ x 2 behind.  Every wait is
-// time-limited (SP_DEV_TIMEOUT).
+// Warps 0-7 softmax; 8-11 bring queries and output gradients (a segment ahead into shared memory,
+// then into TMEM) and write dQ out; 12 MMA issuer and TMEM; 13 K, 14 V (TMA boxes of whole pages, cp.async
+// elsewhere).  TMEM: [S dP] x 2 in columns 0-255, dQ, Q, dO behind.  Every wait is time-limited
+// (SP_DEV_TIMEOUT).
 #include <string.h>
 
 #include "sp_attn_plan.cuh"
@@ -28,27 +28,26 @@ namespace {
 
 constexpr int TILE = 64;
 constexpr int SLOT = TILE * DH * 2;             // K or V of a tile, 16 KB
-constexpr int A_TILE = 128 * DH * 2;            // an M tile of queries or output gradients, 32 KB
-constexpr int A_HALF = A_TILE / 2;              // its 64-dim halves
+constexpr int STAGE_ROW = DH * 2 + 16;          // a staged row of queries or output gradients
 constexpr int ROWS = 128;                       // most rows of a block
 constexpr int MAX_RING = 8;
+constexpr int BAR_EPI = 1;                      // named barrier of warps 8-11
 constexpr int SMEM_MAX = 227 * 1024;
-constexpr int THREADS = 544;
-constexpr int EPI = 8, MMA = 12, K_WARP = 13, V_WARP = 15;
-constexpr uint32_t Q_COL = 256;                 // TMEM: dQ accumulators
+constexpr int THREADS = 512;
+constexpr int EPI = 8, MMA = 12, K_WARP = 13, V_WARP = 14;
+constexpr uint32_t DQ_COL = 256, Q_COL = 384, DO_COL = 448;  // TMEM: dQ, queries, output gradients
 // Fewest tiles a share holds on average, and the cost of a segment in tiles.
 constexpr int kBackMinTiles = 4;
 constexpr int kBackSegCost = 4;
 
 struct Layout {
     int nk, nv;                                 // ring slots
-    int n_q;                                    // buffers of queries: 2 up to 64 rows
-    int off_q, off_do, off_k, off_v, off_tab;
+    int off_q, off_do, off_k, off_v, off_tab;   // (off_q, off_do: staged rows)
     int smem;
 };
 struct Bars {
     uint64_t k_full[MAX_RING], k_empty[MAX_RING], v_full[MAX_RING], v_empty[MAX_RING];
-    uint64_t s_full[2], p_full[2], q_full[2], q_empty[2], dq_full[2], dq_empty[2], fin;
+    uint64_t s_full[2], p_full[2], q_full, q_empty, dq_full, dq_empty, fin;
     uint32_t tmem;
     int abort;
     int wsum[32];
@@ -184,10 +183,10 @@ struct Walk {
     }
 };
 
-// Queries and output gradients of sequence b into the A operands, rows [r0, r0 + rows) of the tiles;
-// zeros for rows of nodes that are not there.  16 lanes a row, four rows of each under way together.
-__device__ __forceinline__ void load_rows(const TreeBackArgs &x, int b, int n, int g, int rb, uint8_t *Q, uint8_t *dO, int r0,
-                                          int wi, int lane) {
+// Queries and output gradients of sequence b, a block's rows, into their staging places; zeros for
+// rows of nodes that are not there.  16 lanes a row, four rows of each under way together.
+__device__ __forceinline__ void stage_rows(const TreeBackArgs &x, int b, int n, int g, int rb, uint8_t *Q, uint8_t *dO, int wi,
+                                           int lane) {
     const TreeArgs &a = x.t;
     const int c = lane & 15;
     constexpr int AT_ONCE = 4;
@@ -206,14 +205,25 @@ __device__ __forceinline__ void load_rows(const TreeBackArgs &x, int b, int n, i
         }
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
-            const int r = r0 + r1 + k * 8;
-            if (r1 + k * 8 >= a.rb_rows) break;
-            const uint32_t at = (uint32_t)((c >> 3) * A_HALF + r * 128 + (((c & 7) ^ (r & 7)) << 4));
-            st_shared_v4(Q + at, q[k].x, q[k].y, q[k].z, q[k].w);
-            st_shared_v4(dO + at, go[k].x, go[k].y, go[k].z, go[k].w);
+            const int r = r1 + k * 8;
+            if (r >= a.rb_rows) break;
+            st_shared_v4(Q + r * STAGE_ROW + c * 16, q[k].x, q[k].y, q[k].z, q[k].w);
+            st_shared_v4(dO + r * STAGE_ROW + c * 16, go[k].x, go[k].y, go[k].z, go[k].w);
         }
     }
-    fence_proxy_async();  // -> tensor-core reads
+}
+// A staged row into 64 TMEM columns of its lane.
+__device__ __forceinline__ void row_to_tmem(uint32_t addr, const uint8_t *row) {
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+        uint32_t v[16];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 u = *(const uint4 *)(row + h * 64 + i * 16);
+            v[4 * i] = u.x, v[4 * i + 1] = u.y, v[4 * i + 2] = u.z, v[4 * i + 3] = u.w;
+        }
+        st16_async(addr + h * 16, v);
+    }
 }
 
 __global__ void __launch_bounds__(THREADS, 1)
@@ -242,22 +252,22 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (threadIdx.x == THREADS - 1) {
 #pragma unroll 1
         for (int i = 0; i < lay.nk; ++i) {
-            mbar_init(&bars->k_full[i], 64);
+            mbar_init(&bars->k_full[i], 32);
             mbar_init(&bars->k_empty[i], 1);
         }
 #pragma unroll 1
         for (int i = 0; i < lay.nv; ++i) {
-            mbar_init(&bars->v_full[i], 64);
+            mbar_init(&bars->v_full[i], 32);
             mbar_init(&bars->v_empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bars->s_full[i], 1);
             mbar_init(&bars->p_full[i], 4);
-            mbar_init(&bars->q_full[i], 4);
-            mbar_init(&bars->q_empty[i], 1);
-            mbar_init(&bars->dq_full[i], 1);
-            mbar_init(&bars->dq_empty[i], 4);
         }
+        mbar_init(&bars->q_full, 4);
+        mbar_init(&bars->q_empty, 1);
+        mbar_init(&bars->dq_full, 1);
+        mbar_init(&bars->dq_empty, 4);
         mbar_init(&bars->fin, 1);
         bars->abort = 0;
         fence_mbar_init();
@@ -351,22 +361,33 @@ __global__ void __launch_bounds__(THREADS, 1)
         const int quad = warp - EPI, r = quad * 32 + lane, rr = rb * a.rb_rows + r;
         const bool active = r < a.rb_rows && rr < a.R;
         const bool warp_active = __any_sync(0xffffffffu, active);
-        const uint32_t lane_base = tmem + ((uint32_t)(quad * 32) << 16) + Q_COL;
+        const uint32_t lane_base = tmem + ((uint32_t)(quad * 32) << 16);
         const int n_seg = sh.b1 - sh.b0;
+        // the rows of segment j: staged; into TMEM once the scores before have read theirs
         const auto load = [&](int j) {
-            const int buf = lay.n_q == 2 ? j & 1 : 0, use = lay.n_q == 2 ? j >> 1 : j;
-            if (!wait_warp(&bars->q_empty[buf], (use & 1) ^ 1, abort)) return false;
             const int b = sh.b0 + j;
-            load_rows(args, b, nodes[b], g, rb, smem + lay.off_q, smem + lay.off_do, buf * 64, quad, lane);
-            arrive_warp(&bars->q_full[buf], lane);
-            return true;
+            named_sync(BAR_EPI, 128);  // (the staged rows before are in TMEM)
+            stage_rows(args, b, nodes[b], g, rb, smem + lay.off_q, smem + lay.off_do, quad, lane);
+            named_sync(BAR_EPI, 128);
+            const bool free = wait_warp(&bars->q_empty, (j & 1) ^ 1, abort);
+            if (free && warp_active) {
+                tc_fence_after();
+                const int from = min(r, a.rb_rows - 1);  // (lanes behind the rows: any)
+                row_to_tmem(lane_base + Q_COL, smem + lay.off_q + from * STAGE_ROW);
+                row_to_tmem(lane_base + DO_COL, smem + lay.off_do + from * STAGE_ROW);
+                st_wait();
+                tc_fence_before();
+            }
+            if (free) arrive_warp(&bars->q_full, lane);
+            return free;
         };
+        // (a warp whose wait ran out goes on to the barriers that the others meet at)
         bool ok = n_seg == 0 || load(0);
         pdl_wait();  // the nodes' part of dQ; nothing is written before
 #pragma unroll 1
-        for (int j = 0; ok && j < n_seg; ++j) {
-            if (j + 1 < n_seg) ok = load(j + 1);
-            const int b = sh.b0 + j, buf = j & 1;
+        for (int j = 0; j < n_seg; ++j) {
+            if (j + 1 < n_seg) ok = load(j + 1) && ok;
+            const int b = sh.b0 + j;
             const Seg sg = piece(sh, b);
             const int n = nodes[b];
             const int j_first = group_of(cuts, n_grp, sg.xp), j_last = group_of(cuts, n_grp, sg.xp + sg.nt - 1);
@@ -376,15 +397,14 @@ __global__ void __launch_bounds__(THREADS, 1)
             const size_t row = ((size_t)b * Hkv + g) * a.R + rr;
             bool live = false;
             if (active && whole) live = node < n && __ldcg(&args.stat[row].x) != INFINITY;
-            ok = ok && wait_warp(&bars->dq_full[buf], (j >> 1) & 1, abort);
-            if (!ok) break;
+            ok = ok && wait_warp(&bars->dq_full, j & 1, abort);
             tc_fence_after();
-            if (warp_active) {
+            if (ok && warp_active) {
 #pragma unroll 1
                 for (int d = 0; d < DH; d += 32) {
                     float v[32];
                     __syncwarp();
-                    ld32_async(lane_base + (uint32_t)(buf * DH + d), v);
+                    ld32_async(lane_base + DQ_COL + (uint32_t)d, v);
                     ld_wait(v);
                     if (!active) continue;
                     if (whole) {
@@ -408,13 +428,11 @@ __global__ void __launch_bounds__(THREADS, 1)
                 }
             }
             tc_fence_before();
-            arrive_warp(&bars->dq_empty[buf], lane);
+            if (ok) arrive_warp(&bars->dq_empty, lane);
         }
-    } else if (warp >= K_WARP) {
+    } else if (warp == K_WARP || warp == V_WARP) {
         // ------------------------------------------------------------ K and V
-        const bool is_v = warp >= V_WARP;
-        const int pidx = warp - (is_v ? V_WARP : K_WARP), ptid = pidx * 32 + lane;
-        const bool lead = pidx == 0;
+        const bool is_v = warp == V_WARP;
         uint64_t *full = is_v ? bars->v_full : bars->k_full, *empty = is_v ? bars->v_empty : bars->k_empty;
         uint8_t *ring = smem + (is_v ? lay.off_v : lay.off_k);
         const CUtensorMap *map = is_v ? &map_v : &map_k;
@@ -448,7 +466,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 }
                 uint8_t *dst = ring + rg.slot * SLOT;
                 bool plain = false;  // this thread wrote shared memory or issued cp.async
-                if (n_pg > 0 && lead) {
+                if (n_pg > 0) {
                     const bool have = lane < n_pg && page >= 0;
                     const unsigned okm = __ballot_sync(0xffffffffu, have);
                     if (lane == 0 && okm) expect_tx(&full[rg.slot], __popc(okm) * P * ROW);
@@ -475,10 +493,10 @@ __global__ void __launch_bounds__(THREADS, 1)
                         src = pool + ((size_t)max(pg, 0) * Hkv + g) * P * ROW;
                         step = ROW;
                     }
-                    const int c = ptid & 15, r1 = ptid >> 4;
+                    const int c = lane & 15, r1 = lane >> 4;
                     src += (size_t)r1 * step + c * 16;
 #pragma unroll 4
-                    for (int r = r1; r < n_tok - r0; r += 4, src += 4 * step) {
+                    for (int r = r1; r < n_tok - r0; r += 2, src += 2 * step) {
                         uint8_t *d = dst + kv_off(r0 + r, c);
                         if (have) cp_async16(d, src);
                         else st_shared_v4(d, 0, 0, 0, 0);
@@ -488,7 +506,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                     plain = true;
                     const int from = max(n_tok, 0);
 #pragma unroll 1
-                    for (int idx = ptid; idx < (TILE - from) * 16; idx += 64)
+                    for (int idx = lane; idx < (TILE - from) * 16; idx += 32)
                         st_shared_v4(dst + kv_off(from + (idx >> 4), idx & 15), 0, 0, 0, 0);
                 }
                 if (plain) {
@@ -502,7 +520,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");  // nothing lands after the CTA is gone
-        if (lead && lane == 0) {
+        if (lane == 0) {
             // drain copies still in flight (only possible after an abort)
             Ring rd(rg.n);
 #pragma unroll 1
@@ -511,14 +529,13 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         bad = __any_sync(0xffffffffu, bad);
         if (bad && lane == 0 && a.status) atomicOr(a.status, SP_DEV_BAD_PAGE);
-    } else {
+    } else if (warp == MMA) {
         // ------------------------------------------------------------ MMA issue
         // S and dP run up to two tiles ahead of dQ, into the buffer that the softmax of two tiles
         // before has read (its gradients are in front of it in the pipe).  One issuer sees every use
         // of every slot in order.
         const bool on = elect_one();
         constexpr uint32_t idesc_s = idesc_bf16_f32(128, TILE), idesc_q = idesc_bf16_f32_bmn(128, DH);
-        const uint64_t dq0 = sw128_kmajor_desc(smem + lay.off_q), do0 = sw128_kmajor_desc(smem + lay.off_do);
         const uint64_t dk0 = sw128_kmajor_desc_sbo(smem + lay.off_k, GROUP_STRIDE);
         const uint64_t dv0 = sw128_kmajor_desc_sbo(smem + lay.off_v, GROUP_STRIDE);
         const uint64_t dkt0 = sw128_mnmajor_desc2(smem + lay.off_k, HALF_STRIDE, GROUP_STRIDE);
@@ -533,31 +550,29 @@ __global__ void __launch_bounds__(THREADS, 1)
             while (ok && done < n_tiles) {
 #pragma unroll 1
                 while (ok && issued < n_tiles && ahead < 2) {
-                    const int qb = lay.n_q == 2 ? in.j & 1 : 0, use = lay.n_q == 2 ? in.j >> 1 : in.j;
                     if (in.first()) {
                         // (queries that are not there yet do not hold up the tiles under way)
-                        if (ahead > 0 && !__all_sync(0xffffffffu, mbar_try_wait(&bars->q_full[qb], use & 1))) break;
-                        ok = wait_warp(&bars->q_full[qb], use & 1, abort);
+                        if (ahead > 0 && !__all_sync(0xffffffffu, mbar_try_wait(&bars->q_full, in.j & 1))) break;
+                        ok = wait_warp(&bars->q_full, in.j & 1, abort);
                     }
                     ok = ok && wait_warp(&bars->k_full[rk.slot], rk.ph, abort) && wait_warp(&bars->v_full[rv.slot], rv.ph, abort);
                     if (!ok) break;
                     tc_fence_after();
                     fence_proxy_async();  // cp.async data -> tensor-core reads
                     const uint32_t d = tmem + (uint32_t)((issued & 1) * 128);
-                    const uint64_t q = dq0 + (uint32_t)(qb * (64 * 128 >> 4)), go = do0 + (uint32_t)(qb * (64 * 128 >> 4));
                     const uint64_t k = dk0 + (uint32_t)(rk.slot * (SLOT >> 4)), v = dv0 + (uint32_t)(rv.slot * (SLOT >> 4));
                     if (on) {
 #pragma unroll
-                        for (int kk = 0; kk < 8; ++kk)  // 16 dims: 32 B of a row of dim half kk / 4
-                            mma_bf16(d, q + (uint64_t)((kk >> 2) * (A_HALF >> 4) + (kk & 3) * 2),
-                                     k + (uint64_t)((kk >> 2) * (HALF_STRIDE >> 4) + (kk & 3) * 2), idesc_s, kk > 0);
+                        for (int kk = 0; kk < 8; ++kk)  // 16 dims: 8 columns of Q, 32 B of a row of K's dim half kk / 4
+                            mma_bf16_ts(d, tmem + Q_COL + (uint32_t)(kk * 8),
+                                        k + (uint64_t)((kk >> 2) * (HALF_STRIDE >> 4) + (kk & 3) * 2), idesc_s, kk > 0);
 #pragma unroll
                         for (int kk = 0; kk < 8; ++kk)
-                            mma_bf16(d + 64, go + (uint64_t)((kk >> 2) * (A_HALF >> 4) + (kk & 3) * 2),
-                                     v + (uint64_t)((kk >> 2) * (HALF_STRIDE >> 4) + (kk & 3) * 2), idesc_s, kk > 0);
+                            mma_bf16_ts(d + 64, tmem + DO_COL + (uint32_t)(kk * 8),
+                                        v + (uint64_t)((kk >> 2) * (HALF_STRIDE >> 4) + (kk & 3) * 2), idesc_s, kk > 0);
                         mma_commit(&bars->v_empty[rv.slot]);
                         mma_commit(&bars->s_full[issued & 1]);
-                        if (in.last()) mma_commit(&bars->q_empty[qb]);
+                        if (in.last()) mma_commit(&bars->q_empty);
                     }
                     __syncwarp();
                     rk.next();
@@ -567,9 +582,9 @@ __global__ void __launch_bounds__(THREADS, 1)
                     ++ahead;
                 }
                 if (!ok) break;
-                const int w = done & 1, buf = out.j & 1;
-                // (both segments ago: their dQ has been read)
-                if (out.first() && out.j >= 2) ok = wait_warp(&bars->dq_empty[buf], ((out.j >> 1) - 1) & 1, abort);
+                const int w = done & 1;
+                // (the segment before: its dQ has been read)
+                if (out.first() && out.j >= 1) ok = wait_warp(&bars->dq_empty, (out.j - 1) & 1, abort);
                 ok = ok && wait_warp(&bars->p_full[w], (p_ph >> w) & 1, abort);
                 if (!ok) break;
                 p_ph ^= 1u << w;
@@ -578,10 +593,10 @@ __global__ void __launch_bounds__(THREADS, 1)
                 if (on) {
 #pragma unroll
                     for (int kk = 0; kk < TILE / 16; ++kk)  // 16 tokens: 8 columns of ds, two 8-token groups of K
-                        mma_bf16_ts(tmem + Q_COL + (uint32_t)(buf * DH), tmem + (uint32_t)(w * 128 + kk * 8),
+                        mma_bf16_ts(tmem + DQ_COL, tmem + (uint32_t)(w * 128 + kk * 8),
                                     k + (uint64_t)(kk * (2 * GROUP_STRIDE >> 4)), idesc_q, kk > 0 || !out.first());
                     mma_commit(&bars->k_empty[rk2.slot]);
-                    if (out.last()) mma_commit(&bars->dq_full[buf]);
+                    if (out.last()) mma_commit(&bars->dq_full);
                 }
                 __syncwarp();
                 rk2.next();
@@ -637,12 +652,9 @@ __global__ void __launch_bounds__(SUM_THREADS) tree_back_tc_sum_kernel(const __g
 bool make_layout(const TreeArgs &a, int rb_rows, Layout *lay) {
     const int tab = (4 * a.B + 1) * 4;
     lay->off_tab = OFF_FRONT;
-    lay->n_q = rb_rows <= 64 ? 2 : 1;
-    // (a second buffer is the tile's other 64 rows; the product of a block of up to 64 rows reads
-    // whatever lies behind them, into rows that nobody uses)
-    lay->off_q = (OFF_FRONT + tab + 1023) & ~1023;
-    lay->off_do = lay->off_q + A_TILE;
-    const int at = lay->off_do + A_TILE, slots = (SMEM_MAX - 1024 - at) / SLOT;
+    lay->off_q = (OFF_FRONT + tab + 15) & ~15;
+    lay->off_do = lay->off_q + rb_rows * STAGE_ROW;
+    const int at = (lay->off_do + rb_rows * STAGE_ROW + 1023) & ~1023, slots = (SMEM_MAX - 1024 - at) / SLOT;
     if (slots < 4) return false;
     lay->nv = slots / 2 < MAX_RING ? slots / 2 : MAX_RING;
     lay->nk = slots - lay->nv < MAX_RING ? slots - lay->nv : MAX_RING;
