@@ -440,30 +440,26 @@ __global__ void __launch_bounds__(THREADS, 1)
         const uint64_t pol = policy_evict_first();
         Ring rg(is_v ? lay.nv : lay.nk);
         int bad = 0, filled = 0;
-        bool stop = false;
+        // the tile's page ids, a lane each (-1: none), asked for a tile ahead: an answer that comes behind
+        // the cache stream takes longer than a tile
+        const auto ask = [&](const Walk &w) {
+            const int b = sh.b0 + w.j, t0 = (w.sg.t_a + w.i) * TILE, lp = (t0 >> P_bits) + lane;
+            if (!paged || lane * P >= min(TILE, lens[b] - t0) || lp >= a.cache.kv.max_pages) return -1;
+            return __ldg(a.cache.kv.page_table + (size_t)sids[b] * a.cache.kv.max_pages + lp);
+        };
+        if (n_tiles > 0) {
+            Walk at(sh);
+            int next = ask(at);
 #pragma unroll 1
-        for (int b = sh.b0; b < sh.b1 && !stop; ++b) {
-            const Seg sg = piece(sh, b);
-            const int sid = sids[b], L = lens[b];
-            const uint8_t *seq = nullptr;  // a contiguous sequence's rows of head g, a token apart
-            if (!paged && L > 0)
-                seq = (const uint8_t *)(is_v ? a.cache.kv.v_seq : a.cache.kv.k_seq)[sid] + (size_t)g * ROW;
-            const size_t seq_step = (size_t)Hkv * ROW;
-#pragma unroll 1
-            for (int i = 0; i < sg.n; ++i) {
-                const int t0 = (sg.t_a + i) * TILE, n_tok = min(TILE, L - t0);
+            for (int x = 0; x < n_tiles; ++x) {
+                const int b = sh.b0 + at.j, t0 = (at.sg.t_a + at.i) * TILE, n_tok = min(TILE, lens[b] - t0);
                 const int n_pg = paged ? n_tok >> P_bits : 0;  // whole pages
-                int page = -1;                                 // ids, asked for before the wait
-                if (paged && lane * P < n_tok) {
-                    const int lp = (t0 >> P_bits) + lane;
-                    page = lp < a.cache.kv.max_pages ? __ldg(a.cache.kv.page_table + (size_t)sid * a.cache.kv.max_pages + lp) : -1;
-                    if (page < 0 || page >= a.cache.kv.n_pages) page = -1, bad = 1;
-                }
+                int page = next;
+                if (paged && lane * P < n_tok && (page < 0 || page >= a.cache.kv.n_pages)) page = -1, bad = 1;
+                at.next();
+                if (x + 1 < n_tiles) next = ask(at);
                 // warp-uniform verdict: the collectives below need every lane
-                if (!wait_warp(&empty[rg.slot], rg.ph ^ 1, abort)) {
-                    stop = true;
-                    break;
-                }
+                if (!wait_warp(&empty[rg.slot], rg.ph ^ 1, abort)) break;
                 uint8_t *dst = ring + rg.slot * SLOT;
                 bool plain = false;  // this thread wrote shared memory or issued cp.async
                 if (n_pg > 0) {
@@ -484,14 +480,16 @@ __global__ void __launch_bounds__(THREADS, 1)
                 const int r0 = n_pg * (paged ? P : 0);  // first row not covered by TMA
                 if (r0 < n_tok) {
                     plain = true;
-                    const uint8_t *src = seq + (size_t)t0 * seq_step;
-                    size_t step = seq_step;
+                    const uint8_t *src;
+                    size_t step = ROW;
                     bool have = true;
-                    if (paged) {  // the last, partial page
+                    if (!paged) {  // a contiguous sequence's rows of head g, a token apart
+                        step = (size_t)Hkv * ROW;
+                        src = (const uint8_t *)(is_v ? a.cache.kv.v_seq : a.cache.kv.k_seq)[sids[b]] + (size_t)g * ROW + (size_t)t0 * step;
+                    } else {  // the last, partial page
                         const int pg = __shfl_sync(0xffffffffu, page, n_pg);
                         have = pg >= 0;
                         src = pool + ((size_t)max(pg, 0) * Hkv + g) * P * ROW;
-                        step = ROW;
                     }
                     const int c = lane & 15, r1 = lane >> 4;
                     src += (size_t)r1 * step + c * 16;
