@@ -53,8 +53,14 @@ sp_status check_vocab(const sp_vocab_dims *d, bool backward, VocabArgs *a) {
         return fail(SP_ERR_UNSUPPORTED, "the tensor-core kernels need bf16 and d_model, h_stride and w_stride in multiples of 8");
     if (a->n == 0) return SP_OK;
     if (tensor) plan_vocab_tc(a, backward, sm_count());
-    else plan_vocab_simt(a, backward);
+    else plan_vocab_simt(a, backward, sm_count());
     a->hc = tensor ? (bf16 *)256 : nullptr;  // (placed by lay_out)
+    if (backward) {
+        // most rows of partial dh for any number of kept tokens (see split_count)
+        const long long tm = tensor ? 256 : 64, m_tiles = ceil_div_ll(a->n, tm);
+        const long long more = ceil_div_ll(8ll * a->pairs, ceil_div_ll(a->d, tm));
+        a->acc_rows = (m_tiles + (more < 15 * m_tiles ? more : 15 * m_tiles)) * tm;
+    }
     return SP_OK;
 }
 
@@ -75,7 +81,7 @@ size_t lay_out(VocabArgs *a, bool backward, char *base) {
         a->at = (float *)take((size_t)a->n * sizeof(float));
     } else {
         a->grad = take((size_t)a->pad * a->piece * (tensor ? sizeof(bf16) : sizeof(float)));
-        a->acc = (float *)take((size_t)a->planes * a->n * a->d * sizeof(float));
+        a->acc = (float *)take((size_t)a->acc_rows * a->d * sizeof(float));
     }
     return at;
 }
@@ -177,7 +183,7 @@ sp_status sp_vocab_loss(sp_stream stream, const sp_vocab_dims *dims, const void 
     a.status = d_status;
     const cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e = launch_vocab_keep(a, false, st);
-    if (e == cudaSuccess) e = a.hc ? launch_vocab_loss_tc(a, sm_count(), st) : launch_vocab_loss_simt(a, st);
+    if (e == cudaSuccess) e = a.hc ? launch_vocab_loss_tc(a, st) : launch_vocab_loss_simt(a, st);
     if (e == cudaSuccess) e = launch_vocab_finish_loss(a, st);
     return launched(e, "sp_vocab_loss");
 }
@@ -209,7 +215,7 @@ sp_status sp_vocab_loss_backward(sp_stream stream, const sp_vocab_dims *dims, co
     a.dw = d_grad_w;
     a.status = d_status;
     cudaError_t e = launch_vocab_keep(a, true, st);
-    if (e == cudaSuccess) e = a.hc ? launch_vocab_backward_tc(a, sm_count(), st) : launch_vocab_backward_simt(a, st);
+    if (e == cudaSuccess) e = a.hc ? launch_vocab_backward_tc(a, st) : launch_vocab_backward_simt(a, st);
     if (e == cudaSuccess) e = launch_vocab_finish_dh(a, st);
     return launched(e, "sp_vocab_loss_backward");
 }

@@ -31,7 +31,7 @@ constexpr int OFF_BAR = STAGES * STAGE, SMEM = OFF_BAR + 256 + 1024 /*align*/;
 constexpr int THREADS = 384;                     // warps 0-7 epilogue, 8 TMA, 9 MMA (rank 0), 10 TMEM
 constexpr int TMA = 8, MMA = 9, TMEM = 10, EPI_THREADS = 256;
 constexpr int TMEM_COLS = 2 * TN;
-constexpr long long GRAD_BYTES = 256ll << 20;    // most bytes of a piece's g
+constexpr long long GRAD_BYTES = 512ll << 20;    // most bytes of a piece's g
 
 template <int KIND>
 struct Kind {
@@ -40,17 +40,21 @@ struct Kind {
 
 // Tiles of a product over `count` kept tokens and `piece` vocabulary rows.
 struct Tiles {
-    int m, n, kb, splits;
+    int m, n, kb, splits, per;
     __device__ __forceinline__ int items() const { return m * n * splits; }
 };
 template <int KIND>
-__device__ __forceinline__ Tiles tiles_of(const VocabArgs &a, int count, int piece, int splits) {
+__device__ __forceinline__ Tiles tiles_of(const VocabArgs &a, int count, int piece) {
     Tiles t;
-    t.m = KIND == DW ? ceil_div(piece, TM) : ceil_div(KIND == GRAD ? max(count, 1) : count, TM);
+    // (without a token one tile is formed whose rows are nobody's; DW's k-block 0 of g and h is cleared)
+    t.m = KIND == DW ? ceil_div(piece, TM) : ceil_div(max(count, 1), TM);
     t.n = ceil_div(KIND == LOSS || KIND == GRAD ? piece : a.d, TN);
-    // (without a token DW is a product of zeros: k-block 0 of g and h is cleared)
     t.kb = KIND == DH ? ceil_div(piece, BK) : KIND == DW ? ceil_div(max(count, 1), BK) : ceil_div(a.d, BK);
-    t.splits = splits;
+    t.splits = 1, t.per = t.kb;
+    if (KIND == DH) {
+        const DhPlan p = dh_plan(a, count);
+        t.splits = p.k.s, t.per = p.k.per;
+    }
     return t;
 }
 struct Item {
@@ -59,7 +63,7 @@ struct Item {
 // Neighbouring pairs take tiles that share what does not stay in L2: rows of the vocabulary (LOSS,
 // GRAD), columns of W (DH); DW walks all of h's columns (which stay) for a tile of g.
 template <int KIND>
-__device__ __forceinline__ Item item_of(const Tiles &t, int it, int kb_per_split) {
+__device__ __forceinline__ Item item_of(const Tiles &t, int it) {
     Item x;
     int m, n;
     if (KIND == DW) {
@@ -71,15 +75,15 @@ __device__ __forceinline__ Item item_of(const Tiles &t, int it, int kb_per_split
         n = q % t.n, x.split = q / t.n;
     }
     x.m0 = m * TM, x.n0 = n * TN, x.nt = n;
-    x.kb0 = x.split * kb_per_split;
-    x.nkb = min(kb_per_split, t.kb - x.kb0);
+    x.kb0 = x.split * t.per;
+    x.nkb = min(t.per, t.kb - x.kb0);  // (<= 0: a split that the last, shorter piece leaves nothing)
     return x;
 }
 
 template <int KIND>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     vocab_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                    const __grid_constant__ VocabArgs a, int v0, int splits, int kb_per_split) {
+                    const __grid_constant__ VocabArgs a, int v0) {
     typedef Kind<KIND> Ki;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -117,19 +121,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    pdl_wait();
-    const int piece = min(a.piece, a.V - v0), count = *a.count;
-    const Tiles t = tiles_of<KIND>(a, count, piece, splits);
-    const int n_items = t.items();
+    const int piece = min(a.piece, a.V - v0);
 
     if (warp == TMA && lane == 0) {
         // what is read again soon stays in L2, the vocabulary's rows of LOSS pass through
         const uint64_t pol_a = KIND == LOSS || KIND == GRAD ? policy_evict_last() : policy_evict_normal();
         const uint64_t pol_b = KIND == LOSS ? policy_evict_first() : KIND == DW ? policy_evict_last() : policy_evict_normal();
+        // Up to 256 tokens the logits' first tile is known before the tokens are counted, and W does
+        // not depend on them: its k-blocks are asked for while the kernel in front still runs
+        // (which has waited for the caller's earlier work before it let this one start).
+        int pre = 0;
+        if ((KIND == LOSS || KIND == GRAD) && a.pad == TM && cl < ceil_div(piece, TN)) {
+            pre = min(STAGES, ceil_div(a.d, BK));
+            for (int i = 0; i < pre; ++i) {
+                if (rank == 0) mbar_arrive_expect_tx(&full[i], 2 * STAGE);
+                tma_load_2d_pair(smem + i * STAGE + HALF, &map_b, map_rank(&full[i], 0), i * BK, v0 + cl * TN + (int)rank * 128, pol_b);
+            }
+        }
+        pdl_wait();
+        const Tiles t = tiles_of<KIND>(a, *a.count, piece);
+        const int n_items = t.items();
         int gi = 0;
         bool ok = true;
         for (int it = cl; ok && it < n_items; it += n_cl) {
-            const Item x = item_of<KIND>(t, it, kb_per_split);
+            const Item x = item_of<KIND>(t, it);
             const int ma = x.m0 + (int)rank * 128, nb = x.n0 + (int)rank * 128;
             for (int i = 0; i < x.nkb; ++i, ++gi) {
                 const int s = gi % STAGES, k = (x.kb0 + i) * BK;
@@ -137,7 +152,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                     ok = false;
                     break;
                 }
-                if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * STAGE);
+                if (rank == 0 && gi >= pre) mbar_arrive_expect_tx(&full[s], 2 * STAGE);
                 const uint32_t bar = map_rank(&full[s], 0);
                 uint8_t *sa = smem + s * STAGE, *sb = sa + HALF;
                 if (Ki::A_MN) {
@@ -150,7 +165,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                     const int kv = KIND == DH ? v0 + k : k;
                     tma_load_2d_pair(sb, &map_b, bar, nb, kv, pol_b);
                     tma_load_2d_pair(sb + HALF / 2, &map_b, bar, nb + 64, kv, pol_b);
-                } else {
+                } else if (gi >= pre) {
                     tma_load_2d_pair(sb, &map_b, bar, k, v0 + nb, pol_b);
                 }
             }
@@ -162,10 +177,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         constexpr uint32_t idesc = idesc_bf16_f32(TM, TN) | (Ki::A_MN ? 1u << 15 : 0u) | (Ki::B_MN ? 1u << 16 : 0u);
         // a step of 16 along K: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major tile
         constexpr uint64_t step_a = Ki::A_MN ? 2048 >> 4 : 32 >> 4, step_b = Ki::B_MN ? 2048 >> 4 : 32 >> 4;
+        pdl_wait();
+        const Tiles t = tiles_of<KIND>(a, *a.count, piece);
+        const int n_items = t.items();
         int gi = 0, n = 0;
         bool ok = true;
-        for (int it = cl; ok && it < n_items; it += n_cl, ++n) {
-            const Item x = item_of<KIND>(t, it, kb_per_split);
+        for (int it = cl; ok && it < n_items; it += n_cl) {
+            const Item x = item_of<KIND>(t, it);
+            if (KIND == DH && x.nkb <= 0) continue;
             const int buf = n & 1;
             const uint32_t acc = tmem + (uint32_t)(buf * TN);
             // both CTAs' epilogues have read this accumulator's previous tile
@@ -187,15 +206,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                 mma_commit_pair(&empty[s]);
             }
             if (ok) mma_commit_pair(&acc_full[buf]);
+            ++n;
         }
         mma_commit_pair(fin);  // every MMA is finished before TMEM and shared memory go away
         mbar_wait_drain(fin, 0);
     } else if (warp < 8) {
         // a row a thread: warp w reads TMEM lanes 32 (w & 3).. and columns 128 (w >> 2)..
         const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane;
-        int n = 0;
-        for (int it = cl; it < n_items; it += n_cl, ++n) {
-            const Item x = item_of<KIND>(t, it, kb_per_split);
+        pdl_wait();
+        const int count = *a.count;
+        const Tiles t = tiles_of<KIND>(a, count, piece);
+        const int n_items = t.items();
+        int n = -1;
+        for (int it = cl; it < n_items; it += n_cl) {
+            const Item x = item_of<KIND>(t, it);
+            if (KIND == DH && x.nkb <= 0) continue;
+            ++n;
             const int buf = n & 1, m = x.m0 + (int)rank * 128 + row;
             VocabRow info{0.f, 0.f, -1, 0};
             if ((KIND == LOSS || KIND == GRAD) && m < count) info = a.rows[m];
@@ -215,7 +241,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                     float top = mx;
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
-                        v[j] = j < left ? v[j] * LOG2E : -INFINITY;
+                        if (j >= left) v[j] = -INFINITY;
                         top = fmaxf(top, v[j]);
                     }
                     const int hit = info.target - (c0 + c);
@@ -226,11 +252,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                         a.at[m] = z;
                     }
                     const float mu = top == -INFINITY ? 0.f : top;
-                    sum *= mx == -INFINITY ? 1.f : fast_exp2(mx - mu);
+                    sum *= mx == -INFINITY ? 1.f : fast_exp2((mx - mu) * LOG2E);
                     mx = top;
                     float s4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) s4[j & 3] += fast_exp2(v[j] - mu);
+                    for (int j = 0; j < 32; ++j) s4[j & 3] += fast_exp2((v[j] - mu) * LOG2E);
                     sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
                 } else if constexpr (KIND == GRAD) {
                     const int left = m < count ? piece - (c0 + c) : 0, hit = info.target - v0 - (c0 + c);
@@ -240,7 +266,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                         float g[2];
 #pragma unroll
                         for (int q = 0; q < 2; ++q) {
-                            const float p = fast_exp2(fmaf(v[j + q], LOG2E, -info.lse2));
+                            const float p = fast_exp2((v[j + q] - info.lse) * LOG2E);
                             g[q] = j + q < left ? (j + q == hit ? p - 1.f : p) * info.g : 0.f;
                         }
                         w[j / 2] = pack2_bf16(g[0], g[1]);
@@ -250,7 +276,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                     for (int j = 0; j < 4; ++j) to[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
                 } else if constexpr (KIND == DH) {
                     if (m >= count) continue;
-                    float *to = a.acc + ((size_t)x.split * a.n + m) * a.d + c0 + c;
+                    float *to = a.acc + ((size_t)x.split * (t.m * TM) + m) * a.d + c0 + c;
 #pragma unroll
                     for (int j = 0; j < 32; j += 4) {
                         if (c0 + c + j >= a.d) break;
@@ -291,18 +317,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
 }
 
 template <int KIND>
-cudaError_t run(const VocabArgs &a, const CUtensorMap &ma, const CUtensorMap &mb, int v0, int n_sm, cudaStream_t st) {
+cudaError_t run(const VocabArgs &a, const CUtensorMap &ma, const CUtensorMap &mb, int v0, cudaStream_t st) {
     static bool known[MAX_DEVICES] = {};
     const cudaError_t e = allow_smem(vocab_tc_kernel<KIND>, SMEM, known);
     if (e != cudaSuccess) return e;
     const int piece = a.V - v0 < a.piece ? a.V - v0 : a.piece;
     const long long m = KIND == DW ? ceil_div(piece, TM) : a.pad / TM, n = ceil_div(KIND == LOSS || KIND == GRAD ? piece : a.d, TN);
-    const int kb = ceil_div(KIND == DH ? piece : a.d, BK), splits = KIND == DH ? a.planes : 1;
-    const int per = KIND == DW ? 0x7fffffff : ceil_div(kb, splits);
-    const long long items = m * n * splits;
-    const int pairs = n_sm / 2 > 0 ? n_sm / 2 : 1;
+    const long long items = m * n * (KIND == DH ? 16 : 1);
+    const int pairs = a.pairs;
     return launch_k(vocab_tc_kernel<KIND>, dim3(2 * (items < pairs ? (unsigned)items : (unsigned)pairs)), dim3(THREADS), (size_t)SMEM,
-                    st, ma, mb, a, v0, splits, per);
+                    st, ma, mb, a, v0);
 }
 
 }  // namespace
@@ -313,7 +337,7 @@ bool vocab_tc_supported(const VocabArgs &a) {
 
 void plan_vocab_tc(VocabArgs *a, bool backward, int n_sm) {
     a->pad = ceil_div(a->n, TM) * TM;
-    a->planes = 1;
+    a->pairs = n_sm / 2 > 0 ? n_sm / 2 : 1;
     const int tiles = ceil_div(a->V, TN);
     a->parts = 2 * tiles;
     a->piece = tiles * TN;
@@ -324,25 +348,16 @@ void plan_vocab_tc(VocabArgs *a, bool backward, int n_sm) {
     a->n_pieces = (int)ceil_div_ll(tiles, most);
     a->piece = ceil_div(tiles, a->n_pieces) * TN;
     a->n_pieces = ceil_div(a->V, a->piece);
-    // few tiles of dh: K is split over the pairs that would be idle
-    const long long t = (long long)(a->pad / TM) * ceil_div(a->d, TN);
-    const int pairs = n_sm / 2 > 0 ? n_sm / 2 : 1, kb = a->piece / BK;
-    int s = t < pairs ? (int)(pairs / t) : 1;
-    if (s > kb / 8) s = kb / 8 > 0 ? kb / 8 : 1;
-    // no split may be empty, of the last, shorter piece neither
-    const int last_kb = ceil_div(a->V - (a->n_pieces - 1) * a->piece, BK);
-    while (s > 1 && ((s - 1) * ceil_div(kb, s) >= kb || (s - 1) * ceil_div(last_kb, s) >= last_kb)) --s;
-    a->planes = s;
 }
 
-cudaError_t launch_vocab_loss_tc(const VocabArgs &a, int n_sm, cudaStream_t st) {
+cudaError_t launch_vocab_loss_tc(const VocabArgs &a, cudaStream_t st) {
     CUtensorMap mh, mw;
     if (!encode_tile_bf16(&mh, a.hc, a.d, a.pad, a.d, 128) || !encode_tile_bf16(&mw, a.w, a.d, a.V, a.ws, 128))
         return cudaErrorInvalidValue;
-    return run<LOSS>(a, mh, mw, 0, n_sm, st);
+    return run<LOSS>(a, mh, mw, 0, st);
 }
 
-cudaError_t launch_vocab_backward_tc(const VocabArgs &a, int n_sm, cudaStream_t st) {
+cudaError_t launch_vocab_backward_tc(const VocabArgs &a, cudaStream_t st) {
     CUtensorMap mh, mw, mg, mwt, mgt, mht;
     if (!encode_tile_bf16(&mh, a.hc, a.d, a.pad, a.d, 128) || !encode_tile_bf16(&mw, a.w, a.d, a.V, a.ws, 128) ||
         !encode_tile_bf16(&mg, a.grad, a.piece, a.pad, a.piece, 128) || !encode_tile_bf16(&mwt, a.w, a.d, a.V, a.ws, 64) ||
@@ -350,9 +365,9 @@ cudaError_t launch_vocab_backward_tc(const VocabArgs &a, int n_sm, cudaStream_t 
         return cudaErrorInvalidValue;
     for (int i = 0; i < a.n_pieces; ++i) {
         const int v0 = i * a.piece;
-        cudaError_t e = run<GRAD>(a, mh, mw, v0, n_sm, st);
-        if (e == cudaSuccess) e = run<DH>(a, mg, mwt, v0, n_sm, st);
-        if (e == cudaSuccess && a.dw) e = run<DW>(a, mgt, mht, v0, n_sm, st);
+        cudaError_t e = run<GRAD>(a, mh, mw, v0, st);
+        if (e == cudaSuccess) e = run<DH>(a, mg, mwt, v0, st);
+        if (e == cudaSuccess && a.dw) e = run<DW>(a, mgt, mht, v0, st);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
