@@ -12,8 +12,7 @@ namespace sp {
 
 namespace {
 
-constexpr int MAX_CH = 4;        // 8-element chunks of a row a thread holds
-constexpr int LOOP_THREADS = 256;
+constexpr int LOOP_THREADS = 256, MAX_THREADS = 512;
 
 // rstd as a power of two times a float: rows whose squares leave fp32 still have a norm.
 struct Rstd {
@@ -34,30 +33,54 @@ __device__ __forceinline__ bool out_of_range(float sq, float eps) {
     return sq > 1.3e36f || (sq < 8.7e-19f && eps < 9.1e-13f);  // (2^120, 2^-60, 2^-40)
 }
 
-// Sums (or maxima) of two values over the TPR threads of a row; every thread gets them.
-template <int TPR, bool MAX = false, typename T>
-__device__ __forceinline__ void reduce2(T &a, T &b, T (*buf)[2]) {
+// Sums (or maxima) of two values over the threads of a row (a warp, or WARP = false: the block);
+// every thread gets them.  Uses of buf one after another alternate between its halves: a barrier a use.
+template <bool WARP, bool MAX = false, typename T>
+__device__ __forceinline__ void reduce2(T &a, T &b, T (*buf)[32][2], int &half) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         const T x = __shfl_xor_sync(0xffffffffu, a, o), y = __shfl_xor_sync(0xffffffffu, b, o);
         a = MAX ? max(a, x) : a + x;
         b = MAX ? max(b, y) : b + y;
     }
-    if constexpr (TPR > 32) {
-        constexpr int W = TPR / 32;
-        const int warp = threadIdx.x >> 5, first = warp / W * W;
-        __syncthreads();  // (an earlier use is read)
-        if ((threadIdx.x & 31) == 0) buf[warp][0] = a, buf[warp][1] = b;
+    if constexpr (!WARP) {
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+        if (lane == 0) buf[half][warp][0] = a, buf[half][warp][1] = b;
         __syncthreads();
-        a = buf[first][0], b = buf[first][1];
+        a = lane < warps ? buf[half][lane][0] : T(0), b = lane < warps ? buf[half][lane][1] : T(0);  // (maxima are >= 0)
+        half ^= 1;
 #pragma unroll
-        for (int w = 1; w < W; ++w) {
-            a = MAX ? max(a, buf[first + w][0]) : a + buf[first + w][0];
-            b = MAX ? max(b, buf[first + w][1]) : b + buf[first + w][1];
+        for (int o = 16; o; o >>= 1) {
+            const T x = __shfl_xor_sync(0xffffffffu, a, o), y = __shfl_xor_sync(0xffffffffu, b, o);
+            a = MAX ? max(a, x) : a + x;
+            b = MAX ? max(b, y) : b + y;
         }
     }
 }
 
+// Eight elements as they lie in memory.
+template <typename T>
+struct Raw {
+    uint4 u[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T *p) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) u[i] = *(const uint4 *)(p + i * (16 / (int)sizeof(T)));
+    }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) u[i] = make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        if constexpr (sizeof(T) == 4) {
+            v[0] = __uint_as_float(u[0].x), v[1] = __uint_as_float(u[0].y), v[2] = __uint_as_float(u[0].z), v[3] = __uint_as_float(u[0].w);
+            v[4] = __uint_as_float(u[1].x), v[5] = __uint_as_float(u[1].y), v[6] = __uint_as_float(u[1].z), v[7] = __uint_as_float(u[1].w);
+        } else {
+            const uint32_t w[4] = {u[0].x, u[0].y, u[0].z, u[0].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+};
 template <typename T>
 __device__ __forceinline__ void store8(T *p, const float (&v)[8]) {
     if constexpr (sizeof(T) == 4) {
@@ -78,93 +101,98 @@ __device__ __forceinline__ void gain8(const float *g, int e, float (&v)[8]) {
 // The 8-bit code of a value times the row's factor; what is not finite becomes NaN.
 __device__ __forceinline__ float code_in(float v, float f) { return isfinite(v) ? v * f : NAN; }
 
-// TPR threads a row, CH chunks a thread.
-template <typename T, int TPR, int CH, bool E8>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) norm_kernel(const __grid_constant__ NormArgs a) {
-    constexpr int BLOCK = TPR < 128 ? 128 : TPR;
-    __shared__ float buf[BLOCK / 32][2];
-    __shared__ double dbuf[BLOCK / 32][2];
+// A row a block (WARP: a warp), CH chunks a thread; rows gridDim apart, the next one's loads under
+// way while this one is reduced and written.
+template <typename T, bool WARP, int CH, bool E8>
+__global__ void __launch_bounds__(WARP ? 128 : MAX_THREADS) norm_kernel(const __grid_constant__ NormArgs a) {
+    __shared__ float buf[2][32][2];
+    __shared__ double dbuf[2][32][2];
+    int half = 0, dhalf = 0;
     pdl_wait();
     pdl_trigger();
-    const int t = threadIdx.x % TPR;
-    const long long row = (long long)blockIdx.x * (BLOCK / TPR) + threadIdx.x / TPR;
-    const bool live = row < a.n;
-    float v[CH][8];
-    float sq = 0.f, none = 0.f;
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        const int e = (c * TPR + t) * 8;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[c][i] = 0.f;
-        if (live && e < a.d) load8((const T *)a.x + row * a.xs + e, v[c]);
-    }
-    if (a.r) {
-        float r[CH][8];
+    const int tpr = WARP ? 32 : blockDim.x, t = WARP ? threadIdx.x & 31 : threadIdx.x;
+    const int rows_b = WARP ? blockDim.x >> 5 : 1;
+    const long long step = (long long)gridDim.x * rows_b;
+    long long row = (long long)blockIdx.x * rows_b + (WARP ? threadIdx.x >> 5 : 0);
+    Raw<T> x[CH], r[CH];
+    const auto load = [&](long long at) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int e = (c * TPR + t) * 8;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) r[c][i] = 0.f;
-            if (live && e < a.d) load8((const T *)a.r + row * a.rs + e, r[c]);
+            const int e = (c * tpr + t) * 8;
+            x[c].zero();
+            r[c].zero();
+            if (e < a.d) {
+                x[c].load((const T *)a.x + at * a.xs + e);
+                if (a.r) r[c].load((const T *)a.r + at * a.rs + e);
+            }
         }
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] += r[c][i];
-    }
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sq += v[c][i] * v[c][i];
-    reduce2<TPR>(sq, none, buf);
-    Rstd rs{1.f, rsqrtf(sq / (float)a.d + a.eps)};
-    // (a verdict of the block: reduce2 meets at its barriers)
-    if (__syncthreads_or(out_of_range(sq, a.eps))) {
-        double q = 0.0, z = 0.0;
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) q += (double)v[c][i] * v[c][i];
-        reduce2<TPR>(q, z, dbuf);
-        if (out_of_range(sq, a.eps)) rs = rstd_of(q / a.d + a.eps);
-    }
-    float amax = 0.f;
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        const int e = (c * TPR + t) * 8;
-        if (!live || e >= a.d) continue;
-        if (a.sum) store8((T *)a.sum + row * a.ss + e, v[c]);
-        float g[8];
-        gain8(a.gain, e, g);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[c][i] = rs.of(v[c][i]) * g[i];
-            if (E8 && isfinite(v[c][i])) amax = fmaxf(amax, fabsf(v[c][i]));
-        }
-        if constexpr (!E8) store8((T *)a.y + row * a.ys + e, v[c]);
-    }
-    if constexpr (E8) {
-        reduce2<TPR, true>(amax, none, buf);
-        amax = fmaxf(amax, kMinAmax);
-        const float f = kMaxCode / amax;
+    };
+    if (row < a.n) load(row);
+    for (; row < a.n; row += step) {
+        float v[CH][8];
+        float sq = 0.f, none = 0.f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int e = (c * TPR + t) * 8;
-            if (!live || e >= a.d) continue;
-            uint32_t w[4];
+            float z[8];
+            x[c].get(v[c]);
+            r[c].get(z);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = float_to_codes2(code_in(v[c][2 * i], f), code_in(v[c][2 * i + 1], f));
-            *(uint2 *)((uint8_t *)a.y + row * a.ys + e) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+            for (int i = 0; i < 8; ++i) {
+                v[c][i] += z[i];
+                sq += v[c][i] * v[c][i];
+            }
         }
-        if (live && t == 0) a.y_scale[row] = amax * (1.f / kMaxCode);
+        if (row + step < a.n) load(row + step);
+        reduce2<WARP>(sq, none, buf, half);
+        Rstd rs{1.f, rsqrtf(sq / (float)a.d + a.eps)};
+        if (out_of_range(sq, a.eps)) {  // (the same for the row's threads)
+            double q = 0.0, z = 0.0;
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) q += (double)v[c][i] * v[c][i];
+            reduce2<WARP>(q, z, dbuf, dhalf);
+            rs = rstd_of(q / a.d + a.eps);
+        }
+        float amax = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int e = (c * tpr + t) * 8;
+            if (e >= a.d) continue;
+            if (a.sum) store8((T *)a.sum + row * a.ss + e, v[c]);
+            float g[8];
+            gain8(a.gain, e, g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[c][i] = rs.of(v[c][i]) * g[i];
+                if (E8 && isfinite(v[c][i])) amax = fmaxf(amax, fabsf(v[c][i]));
+            }
+            if constexpr (!E8) store8((T *)a.y + row * a.ys + e, v[c]);
+        }
+        if constexpr (E8) {
+            reduce2<WARP, true>(amax, none, buf, half);
+            amax = fmaxf(amax, kMinAmax);
+            const float f = kMaxCode / amax;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int e = (c * tpr + t) * 8;
+                if (e >= a.d) continue;
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = float_to_codes2(code_in(v[c][2 * i], f), code_in(v[c][2 * i + 1], f));
+                *(uint2 *)((uint8_t *)a.y + row * a.ys + e) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+            }
+            if (t == 0) a.y_scale[row] = amax * (1.f / kMaxCode);
+        }
     }
 }
 
 // Rows of any length and alignment: an element a thread, the row read again for each use.
 template <typename T>
 __global__ void __launch_bounds__(LOOP_THREADS) norm_loop_kernel(const __grid_constant__ NormArgs a) {
-    __shared__ float buf[LOOP_THREADS / 32][2];
-    __shared__ double dbuf[LOOP_THREADS / 32][2];
+    __shared__ float buf[2][32][2];
+    __shared__ double dbuf[2][32][2];
+    int half = 0, dhalf = 0;
     pdl_wait();
     pdl_trigger();
     const long long row = blockIdx.x;
@@ -176,7 +204,7 @@ __global__ void __launch_bounds__(LOOP_THREADS) norm_loop_kernel(const __grid_co
         const float v = value(e);
         sq += v * v;
     }
-    reduce2<LOOP_THREADS>(sq, none, buf);
+    reduce2<false>(sq, none, buf, half);
     Rstd rs{1.f, rsqrtf(sq / (float)a.d + a.eps)};
     if (out_of_range(sq, a.eps)) {  // (the same for all threads)
         double q = 0.0, z = 0.0;
@@ -184,7 +212,7 @@ __global__ void __launch_bounds__(LOOP_THREADS) norm_loop_kernel(const __grid_co
             const double v = value(e);
             q += v * v;
         }
-        reduce2<LOOP_THREADS>(q, z, dbuf);
+        reduce2<false>(q, z, dbuf, dhalf);
         rs = rstd_of(q / a.d + a.eps);
     }
     float amax = 0.f;
@@ -194,7 +222,7 @@ __global__ void __launch_bounds__(LOOP_THREADS) norm_loop_kernel(const __grid_co
             const float y = normed(value(e), rs, e);
             if (isfinite(y)) amax = fmaxf(amax, fabsf(y));
         }
-        reduce2<LOOP_THREADS, true>(amax, none, buf);
+        reduce2<false, true>(amax, none, buf, half);
         amax = fmaxf(amax, kMinAmax);
         if (threadIdx.x == 0) a.y_scale[row] = amax * (1.f / kMaxCode);
     }
@@ -207,99 +235,101 @@ __global__ void __launch_bounds__(LOOP_THREADS) norm_loop_kernel(const __grid_co
     }
 }
 
-// Backward: a block walks rows gridDim apart; a thread keeps its columns' part of the gain's gradient.
-template <typename T, int TPR, int CH>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) norm_back_kernel(const __grid_constant__ NormBackArgs a) {
-    constexpr int BLOCK = TPR < 128 ? 128 : TPR, RPB = BLOCK / TPR;
-    __shared__ float buf[BLOCK / 32][2];
-    __shared__ double dbuf[BLOCK / 32][2];
+// Backward, likewise; a thread keeps its columns' part of the gain's gradient, and the gain.
+template <typename T, bool WARP, int CH>
+__global__ void __launch_bounds__(WARP ? 128 : MAX_THREADS) norm_back_kernel(const __grid_constant__ NormBackArgs a) {
+    __shared__ float buf[2][32][2];
+    __shared__ double dbuf[2][32][2];
+    int half = 0, dhalf = 0;
     pdl_wait();
     pdl_trigger();
-    const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-    float dg[CH][8];
+    const int tpr = WARP ? 32 : blockDim.x, t = WARP ? threadIdx.x & 31 : threadIdx.x;
+    const int rows_b = WARP ? blockDim.x >> 5 : 1;
+    const long long step = (long long)gridDim.x * rows_b;
+    const long long first = (long long)blockIdx.x * rows_b + (WARP ? threadIdx.x >> 5 : 0);
+    float dg[CH][8], g[CH][8];
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+    for (int c = 0; c < CH; ++c) {
+        const int e = (c * tpr + t) * 8;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dg[c][i] = 0.f;
-    // (the same number of steps for all threads: they meet at barriers)
-    for (long long first = (long long)blockIdx.x * RPB; first < a.n; first += (long long)gridDim.x * RPB) {
-        const long long row = first + sub;
-        const bool live = row < a.n;
-        float s[CH][8], y[CH][8];
+        for (int i = 0; i < 8; ++i) dg[c][i] = g[c][i] = 0.f;
+        if (e < a.d) gain8(a.gain, e, g[c]);
+    }
+    Raw<T> rs_[CH], ry[CH], rd[CH];
+    const auto load = [&](long long at) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int e = (c * TPR + t) * 8;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s[c][i] = y[c][i] = 0.f;
-            if (live && e < a.d) {
-                load8((const T *)a.s + row * a.ss + e, s[c]);
-                load8((const T *)a.dy + row * a.ys + e, y[c]);
+            const int e = (c * tpr + t) * 8;
+            rs_[c].zero();
+            ry[c].zero();
+            if (e < a.d) {
+                rs_[c].load((const T *)a.s + at * a.ss + e);
+                ry[c].load((const T *)a.dy + at * a.ys + e);
             }
         }
+    };
+    if (first < a.n) load(first);
+    for (long long row = first; row < a.n; row += step) {
+        float s[CH][8], y[CH][8];
         float sq = 0.f, dot = 0.f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int e = (c * TPR + t) * 8;
-            float g[8];
-            if (e < a.d) gain8(a.gain, e, g);
+            const int e = (c * tpr + t) * 8;
+            rd[c].zero();
+            if (a.ds && e < a.d) rd[c].load((const T *)a.ds + row * a.rs + e);
+            rs_[c].get(s[c]);
+            ry[c].get(y[c]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (e >= a.d) g[i] = 0.f;
                 sq += s[c][i] * s[c][i];
-                dot += y[c][i] * g[i] * s[c][i];
+                dot += y[c][i] * g[c][i] * s[c][i];
             }
         }
-        reduce2<TPR>(sq, dot, buf);
+        if (row + step < a.n) load(row + step);
+        reduce2<WARP>(sq, dot, buf, half);
         Rstd rs{1.f, rsqrtf(sq / (float)a.d + a.eps)};
         float m = rs.f2 * dot / (float)a.d;
-        if (__syncthreads_or(out_of_range(sq, a.eps) || !isfinite(m))) {
+        if (out_of_range(sq, a.eps) || !isfinite(m)) {  // (the same for the row's threads)
             double q = 0.0, z = 0.0;
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                const int e = (c * TPR + t) * 8;
-                float g[8];
-                if (e < a.d) gain8(a.gain, e, g);
+            for (int c = 0; c < CH; ++c)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     q += (double)s[c][i] * s[c][i];
-                    if (e < a.d) z += (double)y[c][i] * g[i] * s[c][i];
+                    z += (double)y[c][i] * g[c][i] * s[c][i];
                 }
-            }
-            reduce2<TPR>(q, z, dbuf);
-            if (out_of_range(sq, a.eps) || !isfinite(m)) {
-                rs = rstd_of(q / a.d + a.eps);
-                m = (float)(z / a.d * rs.f1 * rs.f2);
-            }
+            reduce2<WARP>(q, z, dbuf, dhalf);
+            rs = rstd_of(q / a.d + a.eps);
+            m = (float)(z / a.d * rs.f1 * rs.f2);
         }
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int e = (c * TPR + t) * 8;
-            if (!live || e >= a.d) continue;
-            float g[8], ds[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (a.ds) load8((const T *)a.ds + row * a.rs + e, ds);
-            gain8(a.gain, e, g);
+            const int e = (c * tpr + t) * 8;
+            float ds[8];
+            rd[c].get(ds);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float xh = rs.of(s[c][i]);
                 dg[c][i] += y[c][i] * xh;
-                ds[i] += rs.of(y[c][i] * g[i] - xh * m);
+                ds[i] += rs.of(y[c][i] * g[c][i] - xh * m);
             }
-            store8((T *)a.dx + row * a.xs + e, ds);
+            if (e < a.d) store8((T *)a.dx + row * a.xs + e, ds);
         }
     }
     if (a.dgain) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int e = (c * TPR + t) * 8;
-            if (e < a.d) store8(a.part + ((size_t)blockIdx.x * RPB + sub) * a.d + e, dg[c]);
+            const int e = (c * tpr + t) * 8;
+            if (e < a.d) store8(a.part + first * a.d + e, dg[c]);
         }
     }
 }
 
 template <typename T>
 __global__ void __launch_bounds__(LOOP_THREADS) norm_back_loop_kernel(const __grid_constant__ NormBackArgs a) {
-    __shared__ float buf[LOOP_THREADS / 32][2];
-    __shared__ double dbuf[LOOP_THREADS / 32][2];
+    __shared__ float buf[2][32][2];
+    __shared__ double dbuf[2][32][2];
+    int half = 0, dhalf = 0;
     pdl_wait();
     pdl_trigger();
     float *part = a.part + (size_t)blockIdx.x * a.d;
@@ -313,7 +343,7 @@ __global__ void __launch_bounds__(LOOP_THREADS) norm_back_loop_kernel(const __gr
             sq += v * v;
             dot += to_f(dy[e]) * (a.gain ? a.gain[e] : 1.f) * v;
         }
-        reduce2<LOOP_THREADS>(sq, dot, buf);
+        reduce2<false>(sq, dot, buf, half);
         Rstd rs{1.f, rsqrtf(sq / (float)a.d + a.eps)};
         float m = rs.f2 * dot / (float)a.d;
         if (out_of_range(sq, a.eps) || !isfinite(m)) {  // (the same for all threads)
@@ -323,7 +353,7 @@ __global__ void __launch_bounds__(LOOP_THREADS) norm_back_loop_kernel(const __gr
                 q += v * v;
                 z += (double)to_f(dy[e]) * (a.gain ? a.gain[e] : 1.f) * v;
             }
-            reduce2<LOOP_THREADS>(q, z, dbuf);
+            reduce2<false>(q, z, dbuf, dhalf);
             rs = rstd_of(q / a.d + a.eps);
             m = (float)(z / a.d * rs.f1 * rs.f2);
         }
@@ -337,8 +367,8 @@ __global__ void __launch_bounds__(LOOP_THREADS) norm_back_loop_kernel(const __gr
 }
 
 // dg: the partial rows added in their order, a column a thread of the first warp's
-// lanes, the rows split over eight warps whose sums are added in order.
-constexpr int SUM_WARPS = 8;
+// lanes, the rows split over 32 warps whose sums are added in order.
+constexpr int SUM_WARPS = 32;
 __global__ void __launch_bounds__(32 * SUM_WARPS) norm_gain_kernel(const float *part, int parts, int d, float *dgain) {
     __shared__ float sums[SUM_WARPS][32];
     pdl_wait();
@@ -359,79 +389,62 @@ __global__ void __launch_bounds__(32 * SUM_WARPS) norm_gain_kernel(const float *
     }
 }
 
-// Threads a row and chunks a thread: the fewest threads (a multiple of a warp, a power of two) that
-// hold a row in up to four chunks; 0: too long.
+// Rows of up to 1024 elements a warp, up to 16384 a block, two chunks a thread while that is enough;
+// threads 0: longer ones.
 struct Shape {
-    int tpr, ch;
+    bool warp;
+    int threads, ch, rows;  // of a block
 };
+constexpr Shape kLoop{false, LOOP_THREADS, 0, 1};
 Shape shape_of(int d) {
     const int chunks = ceil_div(d, 8);
-    int tpr = 32;
-    while (tpr < 1024 && tpr * 2 < chunks) tpr *= 2;  // two chunks a thread until 1024 threads
-    const int ch = ceil_div(chunks, tpr);
-    return Shape{ch <= MAX_CH ? tpr : 0, ch <= 1 ? 1 : ch <= 2 ? 2 : 4};
+    if (chunks <= 128) return Shape{true, 128, chunks <= 32 ? 1 : chunks <= 64 ? 2 : 4, 4};
+    const int ch = chunks <= 2 * MAX_THREADS ? 2 : 4, threads = ceil_div(ceil_div(chunks, ch), 32) * 32;
+    return threads <= MAX_THREADS ? Shape{false, threads, ch, 1} : Shape{false, 0, 0, 1};
 }
 bool whole16(const void *p, long long stride, int es) { return !(((uintptr_t)p | (uintptr_t)(stride * es)) & 15); }
 
-template <typename T, int TPR, int CH>
-cudaError_t run_norm(const NormArgs &a, cudaStream_t st) {
-    constexpr int BLOCK = TPR < 128 ? 128 : TPR;
-    const dim3 grid((unsigned)ceil_div_ll(a.n, BLOCK / TPR));
-    if (a.out_dtype == SP_E4M3) return launch_k(norm_kernel<T, TPR, CH, true>, grid, dim3(BLOCK), 0, st, a);
-    return launch_k(norm_kernel<T, TPR, CH, false>, grid, dim3(BLOCK), 0, st, a);
+// Blocks that walk `n` rows, `per_sm` threads an SM.
+int blocks_of(const Shape &s, long long n, int n_sm, int per_sm) {
+    const long long all = ceil_div_ll(n, s.rows), held = (long long)n_sm * (per_sm / s.threads > 1 ? per_sm / s.threads : 1);
+    return (int)(all < held ? all : held);
 }
-template <typename T, int TPR, int CH>
-cudaError_t run_back(const NormBackArgs &a, int parts, cudaStream_t st) {
-    constexpr int BLOCK = TPR < 128 ? 128 : TPR;
-    return launch_k(norm_back_kernel<T, TPR, CH>, dim3(parts / (BLOCK / TPR)), dim3(BLOCK), 0, st, a);
-}
-// f(TPR, CH) of a shape
-#define SP_NORM_SHAPES(CALL)                                                                       \
-    switch (s.tpr) {                                                                               \
-    case 32: return s.ch == 1 ? CALL(32, 1) : CALL(32, 2);                                         \
-    case 64: return CALL(64, 2);                                                                   \
-    case 128: return CALL(128, 2);                                                                 \
-    case 256: return CALL(256, 2);                                                                 \
-    case 512: return CALL(512, 2);                                                                 \
-    default: return s.ch <= 2 ? CALL(1024, 2) : CALL(1024, 4);                                     \
-    }
-template <typename T>
-cudaError_t norm_shapes(const NormArgs &a, Shape s, cudaStream_t st) {
-#define SP_CALL(TPR, CH) run_norm<T, TPR, CH>(a, st)
-    SP_NORM_SHAPES(SP_CALL)
-#undef SP_CALL
+constexpr int FWD_THREADS = 1024, BACK_THREADS = 640;
+template <typename T, bool E8>
+cudaError_t norm_shapes(const NormArgs &a, const Shape &s, int n_sm, cudaStream_t st) {
+    const auto k = s.warp ? s.ch == 1 ? norm_kernel<T, true, 1, E8> : s.ch == 2 ? norm_kernel<T, true, 2, E8> : norm_kernel<T, true, 4, E8>
+                          : s.ch == 2 ? norm_kernel<T, false, 2, E8> : norm_kernel<T, false, 4, E8>;
+    return launch_k(k, dim3(blocks_of(s, a.n, n_sm, FWD_THREADS)), dim3(s.threads), 0, st, a);
 }
 template <typename T>
-cudaError_t back_shapes(const NormBackArgs &a, Shape s, int parts, cudaStream_t st) {
-#define SP_CALL(TPR, CH) run_back<T, TPR, CH>(a, parts, st)
-    SP_NORM_SHAPES(SP_CALL)
-#undef SP_CALL
+cudaError_t back_shapes(const NormBackArgs &a, const Shape &s, int n_sm, cudaStream_t st) {
+    const auto k = s.warp ? s.ch == 1 ? norm_back_kernel<T, true, 1> : s.ch == 2 ? norm_back_kernel<T, true, 2> : norm_back_kernel<T, true, 4>
+                          : s.ch == 2 ? norm_back_kernel<T, false, 2> : norm_back_kernel<T, false, 4>;
+    return launch_k(k, dim3(blocks_of(s, a.n, n_sm, BACK_THREADS)), dim3(s.threads), 0, st, a);
 }
-#undef SP_NORM_SHAPES
 
 }  // namespace
 
-cudaError_t launch_norm(const NormArgs &a, cudaStream_t st) {
+cudaError_t launch_norm(const NormArgs &a, int n_sm, cudaStream_t st) {
     const int es = a.dtype == SP_F32 ? 4 : 2;
     const bool e8 = a.out_dtype == SP_E4M3;
     const bool y_whole = e8 ? !(((uintptr_t)a.y | (uintptr_t)a.ys) & 7) : whole16(a.y, a.ys, es);
     const bool vec = a.d % 8 == 0 && whole16(a.x, a.xs, es) && (!a.r || whole16(a.r, a.rs, es)) &&
                      (!a.sum || whole16(a.sum, a.ss, es)) && y_whole && whole16(a.gain, 0, 4);
     const Shape s = shape_of(a.d);
-    if (!vec || !s.tpr) {
+    if (!vec || !s.threads) {
         if (a.dtype == SP_F32) return launch_k(norm_loop_kernel<float>, dim3(a.n), dim3(LOOP_THREADS), 0, st, a);
         return launch_k(norm_loop_kernel<bf16>, dim3(a.n), dim3(LOOP_THREADS), 0, st, a);
     }
-    return a.dtype == SP_F32 ? norm_shapes<float>(a, s, st) : norm_shapes<bf16>(a, s, st);
+    if (e8) return a.dtype == SP_F32 ? norm_shapes<float, true>(a, s, n_sm, st) : norm_shapes<bf16, true>(a, s, n_sm, st);
+    return a.dtype == SP_F32 ? norm_shapes<float, false>(a, s, n_sm, st) : norm_shapes<bf16, false>(a, s, n_sm, st);
 }
 
-// A multiple of the rows that a block takes at once, for both kinds of kernel.
 int norm_back_parts(int n, int d, int n_sm) {
-    const Shape s = shape_of(d);
-    const int tpr = s.tpr ? s.tpr : LOOP_THREADS, rpb = tpr < 128 ? 128 / tpr : 1;
-    const int per_sm = tpr <= 128 ? 8 : tpr >= 1024 ? 1 : 1024 / tpr;
-    const long long blocks = ceil_div_ll(n, rpb);
-    return (int)(blocks < (long long)n_sm * per_sm ? blocks : (long long)n_sm * per_sm) * rpb;
+    Shape s = shape_of(d);
+    if (!s.threads) s = kLoop;
+    const int held = blocks_of(s, n, n_sm, BACK_THREADS) * s.rows, loop = blocks_of(kLoop, n, n_sm, BACK_THREADS);
+    return held > loop ? held : loop;  // (which kernel it is depends on the alignment)
 }
 
 cudaError_t launch_norm_backward(const NormBackArgs &a, int n_sm, cudaStream_t st) {
@@ -439,13 +452,15 @@ cudaError_t launch_norm_backward(const NormBackArgs &a, int n_sm, cudaStream_t s
     const bool vec = a.d % 8 == 0 && whole16(a.dx, a.xs, es) && (!a.ds || whole16(a.ds, a.rs, es)) &&
                      whole16(a.s, a.ss, es) && whole16(a.dy, a.ys, es) && whole16(a.gain, 0, 4);
     const Shape s = shape_of(a.d);
-    const int parts = norm_back_parts(a.n, a.d, n_sm);
+    const bool loop = !vec || !s.threads;
+    int parts = blocks_of(loop ? kLoop : s, a.n, n_sm, BACK_THREADS);
     cudaError_t e;
-    if (!vec || !s.tpr) {
+    if (loop) {
         const auto k = a.dtype == SP_F32 ? norm_back_loop_kernel<float> : norm_back_loop_kernel<bf16>;
         e = launch_k(k, dim3(parts), dim3(LOOP_THREADS), 0, st, a);
     } else {
-        e = a.dtype == SP_F32 ? back_shapes<float>(a, s, parts, st) : back_shapes<bf16>(a, s, parts, st);
+        e = a.dtype == SP_F32 ? back_shapes<float>(a, s, n_sm, st) : back_shapes<bf16>(a, s, n_sm, st);
+        parts *= s.rows;
     }
     if (e != cudaSuccess || !a.dgain) return e;
     return launch_k(norm_gain_kernel, dim3(ceil_div(a.d, 32)), dim3(32 * SUM_WARPS), 0, st, (const float *)a.part, parts, a.d,

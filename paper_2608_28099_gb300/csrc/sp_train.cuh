@@ -26,7 +26,7 @@ struct NormBackArgs {
     float *dgain;                  // or NULL
     float *part;                   // [norm_back_parts][d], for dgain
 };
-cudaError_t launch_norm(const NormArgs &a, cudaStream_t st);
+cudaError_t launch_norm(const NormArgs &a, int n_sm, cudaStream_t st);
 // Partial rows of the gain's gradient.
 int norm_back_parts(int n, int d, int n_sm);
 cudaError_t launch_norm_backward(const NormBackArgs &a, int n_sm, cudaStream_t st);

@@ -125,7 +125,7 @@ sp_status sp_norm(sp_stream stream, const sp_norm_dims *dims, const void *d_x, c
         return fail(SP_ERR_INVALID_ARG, "outputs overlap each other or, in another stride or type, their inputs");
     NormArgs a{dims->n_rows, dims->d, dims->dtype, dims->out_dtype, dims->eps, st[0], st[1], st[2], st[3], d_x, d_residual,
                d_gain, d_sum, d_y, d_y_scale};
-    return launched(launch_norm(a, (cudaStream_t)stream), "sp_norm");
+    return launched(launch_norm(a, sm_count(), (cudaStream_t)stream), "sp_norm");
 }
 
 size_t sp_norm_backward_workspace_bytes(const sp_norm_dims *dims) {
