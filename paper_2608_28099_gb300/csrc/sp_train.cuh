@@ -50,8 +50,10 @@ struct VocabArgs {
     // workspace
     int *count;                    // tokens kept
     VocabRow *rows;                // [n]
-    bf16 *hc;                      // tensor cores: [pad][d] kept tokens' rows, then zeros
+    void *hc;                      // [pad][d] kept tokens' rows (tensor cores: then zeros)
+    int tensor;                    // which kernels
     int pad;                       // n rounded up to whole tiles
+    int tn;                        // forward, tensor cores: vocabulary rows of a tile
     float2 *part;                  // forward: [n][parts] (max, sum of exponentials) of a piece of the vocabulary
     float *at;                     // forward: [n] the target's logit
     int parts;
@@ -71,11 +73,12 @@ struct Splits {
 __host__ __device__ inline Splits split_count(int m_tiles, int n_tiles, int kb, int units, float plane) {
     Splits best{1, kb};
     float least = 3e38f;
-    const long long tiles = (long long)m_tiles * n_tiles;
+    if ((long long)m_tiles * n_tiles >= 8ll * units) return best;
+    const int tiles = m_tiles * n_tiles;
     for (int s = 1; s <= 16; ++s) {
         const int per = ceil_div(kb, s);
-        if ((s > 1 && tiles * (s - 1) >= 8ll * units) || (s - 1) * per >= kb) continue;
-        const float cost = (float)ceil_div_ll(tiles * s, units) * (float)(per + 4) + plane * (float)(s - 1) * (float)tiles / (float)units;
+        if (tiles * (s - 1) >= 8 * units || (s - 1) * per >= kb) continue;
+        const float cost = (float)ceil_div(tiles * s, units) * (float)(per + 4) + plane * (float)(s - 1) * (float)tiles / (float)units;
         if (cost < least) least = cost, best = Splits{s, per};
     }
     return best;
@@ -93,19 +96,19 @@ cudaError_t launch_vocab_backward_tc(const VocabArgs &a, cudaStream_t st);
 cudaError_t launch_vocab_keep(const VocabArgs &a, bool backward, cudaStream_t st);
 cudaError_t launch_vocab_finish_loss(const VocabArgs &a, cudaStream_t st);
 cudaError_t launch_vocab_finish_dh(const VocabArgs &a, cudaStream_t st);
-// dh's tiles and their splits for `count` kept tokens, by either kind of kernel (hc: tensor cores).
+// dh's tiles and their splits for `count` kept tokens, by either kind of kernel.
 struct DhPlan {
     int m_tiles, rows;
     Splits k;
 };
 __host__ __device__ inline DhPlan dh_plan(const VocabArgs &a, int count) {
-    const int tm = a.hc ? 256 : 64, tn = tm, bk = a.hc ? 64 : 16, piece = a.piece < a.V ? a.piece : a.V;
+    const int tm = a.tensor ? 256 : 64, tn = tm, bk = a.tensor ? 64 : 32, piece = a.piece < a.V ? a.piece : a.V;
     DhPlan p;
     p.m_tiles = ceil_div(count < 1 ? 1 : count, tm);
     p.rows = p.m_tiles * tm;
     // (a k-block of 256 x 256 x 64 takes a pair 0.27 us, in which two passes over 0.3 tiles of fp32 partials fit
-    // the HBM's share of a pair; of 64 x 64 x 16 some 0.5 us, which a partial does not weigh against)
-    p.k = split_count(p.m_tiles, ceil_div(a.d, tn), ceil_div(piece, bk), a.pairs, a.hc ? 24.f : 2.f);
+    // the HBM's share of a pair; of 64 x 64 x 32 some 0.7 us, which a partial does not weigh against)
+    p.k = split_count(p.m_tiles, ceil_div(a.d, tn), ceil_div(piece, bk), a.pairs, a.tensor ? 24.f : 2.f);
     return p;
 }
 

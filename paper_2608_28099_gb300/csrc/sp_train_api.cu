@@ -54,7 +54,7 @@ sp_status check_vocab(const sp_vocab_dims *d, bool backward, VocabArgs *a) {
     if (a->n == 0) return SP_OK;
     if (tensor) plan_vocab_tc(a, backward, sm_count());
     else plan_vocab_simt(a, backward, sm_count());
-    a->hc = tensor ? (bf16 *)256 : nullptr;  // (placed by lay_out)
+    a->tensor = tensor;
     if (backward) {
         // most rows of partial dh for any number of kept tokens (see split_count)
         const long long tm = tensor ? 256 : 64, m_tiles = ceil_div_ll(a->n, tm);
@@ -67,7 +67,7 @@ sp_status check_vocab(const sp_vocab_dims *d, bool backward, VocabArgs *a) {
 // Places the workspace's parts from `base` on; returns their bytes (never 0: that answers an error).
 size_t lay_out(VocabArgs *a, bool backward, char *base) {
     size_t at = 0;
-    const bool tensor = a->hc != nullptr;
+    const size_t es = elem_bytes(a->dtype);
     const auto take = [&](size_t bytes) {
         char *p = base + at;
         at += align256(bytes);
@@ -75,12 +75,12 @@ size_t lay_out(VocabArgs *a, bool backward, char *base) {
     };
     a->count = (int *)take(sizeof(int));
     a->rows = (VocabRow *)take((size_t)a->n * sizeof(VocabRow));
-    if (tensor) a->hc = (bf16 *)take((size_t)a->pad * a->d * sizeof(bf16));
+    a->hc = take((size_t)a->pad * a->d * es);
     if (!backward) {
         a->part = (float2 *)take((size_t)a->n * a->parts * sizeof(float2));
         a->at = (float *)take((size_t)a->n * sizeof(float));
     } else {
-        a->grad = take((size_t)a->pad * a->piece * (tensor ? sizeof(bf16) : sizeof(float)));
+        a->grad = take((size_t)a->pad * a->piece * (a->tensor ? sizeof(bf16) : sizeof(float)));
         a->acc = (float *)take((size_t)a->acc_rows * a->d * sizeof(float));
     }
     return at;
@@ -89,9 +89,9 @@ size_t lay_out(VocabArgs *a, bool backward, char *base) {
 sp_status check_vocab_buffers(VocabArgs *a, bool backward, const void *d_h, const void *d_w, const int *d_targets,
                               const void *d_dh, const void *d_dw, void *d_workspace, size_t workspace_bytes) {
     if (!d_h || !d_w || !d_targets || !d_workspace) return fail(SP_ERR_INVALID_ARG, "a required pointer is NULL");
-    const size_t to = a->hc ? 16 : elem_bytes(a->dtype);
+    const size_t to = a->tensor ? 16 : elem_bytes(a->dtype);
     if (!aligned(d_h, to) || !aligned(d_w, to) || !aligned(d_dh, to) || !aligned(d_dw, to))
-        return fail(SP_ERR_INVALID_ARG, a->hc ? "h, w and their gradients must be 16-byte aligned (path 1: to their type)"
+        return fail(SP_ERR_INVALID_ARG, a->tensor ? "h, w and their gradients must be 16-byte aligned (path 1: to their type)"
                                               : "h, w and their gradients must be aligned to their type");
     if (!aligned(d_workspace, 256)) return fail(SP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     const size_t need = lay_out(a, backward, (char *)d_workspace);
@@ -183,7 +183,7 @@ sp_status sp_vocab_loss(sp_stream stream, const sp_vocab_dims *dims, const void 
     a.status = d_status;
     const cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e = launch_vocab_keep(a, false, st);
-    if (e == cudaSuccess) e = a.hc ? launch_vocab_loss_tc(a, st) : launch_vocab_loss_simt(a, st);
+    if (e == cudaSuccess) e = a.tensor ? launch_vocab_loss_tc(a, st) : launch_vocab_loss_simt(a, st);
     if (e == cudaSuccess) e = launch_vocab_finish_loss(a, st);
     return launched(e, "sp_vocab_loss");
 }
@@ -215,7 +215,7 @@ sp_status sp_vocab_loss_backward(sp_stream stream, const sp_vocab_dims *dims, co
     a.dw = d_grad_w;
     a.status = d_status;
     cudaError_t e = launch_vocab_keep(a, true, st);
-    if (e == cudaSuccess) e = a.hc ? launch_vocab_backward_tc(a, st) : launch_vocab_backward_simt(a, st);
+    if (e == cudaSuccess) e = a.tensor ? launch_vocab_backward_tc(a, st) : launch_vocab_backward_simt(a, st);
     if (e == cudaSuccess) e = launch_vocab_finish_dh(a, st);
     return launched(e, "sp_vocab_loss_backward");
 }

@@ -18,8 +18,8 @@ constexpr int THREADS = 256, WARPS = THREADS / 32;
 __device__ __forceinline__ bool has_target(int t, int V) { return t >= 0 && t < V; }
 
 // Rows of the products: a token with a target gets the next row.  Every block counts the targets in
-// front of its own `per` tokens and in all (n ints from L2), then copies its rows where they go (bf16,
-// tensor cores), a warp a row, and clears what is known to be 0: losses and gradients of the others, and
+// front of its own `per` tokens and in all (n ints from L2), then copies its rows where they go,
+// a warp a row, and clears what is known to be 0: losses and gradients of the others, and
 // rows behind the last one up to a whole k-block.
 template <typename T>
 __global__ void __launch_bounds__(THREADS) vocab_keep_kernel(const __grid_constant__ VocabArgs a, int per, int backward) {
@@ -80,9 +80,14 @@ __global__ void __launch_bounds__(THREADS) vocab_keep_kernel(const __grid_consta
             if (q < 0) {
                 if (backward)
                     for (int e = lane; e < a.d; e += 32) ((T *)a.dh)[(size_t)(g0 + i) * a.hs + e] = from_f<T>(0.f);
-            } else if (a.hc) {
+            } else if (!a.tensor) {
+                const T *src = (const T *)a.h + (size_t)(g0 + i) * a.hs;
+                T *dst = (T *)a.hc + (size_t)q * a.d;
+#pragma unroll 8
+                for (int e = lane; e < a.d; e += 32) dst[e] = src[e];
+            } else {
                 const uint4 *src = (const uint4 *)((const T *)a.h + (size_t)(g0 + i) * a.hs);
-                uint4 *dst = (uint4 *)(a.hc + (size_t)q * a.d);  // (d is a multiple of 8, rows are aligned)
+                uint4 *dst = (uint4 *)((bf16 *)a.hc + (size_t)q * a.d);  // (d is a multiple of 8, rows are aligned)
                 constexpr int AT_ONCE = 8;
                 for (int e0 = lane; e0 < a.d / 8; e0 += 32 * AT_ONCE) {
                     uint4 v4[AT_ONCE];
@@ -96,10 +101,10 @@ __global__ void __launch_bounds__(THREADS) vocab_keep_kernel(const __grid_consta
             }
         }
     }
-    if (a.hc && backward) {
+    if (a.tensor && backward) {
         const int end = min(a.pad, max(ceil_div(all, 64), 1) * 64);
         for (int p = all + blockIdx.x; p < end; p += gridDim.x)
-            for (int e = threadIdx.x; e < a.d / 8; e += THREADS) *(uint4 *)(a.hc + (size_t)p * a.d + e * 8) = make_uint4(0, 0, 0, 0);
+            for (int e = threadIdx.x; e < a.d / 8; e += THREADS) *(uint4 *)((bf16 *)a.hc + (size_t)p * a.d + e * 8) = make_uint4(0, 0, 0, 0);
     }
 }
 
@@ -150,30 +155,36 @@ __global__ void __launch_bounds__(THREADS) vocab_finish_dh_kernel(const __grid_c
     const float *from = a.acc + (size_t)p * a.d;
     const DhPlan plan = dh_plan(a, *a.count);
     const size_t plane = (size_t)plan.rows * a.d;
-    if (a.hc) {  // (d a multiple of 8, rows aligned)
+    if (a.tensor) {  // (d a multiple of 8, rows aligned)
         for (int e = threadIdx.x * 4; e < a.d; e += THREADS * 4) {
-            float4 s = *(const float4 *)(from + e);
-            for (int q = 1; q < plan.k.s; ++q) {
-                const float4 v = *(const float4 *)(from + q * plane + e);
-                s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+            constexpr int AT_ONCE = 8;  // planes under way together
+            for (int q0 = 0; q0 < plan.k.s; q0 += AT_ONCE) {
+                float4 v[AT_ONCE];
+#pragma unroll
+                for (int q = 0; q < AT_ONCE; ++q)
+                    v[q] = q0 + q < plan.k.s ? __ldcs((const float4 *)(from + (q0 + q) * plane + e)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int q = 0; q < AT_ONCE; ++q) s.x += v[q].x, s.y += v[q].y, s.z += v[q].z, s.w += v[q].w;
             }
             *(uint2 *)((bf16 *)to + e) = make_uint2(pack2_bf16(s.x, s.y), pack2_bf16(s.z, s.w));
         }
     } else {
         for (int e = threadIdx.x; e < a.d; e += THREADS) {
-            float s = from[e];
-            for (int q = 1; q < plan.k.s; ++q) s += from[q * plane + e];
+            float s = 0.f;
+#pragma unroll 8
+            for (int q = 0; q < plan.k.s; ++q) s += from[q * plane + e];
             to[e] = from_f<T>(s);
         }
     }
 }
 
 // ---------------------------------------------------------------------------
-// Products on CUDA cores: C[m][n] = sum_k A(m, k) B(n, k) in 64 x 64 tiles, 16 of K at a time through
+// Products on CUDA cores: C[m][n] = sum_k A(m, k) B(n, k) in 64 x 64 tiles, 32 of K at a time through
 // two buffers in shared memory, the next ones' loads under way beside the products, 4 x 4 elements a
 // thread, fp32 throughout; dh's tiles split along K where they are few.
 enum { LOSS = 0, GRAD = 1, DH = 2, DW = 3 };
-constexpr int BM = 64, BK = 16, LOADS = BM * BK / THREADS;
+constexpr int BM = 64, BK = 32, LOADS = BM * BK / THREADS;
 
 template <typename T, int KIND>
 __global__ void __launch_bounds__(THREADS) vocab_simt_kernel(const __grid_constant__ VocabArgs a, int v0) {
@@ -201,11 +212,11 @@ __global__ void __launch_bounds__(THREADS) vocab_simt_kernel(const __grid_consta
         if (tid < BM) rows[tid] = m0 + tid < count ? a.rows[m0 + tid] : VocabRow{0.f, 0.f, -1, 0};
         __syncthreads();
     }
-    const T *h = (const T *)a.h, *w = (const T *)a.w;
+    const T *h = (const T *)a.hc, *w = (const T *)a.w;
     const float *grad = (const float *)a.grad;
     const auto A = [&](int m, int k) -> float {
         if (m0 + m >= M || k >= k_hi) return 0.f;
-        if (KIND == LOSS || KIND == GRAD) return to_f(h[(size_t)rows[m].token * a.hs + k]);
+        if (KIND == LOSS || KIND == GRAD) return to_f(h[(size_t)(m0 + m) * a.d + k]);
         if (KIND == DH) return grad[(size_t)(m0 + m) * a.piece + k];
         return grad[(size_t)k * a.piece + m0 + m];
     };
@@ -213,7 +224,7 @@ __global__ void __launch_bounds__(THREADS) vocab_simt_kernel(const __grid_consta
         if (n0 + n >= N || k >= k_hi) return 0.f;
         if (KIND == LOSS || KIND == GRAD) return to_f(w[(size_t)(v0 + n0 + n) * a.ws + k]);
         if (KIND == DH) return to_f(w[(size_t)(v0 + k) * a.ws + n0 + n]);
-        return to_f(h[(size_t)a.rows[k].token * a.hs + n0 + n]);
+        return to_f(h[(size_t)k * a.d + n0 + n]);
     };
     // neighbouring threads along whichever index is contiguous in memory
     const auto place = [&](bool mn, int x, int *k, int *m) { *k = mn ? x / BM : x % BK, *m = mn ? x % BM : x / BK; };

@@ -24,7 +24,8 @@ using namespace sm100;
 
 enum { LOSS = 0, GRAD = 1, DH = 2, DW = 3 };
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int TM = 256, TN = 256, BK = 64;       // a pair's tile; a CTA holds 128 x 256 of it
+constexpr int TM = 256, TN = 256, BK = 64;       // a pair's tile; a CTA holds 128 x 256 of it.  LOSS may take
+                                                 // tiles of fewer columns (VocabArgs::tn)
 constexpr int HALF = 128 * BK * 2;               // a CTA's part of an operand's k-block, 16 KB
 constexpr int STAGE = 2 * HALF, STAGES = 6;
 constexpr int OFF_BAR = STAGES * STAGE, SMEM = OFF_BAR + 256 + 1024 /*align*/;
@@ -44,11 +45,15 @@ struct Tiles {
     __device__ __forceinline__ int items() const { return m * n * splits; }
 };
 template <int KIND>
+__device__ __forceinline__ int cols_of(const VocabArgs &a) {
+    return KIND == LOSS ? a.tn : TN;
+}
+template <int KIND>
 __device__ __forceinline__ Tiles tiles_of(const VocabArgs &a, int count, int piece) {
     Tiles t;
     // (without a token one tile is formed whose rows are nobody's; DW's k-block 0 of g and h is cleared)
     t.m = KIND == DW ? ceil_div(piece, TM) : ceil_div(max(count, 1), TM);
-    t.n = ceil_div(KIND == LOSS || KIND == GRAD ? piece : a.d, TN);
+    t.n = ceil_div(KIND == LOSS || KIND == GRAD ? piece : a.d, cols_of<KIND>(a));
     t.kb = KIND == DH ? ceil_div(piece, BK) : KIND == DW ? ceil_div(max(count, 1), BK) : ceil_div(a.d, BK);
     t.splits = 1, t.per = t.kb;
     if (KIND == DH) {
@@ -63,7 +68,7 @@ struct Item {
 // Neighbouring pairs take tiles that share what does not stay in L2: rows of the vocabulary (LOSS,
 // GRAD), columns of W (DH); DW walks all of h's columns (which stay) for a tile of g.
 template <int KIND>
-__device__ __forceinline__ Item item_of(const Tiles &t, int it) {
+__device__ __forceinline__ Item item_of(const Tiles &t, int it, int tn) {
     Item x;
     int m, n;
     if (KIND == DW) {
@@ -74,7 +79,7 @@ __device__ __forceinline__ Item item_of(const Tiles &t, int it) {
         const int q = it / t.m;
         n = q % t.n, x.split = q / t.n;
     }
-    x.m0 = m * TM, x.n0 = n * TN, x.nt = n;
+    x.m0 = m * TM, x.n0 = n * tn, x.nt = n;
     x.kb0 = x.split * t.per;
     x.nkb = min(t.per, t.kb - x.kb0);  // (<= 0: a split that the last, shorter piece leaves nothing)
     return x;
@@ -122,6 +127,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     const int piece = min(a.piece, a.V - v0);
+    const int tn = cols_of<KIND>(a);              // (a CTA holds half of B's rows)
+    const uint32_t stage_tx = KIND == LOSS ? 2 * HALF + (uint32_t)tn * BK * 2 : 2 * STAGE;  // both CTAs' bytes
 
     if (warp == TMA && lane == 0) {
         // what is read again soon stays in L2, the vocabulary's rows of LOSS pass through
@@ -131,11 +138,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         // not depend on them: its k-blocks are asked for while the kernel in front still runs
         // (which has waited for the caller's earlier work before it let this one start).
         int pre = 0;
-        if ((KIND == LOSS || KIND == GRAD) && a.pad == TM && cl < ceil_div(piece, TN)) {
+        if ((KIND == LOSS || KIND == GRAD) && a.pad == TM && cl < ceil_div(piece, tn)) {
             pre = min(STAGES, ceil_div(a.d, BK));
             for (int i = 0; i < pre; ++i) {
-                if (rank == 0) mbar_arrive_expect_tx(&full[i], 2 * STAGE);
-                tma_load_2d_pair(smem + i * STAGE + HALF, &map_b, map_rank(&full[i], 0), i * BK, v0 + cl * TN + (int)rank * 128, pol_b);
+                if (rank == 0) mbar_arrive_expect_tx(&full[i], stage_tx);
+                tma_load_2d_pair(smem + i * STAGE + HALF, &map_b, map_rank(&full[i], 0), i * BK, v0 + cl * tn + (int)rank * (tn / 2), pol_b);
             }
         }
         pdl_wait();
@@ -144,15 +151,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         int gi = 0;
         bool ok = true;
         for (int it = cl; ok && it < n_items; it += n_cl) {
-            const Item x = item_of<KIND>(t, it);
-            const int ma = x.m0 + (int)rank * 128, nb = x.n0 + (int)rank * 128;
+            const Item x = item_of<KIND>(t, it, tn);
+            const int ma = x.m0 + (int)rank * 128, nb = x.n0 + (int)rank * (tn / 2);
             for (int i = 0; i < x.nkb; ++i, ++gi) {
                 const int s = gi % STAGES, k = (x.kb0 + i) * BK;
                 if (gi >= STAGES && !mbar_wait(&empty[s], ((gi / STAGES) & 1) ^ 1, abort)) {
                     ok = false;
                     break;
                 }
-                if (rank == 0 && gi >= pre) mbar_arrive_expect_tx(&full[s], 2 * STAGE);
+                if (rank == 0 && gi >= pre) mbar_arrive_expect_tx(&full[s], stage_tx);
                 const uint32_t bar = map_rank(&full[s], 0);
                 uint8_t *sa = smem + s * STAGE, *sb = sa + HALF;
                 if (Ki::A_MN) {
@@ -174,7 +181,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         for (int j = gi > STAGES ? gi - STAGES : 0; j < gi; ++j)
             if (!mbar_wait_drain(&empty[j % STAGES], (j / STAGES) & 1)) break;
     } else if (warp == MMA && lane == 0 && rank == 0) {
-        constexpr uint32_t idesc = idesc_bf16_f32(TM, TN) | (Ki::A_MN ? 1u << 15 : 0u) | (Ki::B_MN ? 1u << 16 : 0u);
+        const uint32_t idesc = idesc_bf16_f32(TM, tn) | (Ki::A_MN ? 1u << 15 : 0u) | (Ki::B_MN ? 1u << 16 : 0u);
         // a step of 16 along K: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major tile
         constexpr uint64_t step_a = Ki::A_MN ? 2048 >> 4 : 32 >> 4, step_b = Ki::B_MN ? 2048 >> 4 : 32 >> 4;
         pdl_wait();
@@ -183,7 +190,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         int gi = 0, n = 0;
         bool ok = true;
         for (int it = cl; ok && it < n_items; it += n_cl) {
-            const Item x = item_of<KIND>(t, it);
+            const Item x = item_of<KIND>(t, it, tn);
             if (KIND == DH && x.nkb <= 0) continue;
             const int buf = n & 1;
             const uint32_t acc = tmem + (uint32_t)(buf * TN);
@@ -219,7 +226,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         const int n_items = t.items();
         int n = -1;
         for (int it = cl; it < n_items; it += n_cl) {
-            const Item x = item_of<KIND>(t, it);
+            const Item x = item_of<KIND>(t, it, tn);
             if (KIND == DH && x.nkb <= 0) continue;
             ++n;
             const int buf = n & 1, m = x.m0 + (int)rank * 128 + row;
@@ -228,16 +235,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
             const bool have = __all_sync(0xffffffffu, mbar_wait(&acc_full[buf], (n >> 1) & 1, abort));
             tc_fence_after();
             if (!have) break;
-            const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * TN + half * 128);
-            const int c0 = x.n0 + half * 128;     // first column
+            const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * TN + half * (tn / 2));
+            const int c0 = x.n0 + half * (tn / 2);  // first column
             float mx = -INFINITY, sum = 0.f;
 #pragma unroll 1
-            for (int c = 0; c < 128; c += 32) {
+            for (int c = 0; c < tn / 2; c += 32) {
                 float v[32];
                 __syncwarp();  // (rows that store nothing have skipped ahead)
-                tmem_ld32(at + c, v);
+                tmem_ld32(at + c, v);  // (behind the half's last column: not looked at)
                 if constexpr (KIND == LOSS) {
-                    const int left = piece - (c0 + c);
+                    const int left = min(piece - (c0 + c), tn / 2 - c);
                     float top = mx;
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
@@ -245,7 +252,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                         top = fmaxf(top, v[j]);
                     }
                     const int hit = info.target - (c0 + c);
-                    if (hit >= 0 && hit < 32) {  // (rare: once a row)
+                    if (hit >= 0 && hit < min(32, left)) {  // (rare: once a row)
                         float z = 0.f;
 #pragma unroll
                         for (int j = 0; j < 32; ++j) z = j == hit ? v[j] : z;
@@ -322,7 +329,8 @@ cudaError_t run(const VocabArgs &a, const CUtensorMap &ma, const CUtensorMap &mb
     const cudaError_t e = allow_smem(vocab_tc_kernel<KIND>, SMEM, known);
     if (e != cudaSuccess) return e;
     const int piece = a.V - v0 < a.piece ? a.V - v0 : a.piece;
-    const long long m = KIND == DW ? ceil_div(piece, TM) : a.pad / TM, n = ceil_div(KIND == LOSS || KIND == GRAD ? piece : a.d, TN);
+    const long long m = KIND == DW ? ceil_div(piece, TM) : a.pad / TM;
+    const long long n = ceil_div(KIND == LOSS || KIND == GRAD ? piece : a.d, KIND == LOSS ? a.tn : TN);
     const long long items = m * n * (KIND == DH ? 16 : 1);
     const int pairs = a.pairs;
     return launch_k(vocab_tc_kernel<KIND>, dim3(2 * (items < pairs ? (unsigned)items : (unsigned)pairs)), dim3(THREADS), (size_t)SMEM,
@@ -338,9 +346,19 @@ bool vocab_tc_supported(const VocabArgs &a) {
 void plan_vocab_tc(VocabArgs *a, bool backward, int n_sm) {
     a->pad = ceil_div(a->n, TM) * TM;
     a->pairs = n_sm / 2 > 0 ? n_sm / 2 : 1;
-    const int tiles = ceil_div(a->V, TN);
+    a->tn = TN;
+    if (!backward && a->n <= TM) {
+        // W is read once and bounds the call: tiles of the width whose rounds over the pairs read the fewest rows
+        // (32000 rows: 2 x 224 instead of 2 x 256 a pair)
+        long long least = 1ll << 62;
+        for (int tn = TN; tn >= 128; tn -= 32) {
+            const long long rows = ceil_div_ll(ceil_div(a->V, tn), a->pairs) * tn;
+            if (rows < least) least = rows, a->tn = tn;
+        }
+    }
+    const int tiles = ceil_div(a->V, a->tn);
     a->parts = 2 * tiles;
-    a->piece = tiles * TN;
+    a->piece = tiles * a->tn;
     a->n_pieces = 1;
     if (!backward) return;
     long long most = GRAD_BYTES / 2 / a->pad / TN;  // tiles of a piece
@@ -350,18 +368,20 @@ void plan_vocab_tc(VocabArgs *a, bool backward, int n_sm) {
     a->n_pieces = ceil_div(a->V, a->piece);
 }
 
+// (The maps of the kept tokens' rows end behind the n-th: rows of a tile that cannot be there are zeros that
+// nothing fetches.  48 tokens against 32000 rows of 2560: 38 us with all 256 rows of the tile.)
 cudaError_t launch_vocab_loss_tc(const VocabArgs &a, cudaStream_t st) {
     CUtensorMap mh, mw;
-    if (!encode_tile_bf16(&mh, a.hc, a.d, a.pad, a.d, 128) || !encode_tile_bf16(&mw, a.w, a.d, a.V, a.ws, 128))
+    if (!encode_tile_bf16(&mh, a.hc, a.d, a.n, a.d, 128) || !encode_tile_bf16(&mw, a.w, a.d, a.V, a.ws, a.tn / 2))
         return cudaErrorInvalidValue;
     return run<LOSS>(a, mh, mw, 0, st);
 }
 
 cudaError_t launch_vocab_backward_tc(const VocabArgs &a, cudaStream_t st) {
     CUtensorMap mh, mw, mg, mwt, mgt, mht;
-    if (!encode_tile_bf16(&mh, a.hc, a.d, a.pad, a.d, 128) || !encode_tile_bf16(&mw, a.w, a.d, a.V, a.ws, 128) ||
+    if (!encode_tile_bf16(&mh, a.hc, a.d, a.n, a.d, 128) || !encode_tile_bf16(&mw, a.w, a.d, a.V, a.ws, 128) ||
         !encode_tile_bf16(&mg, a.grad, a.piece, a.pad, a.piece, 128) || !encode_tile_bf16(&mwt, a.w, a.d, a.V, a.ws, 64) ||
-        !encode_tile_bf16(&mgt, a.grad, a.piece, a.pad, a.piece, 64) || !encode_tile_bf16(&mht, a.hc, a.d, a.pad, a.d, 64))
+        !encode_tile_bf16(&mgt, a.grad, a.piece, a.pad, a.piece, 64) || !encode_tile_bf16(&mht, a.hc, a.d, a.n, a.d, 64))
         return cudaErrorInvalidValue;
     for (int i = 0; i < a.n_pieces; ++i) {
         const int v0 = i * a.piece;
