@@ -194,17 +194,17 @@ struct TreeBackArgs {
     float *dq_new;                 // [B][Hkv][R][dh]: the nodes' own part of dq, unscaled
     float scale;
 };
-// Row statistics, gradients of the nodes' keys and values, the nodes' part of dq.
-cudaError_t launch_tree_back_rows(const TreeBackArgs &a, cudaStream_t st);
-cudaError_t launch_tree_back_rows_tc(const TreeBackArgs &a, cudaStream_t st);  // bf16 rows of 128 dims
-// The cache's part of dq on CUDA cores in shares (t.part_o: [slot][row][dh]), and the sum of all parts.
+// Row statistics, gradients of the nodes' keys and values and the nodes' part of dq; then the cache's
+// part of dq in shares (t.part_o: [slot][row][dh]), and the sum of all parts.  CUDA cores:
 cudaError_t launch_tree_back_simt(const TreeBackArgs &a, cudaStream_t st);
 size_t tree_back_simt_slots(const TreeArgs &a);
-// The same on tensor cores: head_dim 128, bf16 rows and cache, B <= 2048.
+// Tensor cores: head_dim 128, bf16 rows and cache, B <= 2048.
 bool tree_back_tc_supported(const TreeArgs &a);
 void plan_tree_back_tc(TreeArgs *a, int n_sm);
 size_t tree_back_tc_slots(const TreeArgs &a);
 int tree_back_tc_groups(const TreeArgs &a);
 cudaError_t launch_tree_back_tc(const TreeBackArgs &a, int2 *split_tab, cudaStream_t st);
+// What is not the cache's, by a kernel of its own: bf16 rows of 128 dims.
+cudaError_t launch_tree_back_rows_tc(const TreeBackArgs &a, cudaStream_t st);
 
 }  // namespace sp

@@ -411,9 +411,7 @@ sp_status sp_attend_tree_backward(sp_stream stream, const sp_tree_dims *dims, co
     at += back_part_bytes(a);
     int2 *split_tab = (int2 *)at;
     const cudaStream_t st = (cudaStream_t)stream;
-    cudaError_t e = a.tensor ? launch_tree_back_rows_tc(x, st) : launch_tree_back_rows(x, st);
-    if (e == cudaSuccess) e = a.tensor ? launch_tree_back_tc(x, split_tab, st) : launch_tree_back_simt(x, st);
-    return launched(e, "sp_attend_tree_backward");
+    return launched(a.tensor ? launch_tree_back_tc(x, split_tab, st) : launch_tree_back_simt(x, st), "sp_attend_tree_backward");
 }
 
 }  // extern "C"

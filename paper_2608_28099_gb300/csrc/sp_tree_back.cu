@@ -337,13 +337,9 @@ cudaError_t run_simt(const TreeBackArgs &a, cudaStream_t st) {
 
 size_t tree_back_simt_slots(const TreeArgs &a) { return (size_t)a.B * a.Hkv * a.n_rb * a.n_splits; }
 
-cudaError_t launch_tree_back_rows(const TreeBackArgs &a, cudaStream_t st) {
-    if (a.t.dh == 128) return run_rows<128>(a, st);
-    if (a.t.dh == 64) return run_rows<64>(a, st);
-    return run_rows<32>(a, st);
-}
-
 cudaError_t launch_tree_back_simt(const TreeBackArgs &a, cudaStream_t st) {
+    const cudaError_t e = a.t.dh == 128 ? run_rows<128>(a, st) : a.t.dh == 64 ? run_rows<64>(a, st) : run_rows<32>(a, st);
+    if (e != cudaSuccess) return e;
     if (a.t.dh == 128) return run_simt<128>(a, st);
     if (a.t.dh == 64) return run_simt<64>(a, st);
     return run_simt<32>(a, st);

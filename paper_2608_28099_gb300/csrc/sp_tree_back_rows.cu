@@ -12,13 +12,11 @@
 //
 // Bound by latency: loads, two barriers and five short products a 64 rows.
 #include "sp_cache.cuh"
-#include "sp_sm100.cuh"
+#include "sp_mma16.cuh"
 
 namespace sp {
 
 namespace {
-
-using namespace sm100;
 
 constexpr int DH = 128, LD = DH + 8;  // elements of a row in shared memory (rows 4 banks apart)
 
@@ -33,46 +31,6 @@ struct Smem {
     unsigned odd_row[ROWS];            // bit 0: q, bit 1: dout held something not finite
     unsigned odd_node[NP];             // bit 0: k, bit 1: v
 };
-
-__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], const void *p) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-                 : "r"(smem_u32(p)));
-}
-__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], const void *p) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-                 : "r"(smem_u32(p)));
-}
-__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// Eight elements with the non-finite ones taken out; whether there were any.
-__device__ __forceinline__ bool take_finite(uint4 &u) {
-    uint32_t w[4] = {u.x, u.y, u.z, u.w};
-    bool odd = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const bool lo = (w[i] & 0x7f80u) == 0x7f80u, hi = (w[i] & 0x7f800000u) == 0x7f800000u;
-        odd = odd || lo || hi;
-        w[i] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
-    }
-    u = make_uint4(w[0], w[1], w[2], w[3]);
-    return odd;
-}
-__device__ __forceinline__ float dot8(uint4 a, uint4 b) {
-    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        s += __uint_as_float(x[i] << 16) * __uint_as_float(y[i] << 16);
-        s += __uint_as_float(x[i] & 0xffff0000u) * __uint_as_float(y[i] & 0xffff0000u);
-    }
-    return s;
-}
 
 // NP: nodes, rounded up to 16, 32 or 64.
 template <int NP, int WARPS>

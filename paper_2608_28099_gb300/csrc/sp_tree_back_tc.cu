@@ -2,10 +2,10 @@
 // cores: head_dim 128, bf16 rows and cache.  Per key tile of 64 cached tokens and block of up to 128
 // query rows of a kv head, rows on the MMA's M side:
 //   S = Q K^T, dP = dO V^T   128 x 64 each, Q and dO in TMEM, K and V in shared memory
-//   ds = p (dP - D)          p = exp(scale S - lse), a row a thread, written as bf16 over S in TMEM
+//   ds = p (dP - D)          p = exp(scale S - lse), a row a thread, written as bf16 over dP in TMEM
 //   dQ += ds K               from TMEM; K is read a second time where it lies (MN-major)
 // The log sums are known, so that a tile's weights are final: nothing is rescaled, two softmax
-// warpgroups take alternate tiles into one accumulator, and parts of dQ are sums.
+// warpgroups take half a tile's tokens each, and parts of dQ are sums.
 //
 // Work: the cached tokens of every sequence are cut into tiles, the list of all tiles into shares (as
 // in sp_attn_plan.cuh), CTA (share, kv head, row block) walks its share; its piece of a sequence is
@@ -21,6 +21,7 @@
 #include "sp_attn_plan.cuh"
 #include "sp_cache.cuh"
 #include "sp_gemm.cuh"
+#include "sp_mma16.cuh"
 
 namespace sp {
 
@@ -28,7 +29,8 @@ namespace {
 
 constexpr int TILE = 64;
 constexpr int SLOT = TILE * DH * 2;             // K or V of a tile, 16 KB
-constexpr int STAGE_ROW = DH * 2 + 16;          // a staged row of queries or output gradients
+constexpr int LD = DH + 8, STAGE_ROW = LD * 2;  // a staged row of queries or output gradients: elements, bytes
+constexpr int MAX_NODES = 16;                   // most nodes whose products are formed here
 constexpr int ROWS = 128;                       // most rows of a block
 constexpr int MAX_RING = 8;
 constexpr int BAR_EPI = 1;                      // named barrier of warps 8-11
@@ -42,7 +44,7 @@ constexpr int kBackSegCost = 4;
 
 struct Layout {
     int nk, nv;                                 // ring slots
-    int off_q, off_do, off_k, off_v, off_tab;   // (off_q, off_do: staged rows)
+    int off_q, off_do, off_n, off_k, off_v, off_tab;  // (off_q, off_do: staged rows; off_n: Nodes)
     int smem;
 };
 struct Bars {
@@ -51,6 +53,15 @@ struct Bars {
     uint32_t tmem;
     int abort;
     int wsum[32];
+};
+// What the segments' rows need, and the nodes of one.
+struct Nodes {
+    float2 stat[2][ROWS];              // by segment parity: (log sum in log2 units, out.dout)
+    unsigned long long sees[ROWS];
+    unsigned odd_row[ROWS];            // bit 0: q, bit 1: dout held something not finite
+    unsigned odd_node[MAX_NODES];      // bit 0: k, bit 1: v
+    bf16 k[MAX_NODES][LD], v[MAX_NODES][LD];
+    bf16 p[64][MAX_NODES + 8], ds[64][MAX_NODES + 8];
 };
 constexpr int OFF_CUTS = 1024;
 constexpr int OFF_FRONT = OFF_CUTS + (MAX_GRP + 4) * 4;
@@ -102,7 +113,7 @@ __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.
 // The tile list: prefix[b] = tiles of the sequences before b (one for an empty sequence), each
 // sequence's cache id, length and node count.  By all THREADS threads.
 __device__ __forceinline__ void back_prefix(const TreeArgs &a, int *prefix, int *sids, int *lens, int *nodes, int *wsum,
-                                            int *status) {
+                                            int *status, int *node_status) {
     const int B = a.B, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int per = (B + THREADS - 1) / THREADS;
     const int b0 = min(B, (int)threadIdx.x * per), b1 = min(B, b0 + per);
@@ -113,7 +124,7 @@ __device__ __forceinline__ void back_prefix(const TreeArgs &a, int *prefix, int 
         const SeqRef sq = resolve_seq(a.seq_ids, a.seq_lens, 0, b, a.cache.kv.n_seqs, a.most_len, status);
         sids[b] = sq.sid;
         lens[b] = sq.len;
-        nodes[b] = checked_nodes(a, n, nullptr);
+        nodes[b] = checked_nodes(a, n, node_status);
         const int v = max(1, ceil_div(sq.len, TILE));
         prefix[b] = v;
         sum += v;
@@ -184,31 +195,204 @@ struct Walk {
 };
 
 // Queries and output gradients of sequence b, a block's rows, into their staging places; zeros for
-// rows of nodes that are not there.  16 lanes a row, four rows of each under way together.
-__device__ __forceinline__ void stage_rows(const TreeBackArgs &x, int b, int n, int g, int rb, uint8_t *Q, uint8_t *dO, int wi,
-                                           int lane) {
+// rows of nodes that are not there, and up to whole 16 rows.  16 lanes a row, four rows of each under
+// way together.  NODES: the rows' statistics and what the products between nodes need of them, too.
+template <bool NODES>
+__device__ __forceinline__ void stage_rows(const TreeBackArgs &x, int b, int n, int g, int rb, uint8_t *Q, uint8_t *dO, Nodes *ns,
+                                           float2 *stat, int wi, int lane) {
     const TreeArgs &a = x.t;
-    const int c = lane & 15;
+    const int c = lane & 15, rows = (a.rb_rows + 15) & ~15;
     constexpr int AT_ONCE = 4;
 #pragma unroll 1
-    for (int r1 = wi * 2 + (lane >> 4); r1 < a.rb_rows; r1 += AT_ONCE * 8) {
-        uint4 q[AT_ONCE], go[AT_ONCE];
+    for (int r1 = wi * 2 + (lane >> 4); r1 < rows; r1 += AT_ONCE * 8) {
+        uint4 q[AT_ONCE], go[AT_ONCE], o[AT_ONCE];
+        float lse[AT_ONCE];
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
             const int r = r1 + k * 8, rr = rb * a.rb_rows + r, node = rr / a.G;
-            q[k] = go[k] = make_uint4(0, 0, 0, 0);
+            q[k] = go[k] = o[k] = make_uint4(0, 0, 0, 0);
+            lse[k] = -INFINITY;
             if (r < a.rb_rows && rr < a.R && node < n) {
-                const size_t head = (size_t)(g * a.G + rr - node * a.G) * DH + c * 8, row = (size_t)b * a.N + node;
+                const int hd = g * a.G + rr - node * a.G;
+                const size_t head = (size_t)hd * DH + c * 8, row = (size_t)b * a.N + node;
                 q[k] = *(const uint4 *)((const bf16 *)a.q + row * a.qs + head);
                 go[k] = *(const uint4 *)((const bf16 *)x.dout + row * a.Hq * DH + head);
+                if (NODES) {
+                    o[k] = *(const uint4 *)((const bf16 *)a.out + row * a.Hq * DH + head);
+                    lse[k] = a.lse[row * a.Hq + hd];
+                }
             }
         }
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
-            const int r = r1 + k * 8;
-            if (r >= a.rb_rows) break;
+            const int r = r1 + k * 8;  // (rows come in pairs: the warp's lanes agree on the end)
+            if (r - (lane >> 4) >= rows) break;
             st_shared_v4(Q + r * STAGE_ROW + c * 16, q[k].x, q[k].y, q[k].z, q[k].w);
             st_shared_v4(dO + r * STAGE_ROW + c * 16, go[k].x, go[k].y, go[k].z, go[k].w);
+            if constexpr (NODES) {
+                float d = dot8(go[k], o[k]);
+#pragma unroll
+                for (int y = 8; y; y >>= 1) d += __shfl_xor_sync(0xffffffffu, d, y);
+                const unsigned half = 0xffffu << (lane & 16);
+                const bool qo = __ballot_sync(0xffffffffu, take_finite(q[k])) & half;
+                const bool oo = __ballot_sync(0xffffffffu, take_finite(go[k])) & half;
+                if (c == 0) {
+                    float2 st = make_float2(INFINITY, 0.f);
+                    if (lse[k] != -INFINITY) st = make_float2(lse[k] == INFINITY ? NAN : lse[k] * 1.4426950408889634f, d);
+                    stat[r] = st;
+                    ns->sees[r] = st.x == INFINITY ? 0 : tree_mask(a, b, r / a.G, n);
+                    ns->odd_row[r] = (qo ? 1u : 0u) | (oo ? 2u : 0u);
+                }
+            }
+        }
+    }
+}
+// What lies between the nodes of sequence b (one row block, at most 16 nodes): gradients of their
+// keys and values, and their part of dQ, from the staged rows.  mma.sync by four warps that have
+// nothing else to do while a segment's tiles are under way; the operands and what becomes of
+// non-finite elements are those of sp_tree_back_rows.cu.
+__device__ __forceinline__ void node_products(const TreeBackArgs &x, int b, int n, int g, uint8_t *Q, uint8_t *dO, Nodes &s,
+                                              const float2 *stat, int wi, int lane) {
+    const TreeArgs &a = x.t;
+    const int c = lane & 15, rows = (a.rb_rows + 15) & ~15;
+    constexpr int NP = MAX_NODES, NT = DH / 4 / 8;
+#pragma unroll
+    for (int j0 = 0; j0 < NP; j0 += 8) {
+        const int j = j0 + wi * 2 + (lane >> 4);
+        uint4 k = make_uint4(0, 0, 0, 0), v = k;
+        if (j < n) {
+            const size_t r = (size_t)b * a.N + j;
+            k = *(const uint4 *)((const bf16 *)a.k_new + r * a.ks + (size_t)g * DH + c * 8);
+            v = *(const uint4 *)((const bf16 *)a.v_new + r * a.vs + (size_t)g * DH + c * 8);
+        }
+        const unsigned half = 0xffffu << (lane & 16);
+        const bool ko = __ballot_sync(0xffffffffu, take_finite(k)) & half, vo = __ballot_sync(0xffffffffu, take_finite(v)) & half;
+        *(uint4 *)&s.k[j][c * 8] = k;
+        *(uint4 *)&s.v[j][c * 8] = v;
+        if (c == 0) s.odd_node[j] = (ko ? 1u : 0u) | (vo ? 2u : 0u);
+    }
+    {  // a row a thread: non-finite elements out (rare; the raw rows are in TMEM)
+        const int r = wi * 32 + lane;
+        if (r < rows && s.odd_row[r]) {
+#pragma unroll 1
+            for (int e = 0; e < DH * 2; e += 16) {
+                uint4 q = *(uint4 *)(Q + r * STAGE_ROW + e), go = *(uint4 *)(dO + r * STAGE_ROW + e);
+                take_finite(q);
+                take_finite(go);
+                *(uint4 *)(Q + r * STAGE_ROW + e) = q;
+                *(uint4 *)(dO + r * STAGE_ROW + e) = go;
+            }
+        }
+    }
+    named_sync(BAR_EPI, 128);
+    float dk[NT][4], dv[NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dk[j][e] = dv[j][e] = 0.f;
+    const size_t row0 = ((size_t)b * a.Hkv + g) * a.R;
+    const auto q_at = [&](int r, int d) { return (const bf16 *)(Q + r * STAGE_ROW) + d; };
+    const auto o_at = [&](int r, int d) { return (const bf16 *)(dO + r * STAGE_ROW) + d; };
+#pragma unroll 1
+    for (int r0 = 0; r0 < rows; r0 += 64) {
+        if (r0) named_sync(BAR_EPI, 128);  // (the weights before are read)
+        const int wr = wi * 16, r_lo = wr + (lane >> 2), col = (lane & 3) * 2;
+        if (r0 + wr < rows) {
+            float y[NP / 8][4], dp[NP / 8][4];
+            uint32_t ds_frag[NP / 8][2];
+#pragma unroll
+            for (int j = 0; j < NP / 8; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[j][e] = dp[j][e] = 0.f;
+#pragma unroll
+            for (int kk = 0; kk < DH / 16; ++kk) {
+                uint32_t qa[4], oa[4], kb[4], vb[4];
+                ldsm4(qa, q_at(r0 + wr + (lane & 15), kk * 16 + (lane >> 4) * 8));
+                ldsm4(oa, o_at(r0 + wr + (lane & 15), kk * 16 + (lane >> 4) * 8));
+                const int node = (lane & 7) + (lane >> 4) * 8, d = kk * 16 + ((lane >> 3) & 1) * 8;
+                ldsm4(kb, &s.k[node][d]);
+                ldsm4(vb, &s.v[node][d]);
+                mma16816(y[0], qa, kb[0], kb[1]);
+                mma16816(y[1], qa, kb[2], kb[3]);
+                mma16816(dp[0], oa, vb[0], vb[1]);
+                mma16816(dp[1], oa, vb[2], vb[3]);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int rl = r_lo + 8 * h, r = r0 + rl;
+                const float2 st = stat[r];
+                const unsigned long long sees = s.sees[r];
+                const unsigned odd = s.odd_row[r];
+#pragma unroll
+                for (int j = 0; j < NP / 8; ++j) {
+                    float p[2], d[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int node = j * 8 + col + e;
+                        const bool vis = (sees >> node) & 1;
+                        const unsigned on = s.odd_node[node];
+                        float w = fast_exp2(fmaf(y[j][2 * h + e], a.scale_log2, -st.x));
+                        if ((odd | on) & 1u) w = NAN;
+                        float z = w * (dp[j][2 * h + e] - st.y);
+                        if ((odd | on) & 2u) z = NAN;
+                        if (odd & 2u) w = NAN;
+                        p[e] = vis ? w : 0.f;
+                        d[e] = vis ? z : 0.f;
+                    }
+                    ds_frag[j][h] = pack_bf16(d[0], d[1]);
+                    *(uint32_t *)&s.p[rl][j * 8 + col] = pack_bf16(p[0], p[1]);
+                    *(uint32_t *)&s.ds[rl][j * 8 + col] = ds_frag[j][h];
+                }
+            }
+            const uint32_t da[4] = {ds_frag[0][0], ds_frag[0][1], ds_frag[1][0], ds_frag[1][1]};
+#pragma unroll 2
+            for (int j = 0; j < DH / 16; ++j) {  // the nodes' part of dQ, 16 dims at a time
+                uint32_t kb[4];
+                float u0[4] = {0.f, 0.f, 0.f, 0.f}, u1[4] = {0.f, 0.f, 0.f, 0.f};
+                ldsm4t(kb, &s.k[lane & 15][j * 16 + (lane >> 4) * 8]);
+                mma16816(u0, da, kb[0], kb[1]);
+                mma16816(u1, da, kb[2], kb[3]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int rr = r0 + r_lo + 8 * h;
+                    if (rr >= a.R) continue;
+                    float *to = x.dq_new + (row0 + rr) * DH + j * 16 + col;
+                    *(float2 *)to = make_float2(u0[2 * h], u0[2 * h + 1]);
+                    *(float2 *)(to + 8) = make_float2(u1[2 * h], u1[2 * h + 1]);
+                }
+            }
+        }
+        named_sync(BAR_EPI, 128);
+        const int d0 = wi * (DH / 4);
+#pragma unroll 1
+        for (int kk = 0; kk < 4 && r0 + kk * 16 < rows; ++kk) {
+            uint32_t da[4], pa[4];
+            const int r = kk * 16 + (lane & 7) + (lane >> 4) * 8, node = ((lane >> 3) & 1) * 8;
+            ldsm4t(da, &s.ds[r][node]);
+            ldsm4t(pa, &s.p[r][node]);
+#pragma unroll
+            for (int j = 0; j < NT / 2; ++j) {
+                uint32_t qb[4], ob[4];
+                ldsm4t(qb, q_at(r0 + kk * 16 + (lane & 15), d0 + j * 16 + (lane >> 4) * 8));
+                ldsm4t(ob, o_at(r0 + kk * 16 + (lane & 15), d0 + j * 16 + (lane >> 4) * 8));
+                mma16816(dk[2 * j], da, qb[0], qb[1]);
+                mma16816(dk[2 * j + 1], da, qb[2], qb[3]);
+                mma16816(dv[2 * j], pa, ob[0], ob[1]);
+                mma16816(dv[2 * j + 1], pa, ob[2], ob[3]);
+            }
+        }
+    }
+    const int d0 = wi * (DH / 4) + (lane & 3) * 2;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int node = (lane >> 2) + 8 * h;
+        if (node >= a.N) continue;
+        const size_t r = (size_t)b * a.N + node;
+        bf16 *tk = (bf16 *)x.dk + r * a.ks + (size_t)g * DH + d0, *tv = (bf16 *)x.dv + r * a.vs + (size_t)g * DH + d0;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            *(uint32_t *)(tk + j * 8) = pack_bf16(dk[j][2 * h] * x.scale, dk[j][2 * h + 1] * x.scale);
+            *(uint32_t *)(tv + j * 8) = pack_bf16(dv[j][2 * h], dv[j][2 * h + 1]);
         }
     }
 }
@@ -226,6 +410,8 @@ __device__ __forceinline__ void row_to_tmem(uint32_t addr, const uint8_t *row) {
     }
 }
 
+// NODES: the row statistics and what lies between the nodes are formed here, else by a kernel in front.
+template <bool NODES>
 __global__ void __launch_bounds__(THREADS, 1)
     tree_back_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                         const __grid_constant__ TreeBackArgs args, const __grid_constant__ Layout lay, int2 *split_tab) {
@@ -241,9 +427,13 @@ __global__ void __launch_bounds__(THREADS, 1)
     const bool paged = a.cache.kv.layout == SP_KV_PAGED;
     const int P = a.cache.kv.page_size, P_bits = 31 - __clz(max(P, 1));
     constexpr int ROW = DH * 2;
-    // The kernel in front of this one has waited for the caller's earlier work before it let this one
-    // start: lengths, counts, queries and the cache may be read; its own results only behind the wait.
-    back_prefix(a, prefix, sids, lens, nodes, bars->wsum, blockIdx.x == 0 ? a.status : nullptr);
+    // The first kernel of its call reads nothing of the caller's before the wait.  Behind a kernel of the
+    // call, which has waited before it let this one start: lengths, counts, queries and the cache may be
+    // read, that kernel's results only behind the wait.
+    if (NODES) pdl_wait();
+    Nodes *ns = (Nodes *)(smem + lay.off_n);
+    back_prefix(a, prefix, sids, lens, nodes, bars->wsum, blockIdx.x == 0 ? a.status : nullptr,
+                NODES && blockIdx.x == 0 ? a.status : nullptr);
     const int T = prefix[B];
     const int n_grp = share_count((int)gridDim.x / Hv, T, B, a.plan.tc_min_tiles);
     const int grp = blockIdx.x / Hv, hv = blockIdx.x - grp * Hv, g = hv / a.n_rb, rb = hv - g * a.n_rb;
@@ -262,7 +452,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bars->s_full[i], 1);
-            mbar_init(&bars->p_full[i], 4);
+            mbar_init(&bars->p_full[i], 8);
         }
         mbar_init(&bars->q_full, 4);
         mbar_init(&bars->q_empty, 1);
@@ -304,57 +494,58 @@ __global__ void __launch_bounds__(THREADS, 1)
 
     if (warp < 8) {
         // ------------------------------------------------------------ weights and their gradients
-        const int w = warp >> 2, r = threadIdx.x & 127;  // tiles of this parity; row, TMEM lane
+        const int c0 = (warp >> 2) * 32, r = threadIdx.x & 127;  // this warpgroup's tokens of a tile; row, TMEM lane
         const int rr = rb * a.rb_rows + r;
         const bool active = r < a.rb_rows && rr < a.R;
         const bool warp_active = __any_sync(0xffffffffu, active);
-        const uint32_t s_col = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(w * 128);
-        pdl_wait();  // the row statistics
+        const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        if (!NODES) pdl_wait();  // the row statistics
         bool ok = true;
-        uint32_t ph = 0;
-        int at = 0;  // tiles in front of the segment
+        int tile = 0;
 #pragma unroll 1
         for (int b = sh.b0; ok && b < sh.b1; ++b) {
             const Seg sg = piece(sh, b);
-            const int left = lens[b] - sg.t_a * TILE;
+            const int left = lens[b] - sg.t_a * TILE - c0;
             float2 st = make_float2(INFINITY, 0.f);
-            if (active) st = __ldcg(args.stat + ((size_t)b * Hkv + g) * a.R + rr);
+            if (!NODES && active) st = __ldcg(args.stat + ((size_t)b * Hkv + g) * a.R + rr);
 #pragma unroll 1
-            for (int i = (at + w) & 1; i < sg.n; i += 2) {
-                ok = ok && wait_warp(&bars->s_full[w], ph, abort);
-                ph ^= 1;
+            for (int i = 0; i < sg.n; ++i, ++tile) {
+                const int w = tile & 1;
+                const uint32_t s_col = lane_base + (uint32_t)(w * 128);
+                ok = ok && wait_warp(&bars->s_full[w], (tile >> 1) & 1, abort);
                 if (!ok) break;
                 tc_fence_after();
+                // (there since the queries are: the scores waited for both)
+                if (NODES && i == 0 && active) {
+                    const volatile float *at = &ns->stat[(b - sh.b0) & 1][r].x;
+                    st = make_float2(at[0], at[1]);
+                }
                 if (warp_active) {
                     const int n_tok = left - i * TILE;
+                    float s[32], d[32];
+                    ld32_async(s_col + c0, s);
+                    ld32_async(s_col + 64 + c0, d);
+                    ld_wait(s);
+                    ld_wait(d);
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        float s[32], d[32];
-                        ld32_async(s_col + c * 32, s);
-                        ld32_async(s_col + 64 + c * 32, d);
-                        ld_wait(s);
-                        ld_wait(d);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const float p = fast_exp2(fmaf(s[e], a.scale_log2, -st.x));
-                            s[e] = p * (d[e] - st.y);
-                        }
-                        if (n_tok < TILE) {  // past the end: what was loaded there is nothing
-#pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                if (c * 32 + e >= n_tok) s[e] = 0.f;
-                        }
-                        uint32_t pk[16];
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) pk[e] = pack_bf16(s[2 * e], s[2 * e + 1]);
-                        st16_async(s_col + c * 16, pk);  // over scores that this warp has read
+                    for (int e = 0; e < 32; ++e) {
+                        const float p = fast_exp2(fmaf(s[e], a.scale_log2, -st.x));
+                        s[e] = p * (d[e] - st.y);
                     }
+                    if (n_tok < 32) {  // past the end: what was loaded there is nothing
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (e >= n_tok) s[e] = 0.f;
+                    }
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) pk[e] = pack_bf16(s[2 * e], s[2 * e + 1]);
+                    st16_async(s_col + 64 + c0, pk);  // over products that this warp has read
                     st_wait();
                 }
                 tc_fence_before();
                 arrive_warp(&bars->p_full[w], lane);
             }
-            at += sg.n;
         }
     } else if (warp < MMA) {
         // ------------------------------------------------------------ queries in, dQ out
@@ -367,7 +558,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         const auto load = [&](int j) {
             const int b = sh.b0 + j;
             named_sync(BAR_EPI, 128);  // (the staged rows before are in TMEM)
-            stage_rows(args, b, nodes[b], g, rb, smem + lay.off_q, smem + lay.off_do, quad, lane);
+            stage_rows<NODES>(args, b, nodes[b], g, rb, smem + lay.off_q, smem + lay.off_do, ns, ns->stat[j & 1], quad, lane);
             named_sync(BAR_EPI, 128);
             const bool free = wait_warp(&bars->q_empty, (j & 1) ^ 1, abort);
             if (free && warp_active) {
@@ -383,7 +574,17 @@ __global__ void __launch_bounds__(THREADS, 1)
         };
         // (a warp whose wait ran out goes on to the barriers that the others meet at)
         bool ok = n_seg == 0 || load(0);
-        pdl_wait();  // the nodes' part of dQ; nothing is written before
+        if (!NODES) pdl_wait();  // the nodes' part of dQ; nothing is written before
+        // the share that has a sequence's first tile forms what lies between its nodes
+        const auto between = [&](int j) {
+            const int b = sh.b0 + j;
+            if (!NODES || sh.x0 > prefix[b]) return;
+            const float2 *stat = ns->stat[j & 1];
+            node_products(args, b, nodes[b], g, smem + lay.off_q, smem + lay.off_do, *ns, stat, quad, lane);
+            if (active) args.stat[((size_t)b * Hkv + g) * a.R + rr] = stat[r];
+            named_sync(BAR_EPI, 128);  // (dq_new is read by other threads)
+        };
+        if (n_seg > 0) between(0);
 #pragma unroll 1
         for (int j = 0; j < n_seg; ++j) {
             if (j + 1 < n_seg) ok = load(j + 1) && ok;
@@ -396,7 +597,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             const int node = rr / a.G;
             const size_t row = ((size_t)b * Hkv + g) * a.R + rr;
             bool live = false;
-            if (active && whole) live = node < n && __ldcg(&args.stat[row].x) != INFINITY;
+            if (active && whole) live = node < n && (NODES ? ns->stat[j & 1][r].x : __ldcg(&args.stat[row].x)) != INFINITY;
             ok = ok && wait_warp(&bars->dq_full, j & 1, abort);
             tc_fence_after();
             if (ok && warp_active) {
@@ -429,6 +630,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
             tc_fence_before();
             if (ok) arrive_warp(&bars->dq_empty, lane);
+            if (j + 1 < n_seg) between(j + 1);
         }
     } else if (warp == K_WARP || warp == V_WARP) {
         // ------------------------------------------------------------ K and V
@@ -591,7 +793,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 if (on) {
 #pragma unroll
                     for (int kk = 0; kk < TILE / 16; ++kk)  // 16 tokens: 8 columns of ds, two 8-token groups of K
-                        mma_bf16_ts(tmem + DQ_COL, tmem + (uint32_t)(w * 128 + kk * 8),
+                        mma_bf16_ts(tmem + DQ_COL, tmem + (uint32_t)(w * 128 + 64 + (kk >> 1) * 32 + (kk & 1) * 8),
                                     k + (uint64_t)(kk * (2 * GROUP_STRIDE >> 4)), idesc_q, kk > 0 || !out.first());
                     mma_commit(&bars->k_empty[rk2.slot]);
                     if (out.last()) mma_commit(&bars->dq_full);
@@ -647,12 +849,14 @@ __global__ void __launch_bounds__(SUM_THREADS) tree_back_tc_sum_kernel(const __g
         live ? make_uint2(pack_bf16(s.x * f, s.y * f), pack_bf16(s.z * f, s.w * f)) : make_uint2(0, 0);
 }
 
-bool make_layout(const TreeArgs &a, int rb_rows, Layout *lay) {
+bool make_layout(const TreeArgs &a, int rb_rows, bool nodes, Layout *lay) {
     const int tab = (4 * a.B + 1) * 4;
     lay->off_tab = OFF_FRONT;
     lay->off_q = (OFF_FRONT + tab + 15) & ~15;
-    lay->off_do = lay->off_q + rb_rows * STAGE_ROW;
-    const int at = (lay->off_do + rb_rows * STAGE_ROW + 1023) & ~1023, slots = (SMEM_MAX - 1024 - at) / SLOT;
+    const int rows = (rb_rows + 15) & ~15;
+    lay->off_do = lay->off_q + rows * STAGE_ROW;
+    lay->off_n = lay->off_do + rows * STAGE_ROW;
+    const int at = (lay->off_n + (nodes ? (int)sizeof(Nodes) : 0) + 1023) & ~1023, slots = (SMEM_MAX - 1024 - at) / SLOT;
     if (slots < 4) return false;
     lay->nv = slots / 2 < MAX_RING ? slots / 2 : MAX_RING;
     lay->nk = slots - lay->nv < MAX_RING ? slots - lay->nv : MAX_RING;
@@ -666,7 +870,7 @@ bool make_layout(const TreeArgs &a, int rb_rows, Layout *lay) {
 
 bool tree_back_tc_supported(const TreeArgs &a) {
     Layout lay;
-    return a.dh == DH && a.dtype == SP_BF16 && a.cache.dtype == SP_BF16 && a.B <= MAX_B && make_layout(a, ROWS, &lay) &&
+    return a.dh == DH && a.dtype == SP_BF16 && a.cache.dtype == SP_BF16 && a.B <= MAX_B && make_layout(a, ROWS, true, &lay) &&
            (a.cache.kv.layout == SP_KV_CONTIGUOUS || (long long)a.cache.kv.n_pages * a.Hkv * a.cache.kv.page_size <= 0x7fffffffLL);
 }
 
@@ -692,7 +896,8 @@ size_t tree_back_tc_slots(const TreeArgs &a) { return 2 * (size_t)a.plan.tc_ctas
 cudaError_t launch_tree_back_tc(const TreeBackArgs &args, int2 *split_tab, cudaStream_t st) {
     const TreeArgs &a = args.t;
     Layout lay;
-    if (!make_layout(a, a.rb_rows, &lay)) return cudaErrorInvalidValue;
+    const bool nodes = a.n_rb == 1 && a.N <= MAX_NODES;
+    if (!make_layout(a, a.rb_rows, nodes, &lay)) return cudaErrorInvalidValue;
     CUtensorMap mk, mv;
     memset(&mk, 0, sizeof mk);
     memset(&mv, 0, sizeof mv);
@@ -702,10 +907,13 @@ cudaError_t launch_tree_back_tc(const TreeBackArgs &args, int2 *split_tab, cudaS
             !encode_kv_pages_bf16(&mv, a.cache.kv.v_pool, blocks, a.cache.kv.page_size))
             return cudaErrorInvalidValue;
     }
-    static bool known[MAX_DEVICES] = {};
-    cudaError_t e = allow_smem(tree_back_tc_kernel, SMEM_MAX, known);
+    cudaError_t e = nodes ? cudaSuccess : launch_tree_back_rows_tc(args, st);
     if (e != cudaSuccess) return e;
-    e = launch_k(tree_back_tc_kernel, dim3(a.plan.tc_ctas), dim3(THREADS), (size_t)lay.smem, st, mk, mv, args, lay, split_tab);
+    static bool known[2][MAX_DEVICES] = {};
+    const auto kernel = nodes ? tree_back_tc_kernel<true> : tree_back_tc_kernel<false>;
+    e = allow_smem(kernel, SMEM_MAX, known[nodes]);
+    if (e != cudaSuccess) return e;
+    e = launch_k(kernel, dim3(a.plan.tc_ctas), dim3(THREADS), (size_t)lay.smem, st, mk, mv, args, lay, split_tab);
     if (e != cudaSuccess) return e;
     return launch_k(tree_back_tc_sum_kernel, dim3(a.Hkv * a.n_rb, tree_back_tc_groups(a), ceil_div(a.rb_rows, SUM_ROWS)),
                     dim3(SUM_THREADS), 0, st, args, (const int2 *)split_tab);
