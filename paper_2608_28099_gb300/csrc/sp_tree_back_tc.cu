@@ -27,8 +27,8 @@ namespace sp {
 
 namespace {
 
-constexpr int TILE = 64;
-constexpr int SLOT = TILE * DH * 2;             // K or V of a tile, 16 KB
+constexpr int TILE = 128;
+constexpr int SLOT = TILE * DH * 2;             // K or V of a tile, 32 KB
 constexpr int LD = DH + 8, STAGE_ROW = LD * 2;  // a staged row of queries or output gradients: elements, bytes
 constexpr int MAX_NODES = 16;                   // most nodes whose products are formed here
 constexpr int ROWS = 128;                       // most rows of a block
@@ -37,10 +37,10 @@ constexpr int BAR_EPI = 1;                      // named barrier of warps 8-11
 constexpr int SMEM_MAX = 227 * 1024;
 constexpr int THREADS = 512;
 constexpr int EPI = 8, MMA = 12, K_WARP = 13, V_WARP = 14;
-constexpr uint32_t DQ_COL = 256, Q_COL = 384, DO_COL = 448;  // TMEM: dQ, queries, output gradients
+constexpr uint32_t DP_COL = 128, DQ_COL = 256, Q_COL = 384, DO_COL = 448;  // TMEM: S, dP, dQ, Q, dO
 // Fewest tiles a share holds on average, and the cost of a segment in tiles.
-constexpr int kBackMinTiles = 4;
-constexpr int kBackSegCost = 4;
+constexpr int kBackMinTiles = 2;
+constexpr int kBackSegCost = 2;
 
 struct Layout {
     int nk, nv;                                 // ring slots
@@ -49,7 +49,7 @@ struct Layout {
 };
 struct Bars {
     uint64_t k_full[MAX_RING], k_empty[MAX_RING], v_full[MAX_RING], v_empty[MAX_RING];
-    uint64_t s_full[2], p_full[2], q_full, q_empty, dq_full, dq_empty, fin;
+    uint64_t s_full, d_full, p_full, q_full, q_empty, dq_full, dq_empty, fin;
     uint32_t tmem;
     int abort;
     int wsum[32];
@@ -450,10 +450,9 @@ __global__ void __launch_bounds__(THREADS, 1)
             mbar_init(&bars->v_full[i], 32);
             mbar_init(&bars->v_empty[i], 1);
         }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&bars->s_full[i], 1);
-            mbar_init(&bars->p_full[i], 8);
-        }
+        mbar_init(&bars->s_full, 1);
+        mbar_init(&bars->d_full, 1);
+        mbar_init(&bars->p_full, 8);
         mbar_init(&bars->q_full, 4);
         mbar_init(&bars->q_empty, 1);
         mbar_init(&bars->dq_full, 1);
@@ -494,14 +493,14 @@ __global__ void __launch_bounds__(THREADS, 1)
 
     if (warp < 8) {
         // ------------------------------------------------------------ weights and their gradients
-        const int c0 = (warp >> 2) * 32, r = threadIdx.x & 127;  // this warpgroup's tokens of a tile; row, TMEM lane
+        const int c0 = (warp >> 2) * 64, r = threadIdx.x & 127;  // this warpgroup's tokens of a tile; row, TMEM lane
         const int rr = rb * a.rb_rows + r;
         const bool active = r < a.rb_rows && rr < a.R;
         const bool warp_active = __any_sync(0xffffffffu, active);
-        const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t s_col = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)c0;
         if (!NODES) pdl_wait();  // the row statistics
         bool ok = true;
-        int tile = 0;
+        uint32_t ph = 0;
 #pragma unroll 1
         for (int b = sh.b0; ok && b < sh.b1; ++b) {
             const Seg sg = piece(sh, b);
@@ -509,10 +508,8 @@ __global__ void __launch_bounds__(THREADS, 1)
             float2 st = make_float2(INFINITY, 0.f);
             if (!NODES && active) st = __ldcg(args.stat + ((size_t)b * Hkv + g) * a.R + rr);
 #pragma unroll 1
-            for (int i = 0; i < sg.n; ++i, ++tile) {
-                const int w = tile & 1;
-                const uint32_t s_col = lane_base + (uint32_t)(w * 128);
-                ok = ok && wait_warp(&bars->s_full[w], (tile >> 1) & 1, abort);
+            for (int i = 0; i < sg.n; ++i, ph ^= 1) {
+                ok = ok && wait_warp(&bars->s_full, ph, abort);
                 if (!ok) break;
                 tc_fence_after();
                 // (there since the queries are: the scores waited for both)
@@ -520,31 +517,41 @@ __global__ void __launch_bounds__(THREADS, 1)
                     const volatile float *at = &ns->stat[(b - sh.b0) & 1][r].x;
                     st = make_float2(at[0], at[1]);
                 }
-                if (warp_active) {
-                    const int n_tok = left - i * TILE;
-                    float s[32], d[32];
-                    ld32_async(s_col + c0, s);
-                    ld32_async(s_col + 64 + c0, d);
+                const int n_tok = left - i * TILE;
+                float s[64];
+                if (warp_active) {  // the weights, while dP is formed
+                    ld32_async(s_col, s);
+                    ld32_async(s_col + 32, s + 32);
                     ld_wait(s);
-                    ld_wait(d);
+                    ld_wait(s + 32);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const float p = fast_exp2(fmaf(s[e], a.scale_log2, -st.x));
-                        s[e] = p * (d[e] - st.y);
+                    for (int e = 0; e < 64; ++e) s[e] = fast_exp2(fmaf(s[e], a.scale_log2, -st.x));
+                }
+                ok = wait_warp(&bars->d_full, ph, abort);
+                if (!ok) break;
+                tc_fence_after();
+                if (warp_active) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float d[32];
+                        ld32_async(s_col + DP_COL + c * 32, d);
+                        ld_wait(d);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) d[e] = s[c * 32 + e] * (d[e] - st.y);
+                        if (n_tok < c * 32 + 32) {  // past the end: what was loaded there is nothing
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (c * 32 + e >= n_tok) d[e] = 0.f;
+                        }
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) pk[e] = pack_bf16(d[2 * e], d[2 * e + 1]);
+                        st16_async(s_col + c * 16, pk);  // over scores that this warp has read
                     }
-                    if (n_tok < 32) {  // past the end: what was loaded there is nothing
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (e >= n_tok) s[e] = 0.f;
-                    }
-                    uint32_t pk[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) pk[e] = pack_bf16(s[2 * e], s[2 * e + 1]);
-                    st16_async(s_col + 64 + c0, pk);  // over products that this warp has read
                     st_wait();
                 }
                 tc_fence_before();
-                arrive_warp(&bars->p_full[w], lane);
+                arrive_warp(&bars->p_full, lane);
             }
         }
     } else if (warp < MMA) {
@@ -731,78 +738,65 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (bad && lane == 0 && a.status) atomicOr(a.status, SP_DEV_BAD_PAGE);
     } else if (warp == MMA) {
         // ------------------------------------------------------------ MMA issue
-        // S and dP run up to two tiles ahead of dQ, into the buffer that the softmax of two tiles
-        // before has read (its gradients are in front of it in the pipe).  One issuer sees every use
-        // of every slot in order.
+        // One issuer, one tile at a time: S into the columns that the gradients before lay in (their
+        // product is in front of it in the pipe), dP, and, when the softmax is done, dQ.
         const bool on = elect_one();
         constexpr uint32_t idesc_s = idesc_bf16_f32(128, TILE), idesc_q = idesc_bf16_f32_bmn(128, DH);
         const uint64_t dk0 = sw128_kmajor_desc_sbo(smem + lay.off_k, GROUP_STRIDE);
         const uint64_t dv0 = sw128_kmajor_desc_sbo(smem + lay.off_v, GROUP_STRIDE);
         const uint64_t dkt0 = sw128_mnmajor_desc2(smem + lay.off_k, HALF_STRIDE, GROUP_STRIDE);
-        Ring rk(lay.nk), rv(lay.nv), rk2(lay.nk);  // of S, of dP, of dQ
-        uint32_t p_ph = 0;                         // phases of p_full, a bit a buffer
+        Ring rk(lay.nk), rv(lay.nv);
         bool ok = n_tiles > 0;
         if (ok) {
-            Walk in(sh), out(sh);
-            int ahead = 0;  // tiles whose S is issued, whose dQ is not
-            int issued = 0, done = 0;
+            Walk at(sh);
 #pragma unroll 1
-            while (ok && done < n_tiles) {
-#pragma unroll 1
-                while (ok && issued < n_tiles && ahead < 2) {
-                    if (in.first()) {
-                        // (queries that are not there yet do not hold up the tiles under way)
-                        if (ahead > 0 && !__all_sync(0xffffffffu, mbar_try_wait(&bars->q_full, in.j & 1))) break;
-                        ok = wait_warp(&bars->q_full, in.j & 1, abort);
-                    }
-                    ok = ok && wait_warp(&bars->k_full[rk.slot], rk.ph, abort) && wait_warp(&bars->v_full[rv.slot], rv.ph, abort);
-                    if (!ok) break;
-                    tc_fence_after();
-                    fence_proxy_async();  // cp.async data -> tensor-core reads
-                    const uint32_t d = tmem + (uint32_t)((issued & 1) * 128);
-                    const uint64_t k = dk0 + (uint32_t)(rk.slot * (SLOT >> 4)), v = dv0 + (uint32_t)(rv.slot * (SLOT >> 4));
-                    if (on) {
-#pragma unroll
-                        for (int kk = 0; kk < 8; ++kk)  // 16 dims: 8 columns of Q, 32 B of a row of K's dim half kk / 4
-                            mma_bf16_ts(d, tmem + Q_COL + (uint32_t)(kk * 8),
-                                        k + (uint64_t)((kk >> 2) * (HALF_STRIDE >> 4) + (kk & 3) * 2), idesc_s, kk > 0);
-#pragma unroll
-                        for (int kk = 0; kk < 8; ++kk)
-                            mma_bf16_ts(d + 64, tmem + DO_COL + (uint32_t)(kk * 8),
-                                        v + (uint64_t)((kk >> 2) * (HALF_STRIDE >> 4) + (kk & 3) * 2), idesc_s, kk > 0);
-                        mma_commit(&bars->v_empty[rv.slot]);
-                        mma_commit(&bars->s_full[issued & 1]);
-                        if (in.last()) mma_commit(&bars->q_empty);
-                    }
-                    __syncwarp();
-                    rk.next();
-                    rv.next();
-                    in.next();
-                    ++issued;
-                    ++ahead;
-                }
+            for (int x = 0; ok && x < n_tiles; ++x) {
+                if (at.first()) ok = wait_warp(&bars->q_full, at.j & 1, abort);
+                ok = ok && wait_warp(&bars->k_full[rk.slot], rk.ph, abort);
                 if (!ok) break;
-                const int w = done & 1;
-                // (the segment before: its dQ has been read)
-                if (out.first() && out.j >= 1) ok = wait_warp(&bars->dq_empty, (out.j - 1) & 1, abort);
-                ok = ok && wait_warp(&bars->p_full[w], (p_ph >> w) & 1, abort);
-                if (!ok) break;
-                p_ph ^= 1u << w;
                 tc_fence_after();
-                const uint64_t k = dkt0 + (uint32_t)(rk2.slot * (SLOT >> 4));
+                fence_proxy_async();  // cp.async data -> tensor-core reads
+                const uint64_t k = dk0 + (uint32_t)(rk.slot * (SLOT >> 4)), v = dv0 + (uint32_t)(rv.slot * (SLOT >> 4));
                 if (on) {
 #pragma unroll
-                    for (int kk = 0; kk < TILE / 16; ++kk)  // 16 tokens: 8 columns of ds, two 8-token groups of K
-                        mma_bf16_ts(tmem + DQ_COL, tmem + (uint32_t)(w * 128 + 64 + (kk >> 1) * 32 + (kk & 1) * 8),
-                                    k + (uint64_t)(kk * (2 * GROUP_STRIDE >> 4)), idesc_q, kk > 0 || !out.first());
-                    mma_commit(&bars->k_empty[rk2.slot]);
-                    if (out.last()) mma_commit(&bars->dq_full);
+                    for (int kk = 0; kk < 8; ++kk)  // 16 dims: 8 columns of Q, 32 B of a row of K's dim half kk / 4
+                        mma_bf16_ts(tmem, tmem + Q_COL + (uint32_t)(kk * 8),
+                                    k + (uint64_t)((kk >> 2) * (HALF_STRIDE >> 4) + (kk & 3) * 2), idesc_s, kk > 0);
+                    mma_commit(&bars->s_full);
                 }
                 __syncwarp();
-                rk2.next();
-                out.next();
-                ++done;
-                --ahead;
+                ok = wait_warp(&bars->v_full[rv.slot], rv.ph, abort);
+                if (!ok) break;
+                tc_fence_after();
+                fence_proxy_async();
+                if (on) {
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)
+                        mma_bf16_ts(tmem + DP_COL, tmem + DO_COL + (uint32_t)(kk * 8),
+                                    v + (uint64_t)((kk >> 2) * (HALF_STRIDE >> 4) + (kk & 3) * 2), idesc_s, kk > 0);
+                    mma_commit(&bars->d_full);
+                    mma_commit(&bars->v_empty[rv.slot]);
+                    if (at.last()) mma_commit(&bars->q_empty);
+                }
+                __syncwarp();
+                // (the segment before: its dQ has been read)
+                if (at.first() && at.j >= 1) ok = wait_warp(&bars->dq_empty, (at.j - 1) & 1, abort);
+                ok = ok && wait_warp(&bars->p_full, x & 1, abort);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t kt = dkt0 + (uint32_t)(rk.slot * (SLOT >> 4));
+                if (on) {
+#pragma unroll
+                    for (int kk = 0; kk < TILE / 16; ++kk)  // 16 tokens: 8 columns of ds (of its half's), two 8-token groups of K
+                        mma_bf16_ts(tmem + DQ_COL, tmem + (uint32_t)((kk >> 2) * 64 + (kk & 3) * 8),
+                                    kt + (uint64_t)(kk * (2 * GROUP_STRIDE >> 4)), idesc_q, kk > 0 || !at.first());
+                    mma_commit(&bars->k_empty[rk.slot]);
+                    if (at.last()) mma_commit(&bars->dq_full);
+                }
+                __syncwarp();
+                rk.next();
+                rv.next();
+                at.next();
             }
         }
         if (on) mma_commit(&bars->fin);  // completes when every MMA is done
@@ -857,8 +851,8 @@ bool make_layout(const TreeArgs &a, int rb_rows, bool nodes, Layout *lay) {
     lay->off_do = lay->off_q + rows * STAGE_ROW;
     lay->off_n = lay->off_do + rows * STAGE_ROW;
     const int at = (lay->off_n + (nodes ? (int)sizeof(Nodes) : 0) + 1023) & ~1023, slots = (SMEM_MAX - 1024 - at) / SLOT;
-    if (slots < 4) return false;
-    lay->nv = slots / 2 < MAX_RING ? slots / 2 : MAX_RING;
+    if (slots < 3) return false;
+    lay->nv = slots / 2 < MAX_RING ? slots / 2 : MAX_RING;  // (K is held until dQ has read it)
     lay->nk = slots - lay->nv < MAX_RING ? slots - lay->nv : MAX_RING;
     lay->off_k = at;
     lay->off_v = lay->off_k + lay->nk * SLOT;
