@@ -1,7 +1,7 @@
 // The cache's part of the backward pass of tree attention (sp_tree_back.cu) on tcgen05 tensor
-// cores: head_dim 128, bf16 rows and cache.  Per key tile of 64 cached tokens and block of up to 128
+// cores: head_dim 128, bf16 rows and cache.  Per key tile of 128 cached tokens and block of up to 128
 // query rows of a kv head, rows on the MMA's M side:
-//   S = Q K^T, dP = dO V^T   128 x 64 each, Q and dO in TMEM, K and V in shared memory
+//   S = Q K^T, dP = dO V^T   128 x 128 each, Q and dO in TMEM, K and V in shared memory
 //   ds = p (dP - D)          p = exp(scale S - lse), a row a thread, written as bf16 over dP in TMEM
 //   dQ += ds K               from TMEM; K is read a second time where it lies (MN-major)
 // The log sums are known, so that a tile's weights are final: nothing is rescaled, two softmax
@@ -14,7 +14,7 @@
 //
 // Warps 0-7 softmax; 8-11 bring queries and output gradients (a segment ahead into shared memory,
 // then into TMEM) and write dQ out; 12 MMA issuer and TMEM; 13 K, 14 V (TMA boxes of whole pages, cp.async
-// elsewhere).  TMEM: [S dP] x 2 in columns 0-255, dQ, Q, dO behind.  Every wait is time-limited
+// elsewhere).  TMEM: S, dP, dQ, Q, dO in all 512 columns.  Every wait is time-limited
 // (SP_DEV_TIMEOUT).
 #include <string.h>
 
@@ -49,7 +49,7 @@ struct Layout {
 };
 struct Bars {
     uint64_t k_full[MAX_RING], k_empty[MAX_RING], v_full[MAX_RING], v_empty[MAX_RING];
-    uint64_t s_full, d_full, p_full, q_full, q_empty, dq_full, dq_empty, fin;
+    uint64_t s_full, s_read, d_full, p_full, q_full, q_empty, dq_full, dq_empty, fin;
     uint32_t tmem;
     int abort;
     int wsum[32];
@@ -451,6 +451,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             mbar_init(&bars->v_empty[i], 1);
         }
         mbar_init(&bars->s_full, 1);
+        mbar_init(&bars->s_read, 8);
         mbar_init(&bars->d_full, 1);
         mbar_init(&bars->p_full, 8);
         mbar_init(&bars->q_full, 4);
@@ -526,7 +527,9 @@ __global__ void __launch_bounds__(THREADS, 1)
                     ld_wait(s + 32);
 #pragma unroll
                     for (int e = 0; e < 64; ++e) s[e] = fast_exp2(fmaf(s[e], a.scale_log2, -st.x));
+                    tc_fence_before();
                 }
+                arrive_warp(&bars->s_read, lane);  // the next scores may be formed
                 ok = wait_warp(&bars->d_full, ph, abort);
                 if (!ok) break;
                 tc_fence_after();
@@ -546,7 +549,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                         uint32_t pk[16];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) pk[e] = pack_bf16(d[2 * e], d[2 * e + 1]);
-                        st16_async(s_col + c * 16, pk);  // over scores that this warp has read
+                        st16_async(s_col + DP_COL + c * 16, pk);  // over products that this warp has read
                     }
                     st_wait();
                 }
@@ -738,25 +741,28 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (bad && lane == 0 && a.status) atomicOr(a.status, SP_DEV_BAD_PAGE);
     } else if (warp == MMA) {
         // ------------------------------------------------------------ MMA issue
-        // One issuer, one tile at a time: S into the columns that the gradients before lay in (their
-        // product is in front of it in the pipe), dP, and, when the softmax is done, dQ.
+        // One issuer.  Per tile x: dP, beside which the softmax forms the weights; the scores of tile
+        // x + 1 as soon as it has read those of x, beside which it forms ds (over dP); dQ, which is in front
+        // of the next dP in the pipe.  Where tile x + 1 begins a segment whose queries are not there
+        // yet, its scores come behind dQ.
         const bool on = elect_one();
         constexpr uint32_t idesc_s = idesc_bf16_f32(128, TILE), idesc_q = idesc_bf16_f32_bmn(128, DH);
         const uint64_t dk0 = sw128_kmajor_desc_sbo(smem + lay.off_k, GROUP_STRIDE);
         const uint64_t dv0 = sw128_kmajor_desc_sbo(smem + lay.off_v, GROUP_STRIDE);
         const uint64_t dkt0 = sw128_mnmajor_desc2(smem + lay.off_k, HALF_STRIDE, GROUP_STRIDE);
-        Ring rk(lay.nk), rv(lay.nv);
+        Ring rk(lay.nk), rv(lay.nv), rk2(lay.nk);  // of S, of dP, of dQ
         bool ok = n_tiles > 0;
         if (ok) {
-            Walk at(sh);
-#pragma unroll 1
-            for (int x = 0; ok && x < n_tiles; ++x) {
-                if (at.first()) ok = wait_warp(&bars->q_full, at.j & 1, abort);
+            Walk in(sh), at(sh);                   // the tiles of S, of dP and dQ
+            int scored = 0;
+            const auto scores = [&]() {
+                if (in.first()) ok = wait_warp(&bars->q_full, in.j & 1, abort);
                 ok = ok && wait_warp(&bars->k_full[rk.slot], rk.ph, abort);
-                if (!ok) break;
+                if (scored > 0) ok = ok && wait_warp(&bars->s_read, (scored - 1) & 1, abort);
+                if (!ok) return;
                 tc_fence_after();
                 fence_proxy_async();  // cp.async data -> tensor-core reads
-                const uint64_t k = dk0 + (uint32_t)(rk.slot * (SLOT >> 4)), v = dv0 + (uint32_t)(rv.slot * (SLOT >> 4));
+                const uint64_t k = dk0 + (uint32_t)(rk.slot * (SLOT >> 4));
                 if (on) {
 #pragma unroll
                     for (int kk = 0; kk < 8; ++kk)  // 16 dims: 8 columns of Q, 32 B of a row of K's dim half kk / 4
@@ -765,10 +771,18 @@ __global__ void __launch_bounds__(THREADS, 1)
                     mma_commit(&bars->s_full);
                 }
                 __syncwarp();
+                rk.next();
+                in.next();
+                ++scored;
+            };
+            scores();
+#pragma unroll 1
+            for (int x = 0; ok && x < n_tiles; ++x) {
                 ok = wait_warp(&bars->v_full[rv.slot], rv.ph, abort);
                 if (!ok) break;
                 tc_fence_after();
                 fence_proxy_async();
+                const uint64_t v = dv0 + (uint32_t)(rv.slot * (SLOT >> 4));
                 if (on) {
 #pragma unroll
                     for (int kk = 0; kk < 8; ++kk)
@@ -779,24 +793,26 @@ __global__ void __launch_bounds__(THREADS, 1)
                     if (at.last()) mma_commit(&bars->q_empty);
                 }
                 __syncwarp();
+                if (x + 1 < n_tiles && (!in.first() || __all_sync(0xffffffffu, mbar_try_wait(&bars->q_full, in.j & 1)))) scores();
                 // (the segment before: its dQ has been read)
-                if (at.first() && at.j >= 1) ok = wait_warp(&bars->dq_empty, (at.j - 1) & 1, abort);
+                if (at.first() && at.j >= 1) ok = ok && wait_warp(&bars->dq_empty, (at.j - 1) & 1, abort);
                 ok = ok && wait_warp(&bars->p_full, x & 1, abort);
                 if (!ok) break;
                 tc_fence_after();
-                const uint64_t kt = dkt0 + (uint32_t)(rk.slot * (SLOT >> 4));
+                const uint64_t kt = dkt0 + (uint32_t)(rk2.slot * (SLOT >> 4));
                 if (on) {
 #pragma unroll
                     for (int kk = 0; kk < TILE / 16; ++kk)  // 16 tokens: 8 columns of ds (of its half's), two 8-token groups of K
-                        mma_bf16_ts(tmem + DQ_COL, tmem + (uint32_t)((kk >> 2) * 64 + (kk & 3) * 8),
+                        mma_bf16_ts(tmem + DQ_COL, tmem + DP_COL + (uint32_t)((kk >> 2) * 64 + (kk & 3) * 8),
                                     kt + (uint64_t)(kk * (2 * GROUP_STRIDE >> 4)), idesc_q, kk > 0 || !at.first());
-                    mma_commit(&bars->k_empty[rk.slot]);
+                    mma_commit(&bars->k_empty[rk2.slot]);
                     if (at.last()) mma_commit(&bars->dq_full);
                 }
                 __syncwarp();
-                rk.next();
+                rk2.next();
                 rv.next();
                 at.next();
+                if (x + 1 < n_tiles && scored == x + 1) scores();
             }
         }
         if (on) mma_commit(&bars->fin);  // completes when every MMA is done
