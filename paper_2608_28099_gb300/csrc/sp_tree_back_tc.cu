@@ -609,8 +609,11 @@ __global__ void __launch_bounds__(THREADS, 1)
             bool live = false;
             if (active && whole) live = node < n && (NODES ? ns->stat[j & 1][r].x : __ldcg(&args.stat[row].x)) != INFINITY;
             ok = ok && wait_warp(&bars->dq_full, j & 1, abort);
-            tc_fence_after();
+            // the accumulator goes out as it is, so that the next segment may use it at once; a row that is
+            // whole comes back to the thread that wrote it
+            float *mine = a.part_o + (slot * a.rb_rows + r) * DH;
             if (ok && warp_active) {
+                tc_fence_after();
 #pragma unroll 1
                 for (int d = 0; d < DH; d += 32) {
                     float v[32];
@@ -618,28 +621,26 @@ __global__ void __launch_bounds__(THREADS, 1)
                     ld32_async(lane_base + DQ_COL + (uint32_t)d, v);
                     ld_wait(v);
                     if (!active) continue;
-                    if (whole) {
-                        bf16 *to = (bf16 *)args.dq + ((size_t)b * a.N + node) * a.qs + (size_t)(g * a.G + rr - node * a.G) * DH + d;
-                        const float4 *more = (const float4 *)(args.dq_new + row * DH + d);
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8) {
-                            const float4 x = __ldcg(more + e / 4), y = __ldcg(more + e / 4 + 1);
-                            const float f = args.scale;
-                            *(uint4 *)(to + e) = live ? make_uint4(pack_bf16((v[e] + x.x) * f, (v[e + 1] + x.y) * f),
-                                                                   pack_bf16((v[e + 2] + x.z) * f, (v[e + 3] + x.w) * f),
-                                                                   pack_bf16((v[e + 4] + y.x) * f, (v[e + 5] + y.y) * f),
-                                                                   pack_bf16((v[e + 6] + y.z) * f, (v[e + 7] + y.w) * f))
-                                                      : make_uint4(0, 0, 0, 0);
-                        }
-                    } else {
-                        float *to = a.part_o + (slot * a.rb_rows + r) * DH + d;
-#pragma unroll
-                        for (int e = 0; e < 32; e += 4) *(float4 *)(to + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
-                    }
+                    for (int e = 0; e < 32; e += 4) *(float4 *)(mine + d + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                }
+                tc_fence_before();
+            }
+            if (ok) arrive_warp(&bars->dq_empty, lane);
+            if (ok && active && whole) {
+                bf16 *to = (bf16 *)args.dq + ((size_t)b * a.N + node) * a.qs + (size_t)(g * a.G + rr - node * a.G) * DH;
+                const float4 *more = (const float4 *)(args.dq_new + row * DH), *had = (const float4 *)mine;
+                const float f = args.scale;
+#pragma unroll 4
+                for (int e = 0; e < DH / 8; ++e) {
+                    const float4 x = __ldcg(more + 2 * e), y = __ldcg(more + 2 * e + 1), u = had[2 * e], v = had[2 * e + 1];
+                    *(uint4 *)(to + e * 8) = live ? make_uint4(pack_bf16((u.x + x.x) * f, (u.y + x.y) * f),
+                                                               pack_bf16((u.z + x.z) * f, (u.w + x.w) * f),
+                                                               pack_bf16((v.x + y.x) * f, (v.y + y.y) * f),
+                                                               pack_bf16((v.z + y.z) * f, (v.w + y.w) * f))
+                                                  : make_uint4(0, 0, 0, 0);
                 }
             }
-            tc_fence_before();
-            if (ok) arrive_warp(&bars->dq_empty, lane);
             if (j + 1 < n_seg) between(j + 1);
         }
     } else if (warp == K_WARP || warp == V_WARP) {
