@@ -327,6 +327,18 @@ __device__ __forceinline__ uint64_t sw128_kmajor_desc_sbo(const void *tile, uint
     return d;
 }
 
+// The same for rows of 16 bf16 = 32 B with the 32-byte swizzle (8-row groups 256 B
+// apart): 16-byte chunk c of row r lies at 32 r + 16 (c ^ (r >> 2 & 1)).
+__device__ __forceinline__ uint64_t sw32_kmajor_desc(const void *tile) {
+    const uint64_t addr = smem_u32(tile);
+    uint64_t d = (addr & 0x3FFFFull) >> 4;
+    d |= 1ull << 16;
+    d |= (uint64_t)(256 >> 4) << 32;
+    d |= 1ull << 46;
+    d |= 6ull << 61;
+    return d;
+}
+
 // Shared-memory matrix descriptor for an MN-major operand stored with the
 // 128-byte swizzle: rows run along K (8-row groups 1024 B apart), each row holds
 // 64 consecutive MN elements; successive 64-wide MN chunks are `mn_stride`

@@ -9,8 +9,7 @@
 //
 // Work: the cached tokens of every sequence are cut into tiles, the list of all tiles into shares (as
 // in sp_attn_plan.cuh), CTA (share, kv head, row block) walks its share; its piece of a sequence is
-// a segment.  A pair that lies inside one share is finished there (with the nodes' part, formed by the
-// kernel in front), the others leave partials that a second kernel adds in share order.
+// a segment.  A pair that lies inside one share is finished there, the others leave partials that a second kernel adds in share order.
 //
 // Warps 0-7 softmax; 8-11 bring queries and output gradients (a segment ahead into shared memory,
 // then into TMEM) and write dQ out; 12 MMA issuer and TMEM; 13 K, 14 V (TMA boxes of whole pages, cp.async
@@ -40,16 +39,17 @@ constexpr int EPI = 8, MMA = 12, K_WARP = 13, V_WARP = 14;
 constexpr uint32_t DP_COL = 128, DQ_COL = 256, Q_COL = 384, DO_COL = 448;  // TMEM: S, dP, dQ, Q, dO
 // Fewest tiles a share holds on average, and the cost of a segment in tiles.
 constexpr int kBackMinTiles = 2;
-constexpr int kBackSegCost = 2;
+constexpr int kBackSegCost = 5;
 
 struct Layout {
     int nk, nv;                                 // ring slots
-    int off_q, off_do, off_n, off_k, off_v, off_tab;  // (off_q, off_do: staged rows; off_n: Nodes)
+    int off_q, off_do, off_n, off_ds, off_kn, off_k, off_v, off_tab;  // (off_q, off_do: staged rows; off_n:
+                                                // Nodes; off_ds, off_kn: operands of the nodes' part of dQ)
     int smem;
 };
 struct Bars {
     uint64_t k_full[MAX_RING], k_empty[MAX_RING], v_full[MAX_RING], v_empty[MAX_RING];
-    uint64_t s_full, s_read, d_full, p_full, q_full, q_empty, dq_full, dq_empty, fin;
+    uint64_t s_full, s_read, d_full, p_full, n_full, q_full, q_empty, dq_full, dq_empty, fin;
     uint32_t tmem;
     int abort;
     int wsum[32];
@@ -60,9 +60,12 @@ struct Nodes {
     unsigned long long sees[ROWS];
     unsigned odd_row[ROWS];            // bit 0: q, bit 1: dout held something not finite
     unsigned odd_node[MAX_NODES];      // bit 0: k, bit 1: v
-    bf16 k[MAX_NODES][LD], v[MAX_NODES][LD];
-    bf16 p[64][MAX_NODES + 8], ds[64][MAX_NODES + 8];
+    bf16 v[MAX_NODES][LD];
 };
+constexpr int DS_BYTES = ROWS * MAX_NODES * 2;  // gradients of the weights between nodes: the A operand, 32-byte rows
+constexpr int KN_BYTES = MAX_NODES * DH * 2;    // the nodes' keys: the B operand, by segment parity
+constexpr int P_LD = MAX_NODES + 8;             // weights between nodes of 64 rows, in the other parity's place
+static_assert(64 * P_LD * 2 <= KN_BYTES, "weights between nodes");
 constexpr int OFF_CUTS = 1024;
 constexpr int OFF_FRONT = OFF_CUTS + (MAX_GRP + 4) * 4;
 static_assert(sizeof(Bars) <= OFF_CUTS, "barrier block");
@@ -199,10 +202,23 @@ struct Walk {
 // way together.  NODES: the rows' statistics and what the products between nodes need of them, too.
 template <bool NODES>
 __device__ __forceinline__ void stage_rows(const TreeBackArgs &x, int b, int n, int g, int rb, uint8_t *Q, uint8_t *dO, Nodes *ns,
-                                           float2 *stat, int wi, int lane) {
+                                           float2 *stat, uint8_t *kn, bool owner, int wi, int lane) {
     const TreeArgs &a = x.t;
     const int c = lane & 15, rows = (a.rb_rows + 15) & ~15;
     constexpr int AT_ONCE = 4;
+    uint4 nk[2], nv[2];  // the nodes' keys and values, under way beside the first rows
+    if (NODES && owner) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int j = h * 8 + wi * 2 + (lane >> 4);
+            nk[h] = nv[h] = make_uint4(0, 0, 0, 0);
+            if (j < n) {
+                const size_t r = (size_t)b * a.N + j;
+                nk[h] = *(const uint4 *)((const bf16 *)a.k_new + r * a.ks + (size_t)g * DH + c * 8);
+                nv[h] = *(const uint4 *)((const bf16 *)a.v_new + r * a.vs + (size_t)g * DH + c * 8);
+            }
+        }
+    }
 #pragma unroll 1
     for (int r1 = wi * 2 + (lane >> 4); r1 < rows; r1 += AT_ONCE * 8) {
         uint4 q[AT_ONCE], go[AT_ONCE], o[AT_ONCE];
@@ -246,31 +262,29 @@ __device__ __forceinline__ void stage_rows(const TreeBackArgs &x, int b, int n, 
             }
         }
     }
+    if (NODES && owner) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int j = h * 8 + wi * 2 + (lane >> 4);
+            const unsigned half = 0xffffu << (lane & 16);
+            const bool ko = __ballot_sync(0xffffffffu, take_finite(nk[h])) & half;
+            const bool vo = __ballot_sync(0xffffffffu, take_finite(nv[h])) & half;
+            *(uint4 *)(kn + kv_off(j, c)) = nk[h];
+            *(uint4 *)&ns->v[j][c * 8] = nv[h];
+            if (c == 0) ns->odd_node[j] = (ko ? 1u : 0u) | (vo ? 2u : 0u);
+        }
+    }
 }
 // What lies between the nodes of sequence b (one row block, at most 16 nodes): gradients of their
-// keys and values, and their part of dQ, from the staged rows.  mma.sync by four warps that have
-// nothing else to do while a segment's tiles are under way; the operands and what becomes of
-// non-finite elements are those of sp_tree_back_rows.cu.
+// keys and values from the staged rows, and the A operand of their part of dQ, a last product of the
+// segment's accumulator.  mma.sync by four warps that have nothing else to do while a segment's
+// tiles are under way; the operands and what becomes of non-finite elements are those of
+// sp_tree_back_rows.cu.
 __device__ __forceinline__ void node_products(const TreeBackArgs &x, int b, int n, int g, uint8_t *Q, uint8_t *dO, Nodes &s,
-                                              const float2 *stat, int wi, int lane) {
+                                              const float2 *stat, const uint8_t *kn, uint8_t *ds, bf16 *pw, int wi, int lane) {
     const TreeArgs &a = x.t;
-    const int c = lane & 15, rows = (a.rb_rows + 15) & ~15;
+    const int rows = (a.rb_rows + 15) & ~15;
     constexpr int NP = MAX_NODES, NT = DH / 4 / 8;
-#pragma unroll
-    for (int j0 = 0; j0 < NP; j0 += 8) {
-        const int j = j0 + wi * 2 + (lane >> 4);
-        uint4 k = make_uint4(0, 0, 0, 0), v = k;
-        if (j < n) {
-            const size_t r = (size_t)b * a.N + j;
-            k = *(const uint4 *)((const bf16 *)a.k_new + r * a.ks + (size_t)g * DH + c * 8);
-            v = *(const uint4 *)((const bf16 *)a.v_new + r * a.vs + (size_t)g * DH + c * 8);
-        }
-        const unsigned half = 0xffffu << (lane & 16);
-        const bool ko = __ballot_sync(0xffffffffu, take_finite(k)) & half, vo = __ballot_sync(0xffffffffu, take_finite(v)) & half;
-        *(uint4 *)&s.k[j][c * 8] = k;
-        *(uint4 *)&s.v[j][c * 8] = v;
-        if (c == 0) s.odd_node[j] = (ko ? 1u : 0u) | (vo ? 2u : 0u);
-    }
     {  // a row a thread: non-finite elements out (rare; the raw rows are in TMEM)
         const int r = wi * 32 + lane;
         if (r < rows && s.odd_row[r]) {
@@ -290,16 +304,15 @@ __device__ __forceinline__ void node_products(const TreeBackArgs &x, int b, int 
     for (int j = 0; j < NT; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) dk[j][e] = dv[j][e] = 0.f;
-    const size_t row0 = ((size_t)b * a.Hkv + g) * a.R;
     const auto q_at = [&](int r, int d) { return (const bf16 *)(Q + r * STAGE_ROW) + d; };
     const auto o_at = [&](int r, int d) { return (const bf16 *)(dO + r * STAGE_ROW) + d; };
+    const auto ds_at = [&](int r, int chunk) { return ds + r * 32 + ((chunk ^ (r >> 2 & 1)) << 4); };
 #pragma unroll 1
     for (int r0 = 0; r0 < rows; r0 += 64) {
         if (r0) named_sync(BAR_EPI, 128);  // (the weights before are read)
         const int wr = wi * 16, r_lo = wr + (lane >> 2), col = (lane & 3) * 2;
         if (r0 + wr < rows) {
             float y[NP / 8][4], dp[NP / 8][4];
-            uint32_t ds_frag[NP / 8][2];
 #pragma unroll
             for (int j = 0; j < NP / 8; ++j)
 #pragma unroll
@@ -309,9 +322,9 @@ __device__ __forceinline__ void node_products(const TreeBackArgs &x, int b, int 
                 uint32_t qa[4], oa[4], kb[4], vb[4];
                 ldsm4(qa, q_at(r0 + wr + (lane & 15), kk * 16 + (lane >> 4) * 8));
                 ldsm4(oa, o_at(r0 + wr + (lane & 15), kk * 16 + (lane >> 4) * 8));
-                const int node = (lane & 7) + (lane >> 4) * 8, d = kk * 16 + ((lane >> 3) & 1) * 8;
-                ldsm4(kb, &s.k[node][d]);
-                ldsm4(vb, &s.v[node][d]);
+                const int node = (lane & 7) + (lane >> 4) * 8, d = kk * 2 + ((lane >> 3) & 1);
+                ldsm4(kb, kn + kv_off(node, d));
+                ldsm4(vb, &s.v[node][d * 8]);
                 mma16816(y[0], qa, kb[0], kb[1]);
                 mma16816(y[1], qa, kb[2], kb[3]);
                 mma16816(dp[0], oa, vb[0], vb[1]);
@@ -339,37 +352,20 @@ __device__ __forceinline__ void node_products(const TreeBackArgs &x, int b, int 
                         p[e] = vis ? w : 0.f;
                         d[e] = vis ? z : 0.f;
                     }
-                    ds_frag[j][h] = pack_bf16(d[0], d[1]);
-                    *(uint32_t *)&s.p[rl][j * 8 + col] = pack_bf16(p[0], p[1]);
-                    *(uint32_t *)&s.ds[rl][j * 8 + col] = ds_frag[j][h];
-                }
-            }
-            const uint32_t da[4] = {ds_frag[0][0], ds_frag[0][1], ds_frag[1][0], ds_frag[1][1]};
-#pragma unroll 2
-            for (int j = 0; j < DH / 16; ++j) {  // the nodes' part of dQ, 16 dims at a time
-                uint32_t kb[4];
-                float u0[4] = {0.f, 0.f, 0.f, 0.f}, u1[4] = {0.f, 0.f, 0.f, 0.f};
-                ldsm4t(kb, &s.k[lane & 15][j * 16 + (lane >> 4) * 8]);
-                mma16816(u0, da, kb[0], kb[1]);
-                mma16816(u1, da, kb[2], kb[3]);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int rr = r0 + r_lo + 8 * h;
-                    if (rr >= a.R) continue;
-                    float *to = x.dq_new + (row0 + rr) * DH + j * 16 + col;
-                    *(float2 *)to = make_float2(u0[2 * h], u0[2 * h + 1]);
-                    *(float2 *)(to + 8) = make_float2(u1[2 * h], u1[2 * h + 1]);
+                    *(uint32_t *)&pw[rl * P_LD + j * 8 + col] = pack_bf16(p[0], p[1]);
+                    *(uint32_t *)(ds_at(r, j) + col * 2) = pack_bf16(d[0], d[1]);
                 }
             }
         }
         named_sync(BAR_EPI, 128);
         const int d0 = wi * (DH / 4);
-#pragma unroll 1
-        for (int kk = 0; kk < 4 && r0 + kk * 16 < rows; ++kk) {
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+            if (r0 + kk * 16 >= rows) break;
             uint32_t da[4], pa[4];
-            const int r = kk * 16 + (lane & 7) + (lane >> 4) * 8, node = ((lane >> 3) & 1) * 8;
-            ldsm4t(da, &s.ds[r][node]);
-            ldsm4t(pa, &s.p[r][node]);
+            const int r = kk * 16 + (lane & 7) + (lane >> 4) * 8, chunk = (lane >> 3) & 1;
+            ldsm4t(da, ds_at(r0 + r, chunk));
+            ldsm4t(pa, &pw[r * P_LD + chunk * 8]);
 #pragma unroll
             for (int j = 0; j < NT / 2; ++j) {
                 uint32_t qb[4], ob[4];
@@ -454,6 +450,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         mbar_init(&bars->s_read, 8);
         mbar_init(&bars->d_full, 1);
         mbar_init(&bars->p_full, 8);
+        mbar_init(&bars->n_full, 4);
         mbar_init(&bars->q_full, 4);
         mbar_init(&bars->q_empty, 1);
         mbar_init(&bars->dq_full, 1);
@@ -568,7 +565,8 @@ __global__ void __launch_bounds__(THREADS, 1)
         const auto load = [&](int j) {
             const int b = sh.b0 + j;
             named_sync(BAR_EPI, 128);  // (the staged rows before are in TMEM)
-            stage_rows<NODES>(args, b, nodes[b], g, rb, smem + lay.off_q, smem + lay.off_do, ns, ns->stat[j & 1], quad, lane);
+            stage_rows<NODES>(args, b, nodes[b], g, rb, smem + lay.off_q, smem + lay.off_do, ns, ns->stat[j & 1],
+                              smem + lay.off_kn + (j & 1) * KN_BYTES, sh.x0 <= prefix[b], quad, lane);
             named_sync(BAR_EPI, 128);
             const bool free = wait_warp(&bars->q_empty, (j & 1) ^ 1, abort);
             if (free && warp_active) {
@@ -590,9 +588,11 @@ __global__ void __launch_bounds__(THREADS, 1)
             const int b = sh.b0 + j;
             if (!NODES || sh.x0 > prefix[b]) return;
             const float2 *stat = ns->stat[j & 1];
-            node_products(args, b, nodes[b], g, smem + lay.off_q, smem + lay.off_do, *ns, stat, quad, lane);
+            node_products(args, b, nodes[b], g, smem + lay.off_q, smem + lay.off_do, *ns, stat, smem + lay.off_kn + (j & 1) * KN_BYTES,
+                          smem + lay.off_ds, (bf16 *)(smem + lay.off_kn + (~j & 1) * KN_BYTES), quad, lane);
             if (active) args.stat[((size_t)b * Hkv + g) * a.R + rr] = stat[r];
-            named_sync(BAR_EPI, 128);  // (dq_new is read by other threads)
+            fence_proxy_async();  // ds and the nodes' keys -> tensor-core reads
+            arrive_warp(&bars->n_full, lane);
         };
         if (n_seg > 0) between(0);
 #pragma unroll 1
@@ -609,11 +609,12 @@ __global__ void __launch_bounds__(THREADS, 1)
             bool live = false;
             if (active && whole) live = node < n && (NODES ? ns->stat[j & 1][r].x : __ldcg(&args.stat[row].x)) != INFINITY;
             ok = ok && wait_warp(&bars->dq_full, j & 1, abort);
-            // the accumulator goes out as it is, so that the next segment may use it at once; a row that is
-            // whole comes back to the thread that wrote it
-            float *mine = a.part_o + (slot * a.rb_rows + r) * DH;
             if (ok && warp_active) {
                 tc_fence_after();
+                float *part = a.part_o + (slot * a.rb_rows + r) * DH;
+                bf16 *to = (bf16 *)args.dq + ((size_t)b * a.N + node) * a.qs + (size_t)(g * a.G + rr - node * a.G) * DH;
+                const float4 *more = (const float4 *)(args.dq_new + row * DH);
+                const float f = args.scale;
 #pragma unroll 1
                 for (int d = 0; d < DH; d += 32) {
                     float v[32];
@@ -621,26 +622,27 @@ __global__ void __launch_bounds__(THREADS, 1)
                     ld32_async(lane_base + DQ_COL + (uint32_t)d, v);
                     ld_wait(v);
                     if (!active) continue;
+                    if (whole) {
+                        if (!NODES) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4) *(float4 *)(mine + d + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                            for (int e = 0; e < 32; e += 4) {
+                                const float4 y = __ldcg(more + (d + e) / 4);
+                                v[e] += y.x, v[e + 1] += y.y, v[e + 2] += y.z, v[e + 3] += y.w;
+                            }
+                        }
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8)
+                            *(uint4 *)(to + d + e) = live ? make_uint4(pack_bf16(v[e] * f, v[e + 1] * f), pack_bf16(v[e + 2] * f, v[e + 3] * f),
+                                                                       pack_bf16(v[e + 4] * f, v[e + 5] * f), pack_bf16(v[e + 6] * f, v[e + 7] * f))
+                                                          : make_uint4(0, 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4) *(float4 *)(part + d + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                    }
                 }
                 tc_fence_before();
             }
             if (ok) arrive_warp(&bars->dq_empty, lane);
-            if (ok && active && whole) {
-                bf16 *to = (bf16 *)args.dq + ((size_t)b * a.N + node) * a.qs + (size_t)(g * a.G + rr - node * a.G) * DH;
-                const float4 *more = (const float4 *)(args.dq_new + row * DH), *had = (const float4 *)mine;
-                const float f = args.scale;
-#pragma unroll 4
-                for (int e = 0; e < DH / 8; ++e) {
-                    const float4 x = __ldcg(more + 2 * e), y = __ldcg(more + 2 * e + 1), u = had[2 * e], v = had[2 * e + 1];
-                    *(uint4 *)(to + e * 8) = live ? make_uint4(pack_bf16((u.x + x.x) * f, (u.y + x.y) * f),
-                                                               pack_bf16((u.z + x.z) * f, (u.w + x.w) * f),
-                                                               pack_bf16((v.x + y.x) * f, (v.y + y.y) * f),
-                                                               pack_bf16((v.z + y.z) * f, (v.w + y.w) * f))
-                                                  : make_uint4(0, 0, 0, 0);
-                }
-            }
             if (j + 1 < n_seg) between(j + 1);
         }
     } else if (warp == K_WARP || warp == V_WARP) {
@@ -756,6 +758,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (ok) {
             Walk in(sh), at(sh);                   // the tiles of S, of dP and dQ
             int scored = 0;
+            uint32_t n_ph = 0;
             const auto scores = [&]() {
                 if (in.first()) ok = wait_warp(&bars->q_full, in.j & 1, abort);
                 ok = ok && wait_warp(&bars->k_full[rk.slot], rk.ph, abort);
@@ -807,9 +810,25 @@ __global__ void __launch_bounds__(THREADS, 1)
                         mma_bf16_ts(tmem + DQ_COL, tmem + DP_COL + (uint32_t)((kk >> 2) * 64 + (kk & 3) * 8),
                                     kt + (uint64_t)(kk * (2 * GROUP_STRIDE >> 4)), idesc_q, kk > 0 || !at.first());
                     mma_commit(&bars->k_empty[rk2.slot]);
-                    if (at.last()) mma_commit(&bars->dq_full);
                 }
                 __syncwarp();
+                if (at.last()) {
+                    const bool mine = NODES && sh.x0 <= prefix[sh.b0 + at.j];  // the nodes' part, by their sequence's first share
+                    if (mine) {
+                        ok = wait_warp(&bars->n_full, n_ph, abort);
+                        n_ph ^= 1;
+                        if (!ok) break;
+                        tc_fence_after();
+                        fence_proxy_async();
+                    }
+                    if (on) {
+                        if (mine)
+                            mma_bf16(tmem + DQ_COL, sw32_kmajor_desc(smem + lay.off_ds),
+                                     sw128_mnmajor_desc2(smem + lay.off_kn + (at.j & 1) * KN_BYTES, HALF_STRIDE, GROUP_STRIDE), idesc_q, 1u);
+                        mma_commit(&bars->dq_full);
+                    }
+                    __syncwarp();
+                }
                 rk2.next();
                 rv.next();
                 at.next();
@@ -831,7 +850,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 // dQ of the pairs that lie in several shares (at most one starts in each share): a warp per (share,
 // kv head, row), four dims a lane, the partials in share order, SUM_AT of them under way together.
 constexpr int SUM_THREADS = 128, SUM_ROWS = SUM_THREADS / 32, SUM_AT = 8;
-__global__ void __launch_bounds__(SUM_THREADS) tree_back_tc_sum_kernel(const __grid_constant__ TreeBackArgs args, const int2 *split_tab) {
+__global__ void __launch_bounds__(SUM_THREADS) tree_back_tc_sum_kernel(const __grid_constant__ TreeBackArgs args, const int2 *split_tab, int add_nodes) {
     const TreeArgs &a = args.t;
     pdl_wait();
     const int hv = blockIdx.x, j0 = blockIdx.y, Hv = a.Hkv * a.n_rb, g = hv / a.n_rb, rb = hv - g * a.n_rb;
@@ -841,7 +860,7 @@ __global__ void __launch_bounds__(SUM_THREADS) tree_back_tc_sum_kernel(const __g
     const int q = blockIdx.z * SUM_ROWS + (threadIdx.x >> 5), rr = rb * a.rb_rows + q;
     if (q >= a.rb_rows || rr >= a.R) return;
     const size_t at = ((size_t)b * a.Hkv + g) * a.R + rr;
-    float4 s = __ldcg((const float4 *)(args.dq_new + at * DH + c));
+    float4 s = add_nodes ? __ldcg((const float4 *)(args.dq_new + at * DH + c)) : make_float4(0.f, 0.f, 0.f, 0.f);
     const bool live = __ldcg(&args.stat[at].x) != INFINITY;  // (+inf for a node that is not there, too)
 #pragma unroll 1
     for (int e0 = 0; e0 < tab.y; e0 += SUM_AT) {
@@ -867,7 +886,9 @@ bool make_layout(const TreeArgs &a, int rb_rows, bool nodes, Layout *lay) {
     const int rows = (rb_rows + 15) & ~15;
     lay->off_do = lay->off_q + rows * STAGE_ROW;
     lay->off_n = lay->off_do + rows * STAGE_ROW;
-    const int at = (lay->off_n + (nodes ? (int)sizeof(Nodes) : 0) + 1023) & ~1023, slots = (SMEM_MAX - 1024 - at) / SLOT;
+    lay->off_ds = (lay->off_n + (nodes ? (int)sizeof(Nodes) : 0) + 1023) & ~1023;
+    lay->off_kn = lay->off_ds + (nodes ? DS_BYTES : 0);
+    const int at = lay->off_kn + (nodes ? 2 * KN_BYTES : 0), slots = (SMEM_MAX - 1024 - at) / SLOT;
     if (slots < 3) return false;
     lay->nv = slots / 2 < MAX_RING ? slots / 2 : MAX_RING;  // (K is held until dQ has read it)
     lay->nk = slots - lay->nv < MAX_RING ? slots - lay->nv : MAX_RING;
@@ -927,7 +948,7 @@ cudaError_t launch_tree_back_tc(const TreeBackArgs &args, int2 *split_tab, cudaS
     e = launch_k(kernel, dim3(a.plan.tc_ctas), dim3(THREADS), (size_t)lay.smem, st, mk, mv, args, lay, split_tab);
     if (e != cudaSuccess) return e;
     return launch_k(tree_back_tc_sum_kernel, dim3(a.Hkv * a.n_rb, tree_back_tc_groups(a), ceil_div(a.rb_rows, SUM_ROWS)),
-                    dim3(SUM_THREADS), 0, st, args, (const int2 *)split_tab);
+                    dim3(SUM_THREADS), 0, st, args, (const int2 *)split_tab, (int)!nodes);
 }
 
 }  // namespace sp
