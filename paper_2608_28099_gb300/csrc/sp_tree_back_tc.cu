@@ -223,11 +223,13 @@ __device__ __forceinline__ void stage_rows(const TreeBackArgs &x, int b, int n, 
     for (int r1 = wi * 2 + (lane >> 4); r1 < rows; r1 += AT_ONCE * 8) {
         uint4 q[AT_ONCE], go[AT_ONCE], o[AT_ONCE];
         float lse[AT_ONCE];
+        unsigned long long bits[AT_ONCE];
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
             const int r = r1 + k * 8, rr = rb * a.rb_rows + r, node = rr / a.G;
             q[k] = go[k] = o[k] = make_uint4(0, 0, 0, 0);
             lse[k] = -INFINITY;
+            bits[k] = 0;
             if (r < a.rb_rows && rr < a.R && node < n) {
                 const int hd = g * a.G + rr - node * a.G;
                 const size_t head = (size_t)hd * DH + c * 8, row = (size_t)b * a.N + node;
@@ -236,6 +238,7 @@ __device__ __forceinline__ void stage_rows(const TreeBackArgs &x, int b, int n, 
                 if (NODES) {
                     o[k] = *(const uint4 *)((const bf16 *)a.out + row * a.Hq * DH + head);
                     lse[k] = a.lse[row * a.Hq + hd];
+                    bits[k] = tree_mask(a, b, node, n);
                 }
             }
         }
@@ -256,7 +259,7 @@ __device__ __forceinline__ void stage_rows(const TreeBackArgs &x, int b, int n, 
                     float2 st = make_float2(INFINITY, 0.f);
                     if (lse[k] != -INFINITY) st = make_float2(lse[k] == INFINITY ? NAN : lse[k] * 1.4426950408889634f, d);
                     stat[r] = st;
-                    ns->sees[r] = st.x == INFINITY ? 0 : tree_mask(a, b, r / a.G, n);
+                    ns->sees[r] = st.x == INFINITY ? 0 : bits[k];
                     ns->odd_row[r] = (qo ? 1u : 0u) | (oo ? 2u : 0u);
                 }
             }
@@ -601,9 +604,9 @@ __global__ void __launch_bounds__(THREADS, 1)
             const int b = sh.b0 + j;
             const Seg sg = piece(sh, b);
             const int n = nodes[b];
-            const int j_first = group_of(cuts, n_grp, sg.xp), j_last = group_of(cuts, n_grp, sg.xp + sg.nt - 1);
-            const bool whole = j_first == j_last;
-            const size_t slot = ((size_t)grp * 2 + (j_first == grp)) * Hv + hv;
+            // slot of a partial: a share has at most two, of the pair that starts in it and of the one that began before
+            const bool starts = sg.xp >= sh.x0, whole = starts && sg.xp + sg.nt <= sh.x1;
+            const size_t slot = ((size_t)grp * 2 + starts) * Hv + hv;
             const int node = rr / a.G;
             const size_t row = ((size_t)b * Hkv + g) * a.R + rr;
             bool live = false;
