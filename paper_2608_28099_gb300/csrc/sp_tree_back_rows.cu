@@ -71,16 +71,19 @@ __global__ void __launch_bounds__(32 * WARPS) tree_back_rows_tc_kernel(const __g
 #pragma unroll 1
     for (int r0 = 0; r0 < a.R; r0 += ROWS) {
         __syncthreads();  // (the rows before are read)
-        // ---- 16 rows a warp: queries, output gradients, statistics; four rows' loads under way together
+        // ---- 16 rows a warp: queries, output gradients, statistics; AT row pairs' loads under way together
+        constexpr int AT = NP == 64 ? 2 : 4;
 #pragma unroll 1
-        for (int k0 = 0; k0 < 8; k0 += 2) {
-            uint4 q[2], go[2], o[2];
-            float lse[2];
+        for (int k0 = 0; k0 < 8; k0 += AT) {
+            uint4 q[AT], go[AT], o[AT];
+            float lse[AT];
+            unsigned long long bits[AT];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < AT; ++k) {
                 const int rr = r0 + warp * 16 + (k0 + k) * 2 + (lane >> 4), node = rr / a.G;
                 q[k] = go[k] = o[k] = make_uint4(0, 0, 0, 0);
                 lse[k] = -INFINITY;
+                bits[k] = 0;
                 if (rr < a.R && node < n) {
                     const int head = g * a.G + rr - node * a.G;
                     const size_t row = (size_t)b * a.N + node, at = (row * a.Hq + head) * DH + c * 8;
@@ -88,10 +91,11 @@ __global__ void __launch_bounds__(32 * WARPS) tree_back_rows_tc_kernel(const __g
                     go[k] = *(const uint4 *)((const bf16 *)args.dout + at);
                     o[k] = *(const uint4 *)((const bf16 *)a.out + at);
                     lse[k] = a.lse[row * a.Hq + head];
+                    bits[k] = tree_mask(a, b, node, n);
                 }
             }
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < AT; ++k) {
                 const int r = warp * 16 + (k0 + k) * 2 + (lane >> 4), rr = r0 + r;
                 float d = dot8(go[k], o[k]);
 #pragma unroll
@@ -105,7 +109,7 @@ __global__ void __launch_bounds__(32 * WARPS) tree_back_rows_tc_kernel(const __g
                     float2 st = make_float2(INFINITY, 0.f);
                     if (lse[k] != -INFINITY) st = make_float2(lse[k] == INFINITY ? NAN : lse[k] * 1.4426950408889634f, d);
                     s.stat[r] = st;
-                    s.sees[r] = st.x == INFINITY ? 0 : tree_mask(a, b, rr / a.G, n);
+                    s.sees[r] = st.x == INFINITY ? 0 : bits[k];
                     s.odd_row[r] = (qo ? 1u : 0u) | (oo ? 2u : 0u);
                     if (rr < a.R) args.stat[row0 + rr] = st;
                 }
