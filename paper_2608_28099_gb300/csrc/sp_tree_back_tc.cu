@@ -901,6 +901,14 @@ bool make_layout(const TreeArgs &a, int rb_rows, bool nodes, Layout *lay) {
     return lay->smem <= SMEM_MAX;
 }
 
+template <bool NODES>
+cudaError_t run(const TreeBackArgs &a, const Layout &lay, const CUtensorMap &mk, const CUtensorMap &mv, int2 *tab, cudaStream_t st) {
+    static bool known[MAX_DEVICES] = {};
+    const cudaError_t e = allow_smem(tree_back_tc_kernel<NODES>, SMEM_MAX, known);
+    if (e != cudaSuccess) return e;
+    return launch_k(tree_back_tc_kernel<NODES>, dim3(a.t.plan.tc_ctas), dim3(THREADS), (size_t)lay.smem, st, mk, mv, a, lay, tab);
+}
+
 }  // namespace
 
 bool tree_back_tc_supported(const TreeArgs &a) {
@@ -944,11 +952,7 @@ cudaError_t launch_tree_back_tc(const TreeBackArgs &args, int2 *split_tab, cudaS
     }
     cudaError_t e = nodes ? cudaSuccess : launch_tree_back_rows_tc(args, st);
     if (e != cudaSuccess) return e;
-    static bool known[2][MAX_DEVICES] = {};
-    const auto kernel = nodes ? tree_back_tc_kernel<true> : tree_back_tc_kernel<false>;
-    e = allow_smem(kernel, SMEM_MAX, known[nodes]);
-    if (e != cudaSuccess) return e;
-    e = launch_k(kernel, dim3(a.plan.tc_ctas), dim3(THREADS), (size_t)lay.smem, st, mk, mv, args, lay, split_tab);
+    e = nodes ? run<true>(args, lay, mk, mv, split_tab, st) : run<false>(args, lay, mk, mv, split_tab, st);
     if (e != cudaSuccess) return e;
     return launch_k(tree_back_tc_sum_kernel, dim3(a.Hkv * a.n_rb, tree_back_tc_groups(a), ceil_div(a.rb_rows, SUM_ROWS)),
                     dim3(SUM_THREADS), 0, st, args, (const int2 *)split_tab, (int)!nodes);
