@@ -29,9 +29,13 @@ constexpr int TM = 256, TN = 256, BK = 64;       // a pair's tile; a CTA holds 1
 constexpr int HALF = 128 * BK * 2;               // a CTA's part of an operand's k-block, 16 KB
 constexpr int STAGE = 2 * HALF, STAGES = 6;
 constexpr int OFF_BAR = STAGES * STAGE, SMEM = OFF_BAR + 256 + 1024 /*align*/;
-constexpr int THREADS = 384;                     // warps 0-7 epilogue, 8 TMA, 9 MMA (rank 0), 10 TMEM
+constexpr int THREADS = 352;                     // warps 0-7 epilogue, 8 TMA, 9 MMA (rank 0), 10 TMEM
 constexpr int TMA = 8, MMA = 9, TMEM = 10, EPI_THREADS = 256;
 constexpr int TMEM_COLS = 2 * TN;
+// LOSS adds its logits up over 1024 of K at a time: the tensor core cuts what falls below an
+// accumulator's 24 bits, which over longer sums shows in the loss (of its norm, with the whole of K in
+// one accumulator: 2.0e-6 at d = 2560, 2.7e-6 at 4096, 4.5e-6 at 8192; so: 0.9e-6).
+constexpr int LOSS_KB = 1024 / BK;
 constexpr long long GRAD_BYTES = 512ll << 20;    // most bytes of a piece's g
 
 template <int KIND>
@@ -192,13 +196,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         for (int it = cl; ok && it < n_items; it += n_cl) {
             const Item x = item_of<KIND>(t, it, tn);
             if (KIND == DH && x.nkb <= 0) continue;
-            const int buf = n & 1;
-            const uint32_t acc = tmem + (uint32_t)(buf * TN);
-            // both CTAs' epilogues have read this accumulator's previous tile
-            if (n >= 2 && !mbar_wait_cluster(&acc_empty[buf], ((n >> 1) - 1) & 1, abort)) break;
-            tc_fence_after();
+            uint32_t acc = 0;
             for (int i = 0; i < x.nkb; ++i, ++gi) {
-                const int s = gi % STAGES;
+                const int s = gi % STAGES, buf = n & 1;
+                const bool first = KIND == LOSS ? i % LOSS_KB == 0 : i == 0;
+                const bool last = i == x.nkb - 1 || (KIND == LOSS && i % LOSS_KB == LOSS_KB - 1);
+                if (first) {
+                    acc = tmem + (uint32_t)(buf * TN);
+                    // both CTAs' epilogues have read what this accumulator held
+                    if (n >= 2 && !mbar_wait_cluster(&acc_empty[buf], ((n >> 1) - 1) & 1, abort)) {
+                        ok = false;
+                        break;
+                    }
+                }
                 if (!mbar_wait(&full[s], (gi / STAGES) & 1, abort)) {
                     ok = false;
                     break;
@@ -209,11 +219,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                 const uint64_t db = Ki::B_MN ? sw128_mnmajor_desc(sb, HALF / 2) : sw128_kmajor_desc(sb);
 #pragma unroll
                 for (int kk = 0; kk < BK / 16; ++kk)
-                    mma_bf16_pair(acc, da + step_a * kk, db + step_b * kk, idesc, (i > 0 || kk > 0) ? 1u : 0u);
+                    mma_bf16_pair(acc, da + step_a * kk, db + step_b * kk, idesc, !first || kk > 0 ? 1u : 0u);
                 mma_commit_pair(&empty[s]);
+                if (last) {
+                    mma_commit_pair(&acc_full[buf]);
+                    ++n;
+                }
             }
-            if (ok) mma_commit_pair(&acc_full[buf]);
-            ++n;
         }
         mma_commit_pair(fin);  // every MMA is finished before TMEM and shared memory go away
         mbar_wait_drain(fin, 0);
@@ -224,91 +236,115 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         const int count = *a.count;
         const Tiles t = tiles_of<KIND>(a, count, piece);
         const int n_items = t.items();
-        int n = -1;
-        for (int it = cl; it < n_items; it += n_cl) {
-            const Item x = item_of<KIND>(t, it, tn);
-            if (KIND == DH && x.nkb <= 0) continue;
-            ++n;
-            const int buf = n & 1, m = x.m0 + (int)rank * 128 + row;
-            VocabRow info{0.f, 0.f, -1, 0};
-            if ((KIND == LOSS || KIND == GRAD) && m < count) info = a.rows[m];
-            const bool have = __all_sync(0xffffffffu, mbar_wait(&acc_full[buf], (n >> 1) & 1, abort));
+        int n = 0;  // accumulators read
+        const auto wait_acc = [&]() {
+            const bool have = __all_sync(0xffffffffu, mbar_wait(&acc_full[n & 1], (n >> 1) & 1, abort));
             tc_fence_after();
-            if (!have) break;
-            const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * TN + half * (tn / 2));
-            const int c0 = x.n0 + half * (tn / 2);  // first column
-            float mx = -INFINITY, sum = 0.f;
-#pragma unroll 1
-            for (int c = 0; c < tn / 2; c += 32) {
-                float v[32];
-                __syncwarp();  // (rows that store nothing have skipped ahead)
-                tmem_ld32(at + c, v);  // (behind the half's last column: not looked at)
-                if constexpr (KIND == LOSS) {
-                    const int left = min(piece - (c0 + c), tn / 2 - c);
-                    float top = mx;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        if (j >= left) v[j] = -INFINITY;
-                        top = fmaxf(top, v[j]);
-                    }
-                    const int hit = info.target - (c0 + c);
-                    if (hit >= 0 && hit < min(32, left)) {  // (rare: once a row)
-                        float z = 0.f;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) z = j == hit ? v[j] : z;
-                        a.at[m] = z;
-                    }
-                    const float mu = top == -INFINITY ? 0.f : top;
-                    sum *= mx == -INFINITY ? 1.f : fast_exp2((mx - mu) * LOG2E);
-                    mx = top;
-                    float s4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) s4[j & 3] += fast_exp2((v[j] - mu) * LOG2E);
-                    sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
-                } else if constexpr (KIND == GRAD) {
-                    const int left = m < count ? piece - (c0 + c) : 0, hit = info.target - v0 - (c0 + c);
-                    uint32_t w[16];
-#pragma unroll
-                    for (int j = 0; j < 32; j += 2) {
-                        float g[2];
-#pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            const float p = fast_exp2((v[j + q] - info.lse) * LOG2E);
-                            g[q] = j + q < left ? (j + q == hit ? p - 1.f : p) * info.g : 0.f;
-                        }
-                        w[j / 2] = pack2_bf16(g[0], g[1]);
-                    }
-                    uint4 *to = (uint4 *)((bf16 *)a.grad + (size_t)m * a.piece + c0 + c);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) to[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-                } else if constexpr (KIND == DH) {
-                    if (m >= count) continue;
-                    float *to = a.acc + ((size_t)x.split * (t.m * TM) + m) * a.d + c0 + c;
-#pragma unroll
-                    for (int j = 0; j < 32; j += 4) {
-                        if (c0 + c + j >= a.d) break;
-                        float4 y = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-                        if (v0) {
-                            const float4 z = *(const float4 *)(to + j);
-                            y.x += z.x, y.y += z.y, y.z += z.z, y.w += z.w;
-                        }
-                        *(float4 *)(to + j) = y;
-                    }
-                } else {
-                    if (m >= piece) continue;
-                    bf16 *to = (bf16 *)a.dw + (size_t)(v0 + m) * a.ws + c0 + c;
-#pragma unroll
-                    for (int j = 0; j < 32; j += 8) {
-                        if (c0 + c + j >= a.d) break;
-                        *(uint4 *)(to + j) = make_uint4(pack2_bf16(v[j], v[j + 1]), pack2_bf16(v[j + 2], v[j + 3]),
-                                                        pack2_bf16(v[j + 4], v[j + 5]), pack2_bf16(v[j + 6], v[j + 7]));
-                    }
-                }
-            }
-            if (KIND == LOSS && m < count) a.part[(size_t)m * a.parts + 2 * x.nt + half] = make_float2(mx, sum);
+            return have;
+        };
+        const auto acc_at = [&]() { return tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)((n & 1) * TN + half * (tn / 2)); };
+        const auto release_acc = [&]() {
             tc_fence_before();
             asm volatile("bar.sync 1, %0;" ::"n"(EPI_THREADS) : "memory");
-            if (threadIdx.x == 0) mbar_arrive_remote(map_rank(&acc_empty[buf], 0));
+            if (threadIdx.x == 0) mbar_arrive_remote(map_rank(&acc_empty[n & 1], 0));
+            ++n;
+        };
+        bool ok = true;
+        for (int it = cl; ok && it < n_items; it += n_cl) {
+            const Item x = item_of<KIND>(t, it, tn);
+            if (KIND == DH && x.nkb <= 0) continue;
+            const int m = x.m0 + (int)rank * 128 + row, c0 = x.n0 + half * (tn / 2);  // row, first column
+            VocabRow info{0.f, 0.f, -1, 0};
+            if ((KIND == LOSS || KIND == GRAD) && m < count) info = a.rows[m];
+            if constexpr (KIND == LOSS) {
+                constexpr int CH = 16;  // columns read at a time; those behind the half's last one are not looked at
+                float v[TN / 2];
+#pragma unroll
+                for (int c = 0; c < TN / 2; ++c) v[c] = 0.f;
+#pragma unroll 1
+                for (int k = 0; k < x.nkb; k += LOSS_KB) {
+                    ok = wait_acc();
+                    if (!ok) break;
+                    const uint32_t at = acc_at();
+#pragma unroll
+                    for (int c = 0; c < TN / 2; c += CH) {
+                        if (c >= tn / 2) break;
+                        float u[CH];
+                        tmem_ld16(at + c, u);
+#pragma unroll
+                        for (int j = 0; j < CH; ++j) v[c + j] += u[j];
+                    }
+                    release_acc();
+                }
+                if (!ok) break;
+                const int left = min(piece - c0, tn / 2), hit = info.target - c0;
+                float mx = -INFINITY, z = 0.f;
+#pragma unroll
+                for (int c = 0; c < TN / 2; ++c) {
+                    if (c >= left) v[c] = -INFINITY;
+                    mx = fmaxf(mx, v[c]);
+                }
+                if (hit >= 0 && hit < left) {  // (once a row)
+#pragma unroll
+                    for (int c = 0; c < TN / 2; ++c) z = c == hit ? v[c] : z;
+                    a.at[m] = z;
+                }
+                const float mu = mx == -INFINITY ? 0.f : mx;
+                float s4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < TN / 2; ++c) s4[c & 3] += fast_exp2((v[c] - mu) * LOG2E);
+                if (m < count) a.part[(size_t)m * a.parts + 2 * x.nt + half] = make_float2(mx, (s4[0] + s4[1]) + (s4[2] + s4[3]));
+            } else {
+                ok = wait_acc();
+                if (!ok) break;
+                const uint32_t at = acc_at();
+#pragma unroll 1
+                for (int c = 0; c < TN / 2; c += 32) {
+                    float v[32];
+                    __syncwarp();  // (rows that store nothing have skipped ahead)
+                    tmem_ld32(at + c, v);
+                    if constexpr (KIND == GRAD) {
+                        const int left = m < count ? piece - (c0 + c) : 0, hit = info.target - v0 - (c0 + c);
+                        uint32_t w[16];
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2) {
+                            float g[2];
+#pragma unroll
+                            for (int q = 0; q < 2; ++q) {
+                                const float p = fast_exp2((v[j + q] - info.lse) * LOG2E);
+                                g[q] = j + q < left ? (j + q == hit ? p - 1.f : p) * info.g : 0.f;
+                            }
+                            w[j / 2] = pack2_bf16(g[0], g[1]);
+                        }
+                        uint4 *to = (uint4 *)((bf16 *)a.grad + (size_t)m * a.piece + c0 + c);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) to[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+                    } else if constexpr (KIND == DH) {
+                        if (m >= count) continue;
+                        float *to = a.acc + ((size_t)x.split * (t.m * TM) + m) * a.d + c0 + c;
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) {
+                            if (c0 + c + j >= a.d) break;
+                            float4 y = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                            if (v0) {
+                                const float4 z = *(const float4 *)(to + j);
+                                y.x += z.x, y.y += z.y, y.z += z.z, y.w += z.w;
+                            }
+                            *(float4 *)(to + j) = y;
+                        }
+                    } else {
+                        if (m >= piece) continue;
+                        bf16 *to = (bf16 *)a.dw + (size_t)(v0 + m) * a.ws + c0 + c;
+#pragma unroll
+                        for (int j = 0; j < 32; j += 8) {
+                            if (c0 + c + j >= a.d) break;
+                            *(uint4 *)(to + j) = make_uint4(pack2_bf16(v[j], v[j + 1]), pack2_bf16(v[j + 2], v[j + 3]),
+                                                            pack2_bf16(v[j + 4], v[j + 5]), pack2_bf16(v[j + 6], v[j + 7]));
+                        }
+                    }
+                }
+                release_acc();
+            }
         }
     }
     __syncwarp();
