@@ -79,6 +79,12 @@ def test_loss_and_gradient(torch, lens, rows, heads):
     assert float((got.cpu().double() - grad).norm()) <= scale * float(grad.norm())
     again = t.loss_and_gradient(prompt, targets)
     assert torch.equal(again[0], loss) and torch.equal(again[1], got)
+    st = torch.cuda.Stream()  # there a call's set-up runs beside the call before it
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        rows = [t.loss_and_gradient(prompt, targets) for _ in range(3)]
+    st.synchronize()
+    assert all(torch.equal(a, loss) and torch.equal(b, got) for a, b in rows)
 
 
 def test_the_example_runs(torch):
