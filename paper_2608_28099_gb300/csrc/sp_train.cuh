@@ -54,6 +54,8 @@ struct VocabArgs {
     int tensor;                    // which kernels
     int pad;                       // n rounded up to whole tiles
     int tn;                        // forward, tensor cores: vocabulary rows of a tile
+    int direct;                    // forward, tensor cores, one tile of tokens: they are not counted off, row m
+                                   // of the products is token m
     float2 *part;                  // forward: [n][parts] (max, sum of exponentials) of a piece of the vocabulary
     float *at;                     // forward: [n] the target's logit
     int parts;
@@ -64,6 +66,7 @@ struct VocabArgs {
     int pairs;                     // pairs of CTAs (tensor cores), or SMs, that split_count balances over
     int *status;
 };
+__host__ __device__ inline bool has_target(int t, int V) { return t >= 0 && t < V; }
 // Splits along the vocabulary of dh's tiles (tm rows a tile) over `units` of the machine, the same on the
 // host (for all counts) and on the device (for the one it is): the fewest rounds of k-blocks, a split's
 // partial costing some itself (two passes over it: `plane` k-blocks a tile).

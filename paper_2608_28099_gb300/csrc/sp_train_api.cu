@@ -182,7 +182,7 @@ sp_status sp_vocab_loss(sp_stream stream, const sp_vocab_dims *dims, const void 
     a.lse = d_lse;
     a.status = d_status;
     const cudaStream_t st = (cudaStream_t)stream;
-    cudaError_t e = launch_vocab_keep(a, false, st);
+    cudaError_t e = a.direct ? cudaSuccess : launch_vocab_keep(a, false, st);
     if (e == cudaSuccess) e = a.tensor ? launch_vocab_loss_tc(a, st) : launch_vocab_loss_simt(a, st);
     if (e == cudaSuccess) e = launch_vocab_finish_loss(a, st);
     return launched(e, "sp_vocab_loss");

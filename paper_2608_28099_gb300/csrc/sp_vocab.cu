@@ -15,8 +15,6 @@ namespace {
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int THREADS = 256, WARPS = THREADS / 32;
 
-__device__ __forceinline__ bool has_target(int t, int V) { return t >= 0 && t < V; }
-
 // Rows of the products: a token with a target gets the next row.  Every block counts the targets in
 // front of its own `per` tokens and in all (n ints from L2), then copies its rows where they go,
 // a warp a row, and clears what is known to be 0: losses and gradients of the others, and
@@ -113,7 +111,17 @@ __global__ void __launch_bounds__(THREADS) vocab_finish_loss_kernel(const __grid
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, p = blockIdx.x * WARPS + (threadIdx.x >> 5);
-    if (p >= *a.count) return;
+    int token = p;
+    if (a.direct) {
+        if (p >= a.n) return;
+        if (!has_target(a.targets[p], a.V)) {
+            if (lane == 0) a.loss[p] = a.lse[p] = 0.f;
+            return;
+        }
+    } else {
+        if (p >= *a.count) return;
+        token = a.rows[p].token;
+    }
     const float2 *part = a.part + (size_t)p * a.parts;
     float m = -INFINITY, l = 0.f;
     constexpr int AT_ONCE = 8;
@@ -137,10 +145,9 @@ __global__ void __launch_bounds__(THREADS) vocab_finish_loss_kernel(const __grid
 #pragma unroll
     for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
     if (lane == 0) {
-        const int t = a.rows[p].token;
         const float lg = logf(l);
-        a.lse[t] = top + lg;
-        a.loss[t] = (top - a.at[p]) + lg;  // (the maximum and the target's logit may be large and close)
+        a.lse[token] = top + lg;
+        a.loss[token] = (top - a.at[p]) + lg;  // (the maximum and the target's logit may be large and close)
     }
 }
 

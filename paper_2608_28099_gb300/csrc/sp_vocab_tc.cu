@@ -49,6 +49,10 @@ struct Tiles {
     __device__ __forceinline__ int items() const { return m * n * splits; }
 };
 template <int KIND>
+__device__ __forceinline__ int count_of(const VocabArgs &a) {
+    return KIND == LOSS && a.direct ? a.n : *a.count;
+}
+template <int KIND>
 __device__ __forceinline__ int cols_of(const VocabArgs &a) {
     return KIND == LOSS ? a.tn : TN;
 }
@@ -138,11 +142,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         // what is read again soon stays in L2, the vocabulary's rows of LOSS pass through
         const uint64_t pol_a = KIND == LOSS || KIND == GRAD ? policy_evict_last() : policy_evict_normal();
         const uint64_t pol_b = KIND == LOSS ? policy_evict_first() : KIND == DW ? policy_evict_last() : policy_evict_normal();
-        // Up to 256 tokens the logits' first tile is known before the tokens are counted, and W does
-        // not depend on them: its k-blocks are asked for while the kernel in front still runs
-        // (which has waited for the caller's earlier work before it let this one start).
+        // Up to 256 tokens the first tile of GRAD is known before they are counted, and W does not depend
+        // on them: its k-blocks are asked for while the kernel in front still runs (which has
+        // waited for the caller's earlier work before it let this one start).
         int pre = 0;
-        if ((KIND == LOSS || KIND == GRAD) && a.pad == TM && cl < ceil_div(piece, tn)) {
+        if (KIND == GRAD && a.pad == TM && cl < ceil_div(piece, tn)) {
             pre = min(STAGES, ceil_div(a.d, BK));
             for (int i = 0; i < pre; ++i) {
                 if (rank == 0) mbar_arrive_expect_tx(&full[i], stage_tx);
@@ -150,7 +154,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
             }
         }
         pdl_wait();
-        const Tiles t = tiles_of<KIND>(a, *a.count, piece);
+        const Tiles t = tiles_of<KIND>(a, count_of<KIND>(a), piece);
         const int n_items = t.items();
         int gi = 0;
         bool ok = true;
@@ -189,7 +193,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         // a step of 16 along K: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major tile
         constexpr uint64_t step_a = Ki::A_MN ? 2048 >> 4 : 32 >> 4, step_b = Ki::B_MN ? 2048 >> 4 : 32 >> 4;
         pdl_wait();
-        const Tiles t = tiles_of<KIND>(a, *a.count, piece);
+        const Tiles t = tiles_of<KIND>(a, count_of<KIND>(a), piece);
         const int n_items = t.items();
         int gi = 0, n = 0;
         bool ok = true;
@@ -233,7 +237,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         // a row a thread: warp w reads TMEM lanes 32 (w & 3).. and columns 128 (w >> 2)..
         const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane;
         pdl_wait();
-        const int count = *a.count;
+        const int count = count_of<KIND>(a);
         const Tiles t = tiles_of<KIND>(a, count, piece);
         const int n_items = t.items();
         int n = 0;  // accumulators read
@@ -255,7 +259,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
             if (KIND == DH && x.nkb <= 0) continue;
             const int m = x.m0 + (int)rank * 128 + row, c0 = x.n0 + half * (tn / 2);  // row, first column
             VocabRow info{0.f, 0.f, -1, 0};
-            if ((KIND == LOSS || KIND == GRAD) && m < count) info = a.rows[m];
+            if (KIND == LOSS && a.direct) {
+                const int target = m < count ? a.targets[m] : -1;
+                if (has_target(target, a.V)) info.target = target;
+                else if (target >= a.V && it == 0 && a.status) atomicOr(a.status, SP_DEV_BAD_ROW);
+            } else if ((KIND == LOSS || KIND == GRAD) && m < count) {
+                info = a.rows[m];
+            }
             if constexpr (KIND == LOSS) {
                 constexpr int CH = 16;  // columns read at a time; those behind the half's last one are not looked at
                 float v[TN / 2];
@@ -383,7 +393,8 @@ void plan_vocab_tc(VocabArgs *a, bool backward, int n_sm) {
     a->pad = ceil_div(a->n, TM) * TM;
     a->pairs = n_sm / 2 > 0 ? n_sm / 2 : 1;
     a->tn = TN;
-    if (!backward && a->n <= TM) {
+    a->direct = !backward && a->n <= TM;
+    if (a->direct) {
         // W is read once and bounds the call: tiles of the width whose rounds over the pairs read the fewest rows
         // (32000 rows: 2 x 224 instead of 2 x 256 a pair)
         long long least = 1ll << 62;
@@ -408,7 +419,8 @@ void plan_vocab_tc(VocabArgs *a, bool backward, int n_sm) {
 // nothing fetches.  48 tokens against 32000 rows of 2560: 38 us with all 256 rows of the tile.)
 cudaError_t launch_vocab_loss_tc(const VocabArgs &a, cudaStream_t st) {
     CUtensorMap mh, mw;
-    if (!encode_tile_bf16(&mh, a.hc, a.d, a.n, a.d, 128) || !encode_tile_bf16(&mw, a.w, a.d, a.V, a.ws, a.tn / 2))
+    if (!(a.direct ? encode_tile_bf16(&mh, a.h, a.d, a.n, a.hs, 128) : encode_tile_bf16(&mh, a.hc, a.d, a.n, a.d, 128)) ||
+        !encode_tile_bf16(&mw, a.w, a.d, a.V, a.ws, a.tn / 2))
         return cudaErrorInvalidValue;
     return run<LOSS>(a, mh, mw, 0, st);
 }
