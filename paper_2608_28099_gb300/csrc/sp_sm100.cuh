@@ -114,8 +114,9 @@ __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
 // mbar_wait for a barrier that threads of the other CTA arrive on.
 __device__ __forceinline__ bool mbar_wait_cluster(uint64_t *bar, uint32_t parity, volatile int *abort,
                                                   uint64_t limit_ns = kWaitLimitNs) {
-    const uint64_t t0 = global_ns();
-    for (uint32_t it = 1;; ++it) {
+    uint64_t t0 = 0;
+    for (uint32_t it = 0;; ++it) {
+        if (it == 1) t0 = global_ns();  // (not asked for where nothing is waited for)
         uint32_t ok;
         asm volatile(
             "{\n\t.reg .pred p;\n\t"
@@ -125,7 +126,7 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint64_t *bar, uint32_t parity
             : "r"(smem_u32(bar)), "r"(parity)
             : "memory");
         if (ok) return true;
-        if ((it & 63) == 0) {
+        if (it && (it & 63) == 0) {
             if (*abort) return false;
             if (global_ns() - t0 > limit_ns) {
                 *abort = 1;

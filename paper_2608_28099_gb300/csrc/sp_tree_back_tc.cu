@@ -736,13 +736,11 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");  // nothing lands after the CTA is gone
-        if (lane == 0) {
-            // drain copies still in flight (only possible after an abort)
-            Ring rd(rg.n);
-#pragma unroll 1
-            for (int j = 0; j < filled; ++j, rd.next())
-                if (j + rg.n >= filled) mbar_wait_drain(&full[rd.slot], rd.ph);
-        }
+        if (lane == 0)  // bulk copies still in flight (only possible after an abort): the last use of every slot
+            for (int j = 0; j < min(filled, rg.n); ++j) {
+                const int back = j + 1, slot = (rg.slot - back + rg.n) % rg.n;
+                mbar_wait_drain(&full[slot], rg.slot >= back ? rg.ph : rg.ph ^ 1);
+            }
         bad = __any_sync(0xffffffffu, bad);
         if (bad && lane == 0 && a.status) atomicOr(a.status, SP_DEV_BAD_PAGE);
     } else if (warp == MMA) {

@@ -36,6 +36,19 @@ constexpr int TMEM_COLS = 2 * TN;
 // accumulator's 24 bits, which over longer sums shows in the loss (of its norm, with the whole of K in
 // one accumulator: 2.0e-6 at d = 2560, 2.7e-6 at 4096, 4.5e-6 at 8192; so: 0.9e-6).
 constexpr int LOSS_KB = 1024 / BK;
+template <int KIND>
+constexpr int ACC_KB = KIND == 0 ? LOSS_KB : 1 << 30;  // k-blocks of an accumulator
+
+struct Ring {
+    int slot = 0;
+    uint32_t ph = 0;
+    __device__ __forceinline__ void next() {
+        if (++slot == STAGES) {
+            slot = 0;
+            ph ^= 1;
+        }
+    }
+};
 constexpr long long GRAD_BYTES = 512ll << 20;    // most bytes of a piece's g
 
 template <int KIND>
@@ -156,18 +169,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         pdl_wait();
         const Tiles t = tiles_of<KIND>(a, count_of<KIND>(a), piece);
         const int n_items = t.items();
-        int gi = 0;
+        Ring rg;
+        int filled = 0;
         bool ok = true;
         for (int it = cl; ok && it < n_items; it += n_cl) {
             const Item x = item_of<KIND>(t, it, tn);
             const int ma = x.m0 + (int)rank * 128, nb = x.n0 + (int)rank * (tn / 2);
-            for (int i = 0; i < x.nkb; ++i, ++gi) {
-                const int s = gi % STAGES, k = (x.kb0 + i) * BK;
-                if (gi >= STAGES && !mbar_wait(&empty[s], ((gi / STAGES) & 1) ^ 1, abort)) {
+            for (int i = 0; i < x.nkb; ++i, rg.next(), ++filled) {
+                const int s = rg.slot, k = (x.kb0 + i) * BK;
+                if (!mbar_wait(&empty[s], rg.ph ^ 1, abort)) {
                     ok = false;
                     break;
                 }
-                if (rank == 0 && gi >= pre) mbar_arrive_expect_tx(&full[s], stage_tx);
+                if (rank == 0 && filled >= pre) mbar_arrive_expect_tx(&full[s], stage_tx);
                 const uint32_t bar = map_rank(&full[s], 0);
                 uint8_t *sa = smem + s * STAGE, *sb = sa + HALF;
                 if (Ki::A_MN) {
@@ -180,58 +194,57 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                     const int kv = KIND == DH ? v0 + k : k;
                     tma_load_2d_pair(sb, &map_b, bar, nb, kv, pol_b);
                     tma_load_2d_pair(sb + HALF / 2, &map_b, bar, nb + 64, kv, pol_b);
-                } else if (gi >= pre) {
+                } else if (filled >= pre) {
                     tma_load_2d_pair(sb, &map_b, bar, k, v0 + nb, pol_b);
                 }
             }
         }
-        // nothing may land in this CTA after it is gone
-        for (int j = gi > STAGES ? gi - STAGES : 0; j < gi; ++j)
-            if (!mbar_wait_drain(&empty[j % STAGES], (j / STAGES) & 1)) break;
-    } else if (warp == MMA && lane == 0 && rank == 0) {
+        // nothing may land in this CTA after it is gone: the last use of every stage has been read
+        for (int j = 0; j < STAGES; ++j, rg.next())
+            if (!mbar_wait_drain(&empty[rg.slot], rg.ph ^ 1)) break;
+    } else if (warp == MMA && rank == 0) {
+        // by the whole warp, the instructions under `on` (see elect_one)
+        const bool on = elect_one();
         const uint32_t idesc = idesc_bf16_f32(TM, tn) | (Ki::A_MN ? 1u << 15 : 0u) | (Ki::B_MN ? 1u << 16 : 0u);
         // a step of 16 along K: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major tile
         constexpr uint64_t step_a = Ki::A_MN ? 2048 >> 4 : 32 >> 4, step_b = Ki::B_MN ? 2048 >> 4 : 32 >> 4;
+        const uint64_t da0 = Ki::A_MN ? sw128_mnmajor_desc(smem, HALF / 2) : sw128_kmajor_desc(smem);
+        const uint64_t db0 = Ki::B_MN ? sw128_mnmajor_desc(smem + HALF, HALF / 2) : sw128_kmajor_desc(smem + HALF);
         pdl_wait();
         const Tiles t = tiles_of<KIND>(a, count_of<KIND>(a), piece);
         const int n_items = t.items();
-        int gi = 0, n = 0;
+        Ring rg;
+        int n = 0;  // accumulators
         bool ok = true;
+#pragma unroll 1
         for (int it = cl; ok && it < n_items; it += n_cl) {
             const Item x = item_of<KIND>(t, it, tn);
-            if (KIND == DH && x.nkb <= 0) continue;
-            uint32_t acc = 0;
-            for (int i = 0; i < x.nkb; ++i, ++gi) {
-                const int s = gi % STAGES, buf = n & 1;
-                const bool first = KIND == LOSS ? i % LOSS_KB == 0 : i == 0;
-                const bool last = i == x.nkb - 1 || (KIND == LOSS && i % LOSS_KB == LOSS_KB - 1);
-                if (first) {
-                    acc = tmem + (uint32_t)(buf * TN);
-                    // both CTAs' epilogues have read what this accumulator held
-                    if (n >= 2 && !mbar_wait_cluster(&acc_empty[buf], ((n >> 1) - 1) & 1, abort)) {
-                        ok = false;
-                        break;
-                    }
-                }
-                if (!mbar_wait(&full[s], (gi / STAGES) & 1, abort)) {
-                    ok = false;
-                    break;
-                }
-                tc_fence_after();
-                const uint8_t *sa = smem + s * STAGE, *sb = sa + HALF;
-                const uint64_t da = Ki::A_MN ? sw128_mnmajor_desc(sa, HALF / 2) : sw128_kmajor_desc(sa);
-                const uint64_t db = Ki::B_MN ? sw128_mnmajor_desc(sb, HALF / 2) : sw128_kmajor_desc(sb);
+#pragma unroll 1
+            for (int i0 = 0; ok && i0 < x.nkb; i0 += ACC_KB<KIND>) {
+                const int buf = n & 1, end = min(ACC_KB<KIND>, x.nkb - i0);
+                const uint32_t acc = tmem + (uint32_t)(buf * TN);
+                // both CTAs' epilogues have read what this accumulator held
+                if (n >= 2) ok = __all_sync(0xffffffffu, mbar_wait_cluster(&acc_empty[buf], ((n >> 1) - 1) & 1, abort));
+                ++n;
+#pragma unroll 1
+                for (int i = 0; i < end; ++i, rg.next()) {
+                    ok = ok && mbar_wait_warp(&full[rg.slot], rg.ph, abort);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t da = da0 + (uint32_t)(rg.slot * (STAGE >> 4)), db = db0 + (uint32_t)(rg.slot * (STAGE >> 4));
+                    if (on) {
 #pragma unroll
-                for (int kk = 0; kk < BK / 16; ++kk)
-                    mma_bf16_pair(acc, da + step_a * kk, db + step_b * kk, idesc, !first || kk > 0 ? 1u : 0u);
-                mma_commit_pair(&empty[s]);
-                if (last) {
-                    mma_commit_pair(&acc_full[buf]);
-                    ++n;
+                        for (int kk = 0; kk < BK / 16; ++kk)
+                            mma_bf16_pair(acc, da + step_a * kk, db + step_b * kk, idesc, i > 0 || kk > 0 ? 1u : 0u);
+                        mma_commit_pair(&empty[rg.slot]);
+                        if (i == end - 1) mma_commit_pair(&acc_full[buf]);
+                    }
+                    __syncwarp();
                 }
             }
         }
-        mma_commit_pair(fin);  // every MMA is finished before TMEM and shared memory go away
+        if (on) mma_commit_pair(fin);  // every MMA is finished before TMEM and shared memory go away
+        __syncwarp();
         mbar_wait_drain(fin, 0);
     } else if (warp < 8) {
         // a row a thread: warp w reads TMEM lanes 32 (w & 3).. and columns 128 (w >> 2)..
