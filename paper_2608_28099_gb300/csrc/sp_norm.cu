@@ -3,9 +3,12 @@
 // layer, Sec. 3.1):
 //   s = x + r,  y = s rstd g,  rstd = (mean s^2 + eps)^-1/2
 //   dx = rstd (g dy - xh m) + ds,  m = mean(g dy xh),  dg = sum over rows of dy xh,  xh = s rstd
-// Both are bound by HBM: each row is read once into registers (8 elements a chunk, up to
-// four chunks a thread) and one reduction over a row's threads stands between the loads and
-// the stores.
+// Both are bound by HBM: each row is read once into registers (8 elements a chunk, up to four chunks a
+// thread) and one reduction over a row's threads stands between the loads and the stores, so blocks walk
+// rows and have the next one's loads under way meanwhile (without: 143 instead of 99 us, 94 instead
+// of 49).  16384 rows of 5120, bf16 with a residual into 8 bits: 99 us, 5.9 TB/s; backward of 8191 rows of
+// 4096 with the gain's gradient 49 us, 5.5 TB/s, 5 of them its second kernel; of 1500 fp32 rows of 2560
+// without it 12.9 us, 4.8 TB/s, two and a half rows a block.  16 rows of 4096: 4.3 us, one launch.
 #include "sp_train.cuh"
 
 namespace sp {
@@ -404,7 +407,8 @@ Shape shape_of(int d) {
 }
 bool whole16(const void *p, long long stride, int es) { return !(((uintptr_t)p | (uintptr_t)(stride * es)) & 15); }
 
-// Blocks that walk `n` rows, `per_sm` threads an SM.
+// Blocks that walk `n` rows, `per_sm` threads an SM: forward 99 us with 1024, 106 with 1536, 129 with 700
+// (16384 x 5120); backward 49 with 640, 53 with 1024, 61 with 800.
 int blocks_of(const Shape &s, long long n, int n_sm, int per_sm) {
     const long long all = ceil_div_ll(n, s.rows), held = (long long)n_sm * (per_sm / s.threads > 1 ? per_sm / s.threads : 1);
     return (int)(all < held ? all : held);

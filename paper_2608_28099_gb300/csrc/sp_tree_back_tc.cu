@@ -15,6 +15,17 @@
 // then into TMEM) and write dQ out; 12 MMA issuer and TMEM; 13 K, 14 V (TMA boxes of whole pages, cp.async
 // elsewhere).  TMEM: S, dP, dQ, Q, dO in all 512 columns.  Every wait is time-limited
 // (SP_DEV_TIMEOUT).
+//
+// What bounds it: HBM for long sequences.  Eight of 32768 tokens, 40 heads (80 rows a kv head): 182 us,
+// 5.9 TB/s; 64 of 1024 to 8192, 32 heads, 16 rows each: 214 to 229 us, 5.5 to 5.8 TB/s.  A tile's chain is
+// dP (8 MMAs) -> ds -> dQ (8 MMAs), the next tile's S beside ds; an MMA with A in TMEM takes
+// as long for 64 tokens as for 128, which is why tiles have 128 tokens (64: 217 instead of 201 us for the eight,
+// with two tiles under way), and Q and dO lie in TMEM (in shared memory 262 instead of 227, at 64 tokens).
+// Short sequences are segment ends, 8 to 9 us of latencies one after another in warps 8-11 (200 sequences
+// of 50 to 600 tokens: 111 us, 39 by bytes; 128 of 20 to 100: 50).  One sequence of 2048 tokens, 8 rows: 14.6 us,
+// of which 5 are the second kernel and its launch.
+// ds as a sum of two bf16 would halve its part of dQ's error (0.0031 -> 0.0025 of its norm) for 250 instead
+// of 189 us.
 #include <string.h>
 
 #include "sp_attn_plan.cuh"
@@ -37,7 +48,9 @@ constexpr int SMEM_MAX = 227 * 1024;
 constexpr int THREADS = 512;
 constexpr int EPI = 8, MMA = 12, K_WARP = 13, V_WARP = 14;
 constexpr uint32_t DP_COL = 128, DQ_COL = 256, Q_COL = 384, DO_COL = 448;  // TMEM: S, dP, dQ, Q, dO
-// Fewest tiles a share holds on average, and the cost of a segment in tiles.
+// Fewest tiles a share holds on average (one sequence of 2048 tokens: 15.3, 14.7, 15.9 us with 1, 2, 3), and
+// the cost of a segment in tiles (64 sequences of 1024 to 8192 tokens, 16 of 256 to 2048, 32 of 500 to 9000
+// with 32 nodes: 234, 39, 182 us with 2; 226, 43, 188 with 8; 229, 44, 199 with 16).
 constexpr int kBackMinTiles = 2;
 constexpr int kBackSegCost = 5;
 
