@@ -87,12 +87,15 @@ size_t lay_out(VocabArgs *a, bool backward, char *base) {
 }
 
 sp_status check_vocab_buffers(VocabArgs *a, bool backward, const void *d_h, const void *d_w, const int *d_targets,
-                              const void *d_dh, const void *d_dw, void *d_workspace, size_t workspace_bytes) {
+                              const void *d_dh, const void *d_dw, const float *d_lse, const float *d_loss, void *d_workspace,
+                              size_t workspace_bytes) {
     if (!d_h || !d_w || !d_targets || !d_workspace) return fail(SP_ERR_INVALID_ARG, "a required pointer is NULL");
     const size_t to = a->tensor ? 16 : elem_bytes(a->dtype);
     if (!aligned(d_h, to) || !aligned(d_w, to) || !aligned(d_dh, to) || !aligned(d_dw, to))
         return fail(SP_ERR_INVALID_ARG, a->tensor ? "h, w and their gradients must be 16-byte aligned (path 1: to their type)"
                                               : "h, w and their gradients must be aligned to their type");
+    if (!aligned(d_targets, 4) || !aligned(d_lse, 4) || !aligned(d_loss, 4))
+        return fail(SP_ERR_INVALID_ARG, "targets, losses and log sums must be aligned to their type");
     if (!aligned(d_workspace, 256)) return fail(SP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     const size_t need = lay_out(a, backward, (char *)d_workspace);
     if (workspace_bytes < need) return fail(SP_ERR_INVALID_ARG, "workspace too small (%zu < %zu)", workspace_bytes, need);
@@ -176,7 +179,7 @@ sp_status sp_vocab_loss(sp_stream stream, const sp_vocab_dims *dims, const void 
     sp_status s = check_vocab(dims, false, &a);
     if (s != SP_OK || a.n == 0) return s;
     if (!d_loss || !d_lse) return fail(SP_ERR_INVALID_ARG, "a required pointer is NULL");
-    s = check_vocab_buffers(&a, false, d_h, d_w, d_targets, nullptr, nullptr, d_workspace, workspace_bytes);
+    s = check_vocab_buffers(&a, false, d_h, d_w, d_targets, nullptr, nullptr, d_lse, d_loss, d_workspace, workspace_bytes);
     if (s != SP_OK) return s;
     a.loss = d_loss;
     a.lse = d_lse;
@@ -207,7 +210,7 @@ sp_status sp_vocab_loss_backward(sp_stream stream, const sp_vocab_dims *dims, co
         return launched(cudaMemset2DAsync(d_grad_w, (size_t)a.ws * es, 0, (size_t)a.d * es, (size_t)a.V, st), "sp_vocab_loss_backward");
     }
     if (!d_lse || !d_grad_h) return fail(SP_ERR_INVALID_ARG, "a required pointer is NULL");
-    s = check_vocab_buffers(&a, true, d_h, d_w, d_targets, d_grad_h, d_grad_w, d_workspace, workspace_bytes);
+    s = check_vocab_buffers(&a, true, d_h, d_w, d_targets, d_grad_h, d_grad_w, d_lse, d_grad_loss, d_workspace, workspace_bytes);
     if (s != SP_OK) return s;
     a.lse_in = d_lse;
     a.dloss = d_grad_loss;

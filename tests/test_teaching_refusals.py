@@ -100,7 +100,9 @@ def test_vocab_loss():
     calls += [call(vocab_dims(), *[None if i == j else p for j, p in enumerate((h, w, t, loss, lse, ws))], BIG) for i in range(6)]
     calls += [call(vocab_dims(), h + 8, w, t, loss, lse, ws, BIG), call(vocab_dims(), h, w + 2, t, loss, lse, ws, BIG),
               call(vocab_dims(dtype=sp.SP_F32), h + 2, w, t, loss, lse, ws, BIG), call(vocab_dims(), h, w, t, loss, lse, ws + 128, BIG),
-              call(vocab_dims(), h, w, t, loss, lse, ws, 256)]
+              call(vocab_dims(), h, w, t, loss, lse, ws, 256),
+              call(vocab_dims(), h, w, t + 2, loss, lse, ws, BIG), call(vocab_dims(), h, w, t, loss + 1, lse, ws, BIG),
+              call(vocab_dims(), h, w, t, loss, lse + 2, ws, BIG)]
     assert answers(calls) == [BAD] * len(calls)
     refused = [vocab_dims(n=4000001), vocab_dims(V=(1 << 24) + 1), vocab_dims(d=(1 << 20) + 8), vocab_dims(path=2, d=60),
                vocab_dims(path=2, h=68), vocab_dims(path=2, w=68), vocab_dims(path=2, dtype=sp.SP_F32)]
@@ -115,6 +117,7 @@ def test_vocab_loss_backward():
     args = (h, w, t, lse, gl, dh, dw, ws)
     calls = [call(vocab_dims(), *[None if i == j else p for j, p in enumerate(args)], BIG) for i in (0, 1, 2, 3, 5, 7)]
     calls += [call(vocab_dims(), *[p + 4 if i == j else p for j, p in enumerate(args)], BIG) for i in (0, 1, 5, 6, 7)]
+    calls += [call(vocab_dims(), *[p + 2 if i == j else p for j, p in enumerate(args)], BIG) for i in (2, 3, 4)]
     calls += [call(vocab_dims(), *args, 256), call(vocab_dims(d=0), *args, BIG)]
     assert answers(calls) == [BAD] * len(calls)
 
