@@ -56,8 +56,8 @@ sp_status check_vocab(const sp_vocab_dims *d, bool backward, VocabArgs *a) {
     else plan_vocab_simt(a, backward, sm_count());
     a->tensor = tensor;
     if (backward) {
-        // most rows of partial dh for any number of kept tokens (see split_count)
-        const long long tm = tensor ? 256 : 64, m_tiles = ceil_div_ll(a->n, tm);
+        // most rows of partial dh for any number of kept tokens (see plan_dh)
+        const long long tm = a->tm, m_tiles = ceil_div_ll(a->n, tm);
         const long long more = ceil_div_ll(8ll * a->pairs, ceil_div_ll(a->d, tm));
         a->acc_rows = (m_tiles + (more < 15 * m_tiles ? more : 15 * m_tiles)) * tm;
     }
@@ -73,7 +73,7 @@ size_t lay_out(VocabArgs *a, bool backward, char *base) {
         at += align256(bytes);
         return p;
     };
-    a->count = (int *)take(sizeof(int));
+    a->count = (DhPlan *)take(sizeof(DhPlan));
     a->rows = (VocabRow *)take((size_t)a->n * sizeof(VocabRow));
     a->hc = take((size_t)a->pad * a->d * es);
     if (!backward) {

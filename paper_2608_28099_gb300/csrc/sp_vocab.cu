@@ -15,6 +15,31 @@ namespace {
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int THREADS = 256, WARPS = THREADS / 32;
 
+// The splits along the vocabulary of dh's tiles (tm rows a tile) for `kept` tokens: the fewest rounds of
+// k-blocks over the machine's `pairs` units, a split's partial costing some itself (two passes over it: `plane`
+// k-blocks a tile; a k-block of 256 x 256 x 64 takes a pair 0.27 us, in which two passes over 0.3 tiles of fp32
+// partials fit the HBM's share of a pair; a block of CUDA cores some 0.7 us, which a partial does not weigh
+// against).  By a warp, a number of splits a lane.
+constexpr int MAX_SPLITS = 16;
+__device__ __forceinline__ DhPlan plan_dh(const VocabArgs &a, int kept, int lane) {
+    const int tm = a.tm, bk = a.tensor ? 64 : 2048 / tm, kb = ceil_div(min(a.piece, a.V), bk);
+    const int m_tiles = ceil_div(max(kept, 1), tm), n_tiles = ceil_div(a.d, tm), s = lane + 1, per = ceil_div(kb, s);
+    const float plane = a.tensor ? 24.f : 2.f;
+    float cost = 3e38f;
+    if ((long long)m_tiles * n_tiles < 8ll * a.pairs) {
+        const int tiles = m_tiles * n_tiles;
+        if (s <= MAX_SPLITS && tiles * lane < 8 * a.pairs && lane * per < kb)
+            cost = (float)ceil_div(tiles * s, a.pairs) * (float)(per + 4) + plane * (float)lane * (float)tiles / (float)a.pairs;
+    } else if (lane == 0) {
+        cost = 0.f;
+    }
+    float least = cost;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
+    const int best = __ffs(__ballot_sync(0xffffffffu, cost == least));  // (the fewest splits of equal cost)
+    return DhPlan{kept, m_tiles, best, __shfl_sync(0xffffffffu, per, best - 1)};
+}
+
 // Rows of the products: a token with a target gets the next row.  Every block counts the targets in
 // front of its own `per` tokens and in all (n ints from L2), then copies its rows where they go,
 // a warp a row, and clears what is known to be 0: losses and gradients of the others, and
@@ -44,7 +69,10 @@ __global__ void __launch_bounds__(THREADS) vocab_keep_kernel(const __grid_consta
     for (int w = 0; w < WARPS; ++w) f += front[w], all += total[w];
     if (blockIdx.x == 0) {
         if (bad && a.status) atomicOr(a.status, SP_DEV_BAD_ROW);
-        if (threadIdx.x == 0) *a.count = all;
+        if (warp == 0) {
+            const DhPlan plan = backward ? plan_dh(a, all, lane) : DhPlan{all, 0, 0, 0};
+            if (lane == 0) *a.count = plan;
+        }
     }
     for (int g0 = t0; g0 < t1; g0 += THREADS) {  // 256 of its tokens at a time (most blocks have few)
         const int t = g0 + threadIdx.x, v = t < t1 ? a.targets[t] : -1;
@@ -119,7 +147,7 @@ __global__ void __launch_bounds__(THREADS) vocab_finish_loss_kernel(const __grid
             return;
         }
     } else {
-        if (p >= *a.count) return;
+        if (p >= a.count->kept) return;
         token = a.rows[p].token;
     }
     const float2 *part = a.part + (size_t)p * a.parts;
@@ -157,20 +185,20 @@ __global__ void __launch_bounds__(THREADS) vocab_finish_dh_kernel(const __grid_c
     pdl_wait();
     pdl_trigger();
     const int p = blockIdx.x;
-    if (p >= *a.count) return;
+    const DhPlan plan = *a.count;
+    if (p >= plan.kept) return;
     T *to = (T *)a.dh + (size_t)a.rows[p].token * a.hs;
     const float *from = a.acc + (size_t)p * a.d;
-    const DhPlan plan = dh_plan(a, *a.count);
-    const size_t plane = (size_t)plan.rows * a.d;
+    const size_t plane = (size_t)plan.m_tiles * a.tm * a.d;
     if (a.tensor) {  // (d a multiple of 8, rows aligned)
         for (int e = threadIdx.x * 4; e < a.d; e += THREADS * 4) {
             float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
             constexpr int AT_ONCE = 8;  // planes under way together
-            for (int q0 = 0; q0 < plan.k.s; q0 += AT_ONCE) {
+            for (int q0 = 0; q0 < plan.splits; q0 += AT_ONCE) {
                 float4 v[AT_ONCE];
 #pragma unroll
                 for (int q = 0; q < AT_ONCE; ++q)
-                    v[q] = q0 + q < plan.k.s ? __ldcs((const float4 *)(from + (q0 + q) * plane + e)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    v[q] = q0 + q < plan.splits ? __ldcs((const float4 *)(from + (q0 + q) * plane + e)) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int q = 0; q < AT_ONCE; ++q) s.x += v[q].x, s.y += v[q].y, s.z += v[q].z, s.w += v[q].w;
             }
@@ -180,43 +208,52 @@ __global__ void __launch_bounds__(THREADS) vocab_finish_dh_kernel(const __grid_c
         for (int e = threadIdx.x; e < a.d; e += THREADS) {
             float s = 0.f;
 #pragma unroll 8
-            for (int q = 0; q < plan.k.s; ++q) s += from[q * plane + e];
+            for (int q = 0; q < plan.splits; ++q) s += from[q * plane + e];
             to[e] = from_f<T>(s);
         }
     }
 }
 
 // ---------------------------------------------------------------------------
-// Products on CUDA cores: C[m][n] = sum_k A(m, k) B(n, k) in 64 x 64 tiles, 32 of K at a time through
-// two buffers in shared memory, the next ones' loads under way beside the products, 4 x 4 elements a
-// thread, fp32 throughout; dh's tiles split along K where they are few.
+// Products on CUDA cores: C[m][n] = sum_k A(m, k) B(n, k), the operands through two buffers in shared
+// memory, the next ones' loads under way beside the products, 4 x 4 elements a thread, fp32 throughout;
+// dh's tiles split along K where they are few.  Tiles of 64 x 64 by 256 threads and 32 of K at a time, or
+// where these leave SMs idle (VocabArgs::tm) of 32 x 32 and 64 of K, whose quarters four groups of 64 threads
+// take and add up in order: a k-block of the first takes an SM 0.55 us of FMAs alone.
 enum { LOSS = 0, GRAD = 1, DH = 2, DW = 3 };
-constexpr int BM = 64, BK = 32, LOADS = BM * BK / THREADS;
 
-template <typename T, int KIND>
-__global__ void __launch_bounds__(THREADS) vocab_simt_kernel(const __grid_constant__ VocabArgs a, int v0) {
-    __shared__ float As[2][BK][BM + 4], Bs[2][BK][BM + 4];
-    __shared__ VocabRow rows[BM];
-    pdl_wait();
-    pdl_trigger();
-    const int count = *a.count;
+template <int BM>
+struct Simt {
+    static constexpr int BK = 2048 / BM, LOADS = BM * BK / THREADS;
+    static constexpr int PER_ROW = BM / 4, GROUP = PER_ROW * PER_ROW, GROUPS = THREADS / GROUP;  // threads of a tile
+    struct Smem {
+        float a[2][BK][BM + 4], b[2][BK][BM + 4];
+        VocabRow rows[BM];
+    };
+};
+
+template <typename T, int KIND, int BM>
+__device__ __forceinline__ void simt_tile(const VocabArgs &a, int v0, int n0, int m0, int split, typename Simt<BM>::Smem &s) {
+    typedef Simt<BM> S;
+    constexpr int BK = S::BK, LOADS = S::LOADS, GROUPS = S::GROUPS;
+    const DhPlan plan = *a.count;
+    const int count = plan.kept;
     const int piece = min(a.piece, a.V - v0);
     // M, N, K of this product
     const int M = KIND == DW ? piece : count, N = KIND == LOSS || KIND == GRAD ? piece : a.d;
     const int K = KIND == DH ? piece : KIND == DW ? count : a.d;
-    const int n0 = blockIdx.x * BM, m0 = blockIdx.y * BM;
     if (m0 >= M) return;
     int k_lo = 0, k_hi = K, plane_rows = 0;
     if (KIND == DH) {
-        const DhPlan plan = dh_plan(a, count);
-        if ((int)blockIdx.z >= plan.k.s) return;
-        k_lo = min(K, (int)blockIdx.z * plan.k.per * BK);  // (the last piece may leave a split nothing: zeros)
-        k_hi = min(K, k_lo + plan.k.per * BK);
-        plane_rows = plan.rows;
+        if (split >= plan.splits) return;
+        k_lo = min(K, split * plan.per * BK);  // (the last piece may leave a split nothing: zeros)
+        k_hi = min(K, k_lo + plan.per * BK);
+        plane_rows = plan.m_tiles * BM;
     }
-    const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
+    const int tid = threadIdx.x, group = tid / S::GROUP, at = tid % S::GROUP;
+    const int ty = at / S::PER_ROW, tx = at % S::PER_ROW;
     if (KIND != DW) {
-        if (tid < BM) rows[tid] = m0 + tid < count ? a.rows[m0 + tid] : VocabRow{0.f, 0.f, -1, 0};
+        if (tid < BM) s.rows[tid] = m0 + tid < count ? a.rows[m0 + tid] : VocabRow{0.f, 0.f, -1, 0};
         __syncthreads();
     }
     const T *h = (const T *)a.hc, *w = (const T *)a.w;
@@ -254,15 +291,16 @@ __global__ void __launch_bounds__(THREADS) vocab_simt_kernel(const __grid_consta
         for (int i = 0; i < LOADS; ++i) {
             int k, m;
             place(KIND == DW, tid + i * THREADS, &k, &m);
-            As[buf][k][m] = ra[i];
+            s.a[buf][k][m] = ra[i];
             place(KIND == DH || KIND == DW, tid + i * THREADS, &k, &m);
-            Bs[buf][k][m] = rb[i];
+            s.b[buf][k][m] = rb[i];
         }
         __syncthreads();
         if (k0 + BK < k_hi) load(k0 + BK);
 #pragma unroll
-        for (int k = 0; k < BK; ++k) {
-            const float4 x = *(const float4 *)&As[buf][k][ty * 4], y = *(const float4 *)&Bs[buf][k][tx * 4];
+        for (int kk = 0; kk < BK / GROUPS; ++kk) {
+            const int k = group * (BK / GROUPS) + kk;
+            const float4 x = *(const float4 *)&s.a[buf][k][ty * 4], y = *(const float4 *)&s.b[buf][k][tx * 4];
             const float xa[4] = {x.x, x.y, x.z, x.w}, yb[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -270,13 +308,29 @@ __global__ void __launch_bounds__(THREADS) vocab_simt_kernel(const __grid_consta
                 for (int j = 0; j < 4; ++j) c[i][j] += xa[i] * yb[j];
         }
     }
+    constexpr int MINE = 4 / GROUPS;  // rows of the tile that a thread is left with
+    if constexpr (GROUPS > 1) {       // row 4 ty + group of each thread's four, from all groups
+        float(*sum)[4][S::GROUP][4] = (float(*)[4][S::GROUP][4]) & s.a[0][0][0];
+        static_assert(sizeof(float) * GROUPS * 4 * S::GROUP * 4 <= sizeof s.a + sizeof s.b, "sums");
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int ml = ty * 4 + i, m = m0 + ml;
+        for (int i = 0; i < 4; ++i) *(float4 *)sum[group][i][at] = make_float4(c[i][0], c[i][1], c[i][2], c[i][3]);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c[0][j] = 0.f;
+#pragma unroll
+        for (int q = 0; q < GROUPS; ++q) {
+            const float4 y = *(const float4 *)sum[q][group][at];
+            c[0][0] += y.x, c[0][1] += y.y, c[0][2] += y.z, c[0][3] += y.w;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+        const int ml = ty * 4 + (GROUPS > 1 ? group : i), m = m0 + ml;
         if constexpr (KIND == LOSS) {
-            // the 16 threads of a row join their 64 logits
+            // the threads of a row join their logits
             float mx = -INFINITY, l = 0.f;
-            const int tgt = rows[ml].target;
+            const int tgt = s.rows[ml].target;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int v = n0 + tx * 4 + j;
@@ -285,13 +339,13 @@ __global__ void __launch_bounds__(THREADS) vocab_simt_kernel(const __grid_consta
                 if (v == tgt && m < M) a.at[m] = c[i][j];
             }
 #pragma unroll
-            for (int o = 8; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            for (int o = S::PER_ROW / 2; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
             const float mu = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
             for (int j = 0; j < 4; ++j) l += exp2f((c[i][j] - mu) * LOG2E);
 #pragma unroll
-            for (int o = 8; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-            if (tx == 0 && m < M) a.part[(size_t)m * a.parts + blockIdx.x] = make_float2(mx, l);
+            for (int o = S::PER_ROW / 2; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+            if (tx == 0 && m < M) a.part[(size_t)m * a.parts + n0 / BM] = make_float2(mx, l);
         } else {
             if (m >= M) continue;
 #pragma unroll
@@ -299,11 +353,11 @@ __global__ void __launch_bounds__(THREADS) vocab_simt_kernel(const __grid_consta
                 const int n = n0 + tx * 4 + j;
                 if (n >= N) continue;
                 if constexpr (KIND == GRAD) {
-                    const VocabRow r = rows[ml];
+                    const VocabRow r = s.rows[ml];
                     const float p = exp2f((c[i][j] - r.lse) * LOG2E);
                     ((float *)a.grad)[(size_t)m * a.piece + n] = (v0 + n == r.target ? p - 1.f : p) * r.g;
                 } else if constexpr (KIND == DH) {
-                    float *to = a.acc + ((size_t)blockIdx.z * plane_rows + m) * a.d + n;
+                    float *to = a.acc + ((size_t)split * plane_rows + m) * a.d + n;
                     *to = v0 ? *to + c[i][j] : c[i][j];
                 } else {
                     ((T *)a.dw)[(size_t)(v0 + m) * a.ws + n] = from_f<T>(c[i][j]);
@@ -313,20 +367,43 @@ __global__ void __launch_bounds__(THREADS) vocab_simt_kernel(const __grid_consta
     }
 }
 
-template <typename T, int KIND>
+// LOSS or GRAD.
+template <typename T, int KIND, int BM>
+__global__ void __launch_bounds__(THREADS) vocab_simt_kernel(const __grid_constant__ VocabArgs a, int v0) {
+    __shared__ typename Simt<BM>::Smem s;
+    pdl_wait();
+    pdl_trigger();
+    simt_tile<T, KIND, BM>(a, v0, blockIdx.x * BM, blockIdx.y * BM, 0, s);
+}
+// Both products of the gradient's piece: dh's tiles and splits, then dW's tiles.
+template <typename T, int BM>
+__global__ void __launch_bounds__(THREADS) vocab_simt_back_kernel(const __grid_constant__ VocabArgs a, int v0, int dh_blocks) {
+    __shared__ typename Simt<BM>::Smem s;
+    pdl_wait();
+    pdl_trigger();
+    const int i = blockIdx.x, n0 = blockIdx.y * BM;
+    if (i < dh_blocks) {
+        const int m_tiles = a.count->m_tiles, split = i / m_tiles;
+        simt_tile<T, DH, BM>(a, v0, n0, (i - split * m_tiles) * BM, split, s);
+    } else {
+        simt_tile<T, DW, BM>(a, v0, n0, (i - dh_blocks) * BM, 0, s);
+    }
+}
+
+template <typename T, int KIND, int BM>
 cudaError_t run_simt(const VocabArgs &a, int v0, cudaStream_t st) {
     const int piece = a.V - v0 < a.piece ? a.V - v0 : a.piece;
-    const int M = KIND == DW ? piece : a.n, N = KIND == LOSS || KIND == GRAD ? piece : a.d;
-    // (the splits for all counts: blocks of those that this one does not have leave)
-    const int splits = KIND == DH ? 16 : 1;
-    return launch_k(vocab_simt_kernel<T, KIND>, dim3(ceil_div(N, BM), ceil_div(M, BM), splits), dim3(THREADS), 0, st, a, v0);
+    return launch_k(vocab_simt_kernel<T, KIND, BM>, dim3(ceil_div(piece, BM), ceil_div(a.n, BM)), dim3(THREADS), 0, st, a, v0);
 }
-template <typename T>
+template <typename T, int BM>
 cudaError_t backward_simt(const VocabArgs &a, cudaStream_t st) {
     for (int v0 = 0; v0 < a.V; v0 += a.piece) {
-        cudaError_t e = run_simt<T, GRAD>(a, v0, st);
-        if (e == cudaSuccess) e = run_simt<T, DH>(a, v0, st);
-        if (e == cudaSuccess && a.dw) e = run_simt<T, DW>(a, v0, st);
+        cudaError_t e = run_simt<T, GRAD, BM>(a, v0, st);
+        if (e != cudaSuccess) return e;
+        // (as many as any count of tokens has: blocks of those that this one does not have leave)
+        const int piece = a.V - v0 < a.piece ? a.V - v0 : a.piece, dh_blocks = (int)(a.acc_rows / BM);
+        e = launch_k(vocab_simt_back_kernel<T, BM>, dim3(dh_blocks + (a.dw ? ceil_div(piece, BM) : 0), ceil_div(a.d, BM)), dim3(THREADS), 0,
+                     st, a, v0, dh_blocks);
         if (e != cudaSuccess) return e;
         if (a.V - v0 <= a.piece) break;  // (v0 stays below 2^31)
     }
@@ -349,26 +426,31 @@ cudaError_t launch_vocab_finish_dh(const VocabArgs &a, cudaStream_t st) {
                     dim3(THREADS), 0, st, a);
 }
 
-// Pieces of the vocabulary whose gradients take at most 64 MB (or 64 rows), in whole tiles.
+// Tiles of 32 x 32 where 64 x 64 ones of the logits are fewer than two an SM.  Pieces of the vocabulary
+// whose gradients take at most 64 MB (or 64 rows), in whole tiles.
 void plan_vocab_simt(VocabArgs *a, bool backward, int n_sm) {
+    a->tm = (long long)ceil_div(a->n, 64) * ceil_div(a->V, 64) < (backward ? 1ll : 2ll) * n_sm ? 32 : 64;
+    const int tm = a->tm;
     a->pad = a->n;
     a->pairs = 4 * n_sm;
-    a->parts = ceil_div(a->V, BM);
-    a->piece = ceil_div(a->V, BM) * BM;
+    a->parts = ceil_div(a->V, tm);
+    a->piece = ceil_div(a->V, tm) * tm;
     a->n_pieces = 1;
     if (backward) {
-        long long most = (64ll << 20) / 4 / a->n / BM * BM;
-        if (most > 65535ll * BM) most = 65535ll * BM;  // (tiles of M are the grid's second index)
-        a->piece = most < BM ? BM : most < a->V ? (int)most : ceil_div(a->V, BM) * BM;
+        long long most = (64ll << 20) / 4 / a->n / tm * tm;
+        if (most > 65535ll * tm) most = 65535ll * tm;  // (tiles of M are the grid's second index)
+        a->piece = most < tm ? tm : most < a->V ? (int)most : ceil_div(a->V, tm) * tm;
         a->n_pieces = ceil_div(a->V, a->piece);
     }
 }
 
 cudaError_t launch_vocab_loss_simt(const VocabArgs &a, cudaStream_t st) {
-    return a.dtype == SP_F32 ? run_simt<float, LOSS>(a, 0, st) : run_simt<bf16, LOSS>(a, 0, st);
+    if (a.dtype == SP_F32) return a.tm == 32 ? run_simt<float, LOSS, 32>(a, 0, st) : run_simt<float, LOSS, 64>(a, 0, st);
+    return a.tm == 32 ? run_simt<bf16, LOSS, 32>(a, 0, st) : run_simt<bf16, LOSS, 64>(a, 0, st);
 }
 cudaError_t launch_vocab_backward_simt(const VocabArgs &a, cudaStream_t st) {
-    return a.dtype == SP_F32 ? backward_simt<float>(a, st) : backward_simt<bf16>(a, st);
+    if (a.dtype == SP_F32) return a.tm == 32 ? backward_simt<float, 32>(a, st) : backward_simt<float, 64>(a, st);
+    return a.tm == 32 ? backward_simt<bf16, 32>(a, st) : backward_simt<bf16, 64>(a, st);
 }
 
 }  // namespace sp

@@ -72,7 +72,7 @@ struct Tiles {
 };
 template <int KIND>
 __device__ __forceinline__ int count_of(const VocabArgs &a) {
-    return KIND == LOSS && a.direct ? a.n : *a.count;
+    return KIND == LOSS && a.direct ? a.n : a.count->kept;
 }
 template <int KIND>
 __device__ __forceinline__ int cols_of(const VocabArgs &a) {
@@ -87,8 +87,8 @@ __device__ __forceinline__ Tiles tiles_of(const VocabArgs &a, int count, int pie
     t.kb = KIND == DH ? ceil_div(piece, BK) : KIND == DW ? ceil_div(max(count, 1), BK) : ceil_div(a.d, BK);
     t.splits = 1, t.per = t.kb;
     if (KIND == DH) {
-        const DhPlan p = dh_plan(a, count);
-        t.splits = p.k.s, t.per = p.k.per;
+        const DhPlan p = *a.count;
+        t.splits = p.splits, t.per = p.per;
     }
     return t;
 }
@@ -412,6 +412,7 @@ bool vocab_tc_supported(const VocabArgs &a) {
 }
 
 void plan_vocab_tc(VocabArgs *a, bool backward, int n_sm) {
+    a->tm = TM;
     a->pad = ceil_div(a->n, TM) * TM;
     a->pairs = n_sm / 2 > 0 ? n_sm / 2 : 1;
     a->tn = TN;
