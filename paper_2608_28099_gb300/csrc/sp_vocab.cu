@@ -6,6 +6,8 @@
 // Here: what stands around the products (counting off the tokens that have a target, joining the
 // parts of a row's sum, writing gradients back to their tokens), and the products on CUDA cores in
 // fp32 for fp32 rows and unaligned ones.  The tensor-core products are in sp_vocab_tc.cu.
+#include <type_traits>
+
 #include "sp_train.cuh"
 
 namespace sp {
@@ -232,6 +234,10 @@ struct Simt {
     };
 };
 
+template <typename T, int KIND>
+struct SimtA {
+    typedef typename std::conditional<KIND == LOSS || KIND == GRAD, T, float>::type type;
+};
 template <typename T, int KIND, int BM>
 __device__ __forceinline__ void simt_tile(const VocabArgs &a, int v0, int n0, int m0, int split, typename Simt<BM>::Smem &s) {
     typedef Simt<BM> S;
@@ -256,31 +262,48 @@ __device__ __forceinline__ void simt_tile(const VocabArgs &a, int v0, int n0, in
         if (tid < BM) s.rows[tid] = m0 + tid < count ? a.rows[m0 + tid] : VocabRow{0.f, 0.f, -1, 0};
         __syncthreads();
     }
-    const T *h = (const T *)a.hc, *w = (const T *)a.w;
-    const float *grad = (const float *)a.grad;
-    const auto A = [&](int m, int k) -> float {
-        if (m0 + m >= M || k >= k_hi) return 0.f;
-        if (KIND == LOSS || KIND == GRAD) return to_f(h[(size_t)(m0 + m) * a.d + k]);
-        if (KIND == DH) return grad[(size_t)(m0 + m) * a.piece + k];
-        return grad[(size_t)k * a.piece + m0 + m];
+    // element (row, k) of the tile's A and B: at p[row * rows + k * steps]; neighbouring threads along whichever
+    // index is contiguous in memory (k: 8 by 4 rows, whose places in shared memory lie in 32 banks)
+    constexpr bool A_MN = KIND == DW, B_MN = KIND == DH || KIND == DW;
+    typedef typename SimtA<T, KIND>::type TA;
+    const TA *pa0;
+    const T *pb0;
+    size_t rows_a = 1, rows_b = 1, step_a = 1, step_b = 1;
+    if constexpr (KIND == LOSS || KIND == GRAD) {
+        pa0 = (const T *)a.hc + (size_t)m0 * a.d, rows_a = a.d;
+        pb0 = (const T *)a.w + (size_t)(v0 + n0) * a.ws, rows_b = a.ws;
+    } else if constexpr (KIND == DH) {
+        pa0 = (const float *)a.grad + (size_t)m0 * a.piece, rows_a = a.piece;
+        pb0 = (const T *)a.w + (size_t)v0 * a.ws + n0, step_b = a.ws;
+    } else {
+        pa0 = (const float *)a.grad + m0, step_a = a.piece;
+        pb0 = (const T *)a.hc + n0, step_b = a.d;
+    }
+    const auto place = [&](bool mn, int x, int *k, int *m) {
+        if (mn) *k = x / BM, *m = x % BM;
+        else *k = (x & 7) + 8 * ((x >> 5) % (BK / 8)), *m = (x >> 3 & 3) + 4 * ((x >> 5) / (BK / 8));
     };
-    const auto B = [&](int n, int k) -> float {
-        if (n0 + n >= N || k >= k_hi) return 0.f;
-        if (KIND == LOSS || KIND == GRAD) return to_f(w[(size_t)(v0 + n0 + n) * a.ws + k]);
-        if (KIND == DH) return to_f(w[(size_t)(v0 + k) * a.ws + n0 + n]);
-        return to_f(h[(size_t)k * a.d + n0 + n]);
-    };
-    // neighbouring threads along whichever index is contiguous in memory
-    const auto place = [&](bool mn, int x, int *k, int *m) { *k = mn ? x / BM : x % BK, *m = mn ? x % BM : x / BK; };
+    const TA *pa[LOADS];
+    const T *pb[LOADS];
+    int ka[LOADS], kb[LOADS];  // the k of a thread's elements in front of k_hi, or none
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        int k, m;
+        place(A_MN, tid + i * THREADS, &k, &m);
+        pa[i] = pa0 + (size_t)m * rows_a + (size_t)(k_lo + k) * step_a;
+        ka[i] = m0 + m < M ? k : 1 << 30;
+        place(B_MN, tid + i * THREADS, &k, &m);
+        pb[i] = pb0 + (size_t)m * rows_b + (size_t)(k_lo + k) * step_b;
+        kb[i] = n0 + m < N ? k : 1 << 30;
+    }
     float ra[LOADS], rb[LOADS];
     const auto load = [&](int k0) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            int k, m;
-            place(KIND == DW, tid + i * THREADS, &k, &m);
-            ra[i] = A(m, k0 + k);
-            place(KIND == DH || KIND == DW, tid + i * THREADS, &k, &m);
-            rb[i] = B(m, k0 + k);
+            ra[i] = k0 + ka[i] < k_hi ? to_f(*pa[i]) : 0.f;
+            rb[i] = k0 + kb[i] < k_hi ? to_f(*pb[i]) : 0.f;
+            pa[i] += BK * step_a;
+            pb[i] += BK * step_b;
         }
     };
     float c[4][4] = {};
@@ -290,9 +313,9 @@ __device__ __forceinline__ void simt_tile(const VocabArgs &a, int v0, int n0, in
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             int k, m;
-            place(KIND == DW, tid + i * THREADS, &k, &m);
+            place(A_MN, tid + i * THREADS, &k, &m);
             s.a[buf][k][m] = ra[i];
-            place(KIND == DH || KIND == DW, tid + i * THREADS, &k, &m);
+            place(B_MN, tid + i * THREADS, &k, &m);
             s.b[buf][k][m] = rb[i];
         }
         __syncthreads();
