@@ -414,17 +414,29 @@ int blocks_of(const Shape &s, long long n, int n_sm, int per_sm) {
     return (int)(all < held ? all : held);
 }
 constexpr int FWD_THREADS = 1024, BACK_THREADS = 640;
+template <typename T, bool WARP, int CH, bool E8>
+cudaError_t run_norm(const NormArgs &a, const Shape &s, int n_sm, cudaStream_t st) {
+    return launch_k(norm_kernel<T, WARP, CH, E8>, dim3(blocks_of(s, a.n, n_sm, FWD_THREADS)), dim3(s.threads), 0, st, a);
+}
+template <typename T, bool WARP, int CH>
+cudaError_t run_back(const NormBackArgs &a, const Shape &s, int n_sm, cudaStream_t st) {
+    return launch_k(norm_back_kernel<T, WARP, CH>, dim3(blocks_of(s, a.n, n_sm, BACK_THREADS)), dim3(s.threads), 0, st, a);
+}
+template <typename T>
+cudaError_t run_back_loop(const NormBackArgs &a, int parts, cudaStream_t st) {
+    return launch_k(norm_back_loop_kernel<T>, dim3(parts), dim3(LOOP_THREADS), 0, st, a);
+}
 template <typename T, bool E8>
 cudaError_t norm_shapes(const NormArgs &a, const Shape &s, int n_sm, cudaStream_t st) {
-    const auto k = s.warp ? s.ch == 1 ? norm_kernel<T, true, 1, E8> : s.ch == 2 ? norm_kernel<T, true, 2, E8> : norm_kernel<T, true, 4, E8>
-                          : s.ch == 2 ? norm_kernel<T, false, 2, E8> : norm_kernel<T, false, 4, E8>;
-    return launch_k(k, dim3(blocks_of(s, a.n, n_sm, FWD_THREADS)), dim3(s.threads), 0, st, a);
+    const auto run = s.warp ? s.ch == 1 ? run_norm<T, true, 1, E8> : s.ch == 2 ? run_norm<T, true, 2, E8> : run_norm<T, true, 4, E8>
+                            : s.ch == 2 ? run_norm<T, false, 2, E8> : run_norm<T, false, 4, E8>;
+    return run(a, s, n_sm, st);
 }
 template <typename T>
 cudaError_t back_shapes(const NormBackArgs &a, const Shape &s, int n_sm, cudaStream_t st) {
-    const auto k = s.warp ? s.ch == 1 ? norm_back_kernel<T, true, 1> : s.ch == 2 ? norm_back_kernel<T, true, 2> : norm_back_kernel<T, true, 4>
-                          : s.ch == 2 ? norm_back_kernel<T, false, 2> : norm_back_kernel<T, false, 4>;
-    return launch_k(k, dim3(blocks_of(s, a.n, n_sm, BACK_THREADS)), dim3(s.threads), 0, st, a);
+    const auto run = s.warp ? s.ch == 1 ? run_back<T, true, 1> : s.ch == 2 ? run_back<T, true, 2> : run_back<T, true, 4>
+                            : s.ch == 2 ? run_back<T, false, 2> : run_back<T, false, 4>;
+    return run(a, s, n_sm, st);
 }
 
 }  // namespace
@@ -460,8 +472,7 @@ cudaError_t launch_norm_backward(const NormBackArgs &a, int n_sm, cudaStream_t s
     int parts = blocks_of(loop ? kLoop : s, a.n, n_sm, BACK_THREADS);
     cudaError_t e;
     if (loop) {
-        const auto k = a.dtype == SP_F32 ? norm_back_loop_kernel<float> : norm_back_loop_kernel<bf16>;
-        e = launch_k(k, dim3(parts), dim3(LOOP_THREADS), 0, st, a);
+        e = a.dtype == SP_F32 ? run_back_loop<float>(a, parts, st) : run_back_loop<bf16>(a, parts, st);
     } else {
         e = a.dtype == SP_F32 ? back_shapes<float>(a, s, n_sm, st) : back_shapes<bf16>(a, s, n_sm, st);
         parts *= s.rows;

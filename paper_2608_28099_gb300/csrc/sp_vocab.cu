@@ -438,15 +438,16 @@ cudaError_t backward_simt(const VocabArgs &a, cudaStream_t st) {
 cudaError_t launch_vocab_keep(const VocabArgs &a, bool backward, cudaStream_t st) {
     // a warp a row, but no more than 1024 blocks, since each reads all targets
     const int per = a.n <= 1024 * WARPS ? WARPS : ceil_div(a.n, 1024);
-    return launch_k(a.dtype == SP_F32 ? vocab_keep_kernel<float> : vocab_keep_kernel<bf16>, dim3(ceil_div(a.n, per)), dim3(THREADS), 0,
-                    st, a, per, (int)backward);
+    const dim3 grid(ceil_div(a.n, per));
+    if (a.dtype == SP_F32) return launch_k(vocab_keep_kernel<float>, grid, dim3(THREADS), 0, st, a, per, (int)backward);
+    return launch_k(vocab_keep_kernel<bf16>, grid, dim3(THREADS), 0, st, a, per, (int)backward);
 }
 cudaError_t launch_vocab_finish_loss(const VocabArgs &a, cudaStream_t st) {
     return launch_k(vocab_finish_loss_kernel, dim3(ceil_div(a.n, WARPS)), dim3(THREADS), 0, st, a);
 }
 cudaError_t launch_vocab_finish_dh(const VocabArgs &a, cudaStream_t st) {
-    return launch_k(a.dtype == SP_F32 ? vocab_finish_dh_kernel<float> : vocab_finish_dh_kernel<bf16>, dim3(a.n),
-                    dim3(THREADS), 0, st, a);
+    if (a.dtype == SP_F32) return launch_k(vocab_finish_dh_kernel<float>, dim3(a.n), dim3(THREADS), 0, st, a);
+    return launch_k(vocab_finish_dh_kernel<bf16>, dim3(a.n), dim3(THREADS), 0, st, a);
 }
 
 // Tiles of 32 x 32 where 64 x 64 ones of the logits are fewer than two an SM.  Pieces of the vocabulary
