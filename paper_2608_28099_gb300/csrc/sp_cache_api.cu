@@ -150,8 +150,8 @@ sp_status check_tree(const sp_tree_dims *d, const sp_token_cache *cache, int bat
     a->most_len = cache->kv.layout == SP_KV_PAGED && paged < cache->max_seq_len ? (int)paged : cache->max_seq_len;
     a->tensor = d->path != 1 && (backward ? tree_back_tc_supported(*a) : tree_tc_supported(*a));
     if (d->path == 2 && !a->tensor)
-        return fail(SP_ERR_UNSUPPORTED, "the tensor-core kernel needs bf16 rows, a bf16 %scache of head_dim 128 "
-                                        "and a batch of at most 2048", backward ? "" : "or 8-bit ");
+        return fail(SP_ERR_UNSUPPORTED, "the tensor-core kernel needs bf16 rows, a bf16 or 8-bit cache of head_dim 128 "
+                                        "and a batch of at most 2048");
     if (a->tensor && backward) plan_tree_back_tc(a, sm_count());
     else if (a->tensor) plan_tree_tc(a, sm_count());
     else plan_tree_simt(a, sm_count());

@@ -13,7 +13,7 @@
 //
 // Warps 0-7 softmax; 8-11 bring queries and output gradients (a segment ahead into shared memory,
 // then into TMEM) and write dQ out; 12 MMA issuer and TMEM; 13 K, 14 V (TMA boxes of whole pages, cp.async
-// elsewhere).  TMEM: S, dP, dQ, Q, dO in all 512 columns.  Every wait is time-limited
+// elsewhere; 8-bit caches: 15 copies the codes, which 13 and 14 turn into bf16).  TMEM: S, dP, dQ, Q, dO in all 512 columns.  Every wait is time-limited
 // (SP_DEV_TIMEOUT).
 //
 // What bounds it: HBM for long sequences.  Eight of 32768 tokens, 40 heads (80 rows a kv head): 182 us,
@@ -39,6 +39,7 @@ namespace {
 
 constexpr int TILE = 128;
 constexpr int SLOT = TILE * DH * 2;             // K or V of a tile, 32 KB
+constexpr int SCALES = 2 * TILE * 4, RAW = TILE * DH + SCALES;  // a tile's scales; 8-bit codes of K or V with them
 constexpr int LD = DH + 8, STAGE_ROW = LD * 2;  // a staged row of queries or output gradients: elements, bytes
 constexpr int MAX_NODES = 16;                   // most nodes whose products are formed here
 constexpr int ROWS = 128;                       // most rows of a block
@@ -46,7 +47,7 @@ constexpr int MAX_RING = 8;
 constexpr int BAR_EPI = 1;                      // named barrier of warps 8-11
 constexpr int SMEM_MAX = 227 * 1024;
 constexpr int THREADS = 512;
-constexpr int EPI = 8, MMA = 12, K_WARP = 13, V_WARP = 14;
+constexpr int EPI = 8, MMA = 12, K_WARP = 13, V_WARP = 14, COPY_WARP = 15;
 constexpr uint32_t DP_COL = 128, DQ_COL = 256, Q_COL = 384, DO_COL = 448;  // TMEM: S, dP, dQ, Q, dO
 // Fewest tiles a share holds on average (one sequence of 2048 tokens: 15.3, 14.7, 15.9 us with 1, 2, 3), and
 // the cost of a segment in tiles (64 sequences of 1024 to 8192 tokens, 16 of 256 to 2048, 32 of 500 to 9000
@@ -55,9 +56,11 @@ constexpr int kBackMinTiles = 2;
 constexpr int kBackSegCost = 5;
 
 struct Layout {
-    int nk, nv;                                 // ring slots
-    int off_q, off_do, off_n, off_ds, off_kn, off_k, off_v, off_tab;  // (off_q, off_do: staged rows; off_n:
-                                                // Nodes; off_ds, off_kn: operands of the nodes' part of dQ)
+    int nk, nv, nr;                             // ring slots of K and V, of 8-bit codes
+    int off_q, off_do, off_n, off_ds, off_kn, off_k, off_v, off_sc, off_raw, off_tab;  // (off_q, off_do: staged rows; off_n:
+                                                // Nodes; off_ds, off_kn: operands of the nodes' part of dQ;
+                                                // 8-bit caches: off_sc: scales of the tiles in K's slots;
+                                                // off_raw: codes of K or V of a tile, with K the scales of both)
     int smem;
 };
 struct Bars {
@@ -66,6 +69,8 @@ struct Bars {
     uint32_t tmem;
     int abort;
     int wsum[32];
+    uint64_t raw_full[MAX_RING], raw_empty[MAX_RING];  // 8-bit caches
+    int raw_meta[MAX_RING];
 };
 // What the segments' rows need, and the nodes of one.
 struct Nodes {
@@ -422,8 +427,169 @@ __device__ __forceinline__ void row_to_tmem(uint32_t addr, const uint8_t *row) {
     }
 }
 
+// 16 codes of row r (16-byte chunk c of its 128) as bf16, exactly, into a slot.
+__device__ __forceinline__ void put_codes(uint8_t *slot, int r, int c, uint4 u) {
+    const bool odd = c & 4;  // (the dim halves lie 1024 bytes apart: their lanes store chunks of other banks)
+    const uint2 w[2] = {odd ? make_uint2(u.z, u.w) : make_uint2(u.x, u.y), odd ? make_uint2(u.x, u.y) : make_uint2(u.z, u.w)};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float v[8];
+        codes_to_float(w[h], v);
+        st_shared_v4(slot + kv_off(r, 2 * c + (h ? !odd : odd)), pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]),
+                     pack_bf16(v[6], v[7]));
+    }
+}
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+        "l"(src), "r"(bytes), "r"(smem_u32(bar))
+        : "memory");
+}
+__device__ __forceinline__ void cp_async4(void *dst, const void *src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+// The 8-bit cache's codes and scales, copied by one warp (whole pages, or pieces of a row): K of a tile with
+// the scales of both, V of it, and so on around one ring.
+__device__ __forceinline__ void copy_codes(const TreeArgs &a, const Share &sh, const int *sids, const int *lens, int n_tiles, int g,
+                                           Bars *bars, const Layout &lay, uint8_t *smem, volatile int *abort, int lane) {
+    const bool paged = a.cache.kv.layout == SP_KV_PAGED;
+    const int P = a.cache.kv.page_size, P_bits = 31 - __clz(max(P, 1)), Hkv = a.Hkv;
+    struct Tile {
+        int b, t0, n_tok, page;
+    };
+    int bad = 0;
+    const auto ask = [&](const Walk &w) {  // (a lane's page)
+        Tile t;
+        t.b = sh.b0 + w.j;
+        t.t0 = (w.sg.t_a + w.i) * TILE;
+        t.n_tok = min(TILE, lens[t.b] - t.t0);
+        t.page = -1;
+        const int lp = (t.t0 >> P_bits) + lane;
+        if (paged && lane * P < t.n_tok && lp < a.cache.kv.max_pages)
+            t.page = __ldg(a.cache.kv.page_table + (size_t)sids[t.b] * a.cache.kv.max_pages + lp);
+        return t;
+    };
+    Ring rg(lay.nr);
+    int filled = 0;
+    if (n_tiles > 0) {
+        Walk at(sh);
+        Tile t = ask(at);
+#pragma unroll 1
+        for (int x = 0; x < n_tiles; ++x) {
+            Tile next = t;
+            at.next();
+            if (x + 1 < n_tiles) next = ask(at);
+            const bool mine = paged && lane * P < t.n_tok, have = mine && t.page >= 0 && t.page < a.cache.kv.n_pages;
+            if (mine && !have) bad = 1;
+            const unsigned okm = __ballot_sync(0xffffffffu, have);
+            // what the converting warps need: the groups of 16 rows that are there, and the tokens
+            const int units = __ballot_sync(0xffffffffu, lane < 8 && lane * 16 < t.n_tok && (!paged || okm >> (lane * 16 >> P_bits) & 1));
+            const int meta = units | max(t.n_tok, 0) << 8;
+            const size_t row = paged ? ((size_t)t.page * Hkv + g) * P : (size_t)t.t0 * Hkv + g;  // (of a lane's page, if any)
+#pragma unroll 1
+            for (int is_v = 0; is_v < 2; ++is_v) {
+                if (!wait_warp(&bars->raw_empty[rg.slot], rg.ph ^ 1, abort)) goto out;
+                uint64_t *bar = &bars->raw_full[rg.slot];
+                uint8_t *dst = smem + lay.off_raw + rg.slot * RAW;
+                float *sc = (float *)(dst + TILE * DH);
+                if (lane == 0) bars->raw_meta[rg.slot] = meta;
+                if (mine && !have) {  // (scales behind the last token do not matter)
+#pragma unroll 1
+                    for (int r = lane * P; r < (lane + 1) * P; ++r) sc[r] = sc[TILE + r] = 0.f;
+                }
+                __syncwarp();
+                // (a lane's stores are behind its own arrival where every lane arrives)
+                if (!paged) mbar_arrive(bar);
+                else if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(__popc(okm) * P * (is_v ? DH : DH + 8)));
+                __syncwarp();
+                if (units) {
+                    const uint8_t *src = (const uint8_t *)cache_base(a.cache, sids[t.b], is_v) + row * DH;
+                    const float *k0 = is_v ? nullptr : scale_base(a.cache, sids[t.b], 0) + row;
+                    const float *v0 = is_v ? nullptr : scale_base(a.cache, sids[t.b], 1) + row;
+                    if (have) {
+                        bulk_load(dst + lane * P * DH, src, P * DH, bar);
+                        if (!is_v) {
+                            bulk_load(sc + lane * P, k0, P * 4, bar);
+                            bulk_load(sc + TILE + lane * P, v0, P * 4, bar);
+                        }
+                    } else if (!paged) {
+                        const int r0 = lane >> 3, c = lane & 7;
+                        const size_t step = (size_t)Hkv * DH;
+                        src += r0 * step + c * 16;
+#pragma unroll 4
+                        for (int r = r0; r < t.n_tok; r += 4, src += 4 * step) cp_async16(dst + r * DH + c * 16, src);
+                        if (!is_v) {
+#pragma unroll 1
+                            for (int r = lane; r < t.n_tok; r += 32) {
+                                cp_async4(sc + r, k0 + (size_t)r * Hkv);
+                                cp_async4(sc + TILE + r, v0 + (size_t)r * Hkv);
+                            }
+                        }
+                    }
+                }
+                if (!paged) cp_async_mbar_arrive(bar);
+                rg.next();
+                ++filled;
+            }
+            t = next;
+        }
+    }
+out:
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (lane == 0 && paged)  // copies still in flight (only possible after an abort): the last use of every slot
+        for (int j = 1; j <= min(filled, rg.n); ++j)
+            mbar_wait_drain(&bars->raw_full[(rg.slot - j + rg.n) % rg.n], rg.slot >= j ? rg.ph : rg.ph ^ 1);
+    if (__any_sync(0xffffffffu, bad) && lane == 0 && a.status) atomicOr(a.status, SP_DEV_BAD_PAGE);
+}
+// Codes of K (or of V) to bf16 in that operand's ring, K's tiles with their scales.
+__device__ __forceinline__ void convert_codes(bool is_v, int n_tiles, Bars *bars, const Layout &lay, uint8_t *smem, volatile int *abort,
+                                              int lane) {
+    const int r0 = lane >> 3, c = lane & 7;
+    Ring rr(lay.nr), rg(is_v ? lay.nv : lay.nk);
+    uint64_t *full = is_v ? bars->v_full : bars->k_full, *empty = is_v ? bars->v_empty : bars->k_empty;
+    uint8_t *ring = smem + (is_v ? lay.off_v : lay.off_k);
+    if (is_v) rr.next();
+#pragma unroll 1
+    for (int x = 0; x < n_tiles; ++x, rg.next(), rr.next(), rr.next()) {
+        if (!wait_warp(&bars->raw_full[rr.slot], rr.ph, abort) || !wait_warp(&empty[rg.slot], rg.ph ^ 1, abort)) break;
+        uint8_t *slot = ring + rg.slot * SLOT;
+        const uint8_t *raw = smem + lay.off_raw + rr.slot * RAW;
+        const int m = ((volatile int *)bars->raw_meta)[rr.slot], n_tok = m >> 8;
+        if (!is_v) {
+            const float4 *from = (const float4 *)(raw + TILE * DH);
+            float4 *to = (float4 *)(smem + lay.off_sc + rg.slot * SCALES);
+            to[lane] = from[lane];
+            to[32 + lane] = from[32 + lane];
+        }
+        uint4 next[4];
+        const auto load = [&](int i) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int r = i * 16 + k * 4 + r0;
+                next[k] = make_uint4(0, 0, 0, 0);
+                if ((m >> i & 1) && r < n_tok) next[k] = *(const uint4 *)(raw + r * DH + c * 16);
+            }
+        };
+        load(0);
+#pragma unroll 1
+        for (int i = 0; i < TILE / 16; ++i) {
+            uint4 now[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) now[k] = next[k];
+            if (i + 1 < TILE / 16) load(i + 1);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) put_codes(slot, i * 16 + k * 4 + r0, c, now[k]);
+        }
+        fence_proxy_async();
+        mbar_arrive(&full[rg.slot]);
+        arrive_warp(&bars->raw_empty[rr.slot], lane);
+    }
+}
+
 // NODES: the row statistics and what lies between the nodes are formed here, else by a kernel in front.
-template <bool NODES>
+// EIGHT: the cache holds 8-bit codes, whose scales enter S, dP and ds in fp32 (a bf16 holds a code, not its
+// product with the scale).
+template <bool NODES, bool EIGHT>
 __global__ void __launch_bounds__(THREADS, 1)
     tree_back_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                         const __grid_constant__ TreeBackArgs args, const __grid_constant__ Layout lay, int2 *split_tab) {
@@ -462,6 +628,13 @@ __global__ void __launch_bounds__(THREADS, 1)
             mbar_init(&bars->v_full[i], 32);
             mbar_init(&bars->v_empty[i], 1);
         }
+        if (EIGHT) {
+#pragma unroll 1
+            for (int i = 0; i < lay.nr; ++i) {
+                mbar_init(&bars->raw_full[i], paged ? 1 : 64);
+                mbar_init(&bars->raw_empty[i], 1);
+            }
+        }
         mbar_init(&bars->s_full, 1);
         mbar_init(&bars->s_read, 8);
         mbar_init(&bars->d_full, 1);
@@ -474,7 +647,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         mbar_init(&bars->fin, 1);
         bars->abort = 0;
         fence_mbar_init();
-        if (paged) {
+        if (paged && !EIGHT) {
             prefetch_tmap(&map_k);
             prefetch_tmap(&map_v);
         }
@@ -515,6 +688,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (!NODES) pdl_wait();  // the row statistics
         bool ok = true;
         uint32_t ph = 0;
+        Ring rs(lay.nk);
 #pragma unroll 1
         for (int b = sh.b0; ok && b < sh.b1; ++b) {
             const Seg sg = piece(sh, b);
@@ -522,7 +696,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             float2 st = make_float2(INFINITY, 0.f);
             if (!NODES && active) st = __ldcg(args.stat + ((size_t)b * Hkv + g) * a.R + rr);
 #pragma unroll 1
-            for (int i = 0; i < sg.n; ++i, ph ^= 1) {
+            for (int i = 0; i < sg.n; ++i, ph ^= 1, rs.next()) {
                 ok = ok && wait_warp(&bars->s_full, ph, abort);
                 if (!ok) break;
                 tc_fence_after();
@@ -531,6 +705,10 @@ __global__ void __launch_bounds__(THREADS, 1)
                     const volatile float *at = &ns->stat[(b - sh.b0) & 1][r].x;
                     st = make_float2(at[0], at[1]);
                 }
+                // the tile's scales, there with its keys, which stay until its dQ is formed
+                const float4 *ks = (const float4 *)((const float *)(smem + lay.off_sc) + rs.slot * 2 * TILE + c0), *vs = ks + TILE / 4;
+                if (EIGHT) ok = wait_warp(&bars->k_full[rs.slot], rs.ph, abort);
+                if (!ok) break;
                 const int n_tok = left - i * TILE;
                 float s[64];
                 if (warp_active) {  // the weights, while dP is formed
@@ -538,6 +716,13 @@ __global__ void __launch_bounds__(THREADS, 1)
                     ld32_async(s_col + 32, s + 32);
                     ld_wait(s);
                     ld_wait(s + 32);
+                    if constexpr (EIGHT) {
+#pragma unroll
+                        for (int e = 0; e < 64; e += 4) {
+                            const float4 f = ks[e / 4];
+                            s[e] *= f.x, s[e + 1] *= f.y, s[e + 2] *= f.z, s[e + 3] *= f.w;
+                        }
+                    }
 #pragma unroll
                     for (int e = 0; e < 64; ++e) s[e] = fast_exp2(fmaf(s[e], a.scale_log2, -st.x));
                     tc_fence_before();
@@ -552,6 +737,14 @@ __global__ void __launch_bounds__(THREADS, 1)
                         float d[32];
                         ld32_async(s_col + DP_COL + c * 32, d);
                         ld_wait(d);
+                        if constexpr (EIGHT) {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4) {
+                                const float4 f = vs[c * 8 + e / 4], k = ks[c * 8 + e / 4];
+                                d[e] *= f.x, d[e + 1] *= f.y, d[e + 2] *= f.z, d[e + 3] *= f.w;
+                                s[c * 32 + e] *= k.x, s[c * 32 + e + 1] *= k.y, s[c * 32 + e + 2] *= k.z, s[c * 32 + e + 3] *= k.w;
+                            }
+                        }
 #pragma unroll
                         for (int e = 0; e < 32; ++e) d[e] = s[c * 32 + e] * (d[e] - st.y);
                         if (n_tok < c * 32 + 32) {  // past the end: what was loaded there is nothing
@@ -661,7 +854,10 @@ __global__ void __launch_bounds__(THREADS, 1)
             if (ok) arrive_warp(&bars->dq_empty, lane);
             if (j + 1 < n_seg) between(j + 1);
         }
-    } else if (warp == K_WARP || warp == V_WARP) {
+    } else if (EIGHT && warp >= K_WARP) {
+        if (warp == COPY_WARP) copy_codes(a, sh, sids, lens, n_tiles, g, bars, lay, smem, abort, lane);
+        else convert_codes(warp == V_WARP, n_tiles, bars, lay, smem, abort, lane);
+    } else if (!EIGHT && (warp == K_WARP || warp == V_WARP)) {
         // ------------------------------------------------------------ K and V
         const bool is_v = warp == V_WARP;
         uint64_t *full = is_v ? bars->v_full : bars->k_full, *empty = is_v ? bars->v_empty : bars->k_empty;
@@ -893,7 +1089,7 @@ __global__ void __launch_bounds__(SUM_THREADS) tree_back_tc_sum_kernel(const __g
         live ? make_uint2(pack_bf16(s.x * f, s.y * f), pack_bf16(s.z * f, s.w * f)) : make_uint2(0, 0);
 }
 
-bool make_layout(const TreeArgs &a, int rb_rows, bool nodes, Layout *lay) {
+bool make_layout(const TreeArgs &a, int rb_rows, bool nodes, bool eight, Layout *lay) {
     const int tab = (4 * a.B + 1) * 4;
     lay->off_tab = OFF_FRONT;
     lay->off_q = (OFF_FRONT + tab + 15) & ~15;
@@ -902,34 +1098,60 @@ bool make_layout(const TreeArgs &a, int rb_rows, bool nodes, Layout *lay) {
     lay->off_n = lay->off_do + rows * STAGE_ROW;
     lay->off_ds = (lay->off_n + (nodes ? (int)sizeof(Nodes) : 0) + 1023) & ~1023;
     lay->off_kn = lay->off_ds + (nodes ? DS_BYTES : 0);
-    const int at = lay->off_kn + (nodes ? 2 * KN_BYTES : 0), slots = (SMEM_MAX - 1024 - at) / SLOT;
-    if (slots < 3) return false;
-    lay->nv = slots / 2 < MAX_RING ? slots / 2 : MAX_RING;  // (K is held until dQ has read it)
-    lay->nk = slots - lay->nv < MAX_RING ? slots - lay->nv : MAX_RING;
+    const int at = lay->off_kn + (nodes ? 2 * KN_BYTES : 0);
+    int left = SMEM_MAX - 1024 - at;
+    lay->nr = 0;
+    if (eight) {
+        // two slots of K and one of V, then rings of codes, which cover the copies' latency, then more slots
+        const int k_slot = SLOT + SCALES;
+        lay->nk = 2, lay->nv = 1;
+        left -= 2 * k_slot + SLOT;
+        while (lay->nr < 4 && left >= RAW) ++lay->nr, left -= RAW;
+        if (lay->nr < 2) return false;
+        if (left >= SLOT) ++lay->nv, left -= SLOT;
+        if (left >= k_slot) ++lay->nk, left -= k_slot;
+        while (lay->nr < MAX_RING && left >= RAW) ++lay->nr, left -= RAW;
+    } else {
+        const int slots = left / SLOT;
+        if (slots < 3) return false;
+        lay->nv = slots / 2 < MAX_RING ? slots / 2 : MAX_RING;  // (K is held until dQ has read it)
+        lay->nk = slots - lay->nv < MAX_RING ? slots - lay->nv : MAX_RING;
+    }
     lay->off_k = at;
     lay->off_v = lay->off_k + lay->nk * SLOT;
-    lay->smem = lay->off_v + lay->nv * SLOT + 1024;
+    lay->off_sc = lay->off_v + lay->nv * SLOT;
+    lay->off_raw = lay->off_sc + (eight ? lay->nk * SCALES : 0);
+    lay->smem = lay->off_raw + lay->nr * RAW + 1024;
     return lay->smem <= SMEM_MAX;
 }
 
-template <bool NODES>
+// The fewest row blocks whose shared memory fits (0: none; the rings of 8-bit codes and a table of thousands of
+// sequences leave no room for 128 rows).
+int row_blocks(const TreeArgs &a) {
+    Layout lay;
+    for (int n = ceil_div(a.R, ROWS); n <= ceil_div(a.R, 32); ++n)
+        if (make_layout(a, ceil_div(a.R, n), n == 1 && a.N <= MAX_NODES, a.cache.dtype == SP_E4M3, &lay)) return n;
+    return 0;
+}
+
+template <bool NODES, bool EIGHT>
 cudaError_t run(const TreeBackArgs &a, const Layout &lay, const CUtensorMap &mk, const CUtensorMap &mv, int2 *tab, cudaStream_t st) {
     static bool known[MAX_DEVICES] = {};
-    const cudaError_t e = allow_smem(tree_back_tc_kernel<NODES>, SMEM_MAX, known);
+    const cudaError_t e = allow_smem(tree_back_tc_kernel<NODES, EIGHT>, SMEM_MAX, known);
     if (e != cudaSuccess) return e;
-    return launch_k(tree_back_tc_kernel<NODES>, dim3(a.t.plan.tc_ctas), dim3(THREADS), (size_t)lay.smem, st, mk, mv, a, lay, tab);
+    return launch_k(tree_back_tc_kernel<NODES, EIGHT>, dim3(a.t.plan.tc_ctas), dim3(THREADS), (size_t)lay.smem, st, mk, mv, a, lay, tab);
 }
 
 }  // namespace
 
 bool tree_back_tc_supported(const TreeArgs &a) {
-    Layout lay;
-    return a.dh == DH && a.dtype == SP_BF16 && a.cache.dtype == SP_BF16 && a.B <= MAX_B && make_layout(a, ROWS, true, &lay) &&
-           (a.cache.kv.layout == SP_KV_CONTIGUOUS || (long long)a.cache.kv.n_pages * a.Hkv * a.cache.kv.page_size <= 0x7fffffffLL);
+    const bool eight = a.cache.dtype == SP_E4M3;
+    return a.dh == DH && a.dtype == SP_BF16 && (a.cache.dtype == SP_BF16 || eight) && a.B <= MAX_B && row_blocks(a) > 0 &&
+           (eight || a.cache.kv.layout == SP_KV_CONTIGUOUS || (long long)a.cache.kv.n_pages * a.Hkv * a.cache.kv.page_size <= 0x7fffffffLL);
 }
 
 void plan_tree_back_tc(TreeArgs *a, int n_sm) {
-    a->n_rb = ceil_div(a->R, ROWS);
+    a->n_rb = row_blocks(*a);
     a->rb_rows = ceil_div(a->R, a->n_rb);
     const int Hv = a->Hkv * a->n_rb;
     // (the tile list's numbers stay below 2^30)
@@ -950,12 +1172,12 @@ size_t tree_back_tc_slots(const TreeArgs &a) { return 2 * (size_t)a.plan.tc_ctas
 cudaError_t launch_tree_back_tc(const TreeBackArgs &args, int2 *split_tab, cudaStream_t st) {
     const TreeArgs &a = args.t;
     Layout lay;
-    const bool nodes = a.n_rb == 1 && a.N <= MAX_NODES;
-    if (!make_layout(a, a.rb_rows, nodes, &lay)) return cudaErrorInvalidValue;
+    const bool nodes = a.n_rb == 1 && a.N <= MAX_NODES, eight = a.cache.dtype == SP_E4M3;
+    if (!make_layout(a, a.rb_rows, nodes, eight, &lay)) return cudaErrorInvalidValue;
     CUtensorMap mk, mv;
     memset(&mk, 0, sizeof mk);
     memset(&mv, 0, sizeof mv);
-    if (a.cache.kv.layout == SP_KV_PAGED) {
+    if (a.cache.kv.layout == SP_KV_PAGED && !eight) {
         const long long blocks = (long long)a.cache.kv.n_pages * a.Hkv;
         if (!encode_kv_pages_bf16(&mk, a.cache.kv.k_pool, blocks, a.cache.kv.page_size) ||
             !encode_kv_pages_bf16(&mv, a.cache.kv.v_pool, blocks, a.cache.kv.page_size))
@@ -963,7 +1185,8 @@ cudaError_t launch_tree_back_tc(const TreeBackArgs &args, int2 *split_tab, cudaS
     }
     cudaError_t e = nodes ? cudaSuccess : launch_tree_back_rows_tc(args, st);
     if (e != cudaSuccess) return e;
-    e = nodes ? run<true>(args, lay, mk, mv, split_tab, st) : run<false>(args, lay, mk, mv, split_tab, st);
+    const auto go = eight ? nodes ? run<true, true> : run<false, true> : nodes ? run<true, false> : run<false, false>;
+    e = go(args, lay, mk, mv, split_tab, st);
     if (e != cudaSuccess) return e;
     return launch_k(tree_back_tc_sum_kernel, dim3(a.Hkv * a.n_rb, tree_back_tc_groups(a), ceil_div(a.rb_rows, SUM_ROWS)),
                     dim3(SUM_THREADS), 0, st, args, (const int2 *)split_tab, (int)!nodes);

@@ -45,7 +45,7 @@ class Case:
         self.scale = scale or dh ** -0.5
         self.dims = sp.sp_tree_dims(hq, N, dtype, path, 0, scale, *strides)
         self.strides = strides
-        self.tensor = dtype == sp.SP_BF16 and dh == 128 and cdt == sp.SP_BF16 and path != 1
+        self.tensor = dtype == sp.SP_BF16 and dh == 128 and cdt != sp.SP_F32 and path != 1
 
     def forward(self):
         torch, B = self.torch, len(self.lens)
@@ -148,7 +148,7 @@ def test_ragged_batches(torch, cdt, dtype, page, dh, hq, hkv):
     Case(torch, cdt, dtype, page, dh, hq, hkv, [0, 1, 15, 16, 63, 64, 65, 127, 128, 129, 200, 400], 5, seed=page + dh).check()
 
 
-@pytest.mark.parametrize("cdt,dtype", ALL[:2])
+@pytest.mark.parametrize("cdt,dtype", ALL[:3])
 @pytest.mark.parametrize("G,N", [(1, 1), (4, 1), (5, 3), (4, 8), (3, 11), (4, 16), (1, 64), (5, 13), (4, 32), (5, 32), (4, 64),
                                  (8, 64), (40, 2)])
 @pytest.mark.parametrize("page", [0, 16])
@@ -167,16 +167,48 @@ def test_gradients_as_parts_of_a_fused_one(torch, cdt, dtype):
     Case(torch, cdt, dtype, 16, 128, 4, 2, [80, 5], 6, seed=6, strides=(4 * 128 + 16, 2 * 128 + 8, 3 * 128)).check()
 
 
-@pytest.mark.parametrize("cdt,dtype", ALL[:2])
+@pytest.mark.parametrize("cdt,dtype", ALL[:3])
 def test_long_sequences_in_shares(torch, cdt, dtype):
     Case(torch, cdt, dtype, 16, 128, 4, 1, [5000, 17, 2600], 4, seed=7).check()
     Case(torch, cdt, dtype, 0, 128, 4, 1, [9001], 3, seed=8).check()
 
 
-@pytest.mark.parametrize("cdt,dtype", ALL[:2])
+@pytest.mark.parametrize("cdt,dtype", ALL[:3])
 @pytest.mark.parametrize("scale,q_std", [(0.5, 1.0), (0.0, 6.0), (0.0, 0.01)])
 def test_scales_and_sharp_rows(torch, cdt, dtype, scale, q_std):
     Case(torch, cdt, dtype, 16, 128, 4, 2, [300, 40], 5, seed=9, scale=scale, q_std=q_std).check()
+
+
+@pytest.mark.parametrize("path", [0, 1])
+@pytest.mark.parametrize("page", [0, 32])
+@pytest.mark.parametrize("codes,least", [(256, 2.0 ** -10), (8, 8.0)])  # all; 0 and the subnormal ones
+def test_every_code_of_an_8_bit_cache(torch, path, page, codes, least):
+    c = Case(torch, sp.SP_E4M3, sp.SP_BF16, page, 128, 8, 2, [300, 130, 77], 5, path=path, seed=17)
+    g = torch.Generator(device="cuda").manual_seed(17)
+    for pool, scale in ((c.cache.k, c.cache.ks), (c.cache.v, c.cache.vs)):
+        x = torch.randint(0, codes, pool.shape, generator=g, device="cuda", dtype=torch.int32)
+        if codes == 8:
+            x += 128 * torch.randint(0, 2, pool.shape, generator=g, device="cuda", dtype=torch.int32)
+        pool.view(torch.uint8).copy_(torch.where((x & 127) == 127, 0, x).to(torch.uint8))
+        scale.copy_(least * (1 + 7 * torch.rand(scale.shape, generator=g, device="cuda")))
+    c.check()
+
+
+@pytest.mark.parametrize("path", [0, 1])
+@pytest.mark.parametrize("which", ["k", "v"])
+def test_nan_codes_reach_their_sequence_alone(torch, path, which):
+    lens = [70, 200]
+    a = Case(torch, sp.SP_E4M3, sp.SP_BF16, 16, 128, 4, 2, lens, 3, path=path, seed=18)
+    ga = a.forward().backward()
+    b = Case(torch, sp.SP_E4M3, sp.SP_BF16, 16, 128, 4, 2, lens, 3, path=path, seed=18)
+    b.forward()
+    getattr(b.cache, which).view(torch.uint8)[b.cache._at(0, [50])[0], 0, b.cache._at(0, [50])[2], 3] = 0xff
+    gb = b.backward()
+    assert bool(gb[0][:3].view(3, 4, 128)[:, :2].isnan().any(-1).all())   # the heads of kv head 0
+    assert torch.equal(gb[0][:3].view(3, 4, 128)[:, 2:], ga[0][:3].view(3, 4, 128)[:, 2:])
+    assert torch.equal(gb[0][3:], ga[0][3:])
+    for x, y in zip(ga[1:], gb[1:]):
+        assert torch.equal(x, y)
 
 
 @pytest.mark.parametrize("cdt,dtype", ALL[:3])

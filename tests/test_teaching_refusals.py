@@ -152,7 +152,7 @@ def test_attention_backward():
               call(tree_dims(dtype=sp.SP_E4M3)), call(tree_dims(path=3)), call(tree_dims(shared=2)), call(tree_dims(scale=-1.0)),
               call(tree_dims(q=100)), call(tree_dims(k=259)), call(cache=tree_cache(dtype=5))]
     assert answers(calls) == [BAD] * len(calls)
-    refused = [call(tree_dims(path=2, dtype=sp.SP_F32)), call(tree_dims(path=2), tree_cache(sp.SP_E4M3)),
+    refused = [call(tree_dims(path=2, dtype=sp.SP_F32)), call(tree_dims(path=2, dtype=sp.SP_F32), tree_cache(sp.SP_E4M3)),
                call(tree_dims(path=2), tree_cache(sp.SP_F32)), call(tree_dims(path=2), tree_cache(dh=64)),
                call(cache=tree_cache(dh=96)), call(cache=tree_cache(page=8)), call(batch=70000)]
     assert answers(refused) == [NOT] * len(refused)
