@@ -639,8 +639,9 @@ SP_API size_t sp_attend_tree_backward_workspace_bytes(const sp_tree_dims *dims, 
  * arguments give the same bits.  What a row does not see has no influence (see sp_attend_tree); a
  * row that sees a NaN or an infinity may have gradients of NaN in all dims.
  * SP_F32, and shapes that the tensor cores do not take, are computed in fp32 on CUDA cores;
- * SP_BF16 over SP_BF16 caches of head_dim 128 (batch <= 2048) on tensor cores, with weights and their
- * gradients rounded to bf16 as operands of products with fp32 sums. */
+ * SP_BF16 over SP_BF16 and SP_E4M3 caches of head_dim 128 (batch <= 2048) on tensor cores, with weights and
+ * their gradients rounded to bf16 as operands of products with fp32 sums; 8-bit codes are operands as they
+ * are, their scales enter the scores and gradients in fp32. */
 SP_API sp_status sp_attend_tree_backward(sp_stream stream, const sp_tree_dims *dims, const sp_token_cache *cache,
                                          int batch, const int *d_seq_ids, const int *d_seq_lens, const uint64_t *d_mask,
                                          const int *d_n_nodes, const void *d_q, const void *d_k_new,

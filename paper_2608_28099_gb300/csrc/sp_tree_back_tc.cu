@@ -1,5 +1,5 @@
 // The cache's part of the backward pass of tree attention (sp_tree_back.cu) on tcgen05 tensor
-// cores: head_dim 128, bf16 rows and cache.  Per key tile of 128 cached tokens and block of up to 128
+// cores: head_dim 128, bf16 rows, bf16 or 8-bit cache.  Per key tile of 128 cached tokens and block of up to 128
 // query rows of a kv head, rows on the MMA's M side:
 //   S = Q K^T, dP = dO V^T   128 x 128 each, Q and dO in TMEM, K and V in shared memory
 //   ds = p (dP - D)          p = exp(scale S - lse), a row a thread, written as bf16 over dP in TMEM
@@ -24,6 +24,10 @@
 // Short sequences are segment ends, 8 to 9 us of latencies one after another in warps 8-11 (200 sequences
 // of 50 to 600 tokens: 111 us, 39 by bytes; 128 of 20 to 100: 50).  One sequence of 2048 tokens, 8 rows: 14.6 us,
 // of which 5 are the second kernel and its launch.
+// 8-bit caches: 356 and 384 us for the same (7330 and 3250 on CUDA cores), 3.3 us a tile, no unit above 40 %: a
+// tile's codes pass through one warp an operand (without their conversion 279 and 299, without the scales'
+// products 336 and 370; two warps an operand, with 640 threads, 383 and 409; conversion by integer
+// instructions 403 and 442).
 // ds as a sum of two bf16 would halve its part of dQ's error (0.0031 -> 0.0025 of its norm) for 250 instead
 // of 189 us.
 #include <string.h>
@@ -39,7 +43,8 @@ namespace {
 
 constexpr int TILE = 128;
 constexpr int SLOT = TILE * DH * 2;             // K or V of a tile, 32 KB
-constexpr int SCALES = 2 * TILE * 4, RAW = TILE * DH + SCALES;  // a tile's scales; 8-bit codes of K or V with them
+constexpr int SCALES = 3 * TILE * 4;            // a tile's scales: of K times the scores' factor, of K, of V
+constexpr int RAW = TILE * DH + 2 * TILE * 4;   // 8-bit codes of K or V, with K's the scales of both
 constexpr int LD = DH + 8, STAGE_ROW = LD * 2;  // a staged row of queries or output gradients: elements, bytes
 constexpr int MAX_NODES = 16;                   // most nodes whose products are formed here
 constexpr int ROWS = 128;                       // most rows of a block
@@ -542,7 +547,7 @@ out:
     if (__any_sync(0xffffffffu, bad) && lane == 0 && a.status) atomicOr(a.status, SP_DEV_BAD_PAGE);
 }
 // Codes of K (or of V) to bf16 in that operand's ring, K's tiles with their scales.
-__device__ __forceinline__ void convert_codes(bool is_v, int n_tiles, Bars *bars, const Layout &lay, uint8_t *smem, volatile int *abort,
+__device__ __forceinline__ void convert_codes(bool is_v, float scale, int n_tiles, Bars *bars, const Layout &lay, uint8_t *smem, volatile int *abort,
                                               int lane) {
     const int r0 = lane >> 3, c = lane & 7;
     Ring rr(lay.nr), rg(is_v ? lay.nv : lay.nk);
@@ -558,8 +563,10 @@ __device__ __forceinline__ void convert_codes(bool is_v, int n_tiles, Bars *bars
         if (!is_v) {
             const float4 *from = (const float4 *)(raw + TILE * DH);
             float4 *to = (float4 *)(smem + lay.off_sc + rg.slot * SCALES);
-            to[lane] = from[lane];
-            to[32 + lane] = from[32 + lane];
+            const float4 k = from[lane];
+            to[lane] = make_float4(k.x * scale, k.y * scale, k.z * scale, k.w * scale);
+            to[32 + lane] = k;
+            to[64 + lane] = from[32 + lane];
         }
         uint4 next[4];
         const auto load = [&](int i) {
@@ -706,7 +713,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                     st = make_float2(at[0], at[1]);
                 }
                 // the tile's scales, there with its keys, which stay until its dQ is formed
-                const float4 *ks = (const float4 *)((const float *)(smem + lay.off_sc) + rs.slot * 2 * TILE + c0), *vs = ks + TILE / 4;
+                const float4 *kf = (const float4 *)(smem + lay.off_sc + rs.slot * SCALES + c0 * 4), *ks = kf + TILE / 4, *vs = ks + TILE / 4;
                 if (EIGHT) ok = wait_warp(&bars->k_full[rs.slot], rs.ph, abort);
                 if (!ok) break;
                 const int n_tok = left - i * TILE;
@@ -719,12 +726,14 @@ __global__ void __launch_bounds__(THREADS, 1)
                     if constexpr (EIGHT) {
 #pragma unroll
                         for (int e = 0; e < 64; e += 4) {
-                            const float4 f = ks[e / 4];
-                            s[e] *= f.x, s[e + 1] *= f.y, s[e + 2] *= f.z, s[e + 3] *= f.w;
+                            const float4 f = kf[e / 4];
+                            s[e] = fast_exp2(fmaf(s[e], f.x, -st.x)), s[e + 1] = fast_exp2(fmaf(s[e + 1], f.y, -st.x));
+                            s[e + 2] = fast_exp2(fmaf(s[e + 2], f.z, -st.x)), s[e + 3] = fast_exp2(fmaf(s[e + 3], f.w, -st.x));
                         }
-                    }
+                    } else {
 #pragma unroll
-                    for (int e = 0; e < 64; ++e) s[e] = fast_exp2(fmaf(s[e], a.scale_log2, -st.x));
+                        for (int e = 0; e < 64; ++e) s[e] = fast_exp2(fmaf(s[e], a.scale_log2, -st.x));
+                    }
                     tc_fence_before();
                 }
                 arrive_warp(&bars->s_read, lane);  // the next scores may be formed
@@ -856,7 +865,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
     } else if (EIGHT && warp >= K_WARP) {
         if (warp == COPY_WARP) copy_codes(a, sh, sids, lens, n_tiles, g, bars, lay, smem, abort, lane);
-        else convert_codes(warp == V_WARP, n_tiles, bars, lay, smem, abort, lane);
+        else convert_codes(warp == V_WARP, a.scale_log2, n_tiles, bars, lay, smem, abort, lane);
     } else if (!EIGHT && (warp == K_WARP || warp == V_WARP)) {
         // ------------------------------------------------------------ K and V
         const bool is_v = warp == V_WARP;
