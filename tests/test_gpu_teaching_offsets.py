@@ -65,12 +65,12 @@ def test_a_head_of_more_than_2_31_elements(torch):
     assert bool(((dh.double() - exact).abs() <= size * (2 * off + 2.0 ** -7) + exact.abs() * 2.0 ** -8).all())
 
 
-@pytest.mark.parametrize("cdt,dtype", [(sp.SP_BF16, sp.SP_BF16), (sp.SP_F32, sp.SP_F32)])
+@pytest.mark.parametrize("cdt,dtype", [(sp.SP_BF16, sp.SP_BF16), (sp.SP_F32, sp.SP_F32), (sp.SP_E4M3, sp.SP_BF16)])
 def test_pages_behind_2_31_elements(torch, cdt, dtype):
     c = Case(torch, cdt, dtype, 16, 128, 4, 2, [100, 37], 3, seed=21)
     small = c.cache
     pages = 530000  # of 4096 elements
-    for name in ("k", "v"):
+    for name in ("k", "v") + (("ks", "vs") if cdt == sp.SP_E4M3 else ()):  # (an 8-bit cache's scales with its pages)
         old = getattr(small, name)
         big = torch.zeros((pages,) + tuple(old.shape[1:]), dtype=old.dtype, device="cuda")
         big[pages - len(old):] = old
@@ -81,16 +81,17 @@ def test_pages_behind_2_31_elements(torch, cdt, dtype):
     c.check()
 
 
-def test_a_batch_that_fills_the_tables(torch):
+@pytest.mark.parametrize("cdt,hq,N", [(sp.SP_BF16, 2, 2), (sp.SP_E4M3, 2, 2), (sp.SP_E4M3, 16, 9)])
+def test_a_batch_that_fills_the_tables(torch, cdt, hq, N):
     rng = np.random.default_rng(3)
     lens = rng.integers(0, 40, 2048).tolist()
-    c = Case(torch, sp.SP_BF16, sp.SP_BF16, 16, 128, 2, 1, lens, 2, seed=22)
+    c = Case(torch, cdt, sp.SP_BF16, 16, 128, hq, 1, lens, N, path=2, seed=22)
     grads = c.forward().backward()
     assert c.status == 0
     for b in (0, 1, 777, 1500, 2046, 2047):
         want, lim, _, _ = c.reference(b)
         for g, w, m in zip(grads, want, lim):
-            got = g.view(2048, 2, -1)[b].cpu().double().view(w.shape)
+            got = g.view(2048, N, -1)[b].cpu().double().view(w.shape)
             assert bool(((got - w).abs() <= m).all())
 
 
