@@ -218,20 +218,27 @@ __global__ void __launch_bounds__(THREADS) vocab_finish_dh_kernel(const __grid_c
 
 // ---------------------------------------------------------------------------
 // Products on CUDA cores: C[m][n] = sum_k A(m, k) B(n, k), the operands through two buffers in shared
-// memory, the next ones' loads under way beside the products, 4 x 4 elements a thread, fp32 throughout;
-// dh's tiles split along K where they are few.  Tiles of 64 x 64 by 256 threads and 32 of K at a time, or
-// where these leave SMs idle (VocabArgs::tm) of 32 x 32 and 64 of K, whose quarters four groups of 64 threads
-// take and add up in order: a k-block of the first takes an SM 0.55 us of FMAs alone.
+// memory, the next ones' loads under way beside the products, fp32 throughout; dh's tiles split along K
+// where they are few.  Tiles of 64 x 64 and 32 of K at a time, 4 x 4 elements a thread, or where these leave SMs
+// idle (VocabArgs::tm) of 32 x 32 and 64 of K: a k-block of the first takes an SM 0.55 us of FMAs alone.
+// There dh and dW go by 4 x 4, four groups of 64 threads adding up a quarter of K each; the logits by 2 x 2, so that
+// they are the same sums, k after k, in every kernel: exp(l - lse) is only as good as the lse's logits and these agree
+// (by quarters: errors of 4e-6 instead of 6e-7 of the gradients' norm with another kernel's lse).
 enum { LOSS = 0, GRAD = 1, DH = 2, DW = 3 };
 
 template <int BM>
 struct Simt {
     static constexpr int BK = 2048 / BM, LOADS = BM * BK / THREADS;
-    static constexpr int PER_ROW = BM / 4, GROUP = PER_ROW * PER_ROW, GROUPS = THREADS / GROUP;  // threads of a tile
     struct Smem {
         float a[2][BK][BM + 4], b[2][BK][BM + 4];
         VocabRow rows[BM];
     };
+};
+// E x E elements a thread, a tile by GROUP threads.
+template <int KIND, int BM>
+struct Cut {
+    static constexpr int E = BM == 32 && (KIND == LOSS || KIND == GRAD) ? 2 : 4;
+    static constexpr int PER_ROW = BM / E, GROUP = PER_ROW * PER_ROW, GROUPS = THREADS / GROUP;
 };
 
 template <typename T, int KIND>
@@ -241,7 +248,8 @@ struct SimtA {
 template <typename T, int KIND, int BM>
 __device__ __forceinline__ void simt_tile(const VocabArgs &a, int v0, int n0, int m0, int split, typename Simt<BM>::Smem &s) {
     typedef Simt<BM> S;
-    constexpr int BK = S::BK, LOADS = S::LOADS, GROUPS = S::GROUPS;
+    typedef Cut<KIND, BM> C;
+    constexpr int BK = S::BK, LOADS = S::LOADS, GROUPS = C::GROUPS, E = C::E;
     const DhPlan plan = *a.count;
     const int count = plan.kept;
     const int piece = min(a.piece, a.V - v0);
@@ -256,8 +264,8 @@ __device__ __forceinline__ void simt_tile(const VocabArgs &a, int v0, int n0, in
         k_hi = min(K, k_lo + plan.per * BK);
         plane_rows = plan.m_tiles * BM;
     }
-    const int tid = threadIdx.x, group = tid / S::GROUP, at = tid % S::GROUP;
-    const int ty = at / S::PER_ROW, tx = at % S::PER_ROW;
+    const int tid = threadIdx.x, group = tid / C::GROUP, at = tid % C::GROUP;
+    const int ty = at / C::PER_ROW, tx = at % C::PER_ROW;
     if (KIND != DW) {
         if (tid < BM) s.rows[tid] = m0 + tid < count ? a.rows[m0 + tid] : VocabRow{0.f, 0.f, -1, 0};
         __syncthreads();
@@ -306,7 +314,7 @@ __device__ __forceinline__ void simt_tile(const VocabArgs &a, int v0, int n0, in
             pb[i] += BK * step_b;
         }
     };
-    float c[4][4] = {};
+    float c[E][E] = {};
     load(k_lo);
     int buf = 0;
     for (int k0 = k_lo; k0 < k_hi; k0 += BK, buf ^= 1) {
@@ -323,18 +331,24 @@ __device__ __forceinline__ void simt_tile(const VocabArgs &a, int v0, int n0, in
 #pragma unroll
         for (int kk = 0; kk < BK / GROUPS; ++kk) {
             const int k = group * (BK / GROUPS) + kk;
-            const float4 x = *(const float4 *)&s.a[buf][k][ty * 4], y = *(const float4 *)&s.b[buf][k][tx * 4];
-            const float xa[4] = {x.x, x.y, x.z, x.w}, yb[4] = {y.x, y.y, y.z, y.w};
+            float xa[E], yb[E];
+            if constexpr (E == 4) {
+                const float4 x = *(const float4 *)&s.a[buf][k][ty * 4], y = *(const float4 *)&s.b[buf][k][tx * 4];
+                xa[0] = x.x, xa[1] = x.y, xa[2] = x.z, xa[3] = x.w, yb[0] = y.x, yb[1] = y.y, yb[2] = y.z, yb[3] = y.w;
+            } else {
+                const float2 x = *(const float2 *)&s.a[buf][k][ty * 2], y = *(const float2 *)&s.b[buf][k][tx * 2];
+                xa[0] = x.x, xa[1] = x.y, yb[0] = y.x, yb[1] = y.y;
+            }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < E; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) c[i][j] += xa[i] * yb[j];
+                for (int j = 0; j < E; ++j) c[i][j] = fmaf(xa[i], yb[j], c[i][j]);
         }
     }
-    constexpr int MINE = 4 / GROUPS;  // rows of the tile that a thread is left with
+    constexpr int MINE = E / GROUPS;  // rows of the tile that a thread is left with
     if constexpr (GROUPS > 1) {       // row 4 ty + group of each thread's four, from all groups
-        float(*sum)[4][S::GROUP][4] = (float(*)[4][S::GROUP][4]) & s.a[0][0][0];
-        static_assert(sizeof(float) * GROUPS * 4 * S::GROUP * 4 <= sizeof s.a + sizeof s.b, "sums");
+        float(*sum)[4][C::GROUP][4] = (float(*)[4][C::GROUP][4]) & s.a[0][0][0];
+        static_assert(sizeof(float) * GROUPS * 4 * C::GROUP * 4 <= sizeof s.a + sizeof s.b, "sums");
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 4; ++i) *(float4 *)sum[group][i][at] = make_float4(c[i][0], c[i][1], c[i][2], c[i][3]);
@@ -349,31 +363,31 @@ __device__ __forceinline__ void simt_tile(const VocabArgs &a, int v0, int n0, in
     }
 #pragma unroll
     for (int i = 0; i < MINE; ++i) {
-        const int ml = ty * 4 + (GROUPS > 1 ? group : i), m = m0 + ml;
+        const int ml = ty * E + (GROUPS > 1 ? group : i), m = m0 + ml;
         if constexpr (KIND == LOSS) {
             // the threads of a row join their logits
             float mx = -INFINITY, l = 0.f;
             const int tgt = s.rows[ml].target;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int v = n0 + tx * 4 + j;
+            for (int j = 0; j < E; ++j) {
+                const int v = n0 + tx * E + j;
                 if (v >= N) c[i][j] = -INFINITY;
                 mx = fmaxf(mx, c[i][j]);
                 if (v == tgt && m < M) a.at[m] = c[i][j];
             }
 #pragma unroll
-            for (int o = S::PER_ROW / 2; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            for (int o = C::PER_ROW / 2; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
             const float mu = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) l += exp2f((c[i][j] - mu) * LOG2E);
+            for (int j = 0; j < E; ++j) l += exp2f((c[i][j] - mu) * LOG2E);
 #pragma unroll
-            for (int o = S::PER_ROW / 2; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+            for (int o = C::PER_ROW / 2; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
             if (tx == 0 && m < M) a.part[(size_t)m * a.parts + n0 / BM] = make_float2(mx, l);
         } else {
             if (m >= M) continue;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int n = n0 + tx * 4 + j;
+            for (int j = 0; j < E; ++j) {
+                const int n = n0 + tx * E + j;
                 if (n >= N) continue;
                 if constexpr (KIND == GRAD) {
                     const VocabRow r = s.rows[ml];
@@ -450,10 +464,13 @@ cudaError_t launch_vocab_finish_dh(const VocabArgs &a, cudaStream_t st) {
     return launch_k(vocab_finish_dh_kernel<bf16>, dim3(a.n), dim3(THREADS), 0, st, a);
 }
 
-// Tiles of 32 x 32 where 64 x 64 ones of the logits are fewer than two an SM.  Pieces of the vocabulary
+// Tiles of 32 x 32 where 64 x 64 ones of the logits are fewer than the SMs (fp32, forward and backward, us: 250 tokens
+// of 128 against 1000 rows 12 and 25, with 64 x 64 14 and 33; 100 of 512 against 2000 28 and 57, 33 and 56; 300 of
+// 512 against 2000, 160 tiles, 55 and 103, 48 and 107; 500 of 512 against 4000 100 and 273, 85 and 226, which
+// are 24 and 27 TFLOP/s, bound by reads of shared memory).  Pieces of the vocabulary
 // whose gradients take at most 64 MB (or 64 rows), in whole tiles.
 void plan_vocab_simt(VocabArgs *a, bool backward, int n_sm) {
-    a->tm = (long long)ceil_div(a->n, 64) * ceil_div(a->V, 64) < (backward ? 1ll : 2ll) * n_sm ? 32 : 64;
+    a->tm = (long long)ceil_div(a->n, 64) * ceil_div(a->V, 64) < n_sm ? 32 : 64;
     const int tm = a->tm;
     a->pad = a->n;
     a->pairs = 4 * n_sm;
