@@ -59,6 +59,7 @@ struct VocabArgs {
     int tm;                        // rows of a tile of dh (CUDA cores: rows and columns of any)
     int pad;                       // n rounded up to whole tiles
     int tn;                        // forward, tensor cores: vocabulary rows of a tile
+    int box;                       // tensor cores: rows of the tokens that a CTA copies a k-block (up to 128 tokens fewer)
     int direct;                    // forward, tensor cores, one tile of tokens: they are not counted off, row m
                                    // of the products is token m
     float2 *part;                  // forward: [n][parts] (max, sum of exponentials) of a piece of the vocabulary

@@ -158,7 +158,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     const uint32_t tmem = *tmem_slot;
     const int piece = min(a.piece, a.V - v0);
     const int tn = cols_of<KIND>(a);              // (a CTA holds half of B's rows)
-    const uint32_t stage_tx = KIND == LOSS ? 2 * HALF + (uint32_t)tn * BK * 2 : 2 * STAGE;  // both CTAs' bytes
+    // both CTAs' bytes; the logits of up to 128 tokens leave A's other rows as they are (nobody's rows of D)
+    const bool short_a = (KIND == LOSS || KIND == GRAD) && a.box < 128;
+    const uint32_t stage_tx = (short_a ? (uint32_t)a.box * BK * 2 : 2 * HALF) + (uint32_t)tn * BK * 2;
 
     if (warp == TMA && lane == 0) {
         // what is read again soon stays in L2, the vocabulary's rows of LOSS pass through
@@ -196,7 +198,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                 if (Ki::A_MN) {
                     tma_load_2d_pair(sa, &map_a, bar, ma, k, pol_a);
                     tma_load_2d_pair(sa + HALF / 2, &map_a, bar, ma + 64, k, pol_a);
-                } else {
+                } else if (!short_a || rank == 0) {
                     tma_load_2d_pair(sa, &map_a, bar, k, ma, pol_a);
                 }
                 if (Ki::B_MN) {
@@ -327,6 +329,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                 for (int c = 0; c < TN / 2; ++c) s4[c & 3] += fast_exp2((v[c] - mu) * LOG2E);
                 if (m < count) a.part[(size_t)m * a.parts + 2 * x.nt + half] = make_float2(mx, (s4[0] + s4[1]) + (s4[2] + s4[3]));
             } else {
+                // dh in one part goes where it belongs
+                const bool direct_dh = KIND == DH && t.splits == 1 && a.n_pieces == 1;
+                bf16 *dh_row = nullptr;
+                if (direct_dh && m < count) dh_row = (bf16 *)a.dh + (size_t)a.rows[m].token * a.hs;
                 ok = wait_acc();
                 if (!ok) break;
                 const uint32_t at = acc_at();
@@ -353,6 +359,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                         for (int j = 0; j < 4; ++j) to[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
                     } else if constexpr (KIND == DH) {
                         if (m >= count) continue;
+                        if (direct_dh) {
+                            bf16 *to = dh_row + c0 + c;
+#pragma unroll
+                            for (int j = 0; j < 32; j += 8) {
+                                if (c0 + c + j >= a.d) break;
+                                *(uint4 *)(to + j) = make_uint4(pack2_bf16(v[j], v[j + 1]), pack2_bf16(v[j + 2], v[j + 3]),
+                                                                pack2_bf16(v[j + 4], v[j + 5]), pack2_bf16(v[j + 6], v[j + 7]));
+                            }
+                            continue;
+                        }
                         float *to = a.acc + ((size_t)x.split * (t.m * TM) + m) * a.d + c0 + c;
 #pragma unroll
                         for (int j = 0; j < 32; j += 4) {
@@ -416,6 +432,7 @@ void plan_vocab_tc(VocabArgs *a, bool backward, int n_sm) {
     a->pad = ceil_div(a->n, TM) * TM;
     a->pairs = n_sm / 2 > 0 ? n_sm / 2 : 1;
     a->tn = TN;
+    a->box = a->n <= 128 ? ceil_div(a->n, 8) * 8 : 128;
     a->direct = !backward && a->n <= TM;
     if (a->direct) {
         // W is read once and bounds the call: tiles of the width whose rounds over the pairs read the fewest rows
@@ -442,7 +459,7 @@ void plan_vocab_tc(VocabArgs *a, bool backward, int n_sm) {
 // nothing fetches.  48 tokens against 32000 rows of 2560: 38 us with all 256 rows of the tile.)
 cudaError_t launch_vocab_loss_tc(const VocabArgs &a, cudaStream_t st) {
     CUtensorMap mh, mw;
-    if (!(a.direct ? encode_tile_bf16(&mh, a.h, a.d, a.n, a.hs, 128) : encode_tile_bf16(&mh, a.hc, a.d, a.n, a.d, 128)) ||
+    if (!(a.direct ? encode_tile_bf16(&mh, a.h, a.d, a.n, a.hs, a.box) : encode_tile_bf16(&mh, a.hc, a.d, a.n, a.d, 128)) ||
         !encode_tile_bf16(&mw, a.w, a.d, a.V, a.ws, a.tn / 2))
         return cudaErrorInvalidValue;
     return run<LOSS>(a, mh, mw, 0, st);
@@ -450,7 +467,7 @@ cudaError_t launch_vocab_loss_tc(const VocabArgs &a, cudaStream_t st) {
 
 cudaError_t launch_vocab_backward_tc(const VocabArgs &a, cudaStream_t st) {
     CUtensorMap mh, mw, mg, mwt, mgt, mht;
-    if (!encode_tile_bf16(&mh, a.hc, a.d, a.n, a.d, 128) || !encode_tile_bf16(&mw, a.w, a.d, a.V, a.ws, 128) ||
+    if (!encode_tile_bf16(&mh, a.hc, a.d, a.n, a.d, a.box) || !encode_tile_bf16(&mw, a.w, a.d, a.V, a.ws, 128) ||
         !encode_tile_bf16(&mg, a.grad, a.piece, a.pad, a.piece, 128) || !encode_tile_bf16(&mwt, a.w, a.d, a.V, a.ws, 64) ||
         !encode_tile_bf16(&mgt, a.grad, a.piece, a.pad, a.piece, 64) || !encode_tile_bf16(&mht, a.hc, a.d, a.n, a.d, 64))
         return cudaErrorInvalidValue;
