@@ -37,7 +37,10 @@ constexpr int TM = 256, TN = 256, BK = 64;       // a pair's tile; a CTA holds 1
                                                  // tiles of fewer columns (VocabArgs::tn)
 constexpr int HALF = 128 * BK * 2;               // a CTA's part of an operand's k-block, 16 KB
 constexpr int STAGE = 2 * HALF, STAGES = 6;
-constexpr int OFF_BAR = STAGES * STAGE, SMEM = OFF_BAR + 256 + 1024 /*align*/;
+constexpr int OFF_BAR = STAGES * STAGE, OFF_OUT = OFF_BAR + 256;
+constexpr int OUT_ROW = 64 + 16;                 // 32 bf16 of a row on their way out, padded
+template <int KIND>
+constexpr int SMEM = OFF_OUT + (KIND >= 2 ? 8 * 32 * OUT_ROW : 0) + 1024 /*align*/;
 constexpr int THREADS = 352;                     // warps 0-7 epilogue, 8 TMA, 9 MMA (rank 0), 10 TMEM
 constexpr int TMA = 8, MMA = 9, TMEM = 10, EPI_THREADS = 256;
 constexpr int TMEM_COLS = 2 * TN;
@@ -76,7 +79,7 @@ __device__ __forceinline__ int count_of(const VocabArgs &a) {
 }
 template <int KIND>
 __device__ __forceinline__ int cols_of(const VocabArgs &a) {
-    return KIND == LOSS ? a.tn : TN;
+    return KIND == LOSS || KIND == GRAD ? a.tn : TN;
 }
 template <int KIND>
 __device__ __forceinline__ Tiles tiles_of(const VocabArgs &a, int count, int piece) {
@@ -329,15 +332,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                 for (int c = 0; c < TN / 2; ++c) s4[c & 3] += fast_exp2((v[c] - mu) * LOG2E);
                 if (m < count) a.part[(size_t)m * a.parts + 2 * x.nt + half] = make_float2(mx, (s4[0] + s4[1]) + (s4[2] + s4[3]));
             } else {
-                // dh in one part goes where it belongs
-                const bool direct_dh = KIND == DH && t.splits == 1 && a.n_pieces == 1;
-                bf16 *dh_row = nullptr;
-                if (direct_dh && m < count) dh_row = (bf16 *)a.dh + (size_t)a.rows[m].token * a.hs;
+                // bf16 rows go out through shared memory, 64 bytes of a row by four lanes: dW's, and dh's where it
+                // belongs if it comes in one part
+                const bool rows_out = KIND == DW || (KIND == DH && t.splits == 1 && a.n_pieces == 1);
+                uint8_t *stage = smem + OFF_OUT + warp * 32 * OUT_ROW;
+                bf16 *const out = KIND == DW ? (bf16 *)a.dw : (bf16 *)a.dh;
+                long long out_row[4];
+                if (rows_out) {
+                    long long own = -1;
+                    if (KIND == DW && m < piece) own = (long long)(v0 + m) * a.ws;
+                    if (KIND == DH && m < count) own = (long long)a.rows[m].token * a.hs;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) out_row[i] = __shfl_sync(0xffffffffu, own, i * 8 + (lane >> 2));
+                }
                 ok = wait_acc();
                 if (!ok) break;
                 const uint32_t at = acc_at();
 #pragma unroll 1
-                for (int c = 0; c < TN / 2; c += 32) {
+                for (int c = 0; c < tn / 2; c += 32) {
                     float v[32];
                     __syncwarp();  // (rows that store nothing have skipped ahead)
                     tmem_ld32(at + c, v);
@@ -357,18 +369,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                         uint4 *to = (uint4 *)((bf16 *)a.grad + (size_t)m * a.piece + c0 + c);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) to[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-                    } else if constexpr (KIND == DH) {
-                        if (m >= count) continue;
-                        if (direct_dh) {
-                            bf16 *to = dh_row + c0 + c;
+                    } else if (rows_out) {
 #pragma unroll
-                            for (int j = 0; j < 32; j += 8) {
-                                if (c0 + c + j >= a.d) break;
-                                *(uint4 *)(to + j) = make_uint4(pack2_bf16(v[j], v[j + 1]), pack2_bf16(v[j + 2], v[j + 3]),
-                                                                pack2_bf16(v[j + 4], v[j + 5]), pack2_bf16(v[j + 6], v[j + 7]));
-                            }
-                            continue;
-                        }
+                        for (int j = 0; j < 32; j += 8)
+                            *(uint4 *)(stage + lane * OUT_ROW + j * 2) = make_uint4(pack2_bf16(v[j], v[j + 1]), pack2_bf16(v[j + 2], v[j + 3]),
+                                                                                    pack2_bf16(v[j + 4], v[j + 5]), pack2_bf16(v[j + 6], v[j + 7]));
+                        __syncwarp();
+                        const int col = c0 + c + (lane & 3) * 8;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (out_row[i] >= 0 && col < a.d)
+                                *(uint4 *)(out + out_row[i] + col) = *(const uint4 *)(stage + (i * 8 + (lane >> 2)) * OUT_ROW + (lane & 3) * 16);
+                    } else {
+                        if (m >= count) continue;
                         float *to = a.acc + ((size_t)x.split * (t.m * TM) + m) * a.d + c0 + c;
 #pragma unroll
                         for (int j = 0; j < 32; j += 4) {
@@ -379,15 +392,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                                 y.x += z.x, y.y += z.y, y.z += z.z, y.w += z.w;
                             }
                             *(float4 *)(to + j) = y;
-                        }
-                    } else {
-                        if (m >= piece) continue;
-                        bf16 *to = (bf16 *)a.dw + (size_t)(v0 + m) * a.ws + c0 + c;
-#pragma unroll
-                        for (int j = 0; j < 32; j += 8) {
-                            if (c0 + c + j >= a.d) break;
-                            *(uint4 *)(to + j) = make_uint4(pack2_bf16(v[j], v[j + 1]), pack2_bf16(v[j + 2], v[j + 3]),
-                                                            pack2_bf16(v[j + 4], v[j + 5]), pack2_bf16(v[j + 6], v[j + 7]));
                         }
                     }
                 }
@@ -410,14 +414,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
 template <int KIND>
 cudaError_t run(const VocabArgs &a, const CUtensorMap &ma, const CUtensorMap &mb, int v0, cudaStream_t st) {
     static bool known[MAX_DEVICES] = {};
-    const cudaError_t e = allow_smem(vocab_tc_kernel<KIND>, SMEM, known);
+    const cudaError_t e = allow_smem(vocab_tc_kernel<KIND>, SMEM<KIND>, known);
     if (e != cudaSuccess) return e;
     const int piece = a.V - v0 < a.piece ? a.V - v0 : a.piece;
     const long long m = KIND == DW ? ceil_div(piece, TM) : a.pad / TM;
-    const long long n = ceil_div(KIND == LOSS || KIND == GRAD ? piece : a.d, KIND == LOSS ? a.tn : TN);
+    const long long n = ceil_div(KIND == LOSS || KIND == GRAD ? piece : a.d, KIND == LOSS || KIND == GRAD ? a.tn : TN);
     const long long items = m * n * (KIND == DH ? 16 : 1);
     const int pairs = a.pairs;
-    return launch_k(vocab_tc_kernel<KIND>, dim3(2 * (items < pairs ? (unsigned)items : (unsigned)pairs)), dim3(THREADS), (size_t)SMEM,
+    return launch_k(vocab_tc_kernel<KIND>, dim3(2 * (items < pairs ? (unsigned)items : (unsigned)pairs)), dim3(THREADS), (size_t)SMEM<KIND>,
                     st, ma, mb, a, v0);
 }
 
@@ -434,12 +438,13 @@ void plan_vocab_tc(VocabArgs *a, bool backward, int n_sm) {
     a->tn = TN;
     a->box = a->n <= 128 ? ceil_div(a->n, 8) * 8 : 128;
     a->direct = !backward && a->n <= TM;
-    if (a->direct) {
-        // W is read once and bounds the call: tiles of the width whose rounds over the pairs read the fewest rows
-        // (32000 rows: 2 x 224 instead of 2 x 256 a pair)
+    if (a->n <= TM) {
+        // W is read once and bounds the logits: tiles of the width whose rounds over the pairs read the fewest rows
+        // (32000 rows: 2 x 224 instead of 2 x 256 a pair), a tile's ends costing some 64 of them; g's in whole k-blocks
+        // of dh's product (6364 rows of 4096, 48 tokens: 26 us with 256, 22 with 128; 67629 of 1888, 8 tokens: 57 and 64)
         long long least = 1ll << 62;
-        for (int tn = TN; tn >= 128; tn -= 32) {
-            const long long rows = ceil_div_ll(ceil_div(a->V, tn), a->pairs) * tn;
+        for (int tn = TN; tn >= 64; tn -= backward ? 64 : 32) {
+            const long long rows = ceil_div_ll(ceil_div(a->V, tn), a->pairs) * (tn + 64);
             if (rows < least) least = rows, a->tn = tn;
         }
     }
@@ -448,10 +453,10 @@ void plan_vocab_tc(VocabArgs *a, bool backward, int n_sm) {
     a->piece = tiles * a->tn;
     a->n_pieces = 1;
     if (!backward) return;
-    long long most = GRAD_BYTES / 2 / a->pad / TN;  // tiles of a piece
+    long long most = GRAD_BYTES / 2 / a->pad / a->tn;  // tiles of a piece
     if (most < 1) most = 1;
     a->n_pieces = (int)ceil_div_ll(tiles, most);
-    a->piece = ceil_div(tiles, a->n_pieces) * TN;
+    a->piece = ceil_div(tiles, a->n_pieces) * a->tn;
     a->n_pieces = ceil_div(a->V, a->piece);
 }
 
@@ -467,7 +472,7 @@ cudaError_t launch_vocab_loss_tc(const VocabArgs &a, cudaStream_t st) {
 
 cudaError_t launch_vocab_backward_tc(const VocabArgs &a, cudaStream_t st) {
     CUtensorMap mh, mw, mg, mwt, mgt, mht;
-    if (!encode_tile_bf16(&mh, a.hc, a.d, a.n, a.d, a.box) || !encode_tile_bf16(&mw, a.w, a.d, a.V, a.ws, 128) ||
+    if (!encode_tile_bf16(&mh, a.hc, a.d, a.n, a.d, a.box) || !encode_tile_bf16(&mw, a.w, a.d, a.V, a.ws, a.tn / 2) ||
         !encode_tile_bf16(&mg, a.grad, a.piece, a.pad, a.piece, 128) || !encode_tile_bf16(&mwt, a.w, a.d, a.V, a.ws, 64) ||
         !encode_tile_bf16(&mgt, a.grad, a.piece, a.pad, a.piece, 64) || !encode_tile_bf16(&mht, a.hc, a.d, a.n, a.d, 64))
         return cudaErrorInvalidValue;
