@@ -221,6 +221,7 @@ __global__ void __launch_bounds__(THREADS) tree_back_simt_kernel(const __grid_co
 #pragma unroll
         for (int d = 0; d < D; ++d) dq[r][d] = 0.f;
     }
+    const bool mine = row0 + warp * RW < a.R;  // (a warp without rows loads, and leaves shared memory to the others)
     bool bad = false;
     for (int t0 = t_lo; t0 < t_hi; t0 += TOK) {
         __syncthreads();
@@ -251,6 +252,7 @@ __global__ void __launch_bounds__(THREADS) tree_back_simt_kernel(const __grid_co
             for (int x = 0; x < 8; ++x) s.k[tt][e + x] = k[x], s.v[tt][e + x] = v[x];
         }
         __syncthreads();
+        if (!mine) continue;
         float x[RW] = {0.f, 0.f, 0.f, 0.f}, dp[RW] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
         for (int e = 0; e < DH; e += 4) {
