@@ -33,7 +33,7 @@ using namespace sm100;
 
 enum { LOSS = 0, GRAD = 1, DH = 2, DW = 3 };
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int TM = 256, TN = 256, BK = 64;       // a pair's tile; a CTA holds 128 x 256 of it.  LOSS may take
+constexpr int TM = 256, TN = 256, BK = 64;       // a pair's tile; a CTA holds 128 x 256 of it.  LOSS and GRAD may take
                                                  // tiles of fewer columns (VocabArgs::tn)
 constexpr int HALF = 128 * BK * 2;               // a CTA's part of an operand's k-block, 16 KB
 constexpr int STAGE = 2 * HALF, STAGES = 6;
@@ -438,15 +438,13 @@ void plan_vocab_tc(VocabArgs *a, bool backward, int n_sm) {
     a->tn = TN;
     a->box = a->n <= 128 ? ceil_div(a->n, 8) * 8 : 128;
     a->direct = !backward && a->n <= TM;
-    if (a->n <= TM) {
-        // W is read once and bounds the logits: tiles of the width whose rounds over the pairs read the fewest rows
-        // (32000 rows: 2 x 224 instead of 2 x 256 a pair), a tile's ends costing some 64 of them; g's in whole k-blocks
-        // of dh's product (6364 rows of 4096, 48 tokens: 26 us with 256, 22 with 128; 67629 of 1888, 8 tokens: 57 and 64)
-        long long least = 1ll << 62;
-        for (int tn = TN; tn >= 64; tn -= backward ? 64 : 32) {
-            const long long rows = ceil_div_ll(ceil_div(a->V, tn), a->pairs) * (tn + 64);
-            if (rows < least) least = rows, a->tn = tn;
-        }
+    // Tiles of the width whose rounds over the pairs read the fewest rows of W (48 tokens, 32000 rows: 2 x 224 instead
+    // of 2 x 256 a pair), a tile's ends costing some 64 of them; g's in whole k-blocks of dh's product (6364 rows of
+    // 4096, 48 tokens: 26 us with 256, 22 with 128; 67629 of 1888, 8 tokens: 57 and 64).
+    long long least = 1ll << 62;
+    for (int tn = TN; tn >= 64; tn -= backward ? 64 : 32) {
+        const long long rows = ceil_div_ll((long long)ceil_div(a->V, tn) * (a->pad / TM), a->pairs) * (tn + 64);
+        if (rows < least) least = rows, a->tn = tn;
     }
     const int tiles = ceil_div(a->V, a->tn);
     a->parts = 2 * tiles;
