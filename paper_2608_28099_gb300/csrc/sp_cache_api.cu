@@ -154,7 +154,7 @@ sp_status check_tree(const sp_tree_dims *d, const sp_token_cache *cache, int bat
                                         "and a batch of at most 2048");
     if (a->tensor && backward) plan_tree_back_tc(a, sm_count());
     else if (a->tensor) plan_tree_tc(a, sm_count());
-    else plan_tree_simt(a, sm_count());
+    else plan_tree_simt(a, (backward ? 2 : 1) * sm_count());  // (backward: shares half as long, see sp_tree_back.cu)
     return SP_OK;
 }
 

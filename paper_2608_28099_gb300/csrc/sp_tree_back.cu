@@ -27,10 +27,10 @@ struct RowSmem {
     float p[ROWS][MAX_N], ds[ROWS][MAX_N];
     uint64_t sees[ROWS];
 };
-template <int DH>
+template <int DH, int TW>
 struct CacheSmem {
-    float k[TOK][DH + 4], v[TOK][DH + 4];
-    float q[ROWS][DH], dout[ROWS][DH];
+    float k[TOK * TW][DH + 4], v[TOK * TW][DH + 4];
+    float q[ROWS / TW][DH], dout[ROWS / TW][DH];
 };
 
 __device__ __forceinline__ float warp_sum(float x) {
@@ -41,6 +41,10 @@ __device__ __forceinline__ float warp_sum(float x) {
 __device__ __forceinline__ void load_elems(const void *p, int dtype, size_t e, float (&v)[8]) {
     if (dtype == SP_F32) load8((const float *)p + e, v);
     else load8((const bf16 *)p + e, v);
+}
+__device__ __forceinline__ void store8(float *p, const float (&v)[8]) {
+    *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]);
+    *(float4 *)(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
 }
 __device__ __forceinline__ void store_elem(void *p, int dtype, size_t e, float v) {
     if (dtype == SP_F32) ((float *)p)[e] = v;
@@ -185,24 +189,28 @@ __global__ void __launch_bounds__(THREADS) tree_back_rows_kernel(const __grid_co
 }
 
 // ---------------------------------------------------------------------------
-// A block takes 32 rows and a share of a sequence's cached tokens, as the forward kernel does.
-template <int DH>
+// A block takes up to 32 / TW rows and a share of a sequence's cached tokens, four rows and 32 of TW times 32
+// tokens a warp, so that few rows leave fewer warps idle; shares of a sequence for eight blocks an SM.  Bound by the
+// latency of a tile's look-up, loads and products one after another: 40 sequences of 596 to 1988 tokens in 64-token
+// pages, 8 kv heads of 128 fp32 dims: 4 rows 289 us (375 with TW = 1, 340 with longer shares), 32 rows 577 (654). The next
+// tile's loads in registers beside the products take two of three blocks of an SM: 388 and 684.
+template <int DH, int TW>
 __global__ void __launch_bounds__(THREADS) tree_back_simt_kernel(const __grid_constant__ TreeBackArgs args) {
     extern __shared__ __align__(16) uint8_t smem_raw[];
-    CacheSmem<DH> &s = *(CacheSmem<DH> *)smem_raw;
+    CacheSmem<DH, TW> &s = *(CacheSmem<DH, TW> *)smem_raw;
     const TreeArgs &a = args.t;
-    constexpr int C = DH / 8, D = DH / 32;
+    constexpr int C = DH / 8, D = DH / 32, RWARPS = WARPS / TW, MINE = ROWS / TW, TILE = TOK * TW;
     pdl_wait();
     pdl_trigger();
     const int hv = blockIdx.y, g = hv / a.n_rb, rb = hv - g * a.n_rb, b = blockIdx.z, split = blockIdx.x;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rw = warp % RWARPS, tg = warp / RWARPS;
     int *status = threadIdx.x == 0 && hv == 0 && split == 0 ? a.status : nullptr;
     const SeqRef sq = resolve_seq(a.seq_ids, a.seq_lens, 0, b, a.cache.kv.n_seqs, a.most_len, status);
     const int n = tree_nodes(a, b, nullptr);
     const int t_lo = (int)min((long long)sq.len, (long long)split * a.split_tokens);
     const int t_hi = t_lo + min(a.split_tokens, sq.len - t_lo);
     const int row0 = rb * a.rb_rows;
-    for (int i = threadIdx.x; i < ROWS * C; i += THREADS) {
+    for (int i = threadIdx.x; i < MINE * C; i += THREADS) {
         const int r = i / C, e = (i - r * C) * 8, rr = row0 + r;
         float q[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, go[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (rr < a.R && rr / a.G < n) {
@@ -216,16 +224,16 @@ __global__ void __launch_bounds__(THREADS) tree_back_simt_kernel(const __grid_co
     float2 stat[RW];
 #pragma unroll
     for (int r = 0; r < RW; ++r) {
-        const int rr = row0 + warp * RW + r;
+        const int rr = row0 + rw * RW + r;
         stat[r] = rr < a.R ? args.stat[((size_t)b * a.Hkv + g) * a.R + rr] : make_float2(INFINITY, 0.f);
 #pragma unroll
         for (int d = 0; d < D; ++d) dq[r][d] = 0.f;
     }
-    const bool mine = row0 + warp * RW < a.R;  // (a warp without rows loads, and leaves shared memory to the others)
+    const bool mine = row0 + rw * RW < a.R;  // (a warp without rows loads, and leaves shared memory to the others)
     bool bad = false;
-    for (int t0 = t_lo; t0 < t_hi; t0 += TOK) {
+    for (int t0 = t_lo; t0 < t_hi; t0 += TILE) {
         __syncthreads();
-        for (int i = threadIdx.x; i < TOK * C; i += THREADS) {
+        for (int i = threadIdx.x; i < TILE * C; i += THREADS) {
             const int tt = i / C, e = (i - tt * C) * 8, t = t0 + tt;
             float k[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             long long row;
@@ -248,23 +256,23 @@ __global__ void __launch_bounds__(THREADS) tree_back_simt_kernel(const __grid_co
                     bad = true;
                 }
             }
-#pragma unroll
-            for (int x = 0; x < 8; ++x) s.k[tt][e + x] = k[x], s.v[tt][e + x] = v[x];
+            store8(&s.k[tt][e], k);
+            store8(&s.v[tt][e], v);
         }
         __syncthreads();
-        if (!mine) continue;
+        const int here = min(TOK, t_hi - t0 - tg * TOK);
+        if (!mine || here <= 0) continue;
         float x[RW] = {0.f, 0.f, 0.f, 0.f}, dp[RW] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
         for (int e = 0; e < DH; e += 4) {
-            const float4 k = *(const float4 *)&s.k[lane][e], v = *(const float4 *)&s.v[lane][e];
+            const float4 k = *(const float4 *)&s.k[tg * TOK + lane][e], v = *(const float4 *)&s.v[tg * TOK + lane][e];
 #pragma unroll
             for (int r = 0; r < RW; ++r) {
-                const float4 q = *(const float4 *)&s.q[warp * RW + r][e], go = *(const float4 *)&s.dout[warp * RW + r][e];
+                const float4 q = *(const float4 *)&s.q[rw * RW + r][e], go = *(const float4 *)&s.dout[rw * RW + r][e];
                 x[r] += q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w;
                 dp[r] += go.x * v.x + go.y * v.y + go.z * v.z + go.w * v.w;
             }
         }
-        const int here = min(TOK, t_hi - t0);
 #pragma unroll
         for (int r = 0; r < RW; ++r) {
             const float p = lane < here ? exp2f(x[r] * a.scale_log2 - stat[r].x) : 0.f;
@@ -272,46 +280,78 @@ __global__ void __launch_bounds__(THREADS) tree_back_simt_kernel(const __grid_co
         }
 #pragma unroll 4
         for (int y = 0; y < here; ++y) {
-            float k[D];
+            float kd[D];
 #pragma unroll
-            for (int d = 0; d < D; ++d) k[d] = s.k[y][lane + 32 * d];
+            for (int d = 0; d < D; ++d) kd[d] = s.k[tg * TOK + y][lane + 32 * d];
 #pragma unroll
             for (int r = 0; r < RW; ++r) {
                 const float w = __shfl_sync(0xffffffffu, x[r], y);
 #pragma unroll
-                for (int d = 0; d < D; ++d) dq[r][d] += w * k[d];
+                for (int d = 0; d < D; ++d) dq[r][d] += w * kd[d];
             }
         }
     }
     if (bad && a.status) atomicOr(a.status, SP_DEV_BAD_PAGE);
     const size_t slot = ((size_t)b * gridDim.y + hv) * a.n_splits + split;
+    if constexpr (TW > 1) {  // the token groups' sums, added in their order
+        float(*sum)[MINE][DH] = (float(*)[MINE][DH])smem_raw;
+        static_assert(sizeof(float) * TW * MINE * DH <= sizeof s.k, "sums");
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < RW; ++r)
+#pragma unroll
+            for (int d = 0; d < D; ++d) sum[tg][rw * RW + r][lane + 32 * d] = dq[r][d];
+        __syncthreads();
+        if (tg) return;
+#pragma unroll
+        for (int w = 1; w < TW; ++w)
+#pragma unroll
+            for (int r = 0; r < RW; ++r)
+#pragma unroll
+                for (int d = 0; d < D; ++d) dq[r][d] += sum[w][rw * RW + r][lane + 32 * d];
+    }
 #pragma unroll
     for (int r = 0; r < RW; ++r) {
-        if (row0 + warp * RW + r >= a.R) continue;
+        if (row0 + rw * RW + r >= a.R) continue;
 #pragma unroll
-        for (int d = 0; d < D; ++d) a.part_o[(slot * a.rb_rows + warp * RW + r) * DH + lane + 32 * d] = dq[r][d];
+        for (int d = 0; d < D; ++d) a.part_o[(slot * a.rb_rows + rw * RW + r) * DH + lane + 32 * d] = dq[r][d];
     }
 }
 
-// dq: the nodes' part and the shares' parts, a warp a row, in share order.
-template <int DH>
+// dq: the nodes' part and the shares' parts in share order, a warp a row, or (WIDE: many shares) a block a row
+// whose warps take a run of shares each.
+constexpr int MANY_SHARES = 16;
+template <int DH, bool WIDE>
 __global__ void __launch_bounds__(THREADS) tree_back_sum_kernel(const __grid_constant__ TreeBackArgs args) {
     const TreeArgs &a = args.t;
     constexpr int D = DH / 32;
+    __shared__ float sums[WARPS][DH];
     pdl_wait();
     pdl_trigger();
-    const int lane = threadIdx.x & 31;
-    const long long w = (long long)blockIdx.x * WARPS + (threadIdx.x >> 5);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long long w = WIDE ? blockIdx.x : (long long)blockIdx.x * WARPS + warp;
     if (w >= (long long)a.B * a.Hkv * a.R) return;
     const int rr = (int)(w % a.R), g = (int)(w / a.R % a.Hkv), b = (int)(w / a.R / a.Hkv);
     const int rb = rr / a.rb_rows;
     const size_t part0 = ((((size_t)b * a.Hkv + g) * a.n_rb + rb) * a.n_splits) * a.rb_rows + (rr - rb * a.rb_rows);
+    const int per = WIDE ? ceil_div(a.n_splits, WARPS) : a.n_splits, lo = WIDE ? warp * per : 0, hi = min(a.n_splits, lo + per);
     float dq[D];
 #pragma unroll
-    for (int d = 0; d < D; ++d) dq[d] = args.dq_new[(size_t)w * DH + lane + 32 * d];
-    for (int sp = 0; sp < a.n_splits; ++sp)
+    for (int d = 0; d < D; ++d) dq[d] = !WIDE || warp == 0 ? args.dq_new[(size_t)w * DH + lane + 32 * d] : 0.f;
+#pragma unroll 8
+    for (int sp = lo; sp < hi; ++sp)
 #pragma unroll
         for (int d = 0; d < D; ++d) dq[d] += a.part_o[(part0 + (size_t)sp * a.rb_rows) * DH + lane + 32 * d];
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) sums[warp][lane + 32 * d] = dq[d];
+        __syncthreads();
+        if (warp) return;
+#pragma unroll
+        for (int i = 1; i < WARPS; ++i)
+#pragma unroll
+            for (int d = 0; d < D; ++d) dq[d] += sums[i][lane + 32 * d];
+    }
     const bool live = args.stat[w].x != INFINITY;
 #pragma unroll
     for (int d = 0; d < D; ++d)
@@ -325,16 +365,23 @@ cudaError_t run_rows(const TreeBackArgs &a, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     return launch_k(tree_back_rows_kernel<DH>, dim3(a.t.Hkv, a.t.B), dim3(THREADS), sizeof(RowSmem<DH>), st, a);
 }
-template <int DH>
-cudaError_t run_simt(const TreeBackArgs &a, cudaStream_t st) {
+template <int DH, int TW>
+cudaError_t run_cache(const TreeBackArgs &a, cudaStream_t st) {
     static bool known[MAX_DEVICES] = {};
-    cudaError_t e = allow_smem(tree_back_simt_kernel<DH>, (int)sizeof(CacheSmem<DH>), known);
+    constexpr int bytes = (int)sizeof(CacheSmem<DH, TW>);
+    const cudaError_t e = allow_smem(tree_back_simt_kernel<DH, TW>, bytes, known);
     if (e != cudaSuccess) return e;
     const TreeArgs &t = a.t;
-    e = launch_k(tree_back_simt_kernel<DH>, dim3(t.n_splits, t.Hkv * t.n_rb, t.B), dim3(THREADS), sizeof(CacheSmem<DH>), st, a);
+    return launch_k(tree_back_simt_kernel<DH, TW>, dim3(t.n_splits, t.Hkv * t.n_rb, t.B), dim3(THREADS), (size_t)bytes, st, a);
+}
+template <int DH>
+cudaError_t run_simt(const TreeBackArgs &a, cudaStream_t st) {
+    const TreeArgs &t = a.t;
+    const cudaError_t e = t.R <= ROWS / 2 ? run_cache<DH, 2>(a, st) : run_cache<DH, 1>(a, st);
     if (e != cudaSuccess) return e;
     const long long rows = (long long)t.B * t.Hkv * t.R;
-    return launch_k(tree_back_sum_kernel<DH>, dim3((unsigned)ceil_div_ll(rows, WARPS)), dim3(THREADS), 0, st, a);
+    if (t.n_splits > MANY_SHARES) return launch_k(tree_back_sum_kernel<DH, true>, dim3((unsigned)rows), dim3(THREADS), 0, st, a);
+    return launch_k(tree_back_sum_kernel<DH, false>, dim3((unsigned)ceil_div_ll(rows, WARPS)), dim3(THREADS), 0, st, a);
 }
 
 }  // namespace
