@@ -8,7 +8,7 @@
 // registers, so that heads that share a kv head are added in one order), and the cache's part on
 // CUDA cores in fp32 for the shapes and types that the tensor-core kernel does not take.  Bound by
 // shared-memory reads, as the forward kernel is: 64 sequences of 1024 to 8192 tokens, 16 rows, heads of
-// 128 bf16 dims 5775 us (214 on tensor cores), 17 to 20 TFLOP/s.
+// 128 bf16 dims 5475 us (214 on tensor cores), 17 to 20 TFLOP/s.
 #include "sp_cache.cuh"
 
 namespace sp {

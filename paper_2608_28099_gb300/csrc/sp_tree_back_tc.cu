@@ -16,18 +16,18 @@
 // elsewhere; 8-bit caches: 15 copies the codes, which 13 and 14 turn into bf16).  TMEM: S, dP, dQ, Q, dO in all 512 columns.  Every wait is time-limited
 // (SP_DEV_TIMEOUT).
 //
-// What bounds it: HBM for long sequences.  Eight of 32768 tokens, 40 heads (80 rows a kv head): 182 us,
-// 5.9 TB/s; 64 of 1024 to 8192, 32 heads, 16 rows each: 214 to 229 us, 5.5 to 5.8 TB/s.  A tile's chain is
-// dP (8 MMAs) -> ds -> dQ (8 MMAs), the next tile's S beside ds; an MMA with A in TMEM takes
-// as long for 64 tokens as for 128, which is why tiles have 128 tokens (64: 217 instead of 201 us for the eight,
-// with two tiles under way), and Q and dO lie in TMEM (in shared memory 262 instead of 227, at 64 tokens).
+// What bounds it: HBM for long sequences.  Eight of 32768 tokens, 40 heads, 16 nodes (80 rows a kv head):
+// 176 to 184 us, 5.9 TB/s; 64 of 1024 to 8192, 32 heads, 16 nodes: 210 to 226 us, 5.5 to 5.8 TB/s.  A tile's chain is
+// dP (8 MMAs) -> ds -> dQ (8 MMAs), the next tile's S beside ds; an MMA with A in TMEM takes as long for 64
+// tokens as for 128, which is why tiles have 128 tokens (64: 217 instead of 201 us for the eight, with two tiles
+// under way), and Q and dO lie in TMEM (in shared memory 262 instead of 227, at 64 tokens).
 // Short sequences are segment ends, 8 to 9 us of latencies one after another in warps 8-11 (200 sequences
-// of 50 to 600 tokens: 111 us, 39 by bytes; 128 of 20 to 100: 50).  One sequence of 2048 tokens, 8 rows: 14.6 us,
-// of which 5 are the second kernel and its launch.
-// 8-bit caches: 356 and 384 us for the same (7330 and 3250 on CUDA cores), 3.3 us a tile, no unit above 40 %: a
-// tile's codes pass through one warp an operand (without their conversion 279 and 299, without the scales'
-// products 336 and 370; two warps an operand, with 640 threads, 383 and 409; conversion by integer
-// instructions 403 and 442).
+// of 50 to 600 tokens: 111 us, 39 by bytes; 128 of 20 to 100: 50).  One sequence of 2048 tokens, 8 nodes: 14.6
+// us, of which 5 are the second kernel and its launch.
+// 8-bit caches: 355 us for the eight, 384 for 64 of 1024 to 8192 with 4 nodes (5980 and 1790 on CUDA cores), 3.3
+// us a tile, no unit above 40 %: a tile's codes pass through one warp an operand (without their conversion
+// 279 and 299, without the scales' products 336 and 370; two warps an operand, with 640 threads, 383 and 409;
+// conversion by integer instructions 403 and 442).
 // ds as a sum of two bf16 would halve its part of dQ's error (0.0031 -> 0.0025 of its norm) for 250 instead
 // of 189 us.
 #include <string.h>
