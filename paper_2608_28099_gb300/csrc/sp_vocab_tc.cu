@@ -42,7 +42,7 @@ constexpr int OUT_ROW = 64 + 16;                 // 32 bf16 of a row on their wa
 template <int KIND>
 constexpr int SMEM = OFF_OUT + (KIND >= 2 ? 8 * 32 * OUT_ROW : 0) + 1024 /*align*/;
 constexpr int THREADS = 352;                     // warps 0-7 epilogue, 8 TMA, 9 MMA (rank 0), 10 TMEM
-constexpr int TMA = 8, MMA = 9, TMEM = 10, EPI_THREADS = 256;
+constexpr int EPI_WARPS = 8, TMA = 8, MMA = 9, TMEM = 10;
 constexpr int TMEM_COLS = 2 * TN;
 // LOSS adds its logits up over 1024 of K at a time: the tensor core cuts what falls below an
 // accumulator's 24 bits, which over longer sums shows in the loss (of its norm, with the whole of K in
@@ -128,7 +128,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     uint64_t *full = (uint64_t *)(smem + OFF_BAR);  // rank 0's: both CTAs' copies
     uint64_t *empty = full + STAGES;
     uint64_t *acc_full = empty + STAGES;            // [2]
-    uint64_t *acc_empty = acc_full + 2;             // [2], rank 0's: one arrival a CTA
+    uint64_t *acc_empty = acc_full + 2;             // [2], rank 0's: one arrival an epilogue warp of both CTAs
     uint64_t *fin = acc_empty + 2;
     uint32_t *tmem_slot = (uint32_t *)(fin + 1);
     volatile int *abort = (volatile int *)(tmem_slot + 1);
@@ -143,7 +143,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&acc_full[i], 1);
-            mbar_init(&acc_empty[i], 2);
+            mbar_init(&acc_empty[i], 2 * EPI_WARPS);
         }
         mbar_init(fin, 1);
         *abort = 0;
@@ -260,7 +260,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         if (on) mma_commit_pair(fin);  // every MMA is finished before TMEM and shared memory go away
         __syncwarp();
         mbar_wait_drain(fin, 0);
-    } else if (warp < 8) {
+    } else if (warp < EPI_WARPS) {
         // a row a thread: warp w reads TMEM lanes 32 (w & 3).. and columns 128 (w >> 2)..
         const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane;
         pdl_wait();
@@ -275,9 +275,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         };
         const auto acc_at = [&]() { return tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)((n & 1) * TN + half * (tn / 2)); };
         const auto release_acc = [&]() {
+            // (a warp for itself: one whose wait ran out would leave the others at a barrier)
             tc_fence_before();
-            asm volatile("bar.sync 1, %0;" ::"n"(EPI_THREADS) : "memory");
-            if (threadIdx.x == 0) mbar_arrive_remote(map_rank(&acc_empty[n & 1], 0));
+            __syncwarp();
+            if (lane == 0) mbar_arrive_remote(map_rank(&acc_empty[n & 1], 0));
             ++n;
         };
         bool ok = true;
