@@ -723,10 +723,12 @@ SP_API sp_status sp_vocab_loss(sp_stream stream, const sp_vocab_dims *dims, cons
 
 /* Its gradients, the logits formed again a piece of the vocabulary at a time:
  *   g_v = grad_loss (exp(l_v - lse) - [v = target]),  grad_h = sum_v g_v w_v,  grad_w_v = sum g_v h
- *   d_lse          what the forward pass wrote; d_grad_loss [n] float (NULL: ones)
+ *   d_lse          what the forward pass wrote on the same dims (its logits are then the same sums);
+ *                  d_grad_loss [n] float (NULL: ones)
  *   d_grad_h       [n][d], zeros for tokens without a target
  *   d_grad_w       [V][d], or NULL: the head is frozen
- * On tensor cores g is rounded to bf16 as an operand (the target's p - 1 is formed before).  Sums
+ * On tensor cores g is rounded to bf16 as an operand (the target's p - 1 is formed before; its absolute error
+ * is that of a log sum rounded to fp32).  Sums
  * run in one order.  The gradients must not overlap each other or an input. */
 SP_API sp_status sp_vocab_loss_backward(sp_stream stream, const sp_vocab_dims *dims, const void *d_h, const void *d_w,
                                         const int *d_targets, const float *d_lse, const float *d_grad_loss,

@@ -44,12 +44,15 @@ constexpr int SMEM = OFF_OUT + (KIND >= 2 ? 8 * 32 * OUT_ROW : 0) + 1024 /*align
 constexpr int THREADS = 352;                     // warps 0-7 epilogue, 8 TMA, 9 MMA (rank 0), 10 TMEM
 constexpr int EPI_WARPS = 8, TMA = 8, MMA = 9, TMEM = 10;
 constexpr int TMEM_COLS = 2 * TN;
-// LOSS adds its logits up over 1024 of K at a time: the tensor core cuts what falls below an
+// LOSS and GRAD add their logits up over 1024 of K at a time: the tensor core cuts what falls below an
 // accumulator's 24 bits, which over longer sums shows in the loss (of its norm, with the whole of K in
-// one accumulator: 2.0e-6 at d = 2560, 2.7e-6 at 4096, 4.5e-6 at 8192; so: 0.9e-6).
-constexpr int LOSS_KB = 1024 / BK;
+// one accumulator: 2.0e-6 at d = 2560, 2.7e-6 at 4096, 4.5e-6 at 8192; so: 0.9e-6).  GRAD's logits are LOSS's, sum
+// for sum, whatever the tiles' width: exp(l - lse) - 1 of a token that is almost sure of its target is as good as
+// l and the log sum's logits agree (with the whole of K in one accumulator p - 1 of targets with logits of 30 was
+// off by 3.6e-4 at d = 4096 and 9.4e-4 at 8192; so: by the log sum's own rounding, 1e-6).
+constexpr int LOGIT_KB = 1024 / BK;
 template <int KIND>
-constexpr int ACC_KB = KIND == 0 ? LOSS_KB : 1 << 30;  // k-blocks of an accumulator
+constexpr int ACC_KB = KIND <= 1 ? LOGIT_KB : 1 << 30;  // k-blocks of an accumulator
 
 struct Ring {
     int slot = 0;
@@ -294,13 +297,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
             } else if ((KIND == LOSS || KIND == GRAD) && m < count) {
                 info = a.rows[m];
             }
-            if constexpr (KIND == LOSS) {
+            if constexpr (KIND == LOSS || KIND == GRAD) {
                 constexpr int CH = 16;  // columns read at a time; those behind the half's last one are not looked at
                 float v[TN / 2];
 #pragma unroll
                 for (int c = 0; c < TN / 2; ++c) v[c] = 0.f;
 #pragma unroll 1
-                for (int k = 0; k < x.nkb; k += LOSS_KB) {
+                for (int k = 0; k < x.nkb; k += LOGIT_KB) {
                     ok = wait_acc();
                     if (!ok) break;
                     const uint32_t at = acc_at();
@@ -315,6 +318,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                     release_acc();
                 }
                 if (!ok) break;
+                if constexpr (KIND == GRAD) {
+                    const int left = m < count ? piece - c0 : 0, hit = info.target - v0 - c0;
+                    uint4 *to = (uint4 *)((bf16 *)a.grad + (size_t)m * a.piece + c0);
+#pragma unroll
+                    for (int c = 0; c < TN / 2; c += 8) {
+                        if (c >= tn / 2) break;
+                        uint32_t w[4];
+#pragma unroll
+                        for (int j = c; j < c + 8; j += 2) {
+                            float g[2];
+#pragma unroll
+                            for (int q = 0; q < 2; ++q) {
+                                const float p = fast_exp2((v[j + q] - info.lse) * LOG2E);
+                                g[q] = j + q < left ? (j + q == hit ? p - 1.f : p) * info.g : 0.f;
+                            }
+                            w[(j - c) / 2] = pack2_bf16(g[0], g[1]);
+                        }
+                        to[c / 8] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                    continue;
+                }
                 const int left = min(piece - c0, tn / 2), hit = info.target - c0;
                 float mx = -INFINITY, z = 0.f;
 #pragma unroll
@@ -350,27 +374,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                 if (!ok) break;
                 const uint32_t at = acc_at();
 #pragma unroll 1
-                for (int c = 0; c < tn / 2; c += 32) {
+                for (int c = 0; c < TN / 2; c += 32) {
                     float v[32];
                     __syncwarp();  // (rows that store nothing have skipped ahead)
                     tmem_ld32(at + c, v);
-                    if constexpr (KIND == GRAD) {
-                        const int left = m < count ? piece - (c0 + c) : 0, hit = info.target - v0 - (c0 + c);
-                        uint32_t w[16];
-#pragma unroll
-                        for (int j = 0; j < 32; j += 2) {
-                            float g[2];
-#pragma unroll
-                            for (int q = 0; q < 2; ++q) {
-                                const float p = fast_exp2((v[j + q] - info.lse) * LOG2E);
-                                g[q] = j + q < left ? (j + q == hit ? p - 1.f : p) * info.g : 0.f;
-                            }
-                            w[j / 2] = pack2_bf16(g[0], g[1]);
-                        }
-                        uint4 *to = (uint4 *)((bf16 *)a.grad + (size_t)m * a.piece + c0 + c);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) to[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-                    } else if (rows_out) {
+                    if (rows_out) {
 #pragma unroll
                         for (int j = 0; j < 32; j += 8)
                             *(uint4 *)(stage + lane * OUT_ROW + j * 2) = make_uint4(pack2_bf16(v[j], v[j + 1]), pack2_bf16(v[j + 2], v[j + 3]),
