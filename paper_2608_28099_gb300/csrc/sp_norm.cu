@@ -16,6 +16,10 @@ namespace sp {
 namespace {
 
 constexpr int LOOP_THREADS = 256, MAX_THREADS = 512;
+// Rows of any length: a thread adds RUN terms after one another and its runs with what each addition cuts off, so
+// that a sum's error does not grow with the row (2^24 equal elements, 65536 a thread, added up in one fp32
+// number: norms off by 3e-4).
+constexpr int RUN = 16;
 
 // rstd as a power of two times a float: rows whose squares leave fp32 still have a norm.
 struct Rstd {
@@ -59,6 +63,36 @@ __device__ __forceinline__ void reduce2(T &a, T &b, T (*buf)[32][2], int &half) 
             b = MAX ? max(b, y) : b + y;
         }
     }
+}
+
+// A sum that keeps what its additions cut off (the error-free sum of two numbers, Knuth).
+struct Sum {
+    float s = 0.f, cut = 0.f;
+    __device__ __forceinline__ void add(float x) {
+        const float t = s + x, y = t - s;
+        cut += (s - (t - y)) + (x - y);
+        s = t;
+    }
+    __device__ __forceinline__ float get() const { return isfinite(cut) ? s + cut : s; }  // (beyond fp32: as it is)
+};
+// A thread's part of a row's sums of two terms of each element.
+template <typename F>
+__device__ __forceinline__ float2 thread_sums(int d, const F &term) {
+    int e = threadIdx.x;
+    Sum a, b;
+    for (; e < d - (RUN - 1) * LOOP_THREADS; e += RUN * LOOP_THREADS) {
+        float x = 0.f, y = 0.f;
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) term(e + i * LOOP_THREADS, x, y);
+        a.add(x);
+        b.add(y);
+    }
+    float x = 0.f, y = 0.f;
+    for (; e < d; e += LOOP_THREADS) term(e, x, y);
+    if (d <= (RUN - 1) * LOOP_THREADS) return make_float2(x, y);
+    a.add(x);
+    b.add(y);
+    return make_float2(a.get(), b.get());
 }
 
 // Eight elements as they lie in memory.
@@ -202,11 +236,10 @@ __global__ void __launch_bounds__(LOOP_THREADS) norm_loop_kernel(const __grid_co
     const T *x = (const T *)a.x + row * a.xs, *r = a.r ? (const T *)a.r + row * a.rs : nullptr;
     const auto value = [&](int e) { return to_f(x[e]) + (r ? to_f(r[e]) : 0.f); };
     const auto normed = [&](float v, const Rstd &rs, int e) { return rs.of(v) * (a.gain ? a.gain[e] : 1.f); };
-    float sq = 0.f, none = 0.f;
-    for (int e = threadIdx.x; e < a.d; e += LOOP_THREADS) {
+    float none = 0.f, sq = thread_sums(a.d, [&](int e, float &x, float &) {
         const float v = value(e);
-        sq += v * v;
-    }
+        x += v * v;
+    }).x;
     reduce2<false>(sq, none, buf, half);
     Rstd rs{1.f, rsqrtf(sq / (float)a.d + a.eps)};
     if (out_of_range(sq, a.eps)) {  // (the same for all threads)
@@ -329,66 +362,90 @@ __global__ void __launch_bounds__(WARP ? 128 : MAX_THREADS) norm_back_kernel(con
 }
 
 template <typename T>
+struct LoopRow {
+    const T *s, *dy, *ds;
+    T *dx;
+    __device__ __forceinline__ LoopRow(const NormBackArgs &a, long long row)
+        : s((const T *)a.s + row * a.ss), dy((const T *)a.dy + row * a.ys), ds(a.ds ? (const T *)a.ds + row * a.rs : nullptr),
+          dx((T *)a.dx + row * a.xs) {}
+    // dx of an element, in front of whose store `keep` takes its part of the gain's gradient
+    template <typename F>
+    __device__ __forceinline__ void element(int e, float gain, const Rstd &rs, float m, const F &keep) const {
+        const float xh = rs.of(to_f(s[e])), y = to_f(dy[e]), z = ds ? to_f(ds[e]) : 0.f;
+        keep(y * xh);
+        dx[e] = from_f<T>(z + rs.of(y * gain - xh * m));
+    }
+};
+template <typename T>
 __global__ void __launch_bounds__(LOOP_THREADS) norm_back_loop_kernel(const __grid_constant__ NormBackArgs a) {
     __shared__ float buf[2][32][2];
     __shared__ double dbuf[2][32][2];
     int half = 0, dhalf = 0;
     pdl_wait();
     pdl_trigger();
+    const auto gain = [&](int e) { return a.gain ? a.gain[e] : 1.f; };
     float *part = a.part + (size_t)blockIdx.x * a.d;
     if (a.dgain)
         for (int e = threadIdx.x; e < a.d; e += LOOP_THREADS) part[e] = 0.f;
     for (long long row = blockIdx.x; row < a.n; row += gridDim.x) {
-        const T *s = (const T *)a.s + row * a.ss, *dy = (const T *)a.dy + row * a.ys;
-        float sq = 0.f, dot = 0.f;
-        for (int e = threadIdx.x; e < a.d; e += LOOP_THREADS) {
-            const float v = to_f(s[e]);
-            sq += v * v;
-            dot += to_f(dy[e]) * (a.gain ? a.gain[e] : 1.f) * v;
-        }
+        const LoopRow<T> r(a, row);
+        const float2 mine = thread_sums(a.d, [&](int e, float &x, float &y) {
+            const float v = to_f(r.s[e]);
+            x += v * v;
+            y += to_f(r.dy[e]) * gain(e) * v;
+        });
+        float sq = mine.x, dot = mine.y;
         reduce2<false>(sq, dot, buf, half);
         Rstd rs{1.f, rsqrtf(sq / (float)a.d + a.eps)};
         float m = rs.f2 * dot / (float)a.d;
         if (out_of_range(sq, a.eps) || !isfinite(m)) {  // (the same for all threads)
             double q = 0.0, z = 0.0;
             for (int e = threadIdx.x; e < a.d; e += LOOP_THREADS) {
-                const double v = to_f(s[e]);
+                const double v = to_f(r.s[e]);
                 q += v * v;
-                z += (double)to_f(dy[e]) * (a.gain ? a.gain[e] : 1.f) * v;
+                z += (double)to_f(r.dy[e]) * gain(e) * v;
             }
             reduce2<false>(q, z, dbuf, dhalf);
             rs = rstd_of(q / a.d + a.eps);
             m = (float)(z / a.d * rs.f1 * rs.f2);
         }
-        for (int e = threadIdx.x; e < a.d; e += LOOP_THREADS) {
-            const float xh = rs.of(to_f(s[e])), y = to_f(dy[e]);
-            const float ds = a.ds ? to_f(((const T *)a.ds)[row * a.rs + e]) : 0.f;
-            if (a.dgain) part[e] += y * xh;
-            ((T *)a.dx)[row * a.xs + e] = from_f<T>(ds + rs.of(y * (a.gain ? a.gain[e] : 1.f) - xh * m));
-        }
+        for (int e = threadIdx.x; e < a.d; e += LOOP_THREADS)
+            r.element(e, gain(e), rs, m, [&](float dg) {
+                if (a.dgain) part[e] += dg;
+            });
     }
 }
 
 // dg: the partial rows added in their order, a column a thread of the first warp's
-// lanes, the rows split over 32 warps whose sums are added in order.
-constexpr int SUM_WARPS = 32;
-__global__ void __launch_bounds__(32 * SUM_WARPS) norm_gain_kernel(const float *part, int parts, int d, float *dgain) {
+// lanes, the rows split over 32 warps whose sums are added in pairs.  more: dg holds the sum of rows in front.
+constexpr int SUM_WARPS = 32, FEW_PARTS = 20;
+__global__ void __launch_bounds__(32 * SUM_WARPS) norm_gain_kernel(const float *part, int parts, int d, float *dgain, int more) {
     __shared__ float sums[SUM_WARPS][32];
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = blockIdx.x * 32 + lane;
     const int per = ceil_div(parts, SUM_WARPS), lo = warp * per, hi = min(parts, lo + per);
     float s = 0.f;
-    if (e < d) {
+    if (e < d && per <= FEW_PARTS) {
 #pragma unroll 8
         for (int p = lo; p < hi; ++p) s += part[(size_t)p * d + e];
+    } else if (e < d) {
+        Sum many;
+#pragma unroll 8
+        for (int p = lo; p < hi; ++p) many.add(part[(size_t)p * d + e]);
+        s = many.get();
     }
     sums[warp][lane] = s;
     __syncthreads();
     if (warp == 0 && e < d) {
+        float v[SUM_WARPS];
 #pragma unroll
-        for (int w = 1; w < SUM_WARPS; ++w) s += sums[w][lane];
-        dgain[e] = s;
+        for (int w = 0; w < SUM_WARPS; ++w) v[w] = sums[w][lane];
+#pragma unroll
+        for (int o = SUM_WARPS / 2; o; o >>= 1)
+#pragma unroll
+            for (int w = 0; w < o; ++w) v[w] += v[w + o];
+        dgain[e] = more ? dgain[e] + v[0] : v[0];
     }
 }
 
@@ -414,6 +471,7 @@ int blocks_of(const Shape &s, long long n, int n_sm, int per_sm) {
     return (int)(all < held ? all : held);
 }
 constexpr int FWD_THREADS = 1024, BACK_THREADS = 640;
+constexpr int LEAST_RUN = 208;
 template <typename T, bool WARP, int CH, bool E8>
 cudaError_t run_norm(const NormArgs &a, const Shape &s, int n_sm, cudaStream_t st) {
     return launch_k(norm_kernel<T, WARP, CH, E8>, dim3(blocks_of(s, a.n, n_sm, FWD_THREADS)), dim3(s.threads), 0, st, a);
@@ -469,17 +527,38 @@ cudaError_t launch_norm_backward(const NormBackArgs &a, int n_sm, cudaStream_t s
                      whole16(a.s, a.ss, es) && whole16(a.dy, a.ys, es) && whole16(a.gain, 0, 4);
     const Shape s = shape_of(a.d);
     const bool loop = !vec || !s.threads;
-    int parts = blocks_of(loop ? kLoop : s, a.n, n_sm, BACK_THREADS);
-    cudaError_t e;
-    if (loop) {
-        e = a.dtype == SP_F32 ? run_back_loop<float>(a, parts, st) : run_back_loop<bf16>(a, parts, st);
-    } else {
-        e = a.dtype == SP_F32 ? back_shapes<float>(a, s, n_sm, st) : back_shapes<bf16>(a, s, n_sm, st);
-        parts *= s.rows;
+    const Shape &shape = loop ? kLoop : s;
+    // The gain's gradient of many rows: as many at a time as leave a walker LEAST_RUN rows, or the root of its rows,
+    // to add up in one number, so that no sum is long.  4000001 equal fp32 rows of 64, 1316 a walker: off by up to
+    // 2.0e-5 in one sum, 2.7e-6 so; 2000000 of them 852 us in one launch, 919 in four, 200000 bf16 ones of 2560 815
+    // and 828.  (Walkers that add what they have to their partial rows every 64 rows: 890 and 833, and 1541 instead of
+    // 1473 for 40000 of 12288.)
+    const long long walkers = (long long)blocks_of(shape, a.n, n_sm, BACK_THREADS) * shape.rows, rows = ceil_div_ll(a.n, walkers);
+    long long times = 1;
+    if (a.dgain) {
+        long long run = LEAST_RUN;
+        while (run * run < rows) ++run;
+        times = ceil_div_ll(rows, run);
     }
-    if (e != cudaSuccess || !a.dgain) return e;
-    return launch_k(norm_gain_kernel, dim3(ceil_div(a.d, 32)), dim3(32 * SUM_WARPS), 0, st, (const float *)a.part, parts, a.d,
-                    a.dgain);
+    const long long per = ceil_div_ll(rows, times) * walkers;
+    for (long long r0 = 0; r0 < a.n; r0 += per) {
+        NormBackArgs p = a;
+        const auto from = [&](const void *x, long long stride) { return x ? (const char *)x + r0 * stride * es : nullptr; };
+        p.n = (int)(per < a.n - r0 ? per : a.n - r0);
+        p.dy = from(a.dy, a.ys);
+        p.s = from(a.s, a.ss);
+        p.ds = from(a.ds, a.rs);
+        p.dx = const_cast<char *>(from(a.dx, a.xs));
+        const int parts = blocks_of(shape, p.n, n_sm, BACK_THREADS);
+        cudaError_t e;
+        if (loop) e = a.dtype == SP_F32 ? run_back_loop<float>(p, parts, st) : run_back_loop<bf16>(p, parts, st);
+        else e = a.dtype == SP_F32 ? back_shapes<float>(p, s, n_sm, st) : back_shapes<bf16>(p, s, n_sm, st);
+        if (e == cudaSuccess && a.dgain)
+            e = launch_k(norm_gain_kernel, dim3(ceil_div(a.d, 32)), dim3(32 * SUM_WARPS), 0, st, (const float *)a.part,
+                         parts * shape.rows, a.d, a.dgain, (int)(r0 > 0));
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
 }
 
 }  // namespace sp
