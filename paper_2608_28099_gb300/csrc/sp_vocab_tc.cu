@@ -194,7 +194,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
             const int ma = x.m0 + (int)rank * 128, nb = x.n0 + (int)rank * (tn / 2);
             for (int i = 0; i < x.nkb; ++i, rg.next(), ++filled) {
                 const int s = rg.slot, k = (x.kb0 + i) * BK;
-                if (!mbar_wait(&empty[s], rg.ph ^ 1, abort)) {
+                // (a stage asked for in front is free, and may be read already where the other CTA had all else of
+                // it: its barrier's phase is then one ahead, and the first one would be waited for in vain)
+                if (filled >= pre && !mbar_wait(&empty[s], rg.ph ^ 1, abort)) {
                     ok = false;
                     break;
                 }
