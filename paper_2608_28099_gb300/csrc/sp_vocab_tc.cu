@@ -31,7 +31,11 @@ namespace {
 
 using namespace sm100;
 
-enum { LOSS = 0, GRAD = 1, DH = 2, DW = 3 };
+enum { LOSS = 0, GRAD = 1, DH = 2, DW = 3, DW_LONG = 4 };
+template <int KIND>
+constexpr bool IS_DW = KIND == DW || KIND == DW_LONG;
+template <int KIND>
+constexpr bool IS_LOGITS = KIND == LOSS || KIND == GRAD;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int TM = 256, TN = 256, BK = 64;       // a pair's tile; a CTA holds 128 x 256 of it.  LOSS and GRAD may take
                                                  // tiles of fewer columns (VocabArgs::tn)
@@ -50,9 +54,11 @@ constexpr int TMEM_COLS = 2 * TN;
 // for sum, whatever the tiles' width: exp(l - lse) - 1 of a token that is almost sure of its target is as good as
 // l and the log sum's logits agree (with the whole of K in one accumulator p - 1 of targets with logits of 30 was
 // off by 3.6e-4 at d = 4096 and 9.4e-4 at 8192; so: by the log sum's own rounding, 1e-6).
-constexpr int LOGIT_KB = 1024 / BK;
+// DW_LONG, the head's gradient from more than LONG_DW tokens, adds up that many at a time: in one accumulator that of
+// 4000000 equal tokens was off by 2.6e-2.
+constexpr int LONG_DW = 16384;
 template <int KIND>
-constexpr int ACC_KB = KIND <= 1 ? LOGIT_KB : 1 << 30;  // k-blocks of an accumulator
+constexpr int ACC_KB = IS_LOGITS<KIND> ? 1024 / BK : KIND == DW_LONG ? LONG_DW / BK : 1 << 30;  // k-blocks of an accumulator
 
 struct Ring {
     int slot = 0;
@@ -68,7 +74,7 @@ constexpr long long GRAD_BYTES = 512ll << 20;    // most bytes of a piece's g
 
 template <int KIND>
 struct Kind {
-    static constexpr bool A_MN = KIND == DW, B_MN = KIND == DH || KIND == DW;
+    static constexpr bool A_MN = IS_DW<KIND>, B_MN = KIND == DH || IS_DW<KIND>;
 };
 
 // Tiles of a product over `count` kept tokens and `piece` vocabulary rows.
@@ -82,15 +88,15 @@ __device__ __forceinline__ int count_of(const VocabArgs &a) {
 }
 template <int KIND>
 __device__ __forceinline__ int cols_of(const VocabArgs &a) {
-    return KIND == LOSS || KIND == GRAD ? a.tn : TN;
+    return IS_LOGITS<KIND> ? a.tn : TN;
 }
 template <int KIND>
 __device__ __forceinline__ Tiles tiles_of(const VocabArgs &a, int count, int piece) {
     Tiles t;
     // (without a token one tile is formed whose rows are nobody's; DW's k-block 0 of g and h is cleared)
-    t.m = KIND == DW ? ceil_div(piece, TM) : ceil_div(max(count, 1), TM);
-    t.n = ceil_div(KIND == LOSS || KIND == GRAD ? piece : a.d, cols_of<KIND>(a));
-    t.kb = KIND == DH ? ceil_div(piece, BK) : KIND == DW ? ceil_div(max(count, 1), BK) : ceil_div(a.d, BK);
+    t.m = IS_DW<KIND> ? ceil_div(piece, TM) : ceil_div(max(count, 1), TM);
+    t.n = ceil_div(IS_LOGITS<KIND> ? piece : a.d, cols_of<KIND>(a));
+    t.kb = KIND == DH ? ceil_div(piece, BK) : IS_DW<KIND> ? ceil_div(max(count, 1), BK) : ceil_div(a.d, BK);
     t.splits = 1, t.per = t.kb;
     if (KIND == DH) {
         const DhPlan p = *a.count;
@@ -107,7 +113,7 @@ template <int KIND>
 __device__ __forceinline__ Item item_of(const Tiles &t, int it, int tn) {
     Item x;
     int m, n;
-    if (KIND == DW) {
+    if (IS_DW<KIND>) {
         n = it % t.n, m = it / t.n;
         x.split = 0;
     } else {
@@ -165,13 +171,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     const int piece = min(a.piece, a.V - v0);
     const int tn = cols_of<KIND>(a);              // (a CTA holds half of B's rows)
     // both CTAs' bytes; the logits of up to 128 tokens leave A's other rows as they are (nobody's rows of D)
-    const bool short_a = (KIND == LOSS || KIND == GRAD) && a.box < 128;
+    const bool short_a = IS_LOGITS<KIND> && a.box < 128;
     const uint32_t stage_tx = (short_a ? (uint32_t)a.box * BK * 2 : 2 * HALF) + (uint32_t)tn * BK * 2;
 
     if (warp == TMA && lane == 0) {
         // what is read again soon stays in L2, the vocabulary's rows of LOSS pass through
-        const uint64_t pol_a = KIND == LOSS || KIND == GRAD ? policy_evict_last() : policy_evict_normal();
-        const uint64_t pol_b = KIND == LOSS ? policy_evict_first() : KIND == DW ? policy_evict_last() : policy_evict_normal();
+        const uint64_t pol_a = IS_LOGITS<KIND> ? policy_evict_last() : policy_evict_normal();
+        const uint64_t pol_b = KIND == LOSS ? policy_evict_first() : IS_DW<KIND> ? policy_evict_last() : policy_evict_normal();
         // Up to 256 tokens the first tile of GRAD is known before they are counted, and W does not depend
         // on them: its k-blocks are asked for while the kernel in front still runs (which has
         // waited for the caller's earlier work before it let this one start).
@@ -286,6 +292,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
             if (lane == 0) mbar_arrive_remote(map_rank(&acc_empty[n & 1], 0));
             ++n;
         };
+        // bf16 rows go out through shared memory, 64 bytes of a row by four lanes: where a lane's four rows start (own:
+        // where this one's does, or -1), and 32 columns of every lane's row
+        uint8_t *stage = smem + OFF_OUT + warp * 32 * OUT_ROW;
+        const auto rows_of = [&](long long own, long long (&out_row)[4]) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) out_row[i] = __shfl_sync(0xffffffffu, own, i * 8 + (lane >> 2));
+        };
+        const auto rows_out = [&](const float (&v)[32], bf16 *out, const long long (&out_row)[4], int col) {
+            __syncwarp();  // (the columns before are read)
+#pragma unroll
+            for (int j = 0; j < 32; j += 8)
+                *(uint4 *)(stage + lane * OUT_ROW + j * 2) = make_uint4(pack2_bf16(v[j], v[j + 1]), pack2_bf16(v[j + 2], v[j + 3]),
+                                                                        pack2_bf16(v[j + 4], v[j + 5]), pack2_bf16(v[j + 6], v[j + 7]));
+            __syncwarp();
+            col += (lane & 3) * 8;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (out_row[i] >= 0 && col < a.d)
+                    *(uint4 *)(out + out_row[i] + col) = *(const uint4 *)(stage + (i * 8 + (lane >> 2)) * OUT_ROW + (lane & 3) * 16);
+        };
         bool ok = true;
         for (int it = cl; ok && it < n_items; it += n_cl) {
             const Item x = item_of<KIND>(t, it, tn);
@@ -296,16 +322,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                 const int target = m < count ? a.targets[m] : -1;
                 if (has_target(target, a.V)) info.target = target;
                 else if (target >= a.V && it == 0 && a.status) atomicOr(a.status, SP_DEV_BAD_ROW);
-            } else if ((KIND == LOSS || KIND == GRAD) && m < count) {
+            } else if (IS_LOGITS<KIND> && m < count) {
                 info = a.rows[m];
             }
-            if constexpr (KIND == LOSS || KIND == GRAD) {
+            if constexpr (IS_LOGITS<KIND> || KIND == DW_LONG) {
                 constexpr int CH = 16;  // columns read at a time; those behind the half's last one are not looked at
                 float v[TN / 2];
 #pragma unroll
                 for (int c = 0; c < TN / 2; ++c) v[c] = 0.f;
 #pragma unroll 1
-                for (int k = 0; k < x.nkb; k += LOGIT_KB) {
+                for (int k = 0; k < x.nkb; k += ACC_KB<KIND>) {
                     ok = wait_acc();
                     if (!ok) break;
                     const uint32_t at = acc_at();
@@ -341,6 +367,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                     }
                     continue;
                 }
+                if constexpr (KIND == DW_LONG) {
+                    long long out_row[4];
+                    rows_of(m < piece ? (long long)(v0 + m) * a.ws : -1, out_row);
+#pragma unroll
+                    for (int c = 0; c < TN / 2; c += 32) {
+                        float u[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) u[j] = v[c + j];
+                        rows_out(u, (bf16 *)a.dw, out_row, c0 + c);
+                    }
+                    continue;
+                }
                 const int left = min(piece - c0, tn / 2), hit = info.target - c0;
                 float mx = -INFINITY, z = 0.f;
 #pragma unroll
@@ -359,18 +397,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                 for (int c = 0; c < TN / 2; ++c) s4[c & 3] += fast_exp2((v[c] - mu) * LOG2E);
                 if (m < count) a.part[(size_t)m * a.parts + 2 * x.nt + half] = make_float2(mx, (s4[0] + s4[1]) + (s4[2] + s4[3]));
             } else {
-                // bf16 rows go out through shared memory, 64 bytes of a row by four lanes: dW's, and dh's where it
-                // belongs if it comes in one part
-                const bool rows_out = KIND == DW || (KIND == DH && t.splits == 1 && a.n_pieces == 1);
-                uint8_t *stage = smem + OFF_OUT + warp * 32 * OUT_ROW;
+                // bf16 rows: dW's, and dh's where it belongs if it comes in one part
+                const bool rows = KIND == DW || (KIND == DH && t.splits == 1 && a.n_pieces == 1);
                 bf16 *const out = KIND == DW ? (bf16 *)a.dw : (bf16 *)a.dh;
                 long long out_row[4];
-                if (rows_out) {
+                if (rows) {
                     long long own = -1;
                     if (KIND == DW && m < piece) own = (long long)(v0 + m) * a.ws;
                     if (KIND == DH && m < count) own = (long long)a.rows[m].token * a.hs;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) out_row[i] = __shfl_sync(0xffffffffu, own, i * 8 + (lane >> 2));
+                    rows_of(own, out_row);
                 }
                 ok = wait_acc();
                 if (!ok) break;
@@ -380,17 +415,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                     float v[32];
                     __syncwarp();  // (rows that store nothing have skipped ahead)
                     tmem_ld32(at + c, v);
-                    if (rows_out) {
-#pragma unroll
-                        for (int j = 0; j < 32; j += 8)
-                            *(uint4 *)(stage + lane * OUT_ROW + j * 2) = make_uint4(pack2_bf16(v[j], v[j + 1]), pack2_bf16(v[j + 2], v[j + 3]),
-                                                                                    pack2_bf16(v[j + 4], v[j + 5]), pack2_bf16(v[j + 6], v[j + 7]));
-                        __syncwarp();
-                        const int col = c0 + c + (lane & 3) * 8;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (out_row[i] >= 0 && col < a.d)
-                                *(uint4 *)(out + out_row[i] + col) = *(const uint4 *)(stage + (i * 8 + (lane >> 2)) * OUT_ROW + (lane & 3) * 16);
+                    if (rows) {
+                        rows_out(v, out, out_row, c0 + c);
                     } else {
                         if (m >= count) continue;
                         float *to = a.acc + ((size_t)x.split * (t.m * TM) + m) * a.d + c0 + c;
@@ -428,8 +454,8 @@ cudaError_t run(const VocabArgs &a, const CUtensorMap &ma, const CUtensorMap &mb
     const cudaError_t e = allow_smem(vocab_tc_kernel<KIND>, SMEM<KIND>, known);
     if (e != cudaSuccess) return e;
     const int piece = a.V - v0 < a.piece ? a.V - v0 : a.piece;
-    const long long m = KIND == DW ? ceil_div(piece, TM) : a.pad / TM;
-    const long long n = ceil_div(KIND == LOSS || KIND == GRAD ? piece : a.d, KIND == LOSS || KIND == GRAD ? a.tn : TN);
+    const long long m = IS_DW<KIND> ? ceil_div(piece, TM) : a.pad / TM;
+    const long long n = ceil_div(IS_LOGITS<KIND> ? piece : a.d, IS_LOGITS<KIND> ? a.tn : TN);
     const long long items = m * n * (KIND == DH ? 16 : 1);
     const int pairs = a.pairs;
     return launch_k(vocab_tc_kernel<KIND>, dim3(2 * (items < pairs ? (unsigned)items : (unsigned)pairs)), dim3(THREADS), (size_t)SMEM<KIND>,
@@ -489,7 +515,7 @@ cudaError_t launch_vocab_backward_tc(const VocabArgs &a, cudaStream_t st) {
         const int v0 = i * a.piece;
         cudaError_t e = run<GRAD>(a, mh, mw, v0, st);
         if (e == cudaSuccess) e = run<DH>(a, mg, mwt, v0, st);
-        if (e == cudaSuccess && a.dw) e = run<DW>(a, mgt, mht, v0, st);
+        if (e == cudaSuccess && a.dw) e = a.n > LONG_DW ? run<DW_LONG>(a, mgt, mht, v0, st) : run<DW>(a, mgt, mht, v0, st);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;

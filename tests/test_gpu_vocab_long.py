@@ -67,3 +67,26 @@ def test_long_sums_on_cuda_cores(torch, dtype, n, d, V, head):
             err = float(((dw[row].double() - exact).abs() / lim).max())
             print("dw", row, n, d, V, dtype, err, float(((dw[row].double() - exact) / exact).abs().max()))
             assert err <= 1
+
+
+@pytest.mark.parametrize("n", [40000, 1000003, 4000000])
+@pytest.mark.parametrize("d", [16, 264])
+def test_head_gradient_of_many_tokens_on_tensor_cores(torch, n, d):
+    # two equal rows: every weight is a half, and its gradient a half in bf16, too
+    g = torch.Generator().manual_seed(d)
+    h = (torch.rand((1, d), generator=g) + 0.3).to(torch.bfloat16).cuda().expand(n, d).contiguous()
+    w = torch.full((2, d), 0.25, dtype=torch.bfloat16, device="cuda")
+    t = torch.zeros(n, dtype=torch.int32, device="cuda")
+    t[::3] = -1
+    kept = int((t == 0).sum())
+    dims = dims_of(h, w, d, sp.SP_BF16, 2)
+    _, lse, _ = forward(torch, dims, h, w, t)
+    _, dw, status = backward(torch, dims, h, w, t, lse, None)
+    assert status == 0
+    # an accumulator's sum is cut at its 24 bits 1024 times at most (16384 tokens, 16 a step), each by less than one
+    # part in 2^23 of it; accumulators are added in fp32 (244 at most); then bf16
+    for row, sign in ((0, -0.5), (1, 0.5)):
+        exact = sign * kept * h[0].double()
+        err = ((dw[row].double() - exact) / exact).abs().max()
+        print("dw", n, d, row, float(err))
+        assert float(err) <= 2.0 ** -8 + 1024 * 2.0 ** -23 + 244 * STEP
