@@ -46,7 +46,7 @@ constexpr int OUT_ROW = 64 + 16;                 // 32 bf16 of a row on their wa
 template <int KIND>
 constexpr int SMEM = OFF_OUT + (KIND >= 2 ? 8 * 32 * OUT_ROW : 0) + 1024 /*align*/;
 constexpr int THREADS = 352;                     // warps 0-7 epilogue, 8 TMA, 9 MMA (rank 0), 10 TMEM
-constexpr int EPI_WARPS = 8, TMA = 8, MMA = 9, TMEM = 10;
+constexpr int EPI_WARPS = 8, EPI_THREADS = 32 * EPI_WARPS, TMA = 8, MMA = 9, TMEM = 10;
 constexpr int TMEM_COLS = 2 * TN;
 // LOSS and GRAD add their logits up over 1024 of K at a time: the tensor core cuts what falls below an
 // accumulator's 24 bits, which over longer sums shows in the loss (of its norm, with the whole of K in
@@ -137,7 +137,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     uint64_t *full = (uint64_t *)(smem + OFF_BAR);  // rank 0's: both CTAs' copies
     uint64_t *empty = full + STAGES;
     uint64_t *acc_full = empty + STAGES;            // [2]
-    uint64_t *acc_empty = acc_full + 2;             // [2], rank 0's: one arrival an epilogue warp of both CTAs
+    uint64_t *acc_empty = acc_full + 2;             // [2], rank 0's: one arrival a CTA
     uint64_t *fin = acc_empty + 2;
     uint32_t *tmem_slot = (uint32_t *)(fin + 1);
     volatile int *abort = (volatile int *)(tmem_slot + 1);
@@ -152,7 +152,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&acc_full[i], 1);
-            mbar_init(&acc_empty[i], 2 * EPI_WARPS);
+            mbar_init(&acc_empty[i], 2);
         }
         mbar_init(fin, 1);
         *abort = 0;
@@ -285,12 +285,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
             return have;
         };
         const auto acc_at = [&]() { return tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)((n & 1) * TN + half * (tn / 2)); };
-        const auto release_acc = [&]() {
-            // (a warp for itself: one whose wait ran out would leave the others at a barrier)
+        // All epilogue warps meet here, whatever their waits said, and learn of the others': one that had left
+        // would be waited for without a limit.  (Arrivals of each warp for itself: 40000 tokens of 512 against 2000 rows 147
+        // instead of 140 us.)
+        const auto release_acc = [&](bool have) {
+            int all;
             tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_remote(map_rank(&acc_empty[n & 1], 0));
+            asm volatile(
+                "{\n\t.reg .pred p, q;\n\t"
+                "setp.ne.s32 q, %1, 0;\n\t"
+                "barrier.cta.red.and.pred p, 1, %2, q;\n\t"
+                "selp.s32 %0, 1, 0, p;\n\t}"
+                : "=r"(all)
+                : "r"((int)have), "n"(EPI_THREADS)
+                : "memory");
+            if (all && threadIdx.x == 0) mbar_arrive_remote(map_rank(&acc_empty[n & 1], 0));
             ++n;
+            return all != 0;
         };
         // bf16 rows go out through shared memory, 64 bytes of a row by four lanes: where a lane's four rows start (own:
         // where this one's does, or -1), and 32 columns of every lane's row
@@ -333,7 +344,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
 #pragma unroll 1
                 for (int k = 0; k < x.nkb; k += ACC_KB<KIND>) {
                     ok = wait_acc();
-                    if (!ok) break;
                     const uint32_t at = acc_at();
 #pragma unroll
                     for (int c = 0; c < TN / 2; c += CH) {
@@ -343,27 +353,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
 #pragma unroll
                         for (int j = 0; j < CH; ++j) v[c + j] += u[j];
                     }
-                    release_acc();
+                    ok = release_acc(ok);
+                    if (!ok) break;
                 }
                 if (!ok) break;
                 if constexpr (KIND == GRAD) {
                     const int left = m < count ? piece - c0 : 0, hit = info.target - v0 - c0;
                     uint4 *to = (uint4 *)((bf16 *)a.grad + (size_t)m * a.piece + c0);
 #pragma unroll
-                    for (int c = 0; c < TN / 2; c += 8) {
+                    for (int c = 0; c < TN / 2; c += 32) {  // (64 bytes of a row together)
                         if (c >= tn / 2) break;
-                        uint32_t w[4];
+                        uint32_t w[16];
 #pragma unroll
-                        for (int j = c; j < c + 8; j += 2) {
+                        for (int j = 0; j < 32; j += 2) {
                             float g[2];
 #pragma unroll
                             for (int q = 0; q < 2; ++q) {
-                                const float p = fast_exp2((v[j + q] - info.lse) * LOG2E);
-                                g[q] = j + q < left ? (j + q == hit ? p - 1.f : p) * info.g : 0.f;
+                                const float p = fast_exp2((v[c + j + q] - info.lse) * LOG2E);
+                                g[q] = c + j + q < left ? (c + j + q == hit ? p - 1.f : p) * info.g : 0.f;
                             }
-                            w[(j - c) / 2] = pack2_bf16(g[0], g[1]);
+                            w[j / 2] = pack2_bf16(g[0], g[1]);
                         }
-                        to[c / 8] = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) to[c / 8 + j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
                     }
                     continue;
                 }
@@ -408,7 +420,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                     rows_of(own, out_row);
                 }
                 ok = wait_acc();
-                if (!ok) break;
                 const uint32_t at = acc_at();
 #pragma unroll 1
                 for (int c = 0; c < TN / 2; c += 32) {
@@ -432,7 +443,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                         }
                     }
                 }
-                release_acc();
+                ok = release_acc(ok);
             }
         }
     }

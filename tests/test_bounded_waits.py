@@ -18,19 +18,19 @@ def _roles(name, first):
 BARRIERS = r"bar\.sync|barrier\.cta|barrier\.sync|named_sync|__syncthreads|cluster_sync"
 
 
-def test_vocabulary_kernel_waits_have_a_limit():
+def test_vocabulary_epilogue_has_one_verdict():
+    # the only barrier between the roles takes the eight warps' verdicts and gives them one, so that all go on
+    # or none does, and no warp leaves between its wait and that barrier
     roles = _roles("vocab_tc_kernel", "const uint64_t pol_a")
-    assert "wait_acc" in roles and "release_acc" in roles
-    assert not re.search(BARRIERS, roles)
-
-
-def test_vocabulary_accumulators_are_released_by_every_warp_that_reads_them():
-    # each of the eight warps of both CTAs arrives for itself: the count that the barriers are made with
-    body = KERNELS["vocab_tc_kernel"]
-    assert re.search(r"mbar_init\(&acc_empty\[i\], 2 \* EPI_WARPS\)", body)
-    release = body[body.index("release_acc = "):]
-    release = release[:release.index("};")]
-    assert re.search(r"tc_fence_before\(\);\s*__syncwarp\(\);\s*if \(lane == 0\) mbar_arrive_remote\(", release)
+    assert re.findall(BARRIERS, roles) == ["barrier.cta"] and "barrier.cta.red.and" in roles
+    epilogue = roles[roles.index("const auto release_acc"):]
+    walks = epilogue[epilogue.index("for (int it = cl"):]
+    parts = re.split(r"(ok = wait_acc\(\);|ok = release_acc\(ok\);)", walks)
+    assert parts[1::2] == ["ok = wait_acc();", "ok = release_acc(ok);"] * 2
+    for between in parts[2::4]:
+        assert not re.search(r"\breturn\b|if \(!ok\)|\bok =", between)
+    # what a warp leaves by is the common verdict
+    assert re.match(r"\s*if \(!ok\) break;", parts[4]) and re.match(r"\s*\}", parts[8])
 
 
 @pytest.mark.parametrize("role", ["stage_rows<NODES>", "node_products("])
