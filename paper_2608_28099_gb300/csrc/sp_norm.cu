@@ -8,7 +8,8 @@
 // rows and have the next one's loads under way meanwhile (without: 143 instead of 99 us, 94 instead
 // of 49).  16384 rows of 5120, bf16 with a residual into 8 bits: 99 us, 5.9 TB/s; backward of 8191 rows of
 // 4096 with the gain's gradient 49 us, 5.5 TB/s, 5 of them its second kernel; of 1500 fp32 rows of 2560
-// without it 12.9 us, 4.8 TB/s, two and a half rows a block.  16 rows of 4096: 4.3 us, one launch.
+// without it 12.9 us, 4.8 TB/s: its registers let three blocks of 160 threads onto an SM where the grid has four, so that
+// 456 of the 608 blocks run first and the others behind them.  16 rows of 4096: 4.3 us, one launch.
 #include "sp_train.cuh"
 
 namespace sp {

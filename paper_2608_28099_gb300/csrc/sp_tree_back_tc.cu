@@ -17,7 +17,7 @@
 // (SP_DEV_TIMEOUT).
 //
 // What bounds it: HBM for long sequences.  Eight of 32768 tokens, 40 heads, 16 nodes (80 rows a kv head):
-// 176 to 184 us, 5.9 TB/s; 64 of 1024 to 8192, 32 heads, 16 nodes: 210 to 226 us, 5.5 to 5.8 TB/s.  A tile's chain is
+// 176 to 187 us, 5.8 to 6.1 TB/s; 64 of 1024 to 8192, 32 heads, 16 nodes: 210 to 233 us, 5.4 to 6.0 TB/s.  A tile's chain is
 // dP (8 MMAs) -> ds -> dQ (8 MMAs), the next tile's S beside ds; an MMA with A in TMEM takes as long for 64
 // tokens as for 128, which is why tiles have 128 tokens (64: 217 instead of 201 us for the eight, with two tiles
 // under way), and Q and dO lie in TMEM (in shared memory 262 instead of 227, at 64 tokens).

@@ -1,10 +1,10 @@
 // The vocabulary loss's products on tcgen05 tensor cores, bf16 with fp32 sums:
-//   LOSS  logits of the kept tokens, whose epilogue leaves each row's (max, sum) over 128 columns
+//   LOSS  logits of the kept tokens, whose epilogue leaves each row's (max, sum) over half a tile's columns
 //   GRAD  the same logits, whose epilogue leaves g = dloss (p - 1_t) in bf16 for a piece of the vocabulary
 //   DH    dh (+)= g W over the piece, fp32 planes
-//   DW    dW = g^T h of the piece, bf16
-// Work: tiles of 256 x 256 by pairs of CTAs (tcgen05.mma.cta_group::2, M = 256: each CTA holds 128
-// rows of A and half of B's 256), K in blocks of 64 through a ring of TMA tiles, two accumulators in
+//   DW    dW = g^T h of the piece, bf16 (DW_LONG: from many tokens)
+// Work: tiles of 256 x 256 (DH, DW) or 256 x tn (LOSS, GRAD: 64 to 256 rows of the vocabulary, VocabArgs::tn) by
+// pairs of CTAs (tcgen05.mma.cta_group::2, M = 256: each CTA holds 128 rows of A and half of B's), K in blocks of 64 through a ring of TMA tiles, two accumulators in
 // TMEM so that the epilogue of one tile runs beside the products of the next; persistent, a pair
 // takes tiles in turn.  The operands lie as their tensors do: K contiguous (K-major) for the logits
 // and for g in DH, the other index contiguous (MN-major) for W in DH and for both in DW; no
@@ -13,12 +13,12 @@
 //
 // What bounds it: the tensor pipe, and under it the board's power.  4096 tokens of 4096 (2744 kept)
 // against 65536 rows: LOSS issues its MMAs back to back (1.22 M cycles, 1.21 M of them MMAs) and takes 720 us
-// alone, 860 in a stream of calls, whose clocks settle near 1.65 GHz (1.71 PFLOP/s; a library product of
-// such a stream 1.73).  GRAD takes 775 us alone, DH 800 in three splits (950 in one: 176 tiles for 76 pairs),
+// alone, 860 to 896 in a stream of calls on four boards, whose clocks settle near 1.65 GHz (1.64 to 1.71 PFLOP/s; a
+// library product of such a stream 1.73).  GRAD takes 775 us alone, DH 780 to 800 in three splits (950 in one: 176 tiles for 76 pairs),
 // DW of 2051 tokens of 2560 and 50021 rows 284.  The MMAs are issued by a whole warp in uniform registers, ring
 // slots counted, not divided: by one thread that divided, LOSS took 870 us alone.  256 x 256 tiles by pairs load
 // 64 bytes a cycle and SM from L2; seven stages instead of six change nothing.  Few tokens are bound by W:
-// 48 tokens of 2560 against 32000 rows 33.4 us, 4.9 TB/s, of which 3 are the joining kernel and its launch.
+// 48 tokens of 2560 against 32000 rows 33.4 to 34.4 us, 4.8 TB/s, of which 3 are the joining kernel and its launch.
 #include <string.h>
 
 #include "sp_gemm.cuh"
