@@ -13,7 +13,7 @@
 //
 // What bounds it: the tensor pipe, and under it the board's power.  4096 tokens of 4096 (2744 kept)
 // against 65536 rows: LOSS issues its MMAs back to back (1.22 M cycles, 1.21 M of them MMAs) and takes 720 us
-// alone, 860 to 896 in a stream of calls on four boards, whose clocks settle near 1.65 GHz (1.64 to 1.71 PFLOP/s; a
+// alone, 860 to 896 in a stream of calls on several boards, whose clocks settle near 1.65 GHz (1.64 to 1.71 PFLOP/s; a
 // library product of such a stream 1.73).  GRAD takes 775 us alone, DH 780 to 800 in three splits (950 in one: 176 tiles for 76 pairs),
 // DW of 2051 tokens of 2560 and 50021 rows 284.  The MMAs are issued by a whole warp in uniform registers, ring
 // slots counted, not divided: by one thread that divided, LOSS took 870 us alone.  256 x 256 tiles by pairs load
